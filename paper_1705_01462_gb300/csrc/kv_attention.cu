@@ -1,0 +1,148 @@
+// Attention over the 4-bit cache: the C entry, the choice of kernel and of the split, and the kernel
+// that joins the chunks of a split.
+#include "kv_attention.cuh"
+
+namespace fgq {
+namespace {
+
+using namespace dec;
+
+constexpr int JOIN_THREADS = 256;
+constexpr uint64_t AT_TIMEOUT_NS = 1000000000ull;  // 1 s per wait
+
+// out[row] = sum_c 2^(m_c - m) part_c / sum_c 2^(m_c - m) l_c over the chunks that had work; one block per row,
+// JOIN_THREADS / D chunks at a time.
+template <int D>
+__global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constant__ AttnArgs a, int tile_rows) {
+  constexpr int WAYS = JOIN_THREADS / D;
+  __shared__ float sv[WAYS][D], sl[WAYS], red[JOIN_THREADS / 32];
+  const int64_t orow = blockIdx.x;  // (b, query, head)
+  const int hq = (int)(orow % a.q_heads);
+  const int64_t bt = orow / a.q_heads;
+  const int qi = (int)(bt % a.T), b = (int)(bt / a.T);
+  const int tid = threadIdx.x, d = tid % D, way = tid / D;
+  pdl_wait();
+  const int n = __ldg(a.seq_lens + b);
+  const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
+  const int r0 = (qi * a.group + hq % a.group) / tile_rows * tile_rows;  // the block's tile of query rows
+  int first, end;
+  visible(a, n, nq, r0 / a.group, (min(r0 + tile_rows, a.rows) - 1) / a.group, first, end);
+  first &= ~15;
+  const int chunks = (int)min((int64_t)a.chunks, ((int64_t)end - first + a.chunk - 1) / a.chunk);
+  const float* st = a.stats + orow * a.chunks * 2;
+  const float* part = a.part + orow * a.chunks * D;
+  float m = AT_M0;
+  for (int c = tid; c < chunks; c += JOIN_THREADS) m = fmaxf(m, st[2 * c]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL_MASK, m, o));
+  if ((tid & 31) == 0) red[tid >> 5] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < JOIN_THREADS / 32; ++i) m = fmaxf(m, red[i]);
+  float v = 0.0f, l = 0.0f;
+#pragma unroll 8
+  for (int c = way; c < chunks; c += WAYS) {
+    const float f = ex2(st[2 * c] - m);
+    l = fmaf(f, st[2 * c + 1], l);
+    v = fmaf(f, part[(int64_t)c * D + d], v);
+  }
+  sv[way][d] = v;
+  if (d == 0) sl[way] = l;
+  __syncthreads();
+  if (way == 0) {
+#pragma unroll
+    for (int i = 1; i < WAYS; ++i) {
+      v += sv[i][d];
+      l += sl[i];
+    }
+    store_out(a, orow * D + d, l > 0.0f ? v / l : (l == 0.0f ? 0.0f : l));
+  }
+}
+
+}  // namespace
+
+fgq_status launch_few_rows(const fgq_kv_cache* cache, AttnArgs a, int max_len, cudaStream_t s) {
+  const int D = cache->head_dim, nb = D / 32, gb = cache->group / 32;
+  const bool split = a.type == FGQ_F32;
+  const AttnKernel k = nb == 2   ? attention_kernel_2(gb, split, a.rows)
+                       : nb == 4 ? attention_kernel_4(gb, split, a.rows)
+                                 : attention_kernel_8(gb, split, a.rows);
+  a.row_tiles = (a.rows + k.rows - 1) / k.rows;
+  const int64_t units = (int64_t)a.B * a.c.kv_heads * a.row_tiles;
+  int64_t span = max_len;  // tokens that one block may have to read
+  if (a.window && (int64_t)a.window + k.rows / a.group + 1 < span) span = (int64_t)a.window + k.rows / a.group + 1;
+  span += 15;
+  // chunks for about two waves of blocks, of 128 tokens (a tile for each warp) at least
+  const int64_t want = (2ll * device_sms() * k.per_sm + units - 1) / units;
+  int64_t chunk = (span + want - 1) / want;
+  chunk = (chunk + 127) / 128 * 128;
+  a.chunk = (int)chunk;
+  a.chunks = (int)((span + chunk - 1) / chunk);
+  if (units * a.chunks > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
+  void* tmp = nullptr;
+  const int64_t orows = (int64_t)a.B * a.T * a.q_heads;
+  if (a.chunks > 1) {
+    tmp = scratch_alloc((size_t)orows * a.chunks * (D + 2) * 4, s);
+    if (!tmp) return FGQ_ERR_CUDA;
+    a.part = static_cast<float*>(tmp);
+    a.stats = a.part + (size_t)orows * a.chunks * D;
+  }
+  fgq_status st = k.launch(a, (unsigned)(units * a.chunks), s);
+  if (st == FGQ_OK && a.chunks > 1) {
+    const dim3 grid((unsigned)orows), block(JOIN_THREADS);
+    st = after_launch(D == 64    ? launch_pdl(join_kernel<64>, grid, block, 0, s, a, k.rows)
+                      : D == 128 ? launch_pdl(join_kernel<128>, grid, block, 0, s, a, k.rows)
+                                 : launch_pdl(join_kernel<256>, grid, block, 0, s, a, k.rows));
+  }
+  if (tmp && cudaFreeAsync(tmp, s) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
+  return st;
+}
+
+}  // namespace fgq
+
+using namespace fgq;
+
+extern "C" fgq_status fgq_kv_attention(const fgq_kv_cache* cache, const void* q, fgq_float_type type, int B, int T,
+                                       int q_heads, int64_t q_batch_stride, int64_t q_token_stride,
+                                       const int32_t* page_table, int max_pages, const int32_t* seq_lens,
+                                       const int32_t* q_lens, int max_len, int causal, int window, float scale,
+                                       void* out, cudaStream_t stream) {
+  if (B < 0 || T < 0 || q_heads <= 0 || max_pages < 0 || max_len < 0 || window < 0 || !dec::valid_float(type))
+    return FGQ_ERR_ARG;
+  if ((causal != 0 && causal != 1) || (window && !causal) || !(scale > 0.0f) || dec::nonfinite_host(scale))
+    return FGQ_ERR_ARG;
+  const fgq_status st = dec::check_cache(cache);
+  if (st != FGQ_OK) return st;
+  if (q_heads % cache->kv_heads != 0) return FGQ_ERR_ARG;
+  if (B == 0 || T == 0) return FGQ_OK;
+  if (!q || !out || !page_table || !seq_lens) return FGQ_ERR_ARG;
+  if (!dec::aligned(q, 16) || !dec::aligned(out, 16) || !dec::aligned(page_table, 4) || !dec::aligned(seq_lens, 4) ||
+      !dec::aligned(q_lens, 4) || !dec::stride16(q_batch_stride, type) || !dec::stride16(q_token_stride, type))
+    return FGQ_ERR_ALIGN;
+  const int group = q_heads / cache->kv_heads;
+  const int64_t capacity = (int64_t)max_pages * cache->page_size;
+  if ((int64_t)T * group > INT32_MAX / 2 || (int64_t)B * T * q_heads > INT32_MAX || capacity > INT32_MAX)
+    return FGQ_ERR_UNSUPPORTED;
+  dec::AttnArgs a = {};
+  a.c = dec::view(cache, page_table, max_pages);
+  a.q = q;
+  a.out = out;
+  a.qbs = q_batch_stride;
+  a.qts = q_token_stride;
+  a.seq_lens = seq_lens;
+  a.q_lens = q_lens;
+  a.err = device_error_word();
+  const int64_t lim_us = debug_wait_limit_us();
+  a.timeout_ns = lim_us < 0 ? AT_TIMEOUT_NS : (uint64_t)lim_us * 1000u;
+  a.scale_log2 = scale * 1.44269504f;
+  a.type = type;
+  a.B = B;
+  a.T = T;
+  a.q_heads = q_heads;
+  a.group = group;
+  a.rows = T * group;
+  a.causal = causal;
+  a.window = window;
+  const int bound = max_len > 0 && max_len < capacity ? max_len : (int)(capacity > 0 ? capacity : 1);
+  return launch_few_rows(cache, a, bound, stream);
+}

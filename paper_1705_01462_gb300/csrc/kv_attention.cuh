@@ -1,0 +1,630 @@
+// Attention over the 4-bit cache, few query rows: the cache is read once, in chunks of tokens that
+// blocks take side by side, and dequantized on the way into the matrix instructions.
+//
+// Mathematics.  With k = lo + s c, the score of token t and query row n is
+//   scale * sum_g ( s_tg (q_ng . c_tg) + lo_tg sum(q_ng) )         (g: groups of the head's values)
+// and with v likewise, the output's value d in group g is
+//   sum_t (p_nt s_tg) c_td + sum_t p_nt lo_tg,
+// so both products run on the codes themselves and the parameters are applied to scores and to
+// probabilities.  A code in the low bits of an fp16 is the subnormal c 2^-24 (or 16 c 2^-24, four bits
+// up): one AND per two codes makes a matrix operand, exactly.  Tokens (keys) and values' dimensions (V)
+// are the M = 16 rows of mma.m16n8k16, eight query rows its columns, so that a group of eight query
+// heads pads nothing.  These legacy matrix instructions do here: 16 of them per 2 KB of cache leave the
+// tensor pipe a third busy at full HBM rate, and tcgen05 would want the dequantized operands in shared
+// or tensor memory first.
+//
+// What is rounded: queries to fp16 after scaling each row by a power of two (exact for bf16 and fp16;
+// fp32 queries take two fp16 parts, SPLIT), and p s to fp16 (two parts for SPLIT), scaled by a power of
+// two that follows the largest value scale met.  Scores, statistics and sums are fp32.
+//
+// Softmax.  The reference m of a row moves only when a score exceeds it by more than 8 (in log2 units):
+// probabilities stay below 2^8, and the common tile needs one vote instead of a reduction per row.
+//
+// Split.  A block of 4 warps takes `chunk` tokens of one (sequence, kv head, tile of 8 NT query rows);
+// each warp streams every fourth tile of 32 tokens through a ring of bulk copies of its own (no barrier
+// between warps), and the warps' sums are joined in shared memory.  Several chunks leave (m, l, sum) in
+// fp32, which a second kernel joins.
+#pragma once
+
+#include "decoder_internal.cuh"
+#include "ptx_sm100.cuh"
+
+namespace fgq {
+namespace dec {
+
+struct AttnArgs {
+  CacheView c;
+  const void* q;
+  void* out;
+  int64_t qbs, qts;  // q's batch and token strides, elements
+  const int32_t* seq_lens;
+  const int32_t* q_lens;
+  float* part;   // [row][chunks] partial sums of D values each, or nullptr (one chunk)
+  float* stats;  // [row][chunks][2]: m, l
+  unsigned int* err;
+  uint64_t timeout_ns;
+  float scale_log2;  // scale * log2(e)
+  int type, B, T, q_heads, group, rows, row_tiles, chunks, chunk, causal, window;
+};
+
+constexpr int AT_WARPS = 4;
+constexpr int AT_TILE = 32;  // tokens a warp takes at a time
+constexpr float AT_M0 = -1e30f;
+
+template <int NB>
+struct AttnRing {
+  static constexpr int STAGES = NB == 8 ? 2 : (NB == 4 ? 3 : 4);
+};
+
+// Shared memory of one ring stage: 32 rows of key codes, value codes, key and value parameters.
+template <int NB, int GB>
+struct AttnSmem {
+  static constexpr int D = 32 * NB, NG = NB / GB, STAGES = AttnRing<NB>::STAGES;
+  static constexpr int ROW = D / 2, PAR = 4 * NG;
+  static constexpr int STAGE = AT_TILE * 2 * (ROW + PAR);
+  static constexpr int RING = AT_WARPS * STAGES * STAGE;
+  static constexpr int BARS = AT_WARPS * STAGES * 8;
+  template <int NT>
+  static constexpr int bytes() {
+    // the warps' sums reuse the ring
+    const int join = AT_WARPS * 8 * NT * (D + 2) * 4;
+    return (RING > join ? RING : join) + BARS + 16;
+  }
+};
+
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t h2(float a, float b) { return pack2(a, b, __half()); }
+__device__ __forceinline__ float2 f2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+
+// The words of one thread's piece of a cache row in shared memory (4 N bytes, aligned as that).
+template <int N>
+__device__ __forceinline__ void lds_words(const uint8_t* p, uint32_t (&w)[N]) {
+  if constexpr (N == 1) {
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
+  } else if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    w[0] = v.x, w[1] = v.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p + 4 * i);
+      w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+    }
+  }
+}
+
+// Query row r = i * group + h of (b, kv head): its q elements 8 e .. 8 e + 7 as fp32.
+template <int NB>
+__device__ __forceinline__ void load_q8(const AttnArgs& a, int64_t base, int e, float (&x)[8]) {
+  if (a.type == FGQ_F32)
+    load8(static_cast<const float*>(a.q) + base + 8 * e, x);
+  else if (a.type == FGQ_BF16)
+    load8(static_cast<const __nv_bfloat16*>(a.q) + base + 8 * e, x);
+  else
+    load8(static_cast<const __half*>(a.q) + base + 8 * e, x);
+}
+
+__device__ __forceinline__ void store_out(const AttnArgs& a, int64_t at, float v) {
+  if (a.type == FGQ_F32)
+    static_cast<float*>(a.out)[at] = v;
+  else if (a.type == FGQ_BF16)
+    static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
+  else
+    static_cast<__half*>(a.out)[at] = __float2half_rn(v);
+}
+
+// First and one past the last position that any of the query rows [i0, i1] (by query index) of a
+// sequence of n tokens and nq queries sees.
+__device__ __forceinline__ void visible(const AttnArgs& a, int n, int nq, int i0, int i1, int& first, int& end) {
+  i1 = min(i1, nq - 1);
+  if (i1 < i0 || n <= 0) {
+    first = end = 0;
+    return;
+  }
+  if (!a.causal) {
+    first = 0;
+    end = n;
+    return;
+  }
+  end = max(n - nq + i1 + 1, 0);
+  first = a.window ? max(n - nq + i0 + 1 - a.window, 0) : 0;
+  if (end <= first) first = end = 0;
+}
+
+// Blocks of one SM, by registers and shared memory.
+template <int NB, bool SPLIT, int NT>
+constexpr int attention_blocks_per_sm() {
+  return NB == 8 ? 2 : (NT == 2 || SPLIT ? 3 : 4);
+}
+
+template <int NB, int GB, bool SPLIT, int NT>
+__global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPLIT, NT>())
+    kv_attention_kernel(const __grid_constant__ AttnArgs a) {
+  using S = AttnSmem<NB, GB>;
+  constexpr int D = S::D, NG = S::NG, ROW = S::ROW, PAR = S::PAR, STAGES = S::STAGES;
+  constexpr int NQ = SPLIT ? 2 : 1;  // fp16 parts of a query and of a probability
+  constexpr int NR = 8 * NT;         // query rows of the block
+  extern __shared__ __align__(128) uint8_t smem[];
+  constexpr int BODY = S::template bytes<NT>() - S::BARS - 16;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + BODY);
+  volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + BODY + S::BARS);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int g = lane >> 2, t = lane & 3;
+
+  // block -> (sequence, kv head, tile of query rows, chunk); row tiles of one chunk are neighbours
+  int id = blockIdx.x;
+  const int rt = id % a.row_tiles;
+  id /= a.row_tiles;
+  const int ch = id % a.chunks;
+  id /= a.chunks;
+  const int head = id % a.c.kv_heads;
+  const int b = id / a.c.kv_heads;
+  const int r0 = rt * NR;
+
+  const int n = __ldg(a.seq_lens + b);
+  const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
+  int first, end;
+  visible(a, n, nq, r0 / a.group, (min(r0 + NR, a.rows) - 1) / a.group, first, end);
+  first &= ~15;
+  // this block's tokens [lo, hi): chunks start a multiple of 32 after `first`; the last one takes the rest
+  const int64_t lo64 = (int64_t)first + (int64_t)ch * a.chunk;
+  const int lo = lo64 < end ? (int)lo64 : end;
+  const int hi = ch == a.chunks - 1 ? end : (int)min((int64_t)end, lo64 + a.chunk);
+
+  if (lo >= hi) {  // nothing here: zero output where there is one chunk only, else the join skips it
+    if (a.chunks == 1) {
+      for (int i = threadIdx.x; i < NR * D; i += 32 * AT_WARPS) {
+        const int r = r0 + i / D;
+        if (r < a.rows) {
+          const int qi = r / a.group, h = r - qi * a.group;
+          store_out(a, (((int64_t)b * a.T + qi) * a.q_heads + (int64_t)head * a.group + h) * D + i % D, 0.0f);
+        }
+      }
+    }
+    return;
+  }
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < AT_WARPS * STAGES; ++i) mbar_init(&bars[i], 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  __syncthreads();
+
+  uint8_t* ring = smem + warp * STAGES * S::STAGE;
+  uint64_t* bar = bars + warp * STAGES;
+  const int tiles_all = (hi - lo + AT_TILE - 1) / AT_TILE;
+  const int tiles = (tiles_all - warp + AT_WARPS - 1) / AT_WARPS;  // this warp's
+
+  // lanes 0-7 copy: half (16 tokens) lane / 4, array lane % 4 (key codes, value codes, key, value parameters)
+  const int half = (lane >> 2) & 1, arr = lane & 3;
+  auto page_at = [&](int i) -> int {  // page of this lane's half of the warp's tile i, or -1
+    const int tok = lo + (i * AT_WARPS + warp) * AT_TILE + 16 * half;
+    if (i >= tiles || tok >= hi || lane >= 8) return -1;
+    const uint32_t pi = page_of(a.c, (uint32_t)tok);
+    if (pi >= (uint32_t)a.c.max_pages) return -2;
+    const int page = __ldg(a.c.table + (int64_t)b * a.c.max_pages + pi);
+    return page >= 0 && page < a.c.pages ? page : -2;
+  };
+  auto issue = [&](int i, int page) {
+    if (i >= tiles) return;
+    const int tok = lo + (i * AT_WARPS + warp) * AT_TILE + 16 * half;
+    if (page == -2) record_error(a.err, FGQ_ERR_ARG);
+    const uint32_t ok = __ballot_sync(FULL_MASK, page >= 0) & 0x11u;  // a lane of each half
+    uint64_t* bi = &bar[i % STAGES];
+    if (lane == 0) mbar_arrive_expect_tx(bi, (uint32_t)__popc(ok) * 16u * 2u * (ROW + PAR));
+    __syncwarp();
+    if (page >= 0) {
+      const int slot = tok - (int)page_of(a.c, (uint32_t)tok) * a.c.page_size;
+      const int64_t row = ((int64_t)page * a.c.kv_heads + head) * a.c.page_size + slot;
+      uint8_t* st = ring + (i % STAGES) * S::STAGE;
+      const bool par = arr >= 2, val = arr & 1;
+      const uint32_t bytes = 16u * (par ? PAR : ROW);
+      const uint8_t* src = par ? reinterpret_cast<const uint8_t*>(val ? a.c.v_params : a.c.k_params) + row * PAR
+                               : (val ? a.c.v_codes : a.c.k_codes) + row * ROW;
+      uint8_t* dst = st + (par ? 2 * AT_TILE * ROW + (val ? AT_TILE * PAR : 0) : (val ? AT_TILE * ROW : 0)) +
+                     half * (int)bytes;
+      bulk_load(smem_u32(dst), src, bytes, bi);
+    }
+  };
+  int armed = 0, page = page_at(0);
+#pragma unroll 1
+  for (int i = 0; i < STAGES; ++i) {
+    const int next = page_at(i + 1);
+    issue(i, page);
+    page = next;
+    armed = min(i + 1, tiles);
+  }
+
+  // queries as operand columns: this thread's part of row 8 nt + g, and what rows 8 nt + 2 t, + 1 need
+  uint32_t qf[NT][NQ][2 * NB][2];
+  float qsum[NT][NG][2], mul[NT][2];
+  int see_lo[NT][2], see_hi[NT][2];  // tokens [see_lo, see_hi) that rows 8 nt + 2 t, + 1 see
+  int all_lo = 0, all_hi = INT32_MAX;  // tokens that every row sees
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = r0 + 8 * nt + g;
+    const bool live = r < a.rows;
+    const int qi = live ? r / a.group : 0, h = live ? r - qi * a.group : 0;
+    const int64_t base = (int64_t)b * a.qbs + (int64_t)qi * a.qts + ((int64_t)head * a.group + h) * D;
+    float x[NB][8];
+    float mx = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      if (live)
+        load_q8<NB>(a, base, 4 * j + t, x[j]);
+      else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[j][i]));
+    }
+    mx = fmaxf(mx, __shfl_xor_sync(FULL_MASK, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(FULL_MASK, mx, 2));
+    // the row's largest query to [2^13, 2^14)
+    const int e = mx > 0.0f ? max(-100, min(126, 13 - (int)((__float_as_uint(mx) >> 23) & 255) + 127)) : 0;
+    const float up = pow2f(e);
+    float sums[NG];
+#pragma unroll
+    for (int i = 0; i < NG; ++i) sums[i] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {  // pairs (0, 1), (2, 3), ..; odd ones meet codes times 16
+        const float dn = (w & 1) ? 0.0625f : 1.0f;
+        const float p0 = x[j][2 * w] * up * dn, p1 = x[j][2 * w + 1] * up * dn;
+        const uint32_t hw = h2(p0, p1);
+        const float2 back = f2(hw);
+        float s0 = back.x, s1 = back.y;
+        qf[nt][0][2 * j + (w >> 1)][w & 1] = hw;
+        if constexpr (SPLIT) {
+          const uint32_t lw = h2(p0 - back.x, p1 - back.y);
+          qf[nt][NQ - 1][2 * j + (w >> 1)][w & 1] = lw;
+          const float2 rest = f2(lw);
+          s0 += rest.x, s1 += rest.y;
+        }
+        sums[j / GB] += (s0 + s1) * ((w & 1) ? 16.0f : 1.0f);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      sums[i] += __shfl_xor_sync(FULL_MASK, sums[i], 1);
+      sums[i] += __shfl_xor_sync(FULL_MASK, sums[i], 2);
+      sums[i] *= 5.9604645e-8f;  // 2^-24: the accumulated codes' scale
+    }
+    const float m = pow2f(-e) * a.scale_log2 * 16777216.0f;
+    // positions of the row: [sl, sh)
+    int sl = 0, sh = live ? 0 : INT32_MAX;  // rows past the last: zero queries, masked nowhere
+    if (live && qi < nq) {
+      sh = n, sl = 0;
+      if (a.causal) {
+        sh = n - nq + qi + 1;
+        if (a.window) sl = sh - a.window;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int from = 4 * (2 * t + u);
+#pragma unroll
+      for (int i = 0; i < NG; ++i) qsum[nt][i][u] = __shfl_sync(FULL_MASK, sums[i], from);
+      mul[nt][u] = __shfl_sync(FULL_MASK, m, from);
+      see_lo[nt][u] = __shfl_sync(FULL_MASK, sl, from);
+      see_hi[nt][u] = min(__shfl_sync(FULL_MASK, sh, from), end);
+      all_lo = max(all_lo, see_lo[nt][u]);
+      all_hi = min(all_hi, see_hi[nt][u]);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    all_lo = max(all_lo, __shfl_xor_sync(FULL_MASK, all_lo, o));
+    all_hi = min(all_hi, __shfl_xor_sync(FULL_MASK, all_hi, o));
+  }
+
+  float o[NT][NB][2][4], olo[NT][NG][2], l[NT][2], m[NT][2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      m[nt][u] = AT_M0;
+      l[nt][u] = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) olo[nt][i][u] = 0.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[nt][j][u][i] = 0.0f;
+  }
+  float sigma = 7.888609e-31f;  // 2^-100; a power of two at or above every value scale met so far
+
+  bool ok = true;
+  int done = 0;
+#pragma unroll 1
+  for (int it = 0; it < tiles; ++it) {
+    const int st = it % STAGES;
+    // a limit of 0 (a test's) expires at once, whether the copy has landed or not
+    if (a.timeout_ns == 0 || !mbar_wait_warp(&bar[st], (uint32_t)(it / STAGES) & 1u, a.timeout_ns, abort_flag)) {
+      ok = false;
+      break;
+    }
+    done = it + 1;
+    const int tok0 = lo + (it * AT_WARPS + warp) * AT_TILE;
+    const uint8_t* kc = ring + st * S::STAGE;
+    const uint8_t* vc = kc + AT_TILE * ROW;
+    const uint32_t* kp = reinterpret_cast<const uint32_t*>(vc + AT_TILE * ROW);
+    const uint32_t* vp = kp + AT_TILE * NG;
+
+    // scores of tokens 16 mt + g, + 8 for rows 8 nt + 2 t, + 1
+    float x[2][NT][4];
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      uint32_t wa[NB], wb[NB];
+      lds_words<NB>(kc + (16 * mt + g) * ROW + t * 4 * NB, wa);
+      lds_words<NB>(kc + (16 * mt + g + 8) * ROW + t * 4 * NB, wb);
+      uint32_t pa[NG], pb[NG];
+      lds_words<NG>(reinterpret_cast<const uint8_t*>(kp + (16 * mt + g) * NG), pa);
+      lds_words<NG>(reinterpret_cast<const uint8_t*>(kp + (16 * mt + g + 8) * NG), pb);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[mt][nt][i] = 0.0f;
+#pragma unroll
+      for (int gi = 0; gi < NG; ++gi) {
+        float acc[NT][4];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[nt][i] = 0.0f;
+#pragma unroll
+        for (int jj = 0; jj < GB; ++jj) {
+          const int j = gi * GB + jj;
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const uint32_t va = u ? wa[j] >> 8 : wa[j], vb = u ? wb[j] >> 8 : wb[j];
+            const uint32_t a0 = va & 0x000f000fu, a1 = vb & 0x000f000fu, a2 = va & 0x00f000f0u, a3 = vb & 0x00f000f0u;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int p = 0; p < NQ; ++p)
+                mma16816(acc[nt], a0, a1, a2, a3, qf[nt][p][2 * j + u][0], qf[nt][p][2 * j + u][1]);
+          }
+        }
+        const float sa = __uint_as_float(pa[gi] << 16), la = __uint_as_float(pa[gi] & 0xffff0000u);
+        const float sb = __uint_as_float(pb[gi] << 16), lb = __uint_as_float(pb[gi] & 0xffff0000u);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          x[mt][nt][0] = fmaf(la, qsum[nt][gi][0], fmaf(sa, acc[nt][0], x[mt][nt][0]));
+          x[mt][nt][1] = fmaf(la, qsum[nt][gi][1], fmaf(sa, acc[nt][1], x[mt][nt][1]));
+          x[mt][nt][2] = fmaf(lb, qsum[nt][gi][0], fmaf(sb, acc[nt][2], x[mt][nt][2]));
+          x[mt][nt][3] = fmaf(lb, qsum[nt][gi][1], fmaf(sb, acc[nt][3], x[mt][nt][3]));
+        }
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        x[mt][nt][0] *= mul[nt][0];
+        x[mt][nt][1] *= mul[nt][1];
+        x[mt][nt][2] *= mul[nt][0];
+        x[mt][nt][3] *= mul[nt][1];
+      }
+    }
+    const bool whole = tok0 >= all_lo && tok0 + AT_TILE <= all_hi;
+    if (!whole) {
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int tok = tok0 + 16 * mt + g + 8 * (i >> 1);
+            if (tok < see_lo[nt][i & 1] || tok >= see_hi[nt][i & 1]) x[mt][nt][i] = -INFINITY;
+          }
+    }
+
+    // value parameters of this thread's four tokens; tokens past the end hold nothing
+    uint32_t vw[2][2][NG];
+    float smax = 0.0f;
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        lds_words<NG>(reinterpret_cast<const uint8_t*>(vp + (16 * mt + g + 8 * u) * NG), vw[mt][u]);
+        if (!whole && tok0 + 16 * mt + g + 8 * u >= hi)
+#pragma unroll
+          for (int i = 0; i < NG; ++i) vw[mt][u][i] = 0u;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) smax = fmaxf(smax, __uint_as_float(vw[mt][u][i] << 16));
+      }
+
+    // move a row's reference, or the value scale, only where it has to
+    bool move = smax > sigma;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float top = fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u]));
+        move |= top > m[nt][u] + 8.0f;
+      }
+    if (__any_sync(FULL_MASK, move)) {
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) smax = fmaxf(smax, __shfl_xor_sync(FULL_MASK, smax, s));
+      float keep = 1.0f;
+      if (smax > sigma) {  // the next power of two
+        const float ns = __uint_as_float((__float_as_uint(smax) + 0x7fffffu) & 0x7f800000u);
+        keep = sigma / ns;
+        sigma = ns;
+      }
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          float top = fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u]));
+#pragma unroll
+          for (int s = 16; s >= 4; s >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, s));
+          const float nm = fmaxf(m[nt][u], top), f = ex2(m[nt][u] - nm);
+          m[nt][u] = nm;
+          l[nt][u] *= f;
+#pragma unroll
+          for (int i = 0; i < NG; ++i) olo[nt][i][u] *= f;
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              o[nt][j][w][u] *= f * keep;
+              o[nt][j][w][2 + u] *= f * keep;
+            }
+        }
+    }
+    const float pmul = 64.0f / sigma;
+
+#pragma unroll
+    for (int mt = 0; mt < 2; ++mt) {
+      uint32_t pf[NT][NG][NQ][2];  // probabilities times value scales as operand columns
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float p[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = ex2(x[mt][nt][i] - m[nt][i & 1]);
+        l[nt][0] += p[0] + p[2];
+        l[nt][1] += p[1] + p[3];
+#pragma unroll
+        for (int gi = 0; gi < NG; ++gi) {
+          const float la = __uint_as_float(vw[mt][0][gi] & 0xffff0000u), lb = __uint_as_float(vw[mt][1][gi] & 0xffff0000u);
+          olo[nt][gi][0] = fmaf(p[0], la, fmaf(p[2], lb, olo[nt][gi][0]));
+          olo[nt][gi][1] = fmaf(p[1], la, fmaf(p[3], lb, olo[nt][gi][1]));
+          const float sa = __uint_as_float(vw[mt][0][gi] << 16) * pmul, sb = __uint_as_float(vw[mt][1][gi] << 16) * pmul;
+          const float w0 = p[0] * sa, w1 = p[1] * sa, w2 = p[2] * sb, w3 = p[3] * sb;
+          const uint32_t ha = h2(w0, w1), hb = h2(w2, w3);
+          pf[nt][gi][0][0] = movmatrix(ha);
+          pf[nt][gi][0][1] = movmatrix(hb);
+          if constexpr (SPLIT) {
+            const float2 ra = f2(ha), rb = f2(hb);
+            pf[nt][gi][NQ - 1][0] = movmatrix(h2(w0 - ra.x, w1 - ra.y));
+            pf[nt][gi][NQ - 1][1] = movmatrix(h2(w2 - rb.x, w3 - rb.y));
+          }
+        }
+      }
+      // value codes: dimensions 4 g .. 4 g + 3 of each block, tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+      const uint8_t* vr = vc + (16 * mt + 2 * t) * ROW + g * 2 * NB;
+      uint32_t v0[NB / 2], v1[NB / 2], v2[NB / 2], v3[NB / 2];
+      lds_words<NB / 2>(vr, v0);
+      lds_words<NB / 2>(vr + ROW, v1);
+      lds_words<NB / 2>(vr + 8 * ROW, v2);
+      lds_words<NB / 2>(vr + 9 * ROW, v3);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) {
+        const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
+        const uint32_t va = __byte_perm(v0[j >> 1], v1[j >> 1], sel), vb = __byte_perm(v2[j >> 1], v3[j >> 1], sel);
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          const uint32_t ua = w ? va >> 8 : va, ub = w ? vb >> 8 : vb;
+          const uint32_t a0 = ua & 0x000f000fu, a1 = ua & 0x00f000f0u, a2 = ub & 0x000f000fu, a3 = ub & 0x00f000f0u;
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int p = 0; p < NQ; ++p)
+              mma16816(o[nt][j][w], a0, a1, a2, a3, pf[nt][j / GB][p][0], pf[nt][j / GB][p][1]);
+        }
+      }
+    }
+
+    __syncwarp();  // every lane has read the stage
+    const int next = page_at(it + STAGES + 1);
+    issue(it + STAGES, page);
+    page = next;
+    armed = min(it + STAGES + 1, tiles);
+  }
+  if (!ok) {
+    *abort_flag = 1;
+    record_error(a.err, FGQ_ERR_TIMEOUT);
+    for (int i = done; i < armed; ++i) mbar_wait_bounded(&bar[i % STAGES], (uint32_t)(i / STAGES) & 1u, 1u << 16);
+  }
+
+  // join: each warp's rows to shared memory with its reference, over the ring (every copy has landed)
+  __syncthreads();
+  float* jo = reinterpret_cast<float*>(smem);   // [warp][row][D]
+  float* js = jo + AT_WARPS * NR * D;           // [warp][row][2]: m, l
+  {
+    const float even = 262144.0f * sigma;  // 2^24 / 64 sigma: codes' scale and probabilities' scale
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+#pragma unroll
+        for (int s = 4; s < 32; s <<= 1) {
+          l[nt][u] += __shfl_xor_sync(FULL_MASK, l[nt][u], s);
+#pragma unroll
+          for (int i = 0; i < NG; ++i) olo[nt][i][u] += __shfl_xor_sync(FULL_MASK, olo[nt][i][u], s);
+        }
+        const int row = 8 * nt + 2 * t + u;
+        float* dst = jo + (warp * NR + row) * D;
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int w = 0; w < 2; ++w)
+            *reinterpret_cast<float2*>(dst + 32 * j + 4 * g + 2 * w) =
+                make_float2(fmaf(o[nt][j][w][u], even, olo[nt][j / GB][u]),
+                            fmaf(o[nt][j][w][2 + u], even * 0.0625f, olo[nt][j / GB][u]));
+        if (g == 0) {
+          js[(warp * NR + row) * 2] = m[nt][u];
+          js[(warp * NR + row) * 2 + 1] = l[nt][u];
+        }
+      }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < NR * D; i += 32 * AT_WARPS) {
+    const int row = i / D, d = i % D, r = r0 + row;
+    if (r >= a.rows) break;
+    float mm = AT_M0, ll = 0.0f, v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < AT_WARPS; ++w) mm = fmaxf(mm, js[(w * NR + row) * 2]);
+#pragma unroll
+    for (int w = 0; w < AT_WARPS; ++w) {
+      const float f = ex2(js[(w * NR + row) * 2] - mm);
+      ll = fmaf(f, js[(w * NR + row) * 2 + 1], ll);
+      v = fmaf(f, jo[(w * NR + row) * D + d], v);
+    }
+    const int qi = r / a.group, h = r - qi * a.group;
+    const int64_t orow = ((int64_t)b * a.T + qi) * a.q_heads + (int64_t)head * a.group + h;
+    if (a.chunks == 1) {
+      store_out(a, orow * D + d, ll > 0.0f ? v / ll : (ll == 0.0f ? 0.0f : ll));
+    } else {
+      a.part[(orow * a.chunks + ch) * D + d] = v;
+      if (d == 0) {
+        a.stats[(orow * a.chunks + ch) * 2] = mm;
+        a.stats[(orow * a.chunks + ch) * 2 + 1] = ll;
+      }
+    }
+  }
+}
+
+struct AttnKernel {
+  fgq_status (*launch)(const AttnArgs&, unsigned blocks, cudaStream_t);
+  int rows, per_sm;  // query rows of a block; blocks an SM holds
+};
+
+// The kernel for head_dim = 32 nb, group = 32 gb, fp32 inputs (split) or not, `rows` query rows at hand.
+AttnKernel attention_kernel_2(int gb, bool split, int rows);
+AttnKernel attention_kernel_4(int gb, bool split, int rows);
+AttnKernel attention_kernel_8(int gb, bool split, int rows);
+
+}  // namespace dec
+}  // namespace fgq

@@ -1,0 +1,29 @@
+// Launches of the few-row attention kernel, shared by the files that instantiate it per head size.
+#pragma once
+
+#include "kv_attention.cuh"
+#include "tc_common.cuh"
+
+namespace fgq {
+namespace dec {
+
+template <int NB, int GB, bool SPLIT, int NT>
+fgq_status launch_attention(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
+  constexpr int bytes = AttnSmem<NB, GB>::template bytes<NT>();
+  if (!tc::smem_attr_once<kv_attention_kernel<NB, GB, SPLIT, NT>>(bytes)) return FGQ_ERR_CUDA;
+  kv_attention_kernel<NB, GB, SPLIT, NT><<<blocks, 32 * AT_WARPS, bytes, s>>>(a);
+  return after_launch();
+}
+
+// fp32 inputs double the queries' and probabilities' operands, and 256-value heads the sums: both keep to 8 rows.
+template <int NB, int GB>
+AttnKernel pick(bool split, int rows) {
+  if (split) return {launch_attention<NB, GB, true, 1>, 8, attention_blocks_per_sm<NB, true, 1>()};
+  if constexpr (NB <= 4) {
+    if (rows > 8) return {launch_attention<NB, GB, false, 2>, 16, attention_blocks_per_sm<NB, false, 2>()};
+  }
+  return {launch_attention<NB, GB, false, 1>, 8, attention_blocks_per_sm<NB, false, 1>()};
+}
+
+}  // namespace dec
+}  // namespace fgq

@@ -1,7 +1,8 @@
 """Python binding of libfgq (the FGQ CUDA library): argument marshalling only.
 
 Every function here checks tensor dtypes/devices, passes raw device pointers, sizes and
-the current CUDA stream to the C ABI of ``include/fgq.h`` and raises on a non-OK status.
+the current CUDA stream to the C ABI of ``include/fgq.h`` (and ``include/fgq_decoder.h``) and raises on
+a non-OK status.
 All computation happens in the library's CUDA kernels; there is no CPU fallback, and
 loading fails loudly if the library is missing or CUDA is unavailable.
 """
@@ -21,9 +22,12 @@ U8, S8, U4, S4 = 0, 1, 2, 3
 PATH_AUTO, PATH_SIMT, PATH_TC, PATH_GEMV, PATH_DENSE = 0, 1, 2, 3, 4
 ACT_TYPES = {"u8": U8, "s8": S8, "u4": U4, "s4": S4}
 
+F32, BF16, F16 = 0, 1, 2
+FLOAT_TYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+
 _lib: Optional[ctypes.CDLL] = None
 
-# (name, restype, argtypes) of every exported symbol of include/fgq.h and include/fgq_debug.h
+# (name, restype, argtypes) of every exported symbol of include/fgq.h, fgq_decoder.h and fgq_debug.h
 _vp, _i, _i64, _u32, _u64, _f, _sz = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint32,
                                       ctypes.c_uint64, ctypes.c_float, ctypes.c_size_t)
 SIGNATURES = [
@@ -57,6 +61,12 @@ SIGNATURES = [
     ("fgq_conv2d_group_sums", _i, [_vp, _i] + [_i] * 9 + [_vp, _i, _i, _vp, _vp]),
     ("fgq_conv2d_host_workspace_bytes", _sz, [_i] * 12),
     ("fgq_conv2d_host", _i, [_vp, _vp, _i] + [_i] * 11 + [_vp, _vp, _sz, _vp]),
+    ("fgq_kv_append", _i, [_vp, _vp, _vp, _i, _i, _i, _i64, _i64, _i64, _i64, _vp, _i, _vp, _vp, _vp]),
+    ("fgq_kv_read", _i, [_vp, _vp, _vp, _i, _i, _i, _vp, _i, _vp, _vp, _vp]),
+    ("fgq_kv_attention", _i, [_vp, _vp, _i, _i, _i, _i, _i64, _i64, _vp, _i, _vp, _vp, _i, _i, _i, _f, _vp, _vp]),
+    ("fgq_quantize_tokens", _i, [_vp, _i, _i, _i, _i64, _vp, _vp, _vp]),
+    ("fgq_gemm_w8a8", _i, [_vp, _vp, _i, _i, _vp, _vp, _i, _vp, _vp, _i, _vp]),
+    ("fgq_linear_w8a8", _i, [_vp, _i, _i, _i, _i64, _vp, _vp, _i, _vp, _vp, _vp]),
     ("fgq_stream_status", _i, [_vp]),
     ("fgq_set_path", _i, [_i]),
     ("fgq_last_path", _i, []),
@@ -505,6 +515,198 @@ def fgq_conv2d_host(h_w: torch.Tensor, h_x: torch.Tensor, act_type, B: int, H: i
     _check(lib().fgq_conv2d_host(h_w.data_ptr(), h_x.data_ptr(), _act_type(act_type), B, H, W, C, R, S, stride, pad,
                                  groups, M, G, h_out.data_ptr(), workspace.data_ptr(),
                                  workspace.numel() * workspace.element_size(), _stream(stream)), "fgq_conv2d_host")
+
+
+# --------------------------------------------------------------------------- decoders (fgq_decoder.h)
+
+class _KVCacheStruct(ctypes.Structure):
+    _fields_ = [("k_codes", _vp), ("k_params", _vp), ("v_codes", _vp), ("v_params", _vp), ("pages", _i),
+                ("page_size", _i), ("kv_heads", _i), ("head_dim", _i), ("group", _i)]
+
+
+class KVCache:
+    """A paged cache of keys and values held in 4 bits: codes uint8 [pages][kv heads][page size][head_dim / 2],
+    parameters int32 [pages][kv heads][page size][head_dim / group] (layouts in include/fgq_decoder.h)."""
+
+    __slots__ = ("k_codes", "k_params", "v_codes", "v_params", "pages", "page_size", "kv_heads", "head_dim", "group",
+                 "_c", "_ref")
+
+    def __init__(self, k_codes: torch.Tensor, k_params: torch.Tensor, v_codes: torch.Tensor, v_params: torch.Tensor):
+        if k_codes.dim() != 4 or k_params.dim() != 4 or k_params.shape[-1] == 0:
+            raise ValueError("KVCache: codes and parameters are [pages][kv heads][page size][...]")
+        if k_codes.shape != v_codes.shape or k_params.shape != v_params.shape or \
+                k_codes.shape[:3] != k_params.shape[:3]:
+            raise ValueError("KVCache: the four tensors differ in pages, kv heads, page size or row length")
+        self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
+        self.pages, self.kv_heads, self.page_size, half = k_codes.shape
+        self.head_dim = 2 * half
+        self.group = self.head_dim // k_params.shape[3]
+        self._c = _KVCacheStruct(_dev(k_codes, torch.uint8, "k_codes"), _dev(k_params, torch.int32, "k_params"),
+                                 _dev(v_codes, torch.uint8, "v_codes"), _dev(v_params, torch.int32, "v_params"),
+                                 self.pages, self.page_size, self.kv_heads, self.head_dim, self.group)
+        self._ref = ctypes.addressof(self._c)
+
+
+def kv_cache(pages: int, page_size: int, kv_heads: int, head_dim: int, group: int = 64, device="cuda") -> KVCache:
+    """An empty cache (every value 0)."""
+    _require_cuda()
+    if group <= 0 or head_dim % group:
+        raise ValueError("kv_cache: group must divide head_dim")
+    codes = [torch.zeros((pages, kv_heads, page_size, head_dim // 2), dtype=torch.uint8, device=device) for _ in "kv"]
+    params = [torch.zeros((pages, kv_heads, page_size, head_dim // group), dtype=torch.int32, device=device)
+              for _ in "kv"]
+    return KVCache(codes[0], params[0], codes[1], params[1])
+
+
+def _float_type(t: torch.Tensor, name: str) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    ty = FLOAT_TYPES.get(t.dtype)
+    if ty is None:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return ty
+
+
+def _heads(t: torch.Tensor, heads: Optional[int], D: int, name: str) -> Tuple[int, int, int]:
+    """(type, batch stride, token stride) of a [B][T][heads][D] tensor whose last two axes are contiguous."""
+    ty = _float_type(t, name)
+    if t.dim() != 4 or t.shape[3] != D or (heads is not None and t.shape[2] != heads):
+        raise ValueError(f"{name} must be [B][T][{heads or 'heads'}][{D}], got {tuple(t.shape)}")
+    sb, st, sh, sd = t.stride()
+    if (sd != 1 and D > 1) or (sh != D and t.shape[2] > 1):
+        raise ValueError(f"{name}: heads and head_dim must be contiguous")
+    # an axis of one element may have any stride
+    return ty, sb if t.shape[0] > 1 else 0, st if t.shape[1] > 1 else 0
+
+
+def _table(table: torch.Tensor, B: int) -> Tuple[int, int]:
+    p = _dev(table, torch.int32, "page_table")
+    if table.dim() != 2 or table.shape[0] != B:
+        raise ValueError(f"page_table must be [{B}][max pages], got {tuple(table.shape)}")
+    return p, table.shape[1]
+
+
+def _per_sequence(t: Optional[torch.Tensor], B: int, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if isinstance(t, torch.Tensor) and t.numel() != B:
+        raise ValueError(f"{name} must have {B} entries, got {t.numel()}")
+    return _dev(t, torch.int32, name)
+
+
+def fgq_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, starts: torch.Tensor,
+                  lens: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Quantizes k, v [B][T][kv heads][head_dim] into positions starts[b] + i (i < lens[b], or T) of each sequence."""
+    _require_cuda()
+    ty, kb, kt = _heads(k, cache.kv_heads, cache.head_dim, "k")
+    tv, vb, vt = _heads(v, cache.kv_heads, cache.head_dim, "v")
+    if ty != tv or k.shape != v.shape:
+        raise ValueError("fgq_kv_append: k and v differ in shape or type")
+    B, T = k.shape[:2]
+    tp, mp = _table(page_table, B)
+    _check(lib().fgq_kv_append(cache._ref, k.data_ptr(), v.data_ptr(), ty, B, T, kb, kt, vb, vt, tp, mp,
+                               _per_sequence(starts, B, "starts"), _per_sequence(lens, B, "lens"), _stream(stream)),
+           "fgq_kv_append")
+
+
+def fgq_kv_read(cache: KVCache, page_table: torch.Tensor, starts: torch.Tensor, T: int,
+                lens: Optional[torch.Tensor] = None, dtype=torch.bfloat16, stream=None):
+    """(k, v) [B][T][kv heads][head_dim] of positions starts[b] + i as the values their codes stand for."""
+    _require_cuda()
+    B = page_table.shape[0]
+    tp, mp = _table(page_table, B)
+    if dtype not in FLOAT_TYPES:
+        raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+    k, v = (torch.empty((B, T, cache.kv_heads, cache.head_dim), dtype=dtype, device=page_table.device) for _ in "kv")
+    _check(lib().fgq_kv_read(cache._ref, k.data_ptr(), v.data_ptr(), FLOAT_TYPES[dtype], B, T, tp, mp,
+                             _per_sequence(starts, B, "starts"), _per_sequence(lens, B, "lens"), _stream(stream)),
+           "fgq_kv_read")
+    return k, v
+
+
+def fgq_kv_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, seq_lens: torch.Tensor,
+                     q_lens: Optional[torch.Tensor] = None, causal: bool = True, window: int = 0,
+                     scale: Optional[float] = None, max_len: int = 0, out: Optional[torch.Tensor] = None,
+                     stream=None) -> torch.Tensor:
+    """Attention of q [B][T][heads][head_dim] over the cache (scale: head_dim ** -0.5) -> out of q's shape and type."""
+    _require_cuda()
+    ty, qb, qt = _heads(q, None, cache.head_dim, "q")
+    B, T, heads, D = q.shape
+    tp, mp = _table(page_table, B)
+    if out is None:
+        out = torch.empty((B, T, heads, D), dtype=q.dtype, device=q.device)
+    elif out.shape != q.shape:
+        raise ValueError(f"out must be {tuple(q.shape)}, got {tuple(out.shape)}")
+    _check(lib().fgq_kv_attention(cache._ref, q.data_ptr(), ty, B, T, heads, qb, qt, tp, mp,
+                                  _per_sequence(seq_lens, B, "seq_lens"), _per_sequence(q_lens, B, "q_lens"), max_len,
+                                  int(causal), window, D ** -0.5 if scale is None else scale,
+                                  _dev(out, q.dtype, "out"), _stream(stream)), "fgq_kv_attention")
+    return out
+
+
+def _rows(x: torch.Tensor, name: str) -> Tuple[int, int]:
+    """(type, row stride) of a [P][K] tensor with contiguous rows."""
+    ty = _float_type(x, name)
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name} must be [tokens][features] with contiguous rows")
+    return ty, x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def fgq_quantize_tokens(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Per-token symmetric 8-bit quantization: x [P][K] -> (codes int8 [P][K], scale fp32 [P])."""
+    _require_cuda()
+    ty, ldx = _rows(x, "x")
+    P, K = x.shape
+    q = torch.empty((P, K), dtype=torch.int8, device=x.device)
+    scale = torch.empty(P, dtype=torch.float32, device=x.device)
+    _check(lib().fgq_quantize_tokens(x.data_ptr(), ty, P, K, ldx, q.data_ptr(), scale.data_ptr(), _stream(stream)),
+           "fgq_quantize_tokens")
+    return q, scale
+
+
+def _weights8(wq: torch.Tensor, wscale: torch.Tensor, bias: Optional[torch.Tensor], K: int):
+    if wq.dim() != 2 or wq.shape[1] != K or wscale.numel() != wq.shape[0] or \
+            (bias is not None and bias.numel() != wq.shape[0]):
+        raise ValueError(f"weights must be int8 [M][{K}] with fp32 scales (and bias) [M]")
+    return (_dev(wq, torch.int8, "wq"), _dev(wscale, torch.float32, "wscale"),
+            None if bias is None else _dev(bias, torch.float32, "bias"))
+
+
+def fgq_gemm_w8a8(q: torch.Tensor, scale: torch.Tensor, wq: torch.Tensor, wscale: torch.Tensor,
+                  bias: Optional[torch.Tensor] = None, dtype=torch.float32, y: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """y[p][m] = scale[p] wscale[m] sum_k q[p][k] wq[m][k] + bias[m], of type dtype."""
+    _require_cuda()
+    P, K = q.shape
+    pw, ps, pb = _weights8(wq, wscale, bias, K)
+    if dtype not in FLOAT_TYPES:
+        raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
+    if scale.numel() != P:
+        raise ValueError(f"scale must have {P} entries, got {scale.numel()}")
+    if y is None:
+        y = torch.empty((P, wq.shape[0]), dtype=dtype, device=q.device)
+    elif tuple(y.shape) != (P, wq.shape[0]):
+        raise ValueError(f"y must be {(P, wq.shape[0])}, got {tuple(y.shape)}")
+    _check(lib().fgq_gemm_w8a8(_dev(q, torch.int8, "q"), _dev(scale, torch.float32, "scale"), P, K, pw, ps,
+                               wq.shape[0], pb, _dev(y, dtype, "y"), FLOAT_TYPES[dtype], _stream(stream)),
+           "fgq_gemm_w8a8")
+    return y
+
+
+def fgq_linear_w8a8(x: torch.Tensor, wq: torch.Tensor, wscale: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                    y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """A linear layer on 8-bit integers: x [P][K] quantized per token, times wq [M][K]^T, of x's type."""
+    _require_cuda()
+    ty, ldx = _rows(x, "x")
+    P, K = x.shape
+    pw, ps, pb = _weights8(wq, wscale, bias, K)
+    if y is None:
+        y = torch.empty((P, wq.shape[0]), dtype=x.dtype, device=x.device)
+    elif tuple(y.shape) != (P, wq.shape[0]):
+        raise ValueError(f"y must be {(P, wq.shape[0])}, got {tuple(y.shape)}")
+    _check(lib().fgq_linear_w8a8(x.data_ptr(), ty, P, K, ldx, pw, ps, wq.shape[0], pb, _dev(y, x.dtype, "y"),
+                                 _stream(stream)), "fgq_linear_w8a8")
+    return y
 
 
 def fgq_stream_status(stream=None) -> int:

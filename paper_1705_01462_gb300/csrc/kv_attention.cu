@@ -22,7 +22,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
   const int qi = (int)(bt % a.T), b = (int)(bt / a.T);
   const int tid = threadIdx.x, d = tid % D, way = tid / D;
   pdl_wait();
-  const int n = __ldg(a.seq_lens + b);
+  const int n = seq_len(a, b);
   const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
   const int r0 = (qi * a.group + hq % a.group) / tile_rows * tile_rows;  // the block's tile of query rows
   int first, end;
@@ -72,10 +72,19 @@ fgq_status launch_few_rows(const fgq_kv_cache* cache, AttnArgs a, int max_len, c
   int64_t span = max_len;  // tokens that one block may have to read
   if (a.window && (int64_t)a.window + k.rows / a.group + 1 < span) span = (int64_t)a.window + k.rows / a.group + 1;
   span += 15;
-  // chunks for about two waves of blocks, of 128 tokens (a tile for each warp) at least
-  const int64_t want = (2ll * device_sms() * k.per_sm + units - 1) / units;
-  int64_t chunk = (span + want - 1) / want;
-  chunk = (chunk + 127) / 128 * 128;
+  // the split: whole waves of blocks, as many as cost least if every sequence is as long as the longest may
+  // be, a block costing its tokens and about 256 more; 128 tokens (a tile for each warp) at least
+  const int64_t slots = (int64_t)device_sms() * k.per_sm;
+  int64_t chunk = 0, best = INT64_MAX;
+  for (int waves = 1; waves <= 8; ++waves) {
+    const int64_t n = waves * slots / units > 0 ? waves * slots / units : 1;
+    const int64_t c = ((span + n - 1) / n + 127) / 128 * 128;
+    const int64_t blocks = units * ((span + c - 1) / c), cost = (blocks + slots - 1) / slots * (c + 256);
+    if (cost < best) {
+      best = cost;
+      chunk = c;
+    }
+  }
   a.chunk = (int)chunk;
   a.chunks = (int)((span + chunk - 1) / chunk);
   if (units * a.chunks > INT32_MAX) return FGQ_ERR_UNSUPPORTED;

@@ -4,25 +4,29 @@
 // Mathematics.  With k = lo + s c, the score of token t and query row n is
 //   scale * sum_g ( s_tg (q_ng . c_tg) + lo_tg sum(q_ng) )         (g: groups of the head's values)
 // and with v likewise, the output's value d in group g is
-//   sum_t (p_nt s_tg) c_td + sum_t p_nt lo_tg,
+//   sum_t (p_nt s_tg) (c_td - 8) + sum_t p_nt (lo_tg + 8 s_tg),
 // so both products run on the codes themselves and the parameters are applied to scores and to
 // probabilities.  A code in the low bits of an fp16 is the subnormal c 2^-24 (or 16 c 2^-24, four bits
-// up): one AND per two codes makes a matrix operand, exactly.  Tokens (keys) and values' dimensions (V)
+// up): one AND and one packed product per two codes make the matrix operand c 2^-9, exactly.  (The
+// subnormals themselves lose up to ten bits in the instructions' sums: 7e-5 of the output instead of
+// 1e-6 for fp32.)  Tokens (keys) and values' dimensions (V)
 // are the M = 16 rows of mma.m16n8k16, eight query rows its columns, so that a group of eight query
 // heads pads nothing.  These legacy matrix instructions do here: 16 of them per 2 KB of cache leave the
 // tensor pipe a third busy at full HBM rate, and tcgen05 would want the dequantized operands in shared
 // or tensor memory first.
 //
 // What is rounded: queries to fp16 after scaling each row by a power of two (exact for bf16 and fp16;
-// fp32 queries take two fp16 parts, SPLIT), and p s to fp16 (two parts for SPLIT), scaled by a power of
-// two that follows the largest value scale met.  Scores, statistics and sums are fp32.
+// fp32 queries take two fp16 parts, SPLIT), and p s to fp16 (two parts for SPLIT; value codes are centred
+// so that its error meets values of the size of v).  Scores, statistics and sums are fp32.
 //
-// Softmax.  The reference m of a row moves only when a score exceeds it by more than 8 (in log2 units):
-// probabilities stay below 2^8, and the common tile needs one vote instead of a reduction per row.
+// Softmax.  Probabilities are held as 2^(x - r): r is a row's largest score so far (in log2 units), less
+// 6 - log2(sigma) for the power of two sigma at or above every value scale met, so that p s fits fp16
+// whatever the values' magnitude.  r moves only when a score exceeds its maximum by more than 8, or a
+// value scale sigma: the common tile needs one vote instead of a reduction per row.
 //
 // Split.  A block of 4 warps takes `chunk` tokens of one (sequence, kv head, tile of 8 NT query rows);
 // each warp streams every fourth tile of 32 tokens through a ring of bulk copies of its own (no barrier
-// between warps), and the warps' sums are joined in shared memory.  Several chunks leave (m, l, sum) in
+// between warps), and the warps' sums are joined in shared memory.  Several chunks leave (r, l, sum) in
 // fp32, which a second kernel joins.
 #pragma once
 
@@ -40,7 +44,7 @@ struct AttnArgs {
   const int32_t* seq_lens;
   const int32_t* q_lens;
   float* part;   // [row][chunks] partial sums of D values each, or nullptr (one chunk)
-  float* stats;  // [row][chunks][2]: m, l
+  float* stats;  // [row][chunks][2]: r, l
   unsigned int* err;
   uint64_t timeout_ns;
   float scale_log2;  // scale * log2(e)
@@ -86,8 +90,31 @@ __device__ __forceinline__ uint32_t movmatrix(uint32_t x) {
 }
 __device__ __forceinline__ float ex2(float x) {
   float y;
-  asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// c 2^-9 for the two codes in the low nibbles of w's halves, or the next ones: subnormals scaled to normal
+// fp16, exactly.
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w & 0x000f000fu), "r"(0x78007800u));  // 2^15
+  return r;
+}
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w & 0x00f000f0u), "r"(0x68006800u));  // 2^11
+  return r;
+}
+// (c - 8) 2^-9 likewise.
+__device__ __forceinline__ uint32_t centred_lo(uint32_t w) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w & 0x000f000fu), "r"(0x78007800u), "r"(0xa400a400u));  // -2^-6
+  return r;
+}
+__device__ __forceinline__ uint32_t centred_hi(uint32_t w) {
+  uint32_t r;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w & 0x00f000f0u), "r"(0x68006800u), "r"(0xa400a400u));
+  return r;
 }
 __device__ __forceinline__ uint32_t h2(float a, float b) { return pack2(a, b, __half()); }
 __device__ __forceinline__ float2 f2(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
@@ -127,6 +154,14 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t at, float v
     static_cast<__nv_bfloat16*>(a.out)[at] = __float2bfloat16_rn(v);
   else
     static_cast<__half*>(a.out)[at] = __float2half_rn(v);
+}
+
+// Tokens of sequence b: at most what the table can hold (more is an error), less than 2^31 - 2^12.
+__device__ __forceinline__ int seq_len(const AttnArgs& a, int b) {
+  const int n = __ldg(a.seq_lens + b);
+  const int most = (int)min((int64_t)a.c.max_pages * a.c.page_size, (int64_t)INT32_MAX - 4096);
+  if (n > most) record_error(a.err, FGQ_ERR_ARG);
+  return min(n, most);
 }
 
 // First and one past the last position that any of the query rows [i0, i1] (by query index) of a
@@ -178,7 +213,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
   const int b = id / a.c.kv_heads;
   const int r0 = rt * NR;
 
-  const int n = __ldg(a.seq_lens + b);
+  const int n = seq_len(a, b);
   const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
   int first, end;
   visible(a, n, nq, r0 / a.group, (min(r0 + NR, a.rows) - 1) / a.group, first, end);
@@ -214,43 +249,43 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
   const int tiles = (tiles_all - warp + AT_WARPS - 1) / AT_WARPS;  // this warp's
 
   // lanes 0-7 copy: half (16 tokens) lane / 4, array lane % 4 (key codes, value codes, key, value parameters)
-  const int half = (lane >> 2) & 1, arr = lane & 3;
-  auto page_at = [&](int i) -> int {  // page of this lane's half of the warp's tile i, or -1
-    const int tok = lo + (i * AT_WARPS + warp) * AT_TILE + 16 * half;
-    if (i >= tiles || tok >= hi || lane >= 8) return -1;
-    const uint32_t pi = page_of(a.c, (uint32_t)tok);
-    if (pi >= (uint32_t)a.c.max_pages) return -2;
-    const int page = __ldg(a.c.table + (int64_t)b * a.c.max_pages + pi);
-    return page >= 0 && page < a.c.pages ? page : -2;
-  };
-  auto issue = [&](int i, int page) {
-    if (i >= tiles) return;
-    const int tok = lo + (i * AT_WARPS + warp) * AT_TILE + 16 * half;
-    if (page == -2) record_error(a.err, FGQ_ERR_ARG);
-    const uint32_t ok = __ballot_sync(FULL_MASK, page >= 0) & 0x11u;  // a lane of each half
-    uint64_t* bi = &bar[i % STAGES];
-    if (lane == 0) mbar_arrive_expect_tx(bi, (uint32_t)__popc(ok) * 16u * 2u * (ROW + PAR));
-    __syncwarp();
-    if (page >= 0) {
-      const int slot = tok - (int)page_of(a.c, (uint32_t)tok) * a.c.page_size;
-      const int64_t row = ((int64_t)page * a.c.kv_heads + head) * a.c.page_size + slot;
-      uint8_t* st = ring + (i % STAGES) * S::STAGE;
-      const bool par = arr >= 2, val = arr & 1;
-      const uint32_t bytes = 16u * (par ? PAR : ROW);
-      const uint8_t* src = par ? reinterpret_cast<const uint8_t*>(val ? a.c.v_params : a.c.k_params) + row * PAR
-                               : (val ? a.c.v_codes : a.c.k_codes) + row * ROW;
-      uint8_t* dst = st + (par ? 2 * AT_TILE * ROW + (val ? AT_TILE * PAR : 0) : (val ? AT_TILE * ROW : 0)) +
-                     half * (int)bytes;
-      bulk_load(smem_u32(dst), src, bytes, bi);
+  const bool par = lane & 2, val = lane & 1;
+  const uint32_t row_bytes = par ? PAR : ROW;
+  const uint8_t* src = par ? reinterpret_cast<const uint8_t*>(val ? a.c.v_params : a.c.k_params)
+                           : (val ? a.c.v_codes : a.c.k_codes);
+  const uint32_t dst = smem_u32(ring) + (par ? 2 * AT_TILE * ROW + (val ? AT_TILE * PAR : 0) : (val ? AT_TILE * ROW : 0)) +
+                       ((lane >> 2) & 1) * 16 * row_bytes;
+  const int32_t* table = a.c.table + (int64_t)b * a.c.max_pages;
+  int ptok = lo + warp * AT_TILE + 16 * ((lane >> 2) & 1);  // this lane's next token to look up
+  int page = -1, slot = 0;  // of its half of the next tile to issue, where that begins before hi (want)
+  bool want = false;
+  auto look_up = [&]() {  // positions below hi are inside the table: seq_len() sees to it
+    want = lane < 8 && ptok < hi;
+    if (want) {
+      const uint32_t pi = page_of(a.c, (uint32_t)ptok);
+      slot = ptok - (int)pi * a.c.page_size;
+      page = __ldg(table + pi);
     }
+    ptok += AT_WARPS * AT_TILE;
   };
-  int armed = 0, page = page_at(0);
+  int ist = 0;  // stage of the next tile to issue
+  auto issue = [&]() {
+    const bool good = want && page >= 0 && page < a.c.pages;
+    if (want && !good) record_error(a.err, FGQ_ERR_ARG);
+    const uint32_t ok = __ballot_sync(FULL_MASK, good) & 0x11u;  // a lane of each half
+    if (lane == 0) mbar_arrive_expect_tx(&bar[ist], (uint32_t)__popc(ok) * 16u * 2u * (ROW + PAR));
+    __syncwarp();
+    if (good)
+      bulk_load(dst + ist * S::STAGE, src + (((int64_t)page * a.c.kv_heads + head) * a.c.page_size + slot) * row_bytes,
+                16u * row_bytes, &bar[ist]);
+    ist = ist + 1 == STAGES ? 0 : ist + 1;
+  };
+  look_up();
+  int issued = 0;
 #pragma unroll 1
-  for (int i = 0; i < STAGES; ++i) {
-    const int next = page_at(i + 1);
-    issue(i, page);
-    page = next;
-    armed = min(i + 1, tiles);
+  for (; issued < STAGES && issued < tiles; ++issued) {
+    issue();
+    look_up();
   }
 
   // queries as operand columns: this thread's part of row 8 nt + g, and what rows 8 nt + 2 t, + 1 need
@@ -287,9 +322,8 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {  // pairs (0, 1), (2, 3), ..; odd ones meet codes times 16
-        const float dn = (w & 1) ? 0.0625f : 1.0f;
-        const float p0 = x[j][2 * w] * up * dn, p1 = x[j][2 * w + 1] * up * dn;
+      for (int w = 0; w < 4; ++w) {  // pairs (0, 1), (2, 3), ..
+        const float p0 = x[j][2 * w] * up, p1 = x[j][2 * w + 1] * up;
         const uint32_t hw = h2(p0, p1);
         const float2 back = f2(hw);
         float s0 = back.x, s1 = back.y;
@@ -300,16 +334,16 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
           const float2 rest = f2(lw);
           s0 += rest.x, s1 += rest.y;
         }
-        sums[j / GB] += (s0 + s1) * ((w & 1) ? 16.0f : 1.0f);
+        sums[j / GB] += s0 + s1;
       }
     }
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
       sums[i] += __shfl_xor_sync(FULL_MASK, sums[i], 1);
       sums[i] += __shfl_xor_sync(FULL_MASK, sums[i], 2);
-      sums[i] *= 5.9604645e-8f;  // 2^-24: the accumulated codes' scale
+      sums[i] *= 0.001953125f;  // 2^-9: the codes' scale
     }
-    const float m = pow2f(-e) * a.scale_log2 * 16777216.0f;
+    const float m = fmaxf(pow2f(-e) * a.scale_log2 * 512.0f, 1e-37f);
     // positions of the row: [sl, sh)
     int sl = 0, sh = live ? 0 : INT32_MAX;  // rows past the last: zero queries, masked nowhere
     if (live && qi < nq) {
@@ -337,12 +371,14 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
     all_hi = min(all_hi, __shfl_xor_sync(FULL_MASK, all_hi, o));
   }
 
-  float o[NT][NB][2][4], olo[NT][NG][2], l[NT][2], m[NT][2];
+  // sums of 2^(x - ref) times codes, times lo, and alone; a row's ref moves when a raw score passes its limit
+  float o[NT][NB][2][4], olo[NT][NG][2], l[NT][2], top[NT][2], ref[NT][2], limit[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      m[nt][u] = AT_M0;
+      top[nt][u] = ref[nt][u] = AT_M0;
+      limit[nt][u] = -INFINITY;
       l[nt][u] = 0.0f;
 #pragma unroll
       for (int i = 0; i < NG; ++i) olo[nt][i][u] = 0.0f;
@@ -354,20 +390,18 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[nt][j][u][i] = 0.0f;
   }
-  float sigma = 7.888609e-31f;  // 2^-100; a power of two at or above every value scale met so far
+  float sigma = 8.6736174e-19f;  // 2^-60; a power of two at or above every value scale met so far
 
   bool ok = true;
-  int done = 0;
+  int done = 0, tok0 = lo + warp * AT_TILE, st = 0;
+  uint32_t phase = 0;
 #pragma unroll 1
-  for (int it = 0; it < tiles; ++it) {
-    const int st = it % STAGES;
+  for (; done < tiles; ++done, tok0 += AT_WARPS * AT_TILE) {
     // a limit of 0 (a test's) expires at once, whether the copy has landed or not
-    if (a.timeout_ns == 0 || !mbar_wait_warp(&bar[st], (uint32_t)(it / STAGES) & 1u, a.timeout_ns, abort_flag)) {
+    if (a.timeout_ns == 0 || !mbar_wait_warp(&bar[st], phase, a.timeout_ns, abort_flag)) {
       ok = false;
       break;
     }
-    done = it + 1;
-    const int tok0 = lo + (it * AT_WARPS + warp) * AT_TILE;
     const uint8_t* kc = ring + st * S::STAGE;
     const uint8_t* vc = kc + AT_TILE * ROW;
     const uint32_t* kp = reinterpret_cast<const uint32_t*>(vc + AT_TILE * ROW);
@@ -400,7 +434,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const uint32_t va = u ? wa[j] >> 8 : wa[j], vb = u ? wb[j] >> 8 : wb[j];
-            const uint32_t a0 = va & 0x000f000fu, a1 = vb & 0x000f000fu, a2 = va & 0x00f000f0u, a3 = vb & 0x00f000f0u;
+            const uint32_t a0 = codes_lo(va), a1 = codes_lo(vb), a2 = codes_hi(va), a3 = codes_hi(vb);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -417,13 +451,6 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
           x[mt][nt][2] = fmaf(lb, qsum[nt][gi][0], fmaf(sb, acc[nt][2], x[mt][nt][2]));
           x[mt][nt][3] = fmaf(lb, qsum[nt][gi][1], fmaf(sb, acc[nt][3], x[mt][nt][3]));
         }
-      }
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        x[mt][nt][0] *= mul[nt][0];
-        x[mt][nt][1] *= mul[nt][1];
-        x[mt][nt][2] *= mul[nt][0];
-        x[mt][nt][3] *= mul[nt][1];
       }
     }
     const bool whole = tok0 >= all_lo && tok0 + AT_TILE <= all_hi;
@@ -454,33 +481,31 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
         for (int i = 0; i < NG; ++i) smax = fmaxf(smax, __uint_as_float(vw[mt][u][i] << 16));
       }
 
-    // move a row's reference, or the value scale, only where it has to
     bool move = smax > sigma;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const float top = fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u]));
-        move |= top > m[nt][u] + 8.0f;
-      }
+      for (int u = 0; u < 2; ++u)
+        move |= fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u])) > limit[nt][u];
     if (__any_sync(FULL_MASK, move)) {
 #pragma unroll
       for (int s = 16; s > 0; s >>= 1) smax = fmaxf(smax, __shfl_xor_sync(FULL_MASK, smax, s));
-      float keep = 1.0f;
-      if (smax > sigma) {  // the next power of two
-        const float ns = __uint_as_float((__float_as_uint(smax) + 0x7fffffu) & 0x7f800000u);
-        keep = sigma / ns;
-        sigma = ns;
-      }
+      if (smax > sigma)  // the next power of two
+        sigma = __uint_as_float((__float_as_uint(smax) + 0x7fffffu) & 0x7f800000u);
+      const float down = 6.0f - (float)((int)(__float_as_uint(sigma) >> 23) - 127);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          float top = fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u]));
+          float h = fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u]));
 #pragma unroll
-          for (int s = 16; s >= 4; s >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL_MASK, top, s));
-          const float nm = fmaxf(m[nt][u], top), f = ex2(m[nt][u] - nm);
-          m[nt][u] = nm;
+          for (int s = 16; s >= 4; s >>= 1) h = fmaxf(h, __shfl_xor_sync(FULL_MASK, h, s));
+          if (h > -INFINITY) {
+            top[nt][u] = fmaxf(top[nt][u], h * mul[nt][u]);
+            limit[nt][u] = (top[nt][u] + 8.0f) / mul[nt][u];
+          }
+          const float nr = top[nt][u] - down, f = ex2(ref[nt][u] - nr);
+          ref[nt][u] = nr;
           l[nt][u] *= f;
 #pragma unroll
           for (int i = 0; i < NG; ++i) olo[nt][i][u] *= f;
@@ -488,12 +513,11 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
           for (int j = 0; j < NB; ++j)
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
-              o[nt][j][w][u] *= f * keep;
-              o[nt][j][w][2 + u] *= f * keep;
+              o[nt][j][w][u] *= f;
+              o[nt][j][w][2 + u] *= f;
             }
         }
     }
-    const float pmul = 64.0f / sigma;
 
 #pragma unroll
     for (int mt = 0; mt < 2; ++mt) {
@@ -502,15 +526,16 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
       for (int nt = 0; nt < NT; ++nt) {
         float p[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = ex2(x[mt][nt][i] - m[nt][i & 1]);
+        for (int i = 0; i < 4; ++i) p[i] = ex2(fmaf(x[mt][nt][i], mul[nt][i & 1], -ref[nt][i & 1]));
         l[nt][0] += p[0] + p[2];
         l[nt][1] += p[1] + p[3];
 #pragma unroll
         for (int gi = 0; gi < NG; ++gi) {
-          const float la = __uint_as_float(vw[mt][0][gi] & 0xffff0000u), lb = __uint_as_float(vw[mt][1][gi] & 0xffff0000u);
+          const float sa = __uint_as_float(vw[mt][0][gi] << 16), sb = __uint_as_float(vw[mt][1][gi] << 16);
+          const float la = fmaf(8.0f, sa, __uint_as_float(vw[mt][0][gi] & 0xffff0000u));  // the codes' centre
+          const float lb = fmaf(8.0f, sb, __uint_as_float(vw[mt][1][gi] & 0xffff0000u));
           olo[nt][gi][0] = fmaf(p[0], la, fmaf(p[2], lb, olo[nt][gi][0]));
           olo[nt][gi][1] = fmaf(p[1], la, fmaf(p[3], lb, olo[nt][gi][1]));
-          const float sa = __uint_as_float(vw[mt][0][gi] << 16) * pmul, sb = __uint_as_float(vw[mt][1][gi] << 16) * pmul;
           const float w0 = p[0] * sa, w1 = p[1] * sa, w2 = p[2] * sb, w3 = p[3] * sb;
           const uint32_t ha = h2(w0, w1), hb = h2(w2, w3);
           pf[nt][gi][0][0] = movmatrix(ha);
@@ -536,7 +561,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           const uint32_t ua = w ? va >> 8 : va, ub = w ? vb >> 8 : vb;
-          const uint32_t a0 = ua & 0x000f000fu, a1 = ua & 0x00f000f0u, a2 = ub & 0x000f000fu, a3 = ub & 0x00f000f0u;
+          const uint32_t a0 = centred_lo(ua), a1 = centred_hi(ua), a2 = centred_lo(ub), a3 = centred_hi(ub);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -547,23 +572,27 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
     }
 
     __syncwarp();  // every lane has read the stage
-    const int next = page_at(it + STAGES + 1);
-    issue(it + STAGES, page);
-    page = next;
-    armed = min(it + STAGES + 1, tiles);
+    if (issued < tiles) {
+      issue();
+      look_up();
+      ++issued;
+    }
+    if (++st == STAGES) {
+      st = 0;
+      phase ^= 1u;
+    }
   }
   if (!ok) {
     *abort_flag = 1;
     record_error(a.err, FGQ_ERR_TIMEOUT);
-    for (int i = done; i < armed; ++i) mbar_wait_bounded(&bar[i % STAGES], (uint32_t)(i / STAGES) & 1u, 1u << 16);
+    for (int i = done; i < issued; ++i) mbar_wait_bounded(&bar[i % STAGES], (uint32_t)(i / STAGES) & 1u, 1u << 16);
   }
 
   // join: each warp's rows to shared memory with its reference, over the ring (every copy has landed)
   __syncthreads();
   float* jo = reinterpret_cast<float*>(smem);   // [warp][row][D]
-  float* js = jo + AT_WARPS * NR * D;           // [warp][row][2]: m, l
+  float* js = jo + AT_WARPS * NR * D;           // [warp][row][2]: r, l
   {
-    const float even = 262144.0f * sigma;  // 2^24 / 64 sigma: codes' scale and probabilities' scale
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -581,10 +610,10 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
 #pragma unroll
           for (int w = 0; w < 2; ++w)
             *reinterpret_cast<float2*>(dst + 32 * j + 4 * g + 2 * w) =
-                make_float2(fmaf(o[nt][j][w][u], even, olo[nt][j / GB][u]),
-                            fmaf(o[nt][j][w][2 + u], even * 0.0625f, olo[nt][j / GB][u]));
+                make_float2(fmaf(o[nt][j][w][u], 512.0f, olo[nt][j / GB][u]),  // 2^9: the codes' scale
+                            fmaf(o[nt][j][w][2 + u], 512.0f, olo[nt][j / GB][u]));
         if (g == 0) {
-          js[(warp * NR + row) * 2] = m[nt][u];
+          js[(warp * NR + row) * 2] = ref[nt][u];
           js[(warp * NR + row) * 2 + 1] = l[nt][u];
         }
       }

@@ -61,10 +61,13 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
 
 }  // namespace
 
-fgq_status launch_few_rows(const fgq_kv_cache* cache, AttnArgs a, int max_len, cudaStream_t s) {
+constexpr int PROMPT_MIN_ROWS = 33;
+
+fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_len, cudaStream_t s) {
   const int D = cache->head_dim, nb = D / 32, gb = cache->group / 32;
   const bool split = a.type == FGQ_F32;
-  const AttnKernel k = nb == 2   ? attention_kernel_2(gb, split, a.rows)
+  const AttnKernel k = !split && a.rows >= PROMPT_MIN_ROWS ? prompt_kernel(D, cache->group, a.rows)
+                       : nb == 2   ? attention_kernel_2(gb, split, a.rows)
                        : nb == 4 ? attention_kernel_4(gb, split, a.rows)
                                  : attention_kernel_8(gb, split, a.rows);
   a.row_tiles = (a.rows + k.rows - 1) / k.rows;
@@ -73,7 +76,7 @@ fgq_status launch_few_rows(const fgq_kv_cache* cache, AttnArgs a, int max_len, c
   if (a.window && (int64_t)a.window + k.rows / a.group + 1 < span) span = (int64_t)a.window + k.rows / a.group + 1;
   span += 15;
   // the split: whole waves of blocks, as many as cost least if every sequence is as long as the longest may
-  // be, a block costing its tokens and about 256 more; 128 tokens (a tile for each warp) at least
+  // be, a block costing its tokens and about 256 more; 128 tokens at least
   const int64_t slots = (int64_t)device_sms() * k.per_sm;
   int64_t chunk = 0, best = INT64_MAX;
   for (int waves = 1; waves <= 8; ++waves) {
@@ -153,5 +156,5 @@ extern "C" fgq_status fgq_kv_attention(const fgq_kv_cache* cache, const void* q,
   a.causal = causal;
   a.window = window;
   const int bound = max_len > 0 && max_len < capacity ? max_len : (int)(capacity > 0 ? capacity : 1);
-  return launch_few_rows(cache, a, bound, stream);
+  return launch_attention_call(cache, a, bound, stream);
 }

@@ -654,6 +654,8 @@ struct AttnKernel {
 AttnKernel attention_kernel_2(int gb, bool split, int rows);
 AttnKernel attention_kernel_4(int gb, bool split, int rows);
 AttnKernel attention_kernel_8(int gb, bool split, int rows);
+// The kernel for many query rows (kv_prompt.cu), bf16 and fp16.
+AttnKernel prompt_kernel(int head_dim, int group, int rows);
 
 }  // namespace dec
 }  // namespace fgq

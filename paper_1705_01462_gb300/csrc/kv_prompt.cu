@@ -2,23 +2,26 @@
 // fp16, on tcgen05.
 //
 // A block takes NQT tiles of 128 query rows (query, head of the group) of one (sequence, kv head) and a
-// chunk of its tokens, 64 at a time:
-//   S[128 x 64] = Q K^T        both operands K-major in shared memory (128-byte swizzle), fp32 S in TMEM
-//   P = 2^(x - r)              one thread a row; P as fp16 over S in TMEM
+// chunk of its tokens, BN at a time:
+//   S[128 x BN] = Q K^T        both operands K-major in shared memory (128-byte swizzle), fp32 S in TMEM
+//   P = 2^(x - r)              one thread a row, 64 tokens (a unit) at a time; P as fp16 over S in TMEM
 //   O[128 x D] += P V          P the TMEM operand, V as it lies, token by token: the MN-major operand
 // K and V are dequantized once per block into shared memory as fp16, so that a value costs its share of
-// 128 NQT rows' arithmetic.  Two tiles of rows and two S buffers each: scores of the next 64 tokens and
-// the other tile's products run while a tile's softmax does.
+// 128 NQT rows' arithmetic.  BN = 128 where it fits: at N = 64 an MMA reads its 128 query rows for half the
+// arithmetic, and the scores of 64 tokens took 1500 clocks where 512 are due.  While a tile of rows does its
+// softmax the other one's products run (NQT = 2), or the next scores into a second buffer (NQT = 1).
 //
-// Range.  Queries are scaled by a power of two per row; K and V by a power of two per 64 tokens (2^-ek,
+// Range.  Queries are scaled by a power of two per row; K and V by a power of two per unit (2^-ek,
 // 2^-ev) that brings their largest magnitude to [2^13, 2^14), so fp16 holds any bf16-ranged cache.  S is
 // multiplied by 2^ek; P takes 2^ev: p = 2^(x + ev - r) against V 2^-ev, and l sums p 2^-ev.  r is a row's
-// largest x + ev so far, less 6; it moves only when exceeded by 8 (as in kv_attention.cuh), and only then is
-// O rescaled, after the products that add to it.
+// largest x + ev at its last move, less 6.  It moves only when the unit's probabilities, computed on the old r,
+// sum to more than 2^15, so that fp16 might not hold one: no maximum is taken otherwise, and O is rescaled
+// only then, after the products that add to it.
 // What is rounded: lo + s c, probabilities to fp16 (11 bits); sums and statistics are fp32.
 //
-// Warp roles (one block per SM): warps 0 .. 4 NQT - 1 softmax (TMEM lane = row); the next four dequantize,
-// 16 tokens each; the last warp allocates TMEM and issues the MMAs.
+// Warp roles (one block per SM): warps 0 .. 4 NQT - 1 softmax (TMEM lane = row); the next eight dequantize,
+// in two groups that take units in turn, 16 tokens a warp; the last group of four holds the MMA issuer, which
+// also allocates TMEM.
 // Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded, the roles leave their loops, MMAs in
 // flight are waited for, and TMEM is freed.
 #include "kv_attention.cuh"
@@ -30,22 +33,32 @@ namespace {
 using namespace dec;
 using tc::sw128;
 
-constexpr int PR_BN = 64;          // tokens of a tile
-constexpr int PR_DEQ = 4;          // dequantizing warps
-constexpr int PR_E = 16;           // tiles whose scales are kept: more than any role is ahead of another
+constexpr int PR_UN = 64;          // tokens of a unit: a softmax step, a dequantizing group's step
+constexpr int PR_DEQ = 4;          // dequantizing warps of a group
+constexpr int PR_GROUPS = 2;       // groups of them, taking units in turn
+constexpr int PR_E = 16;           // units whose scales are kept: more than any role is ahead of another
 constexpr uint32_t PR_BAR_DEQ = 1;
 
 template <int D, int NQT>
 struct PrCfg {
-  static constexpr int STAGES = D == 256 ? 2 : 3;
-  static constexpr int Q_TILE = 128 * D * 2, KV_TILE = PR_BN * D * 2;
+  static constexpr int BN = D == 256 ? 64 : 128, H = BN / PR_UN;  // tokens and units of a tile
+  static constexpr int NSB = NQT == 2 ? 1 : 2;                    // S buffers of a tile of rows
+  static constexpr int STAGES = D == 64 ? 3 : 2;
+  static constexpr int Q_TILE = 128 * D * 2, KV_TILE = BN * D * 2;
   static constexpr int SMEM_Q = NQT * Q_TILE;
   static constexpr int SMEM = 1024 + SMEM_Q + 2 * STAGES * KV_TILE;
-  static constexpr int THREADS = 32 * (4 * NQT + PR_DEQ + 1);
-  static constexpr int DEQ0 = 4 * NQT, MMA = DEQ0 + PR_DEQ;
-  static constexpr uint32_t O_COL = NQT * 2 * PR_BN;  // TMEM: NQT x 2 score buffers, then NQT x D sums
+  static constexpr int DEQ0 = 4 * NQT, MMA = DEQ0 + PR_GROUPS * PR_DEQ;
+  static constexpr int THREADS = 32 * (MMA + 4);
+  // TMEM: NQT x NSB score buffers, then NQT x D sums
+  static constexpr uint32_t O_COL = NQT * NSB * BN;
   static constexpr uint32_t COLS = O_COL + NQT * D <= 256 ? 256 : 512;
 };
+
+// Registers of NQT = 2: 640 threads x 96 at launch, shared out to softmax, dequantizing and MMA warpgroups
+// (256 x 104 + 256 x 104 + 128 x 64): the MMA warpgroup gives up what the others take.  NQT = 1 has enough.
+constexpr int PR_REG_SOFTMAX = 104, PR_REG_DEQ = 104, PR_REG_MMA = 64;
+static_assert(256 * PR_REG_SOFTMAX + 256 * PR_REG_DEQ + 128 * PR_REG_MMA <= 640 * 96 && PR_REG_SOFTMAX >= 96 && PR_REG_DEQ >= 96 &&
+                  PR_REG_MMA <= 96, "inc and dec from 96, within the registers of the launch");
 
 // Byte offset of 16-byte piece c (eight values) of row r in a tile of `rows` rows of D fp16: sub-tiles of 64
 // columns, 128-byte swizzle.
@@ -65,25 +78,27 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t bdes
       "r"(a), "l"(bdesc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32]) {
+__device__ __forceinline__ void tmem_st16_u(uint32_t taddr, const uint32_t (&v)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
       "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]),
-      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]),
-      "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]),
-      "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
       : "memory");
 }
 
 // floor(log2 |v|) of a finite v (subnormals: -127), v != 0.
 __device__ __forceinline__ int log2_floor(float v) { return (int)((__float_as_uint(v) >> 23) & 255) - 127; }
 
-// Two codes (integers in fp16) at 1024 + c.
+// The codes in the low nibbles of w's halves as fp16, by way of 1024 + c, and the next ones, of 64 + c.
 __device__ __forceinline__ uint32_t codes2(uint32_t w) {
   uint32_t r;
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"((w & 0x000f000fu) | 0x64006400u), "r"(0x64006400u));
+  return r;
+}
+__device__ __forceinline__ uint32_t codes2_hi(uint32_t w) {
+  uint32_t r;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"((w & 0x00f000f0u) | 0x54005400u), "r"(0x54005400u));
   return r;
 }
 __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
@@ -95,13 +110,14 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
 template <int D, int G, int NQT>
 __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(const __grid_constant__ AttnArgs a) {
   using C = PrCfg<D, NQT>;
-  constexpr int S = C::STAGES, NB = D / 32, NG = D / G, ROWS = 128 * NQT;
+  constexpr int S = C::STAGES, NB = D / 32, NG = D / G, ROWS = 128 * NQT, BN = C::BN, H = C::H, NSB = C::NSB;
   extern __shared__ uint8_t smem_pr[];
-  __shared__ uint64_t k_full[S], k_empty[S], v_full[S], v_empty[S], s_full[NQT][2], p_full[NQT][2], pv_done[NQT], drain_bar;
+  __shared__ uint64_t k_full[S], k_empty[S], v_full[S], v_empty[S], s_full[NQT][NSB], drain_bar;
+  __shared__ uint64_t p_full[NQT][2], pv_done[NQT][2];  // by the unit's parity
   __shared__ uint32_t tmem_slot, abort_word;
   __shared__ float e_k[PR_E];  // 2^ek
   __shared__ int e_v[PR_E];
-  __shared__ float deq_max[2][2][PR_DEQ];
+  __shared__ float deq_max[PR_GROUPS][2][2][PR_DEQ];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_pr) + 1023) & ~uintptr_t(1023));
   uint8_t* kbuf = smem + C::SMEM_Q;
   uint8_t* vbuf = kbuf + S * C::KV_TILE;
@@ -136,21 +152,21 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     }
     return;
   }
-  const int tiles = (hi - lo + PR_BN - 1) / PR_BN;
+  const int tiles = (hi - lo + BN - 1) / BN, units = tiles * H;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
-      mbar_init(&k_full[i], 32 * PR_DEQ);
-      mbar_init(&v_full[i], 32 * PR_DEQ);
+      mbar_init(&k_full[i], 32 * PR_DEQ * H);
+      mbar_init(&v_full[i], 32 * PR_DEQ * H);
       mbar_init(&k_empty[i], 1);
       mbar_init(&v_empty[i], 1);
     }
     for (int q = 0; q < NQT; ++q) {
-      mbar_init(&s_full[q][0], 1);
-      mbar_init(&s_full[q][1], 1);
-      mbar_init(&p_full[q][0], 128);
-      mbar_init(&p_full[q][1], 128);
-      mbar_init(&pv_done[q], 1);
+      for (int i = 0; i < NSB; ++i) mbar_init(&s_full[q][i], 1);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&p_full[q][i], 128);
+        mbar_init(&pv_done[q][i], 1);
+      }
     }
     mbar_init(&drain_bar, 1);
     *abort_flag = 0;
@@ -214,20 +230,23 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 
   // ------------------------------------------------------------------ dequantization
   if (warp >= C::DEQ0 && warp < C::MMA) {
-    const int dw = warp - C::DEQ0;
+    if constexpr (NQT == 2) setmaxnreg_inc<PR_REG_DEQ>();
+    const int grp = (warp - C::DEQ0) / PR_DEQ, dw = (warp - C::DEQ0) % PR_DEQ;
     const int tr = lane & 7, u = lane >> 3;  // token of eight, quarter of its row
     constexpr int WPT = NB;                  // 32-bit words of codes a thread takes of a row
     const int32_t* table = a.c.table + (int64_t)b * a.c.max_pages;
-    uint32_t kw[2][WPT], vw[2][WPT], kp[2][NG], vp[2][NG];
-    int page = -1;
-    auto look_up = [&](int it) {  // the page of this warp's 16 tokens of tile it
-      const int tok = lo + it * PR_BN + 16 * dw;
-      page = -1;
-      if (it < tiles && tok < hi) page = __ldg(table + page_of(a.c, (uint32_t)tok));
+    struct Raw {  // 16 tokens' codes and parameters, two tokens a thread
+      uint32_t kw[2][WPT], vw[2][WPT], kp[2][NG], vp[2][NG];
     };
-    auto fetch = [&](int it) {  // their codes and parameters; zeros past the end
-      const int tok = lo + it * PR_BN + 16 * dw;
-      const bool in = it < tiles && tok < hi;
+    int page = -1;
+    auto look_up = [&](int un) {  // the page of this warp's 16 tokens of unit un
+      const int tok = lo + un * PR_UN + 16 * dw;
+      page = -1;
+      if (un < units && tok < hi) page = __ldg(table + page_of(a.c, (uint32_t)tok));
+    };
+    auto fetch = [&](int un, Raw& x) {  // zeros past the end
+      const int tok = lo + un * PR_UN + 16 * dw;
+      const bool in = un < units && tok < hi;
       const bool good = in && page >= 0 && page < a.c.pages;
       if (in && !good && lane == 0) record_error(a.err, FGQ_ERR_ARG);
       const int slot = tok - (int)page_of(a.c, (uint32_t)tok) * a.c.page_size;
@@ -237,33 +256,36 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         const bool ok = good && tok + 8 * k + tr < hi;
         const int64_t row = row0 + 8 * k + tr;
 #pragma unroll
-        for (int i = 0; i < WPT; ++i) kw[k][i] = vw[k][i] = 0u;
+        for (int i = 0; i < WPT; ++i) x.kw[k][i] = x.vw[k][i] = 0u;
 #pragma unroll
-        for (int i = 0; i < NG; ++i) kp[k][i] = vp[k][i] = 0u;
+        for (int i = 0; i < NG; ++i) x.kp[k][i] = x.vp[k][i] = 0u;
         if (ok) {
-          lds_words<WPT>(a.c.k_codes + row * (D / 2) + u * 4 * WPT, kw[k]);
-          lds_words<WPT>(a.c.v_codes + row * (D / 2) + u * 4 * WPT, vw[k]);
-          lds_words<NG>(reinterpret_cast<const uint8_t*>(a.c.k_params + row * NG), kp[k]);
-          lds_words<NG>(reinterpret_cast<const uint8_t*>(a.c.v_params + row * NG), vp[k]);
+          lds_words<WPT>(a.c.k_codes + row * (D / 2) + u * 4 * WPT, x.kw[k]);
+          lds_words<WPT>(a.c.v_codes + row * (D / 2) + u * 4 * WPT, x.vw[k]);
+          lds_words<NG>(reinterpret_cast<const uint8_t*>(a.c.k_params + row * NG), x.kp[k]);
+          lds_words<NG>(reinterpret_cast<const uint8_t*>(a.c.v_params + row * NG), x.vp[k]);
         }
       }
     };
-    look_up(0);
-    fetch(0);
-    look_up(1);
+    Raw cur, nxt;
+    look_up(grp);
+    fetch(grp, cur);
+    look_up(grp + PR_GROUPS);
     int last_ev = -60;
     bool ok = true;
 #pragma unroll 1
-    for (int it = 0; it < tiles; ++it) {
-      const int st = it % S;
-      // the largest magnitude of the tile's keys and values, over the four warps
+    for (int un = grp; un < units; un += PR_GROUPS) {
+      const int it = un / H, st = it % S, par = (un / PR_GROUPS) & 1;
+      fetch(un + PR_GROUPS, nxt);  // in flight while this unit is converted
+      look_up(un + 2 * PR_GROUPS);
+      // the largest magnitude of the unit's keys and values, over the four warps
       float mk = 0.0f, mv = 0.0f;
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const float kl = __uint_as_float(kp[k][i] & 0xffff0000u), ks = __uint_as_float(kp[k][i] << 16);
-          const float vl = __uint_as_float(vp[k][i] & 0xffff0000u), vs = __uint_as_float(vp[k][i] << 16);
+          const float kl = __uint_as_float(cur.kp[k][i] & 0xffff0000u), ks = __uint_as_float(cur.kp[k][i] << 16);
+          const float vl = __uint_as_float(cur.vp[k][i] & 0xffff0000u), vs = __uint_as_float(cur.vp[k][i] << 16);
           mk = fmaxf(mk, fmaxf(fabsf(kl), fabsf(fmaf(15.0f, ks, kl))));
           mv = fmaxf(mv, fmaxf(fabsf(vl), fabsf(fmaf(15.0f, vs, vl))));
         }
@@ -273,128 +295,138 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         mv = fmaxf(mv, __shfl_xor_sync(FULL_MASK, mv, o));
       }
       if (lane == 0) {
-        deq_max[it & 1][0][dw] = mk;
-        deq_max[it & 1][1][dw] = mv;
+        deq_max[grp][par][0][dw] = mk;
+        deq_max[grp][par][1][dw] = mv;
       }
       ok = tmo != 0 && mbar_wait_warp(&k_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag) &&
            mbar_wait_warp(&v_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
       if (!ok && lane == 0 && !*abort_flag) fail();
-      if (named_bar_or(PR_BAR_DEQ, 32 * PR_DEQ, !ok)) break;
+      if (named_bar_or(PR_BAR_DEQ + grp, 32 * PR_DEQ, !ok)) break;
 #pragma unroll
       for (int i = 0; i < PR_DEQ; ++i) {
-        mk = fmaxf(mk, deq_max[it & 1][0][i]);
-        mv = fmaxf(mv, deq_max[it & 1][1][i]);
+        mk = fmaxf(mk, deq_max[grp][par][0][i]);
+        mv = fmaxf(mv, deq_max[grp][par][1][i]);
       }
       const int ek = mk > 0.0f ? min(114, max(-100, log2_floor(mk) - 13)) : 0;
       const int ev = mv > 0.0f ? min(114, max(-60, log2_floor(mv) - 13)) : last_ev;
       last_ev = ev;
-      if (threadIdx.x == 32 * C::DEQ0) {
-        e_k[it % PR_E] = pow2f(ek);
-        e_v[it % PR_E] = ev;
+      if (dw == 0 && lane == 0) {
+        e_k[un % PR_E] = pow2f(ek);
+        e_v[un % PR_E] = ev;
       }
       const float fk = pow2f(-ek), fv = pow2f(-ev);
       uint8_t* kt = kbuf + st * C::KV_TILE;
       uint8_t* vt = vbuf + st * C::KV_TILE;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int row = 16 * dw + 8 * k + tr;
+        const int row = un % H * PR_UN + 16 * dw + 8 * k + tr;
         uint32_t s2[NG], l2[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const float l = __uint_as_float(kp[k][i] & 0xffff0000u) * fk, s = __uint_as_float(kp[k][i] << 16) * fk;
+          const float l = __uint_as_float(cur.kp[k][i] & 0xffff0000u) * fk, s = __uint_as_float(cur.kp[k][i] << 16) * fk;
           s2[i] = h2(s, s);
           l2[i] = h2(l, l);
         }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {  // values 32 j + 8 u .. + 7
-          const uint32_t w = kw[k][j];
+          const uint32_t w = cur.kw[k][j];
           const int gi = j * 32 / G;
-          *reinterpret_cast<uint4*>(kt + tile_off(row, 4 * j + u, PR_BN)) =
-              make_uint4(hfma2(codes2(w), s2[gi], l2[gi]), hfma2(codes2(w >> 4), s2[gi], l2[gi]),
-                         hfma2(codes2(w >> 8), s2[gi], l2[gi]), hfma2(codes2(w >> 12), s2[gi], l2[gi]));
+          *reinterpret_cast<uint4*>(kt + tile_off(row, 4 * j + u, BN)) =
+              make_uint4(hfma2(codes2(w), s2[gi], l2[gi]), hfma2(codes2_hi(w), s2[gi], l2[gi]),
+                         hfma2(codes2(w >> 8), s2[gi], l2[gi]), hfma2(codes2_hi(w >> 8), s2[gi], l2[gi]));
         }
       }
       fence_proxy_async_smem();
       mbar_arrive(&k_full[st]);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const int row = 16 * dw + 8 * k + tr;
+        const int row = un % H * PR_UN + 16 * dw + 8 * k + tr;
         uint32_t s2[NG], l2[NG];
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const float l = __uint_as_float(vp[k][i] & 0xffff0000u) * fv, s = __uint_as_float(vp[k][i] << 16) * fv;
+          const float l = __uint_as_float(cur.vp[k][i] & 0xffff0000u) * fv, s = __uint_as_float(cur.vp[k][i] << 16) * fv;
           s2[i] = h2(s, s);
           l2[i] = h2(l, l);
         }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
           // 16-bit units (2 u, j) and (2 u + 1, j): NB / 2 words apart, in the half that j says
-          const uint32_t x = vw[k][j >> 1], y = vw[k][NB / 2 + (j >> 1)];
-          const uint32_t p = __byte_perm(x, y, (j & 1) ? 0x7632 : 0x5410);  // nibbles 0-3: values 0-3, 4-7: 4-7
-          const uint32_t q = p >> 16;
+          const uint32_t x = cur.vw[k][j >> 1], y = cur.vw[k][NB / 2 + (j >> 1)];
+          const uint32_t w = __byte_perm(x, y, (j & 1) ? 0x7632 : 0x5410);  // nibbles 0-3: values 0-3, 4-7: 4-7
           const int gi = j * 32 / G;
-          *reinterpret_cast<uint4*>(vt + tile_off(row, 4 * j + u, PR_BN)) =
-              make_uint4(hfma2(codes2((p & 15u) | p << 12), s2[gi], l2[gi]), hfma2(codes2((p >> 8 & 15u) | p << 4), s2[gi], l2[gi]),
-                         hfma2(codes2((q & 15u) | q << 12), s2[gi], l2[gi]), hfma2(codes2((q >> 8 & 15u) | q << 4), s2[gi], l2[gi]));
+          // columns in the order 0 4 1 5 2 6 3 7, as they come; the output puts them right
+          *reinterpret_cast<uint4*>(vt + tile_off(row, 4 * j + u, BN)) =
+              make_uint4(hfma2(codes2(w), s2[gi], l2[gi]), hfma2(codes2_hi(w), s2[gi], l2[gi]),
+                         hfma2(codes2(w >> 8), s2[gi], l2[gi]), hfma2(codes2_hi(w >> 8), s2[gi], l2[gi]));
         }
       }
       fence_proxy_async_smem();
       mbar_arrive(&v_full[st]);
-      fetch(it + 1);
-      look_up(it + 2);
+      cur = nxt;
     }
   }
 
   // ------------------------------------------------------------------ MMA issuer
+  if (warp >= C::MMA) {
+    if constexpr (NQT == 2) setmaxnreg_dec<PR_REG_MMA>();
+  }
   if (warp == C::MMA && lane == 0) {
-    constexpr uint32_t idesc_s = idesc_f16_f32(128, PR_BN);
+    constexpr uint32_t idesc_s = idesc_f16_f32(128, BN);
     constexpr uint32_t idesc_o = idesc_f16_f32(128, D) | 1u << 16;  // B is MN-major
-    bool ok = true;
-    auto scores = [&](int it) {  // S of tile it for every tile of rows
-      const int st = it % S;
-      if (!mbar_wait_timed(&k_full[st], (it / S) & 1, tmo, abort_flag, 0)) return false;
+    auto keys = [&](int it) {  // K of tile it is there
+      if (!mbar_wait_timed(&k_full[it % S], (it / S) & 1, tmo, abort_flag, 0)) return false;
       tc_fence_after();
-      const uint32_t kt = smem_u32(kbuf + st * C::KV_TILE);
-#pragma unroll
-      for (int q = 0; q < NQT; ++q) {
-        const uint32_t qt = smem_u32(smem + q * C::Q_TILE);
-        const uint32_t d = tmem + (uint32_t)((2 * q + (it & 1)) * PR_BN);
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k)
-          mma_f16(d, sdesc_k_sw128(qt + (k >> 2) * 128 * 128) + 2 * (k & 3),
-                  sdesc_k_sw128(kt + (k >> 2) * PR_BN * 128) + 2 * (k & 3), idesc_s, k > 0 ? 1u : 0u);
-        mma_commit(&s_full[q][it & 1]);
-      }
-      mma_commit(&k_empty[st]);
       return true;
     };
-    ok = scores(0);
+    auto scores = [&](int q, int it) {
+      const uint64_t qd = sdesc_k_sw128(smem_u32(smem + q * C::Q_TILE));
+      const uint64_t kd = sdesc_k_sw128(smem_u32(kbuf + it % S * C::KV_TILE));
+      const uint32_t d = tmem + (uint32_t)((q * NSB + it % NSB) * BN);
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k)
+        mma_f16(d, qd + (k >> 2) * (128 * 128 / 16) + 2 * (k & 3), kd + (k >> 2) * (BN * 128 / 16) + 2 * (k & 3), idesc_s,
+                k > 0 ? 1u : 0u);
+      mma_commit(&s_full[q][it % NSB]);
+      if (q == NQT - 1) mma_commit(&k_empty[it % S]);
+    };
+    bool ok = keys(0);
+    if (ok)
+      for (int q = 0; q < NQT; ++q) scores(q, 0);
     for (int it = 0; it < tiles && ok; ++it) {
-      // the next scores go first: their buffer's probabilities were consumed by the products issued before
-      if (it + 1 < tiles && !scores(it + 1)) {
+      // the next scores: into the other buffer before this tile's products (its probabilities went into the
+      // products before), or over this tile's once those are issued
+      const bool more = it + 1 < tiles;
+      if (more && !keys(it + 1)) {
         ok = false;
         break;
       }
-      const int st = it % S;
-      if (!mbar_wait_timed(&v_full[st], (it / S) & 1, tmo, abort_flag, 0)) {
+      if (NSB == 2 && more)
+        for (int q = 0; q < NQT; ++q) scores(q, it + 1);
+      if (!mbar_wait_timed(&v_full[it % S], (it / S) & 1, tmo, abort_flag, 0)) {
         ok = false;
         break;
       }
-      const uint32_t vt = smem_u32(vbuf + st * C::KV_TILE);
 #pragma unroll
-      for (int q = 0; q < NQT; ++q) {
-        if (!mbar_wait_timed(&p_full[q][it & 1], (it >> 1) & 1, tmo, abort_flag, 0)) {
-          ok = false;
-          break;
+      for (int q = 0; q < NQT && ok; ++q) {
+        const uint32_t o = tmem + C::O_COL + (uint32_t)(q * D);
+#pragma unroll
+        for (int h = 0; h < H; ++h) {
+          const int un = it * H + h;
+          if (!mbar_wait_timed(&p_full[q][un & 1], (un >> 1) & 1, tmo, abort_flag, 0)) {
+            ok = false;
+            break;
+          }
+          tc_fence_after();
+          const uint64_t vd = sdesc_mn_sw128(smem_u32(vbuf + it % S * C::KV_TILE + h * PR_UN * 128), BN * 128);
+          const uint32_t p = tmem + (uint32_t)((q * NSB + it % NSB) * BN + h * PR_UN);
+#pragma unroll
+          for (int k = 0; k < PR_UN / 16; ++k)
+            mma_f16_ts(o, p + 8 * k, vd + k * (2048 / 16), idesc_o, un > 0 || k > 0 ? 1u : 0u);
+          mma_commit(&pv_done[q][un & 1]);
         }
-        tc_fence_after();
-        const uint32_t p = tmem + (uint32_t)((2 * q + (it & 1)) * PR_BN), o = tmem + C::O_COL + (uint32_t)(q * D);
-#pragma unroll
-        for (int k = 0; k < PR_BN / 16; ++k)
-          mma_f16_ts(o, p + 8 * k, sdesc_mn_sw128(vt + k * 2048, PR_BN * 128), idesc_o, it > 0 || k > 0 ? 1u : 0u);
-        mma_commit(&pv_done[q]);
+        if (NSB == 1 && ok && more) scores(q, it + 1);
       }
-      if (ok) mma_commit(&v_empty[st]);
+      if (ok) mma_commit(&v_empty[it % S]);
     }
     if (!ok && !*abort_flag) fail();
     mma_commit(&drain_bar);
@@ -403,49 +435,80 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 
   // ------------------------------------------------------------------ softmax
   if (warp < C::DEQ0) {
+    if constexpr (NQT == 2) setmaxnreg_inc<PR_REG_SOFTMAX>();
     const int q = warp >> 2;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t ot = tmem + lanes + C::O_COL + (uint32_t)(q * D);
-    float top = AT_M0, ref = AT_M0, l = 0.0f;
+    float ref = AT_M0, l = 0.0f;
     bool ok = true;
 #pragma unroll 1
-    for (int it = 0; it < tiles; ++it) {
-      if (!mbar_wait_warp(&s_full[q][it & 1], (it >> 1) & 1, tmo, abort_flag)) {
+    for (int un = 0; un < units; ++un) {
+      const int it = un / H;
+      if (un % H == 0 && !mbar_wait_warp(&s_full[q][it % NSB], (it / NSB) & 1, tmo, abort_flag)) {
         ok = false;
         break;
       }
       tc_fence_after();
-      const uint32_t stile = tmem + lanes + (uint32_t)((2 * q + (it & 1)) * PR_BN);
+      const uint32_t stile = tmem + lanes + (uint32_t)((q * NSB + it % NSB) * BN + un % H * PR_UN);
       uint32_t x0[32], x1[32];
       tmem_ld32(stile, x0);
       tmem_ld32(stile + 32, x1);
       tmem_ld_wait_regs(x0);
       reg_fence(x1);
-      const float mk = fmaxf(mul * e_k[it % PR_E], 1e-37f);  // never 0: masked scores are -inf
-      const int ev = e_v[it % PR_E];
-      const int t0 = lo + it * PR_BN;
-      if (!__all_sync(FULL_MASK, t0 >= see_lo && t0 + PR_BN <= see_hi)) {
+      const float mk = fmaxf(mul * e_k[un % PR_E], 1e-37f);  // never 0: masked scores are -inf
+      const int ev = e_v[un % PR_E];
+      const int t0 = lo + un * PR_UN;
+      if (!__all_sync(FULL_MASK, t0 >= see_lo && t0 + PR_UN <= see_hi)) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
           if (t0 + i < see_lo || t0 + i >= see_hi) x0[i] = 0xff800000u;
           if (t0 + 32 + i < see_lo || t0 + 32 + i >= see_hi) x1[i] = 0xff800000u;
         }
       }
-      float h0 = __uint_as_float(x0[0]), h1 = __uint_as_float(x1[0]);
+      // on ref as it is, over the scores in TMEM (which this row keeps in registers); their sum
+      auto probabilities = [&]() {
+        const float off = (float)ev - ref;
+        const uint64_t mk2 = pack_f2(mk, mk), off2 = pack_f2(off, off);
+        uint64_t sum = 0;
 #pragma unroll
-      for (int i = 1; i < 32; ++i) {
-        h0 = fmaxf(h0, __uint_as_float(x0[i]));
-        h1 = fmaxf(h1, __uint_as_float(x1[i]));
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t(&x)[32] = half ? x1 : x0;
+          uint32_t p[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            float a0, a1;
+            unpack_f2(fma_f2(pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), mk2, off2), a0, a1);
+            a0 = ex2(a0);
+            a1 = ex2(a1);
+            sum = half + i == 0 ? pack_f2(a0, a1) : add_f2(sum, pack_f2(a0, a1));
+            p[i] = h2(a0, a1);
+          }
+          tmem_st16_u(stile + 16 * half, p);
+        }
+        float s0, s1;
+        unpack_f2(sum, s0, s1);
+        return s0 + s1;
+      };
+      float sum = probabilities();
+      // the products two units back are in (each phase is waited for in its turn: a later one could not be
+      // told from it by parity)
+      if (un > 1 && !mbar_wait_warp(&pv_done[q][un & 1], ((un >> 1) - 1) & 1, tmo, abort_flag)) {
+        ok = false;
+        break;
       }
-      h0 = fmaxf(h0, h1);
-      const float xt = h0 > -INFINITY ? fmaf(h0, mk, (float)ev) : AT_M0;
-      if (__any_sync(FULL_MASK, xt > top + 8.0f)) {
-        const float nt = fmaxf(top, xt), nr = nt - 6.0f, f = ex2(ref - nr);
-        top = nt;
+      if (__any_sync(FULL_MASK, !(sum <= 32768.0f))) {
+        float h0 = -INFINITY, h1 = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          h0 = fmaxf(h0, __uint_as_float(x0[i]));
+          h1 = fmaxf(h1, __uint_as_float(x1[i]));
+        }
+        h0 = fmaxf(h0, h1);
+        const float nr = h0 > -INFINITY ? fmaxf(ref, fmaf(h0, mk, (float)ev) - 6.0f) : ref, f = ex2(ref - nr);
         ref = nr;
         l *= f;
-        if (it > 0) {  // once the products so far are in
-          if (!mbar_wait_warp(&pv_done[q], (it - 1) & 1, tmo, abort_flag)) {
+        if (un > 0) {  // once the products so far are in
+          if (!mbar_wait_warp(&pv_done[q][(un - 1) & 1], ((un - 1) >> 1) & 1, tmo, abort_flag)) {
             ok = false;
             break;
           }
@@ -461,31 +524,15 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
             tmem_st16(ot + c, w);
           }
         }
+        sum = probabilities();
       }
-      const float off = (float)ev - ref;
-      float s0 = 0.0f, s1 = 0.0f;
-      uint32_t p[32];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float a0 = ex2(fmaf(__uint_as_float(x0[2 * i]), mk, off)), a1 = ex2(fmaf(__uint_as_float(x0[2 * i + 1]), mk, off));
-        const float b0 = ex2(fmaf(__uint_as_float(x1[2 * i]), mk, off)), b1 = ex2(fmaf(__uint_as_float(x1[2 * i + 1]), mk, off));
-        s0 += a0 + a1;
-        s1 += b0 + b1;
-        p[i] = h2(a0, a1);
-        p[16 + i] = h2(b0, b1);
-      }
-      l = fmaf(s0 + s1, pow2f(-ev), l);
-      // every phase of pv_done is waited for in its turn: a later one could not be told from it by parity
-      if (it > 0 && !mbar_wait_warp(&pv_done[q], (it - 1) & 1, tmo, abort_flag)) {
-        ok = false;
-        break;
-      }
-      tmem_st32(stile, p);
+      l = fmaf(sum, pow2f(-ev), l);
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(&p_full[q][it & 1]);
+      mbar_arrive(&p_full[q][un & 1]);
     }
-    if (ok && !mbar_wait_warp(&pv_done[q], (tiles - 1) & 1, tmo, abort_flag)) ok = false;
+    for (int un = units > 1 ? units - 2 : 0; un < units && ok; ++un)
+      ok = mbar_wait_warp(&pv_done[q][un & 1], (un >> 1) & 1, tmo, abort_flag);
     if (!ok && lane == 0 && !*abort_flag) fail();
     if (ok) {
       tc_fence_after();
@@ -507,7 +554,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         tmem_ld_wait_regs16(v);
         float w[2][8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) w[i >> 3][i & 7] = __uint_as_float(v[i]) * inv;
+        for (int i = 0; i < 16; ++i) w[i >> 3][(i & 7) >> 1 | (i & 1) << 2] = __uint_as_float(v[i]) * inv;  // 0 4 1 5 2 6 3 7
         if (r < a.rows) {
 #pragma unroll
           for (int i = 0; i < 2; ++i) {

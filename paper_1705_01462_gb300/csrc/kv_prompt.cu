@@ -14,9 +14,8 @@
 // Range.  Queries are scaled by a power of two per row; K and V by a power of two per unit (2^-ek,
 // 2^-ev) that brings their largest magnitude to [2^13, 2^14), so fp16 holds any bf16-ranged cache.  S is
 // multiplied by 2^ek; P takes 2^ev: p = 2^(x + ev - r) against V 2^-ev, and l sums p 2^-ev.  r is a row's
-// largest x + ev at its last move, less 6.  It moves only when the unit's probabilities, computed on the old r,
-// sum to more than 2^15, so that fp16 might not hold one: no maximum is taken otherwise, and O is rescaled
-// only then, after the products that add to it.
+// largest x + ev at its last move, less 6.  It moves only when exceeded by 8 (as in kv_attention.cuh), and only
+// then is O rescaled, after the products that add to it.
 // What is rounded: lo + s c, probabilities to fp16 (11 bits); sums and statistics are fp32.
 //
 // Warp roles (one block per SM): warps 0 .. 4 NQT - 1 softmax (TMEM lane = row); the next eight dequantize,
@@ -298,8 +297,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         deq_max[grp][par][0][dw] = mk;
         deq_max[grp][par][1][dw] = mv;
       }
-      ok = tmo != 0 && mbar_wait_warp(&k_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag) &&
-           mbar_wait_warp(&v_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
+      ok = ok && tmo != 0 && mbar_wait_warp(&k_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
       if (!ok && lane == 0 && !*abort_flag) fail();
       if (named_bar_or(PR_BAR_DEQ + grp, 32 * PR_DEQ, !ok)) break;
 #pragma unroll
@@ -338,8 +336,11 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       }
       fence_proxy_async_smem();
       mbar_arrive(&k_full[st]);
+      // a warp whose wait expires leaves with its group, at the next unit's barrier
+      ok = mbar_wait_warp(&v_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
+        if (!ok) break;
         const int row = un % H * PR_UN + 16 * dw + 8 * k + tr;
         uint32_t s2[NG], l2[NG];
 #pragma unroll
@@ -361,9 +362,10 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         }
       }
       fence_proxy_async_smem();
-      mbar_arrive(&v_full[st]);
+      if (ok) mbar_arrive(&v_full[st]);
       cur = nxt;
     }
+    if (!ok && lane == 0 && !*abort_flag) fail();
   }
 
   // ------------------------------------------------------------------ MMA issuer
@@ -396,12 +398,11 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       // the next scores: into the other buffer before this tile's products (its probabilities went into the
       // products before), or over this tile's once those are issued
       const bool more = it + 1 < tiles;
-      if (more && !keys(it + 1)) {
-        ok = false;
-        break;
-      }
-      if (NSB == 2 && more)
+      if (NSB == 2 && more) {
+        ok = keys(it + 1);
+        if (!ok) break;
         for (int q = 0; q < NQT; ++q) scores(q, it + 1);
+      }
       if (!mbar_wait_timed(&v_full[it % S], (it / S) & 1, tmo, abort_flag, 0)) {
         ok = false;
         break;
@@ -424,7 +425,10 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
             mma_f16_ts(o, p + 8 * k, vd + k * (2048 / 16), idesc_o, un > 0 || k > 0 ? 1u : 0u);
           mma_commit(&pv_done[q][un & 1]);
         }
-        if (NSB == 1 && ok && more) scores(q, it + 1);
+        if (NSB == 1 && ok && more) {
+          if (q == 0) ok = keys(it + 1);
+          if (ok) scores(q, it + 1);
+        }
       }
       if (ok) mma_commit(&v_empty[it % S]);
     }
@@ -465,46 +469,24 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           if (t0 + 32 + i < see_lo || t0 + 32 + i >= see_hi) x1[i] = 0xff800000u;
         }
       }
-      // on ref as it is, over the scores in TMEM (which this row keeps in registers); their sum
-      auto probabilities = [&]() {
-        const float off = (float)ev - ref;
-        const uint64_t mk2 = pack_f2(mk, mk), off2 = pack_f2(off, off);
-        uint64_t sum = 0;
+      float h0 = -INFINITY, h1 = -INFINITY, h2x = -INFINITY, h3 = -INFINITY;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const uint32_t(&x)[32] = half ? x1 : x0;
-          uint32_t p[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            float a0, a1;
-            unpack_f2(fma_f2(pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), mk2, off2), a0, a1);
-            a0 = ex2(a0);
-            a1 = ex2(a1);
-            sum = half + i == 0 ? pack_f2(a0, a1) : add_f2(sum, pack_f2(a0, a1));
-            p[i] = h2(a0, a1);
-          }
-          tmem_st16_u(stile + 16 * half, p);
-        }
-        float s0, s1;
-        unpack_f2(sum, s0, s1);
-        return s0 + s1;
-      };
-      float sum = probabilities();
+      for (int i = 0; i < 32; i += 4) {
+        h0 = fmaxf(h0, fmaxf(__uint_as_float(x0[i]), __uint_as_float(x1[i])));
+        h1 = fmaxf(h1, fmaxf(__uint_as_float(x0[i + 1]), __uint_as_float(x1[i + 1])));
+        h2x = fmaxf(h2x, fmaxf(__uint_as_float(x0[i + 2]), __uint_as_float(x1[i + 2])));
+        h3 = fmaxf(h3, fmaxf(__uint_as_float(x0[i + 3]), __uint_as_float(x1[i + 3])));
+      }
+      h0 = fmaxf(fmaxf(h0, h1), fmaxf(h2x, h3));
       // the products two units back are in (each phase is waited for in its turn: a later one could not be
       // told from it by parity)
       if (un > 1 && !mbar_wait_warp(&pv_done[q][un & 1], ((un >> 1) - 1) & 1, tmo, abort_flag)) {
         ok = false;
         break;
       }
-      if (__any_sync(FULL_MASK, !(sum <= 32768.0f))) {
-        float h0 = -INFINITY, h1 = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          h0 = fmaxf(h0, __uint_as_float(x0[i]));
-          h1 = fmaxf(h1, __uint_as_float(x1[i]));
-        }
-        h0 = fmaxf(h0, h1);
-        const float nr = h0 > -INFINITY ? fmaxf(ref, fmaf(h0, mk, (float)ev) - 6.0f) : ref, f = ex2(ref - nr);
+      const float xt = h0 > -INFINITY ? fmaf(h0, mk, (float)ev) : AT_M0;
+      if (__any_sync(FULL_MASK, xt > ref + 14.0f)) {
+        const float nr = fmaxf(ref, xt - 6.0f), f = ex2(ref - nr);
         ref = nr;
         l *= f;
         if (un > 0) {  // once the products so far are in
@@ -524,8 +506,29 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
             tmem_st16(ot + c, w);
           }
         }
-        sum = probabilities();
       }
+      const float off = (float)ev - ref;
+      const uint64_t mk2 = pack_f2(mk, mk), off2 = pack_f2(off, off);
+      uint64_t sum0 = 0, sum1 = 0;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t(&x)[32] = half ? x1 : x0;
+        uint32_t p[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          float a0, a1;
+          unpack_f2(fma_f2(pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), mk2, off2), a0, a1);
+          a0 = ex2(a0);
+          a1 = ex2(a1);
+          uint64_t& sum = i & 1 ? sum1 : sum0;
+          sum = add_f2(sum, pack_f2(a0, a1));
+          p[i] = h2(a0, a1);
+        }
+        tmem_st16_u(stile + 16 * half, p);
+      }
+      float s0, s1;
+      unpack_f2(add_f2(sum0, sum1), s0, s1);
+      const float sum = s0 + s1;
       l = fmaf(sum, pow2f(-ev), l);
       tmem_st_wait();
       tc_fence_before();

@@ -200,9 +200,13 @@ static cudaMemPool_t scratch_pool() {
 }
 
 int device_sms() {
+  static std::atomic<int> known[kMaxDevices];  // asked once per device
   int dev = 0, sms = 148;
   cudaGetDevice(&dev);
-  cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  const bool keep = dev >= 0 && dev < kMaxDevices;
+  if (keep && known[dev].load(std::memory_order_relaxed) > 0) return known[dev].load(std::memory_order_relaxed);
+  if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && keep)
+    known[dev].store(sms, std::memory_order_relaxed);
   return sms;
 }
 

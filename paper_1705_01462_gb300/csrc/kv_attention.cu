@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
       v += sv[i][d];
       l += sl[i];
     }
-    store_out(a, orow * D + d, l > 0.0f ? v / l : (l == 0.0f ? 0.0f : l));
+    store_out(a, orow * D + d, normalise(v, l));
   }
 }
 
@@ -91,16 +91,20 @@ fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_
   a.chunk = (int)chunk;
   a.chunks = (int)((span + chunk - 1) / chunk);
   if (units * a.chunks > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
+  // few chunks that all run at once join as a cluster: no temporary and no second launch.  More blocks than
+  // that would wait for eight of them to fit together.
+  a.cluster = k.clusters && a.chunks > 1 && a.chunks <= 8 && units * a.chunks <= slots;
+  const bool join = a.chunks > 1 && !a.cluster;
   void* tmp = nullptr;
   const int64_t orows = (int64_t)a.B * a.T * a.q_heads;
-  if (a.chunks > 1) {
+  if (join) {
     tmp = scratch_alloc((size_t)orows * a.chunks * (D + 2) * 4, s);
     if (!tmp) return FGQ_ERR_CUDA;
     a.part = static_cast<float*>(tmp);
     a.stats = a.part + (size_t)orows * a.chunks * D;
   }
   fgq_status st = k.launch(a, (unsigned)(units * a.chunks), s);
-  if (st == FGQ_OK && a.chunks > 1) {
+  if (st == FGQ_OK && join) {
     const dim3 grid((unsigned)orows), block(JOIN_THREADS);
     st = after_launch(D == 64    ? launch_pdl(join_kernel<64>, grid, block, 0, s, a, k.rows)
                       : D == 128 ? launch_pdl(join_kernel<128>, grid, block, 0, s, a, k.rows)

@@ -26,8 +26,8 @@
 //
 // Split.  A block of 4 warps takes `chunk` tokens of one (sequence, kv head, tile of 8 NT query rows);
 // each warp streams every fourth tile of 32 tokens through a ring of bulk copies of its own (no barrier
-// between warps), and the warps' sums are joined in shared memory.  Several chunks leave (r, l, sum) in
-// fp32, which a second kernel joins.
+// between warps), and the warps' sums are joined in shared memory.  Up to eight chunks of one wave are a
+// cluster, which joins through shared memory too; more leave (r, l, sum) in fp32, which a second kernel joins.
 #pragma once
 
 #include "decoder_internal.cuh"
@@ -49,6 +49,7 @@ struct AttnArgs {
   uint64_t timeout_ns;
   float scale_log2;  // scale * log2(e)
   int type, B, T, q_heads, group, rows, row_tiles, chunks, chunk, causal, window;
+  int cluster;  // the chunks of a tile are a cluster and join in shared memory
 };
 
 constexpr int AT_WARPS = 4;
@@ -182,6 +183,51 @@ __device__ __forceinline__ void visible(const AttnArgs& a, int n, int nq, int i0
   if (end <= first) first = end = 0;
 }
 
+// A row of the output; its value from a sum and a denominator (a row that saw nothing: 0; NaN stays).
+__device__ __forceinline__ int64_t out_row(const AttnArgs& a, int b, int head, int r) {
+  const int qi = r / a.group, h = r - qi * a.group;
+  return ((int64_t)b * a.T + qi) * a.q_heads + (int64_t)head * a.group + h;
+}
+__device__ __forceinline__ float normalise(float v, float l) { return l > 0.0f ? v / l : (l == 0.0f ? 0.0f : l); }
+
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+// A float at this block's shared address `p`, in the cluster's block `rank`.
+__device__ __forceinline__ float ld_cluster(const float* p, uint32_t rank) {
+  uint32_t at;
+  float v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// The rows of a cluster's blocks (chunks of one tile of rows), each block's sums at jo [row][D] and its r, l
+// at js [row][2], joined and stored: block `rank` takes every a.chunks-th run of 128 values.
+template <int NB, int NR>
+__device__ __forceinline__ void join_cluster(const AttnArgs& a, int b, int head, int r0, const float* jo,
+                                             const float* js, int rank) {
+  constexpr int D = 32 * NB;
+  for (int i = threadIdx.x + 32 * AT_WARPS * rank; i < NR * D; i += 32 * AT_WARPS * a.chunks) {
+    const int row = i / D, d = i % D, r = r0 + row;
+    if (r >= a.rows) break;
+    float m[8], mm = AT_M0, ll = 0.0f, v = 0.0f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      m[c] = c < a.chunks ? ld_cluster(js + 2 * row, c) : AT_M0;
+      mm = fmaxf(mm, m[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+      if (m[c] != AT_M0) {  // not a chunk without work: its sums were never written
+        const float f = ex2(m[c] - mm);
+        ll = fmaf(f, ld_cluster(js + 2 * row + 1, c), ll);
+        v = fmaf(f, ld_cluster(jo + row * D + d, c), v);
+      }
+    store_out(a, out_row(a, b, head, r) * D + d, normalise(v, ll));
+  }
+}
+
 // Blocks of one SM, by registers and shared memory.
 template <int NB, bool SPLIT, int NT>
 constexpr int attention_blocks_per_sm() {
@@ -203,12 +249,12 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int g = lane >> 2, t = lane & 3;
 
-  // block -> (sequence, kv head, tile of query rows, chunk); row tiles of one chunk are neighbours
+  // block -> (sequence, kv head, tile of query rows, chunk); a cluster is the chunks of one tile
   int id = blockIdx.x;
-  const int rt = id % a.row_tiles;
-  id /= a.row_tiles;
   const int ch = id % a.chunks;
   id /= a.chunks;
+  const int rt = id % a.row_tiles;
+  id /= a.row_tiles;
   const int head = id % a.c.kv_heads;
   const int b = id / a.c.kv_heads;
   const int r0 = rt * NR;
@@ -223,8 +269,15 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
   const int lo = lo64 < end ? (int)lo64 : end;
   const int hi = ch == a.chunks - 1 ? end : (int)min((int64_t)end, lo64 + a.chunk);
 
+  float* jo = reinterpret_cast<float*>(smem);  // [warp][row][D]: the warps' sums, over the ring
+  float* js = jo + AT_WARPS * NR * D;          // [warp][row][2]: r, l
   if (lo >= hi) {  // nothing here: zero output where there is one chunk only, else the join skips it
-    if (a.chunks == 1) {
+    if (a.cluster) {
+      if (threadIdx.x < NR) js[2 * threadIdx.x] = AT_M0;
+      cluster_sync();
+      join_cluster<NB, NR>(a, b, head, r0, jo, js, ch);
+      cluster_sync();
+    } else if (a.chunks == 1) {
       for (int i = threadIdx.x; i < NR * D; i += 32 * AT_WARPS) {
         const int r = r0 + i / D;
         if (r < a.rows) {
@@ -590,8 +643,6 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
 
   // join: each warp's rows to shared memory with its reference, over the ring (every copy has landed)
   __syncthreads();
-  float* jo = reinterpret_cast<float*>(smem);   // [warp][row][D]
-  float* js = jo + AT_WARPS * NR * D;           // [warp][row][2]: r, l
   {
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -619,6 +670,8 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
       }
   }
   __syncthreads();
+  // the block's rows: from all warps into the first one's place
+  float bm = AT_M0, bl = 0.0f;  // of row threadIdx.x
   for (int i = threadIdx.x; i < NR * D; i += 32 * AT_WARPS) {
     const int row = i / D, d = i % D, r = r0 + row;
     if (r >= a.rows) break;
@@ -631,10 +684,11 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
       ll = fmaf(f, js[(w * NR + row) * 2 + 1], ll);
       v = fmaf(f, jo[(w * NR + row) * D + d], v);
     }
-    const int qi = r / a.group, h = r - qi * a.group;
-    const int64_t orow = ((int64_t)b * a.T + qi) * a.q_heads + (int64_t)head * a.group + h;
-    if (a.chunks == 1) {
-      store_out(a, orow * D + d, ll > 0.0f ? v / ll : (ll == 0.0f ? 0.0f : ll));
+    const int64_t orow = out_row(a, b, head, r);
+    if (a.cluster) {
+      jo[row * D + d] = v;
+    } else if (a.chunks == 1) {
+      store_out(a, orow * D + d, normalise(v, ll));
     } else {
       a.part[(orow * a.chunks + ch) * D + d] = v;
       if (d == 0) {
@@ -643,11 +697,29 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
       }
     }
   }
+  if (a.cluster) {
+    if (threadIdx.x < NR) {
+#pragma unroll
+      for (int w = 0; w < AT_WARPS; ++w) bm = fmaxf(bm, js[(w * NR + threadIdx.x) * 2]);
+#pragma unroll
+      for (int w = 0; w < AT_WARPS; ++w)
+        bl = fmaf(ex2(js[(w * NR + threadIdx.x) * 2] - bm), js[(w * NR + threadIdx.x) * 2 + 1], bl);
+    }
+    __syncthreads();
+    if (threadIdx.x < NR) {
+      js[2 * threadIdx.x] = bm;
+      js[2 * threadIdx.x + 1] = bl;
+    }
+    cluster_sync();
+    join_cluster<NB, NR>(a, b, head, r0, jo, js, ch);
+    cluster_sync();  // no block leaves while another may read its sums
+  }
 }
 
 struct AttnKernel {
   fgq_status (*launch)(const AttnArgs&, unsigned blocks, cudaStream_t);
   int rows, per_sm;  // query rows of a block; blocks an SM holds
+  bool clusters;     // chunks may join as a cluster
 };
 
 // The kernel for head_dim = 32 nb, group = 32 gb, fp32 inputs (split) or not, `rows` query rows at hand.

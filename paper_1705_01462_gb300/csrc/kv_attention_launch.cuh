@@ -11,18 +11,32 @@ template <int NB, int GB, bool SPLIT, int NT>
 fgq_status launch_attention(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
   constexpr int bytes = AttnSmem<NB, GB>::template bytes<NT>();
   if (!tc::smem_attr_once<kv_attention_kernel<NB, GB, SPLIT, NT>>(bytes)) return FGQ_ERR_CUDA;
-  kv_attention_kernel<NB, GB, SPLIT, NT><<<blocks, 32 * AT_WARPS, bytes, s>>>(a);
-  return after_launch();
+  if (!a.cluster) {
+    kv_attention_kernel<NB, GB, SPLIT, NT><<<blocks, 32 * AT_WARPS, bytes, s>>>(a);
+    return after_launch();
+  }
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(32 * AT_WARPS);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)a.chunks;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return after_launch(cudaLaunchKernelEx(&cfg, kv_attention_kernel<NB, GB, SPLIT, NT>, a));
 }
 
 // fp32 inputs double the queries' and probabilities' operands, and 256-value heads the sums: both keep to 8 rows.
 template <int NB, int GB>
 AttnKernel pick(bool split, int rows) {
-  if (split) return {launch_attention<NB, GB, true, 1>, 8, attention_blocks_per_sm<NB, true, 1>()};
+  if (split) return {launch_attention<NB, GB, true, 1>, 8, attention_blocks_per_sm<NB, true, 1>(), true};
   if constexpr (NB <= 4) {
-    if (rows > 8) return {launch_attention<NB, GB, false, 2>, 16, attention_blocks_per_sm<NB, false, 2>()};
+    if (rows > 8) return {launch_attention<NB, GB, false, 2>, 16, attention_blocks_per_sm<NB, false, 2>(), true};
   }
-  return {launch_attention<NB, GB, false, 1>, 8, attention_blocks_per_sm<NB, false, 1>()};
+  return {launch_attention<NB, GB, false, 1>, 8, attention_blocks_per_sm<NB, false, 1>(), true};
 }
 
 }  // namespace dec

@@ -53,11 +53,14 @@ struct PrCfg {
   static constexpr uint32_t COLS = O_COL + NQT * D <= 256 ? 256 : 512;
 };
 
-// Registers of NQT = 2: 640 threads x 96 at launch, shared out to softmax, dequantizing and MMA warpgroups
-// (256 x 104 + 256 x 104 + 128 x 64): the MMA warpgroup gives up what the others take.  NQT = 1 has enough.
-constexpr int PR_REG_SOFTMAX = 104, PR_REG_DEQ = 104, PR_REG_MMA = 64;
-static_assert(256 * PR_REG_SOFTMAX + 256 * PR_REG_DEQ + 128 * PR_REG_MMA <= 640 * 96 && PR_REG_SOFTMAX >= 96 && PR_REG_DEQ >= 96 &&
-                  PR_REG_MMA <= 96, "inc and dec from 96, within the registers of the launch");
+// Registers a thread of the softmax, dequantizing and MMA warpgroups: the last gives up what the others take
+// over the launch's 96 (NQT = 2, 640 threads) or 128 (512).
+template <int NQT>
+struct PrRegs {
+  static constexpr int LAUNCH = NQT == 2 ? 96 : 128, SOFTMAX = NQT == 2 ? 104 : 128, DEQ = NQT == 2 ? 104 : 160, MMA = 64;
+  static_assert(128 * NQT * SOFTMAX + 256 * DEQ + 128 * MMA <= (128 * NQT + 384) * LAUNCH, "the launch's registers");
+  static_assert(SOFTMAX >= LAUNCH && DEQ >= LAUNCH && MMA <= LAUNCH, "inc, inc, dec");
+};
 
 // Byte offset of 16-byte piece c (eight values) of row r in a tile of `rows` rows of D fp16: sub-tiles of 64
 // columns, 128-byte swizzle.
@@ -125,10 +128,10 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   const uint64_t tmo = a.timeout_ns;
 
   int id = blockIdx.x;
-  const int rt = id % a.row_tiles;
-  id /= a.row_tiles;
   const int ch = id % a.chunks;
   id /= a.chunks;
+  const int rt = id % a.row_tiles;
+  id /= a.row_tiles;
   const int head = id % a.c.kv_heads;
   const int b = id / a.c.kv_heads;
   const int r0 = rt * ROWS;
@@ -229,7 +232,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 
   // ------------------------------------------------------------------ dequantization
   if (warp >= C::DEQ0 && warp < C::MMA) {
-    if constexpr (NQT == 2) setmaxnreg_inc<PR_REG_DEQ>();
+    setmaxnreg_inc<PrRegs<NQT>::DEQ>();
     const int grp = (warp - C::DEQ0) / PR_DEQ, dw = (warp - C::DEQ0) % PR_DEQ;
     const int tr = lane & 7, u = lane >> 3;  // token of eight, quarter of its row
     constexpr int WPT = NB;                  // 32-bit words of codes a thread takes of a row
@@ -369,9 +372,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   }
 
   // ------------------------------------------------------------------ MMA issuer
-  if (warp >= C::MMA) {
-    if constexpr (NQT == 2) setmaxnreg_dec<PR_REG_MMA>();
-  }
+  if (warp >= C::MMA) setmaxnreg_dec<PrRegs<NQT>::MMA>();
   if (warp == C::MMA && lane == 0) {
     constexpr uint32_t idesc_s = idesc_f16_f32(128, BN);
     constexpr uint32_t idesc_o = idesc_f16_f32(128, D) | 1u << 16;  // B is MN-major
@@ -439,7 +440,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 
   // ------------------------------------------------------------------ softmax
   if (warp < C::DEQ0) {
-    if constexpr (NQT == 2) setmaxnreg_inc<PR_REG_SOFTMAX>();
+    setmaxnreg_inc<PrRegs<NQT>::SOFTMAX>();
     const int q = warp >> 2;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t ot = tmem + lanes + C::O_COL + (uint32_t)(q * D);
@@ -540,9 +541,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     if (ok) {
       tc_fence_after();
       const int r = r0 + threadIdx.x;
-      const int rr = r < a.rows ? r : 0;
-      const int qi = rr / a.group, h = rr - qi * a.group;
-      const int64_t orow = ((int64_t)b * a.T + qi) * a.q_heads + (int64_t)head * a.group + h;
+      const int64_t orow = out_row(a, b, head, r < a.rows ? r : 0);
       const bool whole = a.chunks == 1;
       const float inv = !whole ? 1.0f : (l > 0.0f ? 1.0f / l : l);  // a row that sees nothing: 0; NaN stays
       float* part = whole ? nullptr : a.part + (orow * a.chunks + ch) * D;
@@ -594,9 +593,9 @@ fgq_status launch_prompt(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
 template <int D, int G>
 AttnKernel pick_prompt(int rows) {
   if constexpr (D <= 128) {
-    if (rows > 128) return {launch_prompt<D, G, 2>, 256, 1};
+    if (rows > 128) return {launch_prompt<D, G, 2>, 256, 1, false};
   }
-  return {launch_prompt<D, G, 1>, 128, 1};
+  return {launch_prompt<D, G, 1>, 128, 1, false};
 }
 
 }  // namespace

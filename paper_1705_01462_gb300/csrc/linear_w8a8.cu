@@ -4,6 +4,8 @@
 // products and sums exact in fp32 below 2^24, so both products run on fp16 matrix instructions (sm_103a's
 // integer tensor rate is far below): few tokens here, bound by the weights' bytes, and more in
 // gemm_w8a8.cu on tcgen05.
+#include <type_traits>
+
 #include "decoder_internal.cuh"
 #include "linear_internal.cuh"
 #include "kv_attention.cuh"  // mma16816
@@ -167,13 +169,16 @@ fgq_status launch_quantize_tokens(const void* x, int type, int P, int K, int64_t
 constexpr int FEW_WARPS = 8;
 
 struct FewArgs {
-  const int8_t* q;
+  const void* x;  // float tokens, ldx elements apart, or nullptr:
+  int64_t ldx;
+  const int8_t* q;  // int8 tokens and their scales
   const float* scale;
   const int8_t* wq;
   const float* wscale;
   const float* bias;
   void* y;
   int P, K, M, ytype;
+  unsigned int* err;
 };
 
 // Four int8 of w as two fp16 pairs.
@@ -215,34 +220,114 @@ __device__ __forceinline__ uint4 load16(const int8_t* row, int k, int K) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int NT, bool ALIGNED>
-__global__ void __launch_bounds__(32 * FEW_WARPS) few_tokens_kernel(const FewArgs a) {
+// The tokens' int8 codes in shared memory where the block quantizes them itself: rows a multiple of 16
+// bytes long and 64 off a multiple of 128, so that eight rows' pieces meet all banks.
+__host__ __device__ constexpr int few_row_bytes(int K) { return (K + 63) / 128 * 128 + 64; }
+
+// X: the type of float tokens that the block quantizes itself (a launch and a round trip less), or int8_t for
+// tokens quantized before.
+template <int NT, bool ALIGNED, typename X>
+__global__ void __launch_bounds__(32 * FEW_WARPS) few_tokens_kernel(const __grid_constant__ FewArgs a) {
+  constexpr bool FLOAT = !std::is_same<X, int8_t>::value;
+  constexpr int AHEAD = 2;  // pieces of 64 whose weights are loaded ahead
   __shared__ float sums[FEW_WARPS][8 * NT][17];
+  __shared__ float red[8 * NT][FEW_WARPS], tscale[8 * NT];
+  extern __shared__ __align__(16) uint8_t codes[];  // [8 NT][few_row_bytes(K)], FLOAT only
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int m0 = blockIdx.x * 16, p0 = blockIdx.y * 8 * NT;
+  const int np = min(8 * NT, a.P - p0);
   const int8_t* wa = a.wq + (int64_t)min(m0 + g, a.M - 1) * a.K;
   const int8_t* wb = a.wq + (int64_t)min(m0 + g + 8, a.M - 1) * a.K;
+  uint4 na[AHEAD], nb[AHEAD];
+  int kn = 64 * warp + 16 * t;  // the next piece to load
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i, kn += 64 * FEW_WARPS) {
+    na[i] = load16<ALIGNED>(wa, kn, a.K);
+    nb[i] = load16<ALIGNED>(wb, kn, a.K);
+  }
+  const int row_bytes = few_row_bytes(a.K);
+  if constexpr (FLOAT) {
+    const X* x = static_cast<const X*>(a.x) + (int64_t)p0 * a.ldx;
+    bool bad = false;
+    for (int p = 0; p < np; ++p) {
+      float mx = 0.0f;
+      for (int k = 8 * threadIdx.x; k < a.K; k += 8 * 32 * FEW_WARPS) {
+        float v[8];
+        load8(x + p * a.ldx + k, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          mx = fmaxf(mx, fabsf(v[i]));
+          if (nonfinite(v[i])) mx = INFINITY;  // the whole row, as the quantizer has it
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL_MASK, mx, o));
+      if (lane == 0) red[p][warp] = mx;
+    }
+    __syncthreads();
+    for (int p = 0; p < 8 * NT; ++p) {
+      float amax = 0.0f;
+      if (p < np) {
+#pragma unroll
+        for (int w = 0; w < FEW_WARPS; ++w) amax = fmaxf(amax, red[p][w]);
+      }
+      if (nonfinite(amax)) {
+        bad = true;
+        amax = 0.0f;
+      }
+      if (threadIdx.x == 0) tscale[p] = __fdiv_rn(amax, 127.0f);
+      const TokenScale ts = token_scale(amax);
+      for (int k = 8 * threadIdx.x; k < row_bytes; k += 8 * 32 * FEW_WARPS) {
+        uint32_t w[2] = {0u, 0u};
+        if (amax > 0.0f && k < a.K) {
+          float v[8];
+          load8(x + p * a.ldx + k, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)((int)token_code(v[i], ts) & 255) << (8 * (i & 3));
+        }
+        *reinterpret_cast<uint2*>(codes + p * row_bytes + k) = make_uint2(w[0], w[1]);
+      }
+    }
+    if (bad && threadIdx.x == 0) record_error(a.err, FGQ_ERR_NONFINITE);
+    __syncthreads();
+  }
   float acc[NT][4];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
-#pragma unroll 4
-  for (int k0 = 64 * warp; k0 < a.K; k0 += 64 * FEW_WARPS) {
-    const int k = k0 + 16 * t;
-    const uint4 va = load16<ALIGNED>(wa, k, a.K), vb = load16<ALIGNED>(wb, k, a.K);
+  auto piece = [&](int k, uint4 va, uint4 vb) {  // 16 bytes of this thread's rows from element k
     uint32_t ha[8], hb[8];
     s8_to_h2(va.x, ha[0], ha[1]), s8_to_h2(va.y, ha[2], ha[3]), s8_to_h2(va.z, ha[4], ha[5]), s8_to_h2(va.w, ha[6], ha[7]);
     s8_to_h2(vb.x, hb[0], hb[1]), s8_to_h2(vb.y, hb[2], hb[3]), s8_to_h2(vb.z, hb[4], hb[5]), s8_to_h2(vb.w, hb[6], hb[7]);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int p = p0 + 8 * nt + g;
-      const uint4 vx = p < a.P ? load16<ALIGNED>(a.q + (int64_t)p * a.K, k, a.K) : make_uint4(0u, 0u, 0u, 0u);
+      const int p = 8 * nt + g;
+      uint4 vx;
+      if constexpr (FLOAT)
+        vx = k < row_bytes ? *reinterpret_cast<const uint4*>(codes + p * row_bytes + k) : make_uint4(0u, 0u, 0u, 0u);
+      else
+        vx = p < np ? load16<ALIGNED>(a.q + (int64_t)(p0 + p) * a.K, k, a.K) : make_uint4(0u, 0u, 0u, 0u);
       uint32_t hx[8];
       s8_to_h2(vx.x, hx[0], hx[1]), s8_to_h2(vx.y, hx[2], hx[3]), s8_to_h2(vx.z, hx[4], hx[5]), s8_to_h2(vx.w, hx[6], hx[7]);
 #pragma unroll
       for (int s = 0; s < 4; ++s)
         mma16816(acc[nt], ha[2 * s], hb[2 * s], ha[2 * s + 1], hb[2 * s + 1], hx[2 * s], hx[2 * s + 1]);
+    }
+  };
+  for (int k0 = 64 * warp; k0 < a.K; k0 += 64 * FEW_WARPS * AHEAD) {
+    uint4 ca[AHEAD], cb[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i, kn += 64 * FEW_WARPS) {
+      ca[i] = na[i];
+      cb[i] = nb[i];
+      na[i] = load16<ALIGNED>(wa, kn, a.K);  // zeros past the end
+      nb[i] = load16<ALIGNED>(wb, kn, a.K);
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int k = k0 + 64 * FEW_WARPS * i;
+      if (k < a.K) piece(k + 16 * t, ca[i], cb[i]);  // the same for the whole warp
     }
   }
 #pragma unroll
@@ -256,26 +341,39 @@ __global__ void __launch_bounds__(32 * FEW_WARPS) few_tokens_kernel(const FewArg
     float v = 0.0f;
 #pragma unroll
     for (int w = 0; w < FEW_WARPS; ++w) v += sums[w][i >> 4][i & 15];
-    v = v * (__ldg(a.scale + p) * __ldg(a.wscale + m));
+    v = v * ((FLOAT ? tscale[i >> 4] : __ldg(a.scale + p)) * __ldg(a.wscale + m));
     if (a.bias) v += __ldg(a.bias + m);
     store_typed(a.y, a.ytype, (int64_t)p * a.M + m, v);
   }
 }
 
-template <int NT>
+template <int NT, typename X>
 fgq_status launch_few_nt(const FewArgs& a, cudaStream_t s) {
   const dim3 grid((unsigned)((a.M + 15) / 16), (unsigned)((a.P + 8 * NT - 1) / (8 * NT)));
-  if (a.K % 16 == 0 && aligned(a.q, 16) && aligned(a.wq, 16))
-    few_tokens_kernel<NT, true><<<grid, 32 * FEW_WARPS, 0, s>>>(a);
+  const int smem = std::is_same<X, int8_t>::value ? 0 : 8 * NT * few_row_bytes(a.K);
+  if (a.K % 16 == 0 && (a.x || aligned(a.q, 16)) && aligned(a.wq, 16))
+    few_tokens_kernel<NT, true, X><<<grid, 32 * FEW_WARPS, smem, s>>>(a);
   else
-    few_tokens_kernel<NT, false><<<grid, 32 * FEW_WARPS, 0, s>>>(a);
+    few_tokens_kernel<NT, false, X><<<grid, 32 * FEW_WARPS, smem, s>>>(a);
   return after_launch();
 }
 
 fgq_status launch_few(const FewArgs& a, cudaStream_t s) {
-  if (a.P <= 8) return launch_few_nt<1>(a, s);
-  if (a.P <= 16) return launch_few_nt<2>(a, s);
-  return launch_few_nt<4>(a, s);
+  if (a.P <= 8) return launch_few_nt<1, int8_t>(a, s);
+  if (a.P <= 16) return launch_few_nt<2, int8_t>(a, s);
+  return launch_few_nt<4, int8_t>(a, s);
+}
+
+// Float tokens that each block quantizes for itself: up to 8 of them while a block's share (every block has
+// all of it to do) stays small, 32 KB of codes, with rows that can be loaded eight elements at a time.
+constexpr int FUSED_MAX_P = 8, FUSED_MAX_CODES = 32768;
+bool fused_fits(const void* x, int type, int P, int K, int64_t ldx) {
+  return P <= FUSED_MAX_P && 8 * few_row_bytes(K) <= FUSED_MAX_CODES && K % 8 == 0 && aligned(x, 16) &&
+         (P == 1 || stride16(ldx, type));
+}
+fgq_status launch_few_float(const FewArgs& a, int type, cudaStream_t s) {
+  if (type == FGQ_F32) return launch_few_nt<1, float>(a, s);
+  return type == FGQ_BF16 ? launch_few_nt<1, __nv_bfloat16>(a, s) : launch_few_nt<1, __half>(a, s);
 }
 
 constexpr int FEW_MAX_P = 32;  // tokens up to which the few-token kernel runs
@@ -312,7 +410,7 @@ fgq_status fgq_gemm_w8a8(const int8_t* q, const float* scale, int P, int K, cons
   if (!scale) return FGQ_ERR_ARG;
   if (!dec::aligned(scale, 4)) return FGQ_ERR_ALIGN;
   if (P > FEW_MAX_P && K > 0) return launch_gemm_w8a8(q, nullptr, 0, scale, P, K, wq, wscale, M, bias, y, ytype, stream);
-  const FewArgs a = {q, scale, wq, wscale, bias, y, P, K, M, ytype};
+  const FewArgs a = {nullptr, 0, q, scale, wq, wscale, bias, y, P, K, M, ytype, nullptr};
   return launch_few(a, stream);
 }
 
@@ -322,6 +420,10 @@ fgq_status fgq_linear_w8a8(const void* x, fgq_float_type type, int P, int K, int
   if (st == FGQ_OK && P > 1 && ldx < K) st = FGQ_ERR_ARG;
   if (st != FGQ_OK || P == 0 || M == 0) return st;
   if (!dec::aligned(x, dec::float_bytes(type))) return FGQ_ERR_ALIGN;
+  if (fused_fits(x, type, P, K, ldx)) {
+    const FewArgs a = {x, ldx, nullptr, nullptr, wq, wscale, bias, y, P, K, M, type, device_error_word()};
+    return launch_few_float(a, type, stream);
+  }
   const bool few = P <= FEW_MAX_P || K == 0;
   const int64_t pitch = few ? K : gemm_w8a8_pitch(K);
   const size_t q_bytes = ((size_t)P * pitch * (few ? 1 : 2) + 255) / 256 * 256;
@@ -330,7 +432,7 @@ fgq_status fgq_linear_w8a8(const void* x, fgq_float_type type, int P, int K, int
   float* scale = reinterpret_cast<float*>(tmp + q_bytes);
   st = launch_quantize_tokens(x, type, P, K, ldx, tmp, pitch, !few, scale, stream);
   if (st == FGQ_OK && few) {
-    const FewArgs a = {reinterpret_cast<const int8_t*>(tmp), scale, wq, wscale, bias, y, P, K, M, type};
+    const FewArgs a = {nullptr, 0, reinterpret_cast<const int8_t*>(tmp), scale, wq, wscale, bias, y, P, K, M, type, nullptr};
     st = launch_few(a, stream);
   } else if (st == FGQ_OK) {
     st = launch_gemm_w8a8(nullptr, tmp, pitch, scale, P, K, wq, wscale, M, bias, y, type, stream);

@@ -532,18 +532,18 @@ class KVCache:
                  "_c", "_ref")
 
     def __init__(self, k_codes: torch.Tensor, k_params: torch.Tensor, v_codes: torch.Tensor, v_params: torch.Tensor):
-        if k_codes.dim() != 4 or k_params.dim() != 4 or k_params.shape[-1] == 0:
+        codes = _dev(k_codes, torch.uint8, "k_codes"), _dev(v_codes, torch.uint8, "v_codes")
+        params = _dev(k_params, torch.int32, "k_params"), _dev(v_params, torch.int32, "v_params")
+        c, p = k_codes.shape, k_params.shape
+        if len(c) != 4 or len(p) != 4 or p[3] == 0:
             raise ValueError("KVCache: codes and parameters are [pages][kv heads][page size][...]")
-        if k_codes.shape != v_codes.shape or k_params.shape != v_params.shape or \
-                k_codes.shape[:3] != k_params.shape[:3]:
+        if v_codes.shape != c or v_params.shape != p or c[:3] != p[:3]:
             raise ValueError("KVCache: the four tensors differ in pages, kv heads, page size or row length")
         self.k_codes, self.k_params, self.v_codes, self.v_params = k_codes, k_params, v_codes, v_params
-        self.pages, self.kv_heads, self.page_size, half = k_codes.shape
+        self.pages, self.kv_heads, self.page_size, half = c
         self.head_dim = 2 * half
-        self.group = self.head_dim // k_params.shape[3]
-        self._c = _KVCacheStruct(_dev(k_codes, torch.uint8, "k_codes"), _dev(k_params, torch.int32, "k_params"),
-                                 _dev(v_codes, torch.uint8, "v_codes"), _dev(v_params, torch.int32, "v_params"),
-                                 self.pages, self.page_size, self.kv_heads, self.head_dim, self.group)
+        self.group = self.head_dim // p[3]
+        self._c = _KVCacheStruct(codes[0], params[0], codes[1], params[1], c[0], c[2], c[1], 2 * half, self.group)
         self._ref = ctypes.addressof(self._c)
 
 
@@ -569,29 +569,34 @@ def _float_type(t: torch.Tensor, name: str) -> int:
 
 def _heads(t: torch.Tensor, heads: Optional[int], D: int, name: str) -> Tuple[int, int, int]:
     """(type, batch stride, token stride) of a [B][T][heads][D] tensor whose last two axes are contiguous."""
-    ty = _float_type(t, name)
-    if t.dim() != 4 or t.shape[3] != D or (heads is not None and t.shape[2] != heads):
-        raise ValueError(f"{name} must be [B][T][{heads or 'heads'}][{D}], got {tuple(t.shape)}")
+    ty = FLOAT_TYPES.get(t.dtype) if isinstance(t, torch.Tensor) and t.is_cuda else None
+    if ty is None:
+        ty = _float_type(t, name)
+    shape = t.shape
+    if len(shape) != 4 or shape[3] != D or (heads is not None and shape[2] != heads):
+        raise ValueError(f"{name} must be [B][T][{heads or 'heads'}][{D}], got {tuple(shape)}")
     sb, st, sh, sd = t.stride()
-    if (sd != 1 and D > 1) or (sh != D and t.shape[2] > 1):
+    if (sd != 1 and D > 1) or (sh != D and shape[2] > 1):
         raise ValueError(f"{name}: heads and head_dim must be contiguous")
     # an axis of one element may have any stride
-    return ty, sb if t.shape[0] > 1 else 0, st if t.shape[1] > 1 else 0
+    return ty, sb if shape[0] > 1 else 0, st if shape[1] > 1 else 0
 
 
 def _table(table: torch.Tensor, B: int) -> Tuple[int, int]:
     p = _dev(table, torch.int32, "page_table")
-    if table.dim() != 2 or table.shape[0] != B:
-        raise ValueError(f"page_table must be [{B}][max pages], got {tuple(table.shape)}")
-    return p, table.shape[1]
+    shape = table.shape
+    if len(shape) != 2 or shape[0] != B:
+        raise ValueError(f"page_table must be [{B}][max pages], got {tuple(shape)}")
+    return p, shape[1]
 
 
 def _per_sequence(t: Optional[torch.Tensor], B: int, name: str) -> Optional[int]:
     if t is None:
         return None
-    if isinstance(t, torch.Tensor) and t.numel() != B:
+    p = _dev(t, torch.int32, name)
+    if t.numel() != B:
         raise ValueError(f"{name} must have {B} entries, got {t.numel()}")
-    return _dev(t, torch.int32, name)
+    return p
 
 
 def fgq_kv_append(cache: KVCache, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, starts: torch.Tensor,
@@ -617,7 +622,8 @@ def fgq_kv_read(cache: KVCache, page_table: torch.Tensor, starts: torch.Tensor, 
     tp, mp = _table(page_table, B)
     if dtype not in FLOAT_TYPES:
         raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-    k, v = (torch.empty((B, T, cache.kv_heads, cache.head_dim), dtype=dtype, device=page_table.device) for _ in "kv")
+    # one allocation for both: each is contiguous
+    k, v = torch.empty((2, B, T, cache.kv_heads, cache.head_dim), dtype=dtype, device=page_table.device).unbind(0)
     _check(lib().fgq_kv_read(cache._ref, k.data_ptr(), v.data_ptr(), FLOAT_TYPES[dtype], B, T, tp, mp,
                              _per_sequence(starts, B, "starts"), _per_sequence(lens, B, "lens"), _stream(stream)),
            "fgq_kv_read")
@@ -634,7 +640,7 @@ def fgq_kv_attention(q: torch.Tensor, cache: KVCache, page_table: torch.Tensor, 
     B, T, heads, D = q.shape
     tp, mp = _table(page_table, B)
     if out is None:
-        out = torch.empty((B, T, heads, D), dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     elif out.shape != q.shape:
         raise ValueError(f"out must be {tuple(q.shape)}, got {tuple(out.shape)}")
     _check(lib().fgq_kv_attention(cache._ref, q.data_ptr(), ty, B, T, heads, qb, qt, tp, mp,

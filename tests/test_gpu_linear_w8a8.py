@@ -84,7 +84,7 @@ def test_largest_sums(P):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-@pytest.mark.parametrize("P,K,M", [(1, 4096, 64), (5, 77, 40), (31, 256, 100), (50, 1001, 130), (150, 768, 300)])
+@pytest.mark.parametrize("P,K,M", [(1, 4096, 64), (5, 77, 40), (3, 4096, 100), (8, 2048, 50), (31, 256, 100), (50, 1001, 130), (150, 768, 300)])
 def test_linear_is_its_two_calls(dtype, P, K, M):
     rng = np.random.default_rng(P * 3 + K)
     wq, ws, wt, st = weights(rng, M, K)

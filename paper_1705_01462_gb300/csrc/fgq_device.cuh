@@ -52,6 +52,11 @@ __device__ __forceinline__ unsigned long long add_f2(unsigned long long a, unsig
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+__device__ __forceinline__ unsigned long long mul_f2(unsigned long long a, unsigned long long b) {
+  unsigned long long r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
 __device__ __forceinline__ unsigned long long fma_f2(unsigned long long a, unsigned long long b,
                                                      unsigned long long c) {
   unsigned long long r;

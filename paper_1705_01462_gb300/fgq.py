@@ -622,8 +622,8 @@ def fgq_kv_read(cache: KVCache, page_table: torch.Tensor, starts: torch.Tensor, 
     tp, mp = _table(page_table, B)
     if dtype not in FLOAT_TYPES:
         raise TypeError(f"dtype must be float32, bfloat16 or float16, got {dtype}")
-    # one allocation for both: each is contiguous
-    k, v = torch.empty((2, B, T, cache.kv_heads, cache.head_dim), dtype=dtype, device=page_table.device).unbind(0)
+    k = torch.empty((B, T, cache.kv_heads, cache.head_dim), dtype=dtype, device=page_table.device)
+    v = torch.empty_like(k)
     _check(lib().fgq_kv_read(cache._ref, k.data_ptr(), v.data_ptr(), FLOAT_TYPES[dtype], B, T, tp, mp,
                              _per_sequence(starts, B, "starts"), _per_sequence(lens, B, "lens"), _stream(stream)),
            "fgq_kv_read")

@@ -7,21 +7,21 @@ namespace {
 
 using namespace dec;
 
-constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_THREADS = 512;
 constexpr uint64_t AT_TIMEOUT_NS = 1000000000ull;  // 1 s per wait
 
-// out[row] = sum_c 2^(m_c - m) part_c / sum_c 2^(m_c - m) l_c over the chunks that had work; one block per row,
-// JOIN_THREADS / D chunks at a time.
+// out[row] = sum_c 2^(r_c - r) part_c / sum_c 2^(r_c - r) l_c over the chunks that had work; one block per row,
+// JOIN_THREADS / D chunks at a time, each thread keeping the largest r so far (one pass, no load waits for
+// another).  What precedes the wait reads only what was there before the attention kernel.
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constant__ AttnArgs a, int tile_rows) {
-  constexpr int WAYS = JOIN_THREADS / D;
-  __shared__ float sv[WAYS][D], sl[WAYS], red[JOIN_THREADS / 32];
+  constexpr int WAYS = JOIN_THREADS / D, AHEAD = 8;
+  __shared__ float sv[WAYS][D], sr[WAYS], sl[WAYS];
   const int64_t orow = blockIdx.x;  // (b, query, head)
   const int hq = (int)(orow % a.q_heads);
   const int64_t bt = orow / a.q_heads;
   const int qi = (int)(bt % a.T), b = (int)(bt / a.T);
   const int tid = threadIdx.x, d = tid % D, way = tid / D;
-  pdl_wait();
   const int n = seq_len(a, b);
   const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
   const int r0 = (qi * a.group + hq % a.group) / tile_rows * tile_rows;  // the block's tile of query rows
@@ -29,31 +29,49 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
   visible(a, n, nq, r0 / a.group, (min(r0 + tile_rows, a.rows) - 1) / a.group, first, end);
   first &= ~15;
   const int chunks = (int)min((int64_t)a.chunks, ((int64_t)end - first + a.chunk - 1) / a.chunk);
-  const float* st = a.stats + orow * a.chunks * 2;
-  const float* part = a.part + orow * a.chunks * D;
-  float m = AT_M0;
-  for (int c = tid; c < chunks; c += JOIN_THREADS) m = fmaxf(m, st[2 * c]);
+  const float2* st = reinterpret_cast<const float2*>(a.stats) + orow * a.chunks;
+  const float* part = a.part + orow * a.chunks * D + d;
+  pdl_wait();
+  float r = AT_M0, v = 0.0f, l = 0.0f;
+  for (int c0 = way; c0 < chunks; c0 += WAYS * AHEAD) {
+    float2 s[AHEAD];
+    float x[AHEAD];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL_MASK, m, o));
-  if ((tid & 31) == 0) red[tid >> 5] = m;
-  __syncthreads();
+    for (int i = 0; i < AHEAD; ++i) {
+      const int c = c0 + i * WAYS;
+      s[i] = c < chunks ? st[c] : make_float2(AT_M0, 0.0f);
+      x[i] = c < chunks ? part[(int64_t)c * D] : 0.0f;
+    }
+    float top = r;
 #pragma unroll
-  for (int i = 0; i < JOIN_THREADS / 32; ++i) m = fmaxf(m, red[i]);
-  float v = 0.0f, l = 0.0f;
-#pragma unroll 8
-  for (int c = way; c < chunks; c += WAYS) {
-    const float f = ex2(st[2 * c] - m);
-    l = fmaf(f, st[2 * c + 1], l);
-    v = fmaf(f, part[(int64_t)c * D + d], v);
+    for (int i = 0; i < AHEAD; ++i) top = fmaxf(top, s[i].x);
+    const float f0 = ex2(r - top);
+    v *= f0;
+    l *= f0;
+    r = top;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const float f = ex2(s[i].x - r);
+      l = fmaf(f, s[i].y, l);
+      v = fmaf(f, x[i], v);
+    }
   }
   sv[way][d] = v;
-  if (d == 0) sl[way] = l;
+  if (d == 0) {
+    sr[way] = r;
+    sl[way] = l;
+  }
   __syncthreads();
   if (way == 0) {
+    float top = AT_M0;
 #pragma unroll
-    for (int i = 1; i < WAYS; ++i) {
-      v += sv[i][d];
-      l += sl[i];
+    for (int i = 0; i < WAYS; ++i) top = fmaxf(top, sr[i]);
+    v = l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < WAYS; ++i) {
+      const float f = ex2(sr[i] - top);
+      v = fmaf(f, sv[i][d], v);
+      l = fmaf(f, sl[i], l);
     }
     store_out(a, orow * D + d, normalise(v, l));
   }
@@ -81,7 +99,7 @@ fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_
   int64_t chunk = 0, best = INT64_MAX;
   for (int waves = 1; waves <= 8; ++waves) {
     const int64_t n = waves * slots / units > 0 ? waves * slots / units : 1;
-    const int64_t c = ((span + n - 1) / n + 127) / 128 * 128;
+    const int64_t r = (span + n - 1) / n, c = r > 512 ? (r + 255) / 256 * 256 : (r + 127) / 128 * 128;
     const int64_t blocks = units * ((span + c - 1) / c), cost = (blocks + slots - 1) / slots * (c + 256);
     if (cost < best) {
       best = cost;

@@ -25,7 +25,7 @@
 // value scale sigma: the common tile needs one vote instead of a reduction per row.
 //
 // Split.  A block of 4 warps takes `chunk` tokens of one (sequence, kv head, tile of 8 NT query rows);
-// each warp streams every fourth tile of 32 tokens through a ring of bulk copies of its own (no barrier
+// each warp streams every fourth tile through a ring of bulk copies of its own (no barrier
 // between warps), and the warps' sums are joined in shared memory.  Up to eight chunks of one wave are a
 // cluster, which joins through shared memory too; more leave (r, l, sum) in fp32, which a second kernel joins.
 #pragma once
@@ -53,20 +53,18 @@ struct AttnArgs {
 };
 
 constexpr int AT_WARPS = 4;
-constexpr int AT_TILE = 32;  // tokens a warp takes at a time
+constexpr int AT_STEP = 32;  // tokens a warp computes at a time
 constexpr float AT_M0 = -1e30f;
 
-template <int NB>
-struct AttnRing {
-  static constexpr int STAGES = NB == 8 ? 2 : (NB == 4 ? 3 : 4);
-};
-
-// Shared memory of one ring stage: 32 rows of key codes, value codes, key and value parameters.
+// Shared memory of one ring stage: TILE rows of key codes, value codes, key and value parameters.  Tiles of 64
+// tokens where they fit: bulk copies are the fewer and the larger for it (524 k copies of 1 KB and 128 bytes
+// took as long as 300 MB from HBM).
 template <int NB, int GB>
 struct AttnSmem {
-  static constexpr int D = 32 * NB, NG = NB / GB, STAGES = AttnRing<NB>::STAGES;
+  static constexpr int D = 32 * NB, NG = NB / GB;
+  static constexpr int TILE = NB == 8 ? 32 : 64, STAGES = NB == 2 ? 3 : 2;
   static constexpr int ROW = D / 2, PAR = 4 * NG;
-  static constexpr int STAGE = AT_TILE * 2 * (ROW + PAR);
+  static constexpr int STAGE = TILE * 2 * (ROW + PAR);
   static constexpr int RING = AT_WARPS * STAGES * STAGE;
   static constexpr int BARS = AT_WARPS * STAGES * 8;
   template <int NT>
@@ -137,16 +135,28 @@ __device__ __forceinline__ void lds_words(const uint8_t* p, uint32_t (&w)[N]) {
   }
 }
 
-// Query row r = i * group + h of (b, kv head): its q elements 8 e .. 8 e + 7 as fp32.
-template <int NB>
-__device__ __forceinline__ void load_q8(const AttnArgs& a, int64_t base, int e, float (&x)[8]) {
-  if (a.type == FGQ_F32)
-    load8(static_cast<const float*>(a.q) + base + 8 * e, x);
-  else if (a.type == FGQ_BF16)
-    load8(static_cast<const __nv_bfloat16*>(a.q) + base + 8 * e, x);
-  else
-    load8(static_cast<const __half*>(a.q) + base + 8 * e, x);
-}
+// Eight query elements 8 e .. 8 e + 7 from element `base` on, as loaded (F32: 32 bytes, else 16) and as fp32.
+template <bool F32>
+struct RawQ {
+  uint4 v[F32 ? 2 : 1];
+  __device__ __forceinline__ void load(const AttnArgs& a, int64_t base, int e) {
+    const uint4* p = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(a.q) + (base + 8 * e) * (F32 ? 4 : 2));
+    v[0] = __ldg(p);
+    if (F32) v[F32 ? 1 : 0] = __ldg(p + 1);
+  }
+  __device__ __forceinline__ void zero() { v[0] = v[F32 ? 1 : 0] = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ __forceinline__ void unpack(const AttnArgs& a, float (&x)[8]) const {
+    if constexpr (F32) {
+      const uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(w[i]);
+    } else if (a.type == FGQ_BF16) {
+      unpack8(v[0], x, __nv_bfloat16());
+    } else {
+      unpack8(v[0], x, __half());
+    }
+  }
+};
 
 __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t at, float v) {
   if (a.type == FGQ_F32)
@@ -231,14 +241,14 @@ __device__ __forceinline__ void join_cluster(const AttnArgs& a, int b, int head,
 // Blocks of one SM, by registers and shared memory.
 template <int NB, bool SPLIT, int NT>
 constexpr int attention_blocks_per_sm() {
-  return NB == 8 ? 2 : (NT == 2 || SPLIT ? 3 : 4);
+  return NB == 8 ? 2 : 3;
 }
 
 template <int NB, int GB, bool SPLIT, int NT>
 __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPLIT, NT>())
     kv_attention_kernel(const __grid_constant__ AttnArgs a) {
   using S = AttnSmem<NB, GB>;
-  constexpr int D = S::D, NG = S::NG, ROW = S::ROW, PAR = S::PAR, STAGES = S::STAGES;
+  constexpr int D = S::D, NG = S::NG, ROW = S::ROW, PAR = S::PAR, STAGES = S::STAGES, TILE = S::TILE;
   constexpr int NQ = SPLIT ? 2 : 1;  // fp16 parts of a query and of a probability
   constexpr int NR = 8 * NT;         // query rows of the block
   extern __shared__ __align__(128) uint8_t smem[];
@@ -258,6 +268,19 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
   const int head = id % a.c.kv_heads;
   const int b = id / a.c.kv_heads;
   const int r0 = rt * NR;
+
+  // the queries are on their way before the cache is: behind its first tiles they took four microseconds
+  RawQ<SPLIT> qraw[NT][NB];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = r0 + 8 * nt + g, qi = r / a.group;
+    const int64_t base = (int64_t)b * a.qbs + (int64_t)qi * a.qts + ((int64_t)head * a.group + (r - qi * a.group)) * D;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      qraw[nt][j].zero();
+      if (r < a.rows) qraw[nt][j].load(a, base, 4 * j + t);
+    }
+  }
 
   const int n = seq_len(a, b);
   const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
@@ -289,6 +312,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
     return;
   }
 
+  pdl_trigger();  // the join may be brought up; it waits for this kernel's end
   if (threadIdx.x == 0) {
     for (int i = 0; i < AT_WARPS * STAGES; ++i) mbar_init(&bars[i], 1);
     *abort_flag = 0;
@@ -298,39 +322,46 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
 
   uint8_t* ring = smem + warp * STAGES * S::STAGE;
   uint64_t* bar = bars + warp * STAGES;
-  const int tiles_all = (hi - lo + AT_TILE - 1) / AT_TILE;
+  const int tiles_all = (hi - lo + TILE - 1) / TILE;
   const int tiles = (tiles_all - warp + AT_WARPS - 1) / AT_WARPS;  // this warp's
 
-  // lanes 0-7 copy: half (16 tokens) lane / 4, array lane % 4 (key codes, value codes, key, value parameters)
+  // lanes 4 k + array copy (key codes, value codes, key, value parameters) from 16-token block k of the tile on,
+  // where that is the tile's first or its page's: as many blocks as lie in the page
+  constexpr int BLOCKS = TILE / 16;
   const bool par = lane & 2, val = lane & 1;
+  const int blk = lane >> 2;
   const uint32_t row_bytes = par ? PAR : ROW;
   const uint8_t* src = par ? reinterpret_cast<const uint8_t*>(val ? a.c.v_params : a.c.k_params)
                            : (val ? a.c.v_codes : a.c.k_codes);
-  const uint32_t dst = smem_u32(ring) + (par ? 2 * AT_TILE * ROW + (val ? AT_TILE * PAR : 0) : (val ? AT_TILE * ROW : 0)) +
-                       ((lane >> 2) & 1) * 16 * row_bytes;
+  const uint32_t dst = smem_u32(ring) + (par ? 2 * TILE * ROW + (val ? TILE * PAR : 0) : (val ? TILE * ROW : 0)) +
+                       blk * 16 * row_bytes;
   const int32_t* table = a.c.table + (int64_t)b * a.c.max_pages;
-  int ptok = lo + warp * AT_TILE + 16 * ((lane >> 2) & 1);  // this lane's next token to look up
-  int page = -1, slot = 0;  // of its half of the next tile to issue, where that begins before hi (want)
-  bool want = false;
+  int ptok = lo + warp * TILE + 16 * blk;  // this lane's block of the next tile to look up
+  int page = -1, slot = 0, run = 0;        // of the next tile to issue: page, slot, tokens to copy
   auto look_up = [&]() {  // positions below hi are inside the table: seq_len() sees to it
-    want = lane < 8 && ptok < hi;
-    if (want) {
+    run = 0;
+    if (blk < BLOCKS && ptok < hi) {
       const uint32_t pi = page_of(a.c, (uint32_t)ptok);
       slot = ptok - (int)pi * a.c.page_size;
-      page = __ldg(table + pi);
+      if (blk == 0 || slot == 0) {
+        page = __ldg(table + pi);
+        run = min(min(TILE - 16 * blk, a.c.page_size - slot), (hi - ptok + 15) & ~15);
+      }
     }
-    ptok += AT_WARPS * AT_TILE;
+    ptok += AT_WARPS * TILE;
   };
   int ist = 0;  // stage of the next tile to issue
   auto issue = [&]() {
-    const bool good = want && page >= 0 && page < a.c.pages;
-    if (want && !good) record_error(a.err, FGQ_ERR_ARG);
-    const uint32_t ok = __ballot_sync(FULL_MASK, good) & 0x11u;  // a lane of each half
-    if (lane == 0) mbar_arrive_expect_tx(&bar[ist], (uint32_t)__popc(ok) * 16u * 2u * (ROW + PAR));
+    if (run > 0 && (page < 0 || page >= a.c.pages)) {
+      record_error(a.err, FGQ_ERR_ARG);
+      run = 0;
+    }
+    const uint32_t tokens = __reduce_add_sync(FULL_MASK, (lane & 3) == 0 ? (uint32_t)run : 0u);
+    if (lane == 0) mbar_arrive_expect_tx(&bar[ist], tokens * 2u * (ROW + PAR));
     __syncwarp();
-    if (good)
+    if (run > 0)
       bulk_load(dst + ist * S::STAGE, src + (((int64_t)page * a.c.kv_heads + head) * a.c.page_size + slot) * row_bytes,
-                16u * row_bytes, &bar[ist]);
+                (uint32_t)run * row_bytes, &bar[ist]);
     ist = ist + 1 == STAGES ? 0 : ist + 1;
   };
   look_up();
@@ -350,17 +381,12 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
   for (int nt = 0; nt < NT; ++nt) {
     const int r = r0 + 8 * nt + g;
     const bool live = r < a.rows;
-    const int qi = live ? r / a.group : 0, h = live ? r - qi * a.group : 0;
-    const int64_t base = (int64_t)b * a.qbs + (int64_t)qi * a.qts + ((int64_t)head * a.group + h) * D;
+    const int qi = live ? r / a.group : 0;
     float x[NB][8];
     float mx = 0.0f;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-      if (live)
-        load_q8<NB>(a, base, 4 * j + t, x[j]);
-      else
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[j][i] = 0.0f;
+      qraw[nt][j].unpack(a, x[j]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[j][i]));
     }
@@ -446,19 +472,23 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
   float sigma = 8.6736174e-19f;  // 2^-60; a power of two at or above every value scale met so far
 
   bool ok = true;
-  int done = 0, tok0 = lo + warp * AT_TILE, st = 0;
+  int done = 0, tile0 = lo + warp * TILE, st = 0;
   uint32_t phase = 0;
 #pragma unroll 1
-  for (; done < tiles; ++done, tok0 += AT_WARPS * AT_TILE) {
+  for (; done < tiles; ++done, tile0 += AT_WARPS * TILE) {
     // a limit of 0 (a test's) expires at once, whether the copy has landed or not
     if (a.timeout_ns == 0 || !mbar_wait_warp(&bar[st], phase, a.timeout_ns, abort_flag)) {
       ok = false;
       break;
     }
-    const uint8_t* kc = ring + st * S::STAGE;
-    const uint8_t* vc = kc + AT_TILE * ROW;
-    const uint32_t* kp = reinterpret_cast<const uint32_t*>(vc + AT_TILE * ROW);
-    const uint32_t* vp = kp + AT_TILE * NG;
+#pragma unroll 1
+    for (int step = 0; step < TILE; step += AT_STEP) {
+    const int tok0 = tile0 + step;
+    if (TILE > AT_STEP && tok0 >= hi) break;
+    const uint8_t* kc = ring + st * S::STAGE + step * ROW;
+    const uint8_t* vc = kc + TILE * ROW;
+    const uint32_t* kp = reinterpret_cast<const uint32_t*>(ring + st * S::STAGE + 2 * TILE * ROW) + step * NG;
+    const uint32_t* vp = kp + TILE * NG;
 
     // scores of tokens 16 mt + g, + 8 for rows 8 nt + 2 t, + 1
     float x[2][NT][4];
@@ -506,7 +536,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
         }
       }
     }
-    const bool whole = tok0 >= all_lo && tok0 + AT_TILE <= all_hi;
+    const bool whole = tok0 >= all_lo && tok0 + AT_STEP <= all_hi;
     if (!whole) {
 #pragma unroll
       for (int mt = 0; mt < 2; ++mt)
@@ -622,6 +652,8 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
               mma16816(o[nt][j][w], a0, a1, a2, a3, pf[nt][j / GB][p][0], pf[nt][j / GB][p][1]);
         }
       }
+    }
+
     }
 
     __syncwarp();  // every lane has read the stage

@@ -156,6 +156,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   }
   const int tiles = (hi - lo + BN - 1) / BN, units = tiles * H;
 
+  pdl_trigger();  // the join may be brought up; it waits for this kernel's end
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init(&k_full[i], 32 * PR_DEQ * H);
@@ -192,7 +193,9 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 #pragma unroll 4
       for (int c = 0; c < D / 8; ++c) {
         float x[8];
-        load_q8<NB>(a, base, c, x);
+        RawQ<false> raw;
+        raw.load(a, base, c);
+        raw.unpack(a, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[i]));
       }
@@ -202,8 +205,11 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     uint8_t* qt = smem + (row >> 7) * C::Q_TILE;
 #pragma unroll 4
     for (int c = 0; c < D / 8; ++c) {
-      float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (live) load_q8<NB>(a, base, c, x);
+      float x[8];
+      RawQ<false> raw;
+      raw.zero();
+      if (live) raw.load(a, base, c);
+      raw.unpack(a, x);
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] *= up;
       store8(reinterpret_cast<__half*>(qt + tile_off(row & 127, c, 128)), x);

@@ -109,6 +109,48 @@ __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
   return r;
 }
 
+// N consecutive words of global memory, aligned as they come together (8 or 16 bytes at most).
+template <int N>
+__device__ __forceinline__ void ldg_words(const void* p, uint32_t (&w)[N]) {
+  if constexpr (N == 1) {
+    w[0] = __ldg(static_cast<const uint32_t*>(p));
+  } else if constexpr (N == 2) {
+    const uint2 v = __ldg(static_cast<const uint2*>(p));
+    w[0] = v.x, w[1] = v.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+      const uint4 v = __ldg(static_cast<const uint4*>(p) + i / 4);
+      w[i] = v.x, w[i + 1] = v.y, w[i + 2] = v.z, w[i + 3] = v.w;
+    }
+  }
+}
+
+// A thread's NB pieces of eight values (piece 4 j + u of row `row`) from codes `w` to fp16 in a tile of BN rows.
+template <int NB, int NG, int BN>
+__device__ __forceinline__ void convert_row(uint32_t tile, int row, int u, const uint32_t (&w)[NB], const uint32_t (&par)[NG],
+                                            float f) {
+  uint32_t s2[NG], l2[NG];
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    const float l = __uint_as_float(par[i] & 0xffff0000u) * f, s = __uint_as_float(par[i] << 16) * f;
+    s2[i] = h2(s, s);
+    l2[i] = h2(l, l);
+  }
+  const uint32_t at = tile + (uint32_t)((row >> 3) * 1024 + (row & 7) * 128);
+  const uint32_t sw[2] = {at + (uint32_t)((u ^ (row & 7)) << 4), at + (uint32_t)(((4 + u) ^ (row & 7)) << 4)};
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int gi = j * NG / NB;
+    const uint32_t x = w[j], y = w[j] >> 8;
+    const uint32_t a = hfma2(codes2(x), s2[gi], l2[gi]), b = hfma2(codes2_hi(x), s2[gi], l2[gi]);
+    const uint32_t c = hfma2(codes2(y), s2[gi], l2[gi]), d = hfma2(codes2_hi(y), s2[gi], l2[gi]);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(sw[j & 1] + (uint32_t)((j >> 1) * BN * 128)), "r"(a),
+                 "r"(b), "r"(c), "r"(d)
+                 : "memory");
+  }
+}
+
 template <int D, int G, int NQT>
 __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(const __grid_constant__ AttnArgs a) {
   using C = PrCfg<D, NQT>;
@@ -159,15 +201,15 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   pdl_trigger();  // the join may be brought up; it waits for this kernel's end
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
-      mbar_init(&k_full[i], 32 * PR_DEQ * H);
-      mbar_init(&v_full[i], 32 * PR_DEQ * H);
+      mbar_init(&k_full[i], PR_DEQ * H);
+      mbar_init(&v_full[i], PR_DEQ * H);
       mbar_init(&k_empty[i], 1);
       mbar_init(&v_empty[i], 1);
     }
     for (int q = 0; q < NQT; ++q) {
       for (int i = 0; i < NSB; ++i) mbar_init(&s_full[q][i], 1);
       for (int i = 0; i < 2; ++i) {
-        mbar_init(&p_full[q][i], 128);
+        mbar_init(&p_full[q][i], 4);
         mbar_init(&pv_done[q][i], 1);
       }
     }
@@ -268,10 +310,10 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 #pragma unroll
         for (int i = 0; i < NG; ++i) x.kp[k][i] = x.vp[k][i] = 0u;
         if (ok) {
-          lds_words<WPT>(a.c.k_codes + row * (D / 2) + u * 4 * WPT, x.kw[k]);
-          lds_words<WPT>(a.c.v_codes + row * (D / 2) + u * 4 * WPT, x.vw[k]);
-          lds_words<NG>(reinterpret_cast<const uint8_t*>(a.c.k_params + row * NG), x.kp[k]);
-          lds_words<NG>(reinterpret_cast<const uint8_t*>(a.c.v_params + row * NG), x.vp[k]);
+          ldg_words<WPT>(a.c.k_codes + row * (D / 2) + u * 4 * WPT, x.kw[k]);
+          ldg_words<WPT>(a.c.v_codes + row * (D / 2) + u * 4 * WPT, x.vw[k]);
+          ldg_words<NG>(a.c.k_params + row * NG, x.kp[k]);
+          ldg_words<NG>(a.c.v_params + row * NG, x.vp[k]);
         }
       }
     };
@@ -322,56 +364,30 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         e_v[un % PR_E] = ev;
       }
       const float fk = pow2f(-ek), fv = pow2f(-ev);
-      uint8_t* kt = kbuf + st * C::KV_TILE;
-      uint8_t* vt = vbuf + st * C::KV_TILE;
+      const uint32_t kt = smem_u32(kbuf + st * C::KV_TILE), vt = smem_u32(vbuf + st * C::KV_TILE);
+      const int row0 = un % H * PR_UN + 16 * dw + tr;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int row = un % H * PR_UN + 16 * dw + 8 * k + tr;
-        uint32_t s2[NG], l2[NG];
-#pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          const float l = __uint_as_float(cur.kp[k][i] & 0xffff0000u) * fk, s = __uint_as_float(cur.kp[k][i] << 16) * fk;
-          s2[i] = h2(s, s);
-          l2[i] = h2(l, l);
-        }
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {  // values 32 j + 8 u .. + 7
-          const uint32_t w = cur.kw[k][j];
-          const int gi = j * 32 / G;
-          *reinterpret_cast<uint4*>(kt + tile_off(row, 4 * j + u, BN)) =
-              make_uint4(hfma2(codes2(w), s2[gi], l2[gi]), hfma2(codes2_hi(w), s2[gi], l2[gi]),
-                         hfma2(codes2(w >> 8), s2[gi], l2[gi]), hfma2(codes2_hi(w >> 8), s2[gi], l2[gi]));
-        }
-      }
+      for (int k = 0; k < 2; ++k) convert_row<NB, NG, BN>(kt, row0 + 8 * k, u, cur.kw[k], cur.kp[k], fk);
       fence_proxy_async_smem();
-      mbar_arrive(&k_full[st]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&k_full[st]);
       // a warp whose wait expires leaves with its group, at the next unit's barrier
       ok = mbar_wait_warp(&v_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
+      if (ok) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        if (!ok) break;
-        const int row = un % H * PR_UN + 16 * dw + 8 * k + tr;
-        uint32_t s2[NG], l2[NG];
+        for (int k = 0; k < 2; ++k) {
+          // 16-bit units (2 u, j) and (2 u + 1, j), NB / 2 words apart and in the half that j says, make the word of
+          // eight values; columns stay in the order 0 4 1 5 2 6 3 7 that nibbles come in, and the output puts them right
+          uint32_t w[NB];
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {
-          const float l = __uint_as_float(cur.vp[k][i] & 0xffff0000u) * fv, s = __uint_as_float(cur.vp[k][i] << 16) * fv;
-          s2[i] = h2(s, s);
-          l2[i] = h2(l, l);
-        }
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-          // 16-bit units (2 u, j) and (2 u + 1, j): NB / 2 words apart, in the half that j says
-          const uint32_t x = cur.vw[k][j >> 1], y = cur.vw[k][NB / 2 + (j >> 1)];
-          const uint32_t w = __byte_perm(x, y, (j & 1) ? 0x7632 : 0x5410);  // nibbles 0-3: values 0-3, 4-7: 4-7
-          const int gi = j * 32 / G;
-          // columns in the order 0 4 1 5 2 6 3 7, as they come; the output puts them right
-          *reinterpret_cast<uint4*>(vt + tile_off(row, 4 * j + u, BN)) =
-              make_uint4(hfma2(codes2(w), s2[gi], l2[gi]), hfma2(codes2_hi(w), s2[gi], l2[gi]),
-                         hfma2(codes2(w >> 8), s2[gi], l2[gi]), hfma2(codes2_hi(w >> 8), s2[gi], l2[gi]));
+          for (int j = 0; j < NB; ++j)
+            w[j] = __byte_perm(cur.vw[k][j >> 1], cur.vw[k][NB / 2 + (j >> 1)], (j & 1) ? 0x7632 : 0x5410);
+          convert_row<NB, NG, BN>(vt, row0 + 8 * k, u, w, cur.vp[k], fv);
         }
       }
       fence_proxy_async_smem();
-      if (ok) mbar_arrive(&v_full[st]);
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(&v_full[st]);
       cur = nxt;
     }
     if (!ok && lane == 0 && !*abort_flag) fail();
@@ -539,7 +555,8 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       l = fmaf(sum, pow2f(-ev), l);
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(&p_full[q][un & 1]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&p_full[q][un & 1]);
     }
     for (int un = units > 1 ? units - 2 : 0; un < units && ok; ++un)
       ok = mbar_wait_warp(&pv_done[q][un & 1], (un >> 1) & 1, tmo, abort_flag);

@@ -8,7 +8,8 @@
 
 #include "decoder_internal.cuh"
 #include "linear_internal.cuh"
-#include "kv_attention.cuh"  // mma16816
+#include "kv_attention.cuh"  // matrix instruction, cluster helpers
+#include "tc_common.cuh"
 
 namespace fgq {
 namespace {
@@ -53,6 +54,7 @@ __global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __
                                                                      void* __restrict__ out, int64_t pitch,
                                                                      float* __restrict__ scale, unsigned int* err) {
   __shared__ float red[QT_THREADS / 32];
+  pdl_trigger();  // the product may be brought up; it waits for this kernel's end
   const int64_t p = blockIdx.x;
   const T* row = x + p * ldx;
   const int tid = threadIdx.x;
@@ -162,11 +164,15 @@ fgq_status launch_quantize_tokens(const void* x, int type, int P, int K, int64_t
 }
 
 // ------------------------------------------------------------------ few tokens
-// A block takes 16 output channels and 8 NT tokens; its 8 warps take every eighth piece of 64 reduction
-// elements, weights as the 16 rows of mma.m16n8k16 and tokens as its columns, and join their sums in
-// shared memory.  Thread (g, t) of a warp loads 16 consecutive bytes of rows g and g + 8 (and of token g):
-// they are its operands of four k-steps, the order of k being free as long as both sides agree.
-constexpr int FEW_WARPS = 8;
+// A block takes 32 output channels, 8 NT tokens and its share of K; its 8 warps take every eighth piece of 64
+// reduction elements, weights as the rows of mma.m16n8k16 (two tiles of 16) and tokens as its columns.  Thread
+// (g, t) of a warp loads 16 consecutive bytes of rows g, g + 8, g + 16 and g + 24 (and of token g): they are its
+// operands of four k-steps, the order of k being free as long as both sides agree.  Four pieces' weights
+// (16 loads a thread; two with 32 tokens, whose sums need the registers) are under way at any time, the first ones
+// before the tokens are there.  The warps' sums
+// are joined in shared memory; K is split over a cluster of up to 8 blocks where channels alone leave SMs idle,
+// and the cluster joins through shared memory too, always in the same order.
+constexpr int FEW_WARPS = 8, FEW_M = 32;
 
 struct FewArgs {
   const void* x;  // float tokens, ldx elements apart, or nullptr:
@@ -177,8 +183,9 @@ struct FewArgs {
   const float* wscale;
   const float* bias;
   void* y;
-  int P, K, M, ytype;
+  int P, K, M, ytype, splits;
   unsigned int* err;
+  int early;  // the kernel before is this library's quantizer: weights may be loaded while it runs
 };
 
 // Four int8 of w as two fp16 pairs.
@@ -188,195 +195,297 @@ __device__ __forceinline__ void s8_to_h2(uint32_t w, uint32_t& lo, uint32_t& hi)
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(lo) : "r"(a), "r"(0x64806480u));
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(hi) : "r"(b), "r"(0x64806480u));
 }
+__device__ __forceinline__ void s8_to_h2(uint4 v, uint32_t (&h)[8]) {
+  s8_to_h2(v.x, h[0], h[1]), s8_to_h2(v.y, h[2], h[3]), s8_to_h2(v.z, h[4], h[5]), s8_to_h2(v.w, h[6], h[7]);
+}
 
-// 16 bytes from row + k, zero from byte K on; ALIGNED: row + k is 16-byte aligned and K a multiple of 16.
-template <bool ALIGNED>
-__device__ __forceinline__ uint4 load16(const int8_t* row, int k, int K) {
-  if (ALIGNED) return k < K ? __ldg(reinterpret_cast<const uint4*>(row + k)) : make_uint4(0u, 0u, 0u, 0u);
-  uint32_t w[4] = {0u, 0u, 0u, 0u};
-  if (k + 19 <= K) {  // whole words around the 16 bytes, all inside the row from k - 3 on
-    const uintptr_t at = reinterpret_cast<uintptr_t>(row + k);
-    const uint32_t sh = 8u * (uint32_t)(at & 3);
-    if (sh == 0) {
-      const uint32_t* a = reinterpret_cast<const uint32_t*>(at);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = __ldg(a + i);
-    } else if (k >= 3) {
-      const uint32_t* a = reinterpret_cast<const uint32_t*>(at & ~uintptr_t(3));
-      uint32_t v[5];
-#pragma unroll
-      for (int i = 0; i < 5; ++i) v[i] = __ldg(a + i);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(v[i], v[i + 1], sh);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) w[i >> 2] |= (uint32_t)(uint8_t)__ldg(row + k + i) << (8 * (i & 3));
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (k + i < K) w[i >> 2] |= (uint32_t)(uint8_t)__ldg(row + k + i) << (8 * (i & 3));
+// 16 bytes from row + k of a matrix [base, end), zero from byte K of the row on.  ALIGNED: row + k is 16-byte
+// aligned and K a multiple of 16.  Otherwise two aligned loads around them, put right; where those would leave
+// the matrix, byte by byte.  READONLY: the data is older than the kernel.
+template <bool ALIGNED, bool READONLY>
+__device__ __forceinline__ uint4 load16(const int8_t* row, int k, int K, const int8_t* base, const int8_t* end) {
+  if (k >= K) return make_uint4(0u, 0u, 0u, 0u);
+  if (ALIGNED) {
+    const uint4* p = reinterpret_cast<const uint4*>(row + k);
+    return READONLY ? __ldg(p) : __ldcg(p);
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(row + k), lo = at & ~uintptr_t(15);
+  uint32_t r[4] = {0u, 0u, 0u, 0u};
+  if (lo < reinterpret_cast<uintptr_t>(base) || lo + 32 > reinterpret_cast<uintptr_t>(end)) {
+#pragma unroll 1
+    for (int i = 0; i < 16 && k + i < K; ++i) {
+      const uint32_t v = (uint32_t)(uint8_t)row[k + i] << (8 * (i & 3));
+      r[0] |= i < 4 ? v : 0u;
+      r[1] |= i >= 4 && i < 8 ? v : 0u;
+      r[2] |= i >= 8 && i < 12 ? v : 0u;
+      r[3] |= i >= 12 ? v : 0u;
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+  }
+  const uint4* p = reinterpret_cast<const uint4*>(lo);
+  const uint4 a = READONLY ? __ldg(p) : __ldcg(p), b = READONLY ? __ldg(p + 1) : __ldcg(p + 1);
+  uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+  const uint32_t off = (uint32_t)(at & 15);
+#pragma unroll
+  for (int i = 0; i < 6; ++i) w[i] = off & 8 ? w[i + 2] : w[i];
+#pragma unroll
+  for (int i = 0; i < 5; ++i) w[i] = off & 4 ? w[i + 1] : w[i];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[i] = __funnelshift_r(w[i], w[i + 1], 8 * (off & 3));
+    const int left = K - k - 4 * i;  // bytes of this word that the row still has
+    if (left < 4) r[i] &= left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+  }
+  return make_uint4(r[0], r[1], r[2], r[3]);
 }
 
 // The tokens' int8 codes in shared memory where the block quantizes them itself: rows a multiple of 16
 // bytes long and 64 off a multiple of 128, so that eight rows' pieces meet all banks.
-__host__ __device__ constexpr int few_row_bytes(int K) { return (K + 63) / 128 * 128 + 64; }
+__host__ __device__ constexpr int few_row_bytes(int pieces) { return (64 * pieces + 63) / 128 * 128 + 64; }
+// Most pieces of a split block.
+__host__ __device__ constexpr int few_pieces(int K, int splits) { return ((K + 63) / 64 + splits - 1) / splits; }
 
 // X: the type of float tokens that the block quantizes itself (a launch and a round trip less), or int8_t for
-// tokens quantized before.
+// tokens that a kernel before has quantized.
 template <int NT, bool ALIGNED, typename X>
-__global__ void __launch_bounds__(32 * FEW_WARPS) few_tokens_kernel(const __grid_constant__ FewArgs a) {
+__global__ void __launch_bounds__(32 * FEW_WARPS, NT >= 8 ? 1 : 2) few_tokens_kernel(const __grid_constant__ FewArgs a) {
   constexpr bool FLOAT = !std::is_same<X, int8_t>::value;
-  constexpr int AHEAD = 2;  // pieces of 64 whose weights are loaded ahead
-  __shared__ float sums[FEW_WARPS][8 * NT][17];
-  __shared__ float red[8 * NT][FEW_WARPS], tscale[8 * NT];
-  extern __shared__ __align__(16) uint8_t codes[];  // [8 NT][few_row_bytes(K)], FLOAT only
+  constexpr int NP = 8 * NT, AHEAD = NT >= 4 ? 2 : 4;
+  extern __shared__ __align__(16) uint8_t few_smem[];
+  float* sums = reinterpret_cast<float*>(few_smem);                        // [warp][token][33]
+  uint8_t* codes = few_smem + FEW_WARPS * NP * (FEW_M + 1) * sizeof(float);  // [token][few_row_bytes], FLOAT only
+  __shared__ float red[NP][FEW_WARPS], tscale[NP];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int m0 = blockIdx.x * 16, p0 = blockIdx.y * 8 * NT;
-  const int np = min(8 * NT, a.P - p0);
-  const int8_t* wa = a.wq + (int64_t)min(m0 + g, a.M - 1) * a.K;
-  const int8_t* wb = a.wq + (int64_t)min(m0 + g + 8, a.M - 1) * a.K;
-  uint4 na[AHEAD], nb[AHEAD];
-  int kn = 64 * warp + 16 * t;  // the next piece to load
+  const int sp = blockIdx.x % a.splits, m0 = blockIdx.x / a.splits * FEW_M, p0 = blockIdx.y * NP;
+  const int np = min(NP, a.P - p0);
+  const int pieces = (a.K + 63) / 64;
+  const int c0 = (int)((int64_t)pieces * sp / a.splits), c1 = (int)((int64_t)pieces * (sp + 1) / a.splits);
+  const int8_t* wend = a.wq + (int64_t)a.M * a.K;
+  const int8_t* wrow[4];
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i, kn += 64 * FEW_WARPS) {
-    na[i] = load16<ALIGNED>(wa, kn, a.K);
-    nb[i] = load16<ALIGNED>(wb, kn, a.K);
-  }
-  const int row_bytes = few_row_bytes(a.K);
+  for (int i = 0; i < 4; ++i) wrow[i] = a.wq + (int64_t)min(m0 + g + 8 * i, a.M - 1) * a.K;
+  uint4 w[AHEAD][4];
+  auto fetch = [&](int c, uint4 (&v)[4]) {
+    const int k = c < c1 ? 64 * c + 16 * t : a.K;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = load16<ALIGNED, true>(wrow[i], k, a.K, a.wq, wend);
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(c0 + warp + i * FEW_WARPS, w[i]);
+
+  const int row_bytes = few_row_bytes(few_pieces(a.K, a.splits));
   if constexpr (FLOAT) {
     const X* x = static_cast<const X*>(a.x) + (int64_t)p0 * a.ldx;
-    bool bad = false;
-    for (int p = 0; p < np; ++p) {
-      float mx = 0.0f;
-      for (int k = 8 * threadIdx.x; k < a.K; k += 8 * 32 * FEW_WARPS) {
-        float v[8];
-        load8(x + p * a.ldx + k, v);
+    float mx[NP];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          mx = fmaxf(mx, fabsf(v[i]));
-          if (nonfinite(v[i])) mx = INFINITY;  // the whole row, as the quantizer has it
+    for (int p = 0; p < NP; ++p) mx[p] = 0.0f;
+    for (int k = 8 * threadIdx.x; k < a.K; k += 8 * 32 * FEW_WARPS) {
+      Raw8<X> raw[NP];  // all rows' loads at once
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        if (p < np) raw[p].load(x + p * a.ldx + k);
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        if (p < np) {
+          float lo, hi;
+          raw[p].extremes(lo, hi);
+          mx[p] = max_nan(mx[p], max_nan(-lo, hi));
         }
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(FULL_MASK, mx, o));
-      if (lane == 0) red[p][warp] = mx;
     }
-    __syncthreads();
-    for (int p = 0; p < 8 * NT; ++p) {
-      float amax = 0.0f;
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
       if (p < np) {
 #pragma unroll
-        for (int w = 0; w < FEW_WARPS; ++w) amax = fmaxf(amax, red[p][w]);
+        for (int o = 16; o > 0; o >>= 1) mx[p] = max_nan(mx[p], __shfl_xor_sync(FULL_MASK, mx[p], o));
+        if (lane == 0) red[p][warp] = mx[p];
       }
-      if (nonfinite(amax)) {
-        bad = true;
-        amax = 0.0f;
-      }
-      if (threadIdx.x == 0) tscale[p] = __fdiv_rn(amax, 127.0f);
-      const TokenScale ts = token_scale(amax);
-      for (int k = 8 * threadIdx.x; k < row_bytes; k += 8 * 32 * FEW_WARPS) {
-        uint32_t w[2] = {0u, 0u};
-        if (amax > 0.0f && k < a.K) {
-          float v[8];
-          load8(x + p * a.ldx + k, v);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)((int)token_code(v[i], ts) & 255) << (8 * (i & 3));
-        }
-        *reinterpret_cast<uint2*>(codes + p * row_bytes + k) = make_uint2(w[0], w[1]);
-      }
-    }
-    if (bad && threadIdx.x == 0) record_error(a.err, FGQ_ERR_NONFINITE);
     __syncthreads();
+    bool bad = false;
+    TokenScale ts[NP];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      if (p < np) {
+        float amax = red[p][0];
+#pragma unroll
+        for (int i = 1; i < FEW_WARPS; ++i) amax = max_nan(amax, red[p][i]);
+        if (nonfinite(amax)) {  // the whole row is 0, as the quantizer has it
+          bad = true;
+          amax = 0.0f;
+        }
+        if (threadIdx.x == 0) tscale[p] = __fdiv_rn(amax, 127.0f);
+        ts[p] = token_scale(amax);
+      }
+    for (int i = 8 * threadIdx.x; i < 64 * (c1 - c0); i += 8 * 32 * FEW_WARPS) {
+      const int k = 64 * c0 + i;
+      Raw8<X> raw[NP];
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        raw[p].zero();
+        if (p < np && k < a.K) raw[p].load(x + p * a.ldx + k);
+      }
+#pragma unroll
+      for (int p = 0; p < NP; ++p)
+        if (p < np) {
+          uint32_t q[2] = {0u, 0u};
+          if (ts[p].amax > 0.0f) {
+            float v[8];
+            raw[p].unpack(v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) q[e >> 2] |= (uint32_t)((int)token_code(v[e], ts[p]) & 255) << (8 * (e & 3));
+          }
+          *reinterpret_cast<uint2*>(codes + p * row_bytes + i) = make_uint2(q[0], q[1]);
+        }
+    }
+    if (bad && threadIdx.x == 0 && blockIdx.x == 0) record_error(a.err, FGQ_ERR_NONFINITE);
+    __syncthreads();
+  } else {
+    pdl_wait();
   }
-  float acc[NT][4];
+
+  float acc[2][NT][4];
 #pragma unroll
-  for (int i = 0; i < NT; ++i)
+  for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = 0.0f;
-  auto piece = [&](int k, uint4 va, uint4 vb) {  // 16 bytes of this thread's rows from element k
-    uint32_t ha[8], hb[8];
-    s8_to_h2(va.x, ha[0], ha[1]), s8_to_h2(va.y, ha[2], ha[3]), s8_to_h2(va.z, ha[4], ha[5]), s8_to_h2(va.w, ha[6], ha[7]);
-    s8_to_h2(vb.x, hb[0], hb[1]), s8_to_h2(vb.y, hb[2], hb[3]), s8_to_h2(vb.z, hb[4], hb[5]), s8_to_h2(vb.w, hb[6], hb[7]);
+    for (int i = 0; i < NT; ++i)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int p = 8 * nt + g;
-      uint4 vx;
-      if constexpr (FLOAT)
-        vx = k < row_bytes ? *reinterpret_cast<const uint4*>(codes + p * row_bytes + k) : make_uint4(0u, 0u, 0u, 0u);
-      else
-        vx = p < np ? load16<ALIGNED>(a.q + (int64_t)(p0 + p) * a.K, k, a.K) : make_uint4(0u, 0u, 0u, 0u);
-      uint32_t hx[8];
-      s8_to_h2(vx.x, hx[0], hx[1]), s8_to_h2(vx.y, hx[2], hx[3]), s8_to_h2(vx.z, hx[4], hx[5]), s8_to_h2(vx.w, hx[6], hx[7]);
-#pragma unroll
-      for (int s = 0; s < 4; ++s)
-        mma16816(acc[nt], ha[2 * s], hb[2 * s], ha[2 * s + 1], hb[2 * s + 1], hx[2 * s], hx[2 * s + 1]);
-    }
-  };
-  for (int k0 = 64 * warp; k0 < a.K; k0 += 64 * FEW_WARPS * AHEAD) {
-    uint4 ca[AHEAD], cb[AHEAD];
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i, kn += 64 * FEW_WARPS) {
-      ca[i] = na[i];
-      cb[i] = nb[i];
-      na[i] = load16<ALIGNED>(wa, kn, a.K);  // zeros past the end
-      nb[i] = load16<ALIGNED>(wb, kn, a.K);
-    }
+      for (int e = 0; e < 4; ++e) acc[mt][i][e] = 0.0f;
+  const int8_t* qend = a.q + (int64_t)a.P * a.K;
+  for (int c = c0 + warp; c < c1; c += FEW_WARPS * AHEAD) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      const int k = k0 + 64 * FEW_WARPS * i;
-      if (k < a.K) piece(k + 16 * t, ca[i], cb[i]);  // the same for the whole warp
+      const int ci = c + i * FEW_WARPS;
+      if (ci >= c1) break;  // the same for the whole warp
+      uint32_t h[4][8];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s8_to_h2(w[i][r], h[r]);
+      fetch(ci + AHEAD * FEW_WARPS, w[i]);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int p = 8 * nt + g;
+        uint4 v = make_uint4(0u, 0u, 0u, 0u);
+        if (p < np) {
+          if constexpr (FLOAT)
+            v = *reinterpret_cast<const uint4*>(codes + p * row_bytes + 64 * (ci - c0) + 16 * t);
+          else
+            v = load16<ALIGNED, false>(a.q + (int64_t)(p0 + p) * a.K, 64 * ci + 16 * t, a.K, a.q, qend);
+        }
+        uint32_t hx[8];
+        s8_to_h2(v, hx);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int mt = 0; mt < 2; ++mt)
+            mma16816(acc[mt][nt], h[2 * mt][2 * s], h[2 * mt + 1][2 * s], h[2 * mt][2 * s + 1], h[2 * mt + 1][2 * s + 1],
+                     hx[2 * s], hx[2 * s + 1]);
+      }
     }
   }
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
+  for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sums[warp][8 * nt + 2 * t + (i & 1)][g + 8 * (i >> 1)] = acc[nt][i];
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        sums[(warp * NP + 8 * nt + 2 * t + (e & 1)) * (FEW_M + 1) + 16 * mt + g + 8 * (e >> 1)] = acc[mt][nt][e];
   __syncthreads();
-  for (int i = threadIdx.x; i < 16 * 8 * NT; i += 32 * FEW_WARPS) {
-    const int m = m0 + (i & 15), p = p0 + (i >> 4);
-    if (m >= a.M || p >= a.P) continue;
-    float v = 0.0f;
-#pragma unroll
-    for (int w = 0; w < FEW_WARPS; ++w) v += sums[w][i >> 4][i & 15];
-    v = v * ((FLOAT ? tscale[i >> 4] : __ldg(a.scale + p)) * __ldg(a.wscale + m));
+  auto put = [&](int i, float v) {  // sum i = token * 32 + channel
+    const int tok = i / FEW_M, m = m0 + i % FEW_M, p = p0 + tok;
+    if (m >= a.M || p >= a.P) return;
+    v = v * ((FLOAT ? tscale[tok] : __ldcg(a.scale + p)) * __ldg(a.wscale + m));
     if (a.bias) v += __ldg(a.bias + m);
     store_typed(a.y, a.ytype, (int64_t)p * a.M + m, v);
+  };
+#pragma unroll
+  for (int n = 0; n < NP * FEW_M / (32 * FEW_WARPS); ++n) {
+    const int i = threadIdx.x + n * 32 * FEW_WARPS;
+    float* at = sums + i / FEW_M * (FEW_M + 1) + i % FEW_M;
+    float v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < FEW_WARPS; ++k) v += at[k * NP * (FEW_M + 1)];
+    if (a.splits == 1)
+      put(i, v);
+    else
+      *at = v;  // the first warp's place: no other thread reads it in this loop
   }
+  if (a.splits > 1) {
+    cluster_sync();
+    for (int i = threadIdx.x + 32 * FEW_WARPS * sp; i < np * FEW_M; i += 32 * FEW_WARPS * a.splits) {
+      float v = 0.0f;
+      for (int k = 0; k < a.splits; ++k) v += ld_cluster(sums + i / FEW_M * (FEW_M + 1) + i % FEW_M, k);
+      put(i, v);
+    }
+    cluster_sync();  // no block leaves while another may read its sums
+  }
+}
+
+constexpr int FEW_MAX_CODES = 65536;  // bytes of codes that a block quantizes itself, at most
+
+template <int NT, bool ALIGNED, typename X>
+fgq_status launch_few_kernel(const FewArgs& a, cudaStream_t s) {
+  constexpr bool FLOAT = !std::is_same<X, int8_t>::value;
+  constexpr int SUMS = FEW_WARPS * 8 * NT * (FEW_M + 1) * 4;
+  const int smem = SUMS + (FLOAT ? 8 * NT * few_row_bytes(few_pieces(a.K, a.splits)) : 0);
+  if (!tc::smem_attr_once<few_tokens_kernel<NT, ALIGNED, X>>(SUMS + (FLOAT ? FEW_MAX_CODES : 0))) return FGQ_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((a.M + FEW_M - 1) / FEW_M * a.splits), (unsigned)((a.P + 8 * NT - 1) / (8 * NT)));
+  cfg.blockDim = dim3(32 * FEW_WARPS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  unsigned n = 0;
+  if (a.early) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (a.splits > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = (unsigned)a.splits;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return after_launch(cudaLaunchKernelEx(&cfg, few_tokens_kernel<NT, ALIGNED, X>, a));
 }
 
 template <int NT, typename X>
 fgq_status launch_few_nt(const FewArgs& a, cudaStream_t s) {
-  const dim3 grid((unsigned)((a.M + 15) / 16), (unsigned)((a.P + 8 * NT - 1) / (8 * NT)));
-  const int smem = std::is_same<X, int8_t>::value ? 0 : 8 * NT * few_row_bytes(a.K);
-  if (a.K % 16 == 0 && (a.x || aligned(a.q, 16)) && aligned(a.wq, 16))
-    few_tokens_kernel<NT, true, X><<<grid, 32 * FEW_WARPS, smem, s>>>(a);
-  else
-    few_tokens_kernel<NT, false, X><<<grid, 32 * FEW_WARPS, smem, s>>>(a);
-  return after_launch();
+  return a.K % 16 == 0 && (a.x || aligned(a.q, 16)) && aligned(a.wq, 16) ? launch_few_kernel<NT, true, X>(a, s)
+                                                                         : launch_few_kernel<NT, false, X>(a, s);
 }
 
-fgq_status launch_few(const FewArgs& a, cudaStream_t s) {
-  if (a.P <= 8) return launch_few_nt<1, int8_t>(a, s);
-  if (a.P <= 16) return launch_few_nt<2, int8_t>(a, s);
-  return launch_few_nt<4, int8_t>(a, s);
+// Blocks that share a K: about two blocks an SM, each with 16 pieces at least (two a warp).
+int few_splits(int P, int K, int M, int nt) {
+  const int64_t blocks = (int64_t)((M + FEW_M - 1) / FEW_M) * ((P + 8 * nt - 1) / (8 * nt));
+  int splits = 1;
+  while (splits < 8 && blocks * splits * 2 <= 2 * device_sms() && (K + 63) / 64 >= 32 * splits) splits *= 2;
+  return splits;
+}
+int few_nt(int P) { return P <= 8 ? 1 : (P <= 16 ? 2 : 4); }
+
+fgq_status launch_few(FewArgs a, cudaStream_t s) {
+  const int nt = few_nt(a.P);
+  a.splits = few_splits(a.P, a.K, a.M, nt);
+  return nt == 1 ? launch_few_nt<1, int8_t>(a, s) : nt == 2 ? launch_few_nt<2, int8_t>(a, s) : launch_few_nt<4, int8_t>(a, s);
 }
 
-// Float tokens that each block quantizes for itself: up to 8 of them while a block's share (every block has
-// all of it to do) stays small, 32 KB of codes, with rows that can be loaded eight elements at a time.
-constexpr int FUSED_MAX_P = 8, FUSED_MAX_CODES = 32768;
-bool fused_fits(const void* x, int type, int P, int K, int64_t ldx) {
-  return P <= FUSED_MAX_P && 8 * few_row_bytes(K) <= FUSED_MAX_CODES && K % 8 == 0 && aligned(x, 16) &&
-         (P == 1 || stride16(ldx, type));
+// Float tokens that each block quantizes for itself: up to 8 of them, rows that can be loaded eight elements at
+// a time, codes that fit beside the sums; every block has all of the rows' maxima to find, so not too long ones.
+constexpr int FUSED_MAX_P = 8, FUSED_MAX_ELEMS = 32768;
+bool fused_fits(const void* x, int type, int P, int K, int M, int64_t ldx) {
+  return P <= FUSED_MAX_P && (int64_t)P * K <= FUSED_MAX_ELEMS && K % 8 == 0 && aligned(x, 16) &&
+         (P == 1 || stride16(ldx, type)) && 8 * few_row_bytes(few_pieces(K, few_splits(P, K, M, 1))) <= FEW_MAX_CODES;
 }
-fgq_status launch_few_float(const FewArgs& a, int type, cudaStream_t s) {
+fgq_status launch_few_float(FewArgs a, int type, cudaStream_t s) {
+  a.splits = few_splits(a.P, a.K, a.M, 1);
   if (type == FGQ_F32) return launch_few_nt<1, float>(a, s);
   return type == FGQ_BF16 ? launch_few_nt<1, __nv_bfloat16>(a, s) : launch_few_nt<1, __half>(a, s);
 }
 
-constexpr int FEW_MAX_P = 32;  // tokens up to which the few-token kernel runs
+#ifndef XP
+#define XP 32
+#endif
+constexpr int FEW_MAX_P = XP;  // tokens up to which the few-token kernel runs
 
 fgq_status check_product(const void* x, int P, int K, const int8_t* wq, const float* wscale, int M, const float* bias,
                          const void* y, int ytype) {
@@ -410,7 +519,7 @@ fgq_status fgq_gemm_w8a8(const int8_t* q, const float* scale, int P, int K, cons
   if (!scale) return FGQ_ERR_ARG;
   if (!dec::aligned(scale, 4)) return FGQ_ERR_ALIGN;
   if (P > FEW_MAX_P && K > 0) return launch_gemm_w8a8(q, nullptr, 0, scale, P, K, wq, wscale, M, bias, y, ytype, stream);
-  const FewArgs a = {nullptr, 0, q, scale, wq, wscale, bias, y, P, K, M, ytype, nullptr};
+  const FewArgs a = {nullptr, 0, q, scale, wq, wscale, bias, y, P, K, M, ytype, 1, nullptr, 0};
   return launch_few(a, stream);
 }
 
@@ -420,8 +529,8 @@ fgq_status fgq_linear_w8a8(const void* x, fgq_float_type type, int P, int K, int
   if (st == FGQ_OK && P > 1 && ldx < K) st = FGQ_ERR_ARG;
   if (st != FGQ_OK || P == 0 || M == 0) return st;
   if (!dec::aligned(x, dec::float_bytes(type))) return FGQ_ERR_ALIGN;
-  if (fused_fits(x, type, P, K, ldx)) {
-    const FewArgs a = {x, ldx, nullptr, nullptr, wq, wscale, bias, y, P, K, M, type, device_error_word()};
+  if (K > 0 && fused_fits(x, type, P, K, M, ldx)) {
+    const FewArgs a = {x, ldx, nullptr, nullptr, wq, wscale, bias, y, P, K, M, type, 1, device_error_word(), 0};
     return launch_few_float(a, type, stream);
   }
   const bool few = P <= FEW_MAX_P || K == 0;
@@ -432,7 +541,7 @@ fgq_status fgq_linear_w8a8(const void* x, fgq_float_type type, int P, int K, int
   float* scale = reinterpret_cast<float*>(tmp + q_bytes);
   st = launch_quantize_tokens(x, type, P, K, ldx, tmp, pitch, !few, scale, stream);
   if (st == FGQ_OK && few) {
-    const FewArgs a = {nullptr, 0, reinterpret_cast<const int8_t*>(tmp), scale, wq, wscale, bias, y, P, K, M, type, nullptr};
+    const FewArgs a = {nullptr, 0, reinterpret_cast<const int8_t*>(tmp), scale, wq, wscale, bias, y, P, K, M, type, 1, nullptr, 1};
     st = launch_few(a, stream);
   } else if (st == FGQ_OK) {
     st = launch_gemm_w8a8(nullptr, tmp, pitch, scale, P, K, wq, wscale, M, bias, y, type, stream);

@@ -5,14 +5,19 @@
 
 namespace fgq {
 
-// Elements of a row of fp16 codes, as gemm_w8a8.cu reads them: whole K-tiles.
-inline int64_t gemm_w8a8_pitch(int K) { return ((int64_t)K + 63) / 64 * 64; }
+// How the product of many tokens is laid out: tile of tokens, splits of K, bytes of its partial sums, and elements
+// of an fp16 operand row (whole K-tiles; zero past K).
+struct GemmPlan {
+  int64_t pitch;
+  size_t part_bytes;
+  int bn, splits;
+};
+GemmPlan plan_gemm_w8a8(int P, int K, int M);
 
-// The product on the tensor cores.  Tokens as int8 q [P][K], or as fp16 rows x16 of `pitch` elements
-// (gemm_w8a8_pitch, zero past K).
-fgq_status launch_gemm_w8a8(const int8_t* q, const void* x16, int64_t pitch, const float* scale, int P, int K,
-                            const int8_t* wq, const float* wscale, int M, const float* bias, void* y, int ytype,
-                            cudaStream_t s);
+// The product on the tensor cores of fp16 operands x16 [P][pitch] and w16 [M][pitch] that the kernel before has
+// written; `part` is a temporary of plan.part_bytes.
+fgq_status launch_gemm_w8a8(const GemmPlan& plan, const void* x16, const void* w16, float* part, const float* scale,
+                            int P, const float* wscale, int M, const float* bias, void* y, int ytype, cudaStream_t s);
 
 __device__ __forceinline__ void store_typed(void* y, int type, int64_t at, float v) {
   if (type == FGQ_F32)

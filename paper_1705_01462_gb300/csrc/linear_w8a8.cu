@@ -17,30 +17,13 @@ namespace {
 using namespace dec;
 
 // ------------------------------------------------------------------ per-token quantization
-// One block per token: the row's largest magnitude, then its codes; a row of up to QT_THREADS * 8 * QT_HELD
-// elements is read once and held in registers.  OUT16: codes as fp16 in rows of `pitch` elements, zero past K
-// (the operand of gemm_w8a8.cu); else int8 [P][K].
-constexpr int QT_THREADS = 256;
-constexpr int QT_HELD = 4;
-
-__device__ __forceinline__ float block_max(float v, float* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL_MASK, v, o));
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int i = 1; i < QT_THREADS / 32; ++i) v = fmaxf(v, red[i]);
-  return v;
-}
-
 // What turns x into its code: rint(fp32(127 x / amax)).
 struct TokenScale {
-  float pre, amax, inv;  // 127 x can overflow for amax above 2^120: both are scaled down first
+  float pre, amax, inv;  // 127 x overflows for amax above 2^120, 1 / amax for tiny ones: both scaled, exactly
 };
 __device__ __forceinline__ TokenScale token_scale(float amax) {
   TokenScale t;
-  t.pre = amax > 1.329228e36f ? 1.52587890625e-5f : 1.0f;
+  t.pre = amax > 1.329228e36f ? 1.52587890625e-5f : (amax < 8.271806e-25f ? 1.8446744e19f : 1.0f);  // 2^-16, 2^64
   t.amax = amax * t.pre;
   t.inv = __frcp_rn(t.amax);
   return t;
@@ -49,143 +32,37 @@ __device__ __forceinline__ float token_code(float x, const TokenScale& t) {
   return fminf(fmaxf(rint_quotient(x * t.pre * 127.0f, t.amax, t.inv), -127.0f), 127.0f);
 }
 
-template <typename T, bool VEC, bool OUT16>
-__global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __restrict__ x, int K, int64_t ldx,
-                                                                     void* __restrict__ out, int64_t pitch,
-                                                                     float* __restrict__ scale, unsigned int* err) {
-  __shared__ float red[QT_THREADS / 32];
-  pdl_trigger();  // the product may be brought up; it waits for this kernel's end
-  const int64_t p = blockIdx.x;
-  const T* row = x + p * ldx;
-  const int tid = threadIdx.x;
-  float mx = 0.0f;
-  bool bad = false;
-  float held[VEC ? QT_HELD : 1][8];
-  if (VEC) {
-#pragma unroll
-    for (int c = 0; c < QT_HELD; ++c) {
-      const int k = 8 * (tid + c * QT_THREADS);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) held[c][i] = 0.0f;
-      if (k < K) load8(row + k, held[c]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        mx = fmaxf(mx, fabsf(held[c][i]));
-        bad |= nonfinite(held[c][i]);
-      }
-    }
-    for (int k = 8 * (tid + QT_HELD * QT_THREADS); k < K; k += 8 * QT_THREADS) {
-      float v[8];
-      load8(row + k, v);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        mx = fmaxf(mx, fabsf(v[i]));
-        bad |= nonfinite(v[i]);
-      }
-    }
-  } else {
-    for (int k = tid; k < K; k += QT_THREADS) {
-      const float v = to_float(row[k]);
-      mx = fmaxf(mx, fabsf(v));
-      bad |= nonfinite(v);
-    }
-  }
-  bad = __syncthreads_or(bad);
-  const float amax = bad ? 0.0f : block_max(mx, red);
-  if (tid == 0) {
-    scale[p] = __fdiv_rn(amax, 127.0f);
-    if (bad) record_error(err, FGQ_ERR_NONFINITE);
-  }
-  const TokenScale ts = token_scale(amax);
-  auto put8 = [&](int k, const float (&v)[8]) {
-    float c[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c[i] = amax > 0.0f ? token_code(v[i], ts) : 0.0f;
-    if (OUT16) {
-      store8(static_cast<__half*>(out) + p * pitch + k, c);
-    } else {
-      uint32_t w[2] = {0u, 0u};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[i >> 2] |= (uint32_t)((int)c[i] & 255) << (8 * (i & 3));
-      *reinterpret_cast<uint2*>(static_cast<int8_t*>(out) + p * pitch + k) = make_uint2(w[0], w[1]);
-    }
-  };
-  if (VEC) {
-#pragma unroll
-    for (int c = 0; c < QT_HELD; ++c) {
-      const int k = 8 * (tid + c * QT_THREADS);
-      if (k < K) put8(k, held[c]);
-    }
-    for (int k = 8 * (tid + QT_HELD * QT_THREADS); k < K; k += 8 * QT_THREADS) {
-      float v[8];
-      load8(row + k, v);
-      put8(k, v);
-    }
-    if (OUT16)
-      for (int k = K + tid; k < pitch; k += QT_THREADS) static_cast<__half*>(out)[p * pitch + k] = __float2half_rn(0.0f);
-  } else {
-    const int to = OUT16 ? (int)pitch : K;
-    for (int k = tid; k < to; k += QT_THREADS) {
-      const float v = k < K ? to_float(row[k]) : 0.0f;
-      const float c = amax > 0.0f && k < K ? token_code(v, ts) : 0.0f;
-      if (OUT16)
-        static_cast<__half*>(out)[p * pitch + k] = __float2half_rn(c);
-      else
-        static_cast<int8_t*>(out)[p * pitch + k] = (int8_t)(int)c;
-    }
-  }
-}
-
+// Codes of eight values as fp32 integers plus kMagicF (whose low bits are the integers).  16-bit types: the
+// correctly rounded quotients, by the reciprocal RN(1 / amax) and the quotients' exact remainders (Markstein):
+// of 127 x by an amax of at most 11 bits, no quotient lies within 2^-12 ulp of a rounding boundary.
 template <typename T>
-fgq_status launch_quantize_tokens_t(const T* x, int P, int K, int64_t ldx, void* out, int64_t pitch, bool out16,
-                                    float* scale, cudaStream_t s) {
-  // eight elements at a time: 16-byte aligned input rows, 8-byte aligned int8 rows
-  const bool vec = K % 8 == 0 && aligned(x, 16) && stride16(ldx, sizeof(T) == 4 ? FGQ_F32 : FGQ_BF16) &&
-                   (out16 || (pitch % 8 == 0 && aligned(out, 8)));
-  unsigned int* err = device_error_word();
-  if (vec && out16)
-    quantize_tokens_kernel<T, true, true><<<P, QT_THREADS, 0, s>>>(x, K, ldx, out, pitch, scale, err);
-  else if (vec)
-    quantize_tokens_kernel<T, true, false><<<P, QT_THREADS, 0, s>>>(x, K, ldx, out, pitch, scale, err);
-  else if (out16)
-    quantize_tokens_kernel<T, false, true><<<P, QT_THREADS, 0, s>>>(x, K, ldx, out, pitch, scale, err);
-  else
-    quantize_tokens_kernel<T, false, false><<<P, QT_THREADS, 0, s>>>(x, K, ldx, out, pitch, scale, err);
-  return after_launch();
+__device__ __forceinline__ void token_codes8(const float (&x)[8], const TokenScale& t, uint32_t (&c)[8]) {
+  if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c[i] = __float_as_uint(token_code(x[i], t) + kMagicF);
+  } else {
+    const uint64_t s2 = pack_f2(127.0f * t.pre, 127.0f * t.pre), y2 = pack_f2(t.inv, t.inv);
+    const uint64_t b2 = pack_f2(-t.amax, -t.amax), m2 = pack_f2(kMagicF, kMagicF);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint64_t a = mul_f2(pack_f2(x[2 * i], x[2 * i + 1]), s2), q = mul_f2(a, y2);
+      float c0, c1;
+      unpack_f2(add_f2(fma_f2(fma_f2(q, b2, a), y2, q), m2), c0, c1);
+      c[2 * i] = __float_as_uint(c0);
+      c[2 * i + 1] = __float_as_uint(c1);
+    }
+  }
+}
+__device__ __forceinline__ uint2 pack_codes8(const uint32_t (&c)[8]) {
+  return make_uint2(__byte_perm(__byte_perm(c[0], c[1], 0x0040), __byte_perm(c[2], c[3], 0x0040), 0x5410),
+                    __byte_perm(__byte_perm(c[4], c[5], 0x0040), __byte_perm(c[6], c[7], 0x0040), 0x5410));
 }
 
-fgq_status launch_quantize_tokens(const void* x, int type, int P, int K, int64_t ldx, void* out, int64_t pitch,
-                                  bool out16, float* scale, cudaStream_t s) {
-  if (type == FGQ_F32)
-    return launch_quantize_tokens_t(static_cast<const float*>(x), P, K, ldx, out, pitch, out16, scale, s);
-  if (type == FGQ_BF16)
-    return launch_quantize_tokens_t(static_cast<const __nv_bfloat16*>(x), P, K, ldx, out, pitch, out16, scale, s);
-  return launch_quantize_tokens_t(static_cast<const __half*>(x), P, K, ldx, out, pitch, out16, scale, s);
-}
-
-// ------------------------------------------------------------------ few tokens
-// A block takes 32 output channels, 8 NT tokens and its share of K; its 8 warps take every eighth piece of 64
-// reduction elements, weights as the rows of mma.m16n8k16 (two tiles of 16) and tokens as its columns.  Thread
-// (g, t) of a warp loads 16 consecutive bytes of rows g, g + 8, g + 16 and g + 24 (and of token g): they are its
-// operands of four k-steps, the order of k being free as long as both sides agree.  Four pieces' weights
-// (16 loads a thread; two with 32 tokens, whose sums need the registers) are under way at any time, the first ones
-// before the tokens are there.  The warps' sums
-// are joined in shared memory; K is split over a cluster of up to 8 blocks where channels alone leave SMs idle,
-// and the cluster joins through shared memory too, always in the same order.
-constexpr int FEW_WARPS = 8, FEW_M = 32;
-
-struct FewArgs {
-  const void* x;  // float tokens, ldx elements apart, or nullptr:
-  int64_t ldx;
-  const int8_t* q;  // int8 tokens and their scales
-  const float* scale;
-  const int8_t* wq;
-  const float* wscale;
-  const float* bias;
-  void* y;
-  int P, K, M, ytype, splits;
-  unsigned int* err;
-  int early;  // the kernel before is this library's quantizer: weights may be loaded while it runs
+// int8 weights to expand to fp16 rows of `pitch` elements (zero past K) beside the tokens' quantization.
+struct Expand {
+  const int8_t* src;
+  __half* dst;
+  int rows, aligned;
 };
 
 // Four int8 of w as two fp16 pairs.
@@ -238,6 +115,211 @@ __device__ __forceinline__ uint4 load16(const int8_t* row, int k, int K, const i
   }
   return make_uint4(r[0], r[1], r[2], r[3]);
 }
+
+// One row of int8 as fp16, by one warp.
+template <bool ALIGNED, bool READONLY>
+__device__ __forceinline__ void expand_row(const Expand& e, int row, int K, int64_t pitch, int lane) {
+  const int8_t* src = e.src + (int64_t)row * K;
+  __half* dst = e.dst + (int64_t)row * pitch;
+  const int8_t* end = e.src + (int64_t)e.rows * K;
+#pragma unroll 2
+  for (int k = 16 * lane; k < pitch; k += 512) {
+    uint32_t h[8];
+    s8_to_h2(load16<ALIGNED, READONLY>(src, k, K, e.src, end), h);
+    *reinterpret_cast<uint4*>(dst + k) = make_uint4(h[0], h[1], h[2], h[3]);
+    *reinterpret_cast<uint4*>(dst + k + 8) = make_uint4(h[4], h[5], h[6], h[7]);
+  }
+}
+
+// WPR warps a token (one where there are many short rows, so that no barrier stands between load and store; eight
+// otherwise), 8 / WPR tokens a block: the row's largest magnitude, then its codes.  Rows of up to 256 WPR HELD
+// elements are read once and held in registers.  OUT16: codes as fp16 in rows of `pitch` elements, zero past K
+// (the operand of gemm_w8a8.cu); else int8 [P][K].  Blocks past the tokens' expand weights, a warp a row.
+constexpr int QT_THREADS = 256, QT_WARPS = QT_THREADS / 32;
+
+template <typename T, bool VEC, bool OUT16, int WPR>
+__global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __restrict__ x, int P, int K, int64_t ldx,
+                                                                     void* __restrict__ out, int64_t pitch,
+                                                                     float* __restrict__ scale, unsigned int* err,
+                                                                     const __grid_constant__ Expand e) {
+  constexpr int RPB = QT_WARPS / WPR, HELD = WPR == 1 ? 8 : 4, LANES = 32 * WPR;
+  __shared__ float red[QT_WARPS];
+  pdl_trigger();  // the product may be brought up; it waits for this kernel's end
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int qblocks = (P + RPB - 1) / RPB;
+  if ((int)blockIdx.x >= qblocks) {
+    for (int row = ((int)blockIdx.x - qblocks) * QT_WARPS + warp; row < e.rows; row += ((int)gridDim.x - qblocks) * QT_WARPS) {
+      if (e.aligned)
+        expand_row<true, true>(e, row, K, pitch, lane);
+      else
+        expand_row<false, true>(e, row, K, pitch, lane);
+    }
+    return;
+  }
+  const int p = blockIdx.x * RPB + warp / WPR;
+  const int tid = threadIdx.x % LANES;
+  if (p >= P) return;  // with WPR = 8 there is no such block
+  const T* row = x + (int64_t)p * ldx;
+  float mx = 0.0f;
+  Raw8<T> held[VEC ? HELD : 1];
+  if constexpr (VEC) {
+#pragma unroll
+    for (int c = 0; c < HELD; ++c) {
+      const int k = 8 * (tid + c * LANES);
+      held[c].zero();
+      if (k < K) held[c].load(row + k);
+    }
+    float lo, hi;
+#pragma unroll
+    for (int c = 0; c < HELD; ++c) {
+      held[c].extremes(lo, hi);
+      mx = max_nan(mx, max_nan(-lo, hi));
+    }
+    for (int k = 8 * (tid + HELD * LANES); k < K; k += 8 * LANES) {
+      Raw8<T> v;
+      v.load(row + k);
+      v.extremes(lo, hi);
+      mx = max_nan(mx, max_nan(-lo, hi));
+    }
+  } else {
+    for (int k = tid; k < K; k += LANES) mx = max_nan(mx, fabsf(to_float(row[k])));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(FULL_MASK, mx, o));
+  if constexpr (WPR > 1) {
+    if (lane == 0) red[warp] = mx;
+    __syncthreads();
+    mx = red[0];
+#pragma unroll
+    for (int i = 1; i < WPR; ++i) mx = max_nan(mx, red[i]);
+  }
+  const bool bad = nonfinite(mx);
+  const float amax = bad ? 0.0f : mx;
+  if (tid == 0) {
+    scale[p] = __fdiv_rn(amax, 127.0f);
+    if (bad) record_error(err, FGQ_ERR_NONFINITE);
+  }
+  const TokenScale ts = token_scale(amax);
+  auto put8 = [&](int k, const Raw8<T>& raw) {
+    float v[8];
+    raw.unpack(v);
+    uint32_t c[8];
+    if (amax > 0.0f) {
+      token_codes8<T>(v, ts, c);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) c[i] = (uint32_t)kMagicI;
+    }
+    if (OUT16) {
+      float f[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(c[i]) - kMagicF;
+      store8(static_cast<__half*>(out) + p * pitch + k, f);
+    } else {
+      *reinterpret_cast<uint2*>(static_cast<int8_t*>(out) + p * pitch + k) = pack_codes8(c);
+    }
+  };
+  if constexpr (VEC) {
+#pragma unroll
+    for (int c = 0; c < HELD; ++c) {
+      const int k = 8 * (tid + c * LANES);
+      if (k < K) put8(k, held[c]);
+    }
+    for (int k = 8 * (tid + HELD * LANES); k < K; k += 8 * LANES) {
+      Raw8<T> v;
+      v.load(row + k);
+      put8(k, v);
+    }
+    if (OUT16)
+      for (int k = K + tid; k < pitch; k += LANES) static_cast<__half*>(out)[p * pitch + k] = __float2half_rn(0.0f);
+  } else {
+    const int to = OUT16 ? (int)pitch : K;
+    for (int k = tid; k < to; k += LANES) {
+      const float v = k < K ? to_float(row[k]) : 0.0f;
+      const float c = amax > 0.0f && k < K ? token_code(v, ts) : 0.0f;
+      if (OUT16)
+        static_cast<__half*>(out)[p * pitch + k] = __float2half_rn(c);
+      else
+        static_cast<int8_t*>(out)[p * pitch + k] = (int8_t)(int)c;
+    }
+  }
+}
+
+template <typename T, bool VEC, bool OUT16>
+fgq_status launch_quantize_tokens_w(const T* x, int P, int K, int64_t ldx, void* out, int64_t pitch, float* scale,
+                                    const Expand& e, cudaStream_t s) {
+  unsigned int* err = device_error_word();
+  // blocks for the weights, a warp a row, up to eight of them an SM
+  const int64_t most = 8ll * device_sms(), want = ((int64_t)e.rows + QT_WARPS - 1) / QT_WARPS;
+  const unsigned eb = (unsigned)(want < most ? want : most);
+  if (VEC && P >= 8 * device_sms() && K <= 2048)
+    quantize_tokens_kernel<T, VEC, OUT16, 1><<<(P + 7) / 8 + eb, QT_THREADS, 0, s>>>(x, P, K, ldx, out, pitch, scale, err, e);
+  else
+    quantize_tokens_kernel<T, VEC, OUT16, 8><<<P + eb, QT_THREADS, 0, s>>>(x, P, K, ldx, out, pitch, scale, err, e);
+  return after_launch();
+}
+
+template <typename T>
+fgq_status launch_quantize_tokens_t(const T* x, int P, int K, int64_t ldx, void* out, int64_t pitch, bool out16,
+                                    float* scale, const Expand& e, cudaStream_t s) {
+  // eight elements at a time: 16-byte aligned input rows, 8-byte aligned int8 rows
+  const bool vec = K % 8 == 0 && aligned(x, 16) && (P == 1 || stride16(ldx, sizeof(T) == 4 ? FGQ_F32 : FGQ_BF16)) &&
+                   (out16 || (pitch % 8 == 0 && aligned(out, 8)));
+  if (vec)
+    return out16 ? launch_quantize_tokens_w<T, true, true>(x, P, K, ldx, out, pitch, scale, e, s)
+                 : launch_quantize_tokens_w<T, true, false>(x, P, K, ldx, out, pitch, scale, e, s);
+  return out16 ? launch_quantize_tokens_w<T, false, true>(x, P, K, ldx, out, pitch, scale, e, s)
+               : launch_quantize_tokens_w<T, false, false>(x, P, K, ldx, out, pitch, scale, e, s);
+}
+
+fgq_status launch_quantize_tokens(const void* x, int type, int P, int K, int64_t ldx, void* out, int64_t pitch,
+                                  bool out16, float* scale, const Expand& e, cudaStream_t s) {
+  if (type == FGQ_F32)
+    return launch_quantize_tokens_t(static_cast<const float*>(x), P, K, ldx, out, pitch, out16, scale, e, s);
+  if (type == FGQ_BF16)
+    return launch_quantize_tokens_t(static_cast<const __nv_bfloat16*>(x), P, K, ldx, out, pitch, out16, scale, e, s);
+  return launch_quantize_tokens_t(static_cast<const __half*>(x), P, K, ldx, out, pitch, out16, scale, e, s);
+}
+
+// int8 tokens and weights as fp16 rows, a warp a row.
+__global__ void __launch_bounds__(256) expand_kernel(const __grid_constant__ Expand w, const __grid_constant__ Expand q, int K,
+                                                     int64_t pitch) {
+  pdl_trigger();
+  const int lane = threadIdx.x & 31;
+  for (int row = blockIdx.x * 8 + (threadIdx.x >> 5); row < w.rows + q.rows; row += gridDim.x * 8) {
+    const Expand& e = row < w.rows ? w : q;
+    const int r = row < w.rows ? row : row - w.rows;
+    if (e.aligned)
+      expand_row<true, true>(e, r, K, pitch, lane);
+    else
+      expand_row<false, true>(e, r, K, pitch, lane);
+  }
+}
+
+// ------------------------------------------------------------------ few tokens
+// A block takes 32 output channels, 8 NT tokens and its share of K; its 8 warps take every eighth piece of 64
+// reduction elements, weights as the rows of mma.m16n8k16 (two tiles of 16) and tokens as its columns.  Thread
+// (g, t) of a warp loads 16 consecutive bytes of rows g, g + 8, g + 16 and g + 24 (and of token g): they are its
+// operands of four k-steps, the order of k being free as long as both sides agree.  Four pieces' weights
+// (16 loads a thread; two with 32 tokens, whose sums need the registers) are under way at any time, the first ones
+// before the tokens are there.  The warps' sums
+// are joined in shared memory; K is split over a cluster of up to 8 blocks where channels alone leave SMs idle,
+// and the cluster joins through shared memory too, always in the same order.
+constexpr int FEW_WARPS = 8, FEW_M = 32;
+
+struct FewArgs {
+  const void* x;  // float tokens, ldx elements apart, or nullptr:
+  int64_t ldx;
+  const int8_t* q;  // int8 tokens and their scales
+  const float* scale;
+  const int8_t* wq;
+  const float* wscale;
+  const float* bias;
+  void* y;
+  int P, K, M, ytype, splits;
+  unsigned int* err;
+  int early;  // the kernel before is this library's quantizer: weights may be loaded while it runs
+};
 
 // The tokens' int8 codes in shared memory where the block quantizes them itself: rows a multiple of 16
 // bytes long and 64 off a multiple of 128, so that eight rows' pieces meet all banks.
@@ -326,14 +408,15 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, NT >= 8 ? 1 : 2) few_tokens_ke
 #pragma unroll
       for (int p = 0; p < NP; ++p)
         if (p < np) {
-          uint32_t q[2] = {0u, 0u};
+          uint2 q = make_uint2(0u, 0u);
           if (ts[p].amax > 0.0f) {
             float v[8];
             raw[p].unpack(v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) q[e >> 2] |= (uint32_t)((int)token_code(v[e], ts[p]) & 255) << (8 * (e & 3));
+            uint32_t c[8];
+            token_codes8<X>(v, ts[p], c);
+            q = pack_codes8(c);
           }
-          *reinterpret_cast<uint2*>(codes + p * row_bytes + i) = make_uint2(q[0], q[1]);
+          *reinterpret_cast<uint2*>(codes + p * row_bytes + i) = q;
         }
     }
     if (bad && threadIdx.x == 0 && blockIdx.x == 0) record_error(a.err, FGQ_ERR_NONFINITE);
@@ -482,10 +565,9 @@ fgq_status launch_few_float(FewArgs a, int type, cudaStream_t s) {
   return type == FGQ_BF16 ? launch_few_nt<1, __nv_bfloat16>(a, s) : launch_few_nt<1, __half>(a, s);
 }
 
-#ifndef XP
-#define XP 32
-#endif
-constexpr int FEW_MAX_P = XP;  // tokens up to which the few-token kernel runs
+inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+constexpr int FEW_MAX_P = 64;  // tokens up to which the few-token kernel runs
 
 fgq_status check_product(const void* x, int P, int K, const int8_t* wq, const float* wscale, int M, const float* bias,
                          const void* y, int ytype) {
@@ -509,7 +591,7 @@ fgq_status fgq_quantize_tokens(const void* x, fgq_float_type type, int P, int K,
   if (P == 0) return FGQ_OK;
   if (!scale || (K > 0 && (!x || !q))) return FGQ_ERR_ARG;
   if (!dec::aligned(x, dec::float_bytes(type)) || !dec::aligned(scale, 4)) return FGQ_ERR_ALIGN;
-  return launch_quantize_tokens(x, type, P, K, ldx, q, K, false, scale, stream);
+  return launch_quantize_tokens(x, type, P, K, ldx, q, K, false, scale, Expand{}, stream);
 }
 
 fgq_status fgq_gemm_w8a8(const int8_t* q, const float* scale, int P, int K, const int8_t* wq, const float* wscale,
@@ -518,7 +600,23 @@ fgq_status fgq_gemm_w8a8(const int8_t* q, const float* scale, int P, int K, cons
   if (st != FGQ_OK || P == 0 || M == 0) return st;
   if (!scale) return FGQ_ERR_ARG;
   if (!dec::aligned(scale, 4)) return FGQ_ERR_ALIGN;
-  if (P > FEW_MAX_P && K > 0) return launch_gemm_w8a8(q, nullptr, 0, scale, P, K, wq, wscale, M, bias, y, ytype, stream);
+  if (P > FEW_MAX_P && K > 0) {
+    const GemmPlan plan = plan_gemm_w8a8(P, K, M);
+    const size_t w_bytes = up256((size_t)M * plan.pitch * 2), q_bytes = up256((size_t)P * plan.pitch * 2);
+    uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(w_bytes + q_bytes + plan.part_bytes, stream));
+    if (!tmp) return FGQ_ERR_CUDA;
+    const bool k16 = K % 16 == 0;
+    const Expand we = {wq, reinterpret_cast<__half*>(tmp), M, k16 && dec::aligned(wq, 16)};
+    const Expand qe = {q, reinterpret_cast<__half*>(tmp + w_bytes), P, k16 && dec::aligned(q, 16)};
+    const int64_t blocks = ((int64_t)P + M + 7) / 8, most = 8ll * device_sms();
+    expand_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, stream>>>(we, qe, K, plan.pitch);
+    fgq_status r = after_launch();
+    if (r == FGQ_OK)
+      r = launch_gemm_w8a8(plan, qe.dst, we.dst, reinterpret_cast<float*>(tmp + w_bytes + q_bytes), scale, P, wscale, M, bias,
+                           y, ytype, stream);
+    if (cudaFreeAsync(tmp, stream) != cudaSuccess && r == FGQ_OK) r = FGQ_ERR_CUDA;
+    return r;
+  }
   const FewArgs a = {nullptr, 0, q, scale, wq, wscale, bias, y, P, K, M, ytype, 1, nullptr, 0};
   return launch_few(a, stream);
 }
@@ -534,17 +632,26 @@ fgq_status fgq_linear_w8a8(const void* x, fgq_float_type type, int P, int K, int
     return launch_few_float(a, type, stream);
   }
   const bool few = P <= FEW_MAX_P || K == 0;
-  const int64_t pitch = few ? K : gemm_w8a8_pitch(K);
-  const size_t q_bytes = ((size_t)P * pitch * (few ? 1 : 2) + 255) / 256 * 256;
-  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(q_bytes + (size_t)P * 4, stream));
+  const GemmPlan plan = few ? GemmPlan{} : plan_gemm_w8a8(P, K, M);
+  const size_t q_bytes = up256((size_t)P * (few ? (int64_t)K : 2 * plan.pitch)), s_bytes = up256((size_t)P * 4);
+  const size_t w_bytes = few ? 0 : up256((size_t)M * plan.pitch * 2);
+  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(q_bytes + s_bytes + w_bytes + plan.part_bytes, stream));
   if (!tmp) return FGQ_ERR_CUDA;
   float* scale = reinterpret_cast<float*>(tmp + q_bytes);
-  st = launch_quantize_tokens(x, type, P, K, ldx, tmp, pitch, !few, scale, stream);
-  if (st == FGQ_OK && few) {
-    const FewArgs a = {nullptr, 0, reinterpret_cast<const int8_t*>(tmp), scale, wq, wscale, bias, y, P, K, M, type, 1, nullptr, 1};
-    st = launch_few(a, stream);
-  } else if (st == FGQ_OK) {
-    st = launch_gemm_w8a8(nullptr, tmp, pitch, scale, P, K, wq, wscale, M, bias, y, type, stream);
+  if (few) {
+    st = launch_quantize_tokens(x, type, P, K, ldx, tmp, K, false, scale, Expand{}, stream);
+    if (st == FGQ_OK) {
+      const FewArgs a = {nullptr, 0, reinterpret_cast<const int8_t*>(tmp), scale, wq, wscale, bias, y, P, K, M, type, 1, nullptr, 1};
+      st = launch_few(a, stream);
+    }
+  } else {
+    // tokens to fp16 codes and weights to fp16 in one launch
+    __half* w16 = reinterpret_cast<__half*>(tmp + q_bytes + s_bytes);
+    const Expand we = {wq, w16, M, K % 16 == 0 && dec::aligned(wq, 16)};
+    st = launch_quantize_tokens(x, type, P, K, ldx, tmp, plan.pitch, true, scale, we, stream);
+    if (st == FGQ_OK)
+      st = launch_gemm_w8a8(plan, tmp, w16, reinterpret_cast<float*>(tmp + q_bytes + s_bytes + w_bytes), scale, P, wscale, M,
+                            bias, y, type, stream);
   }
   if (cudaFreeAsync(tmp, stream) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
   return st;

@@ -474,8 +474,8 @@ __global__ void __launch_bounds__(32 * FEW_WARPS, NT >= 8 ? 1 : 2) few_tokens_ke
   auto put = [&](int i, float v) {  // sum i = token * 32 + channel
     const int tok = i / FEW_M, m = m0 + i % FEW_M, p = p0 + tok;
     if (m >= a.M || p >= a.P) return;
-    v = v * ((FLOAT ? tscale[tok] : __ldcg(a.scale + p)) * __ldg(a.wscale + m));
-    if (a.bias) v += __ldg(a.bias + m);
+    // as gemm_w8a8.cu has it: the two kernels give the same bits wherever the sums are exact
+    v = fmaf(v, (FLOAT ? tscale[tok] : __ldcg(a.scale + p)) * __ldg(a.wscale + m), a.bias ? __ldg(a.bias + m) : 0.0f);
     store_typed(a.y, a.ytype, (int64_t)p * a.M + m, v);
   };
 #pragma unroll

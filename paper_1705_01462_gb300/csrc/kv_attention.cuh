@@ -286,6 +286,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
   const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
   int first, end;
   visible(a, n, nq, r0 / a.group, (min(r0 + NR, a.rows) - 1) / a.group, first, end);
+  const int seen = first;  // tokens before it share its block of 16 and may never have been written
   first &= ~15;
   // this block's tokens [lo, hi): chunks start a multiple of 32 after `first`; the last one takes the rest
   const int64_t lo64 = (int64_t)first + (int64_t)ch * a.chunk;
@@ -549,7 +550,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
           }
     }
 
-    // value parameters of this thread's four tokens; tokens past the end hold nothing
+    // value parameters of this thread's four tokens; tokens past the end, or before the first one seen, hold nothing
     uint32_t vw[2][2][NG];
     float smax = 0.0f;
 #pragma unroll
@@ -557,7 +558,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         lds_words<NG>(reinterpret_cast<const uint8_t*>(vp + (16 * mt + g + 8 * u) * NG), vw[mt][u]);
-        if (!whole && tok0 + 16 * mt + g + 8 * u >= hi)
+        if (!whole && (tok0 + 16 * mt + g + 8 * u >= hi || tok0 + 16 * mt + g + 8 * u < seen))
 #pragma unroll
           for (int i = 0; i < NG; ++i) vw[mt][u][i] = 0u;
 #pragma unroll

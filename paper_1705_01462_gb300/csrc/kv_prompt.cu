@@ -181,6 +181,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
   int first, end;
   visible(a, n, nq, r0 / a.group, (min(r0 + ROWS, a.rows) - 1) / a.group, first, end);
+  const int seen = first;  // tokens before it share its block of 16 and may never have been written
   first &= ~15;
   const int64_t lo64 = (int64_t)first + (int64_t)ch * a.chunk;
   const int lo = lo64 < end ? (int)lo64 : end;
@@ -294,7 +295,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       page = -1;
       if (un < units && tok < hi) page = __ldg(table + page_of(a.c, (uint32_t)tok));
     };
-    auto fetch = [&](int un, Raw& x) {  // zeros past the end
+    auto fetch = [&](int un, Raw& x) {  // zeros where nothing was written
       const int tok = lo + un * PR_UN + 16 * dw;
       const bool in = un < units && tok < hi;
       const bool good = in && page >= 0 && page < a.c.pages;
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       const int64_t row0 = good ? ((int64_t)page * a.c.kv_heads + head) * a.c.page_size + slot : 0;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const bool ok = good && tok + 8 * k + tr < hi;
+        const bool ok = good && tok + 8 * k + tr < hi && tok + 8 * k + tr >= seen;
         const int64_t row = row0 + 8 * k + tr;
 #pragma unroll
         for (int i = 0; i < WPT; ++i) x.kw[k][i] = x.vw[k][i] = 0u;

@@ -7,8 +7,56 @@ namespace {
 
 using namespace dec;
 
-constexpr int JOIN_THREADS = 512;
+constexpr int JOIN_THREADS = 512, JOIN_FEW = 16;
 constexpr uint64_t AT_TIMEOUT_NS = 1000000000ull;  // 1 s per wait
+
+// The chunks of output row orow = (b, query, head) that had work.
+__device__ __forceinline__ int chunks_of(const AttnArgs& a, int64_t orow, int tile_rows) {
+  const int hq = (int)(orow % a.q_heads);
+  const int64_t bt = orow / a.q_heads;
+  const int qi = (int)(bt % a.T), b = (int)(bt / a.T);
+  const int n = seq_len(a, b);
+  const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
+  const int r0 = (qi * a.group + hq % a.group) / tile_rows * tile_rows;  // the block's tile of query rows
+  int first, end;
+  visible(a, n, nq, r0 / a.group, (min(r0 + tile_rows, a.rows) - 1) / a.group, first, end);
+  first &= ~15;
+  return (int)min((int64_t)a.chunks, ((int64_t)end - first + a.chunk - 1) / a.chunk);
+}
+
+// The join where there are at most JOIN_FEW chunks: D / 4 threads a row, four values each, one chunk after
+// another.  With few chunks there are many rows, and a block a row costs its start: 300 queries of 32 heads over
+// 20000 tokens took 223 us with join_kernel throughout and 181 us with this one.  A long row is slow here, as one
+// thread reads all its chunks: one query of 64 heads over 131071 tokens took 50 us instead of 43.
+template <int D>
+__global__ void __launch_bounds__(256) join_few_kernel(const __grid_constant__ AttnArgs a, int tile_rows, int64_t orows) {
+  const int64_t orow = (int64_t)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
+  if (orow >= orows) return;  // no barrier, and no wait needed
+  const int d = threadIdx.x % (D / 4) * 4;
+  const int chunks = chunks_of(a, orow, tile_rows);
+  const float2* st = reinterpret_cast<const float2*>(a.stats) + orow * a.chunks;
+  const float* part = a.part + orow * a.chunks * D + d;
+  pdl_wait();
+  float r = AT_M0, l = 0.0f;
+  float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+  for (int c = 0; c < chunks; ++c) {
+    const float2 s = st[c];
+    const float4 x = *reinterpret_cast<const float4*>(part + (int64_t)c * D);
+    const float top = fmaxf(r, s.x), f0 = ex2(r - top), f = ex2(s.x - top);
+    r = top;
+    l = fmaf(f, s.y, l * f0);
+    v.x = fmaf(f, x.x, v.x * f0);
+    v.y = fmaf(f, x.y, v.y * f0);
+    v.z = fmaf(f, x.z, v.z * f0);
+    v.w = fmaf(f, x.w, v.w * f0);
+  }
+  const int64_t at = orow * D + d;
+  store_out(a, at, normalise(v.x, l));
+  store_out(a, at + 1, normalise(v.y, l));
+  store_out(a, at + 2, normalise(v.z, l));
+  store_out(a, at + 3, normalise(v.w, l));
+}
 
 // out[row] = sum_c 2^(r_c - r) part_c / sum_c 2^(r_c - r) l_c over the chunks that had work; one block per row,
 // JOIN_THREADS / D chunks at a time, each thread keeping the largest r so far (one pass, no load waits for
@@ -18,17 +66,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
   constexpr int WAYS = JOIN_THREADS / D, AHEAD = 8;
   __shared__ float sv[WAYS][D], sr[WAYS], sl[WAYS];
   const int64_t orow = blockIdx.x;  // (b, query, head)
-  const int hq = (int)(orow % a.q_heads);
-  const int64_t bt = orow / a.q_heads;
-  const int qi = (int)(bt % a.T), b = (int)(bt / a.T);
   const int tid = threadIdx.x, d = tid % D, way = tid / D;
-  const int n = seq_len(a, b);
-  const int nq = a.q_lens ? min(__ldg(a.q_lens + b), a.T) : a.T;
-  const int r0 = (qi * a.group + hq % a.group) / tile_rows * tile_rows;  // the block's tile of query rows
-  int first, end;
-  visible(a, n, nq, r0 / a.group, (min(r0 + tile_rows, a.rows) - 1) / a.group, first, end);
-  first &= ~15;
-  const int chunks = (int)min((int64_t)a.chunks, ((int64_t)end - first + a.chunk - 1) / a.chunk);
+  const int chunks = chunks_of(a, orow, tile_rows);
   const float2* st = reinterpret_cast<const float2*>(a.stats) + orow * a.chunks;
   const float* part = a.part + orow * a.chunks * D + d;
   pdl_wait();
@@ -79,39 +118,70 @@ __global__ void __launch_bounds__(JOIN_THREADS) join_kernel(const __grid_constan
 
 }  // namespace
 
-constexpr int PROMPT_MIN_ROWS = 33;
+namespace {
 
-fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_len, cudaStream_t s) {
-  const int D = cache->head_dim, nb = D / 32, gb = cache->group / 32;
-  const bool split = a.type == FGQ_F32;
-  const AttnKernel k = !split && a.rows >= PROMPT_MIN_ROWS ? prompt_kernel(D, cache->group, a.rows)
-                       : nb == 2   ? attention_kernel_2(gb, split, a.rows)
-                       : nb == 4 ? attention_kernel_4(gb, split, a.rows)
-                                 : attention_kernel_8(gb, split, a.rows);
-  a.row_tiles = (a.rows + k.rows - 1) / k.rows;
-  const int64_t units = (int64_t)a.B * a.c.kv_heads * a.row_tiles;
+// How a call could run: a kernel, its chunks of the longest sequence, and the time that takes if every
+// sequence is as long.
+struct Plan {
+  AttnKernel k;
+  int64_t units, chunks, chunk;
+  float us;
+  bool cluster;
+};
+
+// Whole waves of blocks, as many as cost least: a block costs its kernel's start and its tokens, a join kernel 3 us
+// and the partial sums' way to memory and back.
+Plan plan_kernel(const AttnKernel& k, const AttnArgs& a, int D, int max_len) {
+  Plan best = {};
+  best.k = k;
+  best.units = (int64_t)a.B * a.c.kv_heads * ((a.rows + k.rows - 1) / k.rows);
   int64_t span = max_len;  // tokens that one block may have to read
   if (a.window && (int64_t)a.window + k.rows / a.group + 1 < span) span = (int64_t)a.window + k.rows / a.group + 1;
   span += 15;
-  // the split: whole waves of blocks, as many as cost least if every sequence is as long as the longest may
-  // be, a block costing its tokens and about 256 more; 128 tokens at least
   const int64_t slots = (int64_t)device_sms() * k.per_sm;
-  int64_t chunk = 0, best = INT64_MAX;
   for (int waves = 1; waves <= 8; ++waves) {
-    const int64_t n = waves * slots / units > 0 ? waves * slots / units : 1;
-    const int64_t r = (span + n - 1) / n, c = r > 512 ? (r + 255) / 256 * 256 : (r + 127) / 128 * 128;
-    const int64_t blocks = units * ((span + c - 1) / c), cost = (blocks + slots - 1) / slots * (c + 256);
-    if (cost < best) {
-      best = cost;
-      chunk = c;
+    const int64_t want = waves * slots / best.units, n = want > 0 ? want : 1, r = (span + n - 1) / n;
+    const int64_t chunk = r > 512 ? (r + 255) / 256 * 256 : (r + 127) / 128 * 128;  // a tile for each warp
+    const int64_t chunks = (span + chunk - 1) / chunk, blocks = best.units * chunks;
+    // few chunks that all run at once join as a cluster: no temporary and no second launch.  More blocks than that
+    // would wait for eight of them to fit together.  Each of the GPU's eight groups of SMs, which a cluster does
+    // not cross, may leave chunks - 1 places empty: 24 rows of 256 values over 2 sequences of 20000 tokens, 288
+    // blocks in clusters of 6 on 304 places, took 119 us, and 74 as separate blocks.
+    const bool cluster = k.clusters && chunks > 1 && chunks <= 8 && blocks + 8 * (chunks - 1) <= slots;
+    float us = (float)((blocks + slots - 1) / slots) * (k.start_us + (float)chunk / k.rate);
+    if (chunks > 1 && !cluster) us += 3.0f + (float)a.B * a.T * a.q_heads * chunks * D * 8.0f / 4e6f;
+    if (waves == 1 || us < best.us) {
+      best.chunk = chunk;
+      best.chunks = chunks;
+      best.us = us;
+      best.cluster = cluster;
     }
   }
-  a.chunk = (int)chunk;
-  a.chunks = (int)((span + chunk - 1) / chunk);
-  if (units * a.chunks > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
-  // few chunks that all run at once join as a cluster: no temporary and no second launch.  More blocks than
-  // that would wait for eight of them to fit together.
-  a.cluster = k.clusters && a.chunks > 1 && a.chunks <= 8 && units * a.chunks <= slots;
+  return best;
+}
+
+}  // namespace
+
+fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_len, cudaStream_t s) {
+  const int D = cache->head_dim, nb = D / 32, gb = cache->group / 32;
+  Plan p = plan_kernel(nb == 2   ? attention_kernel_2(gb, a.type == FGQ_F32, a.rows)
+                       : nb == 4 ? attention_kernel_4(gb, a.type == FGQ_F32, a.rows)
+                                 : attention_kernel_8(gb, a.type == FGQ_F32, a.rows),
+                       a, D, max_len);
+  // From nine rows on, the prompt kernel may be faster: it dequantizes a tile of the cache once for 128 or 256 rows,
+  // but its block takes an SM to itself and longer to start.  With heads of 128 values, 32 sequences of 2000 tokens
+  // and 8 kv heads, 16 rows take 51 us here and 74 there, 32 rows 97 and 75; with 8 sequences of 4096 and 4 heads,
+  // 24 rows 32 and 31, 64 rows 52 and 33; with one of 1000 and 8, 48 rows 16.5 and 16.5.  So the estimates
+  // decide, and not the number of rows.
+  if (a.type != FGQ_F32 && a.rows > 8) {
+    const Plan q = plan_kernel(prompt_kernel(D, cache->group, a.rows), a, D, max_len);
+    if (q.us < p.us) p = q;
+  }
+  a.row_tiles = (a.rows + p.k.rows - 1) / p.k.rows;
+  if (p.units * p.chunks > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
+  a.chunk = (int)p.chunk;
+  a.chunks = (int)p.chunks;
+  a.cluster = p.cluster;
   const bool join = a.chunks > 1 && !a.cluster;
   void* tmp = nullptr;
   const int64_t orows = (int64_t)a.B * a.T * a.q_heads;
@@ -121,12 +191,18 @@ fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_
     a.part = static_cast<float*>(tmp);
     a.stats = a.part + (size_t)orows * a.chunks * D;
   }
-  fgq_status st = k.launch(a, (unsigned)(units * a.chunks), s);
-  if (st == FGQ_OK && join) {
+  fgq_status st = p.k.launch(a, (unsigned)(p.units * p.chunks), s);
+  if (st == FGQ_OK && join && a.chunks <= JOIN_FEW) {
+    const int rows = 256 / (D / 4);
+    const dim3 grid((unsigned)((orows + rows - 1) / rows)), block(256);
+    st = after_launch(D == 64    ? launch_pdl(join_few_kernel<64>, grid, block, 0, s, a, p.k.rows, orows)
+                      : D == 128 ? launch_pdl(join_few_kernel<128>, grid, block, 0, s, a, p.k.rows, orows)
+                                 : launch_pdl(join_few_kernel<256>, grid, block, 0, s, a, p.k.rows, orows));
+  } else if (st == FGQ_OK && join) {
     const dim3 grid((unsigned)orows), block(JOIN_THREADS);
-    st = after_launch(D == 64    ? launch_pdl(join_kernel<64>, grid, block, 0, s, a, k.rows)
-                      : D == 128 ? launch_pdl(join_kernel<128>, grid, block, 0, s, a, k.rows)
-                                 : launch_pdl(join_kernel<256>, grid, block, 0, s, a, k.rows));
+    st = after_launch(D == 64    ? launch_pdl(join_kernel<64>, grid, block, 0, s, a, p.k.rows)
+                      : D == 128 ? launch_pdl(join_kernel<128>, grid, block, 0, s, a, p.k.rows)
+                                 : launch_pdl(join_kernel<256>, grid, block, 0, s, a, p.k.rows));
   }
   if (tmp && cudaFreeAsync(tmp, s) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
   return st;

@@ -239,13 +239,13 @@ __device__ __forceinline__ void join_cluster(const AttnArgs& a, int b, int head,
 }
 
 // Blocks of one SM, by registers and shared memory.
-template <int NB, bool SPLIT, int NT>
+template <int NB>
 constexpr int attention_blocks_per_sm() {
   return NB == 8 ? 2 : 3;
 }
 
 template <int NB, int GB, bool SPLIT, int NT>
-__global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPLIT, NT>())
+__global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
     kv_attention_kernel(const __grid_constant__ AttnArgs a) {
   using S = AttnSmem<NB, GB>;
   constexpr int D = S::D, NG = S::NG, ROW = S::ROW, PAR = S::PAR, STAGES = S::STAGES, TILE = S::TILE;
@@ -484,176 +484,176 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB, SPL
     }
 #pragma unroll 1
     for (int step = 0; step < TILE; step += AT_STEP) {
-    const int tok0 = tile0 + step;
-    if (TILE > AT_STEP && tok0 >= hi) break;
-    const uint8_t* kc = ring + st * S::STAGE + step * ROW;
-    const uint8_t* vc = kc + TILE * ROW;
-    const uint32_t* kp = reinterpret_cast<const uint32_t*>(ring + st * S::STAGE + 2 * TILE * ROW) + step * NG;
-    const uint32_t* vp = kp + TILE * NG;
+      const int tok0 = tile0 + step;
+      if (TILE > AT_STEP && tok0 >= hi) break;
+      const uint8_t* kc = ring + st * S::STAGE + step * ROW;
+      const uint8_t* vc = kc + TILE * ROW;
+      const uint32_t* kp = reinterpret_cast<const uint32_t*>(ring + st * S::STAGE + 2 * TILE * ROW) + step * NG;
+      const uint32_t* vp = kp + TILE * NG;
 
-    // scores of tokens 16 mt + g, + 8 for rows 8 nt + 2 t, + 1
-    float x[2][NT][4];
+      // scores of tokens 16 mt + g, + 8 for rows 8 nt + 2 t, + 1
+      float x[2][NT][4];
 #pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-      uint32_t wa[NB], wb[NB];
-      lds_words<NB>(kc + (16 * mt + g) * ROW + t * 4 * NB, wa);
-      lds_words<NB>(kc + (16 * mt + g + 8) * ROW + t * 4 * NB, wb);
-      uint32_t pa[NG], pb[NG];
-      lds_words<NG>(reinterpret_cast<const uint8_t*>(kp + (16 * mt + g) * NG), pa);
-      lds_words<NG>(reinterpret_cast<const uint8_t*>(kp + (16 * mt + g + 8) * NG), pb);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[mt][nt][i] = 0.0f;
-#pragma unroll
-      for (int gi = 0; gi < NG; ++gi) {
-        float acc[NT][4];
+      for (int mt = 0; mt < 2; ++mt) {
+        uint32_t wa[NB], wb[NB];
+        lds_words<NB>(kc + (16 * mt + g) * ROW + t * 4 * NB, wa);
+        lds_words<NB>(kc + (16 * mt + g + 8) * ROW + t * 4 * NB, wb);
+        uint32_t pa[NG], pb[NG];
+        lds_words<NG>(reinterpret_cast<const uint8_t*>(kp + (16 * mt + g) * NG), pa);
+        lds_words<NG>(reinterpret_cast<const uint8_t*>(kp + (16 * mt + g + 8) * NG), pb);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[nt][i] = 0.0f;
+          for (int i = 0; i < 4; ++i) x[mt][nt][i] = 0.0f;
 #pragma unroll
-        for (int jj = 0; jj < GB; ++jj) {
-          const int j = gi * GB + jj;
+        for (int gi = 0; gi < NG; ++gi) {
+          float acc[NT][4];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[nt][i] = 0.0f;
+#pragma unroll
+          for (int jj = 0; jj < GB; ++jj) {
+            const int j = gi * GB + jj;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t va = u ? wa[j] >> 8 : wa[j], vb = u ? wb[j] >> 8 : wb[j];
+              const uint32_t a0 = codes_lo(va), a1 = codes_lo(vb), a2 = codes_hi(va), a3 = codes_hi(vb);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int p = 0; p < NQ; ++p)
+                  mma16816(acc[nt], a0, a1, a2, a3, qf[nt][p][2 * j + u][0], qf[nt][p][2 * j + u][1]);
+            }
+          }
+          const float sa = __uint_as_float(pa[gi] << 16), la = __uint_as_float(pa[gi] & 0xffff0000u);
+          const float sb = __uint_as_float(pb[gi] << 16), lb = __uint_as_float(pb[gi] & 0xffff0000u);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            x[mt][nt][0] = fmaf(la, qsum[nt][gi][0], fmaf(sa, acc[nt][0], x[mt][nt][0]));
+            x[mt][nt][1] = fmaf(la, qsum[nt][gi][1], fmaf(sa, acc[nt][1], x[mt][nt][1]));
+            x[mt][nt][2] = fmaf(lb, qsum[nt][gi][0], fmaf(sb, acc[nt][2], x[mt][nt][2]));
+            x[mt][nt][3] = fmaf(lb, qsum[nt][gi][1], fmaf(sb, acc[nt][3], x[mt][nt][3]));
+          }
+        }
+      }
+      const bool whole = tok0 >= all_lo && tok0 + AT_STEP <= all_hi;
+      if (!whole) {
+#pragma unroll
+        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int tok = tok0 + 16 * mt + g + 8 * (i >> 1);
+              if (tok < see_lo[nt][i & 1] || tok >= see_hi[nt][i & 1]) x[mt][nt][i] = -INFINITY;
+            }
+      }
+
+      // value parameters of this thread's four tokens; tokens past the end, or before the first one seen, hold nothing
+      uint32_t vw[2][2][NG];
+      float smax = 0.0f;
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          lds_words<NG>(reinterpret_cast<const uint8_t*>(vp + (16 * mt + g + 8 * u) * NG), vw[mt][u]);
+          if (!whole && (tok0 + 16 * mt + g + 8 * u >= hi || tok0 + 16 * mt + g + 8 * u < seen))
+#pragma unroll
+            for (int i = 0; i < NG; ++i) vw[mt][u][i] = 0u;
+#pragma unroll
+          for (int i = 0; i < NG; ++i) smax = fmaxf(smax, __uint_as_float(vw[mt][u][i] << 16));
+        }
+
+      bool move = smax > sigma;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          move |= fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u])) > limit[nt][u];
+      if (__any_sync(FULL_MASK, move)) {
+#pragma unroll
+        for (int s = 16; s > 0; s >>= 1) smax = fmaxf(smax, __shfl_xor_sync(FULL_MASK, smax, s));
+        if (smax > sigma)  // the next power of two
+          sigma = __uint_as_float((__float_as_uint(smax) + 0x7fffffu) & 0x7f800000u);
+        const float down = 6.0f - (float)((int)(__float_as_uint(sigma) >> 23) - 127);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            const uint32_t va = u ? wa[j] >> 8 : wa[j], vb = u ? wb[j] >> 8 : wb[j];
-            const uint32_t a0 = codes_lo(va), a1 = codes_lo(vb), a2 = codes_hi(va), a3 = codes_hi(vb);
+            float h = fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u]));
+#pragma unroll
+            for (int s = 16; s >= 4; s >>= 1) h = fmaxf(h, __shfl_xor_sync(FULL_MASK, h, s));
+            if (h > -INFINITY) {
+              top[nt][u] = fmaxf(top[nt][u], h * mul[nt][u]);
+              limit[nt][u] = (top[nt][u] + 8.0f) / mul[nt][u];
+            }
+            const float nr = top[nt][u] - down, f = ex2(ref[nt][u] - nr);
+            ref[nt][u] = nr;
+            l[nt][u] *= f;
+#pragma unroll
+            for (int i = 0; i < NG; ++i) olo[nt][i][u] *= f;
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+#pragma unroll
+              for (int w = 0; w < 2; ++w) {
+                o[nt][j][w][u] *= f;
+                o[nt][j][w][2 + u] *= f;
+              }
+          }
+      }
+
+#pragma unroll
+      for (int mt = 0; mt < 2; ++mt) {
+        uint32_t pf[NT][NG][NQ][2];  // probabilities times value scales as operand columns
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float p[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = ex2(fmaf(x[mt][nt][i], mul[nt][i & 1], -ref[nt][i & 1]));
+          l[nt][0] += p[0] + p[2];
+          l[nt][1] += p[1] + p[3];
+#pragma unroll
+          for (int gi = 0; gi < NG; ++gi) {
+            const float sa = __uint_as_float(vw[mt][0][gi] << 16), sb = __uint_as_float(vw[mt][1][gi] << 16);
+            const float la = fmaf(8.0f, sa, __uint_as_float(vw[mt][0][gi] & 0xffff0000u));  // the codes' centre
+            const float lb = fmaf(8.0f, sb, __uint_as_float(vw[mt][1][gi] & 0xffff0000u));
+            olo[nt][gi][0] = fmaf(p[0], la, fmaf(p[2], lb, olo[nt][gi][0]));
+            olo[nt][gi][1] = fmaf(p[1], la, fmaf(p[3], lb, olo[nt][gi][1]));
+            const float w0 = p[0] * sa, w1 = p[1] * sa, w2 = p[2] * sb, w3 = p[3] * sb;
+            const uint32_t ha = h2(w0, w1), hb = h2(w2, w3);
+            pf[nt][gi][0][0] = movmatrix(ha);
+            pf[nt][gi][0][1] = movmatrix(hb);
+            if constexpr (SPLIT) {
+              const float2 ra = f2(ha), rb = f2(hb);
+              pf[nt][gi][NQ - 1][0] = movmatrix(h2(w0 - ra.x, w1 - ra.y));
+              pf[nt][gi][NQ - 1][1] = movmatrix(h2(w2 - rb.x, w3 - rb.y));
+            }
+          }
+        }
+        // value codes: dimensions 4 g .. 4 g + 3 of each block, tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+        const uint8_t* vr = vc + (16 * mt + 2 * t) * ROW + g * 2 * NB;
+        uint32_t v0[NB / 2], v1[NB / 2], v2[NB / 2], v3[NB / 2];
+        lds_words<NB / 2>(vr, v0);
+        lds_words<NB / 2>(vr + ROW, v1);
+        lds_words<NB / 2>(vr + 8 * ROW, v2);
+        lds_words<NB / 2>(vr + 9 * ROW, v3);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+          const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
+          const uint32_t va = __byte_perm(v0[j >> 1], v1[j >> 1], sel), vb = __byte_perm(v2[j >> 1], v3[j >> 1], sel);
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t ua = w ? va >> 8 : va, ub = w ? vb >> 8 : vb;
+            const uint32_t a0 = centred_lo(ua), a1 = centred_hi(ua), a2 = centred_lo(ub), a3 = centred_hi(ub);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int p = 0; p < NQ; ++p)
-                mma16816(acc[nt], a0, a1, a2, a3, qf[nt][p][2 * j + u][0], qf[nt][p][2 * j + u][1]);
-          }
-        }
-        const float sa = __uint_as_float(pa[gi] << 16), la = __uint_as_float(pa[gi] & 0xffff0000u);
-        const float sb = __uint_as_float(pb[gi] << 16), lb = __uint_as_float(pb[gi] & 0xffff0000u);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          x[mt][nt][0] = fmaf(la, qsum[nt][gi][0], fmaf(sa, acc[nt][0], x[mt][nt][0]));
-          x[mt][nt][1] = fmaf(la, qsum[nt][gi][1], fmaf(sa, acc[nt][1], x[mt][nt][1]));
-          x[mt][nt][2] = fmaf(lb, qsum[nt][gi][0], fmaf(sb, acc[nt][2], x[mt][nt][2]));
-          x[mt][nt][3] = fmaf(lb, qsum[nt][gi][1], fmaf(sb, acc[nt][3], x[mt][nt][3]));
-        }
-      }
-    }
-    const bool whole = tok0 >= all_lo && tok0 + AT_STEP <= all_hi;
-    if (!whole) {
-#pragma unroll
-      for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int tok = tok0 + 16 * mt + g + 8 * (i >> 1);
-            if (tok < see_lo[nt][i & 1] || tok >= see_hi[nt][i & 1]) x[mt][nt][i] = -INFINITY;
-          }
-    }
-
-    // value parameters of this thread's four tokens; tokens past the end, or before the first one seen, hold nothing
-    uint32_t vw[2][2][NG];
-    float smax = 0.0f;
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        lds_words<NG>(reinterpret_cast<const uint8_t*>(vp + (16 * mt + g + 8 * u) * NG), vw[mt][u]);
-        if (!whole && (tok0 + 16 * mt + g + 8 * u >= hi || tok0 + 16 * mt + g + 8 * u < seen))
-#pragma unroll
-          for (int i = 0; i < NG; ++i) vw[mt][u][i] = 0u;
-#pragma unroll
-        for (int i = 0; i < NG; ++i) smax = fmaxf(smax, __uint_as_float(vw[mt][u][i] << 16));
-      }
-
-    bool move = smax > sigma;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        move |= fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u])) > limit[nt][u];
-    if (__any_sync(FULL_MASK, move)) {
-#pragma unroll
-      for (int s = 16; s > 0; s >>= 1) smax = fmaxf(smax, __shfl_xor_sync(FULL_MASK, smax, s));
-      if (smax > sigma)  // the next power of two
-        sigma = __uint_as_float((__float_as_uint(smax) + 0x7fffffu) & 0x7f800000u);
-      const float down = 6.0f - (float)((int)(__float_as_uint(sigma) >> 23) - 127);
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          float h = fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u]));
-#pragma unroll
-          for (int s = 16; s >= 4; s >>= 1) h = fmaxf(h, __shfl_xor_sync(FULL_MASK, h, s));
-          if (h > -INFINITY) {
-            top[nt][u] = fmaxf(top[nt][u], h * mul[nt][u]);
-            limit[nt][u] = (top[nt][u] + 8.0f) / mul[nt][u];
-          }
-          const float nr = top[nt][u] - down, f = ex2(ref[nt][u] - nr);
-          ref[nt][u] = nr;
-          l[nt][u] *= f;
-#pragma unroll
-          for (int i = 0; i < NG; ++i) olo[nt][i][u] *= f;
-#pragma unroll
-          for (int j = 0; j < NB; ++j)
-#pragma unroll
-            for (int w = 0; w < 2; ++w) {
-              o[nt][j][w][u] *= f;
-              o[nt][j][w][2 + u] *= f;
-            }
-        }
-    }
-
-#pragma unroll
-    for (int mt = 0; mt < 2; ++mt) {
-      uint32_t pf[NT][NG][NQ][2];  // probabilities times value scales as operand columns
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        float p[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = ex2(fmaf(x[mt][nt][i], mul[nt][i & 1], -ref[nt][i & 1]));
-        l[nt][0] += p[0] + p[2];
-        l[nt][1] += p[1] + p[3];
-#pragma unroll
-        for (int gi = 0; gi < NG; ++gi) {
-          const float sa = __uint_as_float(vw[mt][0][gi] << 16), sb = __uint_as_float(vw[mt][1][gi] << 16);
-          const float la = fmaf(8.0f, sa, __uint_as_float(vw[mt][0][gi] & 0xffff0000u));  // the codes' centre
-          const float lb = fmaf(8.0f, sb, __uint_as_float(vw[mt][1][gi] & 0xffff0000u));
-          olo[nt][gi][0] = fmaf(p[0], la, fmaf(p[2], lb, olo[nt][gi][0]));
-          olo[nt][gi][1] = fmaf(p[1], la, fmaf(p[3], lb, olo[nt][gi][1]));
-          const float w0 = p[0] * sa, w1 = p[1] * sa, w2 = p[2] * sb, w3 = p[3] * sb;
-          const uint32_t ha = h2(w0, w1), hb = h2(w2, w3);
-          pf[nt][gi][0][0] = movmatrix(ha);
-          pf[nt][gi][0][1] = movmatrix(hb);
-          if constexpr (SPLIT) {
-            const float2 ra = f2(ha), rb = f2(hb);
-            pf[nt][gi][NQ - 1][0] = movmatrix(h2(w0 - ra.x, w1 - ra.y));
-            pf[nt][gi][NQ - 1][1] = movmatrix(h2(w2 - rb.x, w3 - rb.y));
+                mma16816(o[nt][j][w], a0, a1, a2, a3, pf[nt][j / GB][p][0], pf[nt][j / GB][p][1]);
           }
         }
       }
-      // value codes: dimensions 4 g .. 4 g + 3 of each block, tokens 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-      const uint8_t* vr = vc + (16 * mt + 2 * t) * ROW + g * 2 * NB;
-      uint32_t v0[NB / 2], v1[NB / 2], v2[NB / 2], v3[NB / 2];
-      lds_words<NB / 2>(vr, v0);
-      lds_words<NB / 2>(vr + ROW, v1);
-      lds_words<NB / 2>(vr + 8 * ROW, v2);
-      lds_words<NB / 2>(vr + 9 * ROW, v3);
-#pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        const uint32_t sel = (j & 1) ? 0x7632 : 0x5410;
-        const uint32_t va = __byte_perm(v0[j >> 1], v1[j >> 1], sel), vb = __byte_perm(v2[j >> 1], v3[j >> 1], sel);
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const uint32_t ua = w ? va >> 8 : va, ub = w ? vb >> 8 : vb;
-          const uint32_t a0 = centred_lo(ua), a1 = centred_hi(ua), a2 = centred_lo(ub), a3 = centred_hi(ub);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int p = 0; p < NQ; ++p)
-              mma16816(o[nt][j][w], a0, a1, a2, a3, pf[nt][j / GB][p][0], pf[nt][j / GB][p][1]);
-        }
-      }
-    }
 
     }
 
@@ -753,6 +753,9 @@ struct AttnKernel {
   fgq_status (*launch)(const AttnArgs&, unsigned blocks, cudaStream_t);
   int rows, per_sm;  // query rows of a block; blocks an SM holds
   bool clusters;     // chunks may join as a cluster
+  // us of a block's start and end, and the tokens per us that it takes in between (all SMs full): fitted to the
+  // times at 32 sequences of 2000 tokens and 16 of 16384, 8 kv heads; they choose a plan and change no result
+  float start_us, rate;
 };
 
 // The kernel for head_dim = 32 nb, group = 32 gb, fp32 inputs (split) or not, `rows` query rows at hand.

@@ -617,9 +617,9 @@ fgq_status launch_prompt(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
 template <int D, int G>
 AttnKernel pick_prompt(int rows) {
   if constexpr (D <= 128) {
-    if (rows > 128) return {launch_prompt<D, G, 2>, 256, 1, false};
+    if (rows > 128) return {launch_prompt<D, G, 2>, 256, 1, false, 9.0f, D == 64 ? 60.0f : 44.0f};
   }
-  return {launch_prompt<D, G, 1>, 128, 1, false};
+  return {launch_prompt<D, G, 1>, 128, 1, false, 8.0f, D == 64 ? 95.0f : (D == 128 ? 67.0f : 33.0f)};
 }
 
 }  // namespace

@@ -82,6 +82,14 @@ int64_t fgq_debug_set_scratch_limit(int64_t bytes);
 int64_t fgq_debug_set_resident_blocks(int64_t blocks);
 
 /*
+ * Restricts this thread's fgq_kv_attention calls to one kernel: 1, the one that takes 8 or 16 query rows of a
+ * kv head at a time; 2, the one that takes 128 or 256 (fp32 queries, which it does not take, still run on the
+ * first); 0, the default, whichever is expected to be faster.  Returns the previous setting, or -1 for
+ * another value.
+ */
+int fgq_debug_set_attention_kernel(int which);
+
+/*
  * Lets FGQ_PATH_DENSE run calls with fp32 alphas on this thread through the split-fp16
  * ablation (allow != 0), outside the fgq_gemm tolerance; 0 restores FGQ_ERR_UNSUPPORTED.
  * Returns the previous setting.

@@ -26,6 +26,7 @@ thread_local int64_t t_wait_limit_us = -1;
 thread_local int64_t t_scratch_limit = -1;
 thread_local int64_t t_resident_blocks = -1;
 thread_local int t_split_fold = 0;
+thread_local int t_attention_kernel = 0;
 thread_local int t_last_cuda_error = 0;  // cudaError_t of the last failed launch on this thread
 thread_local int t_cta_pairs = 0;        // remembered only: every contraction kernel runs on single CTAs
 thread_local int t_max_ksplit = 8;       // group ranges a G >= 64 tile may be split into
@@ -247,6 +248,8 @@ fgq_status after_launch(cudaError_t launch_result) {
 }
 
 int64_t debug_wait_limit_us() { return t_wait_limit_us; }
+
+int debug_attention_kernel() { return t_attention_kernel; }
 
 int debug_max_ksplit() { return t_max_ksplit; }
 
@@ -744,6 +747,13 @@ int64_t fgq_debug_set_scratch_limit(int64_t bytes) {
 int64_t fgq_debug_set_resident_blocks(int64_t blocks) {
   const int64_t prev = t_resident_blocks;
   t_resident_blocks = blocks < 0 ? -1 : blocks;
+  return prev;
+}
+
+int fgq_debug_set_attention_kernel(int which) {
+  if (which < 0 || which > 2) return -1;
+  const int prev = t_attention_kernel;
+  t_attention_kernel = which;
   return prev;
 }
 

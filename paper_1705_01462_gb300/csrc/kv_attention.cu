@@ -173,9 +173,10 @@ fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_
   // and 8 kv heads, 16 rows take 51 us here and 74 there, 32 rows 97 and 75; with 8 sequences of 4096 and 4 heads,
   // 24 rows 32 and 31, 64 rows 52 and 33; with one of 1000 and 8, 48 rows 16.5 and 16.5.  So the estimates
   // decide, and not the number of rows.
-  if (a.type != FGQ_F32 && a.rows > 8) {
+  const int only = debug_attention_kernel();
+  if (a.type != FGQ_F32 && only != 1 && (a.rows > 8 || only == 2)) {
     const Plan q = plan_kernel(prompt_kernel(D, cache->group, a.rows), a, D, max_len);
-    if (q.us < p.us) p = q;
+    if (q.us < p.us || only == 2) p = q;
   }
   a.row_tiles = (a.rows + p.k.rows - 1) / p.k.rows;
   if (p.units * p.chunks > INT32_MAX) return FGQ_ERR_UNSUPPORTED;

@@ -36,21 +36,21 @@ constexpr int PR_UN = 64;          // tokens of a unit: a softmax step, a dequan
 constexpr int PR_DEQ = 4;          // dequantizing warps of a group
 constexpr int PR_GROUPS = 2;       // groups of them, taking units in turn
 constexpr int PR_E = 16;           // units whose scales are kept: more than any role is ahead of another
-constexpr uint32_t PR_BAR_DEQ = 1;
 
 template <int D, int NQT>
 struct PrCfg {
   static constexpr int BN = D == 256 ? 64 : 128, H = BN / PR_UN;  // tokens and units of a tile
   static constexpr int NSB = NQT == 2 ? 1 : 2;                    // S buffers of a tile of rows
-  static constexpr int STAGES = D == 64 ? 3 : 2;
+  // TMEM: NQT x NSB score buffers, NQT x D sums, and NQT x D / 2 words of queries where there is room
+  static constexpr uint32_t O_COL = NQT * NSB * BN, Q_COL = O_COL + NQT * D;
+  static constexpr bool QT = Q_COL + NQT * D / 2 <= 512;
+  static constexpr uint32_t COLS = Q_COL + (QT ? NQT * D / 2 : 0) <= 256 ? 256 : 512;
+  static constexpr int STAGES = D == 128 && !QT ? 2 : 3;
   static constexpr int Q_TILE = 128 * D * 2, KV_TILE = BN * D * 2;
-  static constexpr int SMEM_Q = NQT * Q_TILE;
+  static constexpr int SMEM_Q = QT ? 0 : NQT * Q_TILE;
   static constexpr int SMEM = 1024 + SMEM_Q + 2 * STAGES * KV_TILE;
   static constexpr int DEQ0 = 4 * NQT, MMA = DEQ0 + PR_GROUPS * PR_DEQ;
   static constexpr int THREADS = 32 * (MMA + 4);
-  // TMEM: NQT x NSB score buffers, then NQT x D sums
-  static constexpr uint32_t O_COL = NQT * NSB * BN;
-  static constexpr uint32_t COLS = O_COL + NQT * D <= 256 ? 256 : 512;
 };
 
 // Registers a thread of the softmax, dequantizing and MMA warpgroups: the last gives up what the others take
@@ -156,12 +156,11 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   using C = PrCfg<D, NQT>;
   constexpr int S = C::STAGES, NB = D / 32, NG = D / G, ROWS = 128 * NQT, BN = C::BN, H = C::H, NSB = C::NSB;
   extern __shared__ uint8_t smem_pr[];
-  __shared__ uint64_t k_full[S], k_empty[S], v_full[S], v_empty[S], s_full[NQT][NSB], drain_bar;
+  __shared__ uint64_t k_full[S], k_empty[S], v_full[S], v_empty[S], s_full[NQT][NSB], q_full, drain_bar;
   __shared__ uint64_t p_full[NQT][2], pv_done[NQT][2];  // by the unit's parity
   __shared__ uint32_t tmem_slot, abort_word;
-  __shared__ float e_k[PR_E];  // 2^ek
-  __shared__ int e_v[PR_E];
-  __shared__ float deq_max[PR_GROUPS][2][2][PR_DEQ];
+  __shared__ __align__(16) float e_k[PR_E][PR_DEQ];  // 2^ek of each 16 tokens
+  __shared__ __align__(16) float e_v[PR_E][PR_DEQ], e_u[PR_E][PR_DEQ];  // ev, 2^-ev
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_pr) + 1023) & ~uintptr_t(1023));
   uint8_t* kbuf = smem + C::SMEM_Q;
   uint8_t* vbuf = kbuf + S * C::KV_TILE;
@@ -214,6 +213,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         mbar_init(&pv_done[q][i], 1);
       }
     }
+    mbar_init(&q_full, 4 * NQT);
     mbar_init(&drain_bar, 1);
     *abort_flag = 0;
     fence_mbar_init();
@@ -223,53 +223,6 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     tmem_relinquish();
   }
 
-  // queries: thread = row, scaled to fp16; what its softmax needs
-  float mul = 0.0f;
-  int see_lo = 0, see_hi = 0;
-  if (warp < C::DEQ0) {
-    const int row = threadIdx.x, r = r0 + row;
-    const bool live = r < a.rows;
-    const int qi = live ? r / a.group : 0, h = live ? r - qi * a.group : 0;
-    const int64_t base = (int64_t)b * a.qbs + (int64_t)qi * a.qts + ((int64_t)head * a.group + h) * D;
-    float mx = 0.0f;
-    if (live) {
-#pragma unroll 4
-      for (int c = 0; c < D / 8; ++c) {
-        float x[8];
-        RawQ<false> raw;
-        raw.load(a, base, c);
-        raw.unpack(a, x);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[i]));
-      }
-    }
-    const int e = mx > 0.0f ? max(-100, min(126, 13 - log2_floor(mx))) : 0;
-    const float up = pow2f(e);
-    uint8_t* qt = smem + (row >> 7) * C::Q_TILE;
-#pragma unroll 4
-    for (int c = 0; c < D / 8; ++c) {
-      float x[8];
-      RawQ<false> raw;
-      raw.zero();
-      if (live) raw.load(a, base, c);
-      raw.unpack(a, x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] *= up;
-      store8(reinterpret_cast<__half*>(qt + tile_off(row & 127, c, 128)), x);
-    }
-    fence_proxy_async_smem();
-    mul = pow2f(-e) * a.scale_log2;
-    if (!live) {  // rows past the last: zero queries, masked nowhere but past the end
-      see_hi = end;
-    } else if (qi < nq) {
-      see_hi = n;
-      if (a.causal) {
-        see_hi = n - nq + qi + 1;
-        if (a.window) see_lo = see_hi - a.window;
-      }
-      see_hi = min(see_hi, end);
-    }
-  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -286,110 +239,116 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     const int tr = lane & 7, u = lane >> 3;  // token of eight, quarter of its row
     constexpr int WPT = NB;                  // 32-bit words of codes a thread takes of a row
     const int32_t* table = a.c.table + (int64_t)b * a.c.max_pages;
-    struct Raw {  // 16 tokens' codes and parameters, two tokens a thread
-      uint32_t kw[2][WPT], vw[2][WPT], kp[2][NG], vp[2][NG];
-    };
-    int page = -1;
+    // 16 tokens' codes and parameters, two tokens a thread (tr and tr + 8), loaded a step ahead
+    uint32_t kw[2][WPT], vw[2][WPT], kp[2][NG], vp[2][NG], vn[2][NG];
+    const uint8_t* const kc0 = a.c.k_codes + tr * (D / 2) + u * 4 * WPT;
+    const uint8_t* const vc0 = a.c.v_codes + tr * (D / 2) + u * 4 * WPT;
+    const uint32_t *const kp0 = a.c.k_params + tr * NG, *const vp0 = a.c.v_params + tr * NG;
+    int page = -1, slot = 0;
+    bool in = false;
     auto look_up = [&](int un) {  // the page of this warp's 16 tokens of unit un
       const int tok = lo + un * PR_UN + 16 * dw;
-      page = -1;
-      if (un < units && tok < hi) page = __ldg(table + page_of(a.c, (uint32_t)tok));
+      in = un < units && tok < hi;
+      if (!in) return;
+      const uint32_t pi = page_of(a.c, (uint32_t)tok);
+      slot = tok - (int)pi * a.c.page_size;
+      page = __ldg(table + pi);
     };
-    auto fetch = [&](int un, Raw& x) {  // zeros where nothing was written
-      const int tok = lo + un * PR_UN + 16 * dw;
-      const bool in = un < units && tok < hi;
-      const bool good = in && page >= 0 && page < a.c.pages;
+    int64_t row0 = 0;
+    bool good = false;
+    auto locate = [&]() {
+      good = in && page >= 0 && page < a.c.pages;
       if (in && !good && lane == 0) record_error(a.err, FGQ_ERR_ARG);
-      const int slot = tok - (int)page_of(a.c, (uint32_t)tok) * a.c.page_size;
-      const int64_t row0 = good ? ((int64_t)page * a.c.kv_heads + head) * a.c.page_size + slot : 0;
+      row0 = ((int64_t)page * a.c.kv_heads + head) * a.c.page_size + slot;
+    };
+    // parameters, zeros for tokens that were never written (so their values are 0 whatever the codes)
+    auto params = [&](const uint32_t* p0, int un, uint32_t (&p)[2][NG]) {
+      const int tok = lo + un * PR_UN + 16 * dw + tr;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const bool ok = good && tok + 8 * k + tr < hi && tok + 8 * k + tr >= seen;
-        const int64_t row = row0 + 8 * k + tr;
 #pragma unroll
-        for (int i = 0; i < WPT; ++i) x.kw[k][i] = x.vw[k][i] = 0u;
-#pragma unroll
-        for (int i = 0; i < NG; ++i) x.kp[k][i] = x.vp[k][i] = 0u;
-        if (ok) {
-          ldg_words<WPT>(a.c.k_codes + row * (D / 2) + u * 4 * WPT, x.kw[k]);
-          ldg_words<WPT>(a.c.v_codes + row * (D / 2) + u * 4 * WPT, x.vw[k]);
-          ldg_words<NG>(a.c.k_params + row * NG, x.kp[k]);
-          ldg_words<NG>(a.c.v_params + row * NG, x.vp[k]);
-        }
+        for (int i = 0; i < NG; ++i) p[k][i] = 0u;
+        if (good && tok + 8 * k < hi && tok + 8 * k >= seen) ldg_words<NG>(p0 + row0 * NG + 8 * k * NG, p[k]);
       }
     };
-    Raw cur, nxt;
+    auto codes = [&](const uint8_t* c0, uint32_t (&w)[2][WPT]) {  // of the block's rows, which lie in one page
+      if (!good) return;
+#pragma unroll
+      for (int k = 0; k < 2; ++k) ldg_words<WPT>(c0 + row0 * (D / 2) + 8 * k * (D / 2), w[k]);
+    };
+#pragma unroll
+    for (int i = 0; i < WPT; ++i) kw[0][i] = kw[1][i] = vw[0][i] = vw[1][i] = 0u;
     look_up(grp);
-    fetch(grp, cur);
+    locate();
+    params(kp0, grp, kp);
+    params(vp0, grp, vp);
+    codes(kc0, kw);
+    codes(vc0, vw);
     look_up(grp + PR_GROUPS);
     int last_ev = -60;
-    bool ok = true;
+    bool ok = tmo != 0;
 #pragma unroll 1
     for (int un = grp; un < units; un += PR_GROUPS) {
-      const int it = un / H, st = it % S, par = (un / PR_GROUPS) & 1;
-      fetch(un + PR_GROUPS, nxt);  // in flight while this unit is converted
-      look_up(un + 2 * PR_GROUPS);
-      // the largest magnitude of the unit's keys and values, over the four warps
-      float mk = 0.0f, mv = 0.0f;
+      const int it = un / H, st = it % S;
+      // the largest |lo| and s of the 16 tokens' keys and values, as bf16 bits: every |value| is below
+      // 2 max(|lo|, 16 s) < 2^(ek + 15)
+      uint32_t mk = 0u, mv = 0u;
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int i = 0; i < NG; ++i) {
-          const float kl = __uint_as_float(cur.kp[k][i] & 0xffff0000u), ks = __uint_as_float(cur.kp[k][i] << 16);
-          const float vl = __uint_as_float(cur.vp[k][i] & 0xffff0000u), vs = __uint_as_float(cur.vp[k][i] << 16);
-          mk = fmaxf(mk, fmaxf(fabsf(kl), fabsf(fmaf(15.0f, ks, kl))));
-          mv = fmaxf(mv, fmaxf(fabsf(vl), fabsf(fmaf(15.0f, vs, vl))));
+          mk = __vmaxu2(mk, kp[k][i] & 0x7fff7fffu);
+          mv = __vmaxu2(mv, vp[k][i] & 0x7fff7fffu);
         }
 #pragma unroll
       for (int o = 1; o < 8; o <<= 1) {
-        mk = fmaxf(mk, __shfl_xor_sync(FULL_MASK, mk, o));
-        mv = fmaxf(mv, __shfl_xor_sync(FULL_MASK, mv, o));
+        mk = __vmaxu2(mk, __shfl_xor_sync(FULL_MASK, mk, o));
+        mv = __vmaxu2(mv, __shfl_xor_sync(FULL_MASK, mv, o));
       }
-      if (lane == 0) {
-        deq_max[grp][par][0][dw] = mk;
-        deq_max[grp][par][1][dw] = mv;
-      }
-      ok = ok && tmo != 0 && mbar_wait_warp(&k_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
-      if (!ok && lane == 0 && !*abort_flag) fail();
-      if (named_bar_or(PR_BAR_DEQ + grp, 32 * PR_DEQ, !ok)) break;
-#pragma unroll
-      for (int i = 0; i < PR_DEQ; ++i) {
-        mk = fmaxf(mk, deq_max[grp][par][0][i]);
-        mv = fmaxf(mv, deq_max[grp][par][1][i]);
-      }
-      const int ek = mk > 0.0f ? min(114, max(-100, log2_floor(mk) - 13)) : 0;
-      const int ev = mv > 0.0f ? min(114, max(-60, log2_floor(mv) - 13)) : last_ev;
+      const int ek = mk ? min(114, max(-100, max((int)(mk >> 23), (int)(mk >> 7 & 255) + 4) - (127 + 13))) : 0;
+      const int ev = mv ? min(114, max(-60, max((int)(mv >> 23), (int)(mv >> 7 & 255) + 4) - (127 + 13))) : last_ev;
       last_ev = ev;
-      if (dw == 0 && lane == 0) {
-        e_k[un % PR_E] = pow2f(ek);
-        e_v[un % PR_E] = ev;
-      }
       const float fk = pow2f(-ek), fv = pow2f(-ev);
       const uint32_t kt = smem_u32(kbuf + st * C::KV_TILE), vt = smem_u32(vbuf + st * C::KV_TILE);
-      const int row0 = un % H * PR_UN + 16 * dw + tr;
+      const int row = un % H * PR_UN + 16 * dw + tr;
+      ok = ok && mbar_wait_warp(&k_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
+      if (!ok) break;
+      if (lane == 0) {
+        e_k[un % PR_E][dw] = pow2f(ek);
+        e_v[un % PR_E][dw] = (float)ev;
+        e_u[un % PR_E][dw] = fv;
+      }
 #pragma unroll
-      for (int k = 0; k < 2; ++k) convert_row<NB, NG, BN>(kt, row0 + 8 * k, u, cur.kw[k], cur.kp[k], fk);
+      for (int k = 0; k < 2; ++k) convert_row<NB, NG, BN>(kt, row + 8 * k, u, kw[k], kp[k], fk);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&k_full[st]);
-      // a warp whose wait expires leaves with its group, at the next unit's barrier
+      // the next unit's, in flight while these values are converted
+      locate();
+      params(kp0, un + PR_GROUPS, kp);
+      params(vp0, un + PR_GROUPS, vn);
+      codes(kc0, kw);
+      look_up(un + 2 * PR_GROUPS);
       ok = mbar_wait_warp(&v_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
-      if (ok) {
+      if (!ok) break;
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          // 16-bit units (2 u, j) and (2 u + 1, j), NB / 2 words apart and in the half that j says, make the word of
-          // eight values; columns stay in the order 0 4 1 5 2 6 3 7 that nibbles come in, and the output puts them right
-          uint32_t w[NB];
+      for (int k = 0; k < 2; ++k) {
+        // 16-bit units (2 u, j) and (2 u + 1, j), NB / 2 words apart and in the half that j says, make the word of
+        // eight values; columns stay in the order 0 4 1 5 2 6 3 7 that nibbles come in, and the output puts them right
+        uint32_t w[NB];
 #pragma unroll
-          for (int j = 0; j < NB; ++j)
-            w[j] = __byte_perm(cur.vw[k][j >> 1], cur.vw[k][NB / 2 + (j >> 1)], (j & 1) ? 0x7632 : 0x5410);
-          convert_row<NB, NG, BN>(vt, row0 + 8 * k, u, w, cur.vp[k], fv);
-        }
+        for (int j = 0; j < NB; ++j)
+          w[j] = __byte_perm(vw[k][j >> 1], vw[k][NB / 2 + (j >> 1)], (j & 1) ? 0x7632 : 0x5410);
+        convert_row<NB, NG, BN>(vt, row + 8 * k, u, w, vp[k], fv);
       }
       fence_proxy_async_smem();
       __syncwarp();
-      if (ok && lane == 0) mbar_arrive(&v_full[st]);
-      cur = nxt;
+      if (lane == 0) mbar_arrive(&v_full[st]);
+      codes(vc0, vw);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int i = 0; i < NG; ++i) vp[k][i] = vn[k][i];
     }
     if (!ok && lane == 0 && !*abort_flag) fail();
   }
@@ -405,17 +364,22 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       return true;
     };
     auto scores = [&](int q, int it) {
+      const uint32_t qa = tmem + C::Q_COL + (uint32_t)(q * (D / 2));
       const uint64_t qd = sdesc_k_sw128(smem_u32(smem + q * C::Q_TILE));
       const uint64_t kd = sdesc_k_sw128(smem_u32(kbuf + it % S * C::KV_TILE));
       const uint32_t d = tmem + (uint32_t)((q * NSB + it % NSB) * BN);
 #pragma unroll
-      for (int k = 0; k < D / 16; ++k)
-        mma_f16(d, qd + (k >> 2) * (128 * 128 / 16) + 2 * (k & 3), kd + (k >> 2) * (BN * 128 / 16) + 2 * (k & 3), idesc_s,
-                k > 0 ? 1u : 0u);
+      for (int k = 0; k < D / 16; ++k) {
+        const uint64_t kk = kd + (k >> 2) * (BN * 128 / 16) + 2 * (k & 3);
+        if (C::QT)
+          mma_f16_ts(d, qa + 8 * k, kk, idesc_s, k > 0 ? 1u : 0u);
+        else
+          mma_f16(d, qd + (k >> 2) * (128 * 128 / 16) + 2 * (k & 3), kk, idesc_s, k > 0 ? 1u : 0u);
+      }
       mma_commit(&s_full[q][it % NSB]);
       if (q == NQT - 1) mma_commit(&k_empty[it % S]);
     };
-    bool ok = keys(0);
+    bool ok = mbar_wait_timed(&q_full, 0, tmo, abort_flag, 0) && keys(0);
     if (ok)
       for (int q = 0; q < NQT; ++q) scores(q, 0);
     for (int it = 0; it < tiles && ok; ++it) {
@@ -467,6 +431,62 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     const int q = warp >> 2;
     const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16;
     const uint32_t ot = tmem + lanes + C::O_COL + (uint32_t)(q * D);
+    // queries: thread = row, scaled to fp16; what its softmax needs
+    const int r = r0 + threadIdx.x;
+    const bool live = r < a.rows;
+    const int qi = live ? r / a.group : 0, h = live ? r - qi * a.group : 0;
+    const int64_t base = (int64_t)b * a.qbs + (int64_t)qi * a.qts + ((int64_t)head * a.group + h) * D;
+    float mx = 0.0f;
+    if (live) {
+#pragma unroll 4
+      for (int c = 0; c < D / 8; ++c) {
+        float x[8];
+        RawQ<false> raw;
+        raw.load(a, base, c);
+        raw.unpack(a, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[i]));
+      }
+    }
+    const int e = mx > 0.0f ? max(-100, min(126, 13 - log2_floor(mx))) : 0;
+    const float up = pow2f(e);
+#pragma unroll 1
+    for (int c = 0; c < D / 32; ++c) {
+      uint32_t w[16];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x[8];
+        RawQ<false> raw;
+        raw.zero();
+        if (live) raw.load(a, base, 4 * c + i);
+        raw.unpack(a, x);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[4 * i + k] = h2(x[2 * k] * up, x[2 * k + 1] * up);
+        if (!C::QT)
+          *reinterpret_cast<uint4*>(smem + q * C::Q_TILE + tile_off((int)threadIdx.x & 127, 4 * c + i, 128)) =
+              make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+      }
+      if (C::QT) tmem_st16_u(tmem + lanes + C::Q_COL + (uint32_t)(q * (D / 2) + 16 * c), w);
+    }
+    if (C::QT)
+      tmem_st_wait();
+    else
+      fence_proxy_async_smem();
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&q_full);
+    const float mul = pow2f(-e) * a.scale_log2;
+    int see_lo = 0, see_hi = 0;
+    if (!live) {  // rows past the last: zero queries, masked nowhere but past the end
+      see_hi = end;
+    } else if (qi < nq) {
+      see_hi = n;
+      if (a.causal) {
+        see_hi = n - nq + qi + 1;
+        if (a.window) see_lo = see_hi - a.window;
+      }
+      see_hi = min(see_hi, end);
+    }
     float ref = AT_M0, l = 0.0f;
     bool ok = true;
 #pragma unroll 1
@@ -483,8 +503,12 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       tmem_ld32(stile + 32, x1);
       tmem_ld_wait_regs(x0);
       reg_fence(x1);
-      const float mk = fmaxf(mul * e_k[un % PR_E], 1e-37f);  // never 0: masked scores are -inf
-      const int ev = e_v[un % PR_E];
+      const float4 ek4 = *reinterpret_cast<const float4*>(e_k[un % PR_E]);
+      const float4 ev4 = *reinterpret_cast<const float4*>(e_v[un % PR_E]);
+      // by 16 tokens; never 0, as masked scores are -inf
+      const float mk[4] = {fmaxf(mul * ek4.x, 1e-37f), fmaxf(mul * ek4.y, 1e-37f), fmaxf(mul * ek4.z, 1e-37f),
+                           fmaxf(mul * ek4.w, 1e-37f)};
+      const float ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
       const int t0 = lo + un * PR_UN;
       if (!__all_sync(FULL_MASK, t0 >= see_lo && t0 + PR_UN <= see_hi)) {
 #pragma unroll
@@ -493,22 +517,24 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           if (t0 + 32 + i < see_lo || t0 + 32 + i >= see_hi) x1[i] = 0xff800000u;
         }
       }
-      float h0 = -INFINITY, h1 = -INFINITY, h2x = -INFINITY, h3 = -INFINITY;
+      float xt = AT_M0;  // the largest x + ev
 #pragma unroll
-      for (int i = 0; i < 32; i += 4) {
-        h0 = fmaxf(h0, fmaxf(__uint_as_float(x0[i]), __uint_as_float(x1[i])));
-        h1 = fmaxf(h1, fmaxf(__uint_as_float(x0[i + 1]), __uint_as_float(x1[i + 1])));
-        h2x = fmaxf(h2x, fmaxf(__uint_as_float(x0[i + 2]), __uint_as_float(x1[i + 2])));
-        h3 = fmaxf(h3, fmaxf(__uint_as_float(x0[i + 3]), __uint_as_float(x1[i + 3])));
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t(&x)[32] = i < 2 ? x0 : x1;
+        float h0 = -INFINITY, h1 = -INFINITY;
+#pragma unroll
+        for (int k = 16 * (i & 1); k < 16 * (i & 1) + 16; k += 4) {
+          h0 = fmaxf(h0, fmaxf(__uint_as_float(x[k]), __uint_as_float(x[k + 1])));
+          h1 = fmaxf(h1, fmaxf(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])));
+        }
+        xt = fmaxf(xt, fmaf(fmaxf(h0, h1), mk[i], ev[i]));
       }
-      h0 = fmaxf(fmaxf(h0, h1), fmaxf(h2x, h3));
       // the products two units back are in (each phase is waited for in its turn: a later one could not be
       // told from it by parity)
       if (un > 1 && !mbar_wait_warp(&pv_done[q][un & 1], ((un >> 1) - 1) & 1, tmo, abort_flag)) {
         ok = false;
         break;
       }
-      const float xt = h0 > -INFINITY ? fmaf(h0, mk, (float)ev) : AT_M0;
       if (__any_sync(FULL_MASK, xt > ref + 14.0f)) {
         const float nr = fmaxf(ref, xt - 6.0f), f = ex2(ref - nr);
         ref = nr;
@@ -531,29 +557,33 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           }
         }
       }
-      const float off = (float)ev - ref;
-      const uint64_t mk2 = pack_f2(mk, mk), off2 = pack_f2(off, off);
-      uint64_t sum0 = 0, sum1 = 0;
+      float sum[4];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        uint32_t(&x)[32] = half ? x1 : x0;
+        const uint32_t(&x)[32] = half ? x1 : x0;
         uint32_t p[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          float a0, a1;
-          unpack_f2(fma_f2(pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), mk2, off2), a0, a1);
-          a0 = ex2(a0);
-          a1 = ex2(a1);
-          uint64_t& sum = i & 1 ? sum1 : sum0;
-          sum = add_f2(sum, pack_f2(a0, a1));
-          p[i] = h2(a0, a1);
+        for (int j = 0; j < 2; ++j) {
+          const float m = mk[2 * half + j], off = ev[2 * half + j] - ref;
+          const uint64_t m2 = pack_f2(m, m), off2 = pack_f2(off, off);
+          uint64_t s2 = 0;
+#pragma unroll
+          for (int i = 8 * j; i < 8 * j + 8; ++i) {
+            float a0, a1;
+            unpack_f2(fma_f2(pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), m2, off2), a0, a1);
+            a0 = ex2(a0);
+            a1 = ex2(a1);
+            s2 = add_f2(s2, pack_f2(a0, a1));
+            p[i] = h2(a0, a1);
+          }
+          float s0, s1;
+          unpack_f2(s2, s0, s1);
+          sum[2 * half + j] = s0 + s1;
         }
         tmem_st16_u(stile + 16 * half, p);
       }
-      float s0, s1;
-      unpack_f2(add_f2(sum0, sum1), s0, s1);
-      const float sum = s0 + s1;
-      l = fmaf(sum, pow2f(-ev), l);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) l = fmaf(sum[i], e_u[un % PR_E][i], l);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
@@ -564,7 +594,6 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     if (!ok && lane == 0 && !*abort_flag) fail();
     if (ok) {
       tc_fence_after();
-      const int r = r0 + threadIdx.x;
       const int64_t orow = out_row(a, b, head, r < a.rows ? r : 0);
       const bool whole = a.chunks == 1;
       const float inv = !whole ? 1.0f : (l > 0.0f ? 1.0f / l : l);  // a row that sees nothing: 0; NaN stays
@@ -608,7 +637,7 @@ template <int D, int G, int NQT>
 fgq_status launch_prompt(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
   using C = PrCfg<D, NQT>;
   static_assert(C::SMEM + 2048 <= 232448, "shared memory budget");
-  static_assert(C::O_COL + NQT * D <= 512, "tensor memory budget");
+  static_assert(C::Q_COL <= 512, "tensor memory budget");
   if (!tc::smem_attr_once<kv_prompt_kernel<D, G, NQT>>(C::SMEM)) return FGQ_ERR_CUDA;
   kv_prompt_kernel<D, G, NQT><<<blocks, C::THREADS, C::SMEM, s>>>(a);
   return after_launch();

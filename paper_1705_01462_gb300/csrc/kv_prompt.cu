@@ -355,15 +355,12 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 
   // ------------------------------------------------------------------ MMA issuer
   if (warp >= C::MMA) setmaxnreg_dec<PrRegs<NQT>::MMA>();
-  if (warp == C::MMA && lane == 0) {
+  if (warp == C::MMA) {
     constexpr uint32_t idesc_s = idesc_f16_f32(128, BN);
     constexpr uint32_t idesc_o = idesc_f16_f32(128, D) | 1u << 16;  // B is MN-major
-    auto keys = [&](int it) {  // K of tile it is there
-      if (!mbar_wait_timed(&k_full[it % S], (it / S) & 1, tmo, abort_flag, 0)) return false;
-      tc_fence_after();
-      return true;
-    };
+    auto wait = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity, tmo, abort_flag); };
     auto scores = [&](int q, int it) {
+      if (!elect_one()) return;
       const uint32_t qa = tmem + C::Q_COL + (uint32_t)(q * (D / 2));
       const uint64_t qd = sdesc_k_sw128(smem_u32(smem + q * C::Q_TILE));
       const uint64_t kd = sdesc_k_sw128(smem_u32(kbuf + it % S * C::KV_TILE));
@@ -379,7 +376,8 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       mma_commit(&s_full[q][it % NSB]);
       if (q == NQT - 1) mma_commit(&k_empty[it % S]);
     };
-    bool ok = mbar_wait_timed(&q_full, 0, tmo, abort_flag, 0) && keys(0);
+    bool ok = tmo != 0 && wait(&q_full, 0) && wait(&k_full[0], 0);
+    tc_fence_after();
     if (ok)
       for (int q = 0; q < NQT; ++q) scores(q, 0);
     for (int it = 0; it < tiles && ok; ++it) {
@@ -387,41 +385,42 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       // products before), or over this tile's once those are issued
       const bool more = it + 1 < tiles;
       if (NSB == 2 && more) {
-        ok = keys(it + 1);
+        ok = wait(&k_full[(it + 1) % S], ((it + 1) / S) & 1);
         if (!ok) break;
+        tc_fence_after();
         for (int q = 0; q < NQT; ++q) scores(q, it + 1);
       }
-      if (!mbar_wait_timed(&v_full[it % S], (it / S) & 1, tmo, abort_flag, 0)) {
-        ok = false;
-        break;
-      }
+      ok = wait(&v_full[it % S], (it / S) & 1);
 #pragma unroll
       for (int q = 0; q < NQT && ok; ++q) {
         const uint32_t o = tmem + C::O_COL + (uint32_t)(q * D);
 #pragma unroll
         for (int h = 0; h < H; ++h) {
           const int un = it * H + h;
-          if (!mbar_wait_timed(&p_full[q][un & 1], (un >> 1) & 1, tmo, abort_flag, 0)) {
-            ok = false;
-            break;
-          }
+          ok = wait(&p_full[q][un & 1], (un >> 1) & 1);
+          if (!ok) break;
           tc_fence_after();
-          const uint64_t vd = sdesc_mn_sw128(smem_u32(vbuf + it % S * C::KV_TILE + h * PR_UN * 128), BN * 128);
-          const uint32_t p = tmem + (uint32_t)((q * NSB + it % NSB) * BN + h * PR_UN);
+          if (elect_one()) {
+            const uint64_t vd = sdesc_mn_sw128(smem_u32(vbuf + it % S * C::KV_TILE + h * PR_UN * 128), BN * 128);
+            const uint32_t p = tmem + (uint32_t)((q * NSB + it % NSB) * BN + h * PR_UN);
 #pragma unroll
-          for (int k = 0; k < PR_UN / 16; ++k)
-            mma_f16_ts(o, p + 8 * k, vd + k * (2048 / 16), idesc_o, un > 0 || k > 0 ? 1u : 0u);
-          mma_commit(&pv_done[q][un & 1]);
+            for (int k = 0; k < PR_UN / 16; ++k)
+              mma_f16_ts(o, p + 8 * k, vd + k * (2048 / 16), idesc_o, un > 0 || k > 0 ? 1u : 0u);
+            mma_commit(&pv_done[q][un & 1]);
+            if (q == NQT - 1 && h == H - 1) mma_commit(&v_empty[it % S]);
+          }
         }
         if (NSB == 1 && ok && more) {
-          if (q == 0) ok = keys(it + 1);
+          if (q == 0) {
+            ok = wait(&k_full[(it + 1) % S], ((it + 1) / S) & 1);
+            tc_fence_after();
+          }
           if (ok) scores(q, it + 1);
         }
       }
-      if (ok) mma_commit(&v_empty[it % S]);
     }
-    if (!ok && !*abort_flag) fail();
-    mma_commit(&drain_bar);
+    if (!ok && lane == 0 && !*abort_flag) fail();
+    if (elect_one()) mma_commit(&drain_bar);
     mbar_wait_bounded(&drain_bar, 0, 1u << 20);
   }
 

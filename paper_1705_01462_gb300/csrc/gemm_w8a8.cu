@@ -226,7 +226,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
     if (!ok && !*abort_flag) fail();
   }
 
-  if (warp == GW_MMA_WARP && lane == 0 && rank == 0) {
+  if (warp == GW_MMA_WARP && rank == 0) {  // converged, an elected lane issues: a divergent one takes 100 clocks an MMA
     const uint32_t idesc = idesc_f16_f32(2 * GW_BM, BN);
     int j = 0;
     bool ok = true;
@@ -234,30 +234,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
       int m0, p0, sp, k0, k1;
       coords(tl, m0, p0, sp, k0, k1);
       const int b = tl & 1;
-      if (!mbar_wait_cluster(&acc_empty[b], ((tl >> 1) & 1) ^ 1, tmo, abort_flag)) {
-        ok = false;
-        break;
-      }
+      ok = __all_sync(FULL_MASK, mbar_wait_cluster(&acc_empty[b], ((tl >> 1) & 1) ^ 1, tmo, abort_flag));
+      if (!ok) break;
       tc_fence_after();
       for (int kt = k0; kt < k1; ++kt, ++j) {
         const int st = j % S;
-        if (!mbar_wait_timed(&full[st], (j / S) & 1, tmo, abort_flag, 0) ||
-            !mbar_wait_cluster(&pfull[st], (j / S) & 1, tmo, abort_flag)) {
-          ok = false;
-          break;
-        }
+        ok = mbar_wait_warp(&full[st], (j / S) & 1, tmo, abort_flag) &&
+             __all_sync(FULL_MASK, mbar_wait_cluster(&pfull[st], (j / S) & 1, tmo, abort_flag));
+        if (!ok) break;
         tc_fence_after();
         const uint32_t A = smem_u32(smem + st * C::STAGE);
         const uint64_t ad = sdesc_k_sw128(A), bd = sdesc_k_sw128(A + C::A_BYTES);
+        if (elect_one()) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-          mma_f16_pair(tmem + (uint32_t)(b * BN), ad + 2 * s, bd + 2 * s, idesc, (kt > k0 || s > 0) ? 1u : 0u);
-        mma_commit_pair(&empty[st]);
+          for (int s = 0; s < 4; ++s)
+            mma_f16_pair(tmem + (uint32_t)(b * BN), ad + 2 * s, bd + 2 * s, idesc, (kt > k0 || s > 0) ? 1u : 0u);
+          mma_commit_pair(&empty[st]);
+        }
       }
-      if (ok) mma_commit_pair(&acc_full[b]);
+      if (ok && elect_one()) mma_commit_pair(&acc_full[b]);
     }
-    if (!ok && !*abort_flag) fail();
-    mma_commit_pair(drain_bar);
+    if (!ok && lane == 0 && !*abort_flag) fail();
+    if (elect_one()) mma_commit_pair(drain_bar);
     mbar_wait_bounded(drain_bar, 0, 1u << 20);
   }
 

@@ -319,19 +319,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
   }
 }
 
-// y from the splits' sums, a block a run of 256 channels of one token.
+// y from the splits' sums: a thread one channel of GW_JOIN tokens, so that their loads are in flight together (512 x 4096,
+// two splits: the whole product 39.0 us with one token a thread, 36.8 with four).
+constexpr int GW_JOIN = 4;
 __global__ void __launch_bounds__(256) join_splits_kernel(const __grid_constant__ GwArgs a) {
   const int64_t n = (int64_t)a.P * a.M;
   const int m = blockIdx.x * 256 + threadIdx.x;
   pdl_wait();
   if (m >= a.M) return;
   const float sw = __ldg(a.wscale + m), bias = a.bias ? __ldg(a.bias + m) : 0.0f;
-  for (int p = blockIdx.y; p < a.P; p += gridDim.y) {
-    const float* src = a.part + (int64_t)p * a.M + m;
-    float v = 0.0f;
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) v += src[s * n];
-    store_typed(a.y, a.ytype, (int64_t)p * a.M + m, fmaf(v, a.scale[p] * sw, bias));
+  for (int64_t p = (int64_t)blockIdx.y * GW_JOIN; p < a.P; p += (int64_t)gridDim.y * GW_JOIN) {
+    float v[GW_JOIN] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+    for (int s = 0; s < a.splits; ++s)
+#pragma unroll
+      for (int i = 0; i < GW_JOIN; ++i)
+        if (p + i < a.P) v[i] += a.part[s * n + (p + i) * a.M + m];
+#pragma unroll
+    for (int i = 0; i < GW_JOIN; ++i)
+      if (p + i < a.P) store_typed(a.y, a.ytype, (p + i) * a.M + m, fmaf(v[i], a.scale[p + i] * sw, bias));
   }
 }
 
@@ -346,7 +352,11 @@ fgq_status launch_gw(const GwArgs& a, int grid, cudaStream_t s) {
 GemmPlan plan_gemm_w8a8(int P, int K, int M) {
   GemmPlan g;
   g.pitch = ((int64_t)K + GW_KT - 1) / GW_KT * GW_KT;
-  g.bn = P > 128 ? 256 : 128;
+  // 128 tokens a tile also where pairs remain for twice as many tiles: an MMA then reads half as much again of shared
+  // memory for its arithmetic, but K is split less or not at all (1000 tokens, 1024 -> 2048: 17.4 us, and 22.6 with
+  // 256; 4096 tokens, 512 -> 512: 14.4 and 18.3; 300 tokens, 8192 -> 2048: 32.9 and 33.1)
+  const int64_t tiles256 = (int64_t)((M + 2 * GW_BM - 1) / (2 * GW_BM)) * ((P + 255) / 256);
+  g.bn = P > 128 && tiles256 * 2 > device_sms() / 2 ? 256 : 128;
   // K split over pairs where there are fewer tiles than half of them, 8 K-tiles each at least
   const int64_t tiles = (int64_t)((M + 2 * GW_BM - 1) / (2 * GW_BM)) * ((P + g.bn - 1) / g.bn), pairs = device_sms() / 2;
   const int64_t by_k = g.pitch / GW_KT / 8;
@@ -385,7 +395,8 @@ fgq_status launch_gemm_w8a8(const GemmPlan& plan, const void* x16, const void* w
   const int grid = 2 * (int)(tiles < pairs ? tiles : pairs);
   fgq_status st = plan.bn == 256 ? launch_gw<256>(a, grid, s) : launch_gw<128>(a, grid, s);
   if (st == FGQ_OK && a.part) {
-    const dim3 jg((unsigned)((M + 255) / 256), (unsigned)(P < 65535 ? P : 65535));
+    const int rows = (P + GW_JOIN - 1) / GW_JOIN;
+    const dim3 jg((unsigned)((M + 255) / 256), (unsigned)(rows < 65535 ? rows : 65535));
     st = after_launch(launch_pdl(join_splits_kernel, jg, dim3(256), 0, s, a));
   }
   return st;

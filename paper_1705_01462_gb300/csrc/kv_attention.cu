@@ -136,12 +136,15 @@ Plan plan_kernel(const AttnKernel& k, const AttnArgs& a, int D, int max_len) {
   best.k = k;
   best.units = (int64_t)a.B * a.c.kv_heads * ((a.rows + k.rows - 1) / k.rows);
   int64_t span = max_len;  // tokens that one block may have to read
-  if (a.window && (int64_t)a.window + k.rows / a.group + 1 < span) span = (int64_t)a.window + k.rows / a.group + 1;
-  span += 15;
+  if (a.window) {  // and from the start of a block of 16
+    if ((int64_t)a.window + k.rows / a.group + 1 < span) span = (int64_t)a.window + k.rows / a.group + 1;
+    span += 15;
+  }
   const int64_t slots = (int64_t)device_sms() * k.per_sm;
   for (int waves = 1; waves <= 8; ++waves) {
     const int64_t want = waves * slots / best.units, n = want > 0 ? want : 1, r = (span + n - 1) / n;
-    const int64_t chunk = r > 512 ? (r + 255) / 256 * 256 : (r + 127) / 128 * 128;  // a tile for each warp
+    const int64_t step = k.clusters && r > 512 ? 256 : 128;  // a tile for each warp; for the prompt kernel's block
+    const int64_t chunk = (r + step - 1) / step * step;
     const int64_t chunks = (span + chunk - 1) / chunk, blocks = best.units * chunks;
     // few chunks that all run at once join as a cluster: no temporary and no second launch.  More blocks than that
     // would wait for eight of them to fit together.  Each of the GPU's eight groups of SMs, which a cluster does

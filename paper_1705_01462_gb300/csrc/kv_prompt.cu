@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     constexpr int WPT = NB;                  // 32-bit words of codes a thread takes of a row
     const int32_t* table = a.c.table + (int64_t)b * a.c.max_pages;
     // 16 tokens' codes and parameters, two tokens a thread (tr and tr + 8), loaded a step ahead
-    uint32_t kw[2][WPT], vw[2][WPT], kp[2][NG], vp[2][NG], vn[2][NG];
+    uint32_t kw[2][WPT], vw[2][WPT], kp[2][NG], vp[2][NG], kn[2][NG], vn[2][NG];
     const uint8_t* const kc0 = a.c.k_codes + tr * (D / 2) + u * 4 * WPT;
     const uint8_t* const vc0 = a.c.v_codes + tr * (D / 2) + u * 4 * WPT;
     const uint32_t *const kp0 = a.c.k_params + tr * NG, *const vp0 = a.c.v_params + tr * NG;
@@ -253,6 +253,18 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       const uint32_t pi = page_of(a.c, (uint32_t)tok);
       slot = tok - (int)pi * a.c.page_size;
       page = __ldg(table + pi);
+    };
+    // the lines of 16 tokens' codes and parameters on their way to L2: with rows of 128 bytes the loads a step
+    // ahead are still waited for (8 rows of 256 values, 32 sequences of 2000 tokens: 113 us, and 103 with this), with
+    // shorter ones they are not (128 values: 60.5 us, and 63.8)
+    auto prefetch = [&]() {
+      if (D < 256 || !in || page < 0 || page >= a.c.pages) return;
+      constexpr int LC = D / 16;  // lines of 16 rows of codes
+      const int64_t r = ((int64_t)page * a.c.kv_heads + head) * a.c.page_size + slot;
+      const uint8_t* c = (lane & LC ? a.c.v_codes : a.c.k_codes) + r * (D / 2) + (lane & (LC - 1)) * 128;
+      const uint32_t* p = (lane & 1 ? a.c.v_params : a.c.k_params) + r * NG + (lane >> 1) * 32;
+      if (lane < 2 * LC) asm volatile("prefetch.global.L2 [%0];" ::"l"(c));
+      if (lane < (NG > 2 ? NG : 2)) asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
     };
     int64_t row0 = 0;
     bool good = false;
@@ -318,15 +330,15 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         e_v[un % PR_E][dw] = (float)ev;
         e_u[un % PR_E][dw] = fv;
       }
+      // the next unit's parameters, and then its codes as registers come free, in flight meanwhile
+      locate();
+      params(kp0, un + PR_GROUPS, kn);
+      params(vp0, un + PR_GROUPS, vn);
 #pragma unroll
       for (int k = 0; k < 2; ++k) convert_row<NB, NG, BN>(kt, row + 8 * k, u, kw[k], kp[k], fk);
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(&k_full[st]);
-      // the next unit's, in flight while these values are converted
-      locate();
-      params(kp0, un + PR_GROUPS, kp);
-      params(vp0, un + PR_GROUPS, vn);
       codes(kc0, kw);
       look_up(un + 2 * PR_GROUPS);
       ok = mbar_wait_warp(&v_empty[st], ((it / S) & 1) ^ 1, tmo, abort_flag);
@@ -345,10 +357,14 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       __syncwarp();
       if (lane == 0) mbar_arrive(&v_full[st]);
       codes(vc0, vw);
+      prefetch();
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int i = 0; i < NG; ++i) vp[k][i] = vn[k][i];
+        for (int i = 0; i < NG; ++i) {
+          kp[k][i] = kn[k][i];
+          vp[k][i] = vn[k][i];
+        }
     }
     if (!ok && lane == 0 && !*abort_flag) fail();
   }
@@ -645,9 +661,9 @@ fgq_status launch_prompt(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
 template <int D, int G>
 AttnKernel pick_prompt(int rows) {
   if constexpr (D <= 128) {
-    if (rows > 128) return {launch_prompt<D, G, 2>, 256, 1, false, 9.0f, D == 64 ? 60.0f : 44.0f};
+    if (rows > 128) return {launch_prompt<D, G, 2>, 256, 1, false, 9.0f, D == 64 ? 73.0f : 54.0f};
   }
-  return {launch_prompt<D, G, 1>, 128, 1, false, 8.0f, D == 64 ? 95.0f : (D == 128 ? 67.0f : 33.0f)};
+  return {launch_prompt<D, G, 1>, 128, 1, false, 8.0f, D == 64 ? 122.0f : (D == 128 ? 93.0f : 47.0f)};
 }
 
 }  // namespace

@@ -129,8 +129,10 @@ struct Plan {
   bool cluster;
 };
 
-// Whole waves of blocks, as many as cost least: a block costs its kernel's start and its tokens, a join kernel 3 us
-// and the partial sums' way to memory and back.
+// Whole waves of blocks, as many as cost least: the kernel's start, each further wave's, the tokens of the blocks that
+// follow one another on an SM, and for a join kernel 3 us and the partial sums' way to memory and back.  (One token,
+// 16 sequences of 16384 tokens, 8 kv heads of 128 values: 80 us in one or two waves, 90 in eight; 32 of 3000: 35 us in
+// one, 41 in two; 40 of 1000 to 8000, 4 kv heads: 51 us in one, 41 in two.)
 Plan plan_kernel(const AttnKernel& k, const AttnArgs& a, int D, int max_len) {
   Plan best = {};
   best.k = k;
@@ -140,7 +142,7 @@ Plan plan_kernel(const AttnKernel& k, const AttnArgs& a, int D, int max_len) {
     if ((int64_t)a.window + k.rows / a.group + 1 < span) span = (int64_t)a.window + k.rows / a.group + 1;
     span += 15;
   }
-  const int64_t slots = (int64_t)device_sms() * k.per_sm;
+  const int64_t sms = device_sms(), slots = sms * k.per_sm;
   for (int waves = 1; waves <= 8; ++waves) {
     const int64_t want = waves * slots / best.units, n = want > 0 ? want : 1, r = (span + n - 1) / n;
     const int64_t step = k.clusters && r > 512 ? 256 : 128;  // a tile for each warp; for the prompt kernel's block
@@ -151,7 +153,12 @@ Plan plan_kernel(const AttnKernel& k, const AttnArgs& a, int D, int max_len) {
     // not cross, may leave chunks - 1 places empty: 24 rows of 256 values over 2 sequences of 20000 tokens, 288
     // blocks in clusters of 6 on 304 places, took 119 us, and 74 as separate blocks.
     const bool cluster = k.clusters && chunks > 1 && chunks <= 8 && blocks + 8 * (chunks - 1) <= slots;
-    float us = (float)((blocks + slots - 1) / slots) * (k.start_us + (float)chunk / k.rate);
+    const int64_t full = blocks / slots, rest = blocks % slots, more = (blocks - 1) / slots;
+    // the last blocks share an SM with fewer others, and run up to twice as fast as three together would
+    const int64_t beside = rest ? (rest + sms - 1) / sms : 0, least = k.per_sm < 2 ? k.per_sm : 2;
+    const float last = rest ? (float)(beside > least ? beside : least) / (float)k.per_sm : 0.0f;
+    // and a twelfth of a chunk, as sequences are seldom all as long and shorter chunks even them out
+    float us = k.start_us + (float)more * k.wave_us + ((float)full + last + 0.08f) * (float)chunk / k.rate;
     if (chunks > 1 && !cluster) us += 3.0f + (float)a.B * a.T * a.q_heads * chunks * D * 8.0f / 4e6f;
     if (waves == 1 || us < best.us) {
       best.chunk = chunk;

@@ -753,9 +753,10 @@ struct AttnKernel {
   fgq_status (*launch)(const AttnArgs&, unsigned blocks, cudaStream_t);
   int rows, per_sm;  // query rows of a block; blocks an SM holds
   bool clusters;     // chunks may join as a cluster
-  // us of a block's start and end, and the tokens per us that it takes in between (all SMs full): fitted to the
-  // times at 32 sequences of 2000 tokens and 16 of 16384, 8 kv heads; they choose a plan and change no result
-  float start_us, rate;
+  // us of the launch and a block's start and end, of those again in each further wave, and the tokens per us that a block
+  // takes in between (all SMs full): fitted to the times at 32 sequences of 2000 tokens and 16 of 16384, 8 kv heads;
+  // they choose a plan and change no result
+  float start_us, wave_us, rate;
 };
 
 // The kernel for head_dim = 32 nb, group = 32 gb, fp32 inputs (split) or not, `rows` query rows at hand.

@@ -34,11 +34,11 @@ template <int NB, int GB>
 AttnKernel pick(bool split, int rows) {
   constexpr int per_sm = attention_blocks_per_sm<NB>();
   constexpr float rate = NB == 2 ? 130.0f : (NB == 4 ? 83.0f : 60.0f);
-  if (split) return {launch_attention<NB, GB, true, 1>, 8, per_sm, true, 8.0f, 0.7f * rate};
+  if (split) return {launch_attention<NB, GB, true, 1>, 8, per_sm, true, 8.0f, 3.5f, 0.7f * rate};
   if constexpr (NB <= 4) {
-    if (rows > 8) return {launch_attention<NB, GB, false, 2>, 16, per_sm, true, 8.0f, (NB == 2 ? 0.9f : 0.55f) * rate};
+    if (rows > 8) return {launch_attention<NB, GB, false, 2>, 16, per_sm, true, 8.0f, 3.5f, (NB == 2 ? 0.9f : 0.55f) * rate};
   }
-  return {launch_attention<NB, GB, false, 1>, 8, per_sm, true, 8.0f, rate};
+  return {launch_attention<NB, GB, false, 1>, 8, per_sm, true, 8.0f, 3.5f, rate};
 }
 
 }  // namespace dec

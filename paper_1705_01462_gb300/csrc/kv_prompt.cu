@@ -661,9 +661,9 @@ fgq_status launch_prompt(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
 template <int D, int G>
 AttnKernel pick_prompt(int rows) {
   if constexpr (D <= 128) {
-    if (rows > 128) return {launch_prompt<D, G, 2>, 256, 1, false, 9.0f, D == 64 ? 73.0f : 54.0f};
+    if (rows > 128) return {launch_prompt<D, G, 2>, 256, 1, false, 9.0f, 9.0f, D == 64 ? 73.0f : 54.0f};
   }
-  return {launch_prompt<D, G, 1>, 128, 1, false, 8.0f, D == 64 ? 122.0f : (D == 128 ? 93.0f : 47.0f)};
+  return {launch_prompt<D, G, 1>, 128, 1, false, 8.0f, 8.0f, D == 64 ? 122.0f : (D == 128 ? 93.0f : 47.0f)};
 }
 
 }  // namespace

@@ -202,5 +202,10 @@ __device__ __forceinline__ float rint_quotient(float a, float b, float inv) {
   return r;
 }
 
+// Every thread of the cluster's blocks; shared memory written before is seen after.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
+}
+
 }  // namespace dec
 }  // namespace fgq

@@ -3,9 +3,11 @@
 // Per group of G values of one token and head: lo = min rounded down to bf16, s = (max - lo) / 15
 // rounded up to bf16, codes round((x - lo) / s).  Eight consecutive values, a 16-byte load of 16-bit
 // elements, make one 32-bit word of a key row, or two 16-bit units of a value row; the G / 8 threads of
-// a group find its extremes by shuffles.  Both kernels move each byte once and are bound by HBM;
-// consecutive threads take consecutive values of the dense side, and the 32 to 128 bytes of a cache
-// row are written by neighbouring threads, so that L2 merges them into whole sectors.
+// a group find its extremes by shuffles.  Both kernels move each byte once; consecutive threads take consecutive
+// values of the dense side, and the 32 to 128 bytes of a cache row are written by neighbouring threads, so that
+// L2 merges them into whole sectors.
+// 4 x 8192 tokens, 8 heads of 128 values, bf16, groups of 64: read-back 41 us; appending 53 us, 174 MB at half
+// the copy rate: its 22 instructions a value keep the issue slots 76% busy (ALU pipe 59%).
 #include <type_traits>
 
 #include "decoder_internal.cuh"

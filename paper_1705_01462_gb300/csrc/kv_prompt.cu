@@ -3,24 +3,32 @@
 //
 // A block takes NQT tiles of 128 query rows (query, head of the group) of one (sequence, kv head) and a
 // chunk of its tokens, BN at a time:
-//   S[128 x BN] = Q K^T        both operands K-major in shared memory (128-byte swizzle), fp32 S in TMEM
+//   S[128 x BN] = Q K^T        K K-major in shared memory (128-byte swizzle), Q the TMEM operand; fp32 S in TMEM
 //   P = 2^(x - r)              one thread a row, 64 tokens (a unit) at a time; P as fp16 over S in TMEM
 //   O[128 x D] += P V          P the TMEM operand, V as it lies, token by token: the MN-major operand
 // K and V are dequantized once per block into shared memory as fp16, so that a value costs its share of
-// 128 NQT rows' arithmetic.  BN = 128 where it fits: at N = 64 an MMA reads its 128 query rows for half the
-// arithmetic, and the scores of 64 tokens took 1500 clocks where 512 are due.  While a tile of rows does its
-// softmax the other one's products run (NQT = 2), or the next scores into a second buffer (NQT = 1).
+// 128 NQT rows' arithmetic.  Queries in TMEM are not read from shared memory again with every tile of keys (32 rows of 32
+// sequences of 2000 tokens, heads of 64 values: 53.5 us, and 57.5 from shared memory; of 128: 69.7 and 75.7); two
+// tiles of rows of 128 values leave no columns for them.  BN = 128 where it fits: an MMA of N = 64 takes nearly as
+// long as one of 128 (with BN = 64, 67.8 and 80.6 us there).  While a tile of rows does its softmax the other
+// one's products run (NQT = 2), or the next scores into a second buffer (NQT = 1).
 //
-// Range.  Queries are scaled by a power of two per row; K and V by a power of two per unit (2^-ek,
-// 2^-ev) that brings their largest magnitude to [2^13, 2^14), so fp16 holds any bf16-ranged cache.  S is
-// multiplied by 2^ek; P takes 2^ev: p = 2^(x + ev - r) against V 2^-ev, and l sums p 2^-ev.  r is a row's
-// largest x + ev at its last move, less 6.  It moves only when exceeded by 8 (as in kv_attention.cuh), and only
-// then is O rescaled, after the products that add to it.
+// Range.  Queries are scaled by a power of two per row; K and V by a power of two per 16 tokens (2^-ek,
+// 2^-ev) that brings their largest magnitude below 2^15, at most a factor of 64, so fp16 holds any
+// bf16-ranged cache and each dequantizing warp works by itself.  S is multiplied by 2^ek; P takes 2^ev: p = 2^(x +
+// ev - r) against V 2^-ev, and l sums p 2^-ev.  r is a row's largest x + ev at its last move, less 6.  It moves only when
+// exceeded by 14 - 6 = 8 (as in kv_attention.cuh), and only then is O rescaled, after the products that add to it.
 // What is rounded: lo + s c, probabilities to fp16 (11 bits); sums and statistics are fp32.
+//
+// What bounds it, 2 x 1024 queries of 32 heads over 4096 to 6144 tokens, 8 kv heads of 128 values, 210 us where the products
+// alone are due 92: tensor pipe 35% busy, ALU 47%, shared memory 38% of the time.  A tile of rows waits for
+// its next scores for a third of the time, as TMEM has room for one buffer of them beside the sums; a block's
+// start (8 us) and the second, partial wave of blocks are the rest.  36 rows of 256 values in a window of 4096: 38 us,
+// dequantization (12 values a clock and SM) and the block's start.
 //
 // Warp roles (one block per SM): warps 0 .. 4 NQT - 1 softmax (TMEM lane = row); the next eight dequantize,
 // in two groups that take units in turn, 16 tokens a warp; the last group of four holds the MMA issuer, which
-// also allocates TMEM.
+// also allocates TMEM (converged, an elected lane issues: from a divergent lane an MMA took 100 clocks, 244 us).
 // Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded, the roles leave their loops, MMAs in
 // flight are waited for, and TMEM is freed.
 #include "kv_attention.cuh"

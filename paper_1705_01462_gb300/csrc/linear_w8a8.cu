@@ -117,7 +117,7 @@ __device__ __forceinline__ uint4 load16(const int8_t* row, int k, int K, const i
 }
 
 // One row of int8 as fp16, by one warp.
-template <bool ALIGNED, bool READONLY>
+template <bool ALIGNED>
 __device__ __forceinline__ void expand_row(const Expand& e, int row, int K, int64_t pitch, int lane) {
   const int8_t* src = e.src + (int64_t)row * K;
   __half* dst = e.dst + (int64_t)row * pitch;
@@ -125,7 +125,7 @@ __device__ __forceinline__ void expand_row(const Expand& e, int row, int K, int6
 #pragma unroll 2
   for (int k = 16 * lane; k < pitch; k += 512) {
     uint32_t h[8];
-    s8_to_h2(load16<ALIGNED, READONLY>(src, k, K, e.src, end), h);
+    s8_to_h2(load16<ALIGNED, true>(src, k, K, e.src, end), h);
     *reinterpret_cast<uint4*>(dst + k) = make_uint4(h[0], h[1], h[2], h[3]);
     *reinterpret_cast<uint4*>(dst + k + 8) = make_uint4(h[4], h[5], h[6], h[7]);
   }
@@ -150,9 +150,9 @@ __global__ void __launch_bounds__(QT_THREADS) quantize_tokens_kernel(const T* __
   if ((int)blockIdx.x >= qblocks) {
     for (int row = ((int)blockIdx.x - qblocks) * QT_WARPS + warp; row < e.rows; row += ((int)gridDim.x - qblocks) * QT_WARPS) {
       if (e.aligned)
-        expand_row<true, true>(e, row, K, pitch, lane);
+        expand_row<true>(e, row, K, pitch, lane);
       else
-        expand_row<false, true>(e, row, K, pitch, lane);
+        expand_row<false>(e, row, K, pitch, lane);
     }
     return;
   }
@@ -290,9 +290,9 @@ __global__ void __launch_bounds__(256) expand_kernel(const __grid_constant__ Exp
     const Expand& e = row < w.rows ? w : q;
     const int r = row < w.rows ? row : row - w.rows;
     if (e.aligned)
-      expand_row<true, true>(e, r, K, pitch, lane);
+      expand_row<true>(e, r, K, pitch, lane);
     else
-      expand_row<false, true>(e, r, K, pitch, lane);
+      expand_row<false>(e, r, K, pitch, lane);
   }
 }
 
@@ -330,7 +330,7 @@ __host__ __device__ constexpr int few_pieces(int K, int splits) { return ((K + 6
 // X: the type of float tokens that the block quantizes itself (a launch and a round trip less), or int8_t for
 // tokens that a kernel before has quantized.
 template <int NT, bool ALIGNED, typename X>
-__global__ void __launch_bounds__(32 * FEW_WARPS, NT >= 8 ? 1 : 2) few_tokens_kernel(const __grid_constant__ FewArgs a) {
+__global__ void __launch_bounds__(32 * FEW_WARPS, 2) few_tokens_kernel(const __grid_constant__ FewArgs a) {
   constexpr bool FLOAT = !std::is_same<X, int8_t>::value;
   constexpr int NP = 8 * NT, AHEAD = NT >= 4 ? 2 : 4;
   extern __shared__ __align__(16) uint8_t few_smem[];
@@ -552,9 +552,11 @@ fgq_status launch_few(FewArgs a, cudaStream_t s) {
   return nt == 1 ? launch_few_nt<1, int8_t>(a, s) : nt == 2 ? launch_few_nt<2, int8_t>(a, s) : launch_few_nt<4, int8_t>(a, s);
 }
 
-// Float tokens that each block quantizes for itself: up to 8 of them, rows that can be loaded eight elements at
-// a time, codes that fit beside the sums; every block has all of the rows' maxima to find, so not too long ones.
-constexpr int FUSED_MAX_P = 8, FUSED_MAX_ELEMS = 32768;
+// Float tokens that each block quantizes for itself: rows that can be loaded eight elements at a time, codes that fit
+// beside the sums, and few elements, as every block has all of the rows' maxima to find.  It saves the caller a
+// launch (1.5 to 2 us of 14 to 16 from Python).  On the device, 4096 -> 4096: one and two tokens 10.4 us either way,
+// four 12.3 and 10.3 with a launch of their own, eight 14.4 and 10.3; four of 2048 -> 2000 8.3 either way.
+constexpr int FUSED_MAX_P = 4, FUSED_MAX_ELEMS = 8192;
 bool fused_fits(const void* x, int type, int P, int K, int M, int64_t ldx) {
   return P <= FUSED_MAX_P && (int64_t)P * K <= FUSED_MAX_ELEMS && K % 8 == 0 && aligned(x, 16) &&
          (P == 1 || stride16(ldx, type)) && 8 * few_row_bytes(few_pieces(K, few_splits(P, K, M, 1))) <= FEW_MAX_CODES;
@@ -567,7 +569,9 @@ fgq_status launch_few_float(FewArgs a, int type, cudaStream_t s) {
 
 inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
-constexpr int FEW_MAX_P = 64;  // tokens up to which the few-token kernel runs
+// Tokens up to which the few-token kernel runs, in us here and on tcgen05: 64 tokens, 4096 -> 4096 19.5 and 25.4, 1024 ->
+// 8192 16.9 and 18.3, 8192 -> 1024 15.3 and 25.0; 80 tokens 29.0 and 25.4, 21.9 and 18.6, 20.6 and 25.2.
+constexpr int FEW_MAX_P = 64;
 
 fgq_status check_product(const void* x, int P, int K, const int8_t* wq, const float* wscale, int M, const float* bias,
                          const void* y, int ytype) {

@@ -554,9 +554,10 @@ fgq_status launch_few(FewArgs a, cudaStream_t s) {
 
 // Float tokens that each block quantizes for itself: rows that can be loaded eight elements at a time, codes that fit
 // beside the sums, and few elements, as every block has all of the rows' maxima to find.  It saves the caller a
-// launch (1.5 to 2 us of 14 to 16 from Python).  On the device, 4096 -> 4096: one and two tokens 10.4 us either way,
-// four 12.3 and 10.3 with a launch of their own, eight 14.4 and 10.3; four of 2048 -> 2000 8.3 either way.
-constexpr int FUSED_MAX_P = 4, FUSED_MAX_ELEMS = 8192;
+// launch and a temporary (calls from Python one after another: four tokens, 2048 -> 2000, 10.9 us, eight 15.4 with a
+// launch of their own).  On the device, 4096 -> 4096: one and two tokens 10.4 us either way, four 12.3 and 10.3, eight
+// 14.4 and 10.3: from there on it costs more than it saves.
+constexpr int FUSED_MAX_P = 8, FUSED_MAX_ELEMS = 16384;
 bool fused_fits(const void* x, int type, int P, int K, int M, int64_t ldx) {
   return P <= FUSED_MAX_P && (int64_t)P * K <= FUSED_MAX_ELEMS && K % 8 == 0 && aligned(x, 16) &&
          (P == 1 || stride16(ldx, type)) && 8 * few_row_bytes(few_pieces(K, few_splits(P, K, M, 1))) <= FEW_MAX_CODES;

@@ -91,7 +91,7 @@ fgq_status fgq_kv_read(const fgq_kv_cache* cache, void* k, void* v, fgq_float_ty
  *            (entries above T count as T).  Query i < q_lens[b] stands at position
  *            seq_lens[b] - q_lens[b] + i.
  *   max_len  an upper bound of seq_lens known on the host (0: max_pages page_size).  It shapes
- *            the launch only; longer sequences are still read whole.
+ *            the launch (and so the order of fp32 sums) only; longer sequences are still read whole.
  *   causal   1: a query sees positions up to its own; 0: all seq_lens[b] positions.
  *   window   with causal, > 0: a query sees at most the last `window` positions, its own among
  *            them; 0: no limit.
@@ -100,7 +100,9 @@ fgq_status fgq_kv_read(const fgq_kv_cache* cache, void* k, void* v, fgq_float_ty
  * Scores, softmax statistics and sums are held in fp32.  The products take fp16 operands: codes
  * are exact; queries are scaled by a power of two per row and are exact for bf16 and fp16 (fp32:
  * two fp16 parts, about 22 bits); probability times value scale is rounded to fp16 (fp32: two
- * parts).  Long runs of bf16 or fp16 queries take keys, values and probabilities as fp16.
+ * parts).  More than eight rows (queries times query heads of a kv head) of bf16 or fp16 queries may
+ * run on a second kernel, where that is the faster; it takes keys, values and probabilities as fp16
+ * (fp16 queries: two parts of a probability).
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad cache or type, kv_heads not dividing
  * q_heads, window < 0, a window without causal), FGQ_ERR_ALIGN as fgq_kv_append (q, out too),
  * FGQ_ERR_UNSUPPORTED (more than 2^31 - 1 blocks of work), FGQ_ERR_CUDA (also where a temporary

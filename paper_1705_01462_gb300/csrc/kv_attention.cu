@@ -185,7 +185,9 @@ fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_
   // 64 rows 10.4 and 12.5.  So the estimates decide, and not the number of rows.
   const int only = debug_attention_kernel();
   if (a.type != FGQ_F32 && only != 1 && (a.rows > 8 || only == 2)) {
-    const Plan q = plan_kernel(prompt_kernel(D, cache->group, a.rows), a, D, max_len);
+    AttnKernel k = prompt_kernel(D, cache->group, a.rows);
+    if (a.type == FGQ_F16) k.rate *= 0.85f;  // a second product with the values
+    const Plan q = plan_kernel(k, a, D, max_len);
     if (q.us < p.us || only == 2) p = q;
   }
   a.row_tiles = (a.rows + p.k.rows - 1) / p.k.rows;

@@ -18,7 +18,11 @@
 // bf16-ranged cache and each dequantizing warp works by itself.  S is multiplied by 2^ek; P takes 2^ev: p = 2^(x +
 // ev - r) against V 2^-ev, and l sums p 2^-ev.  r is a row's largest x + ev at its last move, less 6.  It moves only when
 // exceeded by 14 - 6 = 8 (as in kv_attention.cuh), and only then is O rescaled, after the products that add to it.
-// What is rounded: lo + s c, probabilities to fp16 (11 bits); sums and statistics are fp32.
+// What is rounded: lo + s c and probabilities to fp16 (11 bits); sums and statistics are fp32.  For bf16 outputs that is
+// an eighth of the output's own rounding.  For fp16 outputs the probabilities' would weigh as much as the output's
+// (3.3e-4 of the output in all, where the output's alone is 2.1e-4), so they take a second fp16 part in the other
+// half of their scores' columns, and a second product with V (TWO): 2.1e-4, for 261 us instead of 210 with the queries
+// below, 41 instead of 38 with 36 rows of 256 values.
 //
 // What bounds it, 2 x 1024 queries of 32 heads over 4096 to 6144 tokens, 8 kv heads of 128 values, 210 us where the products
 // alone are due 92: tensor pipe 35% busy, ALU 47%, shared memory 38% of the time.  A tile of rows waits for
@@ -159,7 +163,8 @@ __device__ __forceinline__ void convert_row(uint32_t tile, int row, int u, const
   }
 }
 
-template <int D, int G, int NQT>
+// TWO: probabilities as two fp16 parts.
+template <int D, int G, int NQT, bool TWO>
 __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(const __grid_constant__ AttnArgs a) {
   using C = PrCfg<D, NQT>;
   constexpr int S = C::STAGES, NB = D / 32, NG = D / G, ROWS = 128 * NQT, BN = C::BN, H = C::H, NSB = C::NSB;
@@ -430,6 +435,10 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 #pragma unroll
             for (int k = 0; k < PR_UN / 16; ++k)
               mma_f16_ts(o, p + 8 * k, vd + k * (2048 / 16), idesc_o, un > 0 || k > 0 ? 1u : 0u);
+            if constexpr (TWO) {
+#pragma unroll
+              for (int k = 0; k < PR_UN / 16; ++k) mma_f16_ts(o, p + 32 + 8 * k, vd + k * (2048 / 16), idesc_o, 1u);
+            }
             mma_commit(&pv_done[q][un & 1]);
             if (q == NQT - 1 && h == H - 1) mma_commit(&v_empty[it % S]);
           }
@@ -583,7 +592,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       float sum[4];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const uint32_t(&x)[32] = half ? x1 : x0;
+        uint32_t(&x)[32] = half ? x1 : x0;
         uint32_t p[16];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -598,12 +607,21 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
             a1 = ex2(a1);
             s2 = add_f2(s2, pack_f2(a0, a1));
             p[i] = h2(a0, a1);
+            if constexpr (TWO) {
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p[i]));
+              x[2 * i] = h2(a0 - f.x, a1 - f.y);
+            }
           }
           float s0, s1;
           unpack_f2(s2, s0, s1);
           sum[2 * half + j] = s0 + s1;
         }
         tmem_st16_u(stile + 16 * half, p);
+        if constexpr (TWO) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p[i] = x[2 * i];
+          tmem_st16_u(stile + 32 + 16 * half, p);
+        }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) l = fmaf(sum[i], e_u[un % PR_E][i], l);
@@ -656,14 +674,19 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   }
 }
 
-template <int D, int G, int NQT>
-fgq_status launch_prompt(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
+template <int D, int G, int NQT, bool TWO>
+fgq_status launch_prompt_as(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
   using C = PrCfg<D, NQT>;
   static_assert(C::SMEM + 2048 <= 232448, "shared memory budget");
   static_assert(C::Q_COL <= 512, "tensor memory budget");
-  if (!tc::smem_attr_once<kv_prompt_kernel<D, G, NQT>>(C::SMEM)) return FGQ_ERR_CUDA;
-  kv_prompt_kernel<D, G, NQT><<<blocks, C::THREADS, C::SMEM, s>>>(a);
+  if (!tc::smem_attr_once<kv_prompt_kernel<D, G, NQT, TWO>>(C::SMEM)) return FGQ_ERR_CUDA;
+  kv_prompt_kernel<D, G, NQT, TWO><<<blocks, C::THREADS, C::SMEM, s>>>(a);
   return after_launch();
+}
+
+template <int D, int G, int NQT>
+fgq_status launch_prompt(const AttnArgs& a, unsigned blocks, cudaStream_t s) {
+  return a.type == FGQ_F16 ? launch_prompt_as<D, G, NQT, true>(a, blocks, s) : launch_prompt_as<D, G, NQT, false>(a, blocks, s);
 }
 
 template <int D, int G>

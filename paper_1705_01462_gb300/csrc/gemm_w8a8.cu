@@ -10,16 +10,17 @@
 // Warp roles (one block per SM, persistent over tiles):
 //   warps 0-7  epilogue: warp w reads TMEM lanes 32 (w % 4) .. (channels), columns BN / 2 (w / 4) .. (tokens),
 //              applies scales and bias and stores runs of 32 channels;
-//   warp 8     TMEM allocation; in the pair's first block the MMA issuer, in the second the forwarder, which tells
-//              the first of each K-tile that has arrived;
-//   warp 9     TMA producer of the block's own boxes, on the block's own barriers.
+//   warp 8     TMEM allocation; in the pair's first block the MMA issuer;
+//   warp 9     TMA producer of the block's own boxes, which count on the first block's barrier (the loads' cta_group::2
+//              form), so that one wait covers both blocks' operands.
 // Two accumulators: the epilogue of a tile overlaps the MMAs of the next.  Few tiles split K over pairs
 // (fp32 partial sums, joined with scales and bias by a second kernel).
 // 4096 tokens, 4096 -> 8192, bf16: 179 us for the layer, 20 of them quantization and expansion, where the products
 // alone are due 148; at 2048 tokens, 4096 -> 4096 (50 us) the tensor pipe is active 59% of the time: 128 tiles on
 // 76 pairs are two waves.
-// Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded, each role leaves its loop, copies and
-// MMAs in flight are waited for, the two blocks meet, and TMEM is freed.
+// Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded and each role leaves its loop.  At the end, after an expiry
+// or not, the two blocks meet and tell each other how far they came, the first one waits for the MMAs and for boxes that no
+// MMA has read, they meet again, and TMEM is freed.
 #include <cstring>
 
 #include "linear_internal.cuh"
@@ -42,7 +43,7 @@ struct GwCfg {
   static constexpr int A_BYTES = GW_BM * GW_KT * 2, B_BYTES = BN / 2 * GW_KT * 2, STAGE = A_BYTES + B_BYTES;
   static constexpr int STAGES = BN == 256 ? 6 : 8;
   static constexpr int COLS = 2 * BN;  // TMEM columns: two accumulators
-  static constexpr int SMEM = 1024 + STAGES * STAGE + 8 * (3 * STAGES + 5) + 16;
+  static constexpr int SMEM = 1024 + STAGES * STAGE + 8 * (2 * STAGES + 5) + 32;
 };
 static_assert(GwCfg<256>::SMEM <= 232448 && GwCfg<128>::SMEM <= 232448, "shared memory budget");
 
@@ -70,9 +71,25 @@ __device__ __forceinline__ uint32_t map_rank(const void* p, uint32_t rank) {
   return r;
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-  // what is told of is read by MMAs alone (boxes that a barrier has counted, tensor memory behind
-  // tcgen05's fence): a release of this thread's own writes to the cluster, 1800 clocks, has nothing to release
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// A word at this block's shared address `p`, in the cluster's block `rank`.
+__device__ __forceinline__ uint32_t ld_cluster_u32(const uint32_t* p, uint32_t rank) {
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_rank(p, rank)) : "memory");
+  return v;
+}
+// A box into this block's shared memory whose bytes count on a barrier of the pair, `bar` in either block.
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const void* map, int c0, int c1, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], "
+      "[%4];" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(c0), "r"(c1), "r"(bar)
+      : "memory");
+}
+// Bytes that a phase of this block's barrier expects and that were never sent for.
+__device__ __forceinline__ void mbar_forgo_tx(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
 // mbar_wait_timed for arrivals from the other block, polling: a thread that try_wait has suspended is not woken by
 // them (a K-tile took its whole microsecond).
@@ -136,14 +153,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
   constexpr int S = C::STAGES;
   extern __shared__ uint8_t smem_gw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_gw) + 1023) & ~uintptr_t(1023));
-  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S * C::STAGE);  // this block's boxes have arrived
-  uint64_t* pfull = full + S;     // first block: the second one's have
-  uint64_t* empty = pfull + S;    // the MMAs have read them (both blocks)
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + S * C::STAGE);  // first block: both blocks' boxes have arrived
+  uint64_t* empty = full + S;     // the MMAs have read them (both blocks)
   uint64_t* acc_full = empty + S;     // an accumulator is complete (both blocks)
   uint64_t* acc_empty = acc_full + 2;  // first block: both blocks' epilogues have read it
   uint64_t* drain_bar = acc_empty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
   volatile uint32_t* abort_flag = tmem_slot + 1;
+  uint32_t* came = tmem_slot + 2;  // K-tiles asked for by this block; first block: K-tiles that MMAs were committed for
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const uint64_t tmo = a.timeout_ns;
@@ -151,7 +168,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init(&full[i], 1);
-      mbar_init(&pfull[i], 1);
       mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -199,38 +215,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
           break;
         }
         uint8_t* A = smem + st * C::STAGE;
-        mbar_arrive_expect_tx(&full[st], C::STAGE);
-        tma_load_2d(smem_u32(A), &a.w_map, kt * GW_KT, m0 + GW_BM * (int)rank, &full[st]);
-        tma_load_2d(smem_u32(A + C::A_BYTES), &a.x_map, kt * GW_KT, p0 + BN / 2 * (int)rank, &full[st]);
+        // the second block's bytes may come before they are expected: the phase lasts until this arrival
+        if (rank == 0) mbar_arrive_expect_tx(&full[st], 2 * C::STAGE);
+        const uint32_t bar = map_rank(&full[st], 0);
+        tma_load_2d_pair(smem_u32(A), &a.w_map, kt * GW_KT, m0 + GW_BM * (int)rank, bar);
+        tma_load_2d_pair(smem_u32(A + C::A_BYTES), &a.x_map, kt * GW_KT, p0 + BN / 2 * (int)rank, bar);
       }
     }
     if (!ok && !*abort_flag) fail();
-    // boxes that no MMA consumed may still be in flight
-    for (int i = j - S < 0 ? 0 : j - S; i < j; ++i) mbar_wait_bounded(&full[i % S], (i / S) & 1, 1u << 16);
-  }
-
-  if (warp == GW_MMA_WARP && lane == 0 && rank != 0) {  // the forwarder
-    int j = 0;
-    bool ok = true;
-    for (int tl = 0; tl < my_tiles && ok; ++tl) {
-      int m0, p0, sp, k0, k1;
-      coords(tl, m0, p0, sp, k0, k1);
-      for (int kt = k0; kt < k1; ++kt, ++j) {
-        if (!mbar_wait_timed(&full[j % S], (j / S) & 1, tmo, abort_flag, 0)) {
-          ok = false;
-          break;
-        }
-        mbar_arrive_cluster(map_rank(&pfull[j % S], 0));
-      }
-    }
-    if (!ok && !*abort_flag) fail();
+    came[0] = (uint32_t)j;
   }
 
   if (warp == GW_MMA_WARP && rank == 0) {  // converged, an elected lane issues: a divergent one takes 100 clocks an MMA
     const uint32_t idesc = idesc_f16_f32(2 * GW_BM, BN);
     int j = 0;
     bool ok = true;
-    for (int tl = 0; tl < my_tiles && ok; ++tl) {
+    for (int tl = 0; tl < my_tiles; ++tl) {
       int m0, p0, sp, k0, k1;
       coords(tl, m0, p0, sp, k0, k1);
       const int b = tl & 1;
@@ -239,8 +239,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
       tc_fence_after();
       for (int kt = k0; kt < k1; ++kt, ++j) {
         const int st = j % S;
-        ok = mbar_wait_warp(&full[st], (j / S) & 1, tmo, abort_flag) &&
-             __all_sync(FULL_MASK, mbar_wait_cluster(&pfull[st], (j / S) & 1, tmo, abort_flag));
+        ok = __all_sync(FULL_MASK, mbar_wait_cluster(&full[st], (j / S) & 1, tmo, abort_flag));
         if (!ok) break;
         tc_fence_after();
         const uint32_t A = smem_u32(smem + st * C::STAGE);
@@ -252,11 +251,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
           mma_commit_pair(&empty[st]);
         }
       }
-      if (ok && elect_one()) mma_commit_pair(&acc_full[b]);
+      if (!ok) break;
+      if (elect_one()) mma_commit_pair(&acc_full[b]);
     }
     if (!ok && lane == 0 && !*abort_flag) fail();
     if (elect_one()) mma_commit_pair(drain_bar);
-    mbar_wait_bounded(drain_bar, 0, 1u << 20);
+    if (lane == 0) came[1] = (uint32_t)j;
   }
 
   if (warp < GW_EPI_WARPS) {
@@ -312,7 +312,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
 
   tc_fence_before();
   __syncthreads();
-  cluster_sync();  // the MMAs read both blocks' memory, and arrive on both blocks' barriers
+  cluster_sync();  // both blocks' counts are there
+  if (warp == GW_TMA_WARP && lane == 0 && rank == 0) {
+    auto drain = [](uint64_t* bar, int phase) { mbar_wait_bounded(bar, (uint32_t)phase & 1u, 1u << 20); };
+    drain(drain_bar, 0);
+    // boxes that no MMA has read, S at most as each follows a commit S K-tiles back
+    const int done = (int)came[1], mine = (int)came[0], other = (int)ld_cluster_u32(came, 1);
+    for (int i = done; i < (mine > other ? mine : other); ++i) {
+      if (i >= mine)
+        mbar_arrive_expect_tx(&full[i % S], C::STAGE);
+      else if (i >= other)
+        mbar_forgo_tx(&full[i % S], C::STAGE);
+      drain(&full[i % S], i / S);
+    }
+  }
+  cluster_sync();  // the MMAs read both blocks' memory
   if (warp == GW_MMA_WARP) {
     tc_fence_after();
     tmem_dealloc2(tmem, C::COLS);

@@ -19,8 +19,9 @@
 // alone are due 148; at 2048 tokens, 4096 -> 4096 (50 us) the tensor pipe is active 59% of the time: 128 tiles on
 // 76 pairs are two waves.
 // Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded and each role leaves its loop.  At the end, after an expiry
-// or not, the two blocks meet and tell each other how far they came, the first one waits for the MMAs and for boxes that no
-// MMA has read, they meet again, and TMEM is freed.
+// or not, the two blocks meet and tell each other how far they came, each waits for every arrival that the MMAs' commits still
+// make on its barriers and the first one for boxes that no MMA has read, they meet again, and TMEM is freed: nothing is
+// on its way to a block that has left.
 #include <cstring>
 
 #include "linear_internal.cuh"
@@ -160,7 +161,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
   uint64_t* drain_bar = acc_empty + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
   volatile uint32_t* abort_flag = tmem_slot + 1;
-  uint32_t* came = tmem_slot + 2;  // K-tiles asked for by this block; first block: K-tiles that MMAs were committed for
+  uint32_t* came = tmem_slot + 2;  // K-tiles asked for by this block; first block: K-tiles, and tiles, that MMAs were committed for
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const uint64_t tmo = a.timeout_ns;
@@ -228,9 +229,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
 
   if (warp == GW_MMA_WARP && rank == 0) {  // converged, an elected lane issues: a divergent one takes 100 clocks an MMA
     const uint32_t idesc = idesc_f16_f32(2 * GW_BM, BN);
-    int j = 0;
+    int j = 0, tl = 0;
     bool ok = true;
-    for (int tl = 0; tl < my_tiles; ++tl) {
+    for (; tl < my_tiles; ++tl) {
       int m0, p0, sp, k0, k1;
       coords(tl, m0, p0, sp, k0, k1);
       const int b = tl & 1;
@@ -256,7 +257,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
     }
     if (!ok && lane == 0 && !*abort_flag) fail();
     if (elect_one()) mma_commit_pair(drain_bar);
-    if (lane == 0) came[1] = (uint32_t)j;
+    if (lane == 0) {
+      came[1] = (uint32_t)j;
+      came[2] = (uint32_t)tl;
+    }
   }
 
   if (warp < GW_EPI_WARPS) {
@@ -313,20 +317,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
   tc_fence_before();
   __syncthreads();
   cluster_sync();  // both blocks' counts are there
-  if (warp == GW_TMA_WARP && lane == 0 && rank == 0) {
+  if (warp == GW_TMA_WARP && lane == 0) {
     auto drain = [](uint64_t* bar, int phase) { mbar_wait_bounded(bar, (uint32_t)phase & 1u, 1u << 20); };
+    const int done = (int)ld_cluster_u32(came + 1, 0), tiles = (int)ld_cluster_u32(came + 2, 0);
+    for (int i = done > S ? done - S : 0; i < done; ++i) drain(&empty[i % S], i / S);
+    for (int i = tiles > 2 ? tiles - 2 : 0; i < tiles; ++i) drain(&acc_full[i & 1], i >> 1);
     drain(drain_bar, 0);
-    // boxes that no MMA has read, S at most as each follows a commit S K-tiles back
-    const int done = (int)came[1], mine = (int)came[0], other = (int)ld_cluster_u32(came, 1);
-    for (int i = done; i < (mine > other ? mine : other); ++i) {
-      if (i >= mine)
-        mbar_arrive_expect_tx(&full[i % S], C::STAGE);
-      else if (i >= other)
-        mbar_forgo_tx(&full[i % S], C::STAGE);
-      drain(&full[i % S], i / S);
+    if (rank == 0) {  // boxes that no MMA has read, S at most as each follows a commit S K-tiles back
+      const int mine = (int)came[0], other = (int)ld_cluster_u32(came, 1);
+      for (int i = done; i < (mine > other ? mine : other); ++i) {
+        if (i >= mine)
+          mbar_arrive_expect_tx(&full[i % S], C::STAGE);
+        else if (i >= other)
+          mbar_forgo_tx(&full[i % S], C::STAGE);
+        drain(&full[i % S], i / S);
+      }
     }
   }
-  cluster_sync();  // the MMAs read both blocks' memory
+  cluster_sync();  // and nothing is on its way to either
   if (warp == GW_MMA_WARP) {
     tc_fence_after();
     tmem_dealloc2(tmem, C::COLS);

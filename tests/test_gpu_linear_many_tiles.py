@@ -13,9 +13,10 @@ pytestmark = pytest.mark.gpu
 
 
 # 76 pairs, tiles of 256 channels.  Tiles of 256 tokens: 9 x 8 = 72, one a pair; 17 x 11 = 187, two or three a pair, in
-# five and in nine K-tiles, so that the ring of six stages is in another phase at each tile; 79 x 2 = 158.  Tiles of 128 tokens
-# run where there are at most 38 of 256, so a pair never has more than one of those.
-@pytest.mark.parametrize("P,K,M", [(2100, 200, 1800), (4100, 264, 2700), (4097, 576, 2561), (20000, 72, 300), (9000, 65, 257)])
+# five and in nine K-tiles, so that the ring of six stages is in another phase at each tile; 79 x 2 = 158.  Tiles of 128
+# tokens (up to 128 tokens, or at most 38 tiles of 256): 80 and 157 of them.
+@pytest.mark.parametrize("P,K,M", [(2100, 200, 1800), (4100, 264, 2700), (4097, 576, 2561), (20000, 72, 300), (9000, 65, 257),
+                                   (100, 264, 20300), (128, 72, 40001)])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_product(P, K, M, dtype):
     rng = np.random.default_rng(P + K + M)
@@ -80,3 +81,27 @@ def test_wait_expiry_with_several_tiles():
     for _ in range(3):
         assert torch.equal(fgq.fgq_linear_w8a8(x, w, s), want)
     assert fgq.fgq_stream_status() == fgq.FGQ_OK
+
+
+def test_calls_in_quick_succession():
+    """Blocks of the next call, and of another kernel with as much shared memory, start where a pair has just left: nothing that
+    the pair had under way may reach them."""
+    g = torch.Generator(device=dev())
+    g.manual_seed(4)
+    calls = []
+    for P, K, M in ((700, 520, 1800), (4100, 264, 2700), (130, 1024, 260)):
+        x = torch.randn((P, K), generator=g, device=dev()).to(torch.bfloat16)
+        w = torch.randint(-127, 128, (M, K), generator=g, device=dev(), dtype=torch.int8)
+        calls.append((x, w, torch.ones(M, device=dev())))
+    cache = R.Cache(np.random.default_rng(4), 1, [600], 1, 128, 64, 16)
+    cache_t, table = cache.tensors(dev())
+    q = torch.randn((1, 600, 4, 128), generator=g, device=dev()).to(torch.bfloat16)
+    n = torch.tensor([600], dtype=torch.int32, device=dev())
+
+    def all_of_them():
+        return [fgq.fgq_linear_w8a8(*c) for c in calls] + [fgq.fgq_kv_attention(q, fgq.KVCache(*cache_t), table, n)]
+    want = all_of_them()
+    got = [all_of_them() for _ in range(50)]
+    assert fgq.fgq_stream_status() == fgq.FGQ_OK
+    for ys in got:
+        assert all(torch.equal(a, b) for a, b in zip(ys, want))

@@ -62,6 +62,7 @@ struct AttnArgs {
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;  // tokens a warp computes at a time
 constexpr float AT_M0 = -1e30f;
+constexpr float AT_EMPTY = -INFINITY;  // in place of a reference: a cluster's chunk without work, whose sums were never written
 
 // Shared memory of one ring stage: TILE rows of key codes, value codes, key and value parameters.  Tiles of 64
 // tokens where they fit: bulk copies are the fewer and the larger for it (524 k copies of 1 KB and 128 bytes
@@ -228,12 +229,12 @@ __device__ __forceinline__ void join_cluster(const AttnArgs& a, int b, int head,
     float m[8], mm = AT_M0, ll = 0.0f, v = 0.0f;
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
-      m[c] = c < a.chunks ? ld_cluster(js + 2 * row, c) : AT_M0;
+      m[c] = c < a.chunks ? ld_cluster(js + 2 * row, c) : AT_EMPTY;
       mm = fmaxf(mm, m[c]);
     }
 #pragma unroll
     for (int c = 0; c < 8; ++c)
-      if (m[c] != AT_M0) {  // not a chunk without work: its sums were never written
+      if (m[c] != AT_EMPTY) {
         const float f = ex2(m[c] - mm);
         ll = fmaf(f, ld_cluster(js + 2 * row + 1, c), ll);
         v = fmaf(f, ld_cluster(jo + row * D + d, c), v);
@@ -301,7 +302,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
   float* js = jo + AT_WARPS * NR * D;          // [warp][row][2]: r, l
   if (lo >= hi) {  // nothing here: zero output where there is one chunk only, else the join skips it
     if (a.cluster) {
-      if (threadIdx.x < NR) js[2 * threadIdx.x] = AT_M0;
+      if (threadIdx.x < NR) js[2 * threadIdx.x] = AT_EMPTY;
       cluster_sync();
       join_cluster<NB, NR>(a, b, head, r0, jo, js, ch);
       cluster_sync();

@@ -97,7 +97,7 @@ fgq_status fgq_kv_read(const fgq_kv_cache* cache, void* k, void* v, fgq_float_ty
  *            them; 0: no limit.
  *   out      elements of `type`, [B][T][q_heads][head_dim] contiguous, fully written.  A query
  *            that sees nothing, and i >= q_lens[b], give zeros (whatever they hold).  A head of a
- *            query that holds NaN and sees something gives NaN.
+ *            query that holds NaN or Inf and sees something gives NaN.
  * Scores, softmax statistics and sums are held in fp32.  The products take fp16 operands: codes
  * are exact; queries are scaled by a power of two per row and are exact for bf16 and fp16 (fp32:
  * two fp16 parts, about 22 bits); probability times value scale is rounded to fp16 (fp32: two

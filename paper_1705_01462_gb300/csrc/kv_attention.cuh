@@ -175,6 +175,10 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t at, float v
     static_cast<__half*>(a.out)[at] = __float2half_rn(v);
 }
 
+// What the elements of a query row with largest magnitude mx are multiplied by, 2^e; NaN for a row that holds Inf or NaN: no
+// softmax of its scores is defined, and scores of one infinity would pass for a row that sees nothing.
+__device__ __forceinline__ float row_scale(float mx, int e) { return nonfinite(mx) ? __uint_as_float(0x7fc00000u) : pow2f(e); }
+
 // Tokens of sequence b: at most what the table can hold (more is an error), less than 2^31 - 2^12.
 __device__ __forceinline__ int seq_len(const AttnArgs& a, int b) {
   const int n = __ldg(a.seq_lens + b);
@@ -394,13 +398,13 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
     for (int j = 0; j < NB; ++j) {
       qraw[nt][j].unpack(a, x[j]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[j][i]));
+      for (int i = 0; i < 8; ++i) mx = max_nan(mx, fabsf(x[j][i]));
     }
-    mx = fmaxf(mx, __shfl_xor_sync(FULL_MASK, mx, 1));
-    mx = fmaxf(mx, __shfl_xor_sync(FULL_MASK, mx, 2));
+    mx = max_nan(mx, __shfl_xor_sync(FULL_MASK, mx, 1));
+    mx = max_nan(mx, __shfl_xor_sync(FULL_MASK, mx, 2));
     // the row's largest query to [2^13, 2^14)
     const int e = mx > 0.0f ? max(-100, min(126, 13 - (int)((__float_as_uint(mx) >> 23) & 255) + 127)) : 0;
-    const float up = pow2f(e);
+    const float up = row_scale(mx, e);
     float sums[NG];
 #pragma unroll
     for (int i = 0; i < NG; ++i) sums[i] = 0.0f;

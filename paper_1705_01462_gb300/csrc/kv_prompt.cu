@@ -477,11 +477,11 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         raw.load(a, base, c);
         raw.unpack(a, x);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) mx = fmaxf(mx, fabsf(x[i]));
+        for (int i = 0; i < 8; ++i) mx = max_nan(mx, fabsf(x[i]));
       }
     }
     const int e = mx > 0.0f ? max(-100, min(126, 13 - log2_floor(mx))) : 0;
-    const float up = pow2f(e);
+    const float up = row_scale(mx, e);
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
       uint32_t w[16];

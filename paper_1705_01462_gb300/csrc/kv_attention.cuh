@@ -21,10 +21,12 @@
 // their sums off, so SPLIT adds each step's products to the output rounded (51 x 42000 tokens: 1.1e-5 of the
 // output to 6e-7, 207 to 222 us), which would not show in 16-bit outputs.
 //
-// Softmax.  Probabilities are held as 2^(x - r): r is a row's largest score so far (in log2 units), less
-// 6 - log2(sigma) for the power of two sigma at or above every value scale met, so that p s fits fp16
-// whatever the values' magnitude.  r moves only when a score exceeds its maximum by more than 8, or a
-// value scale sigma: the common tile needs one vote instead of a reduction per row.
+// Softmax.  Probabilities are held as 2^(mul (x - r) + 6 - log2(sigma)): x is a score before its scaling, mul the row's factor
+// to log2 units, r the row's largest x at its last move, and sigma a power of two at or above every value scale met, so that
+// p s fits fp16 whatever the values' magnitude.  r moves only when a score exceeds it by more than 8 / mul, or a value
+// scale sigma: the common tile needs one vote instead of a reduction per row.  The difference comes before the product, as
+// mul x - mul r in one multiply-add is off by the rounding of mul r, which scores past 2^25 turn into infinities or zeros.  Sums
+// leave a warp without their 2^(6 - log2(sigma)), so that a join meets no factor but the scores'.
 //
 // Split.  A block of 4 warps takes `chunk` tokens of one (sequence, kv head, tile of 8 NT query rows);
 // each warp streams every fourth tile through a ring of bulk copies of its own (no barrier
@@ -61,7 +63,8 @@ struct AttnArgs {
 
 constexpr int AT_WARPS = 4;
 constexpr int AT_STEP = 32;  // tokens a warp computes at a time
-constexpr float AT_M0 = -1e30f;
+constexpr float AT_M0 = -3.4e38f;   // reference of a row that has seen nothing
+constexpr float AT_TOP = 3.39e38f;  // largest magnitude of the others, in log2 units
 constexpr float AT_EMPTY = -INFINITY;  // in place of a reference: a cluster's chunk without work, whose sums were never written
 
 // Shared memory of one ring stage: TILE rows of key codes, value codes, key and value parameters.  Tiles of 64
@@ -175,6 +178,10 @@ __device__ __forceinline__ void store_out(const AttnArgs& a, int64_t at, float v
     static_cast<__half*>(a.out)[at] = __float2half_rn(v);
 }
 
+// Exponent e of the power of two that takes a query row's largest magnitude mx to [2^13, 2^14) (below it for subnormal ones).
+__device__ __forceinline__ int row_exponent(float mx) {
+  return mx > 0.0f ? max(-114, min(126, 13 + 127 - (int)((__float_as_uint(mx) >> 23) & 255))) : 0;
+}
 // What the elements of a query row with largest magnitude mx are multiplied by, 2^e; NaN for a row that holds Inf or NaN: no
 // softmax of its scores is defined, and scores of one infinity would pass for a row that sees nothing.
 __device__ __forceinline__ float row_scale(float mx, int e) { return nonfinite(mx) ? __uint_as_float(0x7fc00000u) : pow2f(e); }
@@ -402,8 +409,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
     }
     mx = max_nan(mx, __shfl_xor_sync(FULL_MASK, mx, 1));
     mx = max_nan(mx, __shfl_xor_sync(FULL_MASK, mx, 2));
-    // the row's largest query to [2^13, 2^14)
-    const int e = mx > 0.0f ? max(-100, min(126, 13 - (int)((__float_as_uint(mx) >> 23) & 255) + 127)) : 0;
+    const int e = row_exponent(mx);
     const float up = row_scale(mx, e);
     float sums[NG];
 #pragma unroll
@@ -432,7 +438,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
       sums[i] += __shfl_xor_sync(FULL_MASK, sums[i], 2);
       sums[i] *= 0.001953125f;  // 2^-9: the codes' scale
     }
-    const float m = fmaxf(pow2f(-e) * a.scale_log2 * 512.0f, 1e-37f);
+    const float m = fminf(fmaxf(pow2f(-e) * a.scale_log2 * 512.0f, 1e-37f), AT_TOP);  // finite: 0 m is 0
     // positions of the row: [sl, sh)
     int sl = 0, sh = live ? 0 : INT32_MAX;  // rows past the last: zero queries, masked nowhere
     if (live && qi < nq) {
@@ -460,13 +466,13 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
     all_hi = min(all_hi, __shfl_xor_sync(FULL_MASK, all_hi, o));
   }
 
-  // sums of 2^(x - ref) times codes, times lo, and alone; a row's ref moves when a raw score passes its limit
-  float o[NT][NB][2][4], olo[NT][NG][2], l[NT][2], top[NT][2], ref[NT][2], limit[NT][2];
+  // sums of 2^(mul (x - r) + off) times codes, times lo, and alone; a row's -r, which moves when a score passes its limit
+  float o[NT][NB][2][4], olo[NT][NG][2], l[NT][2], nref[NT][2], limit[NT][2];
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      top[nt][u] = ref[nt][u] = AT_M0;
+      nref[nt][u] = -AT_M0;
       limit[nt][u] = -INFINITY;
       l[nt][u] = 0.0f;
 #pragma unroll
@@ -480,6 +486,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
         for (int i = 0; i < 4; ++i) o[nt][j][u][i] = 0.0f;
   }
   float sigma = 8.6736174e-19f;  // 2^-60; a power of two at or above every value scale met so far
+  float off = 66.0f;             // 6 - log2(sigma)
 
   bool ok = true;
   int done = 0, tile0 = lo + warp * TILE, st = 0;
@@ -585,7 +592,8 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
         for (int s = 16; s > 0; s >>= 1) smax = fmaxf(smax, __shfl_xor_sync(FULL_MASK, smax, s));
         if (smax > sigma)  // the next power of two
           sigma = __uint_as_float((__float_as_uint(smax) + 0x7fffffu) & 0x7f800000u);
-        const float down = 6.0f - (float)((int)(__float_as_uint(sigma) >> 23) - 127);
+        const float now = 6.0f - (float)((int)(__float_as_uint(sigma) >> 23) - 127), by = now - off;
+        off = now;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -593,12 +601,9 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
             float h = fmaxf(fmaxf(x[0][nt][u], x[0][nt][2 + u]), fmaxf(x[1][nt][u], x[1][nt][2 + u]));
 #pragma unroll
             for (int s = 16; s >= 4; s >>= 1) h = fmaxf(h, __shfl_xor_sync(FULL_MASK, h, s));
-            if (h > -INFINITY) {
-              top[nt][u] = fmaxf(top[nt][u], h * mul[nt][u]);
-              limit[nt][u] = (top[nt][u] + 8.0f) / mul[nt][u];
-            }
-            const float nr = top[nt][u] - down, f = ex2(ref[nt][u] - nr);
-            ref[nt][u] = nr;
+            const float nr = fminf(nref[nt][u], -h), f = ex2(fmaf(nr - nref[nt][u], mul[nt][u], by));
+            nref[nt][u] = nr;
+            if (h > -INFINITY) limit[nt][u] = __fadd_rd(8.0f / mul[nt][u], -nr);
             l[nt][u] *= f;
 #pragma unroll
             for (int i = 0; i < NG; ++i) olo[nt][i][u] *= f;
@@ -618,8 +623,13 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float p[4];
+          const uint64_t nr2 = pack_f2(nref[nt][0], nref[nt][1]), m2 = pack_f2(mul[nt][0], mul[nt][1]), off2 = pack_f2(off, off);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = ex2(fmaf(x[mt][nt][i], mul[nt][i & 1], -ref[nt][i & 1]));
+          for (int i = 0; i < 4; i += 2) {
+            unpack_f2(fma_f2(add_f2(pack_f2(x[mt][nt][i], x[mt][nt][i + 1]), nr2), m2, off2), p[i], p[i + 1]);
+            p[i] = ex2(p[i]);
+            p[i + 1] = ex2(p[i + 1]);
+          }
           l[nt][0] += p[0] + p[2];
           l[nt][1] += p[1] + p[3];
 #pragma unroll
@@ -704,17 +714,20 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
           for (int i = 0; i < NG; ++i) olo[nt][i][u] += __shfl_xor_sync(FULL_MASK, olo[nt][i][u], s);
         }
         const int row = 8 * nt + 2 * t + u;
+        // r in log2 units; its rounding goes into the sums (past 2^24 there are no fractions left to keep)
+        const float ref = fminf(fmaxf(-nref[nt][u] * mul[nt][u], -AT_TOP), AT_TOP), lost = fmaf(-nref[nt][u], mul[nt][u], -ref);
+        const float back = ex2(fabsf(lost) <= 1.0f ? lost : 0.0f) * pow2f(-(int)off);
         float* dst = jo + (warp * NR + row) * D;
 #pragma unroll
         for (int j = 0; j < NB; ++j)
 #pragma unroll
           for (int w = 0; w < 2; ++w)
             *reinterpret_cast<float2*>(dst + 32 * j + 4 * g + 2 * w) =
-                make_float2(fmaf(o[nt][j][w][u], 512.0f, olo[nt][j / GB][u]),  // 2^9: the codes' scale
-                            fmaf(o[nt][j][w][2 + u], 512.0f, olo[nt][j / GB][u]));
+                make_float2(fmaf(o[nt][j][w][u], 512.0f, olo[nt][j / GB][u]) * back,  // 2^9: the codes' scale
+                            fmaf(o[nt][j][w][2 + u], 512.0f, olo[nt][j / GB][u]) * back);
         if (g == 0) {
-          js[(warp * NR + row) * 2] = ref[nt][u];
-          js[(warp * NR + row) * 2 + 1] = l[nt][u];
+          js[(warp * NR + row) * 2] = nref[nt][u] == -AT_M0 ? AT_M0 : ref;
+          js[(warp * NR + row) * 2 + 1] = l[nt][u] * back;
         }
       }
   }

@@ -14,10 +14,12 @@
 // one's products run (NQT = 2), or the next scores into a second buffer (NQT = 1).
 //
 // Range.  Queries are scaled by a power of two per row; K and V by a power of two per 16 tokens (2^-ek,
-// 2^-ev) that brings their largest magnitude below 2^15, at most a factor of 64, so fp16 holds any
-// bf16-ranged cache and each dequantizing warp works by itself.  S is multiplied by 2^ek; P takes 2^ev: p = 2^(x +
-// ev - r) against V 2^-ev, and l sums p 2^-ev.  r is a row's largest x + ev at its last move, less 6.  It moves only when
-// exceeded by 14 - 6 = 8 (as in kv_attention.cuh), and only then is O rescaled, after the products that add to it.
+// 2^-ev) that brings their largest magnitude below 2^15, at most a factor of 64, and each dequantizing warp works by
+// itself.  S is multiplied by 2^ek; P takes 2^ev: p = 2^(x + ev - r) against V 2^-ev, and l sums p 2^-ev.  r is
+// a row's largest x + ev at its last move, less 6, kept as its x and its ev (er), as a large x has no room for ev.  It moves
+// only when exceeded by 14 - 6 = 8 (as in kv_attention.cuh), and only then is O rescaled, after the products that add to
+// it.  Past scores of 4096 the differences x - r come before anything is added (`big`): in one multiply-add with the
+// rounded reference, scores past 2^25 would turn into infinities or zeros.
 // What is rounded: lo + s c and probabilities to fp16 (11 bits); sums and statistics are fp32.  For bf16 outputs that is
 // an eighth of the output's own rounding.  For fp16 outputs the probabilities' would weigh as much as the output's
 // (3.3e-4 of the output in all, where the output's alone is 2.1e-4), so they take a second fp16 part in the other
@@ -101,9 +103,6 @@ __device__ __forceinline__ void tmem_st16_u(uint32_t taddr, const uint32_t (&v)[
       : "memory");
 }
 
-// floor(log2 |v|) of a finite v (subnormals: -127), v != 0.
-__device__ __forceinline__ int log2_floor(float v) { return (int)((__float_as_uint(v) >> 23) & 255) - 127; }
-
 // The codes in the low nibbles of w's halves as fp16, by way of 1024 + c, and the next ones, of 64 + c.
 __device__ __forceinline__ uint32_t codes2(uint32_t w) {
   uint32_t r;
@@ -173,7 +172,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   __shared__ uint64_t p_full[NQT][2], pv_done[NQT][2];  // by the unit's parity
   __shared__ uint32_t tmem_slot, abort_word;
   __shared__ __align__(16) float e_k[PR_E][PR_DEQ];  // 2^ek of each 16 tokens
-  __shared__ __align__(16) float e_v[PR_E][PR_DEQ], e_u[PR_E][PR_DEQ];  // ev, 2^-ev
+  __shared__ __align__(16) float e_v[PR_E][PR_DEQ];  // ev
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_pr) + 1023) & ~uintptr_t(1023));
   uint8_t* kbuf = smem + C::SMEM_Q;
   uint8_t* vbuf = kbuf + S * C::KV_TILE;
@@ -341,7 +340,6 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       if (lane == 0) {
         e_k[un % PR_E][dw] = pow2f(ek);
         e_v[un % PR_E][dw] = (float)ev;
-        e_u[un % PR_E][dw] = fv;
       }
       // the next unit's parameters, and then its codes as registers come free, in flight meanwhile
       locate();
@@ -480,7 +478,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         for (int i = 0; i < 8; ++i) mx = max_nan(mx, fabsf(x[i]));
       }
     }
-    const int e = mx > 0.0f ? max(-100, min(126, 13 - log2_floor(mx))) : 0;
+    const int e = row_exponent(mx);
     const float up = row_scale(mx, e);
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -507,7 +505,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     tc_fence_before();
     __syncwarp();
     if (lane == 0) mbar_arrive(&q_full);
-    const float mul = pow2f(-e) * a.scale_log2;
+    const float mul = fminf(pow2f(-e) * a.scale_log2, AT_TOP);
     int see_lo = 0, see_hi = 0;
     if (!live) {  // rows past the last: zero queries, masked nowhere but past the end
       see_hi = end;
@@ -519,8 +517,8 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       }
       see_hi = min(see_hi, end);
     }
-    float ref = AT_M0, l = 0.0f;
-    bool ok = true;
+    float yr = AT_M0, er = -60.0f, l = 0.0f;  // the reference: x and ev of the largest x + ev at its last move
+    bool ok = true, big = false;
 #pragma unroll 1
     for (int un = 0; un < units; ++un) {
       const int it = un / H;
@@ -538,7 +536,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       const float4 ek4 = *reinterpret_cast<const float4*>(e_k[un % PR_E]);
       const float4 ev4 = *reinterpret_cast<const float4*>(e_v[un % PR_E]);
       // by 16 tokens; never 0, as masked scores are -inf
-      const float mk[4] = {fmaxf(mul * ek4.x, 1e-37f), fmaxf(mul * ek4.y, 1e-37f), fmaxf(mul * ek4.z, 1e-37f),
+      float mk[4] = {fmaxf(mul * ek4.x, 1e-37f), fmaxf(mul * ek4.y, 1e-37f), fmaxf(mul * ek4.z, 1e-37f),
                            fmaxf(mul * ek4.w, 1e-37f)};
       const float ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
       const int t0 = lo + un * PR_UN;
@@ -549,7 +547,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           if (t0 + 32 + i < see_lo || t0 + 32 + i >= see_hi) x1[i] = 0xff800000u;
         }
       }
-      float xt = AT_M0;  // the largest x + ev
+      float xt = AT_M0, top[4];  // the largest x + ev; the largest scores of each 16
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t(&x)[32] = i < 2 ? x0 : x1;
@@ -559,7 +557,8 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           h0 = fmaxf(h0, fmaxf(__uint_as_float(x[k]), __uint_as_float(x[k + 1])));
           h1 = fmaxf(h1, fmaxf(__uint_as_float(x[k + 2]), __uint_as_float(x[k + 3])));
         }
-        xt = fmaxf(xt, fmaf(fmaxf(h0, h1), mk[i], ev[i]));
+        top[i] = fmaxf(h0, h1);
+        xt = fmaxf(xt, fmaf(top[i], mk[i], ev[i]));
       }
       // the products two units back are in (each phase is waited for in its turn: a later one could not be
       // told from it by parity)
@@ -567,11 +566,19 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         ok = false;
         break;
       }
-      if (__any_sync(FULL_MASK, xt > ref + 14.0f)) {
-        const float nr = fmaxf(ref, xt - 6.0f), f = ex2(ref - nr);
-        ref = nr;
+      if (__builtin_expect(__any_sync(FULL_MASK, xt > yr + er + 8.0f) || big, 0)) {
+        float yn = yr, en = er;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float y = __fmul_rn(top[i], mk[i]);
+          if (__fadd_rn(__fsub_rn(y, yn), ev[i] - en) > 0.0f) yn = y, en = ev[i];
+        }
+        const float f = ex2(__fadd_rn(__fsub_rn(yr, yn), er - en));
         l *= f;
-        if (un > 0) {  // once the products so far are in
+        yr = yn;
+        er = en;
+        big = __any_sync(FULL_MASK, fabsf(yr) > 4096.0f && yr != AT_M0);
+        if (un > 0 && __any_sync(FULL_MASK, f != 1.0f)) {  // once the products so far are in
           if (!mbar_wait_warp(&pv_done[q][(un - 1) & 1], ((un - 1) >> 1) & 1, tmo, abort_flag)) {
             ok = false;
             break;
@@ -589,6 +596,17 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           }
         }
       }
+      float less = yr;
+      if (D < 256 && __builtin_expect(big, 0)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          x0[i] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(x0[i]), mk[i >> 4]), yr));
+          x1[i] = __float_as_uint(__fsub_rn(__fmul_rn(__uint_as_float(x1[i]), mk[2 + (i >> 4)]), yr));
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mk[i] = 1.0f;
+        less = 0.0f;
+      }
       float sum[4];
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
@@ -596,13 +614,17 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         uint32_t p[16];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const float m = mk[2 * half + j], off = ev[2 * half + j] - ref;
-          const uint64_t m2 = pack_f2(m, m), off2 = pack_f2(off, off);
+          // m x + off; with 256 values always m x - yr by itself first, as dequantization leaves the time for it and a branch
+          // (`big`) made the compiler spill (36 rows: 41.8 us, with the branch 45)
+          const float m = mk[2 * half + j], off = ev[2 * half + j] - er + 6.0f - less;
+          const float last = D < 256 ? 0.0f : ev[2 * half + j] - er + 6.0f;
+          const uint64_t m2 = pack_f2(m, m), off2 = pack_f2(off, off), yr2 = pack_f2(-yr, -yr), last2 = pack_f2(last, last);
           uint64_t s2 = 0;
 #pragma unroll
           for (int i = 8 * j; i < 8 * j + 8; ++i) {
             float a0, a1;
-            unpack_f2(fma_f2(pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), m2, off2), a0, a1);
+            const uint64_t xx = pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
+            unpack_f2(D < 256 ? fma_f2(xx, m2, off2) : add_f2(add_f2(mul_f2(xx, m2), yr2), last2), a0, a1);
             a0 = ex2(a0);
             a1 = ex2(a1);
             s2 = add_f2(s2, pack_f2(a0, a1));
@@ -624,7 +646,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) l = fmaf(sum[i], e_u[un % PR_E][i], l);
+      for (int i = 0; i < 4; ++i) l = fmaf(sum[i], ex2(-ev[i]), l);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();
@@ -637,11 +659,12 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       tc_fence_after();
       const int64_t orow = out_row(a, b, head, r < a.rows ? r : 0);
       const bool whole = a.chunks == 1;
-      const float inv = !whole ? 1.0f : (l > 0.0f ? 1.0f / l : l);  // a row that sees nothing: 0; NaN stays
+      // partial sums leave without their 2^(6 - er); a row that sees nothing: 0; NaN stays
+      const float inv = !whole ? pow2f((int)er - 6) : (l > 0.0f ? 1.0f / l : l);
       float* part = whole ? nullptr : a.part + (orow * a.chunks + ch) * D;
       if (!whole && r < a.rows) {
-        a.stats[(orow * a.chunks + ch) * 2] = ref;
-        a.stats[(orow * a.chunks + ch) * 2 + 1] = l;
+        a.stats[(orow * a.chunks + ch) * 2] = yr;
+        a.stats[(orow * a.chunks + ch) * 2 + 1] = l * inv;
       }
 #pragma unroll 1
       for (int c = 0; c < D; c += 16) {

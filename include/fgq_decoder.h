@@ -104,6 +104,8 @@ fgq_status fgq_kv_read(const fgq_kv_cache* cache, void* k, void* v, fgq_float_ty
  * parts).  More than eight rows (queries times query heads of a kv head) of bf16 or fp16 queries may
  * run on a second kernel, where that is the faster; it takes keys, values and probabilities as fp16
  * (fp16 queries: two parts of a probability).
+ * Queries may have any magnitude, keys up to 1e30; values from 1e-18 to 1e30 that lie within 1e25 of one
+ * another in a sequence, or are 0.  Smaller values lose precision (an error of at most 1e-25).
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad cache or type, kv_heads not dividing
  * q_heads, window < 0, a window without causal), FGQ_ERR_ALIGN as fgq_kv_append (q, out too),
  * FGQ_ERR_UNSUPPORTED (more than 2^31 - 1 blocks of work), FGQ_ERR_CUDA (also where a temporary

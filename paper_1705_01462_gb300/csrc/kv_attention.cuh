@@ -485,8 +485,10 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[nt][j][u][i] = 0.0f;
   }
-  float sigma = 8.6736174e-19f;  // 2^-60; a power of two at or above every value scale met so far
-  float off = 66.0f;             // 6 - log2(sigma)
+  // a power of two at or above every value scale met so far, 2^-60 at least; 0 before the first scale above 0: groups of equal
+  // values, zeros among them, have none, and p with 2^60 in it would take them past fp32's range or out of a join
+  float sigma = 0.0f;
+  float off = 6.0f;  // 6 - log2(sigma), or 6
 
   bool ok = true;
   int done = 0, tile0 = lo + warp * TILE, st = 0;
@@ -591,8 +593,8 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
 #pragma unroll
         for (int s = 16; s > 0; s >>= 1) smax = fmaxf(smax, __shfl_xor_sync(FULL_MASK, smax, s));
         if (smax > sigma)  // the next power of two
-          sigma = __uint_as_float((__float_as_uint(smax) + 0x7fffffu) & 0x7f800000u);
-        const float now = 6.0f - (float)((int)(__float_as_uint(sigma) >> 23) - 127), by = now - off;
+          sigma = fmaxf(__uint_as_float((__float_as_uint(smax) + 0x7fffffu) & 0x7f800000u), 8.6736174e-19f);
+        const float now = sigma > 0.0f ? 6.0f - (float)((int)(__float_as_uint(sigma) >> 23) - 127) : 6.0f, by = now - off;
         off = now;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)

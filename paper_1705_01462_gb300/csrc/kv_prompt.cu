@@ -49,6 +49,7 @@ using tc::sw128;
 constexpr int PR_UN = 64;          // tokens of a unit: a softmax step, a dequantizing group's step
 constexpr int PR_DEQ = 4;          // dequantizing warps of a group
 constexpr int PR_GROUPS = 2;       // groups of them, taking units in turn
+constexpr float PR_ZERO = 1e30f;   // in place of ev where 16 tokens' values are all 0: the reference's own serves them
 constexpr int PR_E = 16;           // units whose scales are kept: more than any role is ahead of another
 
 template <int D, int NQT>
@@ -172,7 +173,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   __shared__ uint64_t p_full[NQT][2], pv_done[NQT][2];  // by the unit's parity
   __shared__ uint32_t tmem_slot, abort_word;
   __shared__ __align__(16) float e_k[PR_E][PR_DEQ];  // 2^ek of each 16 tokens
-  __shared__ __align__(16) float e_v[PR_E][PR_DEQ];  // ev
+  __shared__ __align__(16) float e_v[PR_E][PR_DEQ];  // ev, or PR_ZERO
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_pr) + 1023) & ~uintptr_t(1023));
   uint8_t* kbuf = smem + C::SMEM_Q;
   uint8_t* vbuf = kbuf + S * C::KV_TILE;
@@ -309,7 +310,6 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
     codes(kc0, kw);
     codes(vc0, vw);
     look_up(grp + PR_GROUPS);
-    int last_ev = -60;
     bool ok = tmo != 0;
 #pragma unroll 1
     for (int un = grp; un < units; un += PR_GROUPS) {
@@ -330,8 +330,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         mv = __vmaxu2(mv, __shfl_xor_sync(FULL_MASK, mv, o));
       }
       const int ek = mk ? min(114, max(-100, max((int)(mk >> 23), (int)(mk >> 7 & 255) + 4) - (127 + 13))) : 0;
-      const int ev = mv ? min(114, max(-60, max((int)(mv >> 23), (int)(mv >> 7 & 255) + 4) - (127 + 13))) : last_ev;
-      last_ev = ev;
+      const int ev = min(114, max(-60, max((int)(mv >> 23), (int)(mv >> 7 & 255) + 4) - (127 + 13)));
       const float fk = pow2f(-ek), fv = pow2f(-ev);
       const uint32_t kt = smem_u32(kbuf + st * C::KV_TILE), vt = smem_u32(vbuf + st * C::KV_TILE);
       const int row = un % H * PR_UN + 16 * dw + tr;
@@ -339,7 +338,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       if (!ok) break;
       if (lane == 0) {
         e_k[un % PR_E][dw] = pow2f(ek);
-        e_v[un % PR_E][dw] = (float)ev;
+        e_v[un % PR_E][dw] = mv ? (float)ev : PR_ZERO;
       }
       // the next unit's parameters, and then its codes as registers come free, in flight meanwhile
       locate();
@@ -537,8 +536,8 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       const float4 ev4 = *reinterpret_cast<const float4*>(e_v[un % PR_E]);
       // by 16 tokens; never 0, as masked scores are -inf
       float mk[4] = {fmaxf(mul * ek4.x, 1e-37f), fmaxf(mul * ek4.y, 1e-37f), fmaxf(mul * ek4.z, 1e-37f),
-                           fmaxf(mul * ek4.w, 1e-37f)};
-      const float ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
+                     fmaxf(mul * ek4.w, 1e-37f)};
+      float ev[4] = {ev4.x, ev4.y, ev4.z, ev4.w};
       const int t0 = lo + un * PR_UN;
       if (!__all_sync(FULL_MASK, t0 >= see_lo && t0 + PR_UN <= see_hi)) {
 #pragma unroll
@@ -547,7 +546,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           if (t0 + 32 + i < see_lo || t0 + 32 + i >= see_hi) x1[i] = 0xff800000u;
         }
       }
-      float xt = AT_M0, top[4];  // the largest x + ev; the largest scores of each 16
+      float xt = AT_M0, top[4];  // the largest x + ev (past every reference with a PR_ZERO in sight); of each 16 the largest score
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t(&x)[32] = i < 2 ? x0 : x1;
@@ -570,13 +569,15 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         float yn = yr, en = er;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float y = __fmul_rn(top[i], mk[i]);
-          if (__fadd_rn(__fsub_rn(y, yn), ev[i] - en) > 0.0f) yn = y, en = ev[i];
+          const float y = __fmul_rn(top[i], mk[i]), e = ev[i] == PR_ZERO ? er : ev[i];
+          if (__fadd_rn(__fsub_rn(y, yn), e - en) > 0.0f) yn = y, en = e;
         }
-        const float f = ex2(__fadd_rn(__fsub_rn(yr, yn), er - en));
-        l *= f;
+        const float by = __fadd_rn(__fsub_rn(yr, yn), er - en), f = ex2(by);
+        l = l * ex2(0.5f * by) * ex2(0.5f * by);  // 2^-ev is in it: where 2^by alone is no more, it may be
         yr = yn;
         er = en;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ev[i] = ev[i] == PR_ZERO ? er : ev[i];
         big = __any_sync(FULL_MASK, fabsf(yr) > 4096.0f && yr != AT_M0);
         if (un > 0 && __any_sync(FULL_MASK, f != 1.0f)) {  // once the products so far are in
           if (!mbar_wait_warp(&pv_done[q][(un - 1) & 1], ((un - 1) >> 1) & 1, tmo, abort_flag)) {

@@ -549,6 +549,16 @@ int few_nt(int P) { return P <= 8 ? 1 : (P <= 16 ? 2 : 4); }
 fgq_status launch_few(FewArgs a, cudaStream_t s) {
   const int nt = few_nt(a.P);
   a.splits = few_splits(a.P, a.K, a.M, nt);
+  // more tokens than a grid has rows of blocks for (only without features, whose bias any number of tokens takes here)
+  const int most = 65535 * 8 * nt;
+  for (; a.P > most; a.P -= most) {
+    FewArgs part = a;
+    part.P = most;
+    const fgq_status st = launch_few_nt<4, int8_t>(part, s);
+    if (st != FGQ_OK) return st;
+    a.scale += most;
+    a.y = static_cast<uint8_t*>(a.y) + (int64_t)most * a.M * float_bytes(a.ytype);
+  }
   return nt == 1 ? launch_few_nt<1, int8_t>(a, s) : nt == 2 ? launch_few_nt<2, int8_t>(a, s) : launch_few_nt<4, int8_t>(a, s);
 }
 

@@ -265,7 +265,7 @@ extern "C" fgq_status fgq_kv_attention(const fgq_kv_cache* cache, const void* q,
   a.group = group;
   a.rows = T * group;
   a.causal = causal;
-  a.window = window < capacity ? window : 0;  // wider than any sequence: no limit, and no difference past 32 bits
+  a.window = window;
   const int bound = max_len > 0 && max_len < capacity ? max_len : (int)(capacity > 0 ? capacity : 1);
   return launch_attention_call(cache, a, bound, stream);
 }

@@ -194,6 +194,9 @@ __device__ __forceinline__ int seq_len(const AttnArgs& a, int b) {
   return min(n, most);
 }
 
+// First position that a window ending before position `end` leaves (no difference that could wrap around).
+__device__ __forceinline__ int after_window(const AttnArgs& a, int end) { return a.window && end > a.window ? end - a.window : 0; }
+
 // First and one past the last position that any of the query rows [i0, i1] (by query index) of a
 // sequence of n tokens and nq queries sees.
 __device__ __forceinline__ void visible(const AttnArgs& a, int n, int nq, int i0, int i1, int& first, int& end) {
@@ -208,7 +211,7 @@ __device__ __forceinline__ void visible(const AttnArgs& a, int n, int nq, int i0
     return;
   }
   end = max(n - nq + i1 + 1, 0);
-  first = a.window ? max(n - nq + i0 + 1 - a.window, 0) : 0;
+  first = after_window(a, n - nq + i0 + 1);
   if (end <= first) first = end = 0;
 }
 
@@ -445,7 +448,7 @@ __global__ void __launch_bounds__(32 * AT_WARPS, attention_blocks_per_sm<NB>())
       sh = n, sl = 0;
       if (a.causal) {
         sh = n - nq + qi + 1;
-        if (a.window) sl = sh - a.window;
+        sl = after_window(a, sh);
       }
     }
 #pragma unroll

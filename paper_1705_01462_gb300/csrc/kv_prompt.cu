@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       see_hi = n;
       if (a.causal) {
         see_hi = n - nq + qi + 1;
-        if (a.window) see_lo = see_hi - a.window;
+        see_lo = after_window(a, see_hi);
       }
       see_hi = min(see_hi, end);
     }

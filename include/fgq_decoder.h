@@ -63,7 +63,7 @@ typedef struct {
  * No two positions of one call may share a slot.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad cache or type), FGQ_ERR_ALIGN (k, v or a
  * cache array not 16-byte aligned, a stride not a multiple of 16 bytes, an int32 array not 4-byte
- * aligned), FGQ_ERR_UNSUPPORTED (T kv_heads above 2^31 - 1), FGQ_ERR_CUDA.
+ * aligned), FGQ_ERR_UNSUPPORTED (T kv_heads above 2^31 - 1, T above 2^31 - 2^16), FGQ_ERR_CUDA.
  */
 fgq_status fgq_kv_append(const fgq_kv_cache* cache, const void* k, const void* v, fgq_float_type type,
                          int B, int T, int64_t k_batch_stride, int64_t k_token_stride,
@@ -123,7 +123,8 @@ fgq_status fgq_kv_attention(const fgq_kv_cache* cache, const void* q, fgq_float_
  * scale[p] = amax_p / 127, amax_p = max_k |x[p][k]|; a row of zeros gives codes and scale 0.  A row
  * that holds NaN or Inf gets codes and scale 0, and FGQ_ERR_NONFINITE is recorded.
  *   q  out, int8 [P][K] contiguous;  scale  out, fp32 [P].  No alignment beyond the element's.
- * Errors: FGQ_ERR_ARG, FGQ_ERR_ALIGN (x or scale not aligned to their elements), FGQ_ERR_CUDA.
+ * Errors: FGQ_ERR_ARG, FGQ_ERR_ALIGN (x or scale not aligned to their elements), FGQ_ERR_UNSUPPORTED
+ * (P or K above 2^31 - 2^16), FGQ_ERR_CUDA.
  */
 fgq_status fgq_quantize_tokens(const void* x, fgq_float_type type, int P, int K, int64_t ldx, int8_t* q,
                                float* scale, cudaStream_t stream);
@@ -137,7 +138,8 @@ fgq_status fgq_quantize_tokens(const void* x, fgq_float_type type, int P, int K,
  * fp32 as they grow past that.  No alignment beyond the elements'; rows of q and wq that
  * start on 16-byte boundaries (K a multiple of 16) are read fastest.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type), FGQ_ERR_ALIGN (scale, wscale, bias
- * or y not aligned to their elements), FGQ_ERR_CUDA (also where a temporary cannot be had).
+ * or y not aligned to their elements), FGQ_ERR_UNSUPPORTED (P, K or M above 2^31 - 2^16),
+ * FGQ_ERR_CUDA (also where a temporary cannot be had).
  */
 fgq_status fgq_gemm_w8a8(const int8_t* q, const float* scale, int P, int K, const int8_t* wq,
                          const float* wscale, int M, const float* bias, void* y, fgq_float_type ytype,

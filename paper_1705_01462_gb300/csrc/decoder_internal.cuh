@@ -13,6 +13,8 @@
 namespace fgq {
 namespace dec {
 
+// Tokens, features and channels beyond this are refused: kernels round up to tiles, and step past the end, in 32 bits.
+constexpr int MAX_SIZE = INT32_MAX - 65535;
 inline bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline bool valid_float(int t) { return t == FGQ_F32 || t == FGQ_BF16 || t == FGQ_F16; }
 inline bool nonfinite_host(float v) { return !(v - v == 0.0f); }

@@ -276,7 +276,7 @@ template <typename T, int D, int G>
 fgq_status launch_kv(const KvArgs& a, bool append, cudaStream_t s) {
   constexpr int RUN = KvRun<D>::RUN, WARPS = KV_THREADS / 32;
   const int64_t runs = ((int64_t)a.T + RUN - 1) / RUN * a.c.kv_heads, blocks = (runs + WARPS - 1) / WARPS;
-  if ((int64_t)a.T * a.c.kv_heads > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
+  if (a.T > MAX_SIZE || (int64_t)a.T * a.c.kv_heads > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
   const dim3 grid((unsigned)blocks, (unsigned)(a.B < 65535 ? a.B : 65535), 2);
   if (append)
     kv_append_kernel<T, D, G><<<grid, KV_THREADS, 0, s>>>(a);

@@ -588,6 +588,7 @@ fgq_status check_product(const void* x, int P, int K, const int8_t* wq, const fl
                          const void* y, int ytype) {
   if (P < 0 || K < 0 || M < 0 || !valid_float(ytype)) return FGQ_ERR_ARG;
   if (P == 0 || M == 0) return FGQ_OK;
+  if (P > MAX_SIZE || K > MAX_SIZE || M > MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
   if (!wscale || !y || (K > 0 && (!x || !wq))) return FGQ_ERR_ARG;
   if (!aligned(wscale, 4) || !aligned(bias, 4) || !aligned(y, float_bytes(ytype))) return FGQ_ERR_ALIGN;
   return FGQ_OK;
@@ -604,6 +605,7 @@ fgq_status fgq_quantize_tokens(const void* x, fgq_float_type type, int P, int K,
                                cudaStream_t stream) {
   if (P < 0 || K < 0 || !dec::valid_float(type) || (P > 1 && ldx < K)) return FGQ_ERR_ARG;
   if (P == 0) return FGQ_OK;
+  if (P > dec::MAX_SIZE || K > dec::MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
   if (!scale || (K > 0 && (!x || !q))) return FGQ_ERR_ARG;
   if (!dec::aligned(x, dec::float_bytes(type)) || !dec::aligned(scale, 4)) return FGQ_ERR_ALIGN;
   return launch_quantize_tokens(x, type, P, K, ldx, q, K, false, scale, Expand{}, stream);

@@ -147,7 +147,8 @@ fgq_status fgq_gemm_w8a8(const int8_t* q, const float* scale, int P, int K, cons
 
 /*
  * A linear layer: fgq_quantize_tokens of x, then fgq_gemm_w8a8 with y of x's type, the quantized
- * tokens in temporaries of the library.  Results are those of the two calls.
+ * tokens in temporaries of the library.  Results are those of the two calls, also where y takes the place of
+ * x.  (No other output of this header may overlap what its call reads.)
  */
 fgq_status fgq_linear_w8a8(const void* x, fgq_float_type type, int P, int K, int64_t ldx, const int8_t* wq,
                            const float* wscale, int M, const float* bias, void* y, cudaStream_t stream);

@@ -572,6 +572,12 @@ bool fused_fits(const void* x, int type, int P, int K, int M, int64_t ldx) {
   return P <= FUSED_MAX_P && (int64_t)P * K <= FUSED_MAX_ELEMS && K % 8 == 0 && aligned(x, 16) &&
          (P == 1 || stride16(ldx, type)) && 8 * few_row_bytes(few_pieces(K, few_splits(P, K, M, 1))) <= FEW_MAX_CODES;
 }
+// Whether outputs take the place of tokens: blocks that quantize for themselves would read what others have written.
+bool outputs_over_tokens(const void* x, const void* y, int type, int P, int K, int M, int64_t ldx) {
+  const uintptr_t xb = reinterpret_cast<uintptr_t>(x), yb = reinterpret_cast<uintptr_t>(y);
+  const uint64_t xn = ((uint64_t)(P - 1) * (P > 1 ? ldx : 0) + K) * float_bytes(type), yn = (uint64_t)P * M * float_bytes(type);
+  return xb < yb + yn && yb < xb + xn;
+}
 fgq_status launch_few_float(FewArgs a, int type, cudaStream_t s) {
   a.splits = few_splits(a.P, a.K, a.M, 1);
   if (type == FGQ_F32) return launch_few_nt<1, float>(a, s);
@@ -644,7 +650,7 @@ fgq_status fgq_linear_w8a8(const void* x, fgq_float_type type, int P, int K, int
   if (st == FGQ_OK && P > 1 && ldx < K) st = FGQ_ERR_ARG;
   if (st != FGQ_OK || P == 0 || M == 0) return st;
   if (!dec::aligned(x, dec::float_bytes(type))) return FGQ_ERR_ALIGN;
-  if (K > 0 && fused_fits(x, type, P, K, M, ldx)) {
+  if (K > 0 && fused_fits(x, type, P, K, M, ldx) && !outputs_over_tokens(x, y, type, P, K, M, ldx)) {
     const FewArgs a = {x, ldx, nullptr, nullptr, wq, wscale, bias, y, P, K, M, type, 1, device_error_word(), 0};
     return launch_few_float(a, type, stream);
   }

@@ -23,13 +23,14 @@ from paper_1705_01462_gb300 import fgq
 
 
 class PagePool:
-    """Hands out the pages of a cache and keeps the page table of its sequences (host side)."""
+    """Hands out the pages of a cache and keeps the page table and the lengths of its sequences (host side)."""
 
     def __init__(self, pages: int, page_size: int, sequences: int, max_pages: int, device="cuda"):
         self.page_size = page_size
         self._free = list(range(pages - 1, -1, -1))
         self._held: List[List[int]] = [[] for _ in range(sequences)]
         self.table = torch.full((sequences, max_pages), -1, dtype=torch.int32, device=device)
+        self.lengths = [0] * sequences  # tokens of each sequence in the cache
 
     def reserve(self, lengths: Sequence[int]) -> None:
         """Pages for sequences of these lengths; those that they hold already stay."""
@@ -45,9 +46,11 @@ class PagePool:
             held += new
 
     def release(self, b: int) -> None:
+        """Ends sequence b: its pages are free, and its place holds no tokens."""
         self._free += reversed(self._held[b])
         self._held[b] = []
         self.table[b] = -1
+        self.lengths[b] = 0
 
 
 class AttentionBlock:
@@ -65,7 +68,15 @@ class AttentionBlock:
         self.wo = fgq.fgq_quantize_weights_w8(wo)
         self.cache = fgq.kv_cache(pages, page_size, kv_heads, head_dim, group, device=wqkv.device)
         self.pool = PagePool(pages, page_size, sequences, max_pages or pages, device=wqkv.device)
-        self.lengths = [0] * sequences  # tokens of each sequence in the cache
+
+    @property
+    def lengths(self) -> List[int]:
+        """Tokens of each sequence in the cache."""
+        return self.pool.lengths
+
+    def release(self, b: int) -> None:
+        """Ends sequence b; the next tokens given in its place start another."""
+        self.pool.release(b)
 
     def forward(self, x: torch.Tensor, lens: Optional[Sequence[int]] = None) -> torch.Tensor:
         """x [sequences][T][width] -> the same shape and type; lens[b] <= T tokens of sequence b are real (None: T)."""
@@ -81,7 +92,7 @@ class AttentionBlock:
         fgq.fgq_kv_append(self.cache, k, v, self.pool.table, starts_d, lens=lens_d)
         o = fgq.fgq_kv_attention(q, self.cache, self.pool.table, ends_d, q_lens=lens_d, window=self.window,
                                  max_len=max(ends))
-        self.lengths = ends
+        self.pool.lengths = ends
         return fgq.fgq_linear_w8a8(o.view(B * T, -1), *self.wo).view(B, T, width)
 
 

@@ -88,12 +88,13 @@ class AttentionBlock:
         self.pool.reserve(ends)
         starts_d, lens_d, ends_d = torch.tensor([self.lengths, lens, ends], dtype=torch.int32, device=x.device)
         qkv = fgq.fgq_linear_w8a8(x.reshape(B * T, width), *self.wqkv)
-        q, k, v = qkv.view(B, T, -1, self.head_dim).split([self.q_heads, self.kv_heads, self.kv_heads], dim=2)
+        heads = [self.q_heads, self.kv_heads, self.kv_heads]
+        q, k, v = qkv.view(B, T, sum(heads), self.head_dim).split(heads, dim=2)
         fgq.fgq_kv_append(self.cache, k, v, self.pool.table, starts_d, lens=lens_d)
         o = fgq.fgq_kv_attention(q, self.cache, self.pool.table, ends_d, q_lens=lens_d, window=self.window,
                                  max_len=max(ends))
         self.pool.lengths = ends
-        return fgq.fgq_linear_w8a8(o.view(B * T, -1), *self.wo).view(B, T, width)
+        return fgq.fgq_linear_w8a8(o.view(B * T, self.q_heads * self.head_dim), *self.wo).view(B, T, width)
 
 
 def main() -> None:

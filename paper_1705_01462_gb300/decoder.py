@@ -74,12 +74,17 @@ class AttentionBlock:
         """Tokens of each sequence in the cache."""
         return self.pool.lengths
 
+    @lengths.setter
+    def lengths(self, lengths: Sequence[int]) -> None:
+        self.pool.lengths = list(lengths)
+
     def release(self, b: int) -> None:
         """Ends sequence b; the next tokens given in its place start another."""
         self.pool.release(b)
 
     def forward(self, x: torch.Tensor, lens: Optional[Sequence[int]] = None) -> torch.Tensor:
-        """x [sequences][T][width] -> the same shape and type; lens[b] <= T tokens of sequence b are real (None: T)."""
+        """x [sequences][T][width] -> the same shape and type; lens[b] <= T tokens of sequence b are real (None: T), the
+        others finite and their outputs of no meaning."""
         B, T, width = x.shape
         lens = [T] * B if lens is None else list(lens)
         if B != len(self.lengths) or len(lens) != B or any(n < 0 or n > T for n in lens):

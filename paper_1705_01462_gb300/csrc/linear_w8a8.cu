@@ -562,14 +562,16 @@ fgq_status launch_few(FewArgs a, cudaStream_t s) {
   return nt == 1 ? launch_few_nt<1, int8_t>(a, s) : nt == 2 ? launch_few_nt<2, int8_t>(a, s) : launch_few_nt<4, int8_t>(a, s);
 }
 
-// Float tokens that each block quantizes for itself: rows that can be loaded eight elements at a time, codes that fit
-// beside the sums, and few elements, as every block has all of the rows' maxima to find.  It saves the caller a
-// launch and a temporary (calls from Python one after another: four tokens, 2048 -> 2000, 10.9 us, eight 15.4 with a
-// launch of their own).  On the device, 4096 -> 4096: one and two tokens 10.4 us either way, four 12.3 and 10.3, eight
-// 14.4 and 10.3: from there on it costs more than it saves.
-constexpr int FUSED_MAX_P = 8, FUSED_MAX_ELEMS = 16384;
+// 16-bit tokens that each block quantizes for itself: rows that can be loaded eight elements at a time, codes that fit
+// beside the sums, and few elements, as every block has all of the rows' maxima to find.  It saves the caller a launch and a
+// temporary and costs the device time.  Calls from Python one after another, so and with a quantizing launch of their own: one and
+// two tokens, 4096 -> 4096, 12.5 us both, four, 2048 -> 2000, 9.5 and 10.8, eight, 1024 -> 1024, 8.4 and 10.3 (up to 4 us
+// saved where the host is slower); the same calls from a graph, weights from HBM: 9.9 and 8.8, 10.2 and 9.0, 7.0 and 5.6, 6.6
+// and 4.0.  With 16384 elements, or fp32 ones, both are slower so: four tokens, 4096 -> 4096, 14.4 and 12.6 (11.4 and 9.0),
+// four fp32 ones, 2048 -> 2000, 12.4 and 10.5 (10.4 and 5.9).
+constexpr int FUSED_MAX_P = 8, FUSED_MAX_ELEMS = 8192;
 bool fused_fits(const void* x, int type, int P, int K, int M, int64_t ldx) {
-  return P <= FUSED_MAX_P && (int64_t)P * K <= FUSED_MAX_ELEMS && K % 8 == 0 && aligned(x, 16) &&
+  return type != FGQ_F32 && P <= FUSED_MAX_P && (int64_t)P * K <= FUSED_MAX_ELEMS && K % 8 == 0 && aligned(x, 16) &&
          (P == 1 || stride16(ldx, type)) && 8 * few_row_bytes(few_pieces(K, few_splits(P, K, M, 1))) <= FEW_MAX_CODES;
 }
 // Whether outputs take the place of tokens: blocks that quantize for themselves would read what others have written.
@@ -580,7 +582,6 @@ bool outputs_over_tokens(const void* x, const void* y, int type, int P, int K, i
 }
 fgq_status launch_few_float(FewArgs a, int type, cudaStream_t s) {
   a.splits = few_splits(a.P, a.K, a.M, 1);
-  if (type == FGQ_F32) return launch_few_nt<1, float>(a, s);
   return type == FGQ_BF16 ? launch_few_nt<1, __nv_bfloat16>(a, s) : launch_few_nt<1, __half>(a, s);
 }
 

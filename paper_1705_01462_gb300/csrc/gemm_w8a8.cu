@@ -18,10 +18,10 @@
 // 4096 tokens, 4096 -> 8192, bf16: 179 us for the layer, 20 of them quantization and expansion, where the products
 // alone are due 148; at 2048 tokens, 4096 -> 4096 (50 us) the tensor pipe is active 59% of the time: 128 tiles on
 // 76 pairs are two waves.
-// Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded and each role leaves its loop.  At the end, after an expiry
-// or not, the two blocks meet and tell each other how far they came, each waits for every arrival that the MMAs' commits still
-// make on its barriers and the first one for boxes that no MMA has read, they meet again, and TMEM is freed: nothing is
-// on its way to a block that has left.
+// Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded and each role leaves its loop.  Nothing is on its way to a block that
+// leaves: both blocks wait for every arrival that the MMAs' commits make on their barriers, and meet before TMEM is freed.  After
+// an expiry in either they know by then how far each came, wait for the arrivals that there are and the first one for boxes that
+// no MMA has read, and meet again.
 #include <cstring>
 
 #include "linear_internal.cuh"
@@ -79,6 +79,9 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(const uint32_t* p, uint32_t r
   uint32_t v;
   asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(map_rank(p, rank)) : "memory");
   return v;
+}
+__device__ __forceinline__ void st_cluster_u32(const uint32_t* p, uint32_t rank, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_rank(p, rank)), "r"(v) : "memory");
 }
 // A box into this block's shared memory whose bytes count on a barrier of the pair, `bar` in either block.
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const void* map, int c0, int c1, uint32_t bar) {
@@ -162,6 +165,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   uint32_t* came = tmem_slot + 2;  // K-tiles asked for by this block; first block: K-tiles, and tiles, that MMAs were committed for
+  uint32_t* other_failed = came + 3;  // written by the other block
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
   const uint64_t tmo = a.timeout_ns;
@@ -177,6 +181,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
     }
     mbar_init(drain_bar, 1);
     *abort_flag = 0;
+    *other_failed = 0;
     fence_mbar_init();
   }
   if (warp == GW_MMA_WARP) tmem_alloc2(tmem_slot, C::COLS);
@@ -200,6 +205,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
   };
   auto fail = [&]() {
     *abort_flag = 1;
+    st_cluster_u32(other_failed, rank ^ 1u, 1u);
     record_error(a.err, FGQ_ERR_TIMEOUT);
   };
 
@@ -223,8 +229,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
         tma_load_2d_pair(smem_u32(A + C::A_BYTES), &a.x_map, kt * GW_KT, p0 + BN / 2 * (int)rank, bar);
       }
     }
-    if (!ok && !*abort_flag) fail();
     came[0] = (uint32_t)j;
+    // the commits of the last K-tiles: those before them were waited for, those of tiles are by the epilogue
+    for (int i = j - S < 0 ? 0 : j - S; i < j && ok; ++i) ok = mbar_wait_cluster(&empty[i % S], (i / S) & 1, tmo, abort_flag);
+    if (!ok && !*abort_flag) fail();
   }
 
   if (warp == GW_MMA_WARP && rank == 0) {  // converged, an elected lane issues: a divergent one takes 100 clocks an MMA
@@ -256,7 +264,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
       if (elect_one()) mma_commit_pair(&acc_full[b]);
     }
     if (!ok && lane == 0 && !*abort_flag) fail();
-    if (elect_one()) mma_commit_pair(drain_bar);
+    if (!ok && elect_one()) mma_commit_pair(drain_bar);
     if (lane == 0) {
       came[1] = (uint32_t)j;
       came[2] = (uint32_t)tl;
@@ -287,7 +295,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
         // the 32 tokens' scales, one a lane (by now the quantizer has written them: no read-only path)
         const float sx = pw + c + lane < a.P ? a.scale[pw + c + lane] : 0.0f;
         tmem_ld_wait_regs(r);
-        if (c + 32 == BN / 2) {  // this warp has the whole accumulator: free it
+        if (c + 32 == BN / 2 && tl + 2 < my_tiles) {  // this warp has the whole accumulator: free it for the tile after next
           tc_fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive_cluster(map_rank(&acc_empty[b], 0));
@@ -316,13 +324,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
 
   tc_fence_before();
   __syncthreads();
-  cluster_sync();  // both blocks' counts are there
-  if (warp == GW_TMA_WARP && lane == 0) {
+  cluster_sync();  // both blocks' counts and failures are there
+  const bool failed = *abort_flag != 0 || *reinterpret_cast<volatile uint32_t*>(other_failed) != 0;  // the same in both
+  if (failed && warp == GW_TMA_WARP && lane == 0) {
     auto drain = [](uint64_t* bar, int phase) { mbar_wait_bounded(bar, (uint32_t)phase & 1u, 1u << 20); };
     const int done = (int)ld_cluster_u32(came + 1, 0), tiles = (int)ld_cluster_u32(came + 2, 0);
     for (int i = done > S ? done - S : 0; i < done; ++i) drain(&empty[i % S], i / S);
     for (int i = tiles > 2 ? tiles - 2 : 0; i < tiles; ++i) drain(&acc_full[i & 1], i >> 1);
-    drain(drain_bar, 0);
+    if (tiles < my_tiles) drain(drain_bar, 0);
     if (rank == 0) {  // boxes that no MMA has read, S at most as each follows a commit S K-tiles back
       const int mine = (int)came[0], other = (int)ld_cluster_u32(came, 1);
       for (int i = done; i < (mine > other ? mine : other); ++i) {
@@ -334,7 +343,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(GW_THREADS, 1)
       }
     }
   }
-  cluster_sync();  // and nothing is on its way to either
+  if (failed) cluster_sync();  // and nothing is on its way to either
   if (warp == GW_MMA_WARP) {
     tc_fence_after();
     tmem_dealloc2(tmem, C::COLS);

@@ -49,7 +49,6 @@ using tc::sw128;
 constexpr int PR_UN = 64;          // tokens of a unit: a softmax step, a dequantizing group's step
 constexpr int PR_DEQ = 4;          // dequantizing warps of a group
 constexpr int PR_GROUPS = 2;       // groups of them, taking units in turn
-constexpr float PR_ZERO = 1e30f;   // in place of ev where 16 tokens' values are all 0: the reference's own serves them
 constexpr int PR_E = 16;           // units whose scales are kept: more than any role is ahead of another
 
 template <int D, int NQT>
@@ -173,7 +172,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
   __shared__ uint64_t p_full[NQT][2], pv_done[NQT][2];  // by the unit's parity
   __shared__ uint32_t tmem_slot, abort_word;
   __shared__ __align__(16) float e_k[PR_E][PR_DEQ];  // 2^ek of each 16 tokens
-  __shared__ __align__(16) float e_v[PR_E][PR_DEQ];  // ev, or PR_ZERO
+  __shared__ __align__(16) float e_v[PR_E][PR_DEQ], e_u[PR_E][PR_DEQ];  // ev, 2^-ev
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_pr) + 1023) & ~uintptr_t(1023));
   uint8_t* kbuf = smem + C::SMEM_Q;
   uint8_t* vbuf = kbuf + S * C::KV_TILE;
@@ -338,7 +337,8 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
       if (!ok) break;
       if (lane == 0) {
         e_k[un % PR_E][dw] = pow2f(ek);
-        e_v[un % PR_E][dw] = mv ? (float)ev : PR_ZERO;
+        e_v[un % PR_E][dw] = (float)ev;
+        e_u[un % PR_E][dw] = fv;
       }
       // the next unit's parameters, and then its codes as registers come free, in flight meanwhile
       locate();
@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           if (t0 + 32 + i < see_lo || t0 + 32 + i >= see_hi) x1[i] = 0xff800000u;
         }
       }
-      float xt = AT_M0, top[4];  // the largest x + ev (past every reference with a PR_ZERO in sight); of each 16 the largest score
+      float xt = AT_M0, top[4];  // the largest x + ev; the largest scores of each 16
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t(&x)[32] = i < 2 ? x0 : x1;
@@ -569,16 +569,14 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         float yn = yr, en = er;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float y = __fmul_rn(top[i], mk[i]), e = ev[i] == PR_ZERO ? er : ev[i];
-          if (__fadd_rn(__fsub_rn(y, yn), e - en) > 0.0f) yn = y, en = e;
+          const float y = __fmul_rn(top[i], mk[i]);
+          if (__fadd_rn(__fsub_rn(y, yn), ev[i] - en) > 0.0f) yn = y, en = ev[i];
         }
         const float by = __fadd_rn(__fsub_rn(yr, yn), er - en), f = ex2(by);
         l = l * ex2(0.5f * by) * ex2(0.5f * by);  // 2^-ev is in it: where 2^by alone is no more, it may be
         yr = yn;
         er = en;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) ev[i] = ev[i] == PR_ZERO ? er : ev[i];
-        big = __any_sync(FULL_MASK, fabsf(yr) > 4096.0f && yr != AT_M0);
+        big = __any_sync(FULL_MASK, (fabsf(yr) > 4096.0f && yr != AT_M0) || er > 20.0f);
         if (un > 0 && __any_sync(FULL_MASK, f != 1.0f)) {  // once the products so far are in
           if (!mbar_wait_warp(&pv_done[q][(un - 1) & 1], ((un - 1) >> 1) & 1, tmo, abort_flag)) {
             ok = false;
@@ -598,6 +596,11 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         }
       }
       float less = yr;
+      if (__builtin_expect(big, 0)) {
+        // values far below the reference's, zeros among them, add nothing but still weigh: with an ev that leaves p above 2^-126
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ev[i] = fmaxf(ev[i], er - 100.0f);
+      }
       if (D < 256 && __builtin_expect(big, 0)) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
@@ -647,7 +650,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) l = fmaf(sum[i], ex2(-ev[i]), l);
+      for (int i = 0; i < 4; ++i) l = fmaf(sum[i], __builtin_expect(big, 0) ? ex2(-ev[i]) : e_u[un % PR_E][i], l);
       tmem_st_wait();
       tc_fence_before();
       __syncwarp();

@@ -180,8 +180,8 @@ fgq_status launch_attention_call(const fgq_kv_cache* cache, AttnArgs a, int max_
                        a, D, max_len);
   // From nine rows on, the prompt kernel may be faster: it dequantizes a tile of the cache once for 128 or 256 rows,
   // but its block takes an SM to itself and longer to start.  With heads of 128 values, 32 sequences of 2000 tokens
-  // and 8 kv heads, 16 rows take 51 us here and 60 there, 24 rows 93 and 60; with 8 sequences of 4096 and 4 heads,
-  // 8 rows 19 and 23, 64 rows 52 and 25; with 256 values 24 rows 39 and 35; with one sequence of 1000 and 64 values,
+  // and 8 kv heads, 16 rows take 33 us here and 61 there, 64 rows 113 and 62; with 8 sequences of 4096 and 4 heads,
+  // 12 rows 19 and 23, 64 rows 37 and 25; with 256 values 24 rows 39 and 35; with one sequence of 1000 and 64 values,
   // 64 rows 10.4 and 12.5.  So the estimates decide, and not the number of rows.
   const int only = debug_attention_kernel();
   if (a.type != FGQ_F32 && only != 1 && (a.rows > 8 || only == 2)) {

@@ -32,11 +32,11 @@ fgq_status launch_attention(const AttnArgs& a, unsigned blocks, cudaStream_t s) 
 // fp32 inputs double the queries' and probabilities' operands, and 256-value heads the sums: both keep to 8 rows.
 template <int NB, int GB>
 AttnKernel pick(bool split, int rows) {
-  constexpr int per_sm = attention_blocks_per_sm<NB>();
+  constexpr int per_sm = attention_blocks_per_sm<NB, 1>();
   constexpr float rate = NB == 2 ? 130.0f : (NB == 4 ? 83.0f : 60.0f);
   if (split) return {launch_attention<NB, GB, true, 1>, 8, per_sm, true, 8.0f, 3.5f, 0.7f * rate};
   if constexpr (NB <= 4) {
-    if (rows > 8) return {launch_attention<NB, GB, false, 2>, 16, per_sm, true, 8.0f, 3.5f, (NB == 2 ? 0.9f : 0.55f) * rate};
+    if (rows > 8) return {launch_attention<NB, GB, false, 2>, 16, attention_blocks_per_sm<NB, 2>(), true, 8.0f, 3.5f, (NB == 2 ? 0.9f : 0.85f) * rate};
   }
   return {launch_attention<NB, GB, false, 1>, 8, per_sm, true, 8.0f, 3.5f, rate};
 }

@@ -107,9 +107,10 @@ fgq_status fgq_kv_read(const fgq_kv_cache* cache, void* k, void* v, fgq_float_ty
  * Queries may have any magnitude, keys up to 1e30; values from 1e-18 to 1e30 that lie within 1e25 of one
  * another in a sequence, or are 0.  Smaller values lose precision (an error of at most 1e-25).
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad cache or type, kv_heads not dividing
- * q_heads, window < 0, a window without causal), FGQ_ERR_ALIGN as fgq_kv_append (q, out too),
- * FGQ_ERR_UNSUPPORTED (more than 2^31 - 1 blocks of work), FGQ_ERR_CUDA (also where a temporary
- * cannot be had).
+ * q_heads, causal neither 0 nor 1, window < 0, a window without causal, max_len < 0, a scale that is not
+ * finite or not above 0), FGQ_ERR_ALIGN as fgq_kv_append (q, out too), FGQ_ERR_UNSUPPORTED (more than
+ * 2^31 - 1 blocks of work, rows of the output B T q_heads or positions max_pages page_size, or T
+ * q_heads / kv_heads above 2^30), FGQ_ERR_CUDA (also where a temporary cannot be had).
  */
 fgq_status fgq_kv_attention(const fgq_kv_cache* cache, const void* q, fgq_float_type type, int B, int T,
                             int q_heads, int64_t q_batch_stride, int64_t q_token_stride,
@@ -134,8 +135,8 @@ fgq_status fgq_quantize_tokens(const void* x, fgq_float_type type, int P, int K,
  *   y[p][m] = scale[p] wscale[m] sum_k q[p][k] wq[m][k] + bias[m]
  *   q int8 [P][K], scale fp32 [P] (as from fgq_quantize_tokens); wq int8 [M][K], wscale fp32 [M]
  *   (as from fgq_quantize_weights_w8); bias fp32 [M] or NULL; y out, `ytype` [P][M] contiguous.
- * The integer sums are exact below 2^24 in magnitude (always for K <= 1040) and are rounded to
- * fp32 as they grow past that.  No alignment beyond the elements'; rows of q and wq that
+ * The integer sums are exact below 2^24 in magnitude (always for K <= 1040); past that they are cut off
+ * to fp32 once in 16 products, an error of at most K 2^-27 sum_k |q wq|.  No alignment beyond the elements'; rows of q and wq that
  * start on 16-byte boundaries (K a multiple of 16) are read fastest.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type), FGQ_ERR_ALIGN (scale, wscale, bias
  * or y not aligned to their elements), FGQ_ERR_UNSUPPORTED (P, K or M above 2^31 - 2^16),

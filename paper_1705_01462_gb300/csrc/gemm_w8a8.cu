@@ -15,8 +15,8 @@
 //              form), so that one wait covers both blocks' operands.
 // Two accumulators: the epilogue of a tile overlaps the MMAs of the next.  Few tiles split K over pairs
 // (fp32 partial sums, joined with scales and bias by a second kernel).
-// 4096 tokens, 4096 -> 8192, bf16: 179 us for the layer, 20 of them quantization and expansion, where the products
-// alone are due 148; at 2048 tokens, 4096 -> 4096 (50 us) the tensor pipe is active 59% of the time: 128 tiles on
+// 4096 tokens, 4096 -> 8192, bf16: 175 us for the layer, 20 of them quantization and expansion, where the products
+// alone are due 148; at 2048 tokens, 4096 -> 4096 (49 us) the tensor pipe is active 59% of the time: 128 tiles on
 // 76 pairs are two waves.
 // Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded and each role leaves its loop.  Nothing is on its way to a block that
 // leaves: both blocks wait for every arrival that the MMAs' commits make on their barriers, and meet before TMEM is freed.  After
@@ -384,8 +384,8 @@ GemmPlan plan_gemm_w8a8(int P, int K, int M) {
   GemmPlan g;
   g.pitch = ((int64_t)K + GW_KT - 1) / GW_KT * GW_KT;
   // 128 tokens a tile also where pairs remain for twice as many tiles: an MMA then reads half as much again of shared
-  // memory for its arithmetic, but K is split less or not at all (1000 tokens, 1024 -> 2048: 17.4 us, and 22.6 with
-  // 256; 4096 tokens, 512 -> 512: 14.4 and 18.3; 300 tokens, 8192 -> 2048: 32.9 and 33.1)
+  // memory for its arithmetic, but K is split less or not at all (1000 tokens, 1024 -> 2048: 16.7 us, and 22.7 with
+  // 256; 4096 tokens, 512 -> 512: 14.5 and 18.4; 300 tokens, 8192 -> 2048: 31.4 and 33.2)
   const int64_t tiles256 = (int64_t)((M + 2 * GW_BM - 1) / (2 * GW_BM)) * ((P + 255) / 256);
   g.bn = P > 128 && tiles256 * 2 > device_sms() / 2 ? 256 : 128;
   // K split over pairs where there are fewer tiles than half of them, 8 K-tiles each at least

@@ -17,7 +17,9 @@
 //
 // What is rounded: queries to fp16 after scaling each row by a power of two (exact for bf16 and fp16;
 // fp32 queries take two fp16 parts, SPLIT), and p s to fp16 (two parts for SPLIT; value codes are centred
-// so that its error meets values of the size of v).  Scores, statistics and sums are fp32; the instructions cut
+// so that its error meets values of the size of v).  For bf16 outputs that adds 1% to the output's own rounding, for fp16
+// ones a third (2.7e-4 of the output against 2.1e-4, single tokens over 4000): a second part would double the products with
+// the values (in kv_prompt.cu, where it was taken, that is a fifth of the time).  Scores, statistics and sums are fp32; the instructions cut
 // their sums off, so SPLIT adds each step's products to the output rounded (51 x 42000 tokens: 1.1e-5 of the
 // output to 6e-7, 207 to 222 us), which would not show in 16-bit outputs.
 //
@@ -33,10 +35,11 @@
 // between warps), and the warps' sums are joined in shared memory.  Up to eight chunks of one wave are a
 // cluster, which joins through shared memory too; more leave (r, l, sum) in fp32, which a second kernel joins.
 //
-// What bounds it: instructions.  One token each of 16 sequences of 16384 tokens, 32 query and 8 kv heads of 128
-// values, groups of 64: 80 us for 302 MB, 56% of the copy rate; ALU pipe 48%, tensor pipe 18%, issue slots 55% busy over
-// the launch.  More or fewer blocks an SM, shorter tiles, e4m3 products and codes with an offset in place of the
-// packed product were all slower.  One sequence of 131071 tokens, 64 query heads, groups of 128: 41 us (143 MB).
+// What bounds it.  One token each of 16 sequences of 16384 tokens, 32 query and 8 kv heads of 128 values, groups of 64: 80 us
+// for 302 MB, 56% of the copy rate, with no unit saturated: ALU pipe 52%, tensor pipe 19%, issue slots 60%, DRAM 52% busy
+// over the launch.  Twelve warps an SM do not fill one another's waits.  More or fewer blocks an SM, shorter tiles, e4m3
+// products and codes with an offset in place of the packed product were all slower.  One sequence of 131071 tokens, 64 query
+// heads, groups of 128: 41 us (143 MB).
 #pragma once
 
 #include "decoder_internal.cuh"

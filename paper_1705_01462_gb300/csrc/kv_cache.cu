@@ -6,8 +6,9 @@
 // a group find its extremes by shuffles.  Both kernels move each byte once; consecutive threads take consecutive
 // values of the dense side, and the 32 to 128 bytes of a cache row are written by neighbouring threads, so that
 // L2 merges them into whole sectors.
-// 4 x 8192 tokens, 8 heads of 128 values, bf16, groups of 64: read-back 41 us; appending 53 us, 174 MB at half
-// the copy rate: its 22 instructions a value keep the issue slots 76% busy (ALU pipe 59%).
+// 4 x 8192 tokens, 8 heads of 128 values, bf16, groups of 64, 174 MB each: appending 53 us, half the copy rate, as 22
+// instructions a value (about three of them the quotient's) keep the issue slots 76% busy (ALU pipe 59%); read-back 41 us, 16
+// instructions a value, issue slots 75% busy (ALU pipe 66%).
 #include <type_traits>
 
 #include "decoder_internal.cuh"

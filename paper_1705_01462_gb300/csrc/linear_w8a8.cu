@@ -587,8 +587,8 @@ fgq_status launch_few_float(FewArgs a, int type, cudaStream_t s) {
 
 inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
-// Tokens up to which the few-token kernel runs, in us here and on tcgen05: 64 tokens, 4096 -> 4096 19.5 and 25.4, 1024 ->
-// 8192 16.9 and 18.3, 8192 -> 1024 15.3 and 25.0; 80 tokens 29.0 and 25.4, 21.9 and 18.6, 20.6 and 25.2.
+// Tokens up to which the few-token kernel runs, in us here and on tcgen05: 64 tokens, 4096 -> 4096 19.8 and 25.0, 1024 ->
+// 8192 17.1 and 18.3, 8192 -> 1024 15.0 and 25.0; 80 tokens 29.0 and 25.1, 22.1 and 18.6, 20.6 and 25.0.
 constexpr int FEW_MAX_P = 64;
 
 fgq_status check_product(const void* x, int P, int K, const int8_t* wq, const float* wscale, int M, const float* bias,

@@ -620,16 +620,21 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           // m x + off; with 256 values always m x - yr by itself first, as dequantization leaves the time for it and a branch
-          // (`big`) made the compiler spill (36 rows: 41.8 us, with the branch 45)
+          // (`big`) made the compiler spill (36 rows: 42 us, with the branch 45)
           const float m = mk[2 * half + j], off = ev[2 * half + j] - er + 6.0f - less;
           const float last = D < 256 ? 0.0f : ev[2 * half + j] - er + 6.0f;
-          const uint64_t m2 = pack_f2(m, m), off2 = pack_f2(off, off), yr2 = pack_f2(-yr, -yr), last2 = pack_f2(last, last);
+          const uint64_t m2 = pack_f2(m, m), off2 = pack_f2(off, off), last2 = pack_f2(last, last);
           uint64_t s2 = 0;
 #pragma unroll
           for (int i = 8 * j; i < 8 * j + 8; ++i) {
             float a0, a1;
-            const uint64_t xx = pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
-            unpack_f2(D < 256 ? fma_f2(xx, m2, off2) : add_f2(add_f2(mul_f2(xx, m2), yr2), last2), a0, a1);
+            if constexpr (D < 256) {
+              unpack_f2(fma_f2(pack_f2(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), m2, off2), a0, a1);
+            } else {  // (the packed product and difference would become one multiply-add again)
+              a0 = __fsub_rn(__fmul_rn(__uint_as_float(x[2 * i]), m), yr);
+              a1 = __fsub_rn(__fmul_rn(__uint_as_float(x[2 * i + 1]), m), yr);
+              unpack_f2(add_f2(pack_f2(a0, a1), last2), a0, a1);
+            }
             a0 = ex2(a0);
             a1 = ex2(a1);
             s2 = add_f2(s2, pack_f2(a0, a1));

@@ -19,7 +19,8 @@
 // a row's largest x + ev at its last move, less 6, kept as its x and its ev (er), as a large x has no room for ev.  It moves
 // only when exceeded by 14 - 6 = 8 (as in kv_attention.cuh), and only then is O rescaled, after the products that add to
 // it.  Past scores of 4096 the differences x - r come before anything is added (`big`): in one multiply-add with the
-// rounded reference, scores past 2^25 would turn into infinities or zeros.
+// rounded reference, scores past 2^25 would turn into infinities or zeros.  `big` also stands for references of values past
+// 2^33, beside which the exponents of zeros and far smaller values are raised, so that their p stays above 2^-126.
 // What is rounded: lo + s c and probabilities to fp16 (11 bits); sums and statistics are fp32.  For bf16 outputs that is
 // an eighth of the output's own rounding (1.67e-3 of the output in all, 1.66e-3 the output's alone).  For fp16 outputs the
 // probabilities' would weigh as much as the output's (3.3e-4 in all, where the output's alone is 2.1e-4), so they take a second
@@ -566,7 +567,8 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         ok = false;
         break;
       }
-      if (__builtin_expect(__any_sync(FULL_MASK, xt > yr + er + 8.0f) || big, 0)) {
+      float less = yr + (er - 6.0f);  // what the probabilities' exponents leave off
+      if (__builtin_expect(__any_sync(FULL_MASK, xt > less + 14.0f) || big, 0)) {
         float yn = yr, en = er;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -577,6 +579,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         l = l * ex2(0.5f * by) * ex2(0.5f * by);  // 2^-ev is in it: where 2^by alone is no more, it may be
         yr = yn;
         er = en;
+        less = yr + (er - 6.0f);
         big = __any_sync(FULL_MASK, (fabsf(yr) > 4096.0f && yr != AT_M0) || er > 20.0f);
         if (un > 0 && __any_sync(FULL_MASK, f != 1.0f)) {  // once the products so far are in
           if (!mbar_wait_warp(&pv_done[q][(un - 1) & 1], ((un - 1) >> 1) & 1, tmo, abort_flag)) {
@@ -596,7 +599,6 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
           }
         }
       }
-      float less = yr;
       if (__builtin_expect(big, 0)) {
         // values far below the reference's, zeros among them, add nothing but still weigh: with an ev that leaves p above 2^-126
 #pragma unroll
@@ -610,7 +612,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) mk[i] = 1.0f;
-        less = 0.0f;
+        less = er - 6.0f;
       }
       float sum[4];
 #pragma unroll
@@ -621,7 +623,7 @@ __global__ void __launch_bounds__(PrCfg<D, NQT>::THREADS, 1) kv_prompt_kernel(co
         for (int j = 0; j < 2; ++j) {
           // m x + off; with 256 values always m x - yr by itself first, as dequantization leaves the time for it and a branch
           // (`big`) made the compiler spill (36 rows: 42 us, with the branch 45)
-          const float m = mk[2 * half + j], off = ev[2 * half + j] - er + 6.0f - less;
+          const float m = mk[2 * half + j], off = ev[2 * half + j] - less;
           const float last = D < 256 ? 0.0f : ev[2 * half + j] - er + 6.0f;
           const uint64_t m2 = pack_f2(m, m), off2 = pack_f2(off, off), last2 = pack_f2(last, last);
           uint64_t s2 = 0;

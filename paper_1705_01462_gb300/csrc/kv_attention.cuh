@@ -18,7 +18,7 @@
 // What is rounded: queries to fp16 after scaling each row by a power of two (exact for bf16 and fp16;
 // fp32 queries take two fp16 parts, SPLIT), and p s to fp16 (two parts for SPLIT; value codes are centred
 // so that its error meets values of the size of v).  For bf16 outputs that adds 1% to the output's own rounding, for fp16
-// ones a third (2.7e-4 of the output against 2.1e-4, single tokens over 4000): a second part would double the products with
+// ones a third (2.7e-4 of the output against 2.1e-4, single tokens over 4000; 3.4e-4 at most among 1000 cases): a second part would double the products with
 // the values (in kv_prompt.cu, where it was taken, that is a fifth of the time).  Scores, statistics and sums are fp32; the instructions cut
 // their sums off, so SPLIT adds each step's products to the output rounded (51 x 42000 tokens: 1.1e-5 of the
 // output to 6e-7, 207 to 222 us), which would not show in 16-bit outputs.

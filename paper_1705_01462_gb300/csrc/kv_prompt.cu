@@ -24,14 +24,14 @@
 // What is rounded: lo + s c and probabilities to fp16 (11 bits); sums and statistics are fp32.  For bf16 outputs that is
 // an eighth of the output's own rounding (1.67e-3 of the output in all, 1.66e-3 the output's alone).  For fp16 outputs the
 // probabilities' would weigh as much as the output's (3.3e-4 in all, where the output's alone is 2.1e-4), so they take a second
-// fp16 part in the other half of their scores' columns, and a second product with V (TWO): 264 us instead of 215 with the
-// queries below, 41 instead of 38 with 36 rows of 256 values.  Keys and values remain: 2.1e-4 in all where keys are of one
+// fp16 part in the other half of their scores' columns, and a second product with V (TWO): 262 us instead of 216 with the
+// queries below, 42 instead of 39 with 36 rows of 256 values.  Keys and values remain: 2.1e-4 in all where keys are of one
 // size, 2.2e-4 to 2.9e-4 where some of their dimensions are six times as large as the others.
 //
-// What bounds it, 2 x 1024 queries of 32 heads over 4096 to 6144 tokens, 8 kv heads of 128 values, 215 us where the products
+// What bounds it, 2 x 1024 queries of 32 heads over 4096 to 6144 tokens, 8 kv heads of 128 values, 216 us where the products
 // alone are due 92: tensor pipe 34% busy, ALU 46%, shared memory 39% of the time.  A tile of rows waits for
 // its next scores for a third of the time, as TMEM has room for one buffer of them beside the sums; a block's
-// start (8 us) and the second, partial wave of blocks are the rest.  36 rows of 256 values in a window of 4096: 38 us,
+// start (8 us) and the second, partial wave of blocks are the rest.  36 rows of 256 values in a window of 4096: 39 us,
 // dequantization (12 values a clock and SM) and the block's start.
 //
 // Warp roles (one block per SM): warps 0 .. 4 NQT - 1 softmax (TMEM lane = row); the next eight dequantize,

@@ -1,7 +1,8 @@
 /*
  * fgq_decoder.h -- C ABI of libfgq's operators for decoders served from quantized state: a paged
- * cache of keys and values held in 4 bits, the attention that reads it, and linear layers on
- * 8-bit integers with a scale for each token and each output channel.
+ * cache of keys and values held in 4 bits, the attention that reads it, linear layers on
+ * 8-bit integers with a scale for each token and each output channel, linear layers and mixtures of
+ * experts on 4-bit weights with a scale for each group, rotary positions, and the norms between blocks.
  *
  * The conventions of fgq.h hold: device pointers owned by the caller, calls asynchronous on the
  * given stream, host-detected errors returned, kernel-detected errors in the device error word
@@ -153,6 +154,173 @@ fgq_status fgq_gemm_w8a8(const int8_t* q, const float* scale, int P, int K, cons
  */
 fgq_status fgq_linear_w8a8(const void* x, fgq_float_type type, int P, int K, int64_t ldx, const int8_t* wq,
                            const float* wscale, int M, const float* bias, void* y, cudaStream_t stream);
+
+/*
+ * Rotary positions.  A head's first `rot` values are rot / 2 pairs, (j, j + rot / 2) with
+ * FGQ_ROPE_HALF and (2 j, 2 j + 1) with FGQ_ROPE_INTERLEAVED; pair j at position p turns by
+ * p freq_j radians, freq_j = base^(-2 j / rot) changed for long contexts as `scaling` says:
+ *   FGQ_ROPE_PLAIN    as it is;
+ *   FGQ_ROPE_LINEAR   freq_j / factor;
+ *   FGQ_ROPE_BASE     base factor^(rot / (rot - 2)) in the place of base, which divides the slowest pair by factor and
+ *                     leaves the fastest (rot = 2: as it is);
+ *   FGQ_ROPE_RAMP     with n_j = length freq_j / (2 pi), the turns over the context of `length` that a model was trained
+ *                     with, and k = (n_j - low) / (high - low) cut to [0, 1]: k freq_j + (1 - k) freq_j / factor.
+ * The table holds rint(2^64 freq_j / (2 pi)), so that the fraction of a turn at any position is an integer product modulo
+ * 2^64 and far positions lose nothing (freq_j to 2^-65 of a turn a position).
+ */
+typedef enum { FGQ_ROPE_HALF = 0, FGQ_ROPE_INTERLEAVED = 1 } fgq_rope_layout;
+typedef enum { FGQ_ROPE_PLAIN = 0, FGQ_ROPE_LINEAR = 1, FGQ_ROPE_BASE = 2, FGQ_ROPE_RAMP = 3 } fgq_rope_scaling;
+
+/*
+ * Writes the table of rot / 2 entries to HOST memory (no GPU is needed); copy it to the device for fgq_rope.
+ * Errors: FGQ_ERR_ARG (null table, rot not even or below 2, base not finite or not above 1, factor not finite or below 1,
+ * an unknown scaling; FGQ_ROPE_RAMP: length not above 0, high not above low or either not finite).  factor, length, low and high
+ * are looked at where the scaling uses them.
+ */
+fgq_status fgq_rope_table(int rot, double base, fgq_rope_scaling scaling, double factor, double length, double low,
+                          double high, uint64_t* table);
+
+/*
+ * Turns the heads of T tokens per sequence: token i < lens[b] (NULL: i < T) of sequence b stands at position starts[b] + i
+ * (any int32, and past it; negative ones turn backwards).  x, y: elements of `type`, [B][T][heads][head_dim], the last two axes
+ * contiguous, other strides in elements.  Each pair (a, b) becomes magnitude (a cos - b sin, b cos + a sin); inverse
+ * 1: the angle is negated (what gradients of the outputs turn by, and the way back where magnitude is 1).
+ * Values past rot, and tokens i >= lens[b], are those of x.  y may be x (with its strides), or must not overlap it.
+ * Products and sums are fp32, angles within 2^-24 of half a turn, y is rounded once.
+ * Errors: FGQ_ERR_ARG (null pointer, negative size, rot not even, below 2 or above head_dim, a bad type, layout or inverse, a
+ * magnitude that is not finite, y at x with other strides), FGQ_ERR_ALIGN (x or y not aligned to their elements,
+ * table not 8-byte, starts or lens not 4-byte aligned), FGQ_ERR_UNSUPPORTED (B T heads above 2^31 - 1, head_dim above 65536),
+ * FGQ_ERR_CUDA.
+ */
+fgq_status fgq_rope(const void* x, void* y, fgq_float_type type, int B, int T, int heads, int head_dim,
+                    int64_t x_batch_stride, int64_t x_token_stride, int64_t y_batch_stride, int64_t y_token_stride, int rot,
+                    fgq_rope_layout layout, const uint64_t* table, float magnitude, int inverse, const int32_t* starts,
+                    const int32_t* lens, cudaStream_t stream);
+
+/*
+ * What stands between two blocks of a decoder.  For each token, with x a block's output and r the residual stream:
+ *   u = post(x)                    a norm of the block's output, or x (post NULL)
+ *   s = r + scale gate u           element by element; gate NULL: 1; r NULL: 0
+ *   y = pre(s)                     the norm that the next block reads (pre NULL: none, y NULL)
+ * norm(z) = z' / sqrt(mean(z'^2) + eps) weight + bias, with z' = z (FGQ_NORM_RMS) or z - mean(z) (FGQ_NORM_LAYER); weight
+ * NULL: 1, bias NULL: 0; fp32 [K] both.
+ *   x      elements of `type`, [P][K], rows ldx elements apart (ldx >= K).
+ *   gate   elements of `type`, rows ldg elements apart; token p takes row p / tokens_per_gate.
+ *   r      elements of `rtype`, which is `type` or FGQ_F32, rows ldr apart.
+ *   s      out, elements of `rtype`, rows lds apart, or NULL (not written).  May be r, with its stride.
+ *   y      out, elements of `type`, [P][K] contiguous.  May be x where that is contiguous.
+ * Everything between is fp32 and y is formed from s before it is rounded.  Sums of squares are fp32: values up to 1e18.
+ * A token that holds NaN or Inf gives NaN (in s: what fp32 gives); other tokens are as without it.
+ * Errors: FGQ_ERR_ARG (null pointer, negative size, K = 0, bad types or kind, eps not above 0 or not finite, a scale that is not
+ * finite, tokens_per_gate < 1 with a gate, a stride below K, y without pre or pre without y, neither s nor y),
+ * FGQ_ERR_ALIGN (not aligned to the elements), FGQ_ERR_UNSUPPORTED (P or K above 2^31 - 2^16), FGQ_ERR_CUDA.
+ */
+typedef enum { FGQ_NORM_RMS = 0, FGQ_NORM_LAYER = 1 } fgq_norm_kind;
+typedef struct {
+  const float* weight;
+  const float* bias;
+  float eps;
+  int kind; /* fgq_norm_kind */
+} fgq_norm;
+
+fgq_status fgq_add_norm(const void* x, fgq_float_type type, int P, int K, int64_t ldx, const fgq_norm* post, const void* gate,
+                        int64_t ldg, int tokens_per_gate, float scale, const void* r, fgq_float_type rtype, int64_t ldr,
+                        void* s, int64_t lds, const fgq_norm* pre, void* y, cudaStream_t stream);
+
+/*
+ * Weights in 4 bits: `experts` matrices [rows][cols] (1 for a linear layer), a bf16 scale for each group of `group` (32, 64
+ * or 128) consecutive columns of a row; nibble n stands for (n - 8) scale.  Both arrays are laid out in tiles of 16 rows and 128
+ * columns, RT = ceil(rows / 16) by CT = ceil(cols / 128) of them:
+ *   codes   uint8 [experts][RT][CT][1024]: row g + 8 r (g < 8, r < 2), column 32 j + 8 t + i (j, t < 4, i < 8) of the tile is
+ *           nibble (0 4 1 5 2 6 3 7)[i] of little-endian 32-bit word ((8 r + g) 4 + t) 4 + j;
+ *   scales  bf16 [experts][RT][CT][16][128 / group].
+ * So a warp reads a tile as two runs of 512 bytes, and 16 bytes hold what one of its threads multiplies.  What stands for rows and
+ * columns past the matrix may be any finite values.  Both arrays 16-byte aligned.
+ */
+typedef struct {
+  const void* codes;
+  const void* scales;
+  int experts;
+  int rows;
+  int cols;
+  int group;
+} fgq_w4;
+
+/* Bytes of codes and of scales of one matrix (0 for sizes below 0 and a bad group). */
+size_t fgq_w4_code_bytes(int rows, int cols);
+size_t fgq_w4_scale_bytes(int rows, int cols, int group);
+
+/*
+ * w fp32 [experts][rows][cols] contiguous to codes -7 .. 7 in the arrays of `out` (written through its pointers): with amax
+ * a group's largest magnitude, scale = fp32(amax / 7) rounded up to bf16, code = fp32(w / scale) rounded half to even
+ * (0 where the scale is 0).  A group that holds NaN or Inf gets codes and scale 0, and FGQ_ERR_NONFINITE is recorded.
+ * Rows and columns past the matrix get codes and scales 0.
+ * fgq_read_weights_w4 gives back what codes and scales stand for, fp32, exactly.
+ * Errors: FGQ_ERR_ARG (null pointer, a size below 0, a bad group), FGQ_ERR_ALIGN (w not 4-byte, codes or scales not 16-byte
+ * aligned), FGQ_ERR_UNSUPPORTED (rows or cols above 2^31 - 2^16, more than 2^31 - 1 tiles in all), FGQ_ERR_CUDA.
+ */
+fgq_status fgq_quantize_weights_w4(const float* w, const fgq_w4* out, cudaStream_t stream);
+fgq_status fgq_read_weights_w4(const fgq_w4* w, float* out, cudaStream_t stream);
+
+/*
+ * A linear layer: y[p][m] = sum_k x[p][k] W[m][k] + bias[m].
+ *   x    elements of `type`, [P][K] with K = w->cols, rows ldx elements apart (ldx >= K); bias fp32 [M] or NULL.
+ *   y    out, elements of `type`, [P][M] contiguous, M = w->rows; may overlap x.
+ * Codes and 16-bit tokens are exact operands of the products (fp32 tokens: three bf16 parts, exactly), a group's sum takes
+ * its scale in fp32, y is rounded once.  More than 64 tokens of 16 bits run on fp16 operands on tcgen05: weights are exact there too within
+ * 2^26 of their row's largest scale, bf16 tokens within 2^26 of their largest value (smaller ones are off by at most 2^-40
+ * of those).  Scales 2^-100 to 2^100 there.  A token that holds NaN or Inf gives values that are not finite; other tokens are
+ * as without it.
+ * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type, bad weights, more than one matrix, ldx < K), FGQ_ERR_ALIGN (x or y
+ * not aligned to their elements, codes or scales not 16-byte, bias not 4-byte aligned), FGQ_ERR_UNSUPPORTED (P, K or M above
+ * 2^31 - 2^16, more than 2^31 - 1 tiles), FGQ_ERR_CUDA (also where a temporary cannot be had).
+ */
+fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx, const fgq_w4* w, const float* bias, void* y,
+                         cudaStream_t stream);
+
+/*
+ * The experts that a router picks for each token: logits l[p][e] = sum_k x[p][k] router[e][k], the `top` largest first (equal
+ * ones, and NaN, which counts as the smallest: lowest index first), and their weights
+ *   FGQ_SCORE_SOFTMAX   exp(l_e) / sum over all experts of exp(l), or over the chosen ones where renormalize is 1;
+ *   FGQ_SCORE_SIGMOID   1 / (1 + exp(-l_e)), divided by the chosen ones' sum where renormalize is 1;
+ * times scale.  Logits are within about an fp32 rounding of their exact values, and are compared before they are rounded to fp32.
+ *   router   elements of `rtype`, which is `type` or FGQ_F32, [E][K] contiguous.
+ *   ids      out, int32 [P][top];  weights  out, fp32 [P][top].
+ * A token that holds NaN gives weights NaN.
+ * Errors: FGQ_ERR_ARG (null pointer, negative size, K or E below 1, bad types or score, top outside 1 .. E, renormalize neither 0
+ * nor 1, a scale that is not finite, ldx < K), FGQ_ERR_ALIGN, FGQ_ERR_UNSUPPORTED (E above 1024, top above 32, P or K above
+ * 2^31 - 2^16), FGQ_ERR_CUDA (also where a temporary cannot be had).
+ */
+typedef enum { FGQ_SCORE_SOFTMAX = 0, FGQ_SCORE_SIGMOID = 1 } fgq_score;
+
+fgq_status fgq_route_tokens(const void* x, fgq_float_type type, int P, int K, int64_t ldx, const void* router,
+                            fgq_float_type rtype, int E, int top, fgq_score score, int renormalize, float scale,
+                            int32_t* ids, float* weights, cudaStream_t stream);
+
+/*
+ * The sum of chosen experts' gated feed-forward layers:
+ *   y[p] = sum_j weights[p][j] down_e (silu(gate_e x[p]) * (up_e x[p])),  e = ids[p][j],  silu(a) = a / (1 + exp(-a)).
+ *   gate, up   E matrices [F][K], of one group size;  down  E matrices [K][F].
+ *   ids        int32 [P][top], entries outside [0, E) are left out (a token without any gives zeros); an expert may be there
+ *              twice.  weights  fp32 [P][top].
+ *   y          out, elements of `type`, [P][K] contiguous; may be x where that is contiguous.
+ * Between the layers values are held as two bf16 parts, within 2^-17 (fp32: three, exactly fp32).  Sums are fp32, in an order that
+ * depends on the sizes and on the tokens that share an expert.  Made for few tokens: 128 are taken at a
+ * time, and each expert's weights are read again for those after.
+ * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type or weights, sizes that do not fit, top outside 1 .. 32, ldx < K),
+ * FGQ_ERR_ALIGN, FGQ_ERR_UNSUPPORTED (E above 1024, K or F above 2^31 - 2^16, more than 2^31 - 1 tiles), FGQ_ERR_CUDA (also
+ * where a temporary cannot be had).
+ */
+fgq_status fgq_experts_w4(const void* x, fgq_float_type type, int P, int64_t ldx, const int32_t* ids, const float* weights,
+                          int top, const fgq_w4* gate, const fgq_w4* up, const fgq_w4* down, void* y, cudaStream_t stream);
+
+/*
+ * A mixture-of-experts layer: fgq_route_tokens, then fgq_experts_w4, the choice in temporaries of the library.  Results and errors
+ * are those of the two calls.
+ */
+fgq_status fgq_moe_w4(const void* x, fgq_float_type type, int P, int64_t ldx, const void* router, fgq_float_type rtype, int top,
+                      fgq_score score, int renormalize, float scale, const fgq_w4* gate, const fgq_w4* up, const fgq_w4* down,
+                      void* y, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

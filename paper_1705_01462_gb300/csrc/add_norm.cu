@@ -1,0 +1,300 @@
+// Between two blocks of a decoder: the norm of a block's output, its gate and scale, the residual sum, and the norm that the
+// next block reads, in one pass over the data.
+//
+//   u = post(x),  s = r + scale gate u,  y = pre(s);   norm(z) = z' / sqrt(mean z'^2 + eps) weight + bias
+//
+// A row is held in registers (fp32) from its load to its last store, so each input is read and each output written once:
+// the kernel is bound by those bytes.  The threads of a row each hold up to CH pieces of 8 elements; a layer norm takes its mean
+// first and then the squares of what is left, so that a large mean costs no bits.  Sums of a row meet in the same order
+// always: in registers, by shuffles, over the warps through shared memory.  Rows past 16384 elements are read again for
+// each sum instead (long_kernel).
+#include <cmath>
+
+#include "decoder_internal.cuh"
+
+namespace fgq {
+namespace {
+
+using namespace dec;
+
+struct NormArgs {
+  const void* x;
+  const void* gate;
+  const void* r;
+  void* s;
+  void* y;
+  int64_t ldx, ldg, ldr, lds;
+  fgq_norm post, pre;
+  float scale;
+  int P, K, tokens_per_gate, has_post, has_pre;
+};
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL_MASK, v, o);
+  return v;
+}
+
+// Sum over the NT threads of a row, in all of them.  `red` is the block's; two sums in turn take its two halves, so that
+// one barrier a sum is enough.
+template <int NT>
+__device__ __forceinline__ float row_sum(float v, float (*red)[32], int& turn) {
+  v = warp_sum(v);
+  if constexpr (NT > 32) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (lane == 0) red[turn][warp] = v;
+    __syncthreads();
+    v = lane < NT / 32 ? red[turn][lane] : 0.0f;
+    v = warp_sum(v);
+    turn ^= 1;
+  }
+  return v;
+}
+
+template <typename T, bool VEC>
+__device__ __forceinline__ void load_piece(const T* row, int c, int tid, int NT, int K, float (&v)[8]) {
+  if constexpr (VEC) {
+    const int k = 8 * (tid + c * NT);
+    if (k < K) {
+      load8(row + k, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int k = tid + (8 * c + i) * NT;
+      v[i] = k < K ? to_float(row[k]) : 0.0f;
+    }
+  }
+}
+template <typename T, bool VEC>
+__device__ __forceinline__ void store_piece(T* row, int c, int tid, int NT, int K, const float (&v)[8]) {
+  if constexpr (VEC) {
+    const int k = 8 * (tid + c * NT);
+    if (k < K) store8(row + k, v);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int k = tid + (8 * c + i) * NT;
+      if (k < K) from_float(v[i], row[k]);
+    }
+  }
+}
+// Whether element i of piece c is in the row.
+template <bool VEC>
+__device__ __forceinline__ bool in_row(int c, int i, int tid, int NT, int K) {
+  return VEC ? 8 * (tid + c * NT) < K : tid + (8 * c + i) * NT < K;
+}
+
+// v to its norm, in registers.
+template <int NT, int CH, bool VEC>
+__device__ __forceinline__ void normalise(float (&v)[CH][8], const fgq_norm& n, int K, int tid, float (*red)[32], int& turn) {
+  const float inv_k = 1.0f / (float)K;
+  if (n.kind == FGQ_NORM_LAYER) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum += v[c][i];
+    const float mean = row_sum<NT>(sum, red, turn) * inv_k;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[c][i] = in_row<VEC>(c, i, tid, NT, K) ? v[c][i] - mean : 0.0f;
+  }
+  float sq = 0.0f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sq = fmaf(v[c][i], v[c][i], sq);
+  const float inv = rsqrtf(row_sum<NT>(sq, red, turn) * inv_k + n.eps);
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    float w[8], b[8];
+    if (n.weight) load_piece<float, VEC>(n.weight, c, tid, NT, K, w);
+    if (n.bias) load_piece<float, VEC>(n.bias, c, tid, NT, K, b);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float z = v[c][i] * inv;
+      if (n.weight) z *= w[i];
+      if (n.bias) z += b[i];
+      v[c][i] = z;
+    }
+  }
+}
+
+// NT threads a row; blocks of at least 128 threads.
+template <typename T, typename R, int NT, int CH, bool VEC>
+__global__ void __launch_bounds__(NT < 128 ? 128 : NT) add_norm_kernel(const __grid_constant__ NormArgs a) {
+  constexpr int RPB = NT < 128 ? 128 / NT : 1;
+  __shared__ float red[2][32];
+  const int tid = threadIdx.x % NT, p = (int)blockIdx.x * RPB + (int)threadIdx.x / NT;
+  if (p >= a.P) return;  // whole warps; with one row a block there is no such block
+  int turn = 0;
+  float v[CH][8], r[CH][8];
+  const T* x = static_cast<const T*>(a.x) + p * a.ldx;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) load_piece<T, VEC>(x, c, tid, NT, a.K, v[c]);
+  if (a.r) {
+    const R* row = static_cast<const R*>(a.r) + p * a.ldr;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) load_piece<R, VEC>(row, c, tid, NT, a.K, r[c]);
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[c][i] = 0.0f;
+  }
+  if (a.has_post) normalise<NT, CH, VEC>(v, a.post, a.K, tid, red, turn);
+  const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)(p / a.tokens_per_gate) * a.ldg : nullptr;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    float g[8];
+    if (gate) load_piece<T, VEC>(gate, c, tid, NT, a.K, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float u = gate ? v[c][i] * g[i] : v[c][i];
+      v[c][i] = in_row<VEC>(c, i, tid, NT, a.K) ? fmaf(a.scale, u, r[c][i]) : 0.0f;  // past the row: no infinity times 0
+    }
+    if (a.s) store_piece<R, VEC>(static_cast<R*>(a.s) + p * a.lds, c, tid, NT, a.K, v[c]);
+  }
+  if (a.has_pre) {
+    normalise<NT, CH, VEC>(v, a.pre, a.K, tid, red, turn);
+    T* y = static_cast<T*>(a.y) + (int64_t)p * a.K;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) store_piece<T, VEC>(y, c, tid, NT, a.K, v[c]);
+  }
+}
+
+// Rows that registers do not hold, a block each: every sum reads the row again.  Elements are written in the last loop only,
+// each by the thread that reads it, so outputs may take the place of inputs.
+constexpr int LONG_THREADS = 1024;
+template <typename T, typename R>
+__global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constant__ NormArgs a) {
+  __shared__ float red[2][32];
+  int turn = 0;
+  const int p = blockIdx.x;
+  const T* x = static_cast<const T*>(a.x) + p * a.ldx;
+  const R* r = a.r ? static_cast<const R*>(a.r) + p * a.ldr : nullptr;
+  const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)(p / a.tokens_per_gate) * a.ldg : nullptr;
+  const float inv_k = 1.0f / (float)a.K;
+  // sums of f(k) over the row, in pieces that keep fp32's bits
+  auto sum_of = [&](auto f) {
+    float total = 0.0f;
+    for (int k = threadIdx.x; k < a.K; k += LONG_THREADS * 64) {
+      float part = 0.0f;
+      for (int i = 0; i < 64; ++i) {
+        const int64_t at = (int64_t)k + (int64_t)i * LONG_THREADS;
+        if (at < a.K) part += f((int)at);
+      }
+      total += part;
+    }
+    return row_sum<LONG_THREADS>(total, red, turn);
+  };
+  auto stats = [&](auto value, const fgq_norm& n, float& mean, float& inv) {
+    mean = 0.0f;
+    if (n.kind == FGQ_NORM_LAYER) mean = sum_of(value) * inv_k;
+    const float m = mean;
+    inv = rsqrtf(sum_of([&](int k) {
+                   const float z = value(k) - m;
+                   return z * z;
+                 }) * inv_k + n.eps);
+  };
+  auto apply = [&](float z, const fgq_norm& n, float mean, float inv, int k) {
+    z = (z - mean) * inv;
+    if (n.weight) z *= __ldg(n.weight + k);
+    return n.bias ? z + __ldg(n.bias + k) : z;
+  };
+  float m0 = 0.0f, i0 = 0.0f, m1 = 0.0f, i1 = 0.0f;
+  if (a.has_post) stats([&](int k) { return to_float(x[k]); }, a.post, m0, i0);
+  auto stream = [&](int k) {
+    float u = to_float(x[k]);
+    if (a.has_post) u = apply(u, a.post, m0, i0, k);
+    if (gate) u *= to_float(gate[k]);
+    return fmaf(a.scale, u, r ? to_float(r[k]) : 0.0f);
+  };
+  if (a.has_pre) stats(stream, a.pre, m1, i1);
+  for (int64_t at = threadIdx.x; at < a.K; at += LONG_THREADS) {
+    const int k = (int)at;
+    const float s = stream(k);
+    if (a.s) from_float(s, static_cast<R*>(a.s)[p * a.lds + k]);
+    if (a.has_pre) from_float(apply(s, a.pre, m1, i1, k), static_cast<T*>(a.y)[(int64_t)p * a.K + k]);
+  }
+}
+
+template <typename T, typename R, bool VEC>
+fgq_status launch_add_norm(const NormArgs& a, cudaStream_t s) {
+  const unsigned P = (unsigned)a.P;
+  // few rows: one piece a thread, so that a row's loads are all in flight at once; many: two, for fewer barriers a byte
+  const bool few = a.P <= 4 * device_sms();
+  if (a.K <= 512)
+    add_norm_kernel<T, R, 32, 2, VEC><<<(P + 3) / 4, 128, 0, s>>>(a);
+  else if (a.K <= 1024)
+    add_norm_kernel<T, R, 128, 1, VEC><<<P, 128, 0, s>>>(a);
+  else if (a.K <= 2048)
+    few ? add_norm_kernel<T, R, 256, 1, VEC><<<P, 256, 0, s>>>(a) : add_norm_kernel<T, R, 128, 2, VEC><<<P, 128, 0, s>>>(a);
+  else if (a.K <= 4096)
+    few ? add_norm_kernel<T, R, 512, 1, VEC><<<P, 512, 0, s>>>(a) : add_norm_kernel<T, R, 256, 2, VEC><<<P, 256, 0, s>>>(a);
+  else if (a.K <= 8192)
+    add_norm_kernel<T, R, 512, 2, VEC><<<P, 512, 0, s>>>(a);
+  else if (a.K <= 16384)
+    add_norm_kernel<T, R, 1024, 2, VEC><<<P, 1024, 0, s>>>(a);
+  else
+    long_kernel<T, R><<<P, LONG_THREADS, 0, s>>>(a);
+  return after_launch();
+}
+
+template <typename T, typename R>
+fgq_status launch_add_norm(const NormArgs& a, int type, int rtype, cudaStream_t s) {
+  auto rows16 = [&](const void* p, int64_t ld, int t) { return !p || (aligned(p, 16) && stride16(ld, t)); };
+  const bool vec = a.K % 8 == 0 && rows16(a.x, a.ldx, type) && rows16(a.gate, a.ldg, type) && rows16(a.r, a.ldr, rtype) &&
+                   rows16(a.s, a.lds, rtype) && rows16(a.y, a.K, type) && aligned(a.post.weight, 16) && aligned(a.post.bias, 16) &&
+                   aligned(a.pre.weight, 16) && aligned(a.pre.bias, 16);
+  return vec ? launch_add_norm<T, R, true>(a, s) : launch_add_norm<T, R, false>(a, s);
+}
+
+// FGQ_OK, or what is wrong with a norm.
+fgq_status check_norm(const fgq_norm* n) {
+  if (!n) return FGQ_OK;
+  if (n->kind != FGQ_NORM_RMS && n->kind != FGQ_NORM_LAYER) return FGQ_ERR_ARG;
+  if (!(n->eps > 0.0f) || nonfinite_host(n->eps)) return FGQ_ERR_ARG;
+  return FGQ_OK;
+}
+
+}  // namespace
+}  // namespace fgq
+
+using namespace fgq;
+
+extern "C" fgq_status fgq_add_norm(const void* x, fgq_float_type type, int P, int K, int64_t ldx, const fgq_norm* post,
+                                   const void* gate, int64_t ldg, int tokens_per_gate, float scale, const void* r,
+                                   fgq_float_type rtype, int64_t ldr, void* s, int64_t lds, const fgq_norm* pre, void* y,
+                                   cudaStream_t stream) {
+  if (P < 0 || K < 1 || !dec::valid_float(type) || !dec::valid_float(rtype) || (rtype != type && rtype != FGQ_F32)) return FGQ_ERR_ARG;
+  if (check_norm(post) != FGQ_OK || check_norm(pre) != FGQ_OK || dec::nonfinite_host(scale)) return FGQ_ERR_ARG;
+  if (P == 0) return FGQ_OK;
+  if ((pre != nullptr) != (y != nullptr) || (!y && !s) || (gate && tokens_per_gate < 1) || !x) return FGQ_ERR_ARG;
+  if (P > 1 && (ldx < K || (r && ldr < K) || (s && lds < K))) return FGQ_ERR_ARG;
+  if (gate && P > tokens_per_gate && ldg < K) return FGQ_ERR_ARG;
+  if (P > dec::MAX_SIZE || K > dec::MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
+  const uintptr_t e = dec::float_bytes(type), re = dec::float_bytes(rtype);
+  if (!dec::aligned(x, e) || !dec::aligned(gate, e) || !dec::aligned(r, re) || !dec::aligned(s, re) || !dec::aligned(y, e))
+    return FGQ_ERR_ALIGN;
+  for (const fgq_norm* n : {post, pre})
+    if (n && (!dec::aligned(n->weight, 4) || !dec::aligned(n->bias, 4))) return FGQ_ERR_ALIGN;
+  NormArgs a = {};
+  a.x = x, a.gate = gate, a.r = r, a.s = s, a.y = y;
+  // a single row may have any stride
+  a.ldx = P > 1 ? ldx : 0, a.ldr = P > 1 ? ldr : 0, a.lds = P > 1 ? lds : 0, a.ldg = gate && P > tokens_per_gate ? ldg : 0;
+  if (post) a.post = *post, a.has_post = 1;
+  if (pre) a.pre = *pre, a.has_pre = 1;
+  a.scale = scale, a.P = P, a.K = K, a.tokens_per_gate = gate ? tokens_per_gate : 1;
+  if (type == FGQ_F32) return launch_add_norm<float, float>(a, type, rtype, stream);
+  if (type == FGQ_BF16)
+    return rtype == FGQ_F32 ? launch_add_norm<__nv_bfloat16, float>(a, type, rtype, stream)
+                            : launch_add_norm<__nv_bfloat16, __nv_bfloat16>(a, type, rtype, stream);
+  return rtype == FGQ_F32 ? launch_add_norm<__half, float>(a, type, rtype, stream)
+                          : launch_add_norm<__half, __half>(a, type, rtype, stream);
+}

@@ -1,0 +1,556 @@
+// Linear layers on 4-bit weights with a scale for each group: quantization, the product for few tokens, and operands
+// of the product for many.
+//
+// y[p][m] = sum_g s_mg sum_{k in g} c_mk x_pk + bias_m.  Codes c are exact matrix operands and 16-bit tokens are as they are
+// (fp32 ones in three bf16 parts), so a group's sum is that of exact products in fp32, and takes its scale in fp32.
+#include <type_traits>
+
+#include "linear_internal.cuh"
+#include "w4.cuh"
+
+namespace fgq {
+namespace w4 {
+namespace {
+
+// ------------------------------------------------------------------ weights to 4 bits and back
+// A warp a tile of 16 rows and 128 columns, lane (g, t) as in the products: words j of rows g and g + 8.
+__global__ void __launch_bounds__(256) quantize_kernel(const float* __restrict__ w, uint8_t* codes, uint16_t* scales, int rows,
+                                                       int cols, int rt, int ct, int per, int64_t tiles, unsigned int* err) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  for (int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); at < tiles; at += (int64_t)gridDim.x * 8) {
+    const int64_t e = at / ((int64_t)rt * ct);
+    const int in = (int)(at - e * rt * ct), mt = in / ct, kt = in - mt * ct;
+    bool bad = false;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int m = mt * TILE_ROWS + g + 8 * r;
+      const float* row = w + (e * rows + m) * cols;
+      float v[4][8], amax[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        amax[j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int64_t k = (int64_t)kt * TILE_COLS + 32 * j + 8 * t + i;
+          v[j][i] = m < rows && k < cols ? row[k] : 0.0f;
+          amax[j] = max_nan(amax[j], fabsf(v[j][i]));
+        }
+        amax[j] = max_nan(amax[j], __shfl_xor_sync(FULL_MASK, amax[j], 1));
+        amax[j] = max_nan(amax[j], __shfl_xor_sync(FULL_MASK, amax[j], 2));
+      }
+      uint32_t word[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float top = amax[j];  // of the whole group
+        if (per == 2) top = max_nan(amax[j & ~1], amax[j | 1]);
+        if (per == 1) top = max_nan(max_nan(amax[0], amax[1]), max_nan(amax[2], amax[3]));
+        if (nonfinite(top)) {
+          bad = true;
+          top = 0.0f;
+        }
+        const float q = __fdiv_rn(top, 7.0f);
+        const uint32_t up = (__float_as_uint(q) + 0xffffu) & 0xffff0000u;  // a value above bf16's largest is none: top / 7 is
+        const float s = __uint_as_float(up);                               // below it
+        if (t == 0 && j % (4 / per) == 0) scales[at * (TILE_ROWS * per) + (g + 8 * r) * per + j / (4 / per)] = (uint16_t)(up >> 16);
+        word[j] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int c = s > 0.0f ? __float2int_rn(fminf(fmaxf(__fdiv_rn(v[j][i], s), -7.0f), 7.0f)) : 0;
+          word[j] |= (uint32_t)(c + 8) << (4 * ((i >> 1) + 4 * (i & 1)));
+        }
+      }
+      reinterpret_cast<uint4*>(codes + at * TILE_BYTES)[32 * r + lane] = make_uint4(word[0], word[1], word[2], word[3]);
+    }
+    if (bad) record_error(err, FGQ_ERR_NONFINITE);
+  }
+}
+
+__global__ void __launch_bounds__(256) read_kernel(const uint8_t* codes, const uint16_t* scales, float* __restrict__ w, int rows,
+                                                   int cols, int rt, int ct, int per, int64_t tiles) {
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  for (int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); at < tiles; at += (int64_t)gridDim.x * 8) {
+    const int64_t e = at / ((int64_t)rt * ct);
+    const int in = (int)(at - e * rt * ct), mt = in / ct, kt = in - mt * ct;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int m = mt * TILE_ROWS + g + 8 * r;
+      const uint4 v = reinterpret_cast<const uint4*>(codes + at * TILE_BYTES)[32 * r + lane];
+      const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float s = __uint_as_float((uint32_t)scales[at * (TILE_ROWS * per) + (g + 8 * r) * per + j / (4 / per)] << 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int64_t k = (int64_t)kt * TILE_COLS + 32 * j + 8 * t + i;
+          const int n = (int)(word[j] >> (4 * ((i >> 1) + 4 * (i & 1))) & 15u);
+          if (m < rows && k < cols) w[(e * rows + m) * cols + k] = (float)(n - 8) * s;
+        }
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------ tokens as operand rows
+// A block a token: fp32 in three bf16 parts, 16-bit types copied to aligned rows; zeros up to a multiple of 8.
+template <typename T>
+__global__ void __launch_bounds__(256) copy_tokens_kernel(const T* __restrict__ x, int P, int K, int64_t ldx, uint16_t* dst, int64_t pitch) {
+  pdl_trigger();
+  const T* row = x + blockIdx.x * ldx;
+  for (int64_t k = threadIdx.x; k < pitch; k += 256) {
+    if constexpr (std::is_same<T, float>::value) {
+      uint16_t p[3];
+      three_parts(k < K ? row[k] : 0.0f, p);
+      uint16_t* to = dst + 3 * pitch * blockIdx.x + k;
+      to[0] = p[0], to[pitch] = p[1], to[2 * pitch] = p[2];
+    } else {
+      dst[pitch * blockIdx.x + k] = k < K ? *reinterpret_cast<const uint16_t*>(row + k) : (uint16_t)0;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ few tokens
+// A block takes 32 rows of weights, 8 NT columns of tokens and its share of K; its 8 warps take every eighth tile column,
+// weights from memory to registers two tiles ahead, tokens by copies of their own into shared memory as far ahead, so
+// that no barrier stands in the loop.  The warps' sums are joined in shared memory, and those of a cluster's blocks, which
+// split K where rows alone leave SMs idle, through it too, always in the same order.
+constexpr int WARPS = 8, MT = 2, ROWS = MT * TILE_ROWS, AHEAD = 2;
+
+struct FewArgs {
+  Matrix w;
+  TokenRows x;
+  const float* bias;
+  void* y;
+  int P, M, ytype, splits;
+};
+
+template <int NT>
+struct FewSmem {
+  static constexpr int STAGE = 8 * NT * 256, RING = WARPS * AHEAD * STAGE;
+  static constexpr int SUMS = WARPS * 8 * NT * (ROWS + 1) * 4;
+  static constexpr int BYTES = RING > SUMS ? RING : SUMS;
+};
+
+template <typename T, int NT, int PER, int PARTS>
+__global__ void __launch_bounds__(32 * WARPS) few_kernel(const __grid_constant__ FewArgs a) {
+  using S = FewSmem<NT>;
+  constexpr int CPT = columns_per_token(PARTS), TOKENS = 8 * NT / CPT;
+  extern __shared__ __align__(16) uint8_t w4_smem[];
+  __shared__ int64_t rows[8 * NT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int sp = blockIdx.x % a.splits, mt0 = blockIdx.x / a.splits * MT, p0 = blockIdx.y * TOKENS;
+  const int np = min(TOKENS, a.P - p0);
+  if (threadIdx.x < 8 * NT) {
+    const int tok = threadIdx.x / CPT, part = threadIdx.x % CPT;
+    rows[threadIdx.x] = tok < np && part < PARTS ? 2 * ((p0 + tok) * a.x.pitch + part * (a.x.pitch / PARTS)) : -1;
+  }
+  const int c0 = (int)((int64_t)a.w.ct * sp / a.splits), c1 = (int)((int64_t)a.w.ct * (sp + 1) / a.splits);
+  const uint8_t* xb = static_cast<const uint8_t*>(a.x.data);
+  uint8_t* ring = w4_smem + warp * AHEAD * S::STAGE;
+  const uint32_t ring_at = smem_u32(ring);
+  Tile<PER> tile[AHEAD][MT];
+  auto weights = [&](int i, int kt) {
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)  // a row tile past the last is read as the last
+      tile[i][mt].load(a.w.codes, a.w.scales, (int64_t)min(mt0 + mt, a.w.rt - 1) * a.w.ct + kt, lane);
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (c0 + warp + i * WARPS < c1) weights(i, c0 + warp + i * WARPS);
+  __syncthreads();  // rows
+  pdl_wait();
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) {
+    const int kt = c0 + warp + i * WARPS;
+    if (kt < c1) fetch_tokens<NT>(ring_at + i * S::STAGE, xb, rows, kt, a.x.kvalid, lane);
+    cp_async_commit();
+  }
+  float sum[MT][NT][4];
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[mt][nt][e] = 0.0f;
+  for (int kt = c0 + warp; kt < c1; kt += AHEAD * WARPS) {
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int at = kt + i * WARPS, next = at + AHEAD * WARPS;
+      if (at >= c1) break;  // the same for the whole warp
+      cp_async_wait<AHEAD - 1>();
+      __syncwarp();
+      multiply<T, MT, NT, PER>(tile[i], ring + i * S::STAGE, sum, lane);
+      __syncwarp();
+      if (next < c1) {
+        weights(i, next);
+        fetch_tokens<NT>(ring_at + i * S::STAGE, xb, rows, next, a.x.kvalid, lane);
+      }
+      cp_async_commit();
+    }
+  }
+  cp_async_wait<0>();
+  __syncthreads();  // the rings are read
+  float* sums = reinterpret_cast<float*>(w4_smem);  // [warp][column][ROWS + 1]
+  const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        sums[(warp * 8 * NT + 8 * nt + 2 * t + (e & 1)) * (ROWS + 1) + 16 * mt + g + 8 * (e >> 1)] = sum[mt][nt][e];
+  __syncthreads();
+  auto put = [&](int i, float v) {  // sum i = token * 32 + row
+    const int m = mt0 * TILE_ROWS + i % ROWS, p = p0 + i / ROWS;
+    if (m < a.M && p < a.P)
+      store_typed(a.y, a.ytype, (int64_t)p * a.M + m, fmaf(v, Operand<T>::BACK, a.bias ? __ldg(a.bias + m) : 0.0f));
+  };
+  for (int i = threadIdx.x; i < np * ROWS; i += 32 * WARPS) {
+    float* at = sums + i / ROWS * CPT * (ROWS + 1) + i % ROWS;
+    float v = 0.0f;
+#pragma unroll
+    for (int k = 0; k < WARPS; ++k)
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) v += at[(k * 8 * NT + part) * (ROWS + 1)];
+    if (a.splits == 1)
+      put(i, v);
+    else
+      *at = v;  // the first warp's place: no other thread reads it in this loop
+  }
+  if (a.splits > 1) {
+    cluster_sync();
+    for (int i = threadIdx.x + 32 * WARPS * sp; i < np * ROWS; i += 32 * WARPS * a.splits) {
+      float v = 0.0f;
+      for (int k = 0; k < a.splits; ++k) v += ld_cluster(sums + i / ROWS * CPT * (ROWS + 1) + i % ROWS, k);
+      put(i, v);
+    }
+    cluster_sync();  // no block leaves while another may read its sums
+  }
+}
+
+template <typename T, int NT, int PER, int PARTS>
+fgq_status launch_few_kernel(const FewArgs& a, bool early, cudaStream_t s) {
+  constexpr int TOKENS = 8 * NT / columns_per_token(PARTS);
+  if (!tc::smem_attr_once<few_kernel<T, NT, PER, PARTS>>(FewSmem<NT>::BYTES)) return FGQ_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((a.w.rt + MT - 1) / MT * a.splits), (unsigned)((a.P + TOKENS - 1) / TOKENS));
+  cfg.blockDim = dim3(32 * WARPS);
+  cfg.dynamicSmemBytes = FewSmem<NT>::BYTES;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  unsigned n = 0;
+  if (early) {
+    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[n++].val.programmaticStreamSerializationAllowed = 1;
+  }
+  if (a.splits > 1) {
+    attr[n].id = cudaLaunchAttributeClusterDimension;
+    attr[n].val.clusterDim.x = (unsigned)a.splits;
+    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+    ++n;
+  }
+  cfg.attrs = attr;
+  cfg.numAttrs = n;
+  return after_launch(cudaLaunchKernelEx(&cfg, few_kernel<T, NT, PER, PARTS>, a));
+}
+
+template <typename T, int NT, int PARTS>
+fgq_status launch_few_per(const FewArgs& a, bool early, cudaStream_t s) {
+  if (a.w.per == 4) return launch_few_kernel<T, NT, 4, PARTS>(a, early, s);
+  if (a.w.per == 2) return launch_few_kernel<T, NT, 2, PARTS>(a, early, s);
+  return launch_few_kernel<T, NT, 1, PARTS>(a, early, s);
+}
+
+template <typename T, int PARTS>
+fgq_status launch_few_nt(FewArgs a, bool early, cudaStream_t s) {
+  const int64_t columns = (int64_t)a.P * columns_per_token(PARTS);
+  const int nt = columns <= 8 ? 1 : (columns <= 16 ? 2 : 4);
+  const int tokens = 8 * nt / columns_per_token(PARTS);
+  // blocks that share a K: up to two an SM, each with a tile for each warp
+  const int64_t blocks = (int64_t)((a.w.rt + MT - 1) / MT) * ((a.P + tokens - 1) / tokens);
+  a.splits = 1;
+  while (a.splits < 8 && blocks * a.splits * 2 <= 2 * device_sms() && a.w.ct >= 2 * WARPS * a.splits) a.splits *= 2;
+  // more tokens than a grid has rows of blocks for
+  const int most = 65535 * tokens;
+  for (; a.P > most; a.P -= most) {
+    FewArgs part = a;
+    part.P = most;
+    const fgq_status st = launch_few_per<T, 4, PARTS>(part, early, s);
+    if (st != FGQ_OK) return st;
+    a.x.data = static_cast<const uint16_t*>(a.x.data) + most * a.x.pitch;
+    a.y = static_cast<uint8_t*>(a.y) + (int64_t)most * a.M * float_bytes(a.ytype);
+    early = false;
+  }
+  return nt == 1 ? launch_few_per<T, 1, PARTS>(a, early, s)
+                 : nt == 2 ? launch_few_per<T, 2, PARTS>(a, early, s) : launch_few_per<T, 4, PARTS>(a, early, s);
+}
+
+fgq_status launch_few(const FewArgs& a, bool early, cudaStream_t s) {
+  if (a.ytype == FGQ_F32) return launch_few_nt<__nv_bfloat16, 3>(a, early, s);
+  return a.ytype == FGQ_BF16 ? launch_few_nt<__nv_bfloat16, 1>(a, early, s) : launch_few_nt<__half, 1>(a, early, s);
+}
+
+// ------------------------------------------------------------------ operands of the product for many tokens
+// Weights as fp16 rows: c s 2^(12 - e) with 2^e <= the row's largest scale < 2^(e + 1), which has 11 bits at most and is exact down
+// to 2^-29 of it.  Blocks (row tile, part of K): each finds its 16 rows' largest scales, all of them, first.
+constexpr int EX_WARPS = 8;
+__global__ void __launch_bounds__(32 * EX_WARPS) expand_weights_kernel(const __grid_constant__ Matrix w, __half* dst, int64_t pitch,
+                                                                       int M, float* wscale) {
+  __shared__ uint32_t top[TILE_ROWS];
+  pdl_trigger();
+  const int mt = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  if (threadIdx.x < TILE_ROWS) top[threadIdx.x] = 0u;
+  __syncthreads();
+  const uint16_t* sc = w.scales + (int64_t)mt * w.ct * TILE_ROWS * w.per;
+  // magnitudes compare as whole numbers; the order of maxima does not matter
+  for (int64_t i = threadIdx.x; i < (int64_t)w.ct * TILE_ROWS * w.per; i += 32 * EX_WARPS)
+    atomicMax(&top[(int)(i / w.per) % TILE_ROWS], (uint32_t)(__ldg(sc + i) & 0x7fffu));
+  __syncthreads();
+  auto exponent = [&](int r) {  // of the row's largest scale, subnormal ones as the smallest normal
+    const int e = (int)(top[r] >> 7) - 127;
+    return e < -126 ? -126 : e;
+  };
+  if (blockIdx.y == 0 && threadIdx.x < TILE_ROWS && mt * TILE_ROWS + (int)threadIdx.x < M)
+    wscale[mt * TILE_ROWS + threadIdx.x] = pow2f(exponent(threadIdx.x) - 12);
+  const int e0 = exponent(g), e1 = exponent(g + 8);
+  for (int kt = blockIdx.y * EX_WARPS + warp; kt < w.ct; kt += gridDim.y * EX_WARPS) {
+    const int64_t at = (int64_t)mt * w.ct + kt;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int m = mt * TILE_ROWS + g + 8 * r, e = r ? e1 : e0;
+      if (m >= M) continue;
+      const uint4 v = __ldg(reinterpret_cast<const uint4*>(w.codes + at * TILE_BYTES) + 32 * r + lane);
+      const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int64_t k = (int64_t)kt * TILE_COLS + 32 * j + 8 * t;
+        if (k >= pitch) continue;
+        float s = __uint_as_float((uint32_t)__ldg(w.scales + at * (TILE_ROWS * w.per) + (g + 8 * r) * w.per + j * w.per / 4) << 16);
+        // 2^(12 - e) in two factors: it passes fp32's largest for subnormal rows
+        s = s * pow2f((12 - e) / 2) * pow2f((12 - e) - (12 - e) / 2);
+        uint32_t h[4];
+        code_pairs<__half>(word[j], h);
+        float c[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+          c[2 * i] = f.x * (s * Operand<__half>::BACK);
+          c[2 * i + 1] = f.y * (s * Operand<__half>::BACK);
+        }
+        store8(dst + (int64_t)m * pitch + k, c);
+      }
+    }
+  }
+}
+
+// Tokens as fp16 rows, a block each: fp16 as they are; bf16 times 2^(14 - e), 2^e <= the row's largest magnitude < 2^(e + 1).
+// A row with NaN or Inf: its scale is NaN, and so are its outputs.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) expand_tokens_kernel(const T* __restrict__ x, int K, int64_t ldx, __half* dst, int64_t pitch,
+                                                            float* scale) {
+  constexpr bool BF = std::is_same<T, __nv_bfloat16>::value;
+  __shared__ float red[8];
+  pdl_trigger();
+  pdl_wait();  // what reads these rows reads the weights' as well, and waits for this kernel only
+  const int p = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const T* row = x + p * ldx;
+  __half* to = dst + p * pitch;
+  float mul0 = 1.0f, mul1 = 1.0f;
+  if (BF) {
+    float mx = 0.0f;
+    if (VEC) {
+      for (int k = 8 * threadIdx.x; k < K; k += 2048) {
+        Raw8<T> v;
+        v.load(row + k);
+        float lo, hi;
+        v.extremes(lo, hi);
+        mx = max_nan(mx, max_nan(-lo, hi));
+      }
+    } else {
+      for (int k = threadIdx.x; k < K; k += 256) mx = max_nan(mx, fabsf(to_float(row[k])));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(FULL_MASK, mx, o));
+    if (lane == 0) red[warp] = mx;
+    __syncthreads();
+    mx = red[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) mx = max_nan(mx, red[i]);
+    int e = (int)(__float_as_uint(mx) >> 23 & 255u) - 127;
+    if (e < -126) e = -126;
+    const bool bad = nonfinite(mx);
+    if (threadIdx.x == 0) scale[p] = bad ? __uint_as_float(0x7fc00000u) : pow2f(e - 14);
+    mul0 = bad ? 0.0f : pow2f((14 - e) / 2);
+    mul1 = bad ? 0.0f : pow2f((14 - e) - (14 - e) / 2);
+    if (bad) {
+      for (int64_t k = threadIdx.x; k < pitch; k += 256) to[k] = __float2half_rn(0.0f);
+      return;
+    }
+  } else if (threadIdx.x == 0) {
+    scale[p] = 1.0f;
+  }
+  if (VEC) {
+    for (int k = 8 * threadIdx.x; k < pitch; k += 2048) {
+      Raw8<T> v;
+      v.zero();
+      if (k < K) v.load(row + k);
+      float f[8];
+      v.unpack(f);
+      if (BF) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = f[i] * mul0 * mul1;
+      }
+      store8(to + k, f);
+    }
+  } else {
+    for (int64_t k = threadIdx.x; k < pitch; k += 256) {
+      const float f = k < K ? to_float(row[k]) : 0.0f;
+      to[k] = __float2half_rn(BF ? f * mul0 * mul1 : f);
+    }
+  }
+}
+
+inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
+
+fgq_status launch_many(const void* x, int type, int P, int K, int64_t ldx, const fgq_w4* w, const float* bias, void* y,
+                       cudaStream_t s) {
+  const int M = w->rows;
+  const Matrix m = matrix(w);
+  const GemmPlan plan = plan_gemm_w8a8(P, K, M);
+  const size_t w_bytes = up256((size_t)M * plan.pitch * 2), x_bytes = up256((size_t)P * plan.pitch * 2);
+  const size_t ws_bytes = up256((size_t)M * 4), xs_bytes = up256((size_t)P * 4);
+  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(w_bytes + x_bytes + ws_bytes + xs_bytes + plan.part_bytes, s));
+  if (!tmp) return FGQ_ERR_CUDA;
+  __half* w16 = reinterpret_cast<__half*>(tmp);
+  __half* x16 = reinterpret_cast<__half*>(tmp + w_bytes);
+  float* wscale = reinterpret_cast<float*>(tmp + w_bytes + x_bytes);
+  float* xscale = reinterpret_cast<float*>(tmp + w_bytes + x_bytes + ws_bytes);
+  int parts = (m.ct + EX_WARPS - 1) / EX_WARPS;
+  while (parts > 1 && (int64_t)parts * m.rt > 4ll * device_sms()) parts = (parts + 1) / 2;
+  expand_weights_kernel<<<dim3(m.rt, parts), 32 * EX_WARPS, 0, s>>>(m, w16, plan.pitch, M, wscale);
+  fgq_status st = after_launch();
+  const bool vec = K % 8 == 0 && aligned(x, 16) && (P == 1 || stride16(ldx, type));
+  if (st == FGQ_OK) {
+    cudaError_t e;
+    if (type == FGQ_BF16) {
+      const __nv_bfloat16* xb = static_cast<const __nv_bfloat16*>(x);
+      e = vec ? launch_pdl(expand_tokens_kernel<__nv_bfloat16, true>, dim3(P), dim3(256), 0, s, xb, K, ldx, x16, plan.pitch, xscale)
+              : launch_pdl(expand_tokens_kernel<__nv_bfloat16, false>, dim3(P), dim3(256), 0, s, xb, K, ldx, x16, plan.pitch, xscale);
+    } else {
+      const __half* xh = static_cast<const __half*>(x);
+      e = vec ? launch_pdl(expand_tokens_kernel<__half, true>, dim3(P), dim3(256), 0, s, xh, K, ldx, x16, plan.pitch, xscale)
+              : launch_pdl(expand_tokens_kernel<__half, false>, dim3(P), dim3(256), 0, s, xh, K, ldx, x16, plan.pitch, xscale);
+    }
+    st = after_launch(e);
+  }
+  if (st == FGQ_OK)
+    st = launch_gemm_w8a8(plan, x16, w16, reinterpret_cast<float*>(tmp + w_bytes + x_bytes + ws_bytes + xs_bytes), xscale, P,
+                          wscale, M, bias, y, type, s);
+  if (cudaFreeAsync(tmp, s) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
+  return st;
+}
+
+// Outputs without features: the bias.
+__global__ void __launch_bounds__(256) bias_kernel(const float* bias, void* y, int ytype, int P, int M) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)P * M; i += (int64_t)gridDim.x * 256)
+    store_typed(y, ytype, i, bias ? __ldg(bias + i % M) : 0.0f);
+}
+
+// Tokens of 16 bits up to which the few-token kernel runs.
+constexpr int FEW_MAX_P = 64;
+
+bool overlap(const void* x, const void* y, int type, int P, int K, int M, int64_t ldx) {
+  const uintptr_t xb = reinterpret_cast<uintptr_t>(x), yb = reinterpret_cast<uintptr_t>(y);
+  const uint64_t xn = ((uint64_t)(P - 1) * (P > 1 ? ldx : 0) + K) * float_bytes(type), yn = (uint64_t)P * M * float_bytes(type);
+  return xb < yb + yn && yb < xb + xn;
+}
+
+}  // namespace
+
+fgq_status launch_copy_tokens(const void* x, int type, int P, int K, int64_t ldx, void* dst, cudaStream_t s) {
+  const int64_t pitch = copied_pitch(K);
+  uint16_t* d = static_cast<uint16_t*>(dst);
+  if (type == FGQ_F32)
+    copy_tokens_kernel<float><<<P, 256, 0, s>>>(static_cast<const float*>(x), P, K, ldx, d, pitch);
+  else
+    copy_tokens_kernel<__half><<<P, 256, 0, s>>>(static_cast<const __half*>(x), P, K, ldx, d, pitch);
+  return after_launch();
+}
+
+}  // namespace w4
+}  // namespace fgq
+
+using namespace fgq;
+
+extern "C" {
+
+size_t fgq_w4_code_bytes(int rows, int cols) {
+  if (rows < 0 || cols < 0) return 0;
+  return (size_t)w4::row_tiles(rows) * w4::col_tiles(cols) * w4::TILE_BYTES;
+}
+size_t fgq_w4_scale_bytes(int rows, int cols, int group) {
+  if (rows < 0 || cols < 0 || !w4::valid_group(group)) return 0;
+  return (size_t)w4::row_tiles(rows) * w4::col_tiles(cols) * w4::TILE_ROWS * (w4::TILE_COLS / group) * 2;
+}
+
+fgq_status fgq_quantize_weights_w4(const float* w, const fgq_w4* out, cudaStream_t stream) {
+  const fgq_status st = w4::check_weights(out);
+  if (st != FGQ_OK) return st;
+  const int64_t tiles = (int64_t)w4::row_tiles(out->rows) * w4::col_tiles(out->cols) * out->experts;
+  if (tiles == 0) return FGQ_OK;
+  if (!w) return FGQ_ERR_ARG;
+  if (!dec::aligned(w, 4)) return FGQ_ERR_ALIGN;
+  const int64_t blocks = (tiles + 7) / 8, most = 16ll * device_sms();
+  const w4::Matrix m = w4::matrix(out);
+  w4::quantize_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, stream>>>(
+      w, static_cast<uint8_t*>(const_cast<void*>(out->codes)), static_cast<uint16_t*>(const_cast<void*>(out->scales)), out->rows,
+      out->cols, m.rt, m.ct, m.per, tiles, device_error_word());
+  return after_launch();
+}
+
+fgq_status fgq_read_weights_w4(const fgq_w4* w, float* out, cudaStream_t stream) {
+  const fgq_status st = w4::check_weights(w);
+  if (st != FGQ_OK) return st;
+  const int64_t tiles = (int64_t)w4::row_tiles(w->rows) * w4::col_tiles(w->cols) * w->experts;
+  if (tiles == 0) return FGQ_OK;
+  if (!out) return FGQ_ERR_ARG;
+  if (!dec::aligned(out, 4)) return FGQ_ERR_ALIGN;
+  const int64_t blocks = (tiles + 7) / 8, most = 16ll * device_sms();
+  const w4::Matrix m = w4::matrix(w);
+  w4::read_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, stream>>>(m.codes, m.scales, out, w->rows, w->cols, m.rt,
+                                                                                m.ct, m.per, tiles);
+  return after_launch();
+}
+
+fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx, const fgq_w4* w, const float* bias, void* y,
+                         cudaStream_t stream) {
+  using namespace w4;
+  if (P < 0 || !valid_float(type)) return FGQ_ERR_ARG;
+  const fgq_status ok = check_weights(w);
+  if (ok != FGQ_OK) return ok;
+  if (w->experts != 1) return FGQ_ERR_ARG;
+  const int K = w->cols, M = w->rows;
+  if (P > 1 && ldx < K) return FGQ_ERR_ARG;
+  if (P == 0 || M == 0) return FGQ_OK;
+  if (P > MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
+  if (!y || (K > 0 && !x)) return FGQ_ERR_ARG;
+  const uintptr_t e = float_bytes(type);
+  if (!aligned(x, e) || !aligned(y, e) || !aligned(bias, 4)) return FGQ_ERR_ALIGN;
+  if (K == 0) {
+    const int64_t blocks = ((int64_t)P * M + 255) / 256, most = 8ll * device_sms();
+    bias_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, stream>>>(bias, y, type, P, M);
+    return after_launch();
+  }
+  if (type != FGQ_F32 && P > FEW_MAX_P) return launch_many(x, type, P, K, ldx, w, bias, y, stream);
+  FewArgs a = {matrix(w), {x, ldx, K}, bias, y, P, M, type, 1};
+  if (direct_tokens(x, type, P, K, ldx) && !overlap(x, y, type, P, K, M, ldx)) return launch_few(a, false, stream);
+  void* tmp = scratch_alloc(copied_bytes(type, P, K), stream);
+  if (!tmp) return FGQ_ERR_CUDA;
+  const int64_t pitch = copied_pitch(K);
+  a.x = {tmp, type == FGQ_F32 ? 3 * pitch : pitch, (int)pitch};
+  fgq_status st = launch_copy_tokens(x, type, P, K, ldx, tmp, stream);
+  if (st == FGQ_OK) st = launch_few(a, true, stream);
+  if (cudaFreeAsync(tmp, stream) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
+  return st;
+}
+
+}  // extern "C"

@@ -1,0 +1,232 @@
+// What the products on 4-bit weights share: the tile layout, codes as matrix operands, and the loop of one warp.
+#pragma once
+
+#include "decoder_internal.cuh"
+#include "kv_attention.cuh"  // cluster helpers
+#include "tc_common.cuh"
+
+namespace fgq {
+namespace w4 {
+
+using namespace dec;
+
+constexpr int TILE_ROWS = 16, TILE_COLS = 128, TILE_BYTES = TILE_ROWS * TILE_COLS / 2;
+
+inline int row_tiles(int rows) { return (int)(((int64_t)rows + TILE_ROWS - 1) / TILE_ROWS); }
+inline int col_tiles(int cols) { return (int)(((int64_t)cols + TILE_COLS - 1) / TILE_COLS); }
+inline bool valid_group(int g) { return g == 32 || g == 64 || g == 128; }
+
+// FGQ_OK, or what is wrong with weights.
+inline fgq_status check_weights(const fgq_w4* w) {
+  if (!w || w->experts < 0 || w->rows < 0 || w->cols < 0 || !valid_group(w->group)) return FGQ_ERR_ARG;
+  if (w->rows > MAX_SIZE || w->cols > MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
+  const int64_t tiles = (int64_t)row_tiles(w->rows) * col_tiles(w->cols);
+  if (tiles > INT32_MAX || tiles * w->experts > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
+  if (tiles * w->experts > 0) {
+    if (!w->codes || !w->scales) return FGQ_ERR_ARG;
+    if (!aligned(w->codes, 16) || !aligned(w->scales, 16)) return FGQ_ERR_ALIGN;
+  }
+  return FGQ_OK;
+}
+
+// One matrix as kernels take it; `per` groups a tile's row.
+struct Matrix {
+  const uint8_t* codes;
+  const uint16_t* scales;  // bf16
+  int rt, ct, per;
+};
+inline Matrix matrix(const fgq_w4* w) {
+  return {static_cast<const uint8_t*>(w->codes), static_cast<const uint16_t*>(w->scales), row_tiles(w->rows), col_tiles(w->cols),
+          TILE_COLS / w->group};
+}
+
+// Eight codes n of a word as four pairs of matrix operands (n - 8) UNIT: pair i holds values 2 i and 2 i + 1.  In the low
+// byte of a 16-bit float, n and 16 n are subnormals (or, in bf16, carry on past them in the same steps): one AND and one packed
+// multiply-add a pair make the centred code, exactly.
+template <typename T>
+struct Operand;
+template <>
+struct Operand<__half> {  // n 2^-24 2^15 - 8 2^-9
+  static constexpr uint32_t MUL_LO = 0x78007800u, MUL_HI = 0x68006800u, OFF = 0xa400a400u;
+  static constexpr float BACK = 512.0f;  // 1 / UNIT
+  static __device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+  }
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+template <>
+struct Operand<__nv_bfloat16> {  // n 2^-133 2^127 - 8 2^-6
+  static constexpr uint32_t MUL_LO = 0x7f007f00u, MUL_HI = 0x7d007d00u, OFF = 0xbe00be00u;
+  static constexpr float BACK = 64.0f;
+  static __device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+  }
+  static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  }
+};
+template <typename T>
+__device__ __forceinline__ void code_pairs(uint32_t w, uint32_t (&h)[4]) {
+  using O = Operand<T>;
+  const uint32_t v = w >> 8;
+  h[0] = O::fma2(w & 0x000f000fu, O::MUL_LO, O::OFF);
+  h[1] = O::fma2(w & 0x00f000f0u, O::MUL_HI, O::OFF);
+  h[2] = O::fma2(v & 0x000f000fu, O::MUL_LO, O::OFF);
+  h[3] = O::fma2(v & 0x00f000f0u, O::MUL_HI, O::OFF);
+}
+
+// Scales of one row of a tile, PER of them, as loaded.
+template <int PER>
+struct Scales;
+template <>
+struct Scales<4> {
+  uint2 v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = __ldg(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ float get(int i) const {
+    const uint32_t w = i < 2 ? v.x : v.y;
+    return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+  }
+};
+template <>
+struct Scales<2> {
+  uint32_t v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = __ldg(reinterpret_cast<const uint32_t*>(p)); }
+  __device__ __forceinline__ float get(int i) const { return __uint_as_float(i ? v & 0xffff0000u : v << 16); }
+};
+template <>
+struct Scales<1> {
+  uint16_t v;
+  __device__ __forceinline__ void load(const uint16_t* p) { v = __ldg(p); }
+  __device__ __forceinline__ float get(int) const { return __uint_as_float((uint32_t)v << 16); }
+};
+
+// What one thread holds of a tile: 16 bytes of rows g and g + 8, and their scales.
+template <int PER>
+struct Tile {
+  uint4 w[2];
+  Scales<PER> s[2];
+  // tile number `at` of the matrix; lane = 4 g + t
+  __device__ __forceinline__ void load(const uint8_t* codes, const uint16_t* scales, int64_t at, int lane) {
+    const uint4* p = reinterpret_cast<const uint4*>(codes + at * TILE_BYTES) + lane;
+    w[0] = __ldg(p);
+    w[1] = __ldg(p + 32);
+    const uint16_t* q = scales + at * (TILE_ROWS * PER) + (lane >> 2) * PER;
+    s[0].load(q);
+    s[1].load(q + 8 * PER);
+  }
+  __device__ __forceinline__ uint32_t word(int r, int j) const {
+    return j == 0 ? w[r].x : (j == 1 ? w[r].y : (j == 2 ? w[r].z : w[r].w));
+  }
+};
+
+// A warp's stage of tokens in shared memory: 8 NT columns of 128 values, 256 bytes each, 16-byte chunks of odd columns
+// moved by 64 bytes, so that eight lanes that read two columns meet all banks.
+__device__ __forceinline__ uint32_t chunk_at(int col, int chunk) { return (uint32_t)(col * 256 + ((chunk ^ ((col & 1) << 2)) << 4)); }
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Columns [128 kt, + 128) of the tokens into a stage; rows[c]: byte offset of column c's token row from `base`, or -1 (zeros).
+// Columns from kvalid (a multiple of 8) on are zeros.
+template <int NT>
+__device__ __forceinline__ void fetch_tokens(uint32_t stage, const uint8_t* base, const int64_t* rows, int kt, int kvalid, int lane) {
+  const int chunk = lane & 15, k = kt * TILE_COLS + 8 * chunk;
+#pragma unroll
+  for (int i = 0; i < 4 * NT; ++i) {
+    const int col = 2 * i + (lane >> 4);
+    const int64_t at = rows[col];
+    const bool live = at >= 0 && k < kvalid;
+    cp_async16(stage + chunk_at(col, chunk), live ? base + at + 2 * (int64_t)k : base, live);
+  }
+}
+
+// sum[mt][nt] += tile mt times the stage's columns; sums are in units of 1 / BACK.
+template <typename T, int MT, int NT, int PER>
+__device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint8_t* stage, float (&sum)[MT][NT][4], int lane) {
+  const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+  for (int gi = 0; gi < PER; ++gi) {
+    float acc[MT][NT][4];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[mt][nt][e] = 0.0f;
+#pragma unroll
+    for (int j = gi * (4 / PER); j < (gi + 1) * (4 / PER); ++j) {
+      uint4 b[NT];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) b[nt] = *reinterpret_cast<const uint4*>(stage + chunk_at(8 * nt + g, 4 * j + t));
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        uint32_t u[4], v[4];
+        code_pairs<T>(tile[mt].word(0, j), u);
+        code_pairs<T>(tile[mt].word(1, j), v);
+        const uint32_t a0[4] = {u[0], v[0], u[1], v[1]}, a1[4] = {u[2], v[2], u[3], v[3]};
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          Operand<T>::mma(acc[mt][nt], a0, b[nt].x, b[nt].y);
+          Operand<T>::mma(acc[mt][nt], a1, b[nt].z, b[nt].w);
+        }
+      }
+    }
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) {
+      const float s0 = tile[mt].s[0].get(gi), s1 = tile[mt].s[1].get(gi);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        sum[mt][nt][0] = fmaf(acc[mt][nt][0], s0, sum[mt][nt][0]);
+        sum[mt][nt][1] = fmaf(acc[mt][nt][1], s0, sum[mt][nt][1]);
+        sum[mt][nt][2] = fmaf(acc[mt][nt][2], s1, sum[mt][nt][2]);
+        sum[mt][nt][3] = fmaf(acc[mt][nt][3], s1, sum[mt][nt][3]);
+      }
+    }
+  }
+}
+
+// Tokens as operand rows: 16-bit elements, a token's `parts` rows beside one another (fp32: three bf16 parts that add up
+// to it exactly, in four columns of a product; 16-bit: themselves).
+struct TokenRows {
+  const void* data;
+  int64_t pitch;  // elements between tokens
+  int kvalid;     // elements of a row that hold values or zeros, a multiple of 8
+};
+__host__ __device__ constexpr int columns_per_token(int parts) { return parts == 3 ? 4 : parts; }
+
+// fp32 in parts of 8 significant bits, each cut off and the last exact.
+__device__ __forceinline__ void three_parts(float v, uint16_t (&p)[3]) {
+  const float a = __uint_as_float(__float_as_uint(v) & 0xffff0000u), r = v - a;
+  const float b = __uint_as_float(__float_as_uint(r) & 0xffff0000u), c = r - b;
+  p[0] = (uint16_t)(__float_as_uint(a) >> 16);
+  p[1] = (uint16_t)(__float_as_uint(b) >> 16);
+  p[2] = (uint16_t)(__float_as_uint(c) >> 16);
+}
+
+// Whether 16-bit tokens can be read in place: 16-byte pieces that end with the row.
+inline bool direct_tokens(const void* x, int type, int P, int K, int64_t ldx) {
+  return type != FGQ_F32 && K % 8 == 0 && aligned(x, 16) && (P == 1 || stride16(ldx, type));
+}
+inline int64_t copied_pitch(int K) { return ((int64_t)K + 7) / 8 * 8; }
+inline size_t copied_bytes(int type, int P, int K) { return (size_t)P * copied_pitch(K) * 2 * (type == FGQ_F32 ? 3 : 1); }
+// Tokens in operand rows at `dst` (copied_bytes of it).
+fgq_status launch_copy_tokens(const void* x, int type, int P, int K, int64_t ldx, void* dst, cudaStream_t s);
+
+}  // namespace w4
+}  // namespace fgq

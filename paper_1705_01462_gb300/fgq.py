@@ -30,6 +30,7 @@ _lib: Optional[ctypes.CDLL] = None
 # (name, restype, argtypes) of every exported symbol of include/fgq.h, fgq_decoder.h and fgq_debug.h
 _vp, _i, _i64, _u32, _u64, _f, _sz = (ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_uint32,
                                       ctypes.c_uint64, ctypes.c_float, ctypes.c_size_t)
+_d = ctypes.c_double
 SIGNATURES = [
     ("fgq_version", _i, []),
     ("fgq_status_string", ctypes.c_char_p, [_i]),
@@ -67,6 +68,17 @@ SIGNATURES = [
     ("fgq_quantize_tokens", _i, [_vp, _i, _i, _i, _i64, _vp, _vp, _vp]),
     ("fgq_gemm_w8a8", _i, [_vp, _vp, _i, _i, _vp, _vp, _i, _vp, _vp, _i, _vp]),
     ("fgq_linear_w8a8", _i, [_vp, _i, _i, _i, _i64, _vp, _vp, _i, _vp, _vp, _vp]),
+    ("fgq_rope_table", _i, [_i, _d, _i, _d, _d, _d, _d, _vp]),
+    ("fgq_rope", _i, [_vp, _vp, _i] + [_i] * 4 + [_i64] * 4 + [_i, _i, _vp, _f, _i, _vp, _vp, _vp]),
+    ("fgq_add_norm", _i, [_vp, _i, _i, _i, _i64, _vp, _vp, _i64, _i, _f, _vp, _i, _i64, _vp, _i64, _vp, _vp, _vp]),
+    ("fgq_w4_code_bytes", _sz, [_i, _i]),
+    ("fgq_w4_scale_bytes", _sz, [_i, _i, _i]),
+    ("fgq_quantize_weights_w4", _i, [_vp, _vp, _vp]),
+    ("fgq_read_weights_w4", _i, [_vp, _vp, _vp]),
+    ("fgq_linear_w4", _i, [_vp, _i, _i, _i64, _vp, _vp, _vp, _vp]),
+    ("fgq_route_tokens", _i, [_vp, _i, _i, _i, _i64, _vp, _i, _i, _i, _i, _i, _f, _vp, _vp, _vp]),
+    ("fgq_experts_w4", _i, [_vp, _i, _i, _i64, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp]),
+    ("fgq_moe_w4", _i, [_vp, _i, _i, _i64, _vp, _i, _i, _i, _i, _f, _vp, _vp, _vp, _vp, _vp]),
     ("fgq_stream_status", _i, [_vp]),
     ("fgq_set_path", _i, [_i]),
     ("fgq_last_path", _i, []),
@@ -713,6 +725,256 @@ def fgq_linear_w8a8(x: torch.Tensor, wq: torch.Tensor, wscale: torch.Tensor, bia
         raise ValueError(f"y must be {(P, wq.shape[0])}, got {tuple(y.shape)}")
     _check(lib().fgq_linear_w8a8(x.data_ptr(), ty, P, K, ldx, pw, ps, wq.shape[0], pb, _dev(y, x.dtype, "y"),
                                  _stream(stream)), "fgq_linear_w8a8")
+    return y
+
+
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "ramp": 3}
+NORM_KINDS = {"rms": 0, "layer": 1}
+SCORES = {"softmax": 0, "sigmoid": 1}
+
+
+def _named(table, name: str, what: str) -> int:
+    value = table.get(name)
+    if value is None:
+        raise ValueError(f"{what} must be one of {', '.join(table)}, got {name!r}")
+    return value
+
+
+def rope_table(rot: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, length: float = 0.0,
+               low: float = 1.0, high: float = 32.0, device="cuda") -> torch.Tensor:
+    """The angles of fgq_rope: turns a position of each of rot / 2 pairs, in units of 2^-64 (int64), scaled for long contexts
+    as include/fgq_decoder.h says ("linear", "base", "ramp": the last between low and high turns over `length` positions)."""
+    table = torch.empty(max(rot, 0) // 2, dtype=torch.int64)
+    _check(lib().fgq_rope_table(rot, base, _named(ROPE_SCALINGS, scaling, "scaling"), factor, length, low, high,
+                                table.data_ptr()), "fgq_rope_table")
+    return table.to(device)
+
+
+def fgq_rope(x: torch.Tensor, table: torch.Tensor, starts: torch.Tensor, lens: Optional[torch.Tensor] = None,
+             layout: str = "half", magnitude: float = 1.0, inverse: bool = False, out: Optional[torch.Tensor] = None,
+             stream=None) -> torch.Tensor:
+    """x [B][T][heads][D] with the first 2 len(table) values of each head turned by position starts[b] + i (tokens from lens[b]
+    on as they are); out may be x, whose other values then stay where they are."""
+    _require_cuda()
+    if not isinstance(x, torch.Tensor) or x.dim() != 4:
+        raise ValueError("x must be [B][T][heads][D]")
+    B, T, heads, D = x.shape
+    ty, xb, xt = _heads(x, heads, D, "x")
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        yb, yt = T * heads * D, heads * D
+    else:
+        if out.shape != x.shape or out.dtype != x.dtype:
+            raise ValueError(f"out must be {tuple(x.shape)} of {x.dtype}")
+        _, yb, yt = _heads(out, heads, D, "out")
+    pt = _dev(table, torch.int64, "table")
+    _check(lib().fgq_rope(x.data_ptr(), out.data_ptr(), ty, B, T, heads, D, xb, xt, yb, yt, 2 * table.numel(),
+                          _named(ROPE_LAYOUTS, layout, "layout"), pt, magnitude, int(inverse),
+                          _per_sequence(starts, B, "starts"), _per_sequence(lens, B, "lens"), _stream(stream)), "fgq_rope")
+    return out
+
+
+class _NormStruct(ctypes.Structure):
+    _fields_ = [("weight", _vp), ("bias", _vp), ("eps", _f), ("kind", _i)]
+
+
+class Norm:
+    """A norm of fgq_add_norm: kind "rms" or "layer", weight and bias fp32 [K] or None."""
+
+    __slots__ = ("weight", "bias", "eps", "kind", "_c", "_ref")
+
+    def __init__(self, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, kind: str = "rms",
+                 eps: float = 1e-6):
+        self.weight, self.bias, self.eps, self.kind = weight, bias, eps, kind
+        if weight is not None and bias is not None and weight.numel() != bias.numel():
+            raise ValueError("Norm: weight and bias differ in size")
+        self._c = _NormStruct(None if weight is None else _dev(weight, torch.float32, "weight"),
+                              None if bias is None else _dev(bias, torch.float32, "bias"), eps,
+                              _named(NORM_KINDS, kind, "kind"))
+        self._ref = ctypes.addressof(self._c)
+
+    def _of(self, K: int) -> int:
+        if (self.weight is not None and self.weight.numel() != K) or (self.bias is not None and self.bias.numel() != K):
+            raise ValueError(f"Norm: weight and bias must have {K} entries")
+        return self._ref
+
+
+def fgq_add_norm(x: torch.Tensor, residual: Optional[torch.Tensor] = None, norm: Optional[Norm] = None,
+                 post: Optional[Norm] = None, gate: Optional[torch.Tensor] = None, tokens_per_gate: int = 0,
+                 scale: float = 1.0, residual_out: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                 stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+    """(s, y): s = residual + scale gate post(x), y = norm(s) (None without norm).  x [P][K]; residual of x's type or fp32;
+    gate [rows][K] or [K], token p taking row p // tokens_per_gate (0: one row for all); residual_out may be residual."""
+    _require_cuda()
+    ty, ldx = _rows(x, "x")
+    P, K = x.shape
+    rty, ldr, rdtype = ty, 0, x.dtype
+    if residual is not None:
+        rty, ldr = _rows(residual, "residual")
+        rdtype = residual.dtype
+        if residual.shape != x.shape:
+            raise ValueError(f"residual must be {tuple(x.shape)}, got {tuple(residual.shape)}")
+    if residual_out is None:
+        residual_out = torch.empty((P, K), dtype=rdtype, device=x.device)
+        lds = K
+    else:
+        if residual is None:
+            rdtype = residual_out.dtype
+            rty = _float_type(residual_out, "residual_out")
+        if residual_out.shape != x.shape or residual_out.dtype != rdtype:
+            raise ValueError(f"residual_out must be {tuple(x.shape)} of {rdtype}")
+        lds = _rows(residual_out, "residual_out")[1]
+    pg, ldg = None, 0
+    if gate is not None:
+        g = gate if gate.dim() == 2 else gate.view(1, -1)
+        gty, ldg = _rows(g, "gate")
+        per = tokens_per_gate if tokens_per_gate > 0 else max(P, 1)
+        if gty != ty or g.shape[1] != K or g.shape[0] * per < P:
+            raise ValueError(f"gate must be {x.dtype} [rows][{K}], a row for each {per} of {P} tokens")
+        pg, tokens_per_gate = g.data_ptr(), per
+    py = None
+    if norm is not None:
+        if y is None:
+            y = torch.empty((P, K), dtype=x.dtype, device=x.device)
+        elif y.shape != x.shape:
+            raise ValueError(f"y must be {tuple(x.shape)}, got {tuple(y.shape)}")
+        py = _dev(y, x.dtype, "y")
+    elif y is not None:
+        raise ValueError("y without norm")
+    _check(lib().fgq_add_norm(x.data_ptr(), ty, P, K, ldx, None if post is None else post._of(K), pg, ldg, tokens_per_gate,
+                              scale, None if residual is None else residual.data_ptr(), rty, ldr, residual_out.data_ptr(), lds,
+                              None if norm is None else norm._of(K), py, _stream(stream)), "fgq_add_norm")
+    return residual_out, y
+
+
+class _W4Struct(ctypes.Structure):
+    _fields_ = [("codes", _vp), ("scales", _vp), ("experts", _i), ("rows", _i), ("cols", _i), ("group", _i)]
+
+
+class W4Weights:
+    """Weights [rows][cols], or [experts][rows][cols], in 4 bits with a bf16 scale for each group: codes uint8 [experts][row
+    tiles][column tiles][1024], scales bf16 [experts][row tiles][column tiles][16][128 / group] (include/fgq_decoder.h);
+    without the experts' axis: one matrix."""
+
+    __slots__ = ("codes", "scales", "experts", "rows", "cols", "group", "_c", "_ref")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
+        pc, ps = _dev(codes, torch.uint8, "codes"), _dev(scales, torch.bfloat16, "scales")
+        c, s = codes.shape, scales.shape
+        tiles = ((rows + 15) // 16, (cols + 127) // 128)
+        if len(c) not in (3, 4) or len(s) != len(c) + 1 or c[-1] != 1024 or c[:-1] != s[:-2] or c[-3:-1] != tiles or \
+                s[-2] != 16 or s[-1] not in (1, 2, 4):
+            raise ValueError(f"W4Weights: codes are [experts][{tiles[0]}][{tiles[1]}][1024], scales "
+                             f"[experts][{tiles[0]}][{tiles[1]}][16][128 / group]; got {tuple(c)} and {tuple(s)}")
+        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
+        self.experts, self.group = c[0] if len(c) == 4 else 1, 128 // s[-1]
+        self._c = _W4Struct(pc, ps, self.experts, rows, cols, self.group)
+        self._ref = ctypes.addressof(self._c)
+
+
+def fgq_quantize_weights_w4(w: torch.Tensor, group: int = 64, stream=None) -> W4Weights:
+    """w fp32 [rows][cols] or [experts][rows][cols] in 4 bits, a scale for each `group` columns of a row."""
+    _require_cuda()
+    if w.dim() not in (2, 3):
+        raise ValueError("w must be [rows][cols] or [experts][rows][cols]")
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    pw = _dev(w, torch.float32, "w")
+    rows, cols = w.shape[-2:]
+    tiles = tuple(w.shape[:-2]) + ((rows + 15) // 16, (cols + 127) // 128)
+    out = W4Weights(torch.empty(tiles + (1024,), dtype=torch.uint8, device=w.device),
+                    torch.empty(tiles + (16, 128 // group), dtype=torch.bfloat16, device=w.device), rows, cols)
+    _check(lib().fgq_quantize_weights_w4(pw, out._ref, _stream(stream)), "fgq_quantize_weights_w4")
+    return out
+
+
+def fgq_read_weights_w4(w: W4Weights, stream=None) -> torch.Tensor:
+    """What codes and scales stand for, fp32, in the shape that was quantized."""
+    _require_cuda()
+    shape = ((w.experts,) if w.codes.dim() == 4 else ()) + (w.rows, w.cols)
+    out = torch.empty(shape, dtype=torch.float32, device=w.codes.device)
+    _check(lib().fgq_read_weights_w4(w._ref, out.data_ptr(), _stream(stream)), "fgq_read_weights_w4")
+    return out
+
+
+def fgq_linear_w4(x: torch.Tensor, w: W4Weights, bias: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                  stream=None) -> torch.Tensor:
+    """A linear layer on 4-bit weights: x [P][cols] times w [rows][cols]^T plus bias, of x's type."""
+    _require_cuda()
+    ty, ldx = _rows(x, "x")
+    P, K = x.shape
+    if K != w.cols or (bias is not None and bias.numel() != w.rows):
+        raise ValueError(f"x must be [tokens][{w.cols}], bias [{w.rows}]")
+    if y is None:
+        y = torch.empty((P, w.rows), dtype=x.dtype, device=x.device)
+    elif tuple(y.shape) != (P, w.rows):
+        raise ValueError(f"y must be {(P, w.rows)}, got {tuple(y.shape)}")
+    _check(lib().fgq_linear_w4(x.data_ptr(), ty, P, ldx, w._ref, None if bias is None else _dev(bias, torch.float32, "bias"),
+                               _dev(y, x.dtype, "y"), _stream(stream)), "fgq_linear_w4")
+    return y
+
+
+def _router(router: torch.Tensor, x: torch.Tensor) -> Tuple[int, int]:
+    rty = _float_type(router, "router")
+    if router.dim() != 2 or router.shape[1] != x.shape[1] or not router.is_contiguous():
+        raise ValueError(f"router must be contiguous [experts][{x.shape[1]}]")
+    if router.dtype not in (x.dtype, torch.float32):
+        raise TypeError(f"router must be {x.dtype} or float32, got {router.dtype}")
+    return rty, router.data_ptr()
+
+
+def fgq_route_tokens(x: torch.Tensor, router: torch.Tensor, top: int, score: str = "softmax", renormalize: bool = True,
+                     scale: float = 1.0, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """(ids int32 [P][top], weights fp32 [P][top]): the experts with the largest logits router x, and their weights."""
+    _require_cuda()
+    ty, ldx = _rows(x, "x")
+    rty, pr = _router(router, x)
+    P, K = x.shape
+    ids = torch.empty((P, max(top, 0)), dtype=torch.int32, device=x.device)
+    weights = torch.empty((P, max(top, 0)), dtype=torch.float32, device=x.device)
+    _check(lib().fgq_route_tokens(x.data_ptr(), ty, P, K, ldx, pr, rty, router.shape[0], top, _named(SCORES, score, "score"),
+                                  int(renormalize), scale, ids.data_ptr(), weights.data_ptr(), _stream(stream)),
+           "fgq_route_tokens")
+    return ids, weights
+
+
+def _experts_out(x: torch.Tensor, y: Optional[torch.Tensor]) -> torch.Tensor:
+    if y is None:
+        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if y.shape != x.shape:
+        raise ValueError(f"y must be {tuple(x.shape)}, got {tuple(y.shape)}")
+    return y
+
+
+def fgq_experts_w4(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, gate: W4Weights, up: W4Weights, down: W4Weights,
+                   y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """sum_j weights[p][j] down_e (silu(gate_e x[p]) * (up_e x[p])), e = ids[p][j] (left out where it is no expert)."""
+    _require_cuda()
+    ty, ldx = _rows(x, "x")
+    P, K = x.shape
+    if K != gate.cols or ids.dim() != 2 or ids.shape[0] != P or weights.shape != ids.shape:
+        raise ValueError(f"x must be [tokens][{gate.cols}], ids and weights [{P}][top]")
+    y = _experts_out(x, y)
+    _check(lib().fgq_experts_w4(x.data_ptr(), ty, P, ldx, _dev(ids, torch.int32, "ids"), _dev(weights, torch.float32, "weights"),
+                                ids.shape[1], gate._ref, up._ref, down._ref, _dev(y, x.dtype, "y"), _stream(stream)),
+           "fgq_experts_w4")
+    return y
+
+
+def fgq_moe_w4(x: torch.Tensor, router: torch.Tensor, top: int, gate: W4Weights, up: W4Weights, down: W4Weights,
+               score: str = "softmax", renormalize: bool = True, scale: float = 1.0, y: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """A mixture-of-experts layer: fgq_route_tokens, then fgq_experts_w4."""
+    _require_cuda()
+    ty, ldx = _rows(x, "x")
+    rty, pr = _router(router, x)
+    P, K = x.shape
+    if K != gate.cols or router.shape[0] != gate.experts:
+        raise ValueError(f"x must be [tokens][{gate.cols}], router [{gate.experts}][{gate.cols}]")
+    y = _experts_out(x, y)
+    _check(lib().fgq_moe_w4(x.data_ptr(), ty, P, ldx, pr, rty, top, _named(SCORES, score, "score"), int(renormalize), scale,
+                            gate._ref, up._ref, down._ref, _dev(y, x.dtype, "y"), _stream(stream)), "fgq_moe_w4")
     return y
 
 

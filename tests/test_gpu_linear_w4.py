@@ -1,0 +1,177 @@
+"""Linear layers on 4-bit weights: the codes, what they stand for, and the products against their definitions in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import _layer as R
+from _gpu import dev
+from paper_1705_01462_gb300 import fgq
+
+pytestmark = pytest.mark.gpu
+
+# tokens from which 16-bit types may run on the product for many tokens: its bound is the wider one
+MANY = 33
+
+
+@pytest.mark.parametrize("G", [32, 64, 128])
+@pytest.mark.parametrize("shape", [(1, 1), (16, 128), (17, 129), (3, 40, 200), (2, 5, 31)])
+def test_quantize_and_read(G, shape):
+    rng = np.random.default_rng(G)
+    w = (rng.standard_normal(shape) * np.exp(rng.standard_normal(shape[:-1] + (1,)) * 3)).astype(np.float32)
+    w[..., 0, :] = 0
+    w[..., -1, -1] = 1e30
+    got = fgq.fgq_quantize_weights_w4(torch.from_numpy(w).to(dev()), G)
+    c, s = R.quantize_w4(w, G)
+    codes, sc = R.pack_w4(c, s, G)
+    assert np.array_equal(got.codes.cpu().numpy(), codes)
+    assert np.array_equal(got.scales.view(torch.int16).cpu().numpy().view(np.uint16), sc)
+    back = fgq.fgq_read_weights_w4(got)
+    assert np.array_equal(back.cpu().numpy(), R.dequantize_w4(c, s, G).astype(np.float32))
+    assert fgq.fgq_stream_status() == fgq.FGQ_OK
+
+
+def test_quantize_nonfinite_and_halves():
+    w = np.zeros((2, 128), np.float32)
+    w[0, :64] = np.arange(64) % 15 / 2.0  # halves: to even; the largest, 7, has code 7
+    w[0, 70], w[1, 3] = np.nan, -np.inf
+    w[1, 64:] = 3.5
+    got = fgq.fgq_quantize_weights_w4(torch.from_numpy(w).to(dev()), 64)
+    assert fgq.fgq_stream_status() == fgq.FGQ_ERR_NONFINITE
+    back = fgq.fgq_read_weights_w4(got).cpu().numpy()
+    assert np.array_equal(back[0, :64], np.rint(w[0, :64])) and not back[0, 64:].any() and not back[1, :64].any()
+    assert np.all(back[1, 64:] == 3.5)
+
+
+def run(rng, P, K, M, G, dtype, bias=True, ld=0, fill=0, spread=0.3, scale=1.0):
+    x, x64 = R.rng_tensor(rng, (P, K + ld), dtype, scale)
+    c, s = R.random_w4(rng, (M, K), G, spread)
+    w = R.weights(c, s, G, dev(), fill)
+    b = rng.standard_normal(M).astype(np.float32) if bias else None
+    y = fgq.fgq_linear_w4(x.to(dev())[:, :K], w, bias=None if b is None else torch.from_numpy(b).to(dev()))
+    assert fgq.fgq_stream_status() == fgq.FGQ_OK
+    want, bound = R.linear(x64[:, :K], R.dequantize_w4(c, s, G), G, None if b is None else b.astype(np.float64), dtype,
+                           many=dtype != "f32" and P >= MANY)
+    R.check(y.double().cpu().numpy(), want, bound, f"linear {P} x {K} -> {M}")
+    return y
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("G", [32, 64, 128])
+@pytest.mark.parametrize("P,K,M", [(1, 1, 1), (1, 128, 16), (1, 4096, 64), (2, 1000, 33), (3, 136, 40), (8, 1111, 999), (9, 512, 128),
+                                   (17, 257, 50), (31, 2048, 48), (33, 640, 100), (64, 384, 31), (65, 384, 300), (130, 1000, 257)])
+def test_products(dtype, G, P, K, M):
+    run(np.random.default_rng(P * K + M), P, K, M, G, dtype, bias=M % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("P", [1, 5, 20, 70])
+def test_strides_and_padding(dtype, P):
+    """Rows apart, off 16-byte boundaries; whatever codes stand past the matrix."""
+    rng = np.random.default_rng(P)
+    for ld in (8, 1, 5):
+        run(rng, P, 200, 40, 64, dtype, ld=ld, fill=5)
+    run(rng, P, 205, 40, 64, dtype, fill=-3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_accuracy(dtype):
+    """How far from 64 bits over many values: fp32 within 1e-6 of the output's norm, 16-bit types at their output's rounding.
+    (Each rounding is uniform within half a step of a value of random mantissa: 0.41 of the largest, root mean square.)"""
+    rng = np.random.default_rng(7)
+    for P in (4, 40, 100):
+        x, x64 = R.rng_tensor(rng, (P, 2048), dtype)
+        c, s = R.random_w4(rng, (512, 2048), 64)
+        y = fgq.fgq_linear_w4(x.to(dev()), R.weights(c, s, 64, dev())).double().cpu().numpy()
+        want = x64 @ R.dequantize_w4(c, s, 64).T
+        rel = np.linalg.norm(y - want) / np.linalg.norm(want)
+        assert rel <= {"f32": 1e-6, "bf16": 0.5 * 2.0 ** -8, "f16": 0.5 * 2.0 ** -11}[dtype], rel
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("P", [3, 90])
+def test_magnitudes(dtype, P):
+    """Scales that differ by 2^20 within a row, tokens far from 1."""
+    rng = np.random.default_rng(11)
+    run(rng, P, 512, 40, 32, dtype, spread=4.0, bias=False)
+    for scale in (1e-3, 1e3) + (() if dtype == "f16" else (1e-20, 1e20)):
+        run(rng, P, 512, 40, 32, dtype, scale=scale, bias=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("P", [6, 80])
+def test_nonfinite_tokens(dtype, P):
+    rng = np.random.default_rng(5)
+    x = R.rng_tensor(rng, (P, 300), dtype)[0].to(dev())
+    c, s = R.random_w4(rng, (70, 300), 64)
+    w = R.weights(c, s, 64, dev())
+    y0 = fgq.fgq_linear_w4(x, w)
+    x[1, 200], x[4, 0] = float("nan"), -float("inf")
+    y1 = fgq.fgq_linear_w4(x, w)
+    keep = [p for p in range(P) if p not in (1, 4)]
+    assert torch.equal(y0[keep], y1[keep])
+    assert not torch.isfinite(y1[[1, 4]]).any()
+    assert fgq.fgq_stream_status() == fgq.FGQ_OK
+
+
+def test_in_place_empty_streams_graphs():
+    rng = np.random.default_rng(6)
+    c, s = R.random_w4(rng, (256, 256), 64)
+    w = R.weights(c, s, 64, dev())
+    for dtype in ("f32", "bf16"):
+        for P in (1, 12, 100):
+            x = R.rng_tensor(rng, (P, 256), dtype)[0].to(dev())
+            y = fgq.fgq_linear_w4(x, w)
+            z = x.clone()
+            assert torch.equal(fgq.fgq_linear_w4(z, w, y=z), y)
+            side = torch.cuda.Stream()
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                z = fgq.fgq_linear_w4(x, w)
+            side.synchronize()
+            assert torch.equal(z, y)
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                z = fgq.fgq_linear_w4(x, w)
+            x.neg_()
+            graph.replay()
+            assert torch.equal(z, fgq.fgq_linear_w4(x, w)) and torch.equal(z, -y)
+    assert fgq.fgq_linear_w4(x[:0], w).shape == (0, 256)
+    c, s = np.zeros((20, 0), np.int8), np.zeros((20, 0), np.float32)
+    none = fgq.W4Weights(torch.zeros((2, 0, 1024), dtype=torch.uint8, device=dev()),
+                         torch.zeros((2, 0, 16, 2), dtype=torch.bfloat16, device=dev()), 20, 0)
+    b = torch.arange(20, dtype=torch.float32, device=dev())
+    assert torch.equal(fgq.fgq_linear_w4(torch.zeros((3, 0), device=dev()), none, bias=b), b.expand(3, 20))
+    assert not fgq.fgq_linear_w4(torch.zeros((3, 0), device=dev()), none).any()
+
+
+def test_no_scratch():
+    """Calls that need a temporary say so where there is none, and those that do not run."""
+    rng = np.random.default_rng(8)
+    c, s = R.random_w4(rng, (64, 256), 64)
+    w = R.weights(c, s, 64, dev())
+    prev = fgq.fgq_debug_set_scratch_limit(0)
+    try:
+        fgq.fgq_linear_w4(R.rng_tensor(rng, (4, 256), "bf16")[0].to(dev()), w)
+        for P, dtype in ((4, "f32"), (100, "bf16")):
+            with pytest.raises(fgq.FGQError) as e:
+                fgq.fgq_linear_w4(R.rng_tensor(rng, (P, 256), dtype)[0].to(dev()), w)
+            assert e.value.code == fgq.FGQ_ERR_CUDA
+    finally:
+        fgq.fgq_debug_set_scratch_limit(prev)
+
+
+def test_refusals():
+    w = fgq.fgq_quantize_weights_w4(torch.zeros((20, 150), device=dev()))
+    x = torch.zeros((2, 150), device=dev())
+    with pytest.raises(ValueError):
+        fgq.fgq_linear_w4(x[:, :149], w)
+    with pytest.raises(ValueError):
+        fgq.fgq_linear_w4(x, w, bias=torch.zeros(19, device=dev()))
+    with pytest.raises(ValueError):
+        fgq.W4Weights(w.codes, w.scales, 33, 150)
+    with pytest.raises(ValueError):
+        fgq.W4Weights(w.codes, w.scales[:, :, :8], 20, 150)
+    with pytest.raises(ValueError):
+        fgq.fgq_quantize_weights_w4(torch.zeros((20, 150), device=dev()), group=16)
+    with pytest.raises(fgq.FGQError):
+        fgq.fgq_linear_w4(x, fgq.fgq_quantize_weights_w4(torch.zeros((2, 20, 150), device=dev())))

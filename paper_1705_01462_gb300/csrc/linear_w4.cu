@@ -6,7 +6,7 @@
 #include <type_traits>
 
 #include "linear_internal.cuh"
-#include "w4.cuh"
+#include "w4_launch.h"
 
 namespace fgq {
 namespace w4 {
@@ -109,184 +109,34 @@ __global__ void __launch_bounds__(256) copy_tokens_kernel(const T* __restrict__ 
 }
 
 // ------------------------------------------------------------------ few tokens
-// A block takes 32 rows of weights, 8 NT columns of tokens and its share of K; its 8 warps take every eighth tile column,
-// weights from memory to registers two tiles ahead, tokens by copies of their own into shared memory as far ahead, so
-// that no barrier stands in the loop.  The warps' sums are joined in shared memory, and those of a cluster's blocks, which
-// split K where rows alone leave SMs idle, through it too, always in the same order.
-constexpr int WARPS = 8, MT = 2, ROWS = MT * TILE_ROWS, AHEAD = 2;
-
-struct FewArgs {
-  Matrix w;
-  TokenRows x;
-  const float* bias;
-  void* y;
-  int P, M, ytype, splits;
-};
-
-template <int NT>
-struct FewSmem {
-  static constexpr int STAGE = 8 * NT * 256, RING = WARPS * AHEAD * STAGE;
-  static constexpr int SUMS = WARPS * 8 * NT * (ROWS + 1) * 4;
-  static constexpr int BYTES = RING > SUMS ? RING : SUMS;
-};
-
-template <typename T, int NT, int PER, int PARTS>
-__global__ void __launch_bounds__(32 * WARPS) few_kernel(const __grid_constant__ FewArgs a) {
-  using S = FewSmem<NT>;
-  constexpr int CPT = columns_per_token(PARTS), TOKENS = 8 * NT / CPT;
-  extern __shared__ __align__(16) uint8_t w4_smem[];
-  __shared__ int64_t rows[8 * NT];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int sp = blockIdx.x % a.splits, mt0 = blockIdx.x / a.splits * MT, p0 = blockIdx.y * TOKENS;
-  const int np = min(TOKENS, a.P - p0);
-  if (threadIdx.x < 8 * NT) {
-    const int tok = threadIdx.x / CPT, part = threadIdx.x % CPT;
-    rows[threadIdx.x] = tok < np && part < PARTS ? 2 * ((p0 + tok) * a.x.pitch + part * (a.x.pitch / PARTS)) : -1;
-  }
-  const int c0 = (int)((int64_t)a.w.ct * sp / a.splits), c1 = (int)((int64_t)a.w.ct * (sp + 1) / a.splits);
-  const uint8_t* xb = static_cast<const uint8_t*>(a.x.data);
-  uint8_t* ring = w4_smem + warp * AHEAD * S::STAGE;
-  const uint32_t ring_at = smem_u32(ring);
-  Tile<PER> tile[AHEAD][MT];
-  auto weights = [&](int i, int kt) {
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)  // a row tile past the last is read as the last
-      tile[i][mt].load(a.w.codes, a.w.scales, (int64_t)min(mt0 + mt, a.w.rt - 1) * a.w.ct + kt, lane);
-  };
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i)
-    if (c0 + warp + i * WARPS < c1) weights(i, c0 + warp + i * WARPS);
-  __syncthreads();  // rows
-  pdl_wait();
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) {
-    const int kt = c0 + warp + i * WARPS;
-    if (kt < c1) fetch_tokens<NT>(ring_at + i * S::STAGE, xb, rows, kt, a.x.kvalid, lane);
-    cp_async_commit();
-  }
-  float sum[MT][NT][4];
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[mt][nt][e] = 0.0f;
-  for (int kt = c0 + warp; kt < c1; kt += AHEAD * WARPS) {
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int at = kt + i * WARPS, next = at + AHEAD * WARPS;
-      if (at >= c1) break;  // the same for the whole warp
-      cp_async_wait<AHEAD - 1>();
-      __syncwarp();
-      multiply<T, MT, NT, PER>(tile[i], ring + i * S::STAGE, sum, lane);
-      __syncwarp();
-      if (next < c1) {
-        weights(i, next);
-        fetch_tokens<NT>(ring_at + i * S::STAGE, xb, rows, next, a.x.kvalid, lane);
-      }
-      cp_async_commit();
+fgq_status launch_few(RowsArgs a, bool early, cudaStream_t s) {
+  const int cpt = a.ytype == FGQ_F32 ? columns_per_token(3) : 1;
+  const int64_t columns = (int64_t)a.P * cpt;
+  const int nt = columns <= 8 ? 1 : (columns <= 16 ? 2 : (columns <= 32 ? 4 : 8));
+  const int tokens = 8 * nt / cpt;
+  const int64_t tiles = ((int64_t)a.P + tokens - 1) / tokens;
+  if (nt <= 2) {  // one tile of tokens: held in shared memory where it fits
+    const int mt = nt == 1 && a.w.rt >= 40 * device_sms() ? 2 : 1;
+    const ResidentPlan plan = plan_held(nt, mt, a.w.ct, a.w.per);
+    if (plan.warps > 0) {
+      ResidentArgs r = {};
+      r.w = a.w, r.x = a.x, r.bias = a.bias, r.y = a.y, r.P = a.P, r.M = a.M, r.ytype = a.ytype, r.early = early;
+      r.items = (a.w.rt + mt - 1) / mt;
+      if (a.ytype == FGQ_F32) return launch_held_f32(r, nt, mt, plan, early, s);
+      return a.ytype == FGQ_BF16 ? launch_held_bf16(r, nt, mt, plan, early, s) : launch_held_f16(r, nt, mt, plan, early, s);
     }
   }
-  cp_async_wait<0>();
-  __syncthreads();  // the rings are read
-  float* sums = reinterpret_cast<float*>(w4_smem);  // [warp][column][ROWS + 1]
-  const int g = lane >> 2, t = lane & 3;
-#pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        sums[(warp * 8 * NT + 8 * nt + 2 * t + (e & 1)) * (ROWS + 1) + 16 * mt + g + 8 * (e >> 1)] = sum[mt][nt][e];
-  __syncthreads();
-  auto put = [&](int i, float v) {  // sum i = token * 32 + row
-    const int m = mt0 * TILE_ROWS + i % ROWS, p = p0 + i / ROWS;
-    if (m < a.M && p < a.P)
-      store_typed(a.y, a.ytype, (int64_t)p * a.M + m, fmaf(v, Operand<T>::BACK, a.bias ? __ldg(a.bias + m) : 0.0f));
-  };
-  for (int i = threadIdx.x; i < np * ROWS; i += 32 * WARPS) {
-    float* at = sums + i / ROWS * CPT * (ROWS + 1) + i % ROWS;
-    float v = 0.0f;
-#pragma unroll
-    for (int k = 0; k < WARPS; ++k)
-#pragma unroll
-      for (int part = 0; part < PARTS; ++part) v += at[(k * 8 * NT + part) * (ROWS + 1)];
-    if (a.splits == 1)
-      put(i, v);
-    else
-      *at = v;  // the first warp's place: no other thread reads it in this loop
-  }
-  if (a.splits > 1) {
-    cluster_sync();
-    for (int i = threadIdx.x + 32 * WARPS * sp; i < np * ROWS; i += 32 * WARPS * a.splits) {
-      float v = 0.0f;
-      for (int k = 0; k < a.splits; ++k) v += ld_cluster(sums + i / ROWS * CPT * (ROWS + 1) + i % ROWS, k);
-      put(i, v);
-    }
-    cluster_sync();  // no block leaves while another may read its sums
-  }
-}
-
-template <typename T, int NT, int PER, int PARTS>
-fgq_status launch_few_kernel(const FewArgs& a, bool early, cudaStream_t s) {
-  constexpr int TOKENS = 8 * NT / columns_per_token(PARTS);
-  if (!tc::smem_attr_once<few_kernel<T, NT, PER, PARTS>>(FewSmem<NT>::BYTES)) return FGQ_ERR_CUDA;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((a.w.rt + MT - 1) / MT * a.splits), (unsigned)((a.P + TOKENS - 1) / TOKENS));
-  cfg.blockDim = dim3(32 * WARPS);
-  cfg.dynamicSmemBytes = FewSmem<NT>::BYTES;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  unsigned n = 0;
-  if (early) {
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
-  if (a.splits > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = (unsigned)a.splits;
-    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
-    ++n;
-  }
-  cfg.attrs = attr;
-  cfg.numAttrs = n;
-  return after_launch(cudaLaunchKernelEx(&cfg, few_kernel<T, NT, PER, PARTS>, a));
-}
-
-template <typename T, int NT, int PARTS>
-fgq_status launch_few_per(const FewArgs& a, bool early, cudaStream_t s) {
-  if (a.w.per == 4) return launch_few_kernel<T, NT, 4, PARTS>(a, early, s);
-  if (a.w.per == 2) return launch_few_kernel<T, NT, 2, PARTS>(a, early, s);
-  return launch_few_kernel<T, NT, 1, PARTS>(a, early, s);
-}
-
-template <typename T, int PARTS>
-fgq_status launch_few_nt(FewArgs a, bool early, cudaStream_t s) {
-  const int64_t columns = (int64_t)a.P * columns_per_token(PARTS);
-  const int nt = columns <= 8 ? 1 : (columns <= 16 ? 2 : 4);
-  const int tokens = 8 * nt / columns_per_token(PARTS);
-  // blocks that share a K: up to two an SM, each with a tile for each warp
-  const int64_t blocks = (int64_t)((a.w.rt + MT - 1) / MT) * ((a.P + tokens - 1) / tokens);
-  a.splits = 1;
-  while (a.splits < 8 && blocks * a.splits * 2 <= 2 * device_sms() && a.w.ct >= 2 * WARPS * a.splits) a.splits *= 2;
-  // more tokens than a grid has rows of blocks for
-  const int most = 65535 * tokens;
-  for (; a.P > most; a.P -= most) {
-    FewArgs part = a;
-    part.P = most;
-    const fgq_status st = launch_few_per<T, 4, PARTS>(part, early, s);
-    if (st != FGQ_OK) return st;
-    a.x.data = static_cast<const uint16_t*>(a.x.data) + most * a.x.pitch;
-    a.y = static_cast<uint8_t*>(a.y) + (int64_t)most * a.M * float_bytes(a.ytype);
-    early = false;
-  }
-  return nt == 1 ? launch_few_per<T, 1, PARTS>(a, early, s)
-                 : nt == 2 ? launch_few_per<T, 2, PARTS>(a, early, s) : launch_few_per<T, 4, PARTS>(a, early, s);
-}
-
-fgq_status launch_few(const FewArgs& a, bool early, cudaStream_t s) {
-  if (a.ytype == FGQ_F32) return launch_few_nt<__nv_bfloat16, 3>(a, early, s);
-  return a.ytype == FGQ_BF16 ? launch_few_nt<__nv_bfloat16, 1>(a, early, s) : launch_few_nt<__half, 1>(a, early, s);
+  // two row tiles a warp where that leaves two blocks an SM
+  const int mt = nt <= 2 && (a.w.rt + 2 * WARPS - 1) / (2 * WARPS) * tiles >= 2 * device_sms() ? 2 : 1;
+  const int64_t items = (int64_t)((a.w.rt + WARPS * mt - 1) / (WARPS * mt)) * tiles;
+  if (items > INT32_MAX / 8) return FGQ_ERR_UNSUPPORTED;
+  const RowsPlan plan = plan_rows(items, a.w.ct);
+  a.items = (int)items;
+  a.token_tiles = (int)tiles;
+  a.splits = plan.splits;
+  a.early = early;
+  if (a.ytype == FGQ_F32) return launch_rows_f32(a, nt, mt, plan.grid, early, s);
+  return a.ytype == FGQ_BF16 ? launch_rows_bf16(a, nt, mt, plan.grid, early, s) : launch_rows_f16(a, nt, mt, plan.grid, early, s);
 }
 
 // ------------------------------------------------------------------ operands of the product for many tokens
@@ -541,7 +391,8 @@ fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx,
     return after_launch();
   }
   if (type != FGQ_F32 && P > FEW_MAX_P) return launch_many(x, type, P, K, ldx, w, bias, y, stream);
-  FewArgs a = {matrix(w), {x, ldx, K}, bias, y, P, M, type, 1};
+  RowsArgs a = {};
+  a.w = matrix(w), a.x = {x, P > 1 ? ldx : 0, K}, a.bias = bias, a.y = y, a.P = P, a.M = M, a.ytype = type;
   if (direct_tokens(x, type, P, K, ldx) && !overlap(x, y, type, P, K, M, ldx)) return launch_few(a, false, stream);
   void* tmp = scratch_alloc(copied_bytes(type, P, K), stream);
   if (!tmp) return FGQ_ERR_CUDA;

@@ -6,15 +6,14 @@
 //   logits_kernel   four warps an expert, four tokens: products of 8 elements in fp32, their sums as pairs of fp32 (two-sum), so that a
 //                   logit is off by about one fp32 rounding and the choice is that of 64-bit sums but for near ties;
 //   select_kernel   a warp a token: the largest one by one, then the weights;
-//   group_kernel    one block: choices sorted by expert, and cut into units of up to CAP tokens that share an expert;
-//   hidden_kernel   a block 16 rows of gate and the same 16 of up, for one unit: silu(gate) up, left as bf16 parts;
-//   down_kernel     a block 16 rows of down, for all units: sums stay with the block, so nothing is added up across blocks
-//                   and no order depends on which comes first.
-// Bound by the bytes of the experts' weights, each read once (again from L2 where more than CAP tokens share an expert).
+//   group_kernel    one block: choices sorted by expert, and cut into units of up to 8 to 32 tokens that share an expert;
+//   rows_kernel     (w4_rows.cuh) 128 rows of gate and the same of up, for one unit: silu(gate) up, left as bf16 parts;
+//   down_kernel     128 rows of down, for all units: sums stay with the block, or its cluster, so that no order depends on which
+//                   comes first.
+// Bound by the bytes of the experts' weights, each read once (again from L2 for each further unit of an expert).
 #include <type_traits>
 
-#include "linear_internal.cuh"
-#include "w4.cuh"
+#include "w4_launch.h"
 
 namespace fgq {
 namespace w4 {
@@ -102,18 +101,14 @@ __global__ void __launch_bounds__(32 * LG_WARPS) logits_kernel(const __grid_cons
   }
 }
 
-// A unit of work: up to CAP choices of one expert, `count` of them from `start` on in the sorted order.
-struct Unit {
-  int expert, start, count, pad;
-};
-
 struct SelectArgs {
   const double* logits;
   int32_t* ids;
   float* weights;
   // P == 1: what group_kernel would find
   Unit* units;
-  int32_t* order;
+  Choice* choices;
+  int32_t* places;
   int* nunits;
   int P, E, top, score, renormalize;
   float scale;
@@ -200,7 +195,8 @@ __global__ void __launch_bounds__(128) select_kernel(const __grid_constant__ Sel
     a.weights[(int64_t)p * a.top + lane] = w;
     if (a.units) {
       a.units[rank] = {mine_id, rank, 1, 0};
-      a.order[rank] = lane;
+      a.choices[rank] = {0, w};
+      a.places[lane] = rank;
     }
   }
   if (a.units && lane == 0) *a.nunits = a.top;
@@ -231,8 +227,8 @@ __device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
   return before + s - v;
 }
 
-__global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, int A, int E, int cap, Unit* units, int32_t* order,
-                                                           int* nunits) {
+__global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, const float* weights, int A, int top, int E, int cap,
+                                                           Unit* units, Choice* choices, int32_t* places, int* nunits) {
   __shared__ int count[MAX_EXPERTS], start[MAX_EXPERTS], id[CHUNK * MAX_TOP], warp_sums[GR_THREADS / 32];
   pdl_trigger();
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -242,7 +238,10 @@ __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, i
   for (int i = t; i < A; i += GR_THREADS) {
     const int e = __ldcg(ids + i);
     id[i] = e;
-    if (e >= 0 && e < E) atomicAdd(&count[e], 1);
+    if (e >= 0 && e < E)
+      atomicAdd(&count[e], 1);
+    else
+      places[i] = -1;
   }
   __syncthreads();
   const int n = count[t];  // 0 from E on
@@ -259,152 +258,15 @@ __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, i
     for (int i = 0; found < want; i += 32) {
       const bool hit = i + lane < A && id[i + lane] == e;
       const unsigned m = __ballot_sync(FULL_MASK, hit);
-      if (hit) order[at + __popc(m & ((1u << lane) - 1u))] = i + lane;
+      if (hit) {
+        const int place = at + __popc(m & ((1u << lane) - 1u));
+        choices[place] = {(i + lane) / top, __ldcg(weights + i + lane)};
+        places[i + lane] = place;
+      }
       at += __popc(m);
       found += __popc(m);
     }
   }
-}
-
-// ------------------------------------------------------------------ silu(gate x) * (up x)
-constexpr int WARPS = 8, AHEAD = 2;
-
-struct HiddenArgs {
-  Matrix gate, up;
-  TokenRows x;
-  const Unit* units;
-  const int32_t* order;
-  const int* nunits;
-  uint16_t* h;  // [choice][parts][hpitch], in sorted order
-  int64_t hpitch;
-  int F, top, splits;
-};
-
-// v as PARTS bf16 values that add up to it: all of it in three, within 2^-17 in two.
-template <int PARTS>
-__device__ __forceinline__ void hidden_parts(float v, uint16_t (&p)[3]) {
-  if constexpr (PARTS == 3) {
-    three_parts(v, p);
-  } else {
-    const float a = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-    const __nv_bfloat16 b = __float2bfloat16_rn(v - a);
-    p[0] = (uint16_t)(__float_as_uint(a) >> 16);
-    p[1] = *reinterpret_cast<const uint16_t*>(&b);
-  }
-}
-
-template <typename T, int NT, int PER, int PARTS, int HPARTS>
-__global__ void __launch_bounds__(32 * WARPS) hidden_kernel(const __grid_constant__ HiddenArgs a) {
-  constexpr int STAGE = 8 * NT * 256, CPT = columns_per_token(PARTS);
-  extern __shared__ __align__(16) uint8_t w4_smem[];
-  __shared__ int64_t rows[8 * NT];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int sp = blockIdx.x % a.splits, item = blockIdx.x / a.splits;
-  const int unit = item / a.gate.rt, mt = item - unit * a.gate.rt;
-  pdl_wait();
-  pdl_trigger();  // from here on the kernel after may read the units
-  if (unit >= __ldcg(a.nunits)) return;
-  const int4 u = __ldcg(reinterpret_cast<const int4*>(a.units) + unit);  // expert, start, count
-  const int c0 = (int)((int64_t)a.gate.ct * sp / a.splits), c1 = (int)((int64_t)a.gate.ct * (sp + 1) / a.splits);
-  const int64_t first = ((int64_t)u.x * a.gate.rt + mt) * a.gate.ct;
-  Tile<PER> tile[AHEAD][2];
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) {
-    const int kt = c0 + warp + i * WARPS;
-    if (kt < c1) {
-      tile[i][0].load(a.gate.codes, a.gate.scales, first + kt, lane);
-      tile[i][1].load(a.up.codes, a.up.scales, first + kt, lane);
-    }
-  }
-  if (threadIdx.x < 8 * NT) {
-    const int tok = threadIdx.x / CPT, part = threadIdx.x % CPT;
-    rows[threadIdx.x] = tok < u.z && part < PARTS
-                            ? 2 * ((int64_t)(__ldcg(a.order + u.y + tok) / a.top) * a.x.pitch + part * (a.x.pitch / PARTS)) : -1;
-  }
-  __syncthreads();
-  const uint8_t* xb = static_cast<const uint8_t*>(a.x.data);
-  uint8_t* ring = w4_smem + warp * AHEAD * STAGE;
-  const uint32_t ring_at = smem_u32(ring);
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) {
-    const int kt = c0 + warp + i * WARPS;
-    if (kt < c1) fetch_tokens<NT>(ring_at + i * STAGE, xb, rows, kt, a.x.kvalid, lane);
-    cp_async_commit();
-  }
-  float sum[2][NT][4];
-#pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[m][nt][e] = 0.0f;
-  for (int kt = c0 + warp; kt < c1; kt += AHEAD * WARPS) {
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int at = kt + i * WARPS, next = at + AHEAD * WARPS;
-      if (at >= c1) break;  // the same for the whole warp
-      cp_async_wait<AHEAD - 1>();
-      __syncwarp();
-      multiply<T, 2, NT, PER>(tile[i], ring + i * STAGE, sum, lane);
-      __syncwarp();
-      if (next < c1) {
-        tile[i][0].load(a.gate.codes, a.gate.scales, first + next, lane);
-        tile[i][1].load(a.up.codes, a.up.scales, first + next, lane);
-        fetch_tokens<NT>(ring_at + i * STAGE, xb, rows, next, a.x.kvalid, lane);
-      }
-      cp_async_commit();
-    }
-  }
-  cp_async_wait<0>();
-  __syncthreads();
-  constexpr int LD = 33;
-  float* sums = reinterpret_cast<float*>(w4_smem);  // [warp][column][gate rows, up rows]
-  const int g = lane >> 2, t = lane & 3;
-#pragma unroll
-  for (int m = 0; m < 2; ++m)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        sums[(warp * 8 * NT + 8 * nt + 2 * t + (e & 1)) * LD + 16 * m + g + 8 * (e >> 1)] = sum[m][nt][e];
-  __syncthreads();
-  // each value's sum over warps and parts, to the first warp's place
-  for (int i = threadIdx.x; i < u.z * 32; i += 32 * WARPS) {
-    float* at = sums + i / 32 * CPT * LD + i % 32;
-    float v = 0.0f;
-#pragma unroll
-    for (int k = 0; k < WARPS; ++k)
-#pragma unroll
-      for (int part = 0; part < PARTS; ++part) v += at[(k * 8 * NT + part) * LD];
-    *at = v;
-  }
-  if (a.splits > 1)
-    cluster_sync();
-  else
-    __syncthreads();
-  for (int i = threadIdx.x + 32 * WARPS * sp; i < u.z * 16; i += 32 * WARPS * a.splits) {
-    const int tok = i / 16, f = i % 16;
-    const float* at = sums + tok * CPT * LD + f;
-    float gv = 0.0f, uv = 0.0f;
-    if (a.splits == 1) {
-      gv = at[0], uv = at[16];
-    } else {
-      for (int k = 0; k < a.splits; ++k) {
-        gv += ld_cluster(at, k);
-        uv += ld_cluster(at + 16, k);
-      }
-    }
-    gv *= Operand<T>::BACK;
-    uv *= Operand<T>::BACK;
-    const int col = mt * TILE_ROWS + f;
-    const float v = col < a.F ? gv / (1.0f + expf(-gv)) * uv : 0.0f;
-    uint16_t p[3];
-    hidden_parts<HPARTS>(v, p);
-    uint16_t* to = a.h + (int64_t)(u.y + tok) * HPARTS * a.hpitch + col;
-#pragma unroll
-    for (int part = 0; part < HPARTS; ++part) to[part * a.hpitch] = p[part];
-  }
-  if (a.splits > 1) cluster_sync();  // no block leaves while another may read its sums
 }
 
 // ------------------------------------------------------------------ down
@@ -413,83 +275,99 @@ struct DownArgs {
   const uint16_t* h;
   int64_t hpitch;
   const Unit* units;
-  const int32_t* order;
+  const Choice* choices;
   const int* nunits;
-  const float* weights;
   void* y;
-  int P, K, ytype, top, splits;
+  int P, K, ytype, splits;
 };
 
-// The block's warps share the pairs (unit, tile column) in runs of equal length; at a unit's end (or its share of it) a warp adds
-// what it has, by the router's weights, to sums of its own for each token and row.
-template <int NT, int PER, int HPARTS>
-__global__ void __launch_bounds__(32 * WARPS) down_kernel(const __grid_constant__ DownArgs a) {
+constexpr int DOWN_ROWS = WARPS * TILE_ROWS;
+constexpr int DOWN_LD = DOWN_ROWS + 8;  // eight lanes that hold two tokens' rows meet different banks
+
+// A block takes 128 rows of down, 16 a warp, and all pairs (unit, tile column), or a cluster's block its share of them.  At a unit's end (or
+// its share's) each warp adds what it has, by the router's weights, to sums of its rows for every token.
+template <int NT, int PER, int HPARTS, int AHEAD>
+__global__ void __launch_bounds__(THREADS) down_kernel(const __grid_constant__ DownArgs a) {
   using T = __nv_bfloat16;
-  constexpr int STAGE = 8 * NT * 256, CPT = columns_per_token(HPARTS);
+  using R = Ring<NT>;
+  constexpr int CPT = columns_per_token(HPARTS);
   extern __shared__ __align__(16) uint8_t w4_smem[];
+  float* part = reinterpret_cast<float*>(w4_smem + R::TOTAL);  // [token][DOWN_LD]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int sp = blockIdx.x % a.splits, mt = blockIdx.x / a.splits;
-  constexpr int LD = TILE_ROWS + 1;
-  float* part = reinterpret_cast<float*>(w4_smem + WARPS * AHEAD * STAGE);  // [warp][token][LD]
-  float* own = part + warp * a.P * LD;
-  uint8_t* ring = w4_smem + warp * AHEAD * STAGE;
-  const uint32_t ring_at = smem_u32(ring);
-  for (int i = lane; i < a.P * LD; i += 32) own[i] = 0.0f;
-  __syncwarp();
-  // units, the choices' order and their weights are those of kernels before the one that this one waits for
+  const int sp = blockIdx.x % a.splits, rt = blockIdx.x / a.splits * WARPS + warp;
+  const int mt = min(rt, a.down.rt - 1);  // a row tile past the last is read as the last
+  for (int i = threadIdx.x; i < a.P * DOWN_LD; i += THREADS) part[i] = 0.0f;
+  // units and choices are those of kernels before the one that this one waits for
   const int ct = a.down.ct;
-  const int64_t n = (int64_t)__ldcg(a.nunits) * ct;
-  const int share = sp * WARPS + warp, shares = a.splits * WARPS;
-  const int64_t q0 = n * share / shares, q1 = n * (share + 1) / shares;
+  const int64_t all = (int64_t)__ldcg(a.nunits) * ct;
+  const int64_t q0 = all * sp / a.splits, n = all * (sp + 1) / a.splits - q0;
+  // a place in the sequence of stages; the unit after it is asked for a unit ahead
   struct Place {
     int unit, kt;
-    int4 u;
+    int4 u, after;
   };
-  auto place = [&](int64_t q) {
-    Place c;
-    c.unit = (int)(q / ct);
-    c.kt = (int)(q - (int64_t)c.unit * ct);
-    c.u = q < q1 ? __ldcg(reinterpret_cast<const int4*>(a.units) + c.unit) : make_int4(0, 0, 0, 0);
-    return c;
-  };
-  auto advance = [&](Place& c, bool more) {
+  const int units = (int)(all / ct);
+  auto unit_at = [&](int i) { return i < units ? __ldcg(reinterpret_cast<const int4*>(a.units) + i) : make_int4(0, 0, 0, 0); };
+  auto advance = [&](Place& c) {
     if (++c.kt == ct) {
       c.kt = 0;
       ++c.unit;
-      if (more) c.u = __ldcg(reinterpret_cast<const int4*>(a.units) + c.unit);
+      c.u = c.after;
+      c.after = unit_at(c.unit + 1);
+      return true;
     }
+    return false;
   };
+  Place wp;
+  wp.unit = (int)(q0 / ct);
+  wp.kt = (int)(q0 - (int64_t)wp.unit * ct);
+  wp.u = unit_at(wp.unit);
+  wp.after = unit_at(wp.unit + 1);
+  Place xp = wp, now = wp;
   Tile<PER> tile[AHEAD][1];
-  auto weights = [&](int i, const Place& c) {
-    tile[i][0].load(a.down.codes, a.down.scales, ((int64_t)c.u.x * a.down.rt + mt) * ct + c.kt, lane);
+  auto next_weights = [&](int slot) {
+    tile[slot][0].load(a.down.codes, a.down.scales, ((int64_t)wp.u.x * a.down.rt + mt) * ct + wp.kt, lane);
+    advance(wp);
   };
-  auto hidden = [&](int i, const Place& c) {
-    const int chunk = lane & 15, k = c.kt * TILE_COLS + 8 * chunk;
+  Columns<NT> cols;
+  auto columns = [&]() {
 #pragma unroll
-    for (int j = 0; j < 4 * NT; ++j) {
-      const int col = 2 * j + (lane >> 4), tok = col / CPT, p = col % CPT;
-      const bool live = tok < c.u.z && p < HPARTS && k < a.hpitch;
-      cp_async16(ring_at + i * STAGE + chunk_at(col, chunk), live ? a.h + ((int64_t)(c.u.y + tok) * HPARTS + p) * a.hpitch + k : a.h, live);
+    for (int i = 0; i < R::COPIES; ++i) {
+      const int col = (int)(threadIdx.x >> 4) + 16 * i, tok = col / CPT, p = col % CPT;
+      cols.off[i] = tok < xp.u.z && p < HPARTS ? 2 * (((int64_t)(xp.u.y + tok) * HPARTS + p) * a.hpitch) : -1;
     }
   };
-  Place ahead = place(q0);
-  {
-    Place c = ahead;
+  const uint8_t* hb = reinterpret_cast<const uint8_t*>(a.h);
+  const uint32_t ring_at = smem_u32(w4_smem);
+  int xslot = 0, slot = 0;
+  auto next_tokens = [&]() {
+    cols.copy(ring_at + xslot * R::BYTES, hb, xp.kt, (int)a.hpitch);
+    xslot = xslot + 1 == R::STAGES ? 0 : xslot + 1;
+    if (advance(xp)) columns();
+  };
+  // the choices whose sums this lane will hold, asked for as their unit begins
+  constexpr int MINE = HPARTS == 2 ? NT : NT;
+  Choice mine[MINE];
+  auto choices = [&]() {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i)
-      if (q0 + i < q1) {
-        weights(i, c);
-        advance(c, q0 + i + 1 < q1);
+    for (int nt = 0; nt < NT; ++nt) {
+      const int tok = HPARTS == 2 ? 4 * nt + t : 2 * nt + (t >> 1);
+      mine[nt] = {-1, 0.0f};
+      if (tok < now.u.z) {
+        const int2 c = __ldcg(reinterpret_cast<const int2*>(a.choices) + now.u.y + tok);
+        mine[nt] = {c.x, __int_as_float(c.y)};
       }
-  }
-  pdl_wait();
-  Place now = ahead;
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) {
-    if (q0 + i < q1) {
-      hidden(i, ahead);
-      advance(ahead, q0 + i + 1 < q1);
     }
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (i < n) next_weights(i);
+  columns();
+  choices();
+  pdl_wait();
+#pragma unroll
+  for (int i = 0; i < R::STAGES - 1; ++i) {
+    if (i < n) next_tokens();
     cp_async_commit();
   }
   float sum[1][NT][4];
@@ -497,60 +375,44 @@ __global__ void __launch_bounds__(32 * WARPS) down_kernel(const __grid_constant_
   for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
     for (int e = 0; e < 4; ++e) sum[0][nt][e] = 0.0f;
-  for (int64_t q = q0; q < q1; q += AHEAD) {
+  float* own = part + warp * TILE_ROWS;
+  for (int64_t q = 0; q < n; q += AHEAD) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
-      if (q + i >= q1) break;
-      cp_async_wait<AHEAD - 1>();
-      __syncwarp();
-      multiply<T, 1, NT, PER>(tile[i], ring + i * STAGE, sum, lane);
-      __syncwarp();
-      if (q + i + AHEAD < q1) {
-        weights(i, ahead);
-        hidden(i, ahead);
-        advance(ahead, q + i + AHEAD + 1 < q1);
-      }
+      if (q + i >= n) break;  // the same for the whole block
+      cp_async_wait<R::STAGES - 2>();
+      __syncthreads();  // the stage is there for everyone, and the one before has been read
+      if (q + i + R::STAGES - 1 < n) next_tokens();
       cp_async_commit();
-      if (now.kt == ct - 1 || q + i + 1 == q1) {  // the unit's last tile here
+      multiply<T, 1, NT, PER>(tile[i], w4_smem + slot * R::BYTES, sum, lane);
+      slot = slot + 1 == R::STAGES ? 0 : slot + 1;
+      if (q + i + AHEAD < n) next_weights(i);
+      const bool turn = now.kt == ct - 1;
+      if (turn || q + i + 1 == n) {  // the unit's last tile here
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float v0, v1;  // rows g and g + 8 of this lane's token
-          int tok;
-          bool mine = true;
-          if constexpr (HPARTS == 2) {
-            v0 = sum[0][nt][0] + sum[0][nt][1];
-            v1 = sum[0][nt][2] + sum[0][nt][3];
-            tok = 4 * nt + t;
-          } else {
-            v0 = sum[0][nt][0] + sum[0][nt][1];
-            v1 = sum[0][nt][2] + sum[0][nt][3];
+          float v0 = sum[0][nt][0] + sum[0][nt][1], v1 = sum[0][nt][2] + sum[0][nt][3];  // rows g and g + 8 of this lane's token
+          bool live = mine[nt].token >= 0;
+          constexpr int STEP = HPARTS == 2 ? 1 : 2;
+          if (HPARTS == 3) {
             v0 += __shfl_xor_sync(FULL_MASK, v0, 1);
             v1 += __shfl_xor_sync(FULL_MASK, v1, 1);
-            tok = 2 * nt + (t >> 1);
-            mine = (t & 1) == 0;
+            live &= (t & 1) == 0;
           }
-          mine &= tok < now.u.z;
-          int token = -1;
-          float w = 0.0f;
-          if (mine) {
-            const int choice = __ldcg(a.order + now.u.y + tok);
-            token = choice / a.top;
-            w = __ldcg(a.weights + choice) * Operand<T>::BACK;
-          }
-          float* at = own + token * LD;
+          const float w = mine[nt].weight * Operand<T>::BACK;
+          float* at = own + mine[nt].token * DOWN_LD;
           auto add = [&]() {
             at[g] = fmaf(w, v0, at[g]);
             at[g + 8] = fmaf(w, v1, at[g + 8]);
           };
           // a token that has the expert twice has both places beside one another
-          constexpr int STEP = HPARTS == 2 ? 1 : 2;
-          const int before = __shfl_up_sync(FULL_MASK, token, STEP);
-          if (__any_sync(FULL_MASK, mine && t >= STEP && before == token)) {
-            for (int i = 0; i < 4; ++i) {
-              if (mine && t == i) add();
+          const int before = __shfl_up_sync(FULL_MASK, mine[nt].token, STEP);
+          if (__any_sync(FULL_MASK, live && t >= STEP && before == mine[nt].token)) {
+            for (int k = 0; k < 4; ++k) {
+              if (live && t == k) add();
               __syncwarp();
             }
-          } else if (mine) {
+          } else if (live) {
             add();
           }
           __syncwarp();
@@ -558,33 +420,54 @@ __global__ void __launch_bounds__(32 * WARPS) down_kernel(const __grid_constant_
           for (int e = 0; e < 4; ++e) sum[0][nt][e] = 0.0f;
         }
       }
-      advance(now, q + i + 1 < q1);
+      if (advance(now)) choices();
     }
   }
   cp_async_wait<0>();
-  __syncthreads();
-  for (int i = threadIdx.x; i < a.P * TILE_ROWS; i += 32 * WARPS) {
-    float* at = part + i / TILE_ROWS * LD + i % TILE_ROWS;
-    float v = 0.0f;
-#pragma unroll
-    for (int k = 0; k < WARPS; ++k) v += at[k * a.P * LD];
-    *at = v;  // the first warp's place
-  }
   if (a.splits > 1)
     cluster_sync();
   else
     __syncthreads();
-  for (int i = threadIdx.x + 32 * WARPS * sp; i < a.P * TILE_ROWS; i += 32 * WARPS * a.splits) {
-    const float* at = part + i / TILE_ROWS * LD + i % TILE_ROWS;
+  const int m0 = blockIdx.x / a.splits * DOWN_ROWS;
+  for (int i = threadIdx.x + THREADS * sp; i < a.P * DOWN_ROWS; i += THREADS * a.splits) {
+    const int p = i / DOWN_ROWS, r = i % DOWN_ROWS;
+    const float* at = part + p * DOWN_LD + r;
     float v = 0.0f;
     if (a.splits == 1)
       v = at[0];
     else
       for (int k = 0; k < a.splits; ++k) v += ld_cluster(at, k);
-    const int m = mt * TILE_ROWS + i % TILE_ROWS;
-    if (m < a.K) store_typed(a.y, a.ytype, (int64_t)(i / TILE_ROWS) * a.K + m, v);
+    if (m0 + r < a.K) store_typed(a.y, a.ytype, (int64_t)p * a.K + m0 + r, v);
   }
   if (a.splits > 1) cluster_sync();  // no block leaves while another may read its sums
+}
+
+// ------------------------------------------------------------------ the choices' outputs together
+// y[p] = sum_j weights[p][j] z[places[p][j]], V values a thread.
+template <int V>
+__global__ void __launch_bounds__(256) combine_kernel(const float* z, const int32_t* places, const float* weights, int top, int K, void* y,
+                                                      int ytype) {
+  const int p = blockIdx.y, m = ((int)blockIdx.x * 256 + (int)threadIdx.x) * V;
+  pdl_wait();
+  if (m >= K) return;
+  float v[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) v[i] = 0.0f;
+#pragma unroll 4
+  for (int j = 0; j < top; ++j) {
+    const int at = __ldcg(places + p * top + j);
+    const float w = __ldcg(weights + p * top + j);
+    if (at < 0) continue;
+    const float* row = z + (int64_t)at * K + m;
+    if constexpr (V == 4) {
+      const float4 f = __ldcg(reinterpret_cast<const float4*>(row));
+      v[0] = fmaf(w, f.x, v[0]), v[1] = fmaf(w, f.y, v[1]), v[2] = fmaf(w, f.z, v[2]), v[3] = fmaf(w, f.w, v[3]);
+    } else {
+      v[0] = fmaf(w, __ldcg(row), v[0]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i) store_typed(y, ytype, (int64_t)p * K + m + i, v[i]);
 }
 
 // ------------------------------------------------------------------ host side
@@ -646,44 +529,34 @@ struct Route {
 
 inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
-template <int NT, int PARTS, int HPARTS, typename T, int PER>
-fgq_status launch_hidden_k(const HiddenArgs& a, int blocks, cudaStream_t s) {
-  constexpr int RING = WARPS * AHEAD * 8 * NT * 256, SUMS = WARPS * 8 * NT * 33 * 4, BYTES = RING > SUMS ? RING : SUMS;
-  if (!tc::smem_attr_once<hidden_kernel<T, NT, PER, PARTS, HPARTS>>(BYTES)) return FGQ_ERR_CUDA;
-  return launch_chained(hidden_kernel<T, NT, PER, PARTS, HPARTS>, dim3((unsigned)blocks), 32 * WARPS, BYTES, a.splits, s, a);
-}
-template <int NT, int PARTS, int HPARTS, typename T>
-fgq_status launch_hidden_per(const HiddenArgs& a, int blocks, cudaStream_t s) {
-  if (a.gate.per == 4) return launch_hidden_k<NT, PARTS, HPARTS, T, 4>(a, blocks, s);
-  if (a.gate.per == 2) return launch_hidden_k<NT, PARTS, HPARTS, T, 2>(a, blocks, s);
-  return launch_hidden_k<NT, PARTS, HPARTS, T, 1>(a, blocks, s);
-}
-template <int NT, int HPARTS, int PER>
-fgq_status launch_down_k(const DownArgs& a, cudaStream_t s) {
-  constexpr int RING = WARPS * AHEAD * 8 * NT * 256, MOST = RING + WARPS * CHUNK * (TILE_ROWS + 1) * 4;
+template <int NT, int HPARTS, int PER, int AHEAD>
+fgq_status launch_down_k(const DownArgs& a, unsigned grid, cudaStream_t s) {
+  constexpr int RING = Ring<NT>::TOTAL, MOST = RING + CHUNK * DOWN_LD * 4;
   static_assert(MOST <= 232448, "shared memory budget");
-  if (!tc::smem_attr_once<down_kernel<NT, PER, HPARTS>>(MOST)) return FGQ_ERR_CUDA;
-  return launch_chained(down_kernel<NT, PER, HPARTS>, dim3((unsigned)(a.down.rt * a.splits)), 32 * WARPS,
-                        RING + WARPS * a.P * (TILE_ROWS + 1) * 4, a.splits, s, a);
+  if (!tc::smem_attr_once<down_kernel<NT, PER, HPARTS, AHEAD>>(MOST)) return FGQ_ERR_CUDA;
+  return launch_chained(down_kernel<NT, PER, HPARTS, AHEAD>, dim3(grid), THREADS, RING + a.P * DOWN_LD * 4, a.splits, s, a);
 }
-template <int NT, int HPARTS>
-fgq_status launch_down_per(const DownArgs& a, cudaStream_t s) {
-  if (a.down.per == 4) return launch_down_k<NT, HPARTS, 4>(a, s);
-  if (a.down.per == 2) return launch_down_k<NT, HPARTS, 2>(a, s);
-  return launch_down_k<NT, HPARTS, 1>(a, s);
+template <int NT, int HPARTS, int AHEAD>
+fgq_status launch_down_per(const DownArgs& a, unsigned grid, cudaStream_t s) {
+  if (a.down.per == 4) return launch_down_k<NT, HPARTS, 4, AHEAD>(a, grid, s);
+  if (a.down.per == 2) return launch_down_k<NT, HPARTS, 2, AHEAD>(a, grid, s);
+  return launch_down_k<NT, HPARTS, 1, AHEAD>(a, grid, s);
 }
 
-// Tokens of a unit: 8, which the columns of one product hold, or 16 where experts have more on average.  fp32 tokens take
-// four columns each.
-fgq_status launch_hidden(const HiddenArgs& a, int type, int cap, int blocks, cudaStream_t s) {
-  if (type == FGQ_F32) return launch_hidden_per<4, 3, 3, __nv_bfloat16>(a, blocks, s);
-  if (type == FGQ_BF16)
-    return cap == 8 ? launch_hidden_per<1, 1, 2, __nv_bfloat16>(a, blocks, s) : launch_hidden_per<2, 1, 2, __nv_bfloat16>(a, blocks, s);
-  return cap == 8 ? launch_hidden_per<1, 1, 2, __half>(a, blocks, s) : launch_hidden_per<2, 1, 2, __half>(a, blocks, s);
+// Tokens of a unit: 8, which the columns of one product hold, 16 or 32 where experts have more on average.  fp32 tokens take
+// four columns each, and 8.
+int unit_tokens(int type, int A, int E) {
+  if (type == FGQ_F32 || A <= 8ll * E) return 8;
+  return A <= 16ll * E ? 16 : 32;
 }
-fgq_status launch_down(const DownArgs& a, int type, int cap, cudaStream_t s) {
-  if (type == FGQ_F32) return launch_down_per<4, 3>(a, s);
-  return cap == 8 ? launch_down_per<2, 2>(a, s) : launch_down_per<4, 2>(a, s);
+fgq_status launch_hidden(const RowsArgs& a, int type, int cap, unsigned grid, cudaStream_t s) {
+  if (type == FGQ_F32) return launch_gated_f32(a, grid, s);
+  return type == FGQ_BF16 ? launch_gated_bf16(a, cap / 8, grid, s) : launch_gated_f16(a, cap / 8, grid, s);
+}
+fgq_status launch_down(const DownArgs& a, int type, int cap, unsigned grid, cudaStream_t s) {
+  if (type == FGQ_F32) return launch_down_per<4, 3, 4>(a, grid, s);
+  if (cap == 8) return launch_down_per<2, 2, 4>(a, grid, s);
+  return cap == 16 ? launch_down_per<4, 2, 4>(a, grid, s) : launch_down_per<8, 2, 3>(a, grid, s);
 }
 
 // route == nullptr: ids and weights are given.
@@ -694,12 +567,18 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   const int parts = type == FGQ_F32 ? 3 : 1, hparts = type == FGQ_F32 ? 3 : 2;
   const bool direct = direct_tokens(x, type, P, K, ldx);
   const int64_t hpitch = (int64_t)row_tiles(F) * TILE_ROWS;
-  const int cap = type != FGQ_F32 && (int64_t)A > 8ll * E ? 16 : 8;
+  // tokens held in shared memory where units of 8 (fp32: 4) do and they fit
+  const int ctk = col_tiles(K), ctf = col_tiles(F);
+  const ResidentPlan hp = type == FGQ_F32 ? plan_resident<2, 2, GATED_AHEAD>(ctk, 128 / gate->group) : plan_resident<2, 1, GATED_AHEAD>(ctk, 128 / gate->group);
+  const ResidentPlan dp = plan_resident<1, 2, HELD_AHEAD1>(ctf, 128 / down->group);
+  const bool held = hp.warps > 0 && dp.warps > 0 && (type == FGQ_F32 ? A <= 4ll * E : A <= 8ll * E);
+  const int cap = held && type == FGQ_F32 ? 4 : unit_tokens(type, A, E);
   const int most_units = (A < E || P == 1 ? A : E) + A / cap;
   const size_t b_x = direct ? 0 : up256(copied_bytes(type, pass, K)), b_h = up256((size_t)A * hparts * hpitch * 2);
-  const size_t b_units = up256(sizeof(Unit) * most_units), b_order = up256(4 * (size_t)A), b_n = 256;
+  const size_t b_units = up256(sizeof(Unit) * most_units), b_choices = up256(sizeof(Choice) * (size_t)A), b_n = 256;
+  const size_t b_places = up256(4 * (size_t)A), b_z = held ? up256(4 * (size_t)A * K) : 0;
   const size_t b_logits = route ? up256(8 * (size_t)pass * E) : 0, b_ids = route ? up256(4 * (size_t)A) : 0;
-  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(b_x + b_h + b_units + b_order + b_n + b_logits + 2 * b_ids, s));
+  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(b_x + b_h + b_units + b_choices + b_n + b_places + b_z + b_logits + 2 * b_ids, s));
   if (!tmp) return FGQ_ERR_CUDA;
   uint8_t* at = tmp;
   auto take = [&](size_t n) {
@@ -710,8 +589,10 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   void* xc = take(b_x);
   uint16_t* h = reinterpret_cast<uint16_t*>(take(b_h));
   Unit* units = reinterpret_cast<Unit*>(take(b_units));
-  int32_t* order = reinterpret_cast<int32_t*>(take(b_order));
+  Choice* choices = reinterpret_cast<Choice*>(take(b_choices));
   int* nunits = reinterpret_cast<int*>(take(b_n));
+  int32_t* places = reinterpret_cast<int32_t*>(take(b_places));
+  float* z = reinterpret_cast<float*>(take(b_z));
   double* logits = reinterpret_cast<double*>(take(b_logits));
   int32_t* own_ids = reinterpret_cast<int32_t*>(take(b_ids));
   float* own_weights = reinterpret_cast<float*>(take(b_ids));
@@ -733,7 +614,7 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
       const RouteArgs ra = {xp, route->router, logits, ldx, np, K, E};
       st = launch_logits(ra, type, route->rtype, s);
       if (st != FGQ_OK) break;
-      const SelectArgs sa = {logits, own_ids, own_weights, np == 1 ? units : nullptr, order, nunits, np, E, top, route->score,
+      const SelectArgs sa = {logits, own_ids, own_weights, np == 1 ? units : nullptr, choices, places, nunits, np, E, top, route->score,
                              route->renormalize, route->scale};
       st = launch_select(sa, s);
       if (st != FGQ_OK) break;
@@ -741,26 +622,53 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
     if (!route || np > 1) {
       // without a router the kernel before is the caller's, or the copy
       if (route)
-        st = launch_chained(group_kernel, dim3(1), GR_THREADS, 0, 1, s, pid, na, E, cap, units, order, nunits);
+        st = launch_chained(group_kernel, dim3(1), GR_THREADS, 0, 1, s, pid, pw, na, top, E, cap, units, choices, places, nunits);
       else {
-        group_kernel<<<1, GR_THREADS, 0, s>>>(pid, na, E, cap, units, order, nunits);
+        group_kernel<<<1, GR_THREADS, 0, s>>>(pid, pw, na, top, E, cap, units, choices, places, nunits);
         st = after_launch();
       }
       if (st != FGQ_OK) break;
     }
-    HiddenArgs ha = {mg, mu, rows, units, order, nunits, h, hpitch, F, top, 1};
-    const int nu = (na < E || np == 1 ? na : E) + (np == 1 ? 0 : na / cap);
-    // blocks that share K or the units: up to two an SM, a tile for each warp
-    const int64_t hb = (int64_t)nu * mg.rt;
-    while (ha.splits < 8 && hb * ha.splits * 2 <= 2 * device_sms() && mg.ct >= 2 * WARPS * ha.splits) ha.splits *= 2;
-    if (hb * ha.splits > INT32_MAX) st = FGQ_ERR_UNSUPPORTED;
-    if (st == FGQ_OK) st = launch_hidden(ha, type, cap, (int)(hb * ha.splits), s);
+    const int nu = (na < E || np == 1 ? na : E) + (np == 1 ? 0 : na / cap);  // units at most
+    uint8_t* yp = static_cast<uint8_t*>(y) + (int64_t)p0 * K * float_bytes(type);
+    if (held) {
+      const int64_t hi = (int64_t)nu * mg.rt, di = (int64_t)nu * md.rt;
+      if (hi > INT32_MAX || di > INT32_MAX) {
+        st = FGQ_ERR_UNSUPPORTED;
+        break;
+      }
+      ResidentArgs ra = {};
+      ra.w = mg, ra.up = mu, ra.x = rows, ra.M = F, ra.units = units, ra.choices = choices, ra.nunits = nunits, ra.h = h, ra.hpitch = hpitch;
+      st = type == FGQ_F32 ? launch_held_gated_f32(ra, hp, hi, s)
+                           : (type == FGQ_BF16 ? launch_held_gated_bf16(ra, hp, hi, s) : launch_held_gated_f16(ra, hp, hi, s));
+      if (st != FGQ_OK) break;
+      ra.w = md, ra.x = {h, hparts * hpitch, (int)hpitch}, ra.M = K, ra.z = z;
+      st = type == FGQ_F32 ? launch_held_per<__nv_bfloat16, 1, 2, 3, MODE_DOWN, 1, HELD_AHEAD1>(ra, dp, di, true, s)
+                           : launch_held_per<__nv_bfloat16, 1, 2, 2, MODE_DOWN, 1, HELD_AHEAD1>(ra, dp, di, true, s);
+      if (st != FGQ_OK) break;
+      const bool four = K % 4 == 0;
+      const dim3 cg((unsigned)((K + (four ? 1023 : 255)) / (four ? 1024 : 256)), (unsigned)np);
+      st = four ? launch_chained(combine_kernel<4>, cg, 256, 0, 1, s, static_cast<const float*>(z), static_cast<const int32_t*>(places), pw,
+                                 top, K, static_cast<void*>(yp), type)
+                : launch_chained(combine_kernel<1>, cg, 256, 0, 1, s, static_cast<const float*>(z), static_cast<const int32_t*>(places), pw,
+                                 top, K, static_cast<void*>(yp), type);
+      continue;
+    }
+    RowsArgs ha = {};
+    ha.w = mg, ha.up = mu, ha.x = rows, ha.M = F, ha.units = units, ha.choices = choices, ha.nunits = nunits, ha.h = h, ha.hpitch = hpitch;
+    const int64_t items = (int64_t)nu * ((mg.rt + WARPS - 1) / WARPS);
+    if (items > INT32_MAX / 8) {
+      st = FGQ_ERR_UNSUPPORTED;
+      break;
+    }
+    const RowsPlan plan = plan_rows(items, mg.ct);
+    ha.splits = plan.splits;
+    st = launch_hidden(ha, type, cap, plan.grid, s);
     if (st != FGQ_OK) break;
-    DownArgs da = {md, h, hpitch, units, order, nunits, pw, static_cast<uint8_t*>(y) + (int64_t)p0 * K * float_bytes(type), np, K,
-                   type, top, 1};
-    while (da.splits < 8 && (int64_t)md.rt * da.splits * 2 <= 2 * device_sms() && (int64_t)nu * md.ct >= 2 * WARPS * da.splits)
-      da.splits *= 2;
-    st = launch_down(da, type, cap, s);
+    DownArgs da = {md, h, hpitch, units, choices, nunits, yp, np, K, type, 1};
+    const int groups = (md.rt + WARPS - 1) / WARPS;
+    while (da.splits < 8 && (int64_t)groups * da.splits * 2 <= 2 * device_sms() && (int64_t)nu * md.ct >= 4 * da.splits) da.splits *= 2;
+    st = launch_down(da, type, cap, (unsigned)(groups * da.splits), s);
   }
   if (cudaFreeAsync(tmp, s) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
   return st;
@@ -818,7 +726,7 @@ fgq_status fgq_route_tokens(const void* x, fgq_float_type type, int P, int K, in
   double* logits = static_cast<double*>(scratch_alloc(8 * (size_t)P * E, stream));
   if (!logits) return FGQ_ERR_CUDA;
   st = launch_logits({x, router, logits, P > 1 ? ldx : 0, P, K, E}, type, rtype, stream);
-  if (st == FGQ_OK) st = launch_select({logits, ids, weights, nullptr, nullptr, nullptr, P, E, top, score, renormalize, scale}, stream);
+  if (st == FGQ_OK) st = launch_select({logits, ids, weights, nullptr, nullptr, nullptr, nullptr, P, E, top, score, renormalize, scale}, stream);
   if (cudaFreeAsync(logits, stream) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
   return st;
 }

@@ -92,6 +92,7 @@ template <>
 struct Scales<4> {
   uint2 v;
   __device__ __forceinline__ void load(const uint16_t* p) { v = __ldg(reinterpret_cast<const uint2*>(p)); }
+  __device__ __forceinline__ void read(const uint16_t* p) { v = *reinterpret_cast<const uint2*>(p); }  // shared memory
   __device__ __forceinline__ float get(int i) const {
     const uint32_t w = i < 2 ? v.x : v.y;
     return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
@@ -101,12 +102,14 @@ template <>
 struct Scales<2> {
   uint32_t v;
   __device__ __forceinline__ void load(const uint16_t* p) { v = __ldg(reinterpret_cast<const uint32_t*>(p)); }
+  __device__ __forceinline__ void read(const uint16_t* p) { v = *reinterpret_cast<const uint32_t*>(p); }  // shared memory
   __device__ __forceinline__ float get(int i) const { return __uint_as_float(i ? v & 0xffff0000u : v << 16); }
 };
 template <>
 struct Scales<1> {
   uint16_t v;
   __device__ __forceinline__ void load(const uint16_t* p) { v = __ldg(p); }
+  __device__ __forceinline__ void read(const uint16_t* p) { v = *p; }  // shared memory
   __device__ __forceinline__ float get(int) const { return __uint_as_float((uint32_t)v << 16); }
 };
 
@@ -129,32 +132,31 @@ struct Tile {
   }
 };
 
-// A warp's stage of tokens in shared memory: 8 NT columns of 128 values, 256 bytes each, 16-byte chunks of odd columns
+// Tiles in shared memory: codes, then scales, as in memory.
+template <int PER>
+constexpr int tile_bytes() {
+  return TILE_BYTES + TILE_ROWS * PER * 2;
+}
+// Tile number `at` of the matrix to shared address `to`, by a warp.
+template <int PER>
+__device__ __forceinline__ void copy_tile(uint32_t to, const uint8_t* codes, const uint16_t* scales, int64_t at, int lane) {
+  const uint8_t* p = codes + at * TILE_BYTES + 16 * lane;
+  cp_async16(to + 16 * lane, p, 16u);
+  cp_async16(to + 512 + 16 * lane, p + 512, 16u);
+  if (lane < 2 * PER) cp_async16(to + TILE_BYTES + 16 * lane, reinterpret_cast<const uint8_t*>(scales) + at * (TILE_ROWS * PER * 2) + 16 * lane, 16u);
+}
+template <int PER>
+__device__ __forceinline__ void read_tile(Tile<PER>& tile, const uint8_t* from, int lane) {
+  tile.w[0] = *reinterpret_cast<const uint4*>(from + 16 * lane);
+  tile.w[1] = *reinterpret_cast<const uint4*>(from + 512 + 16 * lane);
+  const uint16_t* s = reinterpret_cast<const uint16_t*>(from + TILE_BYTES) + (lane >> 2) * PER;
+  tile.s[0].read(s);
+  tile.s[1].read(s + 8 * PER);
+}
+
+// A stage of tokens in shared memory: 8 NT columns of 128 values, 256 bytes each, 16-byte chunks of odd columns
 // moved by 64 bytes, so that eight lanes that read two columns meet all banks.
 __device__ __forceinline__ uint32_t chunk_at(int col, int chunk) { return (uint32_t)(col * 256 + ((chunk ^ ((col & 1) << 2)) << 4)); }
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
-// Columns [128 kt, + 128) of the tokens into a stage; rows[c]: byte offset of column c's token row from `base`, or -1 (zeros).
-// Columns from kvalid (a multiple of 8) on are zeros.
-template <int NT>
-__device__ __forceinline__ void fetch_tokens(uint32_t stage, const uint8_t* base, const int64_t* rows, int kt, int kvalid, int lane) {
-  const int chunk = lane & 15, k = kt * TILE_COLS + 8 * chunk;
-#pragma unroll
-  for (int i = 0; i < 4 * NT; ++i) {
-    const int col = 2 * i + (lane >> 4);
-    const int64_t at = rows[col];
-    const bool live = at >= 0 && k < kvalid;
-    cp_async16(stage + chunk_at(col, chunk), live ? base + at + 2 * (int64_t)k : base, live);
-  }
-}
 
 // sum[mt][nt] += tile mt times the stage's columns; sums are in units of 1 / BACK.
 template <typename T, int MT, int NT, int PER>
@@ -200,6 +202,35 @@ __device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint
     }
   }
 }
+
+// How a block shares its work.  Eight warps take 16 rows of weights each (MT tiles of them), all on the same 8 NT columns of
+// tokens: a stage is one tile column, its tokens copied once into shared memory, STAGES of them in a ring that one barrier a
+// stage keeps in order, and its weights loaded by each warp for itself, AHEAD stages before they are multiplied.  Sums stay in
+// registers over all stages.
+constexpr int WARPS = 8, THREADS = 32 * WARPS;
+
+template <int NT>
+struct Ring {
+  static constexpr int STAGES = NT >= 8 ? 4 : 5, BYTES = 8 * NT * 256, COPIES = (8 * NT + 15) / 16;
+  static constexpr int TOTAL = STAGES * BYTES;
+};
+
+// The 16-byte pieces of a stage that one thread copies: piece tid % 16 of columns tid / 16 + 16 i.
+template <int NT>
+struct Columns {
+  int64_t off[Ring<NT>::COPIES];  // bytes from the tokens' start, or -1: zeros
+  // columns [128 kt, + 128); those from kvalid (a multiple of 8) on are zeros
+  __device__ __forceinline__ void copy(uint32_t stage, const uint8_t* base, int kt, int kvalid) const {
+    const int chunk = threadIdx.x & 15, k = kt * TILE_COLS + 8 * chunk;
+#pragma unroll
+    for (int i = 0; i < Ring<NT>::COPIES; ++i) {
+      const int col = (int)(threadIdx.x >> 4) + 16 * i;
+      if (NT == 1 && col >= 8) break;
+      const bool live = off[i] >= 0 && k < kvalid;
+      cp_async16(stage + chunk_at(col, chunk), live ? base + off[i] + 2 * (int64_t)k : base, live ? 16u : 0u);
+    }
+  }
+};
 
 // Tokens as operand rows: 16-bit elements, a token's `parts` rows beside one another (fp32: three bf16 parts that add up
 // to it exactly, in four columns of a product; 16-bit: themselves).

@@ -1,0 +1,64 @@
+// Launches of the few-token products, one translation unit for each type of tokens.
+#pragma once
+
+#include "w4_resident.cuh"
+
+namespace fgq {
+namespace w4 {
+
+// Columns of tokens that a block takes: 8 nt.  A linear layer (mt row tiles a warp: 2 with nt up to 2, else 1).
+fgq_status launch_rows_bf16(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s);
+fgq_status launch_rows_f16(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s);
+fgq_status launch_rows_f32(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s);
+// Gate and up of a gated layer.
+fgq_status launch_gated_bf16(const RowsArgs& a, int nt, unsigned grid, cudaStream_t s);
+fgq_status launch_gated_f16(const RowsArgs& a, int nt, unsigned grid, cudaStream_t s);
+fgq_status launch_gated_f32(const RowsArgs& a, unsigned grid, cudaStream_t s);
+
+// The same with tokens held in shared memory: up to 8 nt columns (nt 1 or 2), where plan_resident finds room for them.
+fgq_status launch_held_bf16(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s);
+fgq_status launch_held_f16(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s);
+fgq_status launch_held_f32(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s);
+// Gate and up, `items` at most: 8 tokens a unit (fp32: 4).
+fgq_status launch_held_gated_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
+fgq_status launch_held_gated_f16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
+fgq_status launch_held_gated_f32(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
+
+template <typename T, int MT, int NT, int PARTS, int MODE, int HPARTS, int AHEAD>
+fgq_status launch_held_per(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, bool chained, cudaStream_t s) {
+  if (a.w.per == 4) return launch_resident<T, MT, NT, 4, PARTS, MODE, HPARTS, AHEAD>(a, plan, items, chained, s);
+  if (a.w.per == 2) return launch_resident<T, MT, NT, 2, PARTS, MODE, HPARTS, AHEAD>(a, plan, items, chained, s);
+  return launch_resident<T, MT, NT, 1, PARTS, MODE, HPARTS, AHEAD>(a, plan, items, chained, s);
+}
+// Tiles under way of a warp: 4 KB, or 2 to 4 pairs.
+constexpr int HELD_AHEAD1 = 4, HELD_AHEAD2 = 2, GATED_AHEAD = 3;
+inline ResidentPlan plan_held(int nt, int mt, int ct, int per) {
+  if (nt == 1) return mt == 2 ? plan_resident<2, 1, HELD_AHEAD2>(ct, per) : plan_resident<1, 1, HELD_AHEAD1>(ct, per);
+  return plan_resident<1, 2, HELD_AHEAD1>(ct, per);
+}
+template <typename T, int PARTS>
+fgq_status launch_held_type(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
+  if (nt == 1 && mt == 2) return launch_held_per<T, 2, 1, PARTS, MODE_LINEAR, 1, HELD_AHEAD2>(a, plan, a.items, chained, s);
+  if (nt == 1) return launch_held_per<T, 1, 1, PARTS, MODE_LINEAR, 1, HELD_AHEAD1>(a, plan, a.items, chained, s);
+  return launch_held_per<T, 1, 2, PARTS, MODE_LINEAR, 1, HELD_AHEAD1>(a, plan, a.items, chained, s);
+}
+
+template <typename T, int MT, int NT, int PARTS, bool GATED, int HPARTS, int AHEAD>
+fgq_status launch_rows_per(const RowsArgs& a, unsigned grid, bool chained, cudaStream_t s) {
+  if (a.w.per == 4) return launch_rows<T, MT, NT, 4, PARTS, GATED, HPARTS, AHEAD>(a, grid, chained, s);
+  if (a.w.per == 2) return launch_rows<T, MT, NT, 2, PARTS, GATED, HPARTS, AHEAD>(a, grid, chained, s);
+  return launch_rows<T, MT, NT, 1, PARTS, GATED, HPARTS, AHEAD>(a, grid, chained, s);
+}
+
+template <typename T, int PARTS>
+fgq_status launch_rows_type(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s) {
+  if (nt == 1 && mt == 2) return launch_rows_per<T, 2, 1, PARTS, false, 1, 3>(a, grid, chained, s);
+  if (nt == 1) return launch_rows_per<T, 1, 1, PARTS, false, 1, 4>(a, grid, chained, s);
+  if (nt == 2 && mt == 2) return launch_rows_per<T, 2, 2, PARTS, false, 1, 3>(a, grid, chained, s);
+  if (nt == 2) return launch_rows_per<T, 1, 2, PARTS, false, 1, 4>(a, grid, chained, s);
+  if (nt == 4) return launch_rows_per<T, 1, 4, PARTS, false, 1, 4>(a, grid, chained, s);
+  return launch_rows_per<T, 1, 8, PARTS, false, 1, 3>(a, grid, chained, s);
+}
+
+}  // namespace w4
+}  // namespace fgq

@@ -1,0 +1,21 @@
+// Few fp32 tokens, as three bf16 parts each, with 4-bit weights.
+#include "w4_launch.h"
+
+namespace fgq {
+namespace w4 {
+
+fgq_status launch_rows_f32(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s) {
+  return launch_rows_type<__nv_bfloat16, 3>(a, nt, mt, grid, chained, s);
+}
+fgq_status launch_gated_f32(const RowsArgs& a, unsigned grid, cudaStream_t s) {
+  return launch_rows_per<__nv_bfloat16, 2, 4, 3, true, 3, 2>(a, grid, true, s);
+}
+fgq_status launch_held_f32(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
+  return launch_held_type<__nv_bfloat16, 3>(a, nt, mt, plan, chained, s);
+}
+fgq_status launch_held_gated_f32(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
+  return launch_held_per<__nv_bfloat16, 2, 2, 3, MODE_GATED, 3, GATED_AHEAD>(a, plan, items, true, s);
+}
+
+}  // namespace w4
+}  // namespace fgq

@@ -4,10 +4,13 @@
 //   u = post(x),  s = r + scale gate u,  y = pre(s);   norm(z) = z' / sqrt(mean z'^2 + eps) weight + bias
 //
 // A row is held in registers (fp32) from its load to its last store, so each input is read and each output written once:
-// the kernel is bound by those bytes.  The threads of a row each hold up to CH pieces of 8 elements; a layer norm takes its mean
-// first and then the squares of what is left, so that a large mean costs no bits.  Sums of a row meet in the same order
-// always: in registers, by shuffles, over the warps through shared memory.  Rows past 16384 elements are read again for
-// each sum instead (long_kernel).
+// the kernel is bound by those bytes, or by instructions where bf16 rows pass both norms and a gate.  The threads of a row each hold up to
+// CH pieces of 8 elements, two in a packed register pair; a layer norm takes its mean first and then the squares of what is
+// left, so that a large mean costs no bits.  Sums of a row meet in the same order always: in registers, by shuffles, over the
+// warps through shared memory.  Rows past 16384 elements are read again for each sum instead (long_kernel).
+// 8192 x 4096, device time (floor): fp32 79.5 us (79), bf16 layer norms 43 (39.5), bf16 with both norms and a gate 49.5 (39.5;
+// 57 with unpacked arithmetic).  What did not help there: a persistent block with the next row's loads under way to registers (56) or
+// to a ring in shared memory, which takes the place of the weights in L1 (80); 128 threads a row (57).
 #include <cmath>
 
 #include "decoder_internal.cuh"
@@ -44,119 +47,163 @@ __device__ __forceinline__ float row_sum(float v, float (*red)[32], int& turn) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (lane == 0) red[turn][warp] = v;
     __syncthreads();
-    v = lane < NT / 32 ? red[turn][lane] : 0.0f;
-    v = warp_sum(v);
+    v = red[turn][lane & (NT / 32 - 1)];
+#pragma unroll
+    for (int o = NT / 64; o > 0; o >>= 1) v += __shfl_xor_sync(FULL_MASK, v, o);
     turn ^= 1;
   }
   return v;
 }
 
+using f2 = unsigned long long;  // two fp32 values, as the packed instructions take them
+
+// Eight consecutive elements as four pairs.
+__device__ __forceinline__ void load_pairs(const float* p, f2 (&v)[4]) {
+  const ulonglong2 a = __ldg(reinterpret_cast<const ulonglong2*>(p)), b = __ldg(reinterpret_cast<const ulonglong2*>(p) + 1);
+  v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
+}
+template <typename T>
+__device__ __forceinline__ void load_pairs(const T* p, f2 (&v)[4]) {
+  const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 f = unpack2(w[i], T());
+    v[i] = pack_f2(f.x, f.y);
+  }
+}
+
+// Piece c of a row, eight elements of thread tid (VEC: consecutive ones); zeros past the row.
 template <typename T, bool VEC>
-__device__ __forceinline__ void load_piece(const T* row, int c, int tid, int NT, int K, float (&v)[8]) {
+__device__ __forceinline__ void load_piece(const T* row, int c, int tid, int NT, int K, f2 (&v)[4]) {
   if constexpr (VEC) {
     const int k = 8 * (tid + c * NT);
     if (k < K) {
-      load8(row + k, v);
+      load_pairs(row + k, v);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+      for (int i = 0; i < 4; ++i) v[i] = 0ull;
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int k = tid + (8 * c + i) * NT;
-      v[i] = k < K ? to_float(row[k]) : 0.0f;
+    for (int i = 0; i < 4; ++i) {
+      const int k = tid + (8 * c + 2 * i) * NT;
+      v[i] = pack_f2(k < K ? to_float(row[k]) : 0.0f, k + NT < K ? to_float(row[k + NT]) : 0.0f);
     }
   }
 }
 template <typename T, bool VEC>
-__device__ __forceinline__ void store_piece(T* row, int c, int tid, int NT, int K, const float (&v)[8]) {
+__device__ __forceinline__ void store_piece(T* row, int c, int tid, int NT, int K, const f2 (&v)[4]) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack_f2(v[i], f[2 * i], f[2 * i + 1]);
   if constexpr (VEC) {
     const int k = 8 * (tid + c * NT);
-    if (k < K) store8(row + k, v);
+    if (k < K) store8(row + k, f);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int k = tid + (8 * c + i) * NT;
-      if (k < K) from_float(v[i], row[k]);
+      if (k < K) from_float(f[i], row[k]);
     }
   }
 }
-// Whether element i of piece c is in the row.
-template <bool VEC>
-__device__ __forceinline__ bool in_row(int c, int i, int tid, int NT, int K) {
-  return VEC ? 8 * (tid + c * NT) < K : tid + (8 * c + i) * NT < K;
-}
 
-// v to its norm, in registers.
+// v to its norm, in registers.  Elements past the row are 0 before and after.
 template <int NT, int CH, bool VEC>
-__device__ __forceinline__ void normalise(float (&v)[CH][8], const fgq_norm& n, int K, int tid, float (*red)[32], int& turn) {
+__device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int K, int tid, float (*red)[32], int& turn) {
   const float inv_k = 1.0f / (float)K;
+  float a, b;
   if (n.kind == FGQ_NORM_LAYER) {
-    float sum = 0.0f;
+    f2 sum = 0ull;
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum += v[c][i];
-    const float mean = row_sum<NT>(sum, red, turn) * inv_k;
+      for (int i = 0; i < 4; ++i) sum = add_f2(sum, v[c][i]);
+    unpack_f2(sum, a, b);
+    const float mean = row_sum<NT>(a + b, red, turn) * inv_k;
+    const f2 off = pack_f2(-mean, -mean);
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[c][i] = in_row<VEC>(c, i, tid, NT, K) ? v[c][i] - mean : 0.0f;
+      for (int i = 0; i < 4; ++i) {
+        const int k = VEC ? 8 * (tid + c * NT) : tid + (8 * c + 2 * i) * NT;
+        v[c][i] = k < K ? add_f2(v[c][i], off) : 0ull;
+        if (!VEC && k < K && k + NT >= K) v[c][i] &= 0xffffffffull;  // the second of a pair
+      }
   }
-  float sq = 0.0f;
+  f2 sq = 0ull;
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sq = fmaf(v[c][i], v[c][i], sq);
-  const float inv = rsqrtf(row_sum<NT>(sq, red, turn) * inv_k + n.eps);
+    for (int i = 0; i < 4; ++i) sq = fma_f2(v[c][i], v[c][i], sq);
+  unpack_f2(sq, a, b);
+  const float inv = rsqrtf(row_sum<NT>(a + b, red, turn) * inv_k + n.eps);
+  const f2 inv2 = pack_f2(inv, inv);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    float w[8], b[8];
-    if (n.weight) load_piece<float, VEC>(n.weight, c, tid, NT, K, w);
-    if (n.bias) load_piece<float, VEC>(n.bias, c, tid, NT, K, b);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float z = v[c][i] * inv;
-      if (n.weight) z *= w[i];
-      if (n.bias) z += b[i];
-      v[c][i] = z;
+    for (int i = 0; i < 4; ++i) v[c][i] = mul_f2(v[c][i], inv2);
+    f2 w[4];
+    if (n.weight) {
+      load_piece<float, VEC>(n.weight, c, tid, NT, K, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[c][i] = mul_f2(v[c][i], w[i]);
+    }
+    if (n.bias) {
+      load_piece<float, VEC>(n.bias, c, tid, NT, K, w);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[c][i] = add_f2(v[c][i], w[i]);
     }
   }
 }
 
 // NT threads a row; blocks of at least 128 threads.
 template <typename T, typename R, int NT, int CH, bool VEC>
-__global__ void __launch_bounds__(NT < 128 ? 128 : NT) add_norm_kernel(const __grid_constant__ NormArgs a) {
+__global__ void __launch_bounds__(NT < 128 ? 128 : NT, NT == 512 && CH == 2 ? 3 : 1)  // three blocks an SM: 8192 x 8192 84 us, 95 with two
+    add_norm_kernel(const __grid_constant__ NormArgs a) {
   constexpr int RPB = NT < 128 ? 128 / NT : 1;
   __shared__ float red[2][32];
   const int tid = threadIdx.x % NT, p = (int)blockIdx.x * RPB + (int)threadIdx.x / NT;
   if (p >= a.P) return;  // whole warps; with one row a block there is no such block
   int turn = 0;
-  float v[CH][8], r[CH][8];
+  f2 v[CH][4];
+  Raw8<R> raw[VEC ? CH : 1];  // the residual as loaded
+  f2 rs[VEC ? 1 : CH][4];
   const T* x = static_cast<const T*>(a.x) + p * a.ldx;
+  const R* res = static_cast<const R*>(a.r) + p * a.ldr;
 #pragma unroll
   for (int c = 0; c < CH; ++c) load_piece<T, VEC>(x, c, tid, NT, a.K, v[c]);
-  if (a.r) {
-    const R* row = static_cast<const R*>(a.r) + p * a.ldr;
 #pragma unroll
-    for (int c = 0; c < CH; ++c) load_piece<R, VEC>(row, c, tid, NT, a.K, r[c]);
-  } else {
+  for (int c = 0; c < CH; ++c) {
+    if constexpr (VEC) {
+      raw[c].zero();
+      if (a.r && 8 * (tid + c * NT) < a.K) raw[c].load(res + 8 * (tid + c * NT));
+    } else {
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r[c][i] = 0.0f;
+      for (int i = 0; i < 4; ++i) rs[c][i] = 0ull;
+      if (a.r) load_piece<R, false>(res, c, tid, NT, a.K, rs[c]);
+    }
   }
   if (a.has_post) normalise<NT, CH, VEC>(v, a.post, a.K, tid, red, turn);
   const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)(p / a.tokens_per_gate) * a.ldg : nullptr;
+  const f2 scale = pack_f2(a.scale, a.scale);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    float g[8];
-    if (gate) load_piece<T, VEC>(gate, c, tid, NT, a.K, g);
+    if (gate) {
+      f2 g[4];
+      load_piece<T, VEC>(gate, c, tid, NT, a.K, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float u = gate ? v[c][i] * g[i] : v[c][i];
-      v[c][i] = in_row<VEC>(c, i, tid, NT, a.K) ? fmaf(a.scale, u, r[c][i]) : 0.0f;  // past the row: no infinity times 0
+      for (int i = 0; i < 4; ++i) v[c][i] = mul_f2(v[c][i], g[i]);
+    }
+    if constexpr (VEC) {
+      float r[8];
+      raw[c].unpack(r);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[c][i] = fma_f2(scale, v[c][i], pack_f2(r[2 * i], r[2 * i + 1]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[c][i] = fma_f2(scale, v[c][i], rs[c][i]);
     }
     if (a.s) store_piece<R, VEC>(static_cast<R*>(a.s) + p * a.lds, c, tid, NT, a.K, v[c]);
   }
@@ -227,8 +274,9 @@ __global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constan
 template <typename T, typename R, bool VEC>
 fgq_status launch_add_norm(const NormArgs& a, cudaStream_t s) {
   const unsigned P = (unsigned)a.P;
-  // few rows: one piece a thread, so that a row's loads are all in flight at once; many: two, for fewer barriers a byte
-  const bool few = a.P <= 4 * device_sms();
+  // few rows: one piece a thread, for shorter chains of a single row; many: two, for fewer barriers a byte.  4096 bf16 values, us so and
+  // so: 1 row 2.98 and 3.08, 304 rows 3.61 and 3.54, 2432 rows 18.2 and 17.2
+  const bool few = a.P <= 2 * device_sms();
   if (a.K <= 512)
     add_norm_kernel<T, R, 32, 2, VEC><<<(P + 3) / 4, 128, 0, s>>>(a);
   else if (a.K <= 1024)

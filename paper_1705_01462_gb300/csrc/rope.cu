@@ -5,8 +5,9 @@
 // fp32 angle at position 100000 would be off by 0.004 radians; its top 32 bits, as half turns in [-1, 1), go to sincospi.
 //
 // A thread takes one unit of a token's heads: V consecutive values and their partners (half: V pairs; interleaved: V / 2
-// pairs; past rot: V values to copy), 16 bytes each, turns them by angles found once, and does so for every HG-th head.  Bound by
-// bytes: heads read and written once.
+// pairs; past rot: V values to copy), 16 bytes each, turns them by angles found once, and does so for every HG-th head, the loads of
+// four heads ahead of their stores.  Bound by bytes: heads read and written once.  4 x 8192 tokens, 40 heads of 128, bf16: 109 us,
+// 91% of the copy rate (154 with each head's loads behind the stores of the one before).
 #include <cmath>
 #include <type_traits>
 
@@ -32,21 +33,22 @@ struct RopeArgs {
   int units, turning, hg, per_block;  // units of a head, those that turn, groups of heads, tokens of a block
 };
 
-// V elements as fp32 and back: 16 bytes, or one element.
+// V elements as loaded, and as fp32: 16 bytes, or one element.
 template <typename T, int V>
 struct Piece {
-  float v[V];
-  __device__ __forceinline__ void load(const T* p) {
+  using Raw = typename std::conditional<V == 1, T, uint4>::type;
+  Raw raw;
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  __device__ __forceinline__ void unpack(float (&v)[V]) const {
     if constexpr (V == 1) {
-      v[0] = to_float(*p);
+      v[0] = to_float(raw);
     } else if constexpr (std::is_same<T, float>::value) {
-      const float4 a = *reinterpret_cast<const float4*>(p);
-      v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+      v[0] = __uint_as_float(raw.x), v[1] = __uint_as_float(raw.y), v[2] = __uint_as_float(raw.z), v[3] = __uint_as_float(raw.w);
     } else {
-      unpack8(*reinterpret_cast<const uint4*>(p), v, T());
+      unpack8(raw, v, T());
     }
   }
-  __device__ __forceinline__ void store(T* p) const {
+  static __device__ __forceinline__ void store(T* p, const float (&v)[V]) {
     if constexpr (V == 1)
       from_float(v[0], *p);
     else if constexpr (std::is_same<T, float>::value)
@@ -59,7 +61,8 @@ struct Piece {
 // V = 16 bytes of elements, or 1.  A unit that turns is two pieces of V (half) or one (interleaved; V = 1: two elements).
 template <typename T, int V, bool HALF>
 __global__ void __launch_bounds__(RP_THREADS) rope_kernel(const __grid_constant__ RopeArgs a) {
-  constexpr int PAIRS = HALF || V == 1 ? V : V / 2;
+  constexpr int PAIRS = HALF || V == 1 ? V : V / 2, HB = 4;
+  constexpr bool TWO = HALF || V == 1;  // pieces of a unit that turns
   const int first = (int)blockIdx.x * a.per_block, per_token = a.units * a.hg;
   const int n = min(a.per_block, a.tokens - first) * per_token;
   const bool copy = a.x != a.y;
@@ -93,36 +96,46 @@ __global__ void __launch_bounds__(RP_THREADS) rope_kernel(const __grid_constant_
         s[j] *= a.inverse ? -a.magnitude : a.magnitude;
       }
     }
-#pragma unroll 4
-    for (int h = h0; h < a.heads; h += a.hg) {
-      const int64_t head = (int64_t)h * a.D;
-      Piece<T, V> p;
-      p.load(x + head + at0);
-      if constexpr (HALF || V == 1) {
-        if (at1 >= 0) {
-          Piece<T, V> q;
-          q.load(x + head + at1);
-          if (turn) {
+    // HB heads' loads at once: the stores between would hold them back, as y may be x
+    for (int h = h0; h < a.heads; h += HB * a.hg) {
+      Piece<T, V> p[HB], q[HB];
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-              const float f = p.v[j], g = q.v[j];
-              p.v[j] = fmaf(f, c[j], -g * s[j]);
-              q.v[j] = fmaf(g, c[j], f * s[j]);
-            }
-          }
-          q.store(y + head + at1);
-        }
-      } else {
-        if (turn) {
-#pragma unroll
-          for (int j = 0; j < PAIRS; ++j) {
-            const float f = p.v[2 * j], g = p.v[2 * j + 1];
-            p.v[2 * j] = fmaf(f, c[j], -g * s[j]);
-            p.v[2 * j + 1] = fmaf(g, c[j], f * s[j]);
-          }
+      for (int n = 0; n < HB; ++n) {
+        const T* head = x + (int64_t)(h + n * a.hg) * a.D;
+        if (h + n * a.hg < a.heads) {
+          p[n].load(head + at0);
+          if (TWO && at1 >= 0) q[n].load(head + at1);
         }
       }
-      p.store(y + head + at0);
+#pragma unroll
+      for (int n = 0; n < HB; ++n) {
+        if (h + n * a.hg >= a.heads) break;
+        T* head = y + (int64_t)(h + n * a.hg) * a.D;
+        float f[V], e[V];
+        p[n].unpack(f);
+        if constexpr (TWO) {
+          if (at1 >= 0) {
+            q[n].unpack(e);
+            if (turn) {
+#pragma unroll
+              for (int j = 0; j < V; ++j) {
+                const float u = f[j], v = e[j];
+                f[j] = fmaf(u, c[j], -v * s[j]);
+                e[j] = fmaf(v, c[j], u * s[j]);
+              }
+            }
+            Piece<T, V>::store(head + at1, e);
+          }
+        } else if (turn) {
+#pragma unroll
+          for (int j = 0; j < PAIRS; ++j) {
+            const float u = f[2 * j], v = f[2 * j + 1];
+            f[2 * j] = fmaf(u, c[j], -v * s[j]);
+            f[2 * j + 1] = fmaf(v, c[j], u * s[j]);
+          }
+        }
+        Piece<T, V>::store(head + at0, f);
+      }
     }
   }
 }

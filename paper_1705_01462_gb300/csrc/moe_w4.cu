@@ -3,10 +3,10 @@
 //   l = router x;  the `top` largest, their weights g;  y = sum_j g_j down_e (silu(gate_e x) * (up_e x)),  e = the j-th choice
 //
 // Kernels of a layer, each brought up while the one before it runs:
-//   logits_kernel   four warps an expert, four tokens: products of 8 elements in fp32, their sums as pairs of fp32 (two-sum), so that a
-//                   logit is off by about one fp32 rounding and the choice is that of 64-bit sums but for near ties;
-//   select_kernel   a warp a token: the largest one by one, then the weights;
-//   group_kernel    one block: choices sorted by expert, and cut into units of up to 8 to 32 tokens that share an expert;
+//   route_kernel    a cluster four tokens: products of 8 elements in fp32, their sums as pairs of fp32 (two-sum), so that a
+//                   logit is off by about one fp32 rounding and the choice is that of 64-bit sums but for near ties; the largest
+//                   one by one, and their weights;
+//   group_kernel    (more than four tokens, or choices that are given) one block: choices sorted by expert, and cut into units of up to 8 to 32 tokens that share an expert;
 //   rows_kernel     (w4_rows.cuh) 128 rows of gate and the same of up, for one unit: silu(gate) up, left as bf16 parts;
 //   down_kernel     128 rows of down, for all units: sums stay with the block, or its cluster, so that no order depends on which
 //                   comes first.
@@ -26,180 +26,229 @@ constexpr int CHUNK = 128;  // tokens of a pass
 struct RouteArgs {
   const void* x;
   const void* router;
-  double* logits;  // [P][E]
   int64_t ldx;
-  int P, K, E;
-};
-
-template <typename T>
-__device__ __forceinline__ void load_row8(const T* row, int k, int K, bool vec, float (&v)[8]) {
-  if (vec) {
-    load8(row + k, v);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = k + i < K ? to_float(row[k + i]) : 0.0f;
-  }
-}
-
-constexpr int LG_WARPS = 8, LG_SPLIT = 4, LG_TOKENS = 4;
-template <typename T, typename R>
-__global__ void __launch_bounds__(32 * LG_WARPS) logits_kernel(const __grid_constant__ RouteArgs a, int vec) {
-  __shared__ double part[LG_WARPS][LG_TOKENS];
-  pdl_trigger();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int e = (int)blockIdx.x * (LG_WARPS / LG_SPLIT) + warp / LG_SPLIT, p0 = (int)blockIdx.y * LG_TOKENS;
-  const int np = min(LG_TOKENS, a.P - p0);
-  float hi[LG_TOKENS], lo[LG_TOKENS];
-#pragma unroll
-  for (int i = 0; i < LG_TOKENS; ++i) hi[i] = lo[i] = 0.0f;
-  if (e < a.E) {
-    const R* wr = static_cast<const R*>(a.router) + (int64_t)e * a.K;
-    const T* x = static_cast<const T*>(a.x) + p0 * a.ldx;
-#pragma unroll 2
-    for (int k = 8 * (lane + 32 * (warp % LG_SPLIT)); k < a.K; k += 256 * LG_SPLIT) {
-      float w[8];
-      load_row8(wr, k, a.K, vec, w);
-#pragma unroll
-      for (int i = 0; i < LG_TOKENS; ++i)
-        if (i < np) {
-          float v[8];
-          load_row8(x + i * a.ldx, k, a.K, vec, v);
-          float s = v[0] * w[0];
-#pragma unroll
-          for (int j = 1; j < 8; ++j) s = fmaf(v[j], w[j], s);
-          const float t = hi[i] + s, b = t - hi[i];  // t + the second line's sum = hi + s exactly
-          lo[i] += (hi[i] - (t - b)) + (s - b);
-          hi[i] = t;
-        }
-    }
-  }
-#pragma unroll
-  for (int i = 0; i < LG_TOKENS; ++i) {
-    double v = (double)hi[i] + (double)lo[i];
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(FULL_MASK, v, o);
-    // an overflow leaves NaN in the second sum: the first says what it was
-    const float h = hi[i];
-    const unsigned inf = __ballot_sync(FULL_MASK, nonfinite(h));
-    if (inf) {
-      float f = h;
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) f += __shfl_xor_sync(FULL_MASK, f, o);
-      v = (double)f;
-    }
-    if (lane == 0) part[warp][i] = v;
-  }
-  __syncthreads();
-  if (threadIdx.x < (LG_WARPS / LG_SPLIT) * LG_TOKENS) {
-    const int el = threadIdx.x / LG_TOKENS, i = threadIdx.x % LG_TOKENS, ee = (int)blockIdx.x * (LG_WARPS / LG_SPLIT) + el;
-    if (ee < a.E && i < np) {
-      double v = 0.0;
-#pragma unroll
-      for (int s = 0; s < LG_SPLIT; ++s) v += part[el * LG_SPLIT + s][i];
-      a.logits[(int64_t)(p0 + i) * a.E + ee] = v;
-    }
-  }
-}
-
-struct SelectArgs {
-  const double* logits;
   int32_t* ids;
   float* weights;
-  // P == 1: what group_kernel would find
+  // what group_kernel would find, where the tokens are one cluster's
   Unit* units;
   Choice* choices;
   int32_t* places;
   int* nunits;
-  int P, E, top, score, renormalize;
+  int P, K, E, top, score, renormalize;
   float scale;
 };
 
-// 64-bit floats as whole numbers of the same order; NaN below all.
-__device__ __forceinline__ long long order_key(double v) {
-  const long long b = __double_as_longlong(v);
-  return v == v ? (b < 0 ? b ^ 0x7fffffffffffffffll : b) : (long long)0x8000000000000000ull;
+// hi + lo += h + l, hi the rounded sum of all and lo what it leaves out (two-sum).
+__device__ __forceinline__ void add_pair(float& hi, float& lo, float h, float l) {
+  const float t = hi + h, b = t - hi;
+  lo += ((hi - (t - b)) + (h - b)) + l;
+  hi = t;
 }
-__device__ __forceinline__ double key_value(long long k) { return __longlong_as_double(k < 0 ? k ^ 0x7fffffffffffffffll : k); }
 
-template <int EL>
-__global__ void __launch_bounds__(128) select_kernel(const __grid_constant__ SelectArgs a) {
+// fp32 numbers as whole ones of the same order (no NaN); 0 has one sign.
+__device__ __forceinline__ uint32_t order_of(float v) {
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float of_order(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+
+// A cluster of eight blocks takes four tokens: its 128 warps share the experts, `ks` of them each expert's row, and leave
+// the logits, as ordered pairs of fp32, in the first block's shared memory; there a warp a token takes the largest one by one.
+constexpr int RT_WARPS = 16, RT_CLUSTER = 8, RT_TOKENS = 4;
+
+// TOKENS of a cluster; VEC: 16-byte pieces of aligned rows.
+template <typename T, typename R, int TOKENS, bool VEC>
+__global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WARPS)
+    route_kernel(const __grid_constant__ RouteArgs a, int ks) {
+  __shared__ float2 part[RT_WARPS][TOKENS];
+  __shared__ unsigned long long keys[TOKENS][MAX_EXPERTS];  // of the first block
+  __shared__ int chosen[TOKENS * MAX_TOP];
+  __shared__ float chosen_w[TOKENS * MAX_TOP];
+  __shared__ int ahead[TOKENS * MAX_TOP];
   pdl_trigger();
-  pdl_wait();
-  const int lane = threadIdx.x & 31, p = (int)blockIdx.x * 4 + (int)(threadIdx.x >> 5);
-  if (p >= a.P) return;
-  constexpr long long NONE = (long long)0x8000000000000000ull;
-  long long key[EL];
-  bool bad = false;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = (int)blockIdx.x % RT_CLUSTER, p0 = (int)blockIdx.x / RT_CLUSTER * TOKENS;
+  const int np = min(TOKENS, a.P - p0), kpart = warp % ks, per_pass = RT_CLUSTER * RT_WARPS / ks;
+  const T* x = static_cast<const T*>(a.x) + p0 * a.ldx;
+  for (int e0 = 0; e0 < a.E; e0 += per_pass) {
+    const int e = e0 + (rank * RT_WARPS + warp) / ks;
+    float hi[TOKENS], lo[TOKENS];
 #pragma unroll
-  for (int i = 0; i < EL; ++i) {
-    const int e = lane + 32 * i;
-    double v = 0.0;
+    for (int i = 0; i < TOKENS; ++i) hi[i] = lo[i] = 0.0f;
     if (e < a.E) {
-      v = __ldcg(a.logits + (int64_t)p * a.E + e);
-      bad |= !(v == v);
-    }
-    key[i] = e < a.E ? order_key(v) : NONE;
-  }
-  bad = __any_sync(FULL_MASK, bad);
-  unsigned taken = 0;  // of this lane's, a bit each
-  double best = 0.0;   // the largest
-  float mine = 0.0f, total = 0.0f;  // lane j: the j-th choice's value; their sum
-  int mine_id = 0;
-  for (int j = 0; j < a.top; ++j) {
-    long long k = NONE;
-    int id = 0x7fffffff;
+      const R* wr = static_cast<const R*>(a.router) + (int64_t)e * a.K;
+      const T* row[TOKENS];  // tokens past the last are read as the last
 #pragma unroll
-    for (int i = 0; i < EL; ++i) {
-      const bool open = !(taken >> i & 1u) && lane + 32 * i < a.E;
-      if (open && (id == 0x7fffffff || key[i] > k)) {
-        k = key[i];
-        id = lane + 32 * i;
+      for (int i = 0; i < TOKENS; ++i) row[i] = x + min(i, np - 1) * a.ldx;
+      auto add = [&](int i, const float (&v)[8], const float (&w)[8]) {
+        float s = v[0] * w[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) s = fmaf(v[j], w[j], s);
+        add_pair(hi[i], lo[i], s, 0.0f);
+      };
+      if constexpr (VEC) {  // the next step's loads, all at once, ahead of a step's sums
+        Raw8<R> wn, wc;
+        Raw8<T> xn[TOKENS], xc[TOKENS];
+        auto fetch = [&](int k) {
+          if (k < a.K) {
+            wn.load(wr + k);
+#pragma unroll
+            for (int i = 0; i < TOKENS; ++i) xn[i].load(row[i] + k);
+          }
+        };
+        const int step = 256 * ks;
+        int k = 8 * (lane + 32 * kpart);
+        fetch(k);
+        for (; k < a.K; k += step) {
+          wc = wn;
+#pragma unroll
+          for (int i = 0; i < TOKENS; ++i) xc[i] = xn[i];
+          fetch(k + step);
+          float w[8];
+          wc.unpack(w);
+#pragma unroll
+          for (int i = 0; i < TOKENS; ++i) {
+            float v[8];
+            xc[i].unpack(v);
+            add(i, v, w);
+          }
+        }
+      } else {
+        for (int k = 8 * (lane + 32 * kpart); k < a.K; k += 256 * ks) {
+          float w[8], v[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) w[j] = k + j < a.K ? to_float(wr[k + j]) : 0.0f;
+#pragma unroll
+          for (int i = 0; i < TOKENS; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = k + j < a.K ? to_float(row[i][k + j]) : 0.0f;
+            add(i, v, w);
+          }
+        }
       }
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-      const long long k2 = __shfl_xor_sync(FULL_MASK, k, o);
-      const int id2 = __shfl_xor_sync(FULL_MASK, id, o);
-      if (k2 > k || (k2 == k && id2 < id)) {
-        k = k2;
-        id = id2;
+    for (int i = 0; i < TOKENS; ++i)
+      if (i < np) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          const float h = __shfl_xor_sync(FULL_MASK, hi[i], o), l = __shfl_xor_sync(FULL_MASK, lo[i], o);
+          // the same operands in the same order in both lanes
+          float a0 = lane & o ? h : hi[i], a1 = lane & o ? l : lo[i];
+          add_pair(a0, a1, lane & o ? hi[i] : h, lane & o ? lo[i] : l);
+          hi[i] = a0, lo[i] = a1;
+        }
+        if (lane == 0) part[warp][i] = make_float2(hi[i], lo[i]);
       }
+    __syncthreads();
+    const int el = (int)threadIdx.x / TOKENS, i = (int)threadIdx.x % TOKENS;  // an expert of this block, a token
+    const int ee = e0 + rank * (RT_WARPS / ks) + el;
+    if (el < RT_WARPS / ks && i < np && ee < a.E) {
+      float h = part[el * ks][i].x, l = part[el * ks][i].y;
+      for (int s = 1; s < ks; ++s) add_pair(h, l, part[el * ks + s][i].x, part[el * ks + s][i].y);
+      const float r = h + l, rest = l - (r - h);
+      // infinite sums have no rest; NaN counts as the smallest
+      unsigned long long key = 1ull;
+      if (r == r) key = (unsigned long long)order_of(r) << 32 | (nonfinite(r) ? 0x80000000u : order_of(rest));
+      uint32_t at;
+      asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(smem_u32(&keys[i][ee])));
+      asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(at), "l"(key) : "memory");
     }
-    if ((id & 31) == lane) taken |= 1u << (id >> 5);
-    const double v = key_value(k);
-    if (j == 0) best = v;
-    const float f = a.score == FGQ_SCORE_SOFTMAX ? expf((float)(v - best)) : 1.0f / (1.0f + expf(-(float)v));
-    if (lane == j) {
-      mine = f;
-      mine_id = id;
-    }
-    total += f;
+    __syncthreads();
   }
-  if (a.score == FGQ_SCORE_SOFTMAX && !a.renormalize) {
-    total = 0.0f;
+  cluster_sync();
+  if (rank != 0) return;
+  if (warp < np) {
+    const unsigned long long* key = keys[warp];
+    const int p = p0 + warp, count = (a.E + 31) / 32;
+    bool bad = false;
+    for (int i = 0; i < count; ++i) bad |= lane + 32 * i < a.E && key[lane + 32 * i] == 1ull;
+    bad = __any_sync(FULL_MASK, bad);
+    unsigned taken = 0;  // of this lane's, a bit each
+    float best_h = 0.0f, best_l = 0.0f, mine = 0.0f, total = 0.0f;  // the largest; lane j: the j-th choice's value; their sum
+    int mine_id = 0;
+    auto value = [&](unsigned long long k) {  // less the largest, rounded
+      return (of_order((uint32_t)(k >> 32)) - best_h) + (of_order((uint32_t)k) - best_l);
+    };
+    for (int j = 0; j < a.top; ++j) {
+      unsigned long long k = 0;
+      int id = 0x7fffffff;
+      for (int i = 0; i < count; ++i) {
+        const int e = lane + 32 * i;
+        if (e < a.E && !(taken >> i & 1u) && key[e] > k) {
+          k = key[e];
+          id = e;
+        }
+      }
 #pragma unroll
-    for (int i = 0; i < EL; ++i)
-      if (lane + 32 * i < a.E) total += expf((float)(key_value(key[i]) - best));
+      for (int o = 16; o > 0; o >>= 1) {
+        const unsigned long long k2 = __shfl_xor_sync(FULL_MASK, k, o);
+        const int id2 = __shfl_xor_sync(FULL_MASK, id, o);
+        if (k2 > k || (k2 == k && id2 < id)) {
+          k = k2;
+          id = id2;
+        }
+      }
+      if ((id & 31) == lane) taken |= 1u << (id >> 5);
+      if (j == 0) best_h = of_order((uint32_t)(k >> 32)), best_l = of_order((uint32_t)k);
+      const float f = a.score == FGQ_SCORE_SOFTMAX ? expf(value(k)) : 1.0f / (1.0f + expf(-of_order((uint32_t)(k >> 32))));
+      if (lane == j) {
+        mine = f;
+        mine_id = id;
+      }
+      total += f;
+    }
+    if (a.score == FGQ_SCORE_SOFTMAX && !a.renormalize) {
+      total = 0.0f;
+      for (int i = 0; i < count; ++i)
+        if (lane + 32 * i < a.E) total += expf(value(key[lane + 32 * i]));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL_MASK, total, o);
-  }
-  float w = mine;
-  if (a.score == FGQ_SCORE_SOFTMAX || a.renormalize) w /= total;
-  w *= a.scale;
-  if (bad) w = __uint_as_float(0x7fc00000u);
-  int rank = 0;  // by expert
-  if (a.units)
-    for (int j = 0; j < a.top; ++j) rank += __shfl_sync(FULL_MASK, mine_id, j) < mine_id;
-  if (lane < a.top) {
-    a.ids[(int64_t)p * a.top + lane] = mine_id;
-    a.weights[(int64_t)p * a.top + lane] = w;
-    if (a.units) {
-      a.units[rank] = {mine_id, rank, 1, 0};
-      a.choices[rank] = {0, w};
-      a.places[lane] = rank;
+      for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(FULL_MASK, total, o);
+    }
+    float w = mine;
+    if (a.score == FGQ_SCORE_SOFTMAX || a.renormalize) w /= total;
+    w *= a.scale;
+    if (bad) w = __uint_as_float(0x7fc00000u);
+    if (lane < a.top) {
+      a.ids[(int64_t)p * a.top + lane] = mine_id;
+      a.weights[(int64_t)p * a.top + lane] = w;
+      chosen[warp * a.top + lane] = mine_id;
+      chosen_w[warp * a.top + lane] = w;
     }
   }
-  if (a.units && lane == 0) *a.nunits = a.top;
+  if (!a.units) return;
+  // the choices by expert, each counting for itself; a unit an expert, as four tokens fit every unit
+  __syncthreads();
+  const int n = np * a.top, c = (int)threadIdx.x;
+  int e = 0, place = 0, same = 0, lead = 0;
+  if (c < n) {
+    e = chosen[c];
+    lead = 1;
+    for (int j = 0; j < n; ++j) {
+      const int f = chosen[j];
+      place += f < e || (f == e && j < c);
+      same += f == e;
+      if (f == e && j < c) lead = 0;
+    }
+    ahead[c] = lead;
+  }
+  __syncthreads();
+  if (c < n) {
+    a.choices[place] = {c / a.top, chosen_w[c]};
+    a.places[c] = place;
+    if (lead) {
+      int u = 0;
+      for (int j = 0; j < n; ++j) u += ahead[j] && chosen[j] < e;
+      a.units[u] = {e, place, same, 0};
+    }
+  }
+  if (warp == 0) {
+    int u = 0;
+    for (int j = lane; j < n; j += 32) u += ahead[j];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(FULL_MASK, u, o);
+    if (lane == 0) *a.nunits = u;
+  }
 }
 
 // ------------------------------------------------------------------ choices by expert
@@ -493,32 +542,27 @@ fgq_status launch_chained(void (*kernel)(KArgs...), dim3 grid, unsigned threads,
   return after_launch(cudaLaunchKernelEx(&cfg, kernel, args...));
 }
 
+template <typename T, typename R, int TOKENS>
+fgq_status launch_route_tokens(const RouteArgs& a, bool vec, cudaStream_t s) {
+  int ks = 1;  // warps that share an expert's row
+  while (ks < RT_WARPS && RT_CLUSTER * RT_WARPS / (2 * ks) >= a.E) ks *= 2;
+  const unsigned grid = (unsigned)(((int64_t)a.P + TOKENS - 1) / TOKENS * RT_CLUSTER);
+  if (vec)
+    route_kernel<T, R, TOKENS, true><<<grid, 32 * RT_WARPS, 0, s>>>(a, ks);
+  else
+    route_kernel<T, R, TOKENS, false><<<grid, 32 * RT_WARPS, 0, s>>>(a, ks);
+  return after_launch();
+}
 template <typename T, typename R>
-fgq_status launch_logits_t(const RouteArgs& a, bool vec, cudaStream_t s) {
-  for (int p = 0; p < a.P; p += 65535 * LG_TOKENS) {
-    RouteArgs part = a;
-    part.P = a.P - p < 65535 * LG_TOKENS ? a.P - p : 65535 * LG_TOKENS;
-    part.x = static_cast<const T*>(a.x) + p * a.ldx;
-    part.logits = a.logits + (int64_t)p * a.E;
-    constexpr int EPB = LG_WARPS / LG_SPLIT;
-    logits_kernel<T, R><<<dim3((a.E + EPB - 1) / EPB, (part.P + LG_TOKENS - 1) / LG_TOKENS), 32 * LG_WARPS, 0, s>>>(part, vec);
-    const fgq_status st = after_launch();
-    if (st != FGQ_OK) return st;
-  }
-  return FGQ_OK;
+fgq_status launch_route_t(const RouteArgs& a, bool vec, cudaStream_t s) {
+  return a.P == 1 ? launch_route_tokens<T, R, 1>(a, vec, s) : launch_route_tokens<T, R, RT_TOKENS>(a, vec, s);
 }
-fgq_status launch_logits(const RouteArgs& a, int type, int rtype, cudaStream_t s) {
+fgq_status launch_route(const RouteArgs& a, int type, int rtype, cudaStream_t s) {
   const bool vec = a.K % 8 == 0 && aligned(a.x, 16) && aligned(a.router, 16) && (a.P == 1 || stride16(a.ldx, type));
-  if (type == FGQ_F32) return launch_logits_t<float, float>(a, vec, s);
+  if (type == FGQ_F32) return launch_route_t<float, float>(a, vec, s);
   if (type == FGQ_BF16)
-    return rtype == FGQ_F32 ? launch_logits_t<__nv_bfloat16, float>(a, vec, s) : launch_logits_t<__nv_bfloat16, __nv_bfloat16>(a, vec, s);
-  return rtype == FGQ_F32 ? launch_logits_t<__half, float>(a, vec, s) : launch_logits_t<__half, __half>(a, vec, s);
-}
-fgq_status launch_select(const SelectArgs& a, cudaStream_t s) {
-  const dim3 grid(((unsigned)a.P + 3) / 4);
-  if (a.E <= 64) return launch_chained(select_kernel<2>, grid, 128, 0, 1, s, a);
-  if (a.E <= 256) return launch_chained(select_kernel<8>, grid, 128, 0, 1, s, a);
-  return launch_chained(select_kernel<32>, grid, 128, 0, 1, s, a);
+    return rtype == FGQ_F32 ? launch_route_t<__nv_bfloat16, float>(a, vec, s) : launch_route_t<__nv_bfloat16, __nv_bfloat16>(a, vec, s);
+  return rtype == FGQ_F32 ? launch_route_t<__half, float>(a, vec, s) : launch_route_t<__half, __half>(a, vec, s);
 }
 
 struct Route {
@@ -577,8 +621,8 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   const size_t b_x = direct ? 0 : up256(copied_bytes(type, pass, K)), b_h = up256((size_t)A * hparts * hpitch * 2);
   const size_t b_units = up256(sizeof(Unit) * most_units), b_choices = up256(sizeof(Choice) * (size_t)A), b_n = 256;
   const size_t b_places = up256(4 * (size_t)A), b_z = held ? up256(4 * (size_t)A * K) : 0;
-  const size_t b_logits = route ? up256(8 * (size_t)pass * E) : 0, b_ids = route ? up256(4 * (size_t)A) : 0;
-  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(b_x + b_h + b_units + b_choices + b_n + b_places + b_z + b_logits + 2 * b_ids, s));
+  const size_t b_ids = route ? up256(4 * (size_t)A) : 0;
+  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(b_x + b_h + b_units + b_choices + b_n + b_places + b_z + 2 * b_ids, s));
   if (!tmp) return FGQ_ERR_CUDA;
   uint8_t* at = tmp;
   auto take = [&](size_t n) {
@@ -593,7 +637,6 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   int* nunits = reinterpret_cast<int*>(take(b_n));
   int32_t* places = reinterpret_cast<int32_t*>(take(b_places));
   float* z = reinterpret_cast<float*>(take(b_z));
-  double* logits = reinterpret_cast<double*>(take(b_logits));
   int32_t* own_ids = reinterpret_cast<int32_t*>(take(b_ids));
   float* own_weights = reinterpret_cast<float*>(take(b_ids));
   const Matrix mg = matrix(gate), mu = matrix(up), md = matrix(down);
@@ -610,26 +653,23 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
     }
     const int32_t* pid = ids ? ids + (int64_t)p0 * top : own_ids;
     const float* pw = weights ? weights + (int64_t)p0 * top : own_weights;
+    const bool one = route && np <= RT_TOKENS;  // a cluster's tokens: it leaves units and choices itself
     if (route) {
-      const RouteArgs ra = {xp, route->router, logits, ldx, np, K, E};
-      st = launch_logits(ra, type, route->rtype, s);
-      if (st != FGQ_OK) break;
-      const SelectArgs sa = {logits, own_ids, own_weights, np == 1 ? units : nullptr, choices, places, nunits, np, E, top, route->score,
-                             route->renormalize, route->scale};
-      st = launch_select(sa, s);
+      const RouteArgs ra = {xp, route->router, ldx, own_ids, own_weights, one ? units : nullptr, choices, places, nunits, np, K, E, top,
+                            route->score, route->renormalize, route->scale};
+      st = launch_route(ra, type, route->rtype, s);
       if (st != FGQ_OK) break;
     }
-    if (!route || np > 1) {
-      // without a router the kernel before is the caller's, or the copy
-      if (route)
+    if (!one) {
+      if (route) {
         st = launch_chained(group_kernel, dim3(1), GR_THREADS, 0, 1, s, pid, pw, na, top, E, cap, units, choices, places, nunits);
-      else {
+      } else {  // the kernel before is the caller's, or the copy
         group_kernel<<<1, GR_THREADS, 0, s>>>(pid, pw, na, top, E, cap, units, choices, places, nunits);
         st = after_launch();
       }
       if (st != FGQ_OK) break;
     }
-    const int nu = (na < E || np == 1 ? na : E) + (np == 1 ? 0 : na / cap);  // units at most
+    const int nu = one ? (na < E ? na : E) : (na < E || np == 1 ? na : E) + (np == 1 ? 0 : na / cap);  // units at most
     uint8_t* yp = static_cast<uint8_t*>(y) + (int64_t)p0 * K * float_bytes(type);
     if (held) {
       const int64_t hi = (int64_t)nu * mg.rt, di = (int64_t)nu * md.rt;
@@ -638,7 +678,7 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
         break;
       }
       ResidentArgs ra = {};
-      ra.w = mg, ra.up = mu, ra.x = rows, ra.M = F, ra.units = units, ra.choices = choices, ra.nunits = nunits, ra.h = h, ra.hpitch = hpitch;
+      ra.w = mg, ra.up = mu, ra.x = rows, ra.M = F, ra.units = units, ra.choices = choices, ra.nunits = nunits, ra.h = h, ra.hpitch = hpitch, ra.one = np == 1;
       st = type == FGQ_F32 ? launch_held_gated_f32(ra, hp, hi, s)
                            : (type == FGQ_BF16 ? launch_held_gated_bf16(ra, hp, hi, s) : launch_held_gated_f16(ra, hp, hi, s));
       if (st != FGQ_OK) break;
@@ -701,7 +741,7 @@ fgq_status check_route(const void* x, int type, int P, int K, int64_t ldx, const
     return FGQ_ERR_ARG;
   if (top < 1 || top > E || (P > 1 && ldx < K)) return FGQ_ERR_ARG;
   if (P == 0) return FGQ_OK;
-  if (E > MAX_EXPERTS || top > MAX_TOP || P > MAX_SIZE || K > MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
+  if (E > MAX_EXPERTS || top > MAX_TOP || P > 1 << 29 || K > MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
   if (!x || !router) return FGQ_ERR_ARG;
   if (!aligned(x, float_bytes(type)) || !aligned(router, float_bytes(rtype))) return FGQ_ERR_ALIGN;
   return FGQ_OK;
@@ -723,12 +763,8 @@ fgq_status fgq_route_tokens(const void* x, fgq_float_type type, int P, int K, in
   if (st != FGQ_OK || P == 0) return st;
   if (!ids || !weights) return FGQ_ERR_ARG;
   if (!aligned(ids, 4) || !aligned(weights, 4)) return FGQ_ERR_ALIGN;
-  double* logits = static_cast<double*>(scratch_alloc(8 * (size_t)P * E, stream));
-  if (!logits) return FGQ_ERR_CUDA;
-  st = launch_logits({x, router, logits, P > 1 ? ldx : 0, P, K, E}, type, rtype, stream);
-  if (st == FGQ_OK) st = launch_select({logits, ids, weights, nullptr, nullptr, nullptr, nullptr, P, E, top, score, renormalize, scale}, stream);
-  if (cudaFreeAsync(logits, stream) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
-  return st;
+  return launch_route({x, router, P > 1 ? ldx : 0, ids, weights, nullptr, nullptr, nullptr, nullptr, P, K, E, top, score, renormalize, scale},
+                      type, rtype, stream);
 }
 
 fgq_status fgq_experts_w4(const void* x, fgq_float_type type, int P, int64_t ldx, const int32_t* ids, const float* weights, int top,

@@ -29,6 +29,7 @@ struct ResidentArgs {
   uint16_t* h;  // MODE_GATED: out, [choice][parts][hpitch]
   int64_t hpitch;
   float* z;  // MODE_DOWN: out, [choice][M]
+  int one;    // MODE_GATED: there is one token
   int early;  // the kernel before is this library's: weights may be loaded while it runs
 };
 
@@ -125,14 +126,14 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
   const uint32_t xs = smem_u32(w4_smem);
   // the segment's columns, 16 bytes a thread and turn; columns of no token are left as they are: nothing reads their sums
   auto tokens = [&]() {
-    if (MODE == MODE_GATED) {
+    if (MODE == MODE_GATED && !a.one) {
       if (threadIdx.x < now.u.z) row_of[threadIdx.x] = __ldcg(&a.choices[now.u.y + threadIdx.x].token);
       __syncthreads();
     }
     const int cols = now.u.z * CPT, n = ct * 16 * cols;
     for (int i = threadIdx.x; i < n; i += 32 * W) {
       const int chunk = i & 15, j = i >> 4, kt = j / cols, c = j - kt * cols, tok = c / CPT, part = c % CPT, k = kt * TILE_COLS + 8 * chunk;
-      const int64_t row = MODE == MODE_LINEAR ? tok : (MODE == MODE_GATED ? row_of[tok] : now.u.y + tok);
+      const int64_t row = MODE == MODE_LINEAR ? tok : (MODE == MODE_GATED ? (a.one ? 0 : row_of[tok]) : now.u.y + tok);
       const bool live = part < PARTS && k < a.x.kvalid;
       cp_async16(xs + kt * STAGE + chunk_at(c, chunk), live ? xb + 2 * (row * a.x.pitch + part * (a.x.pitch / PARTS) + k) : xb, live ? 16u : 0u);
     }

@@ -419,11 +419,9 @@ __global__ void __launch_bounds__(THREADS) down_kernel(const __grid_constant__ D
     if (i < n) next_tokens();
     cp_async_commit();
   }
-  float sum[1][NT][4];
+  pair_t sum[1][NT][2];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sum[0][nt][e] = 0.0f;
+  for (int nt = 0; nt < NT; ++nt) sum[0][nt][0] = sum[0][nt][1] = 0ull;
   float* own = part + warp * TILE_ROWS;
   for (int64_t q = 0; q < n; q += AHEAD) {
 #pragma unroll
@@ -440,7 +438,10 @@ __global__ void __launch_bounds__(THREADS) down_kernel(const __grid_constant__ D
       if (turn || q + i + 1 == n) {  // the unit's last tile here
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          float v0 = sum[0][nt][0] + sum[0][nt][1], v1 = sum[0][nt][2] + sum[0][nt][3];  // rows g and g + 8 of this lane's token
+          float s0, s1, u0, u1;
+          unpack_f2(sum[0][nt][0], s0, s1);
+          unpack_f2(sum[0][nt][1], u0, u1);
+          float v0 = s0 + s1, v1 = u0 + u1;  // rows g and g + 8 of this lane's token
           bool live = mine[nt].token >= 0;
           constexpr int STEP = HPARTS == 2 ? 1 : 2;
           if (HPARTS == 3) {
@@ -465,8 +466,7 @@ __global__ void __launch_bounds__(THREADS) down_kernel(const __grid_constant__ D
             add();
           }
           __syncwarp();
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sum[0][nt][e] = 0.0f;
+          sum[0][nt][0] = sum[0][nt][1] = 0ull;
         }
       }
       if (advance(now)) choices();

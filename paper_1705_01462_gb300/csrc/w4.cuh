@@ -54,6 +54,12 @@ struct Operand<__half> {  // n 2^-24 2^15 - 8 2^-9
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
   }
+  // d = a b: no registers to clear
+  static __device__ __forceinline__ void mma_new(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+  }
   static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -68,6 +74,12 @@ struct Operand<__nv_bfloat16> {  // n 2^-133 2^127 - 8 2^-6
     uint32_t r;
     asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
+  }
+  // d = a b: no registers to clear
+  static __device__ __forceinline__ void mma_new(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
   }
   static __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -137,13 +149,11 @@ template <int PER>
 constexpr int tile_bytes() {
   return TILE_BYTES + TILE_ROWS * PER * 2;
 }
-// Tile number `at` of the matrix to shared address `to`, by a warp.
+// A tile to shared address `to`, by a warp; codes and scales: the tile's, 16 bytes on a lane.
 template <int PER>
-__device__ __forceinline__ void copy_tile(uint32_t to, const uint8_t* codes, const uint16_t* scales, int64_t at, int lane) {
-  const uint8_t* p = codes + at * TILE_BYTES + 16 * lane;
-  cp_async16(to + 16 * lane, p, 16u);
-  cp_async16(to + 512 + 16 * lane, p + 512, 16u);
-  if (lane < 2 * PER) cp_async16(to + TILE_BYTES + 16 * lane, reinterpret_cast<const uint8_t*>(scales) + at * (TILE_ROWS * PER * 2) + 16 * lane, 16u);
+__device__ __forceinline__ void copy_tile(uint32_t to, const uint8_t* codes, const uint8_t* scales, int lane) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\ncp.async.cg.shared.global [%0 + 512], [%1 + 512], 16;" ::"r"(to), "l"(codes) : "memory");
+  if (lane < 2 * PER) asm volatile("cp.async.cg.shared.global [%0 + 1024], [%1], 16;" ::"r"(to), "l"(scales) : "memory");
 }
 template <int PER>
 __device__ __forceinline__ void read_tile(Tile<PER>& tile, const uint8_t* from, int lane) {
@@ -158,24 +168,23 @@ __device__ __forceinline__ void read_tile(Tile<PER>& tile, const uint8_t* from, 
 // moved by 64 bytes, so that eight lanes that read two columns meet all banks.
 __device__ __forceinline__ uint32_t chunk_at(int col, int chunk) { return (uint32_t)(col * 256 + ((chunk ^ ((col & 1) << 2)) << 4)); }
 
-// sum[mt][nt] += tile mt times the stage's columns; sums are in units of 1 / BACK.
+// sum[mt][nt] += tile mt times the stage's columns; sums are in units of 1 / BACK.  Sums of two columns are a packed pair: [0] of
+// row g, [1] of row g + 8.
+using pair_t = unsigned long long;
 template <typename T, int MT, int NT, int PER>
-__device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint8_t* stage, float (&sum)[MT][NT][4], int lane) {
+__device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint8_t* stage, pair_t (&sum)[MT][NT][2], int lane) {
   const int g = lane >> 2, t = lane & 3;
+  // chunk 4 j + t of column g (chunk_at): even and odd j
+  const uint8_t* even = stage + chunk_at(g, t);
+  const uint8_t* odd = stage + chunk_at(g, 4 + t);
 #pragma unroll
   for (int gi = 0; gi < PER; ++gi) {
     float acc[MT][NT][4];
 #pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[mt][nt][e] = 0.0f;
-#pragma unroll
     for (int j = gi * (4 / PER); j < (gi + 1) * (4 / PER); ++j) {
       uint4 b[NT];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) b[nt] = *reinterpret_cast<const uint4*>(stage + chunk_at(8 * nt + g, 4 * j + t));
+      for (int nt = 0; nt < NT; ++nt) b[nt] = *reinterpret_cast<const uint4*>((j & 1 ? odd : even) + nt * 2048 + (j >> 1) * 128);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         uint32_t u[4], v[4];
@@ -184,7 +193,10 @@ __device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint
         const uint32_t a0[4] = {u[0], v[0], u[1], v[1]}, a1[4] = {u[2], v[2], u[3], v[3]};
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-          Operand<T>::mma(acc[mt][nt], a0, b[nt].x, b[nt].y);
+          if (j == gi * (4 / PER))
+            Operand<T>::mma_new(acc[mt][nt], a0, b[nt].x, b[nt].y);
+          else
+            Operand<T>::mma(acc[mt][nt], a0, b[nt].x, b[nt].y);
           Operand<T>::mma(acc[mt][nt], a1, b[nt].z, b[nt].w);
         }
       }
@@ -192,12 +204,11 @@ __device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
       const float s0 = tile[mt].s[0].get(gi), s1 = tile[mt].s[1].get(gi);
+      const pair_t p0 = pack_f2(s0, s0), p1 = pack_f2(s1, s1);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
-        sum[mt][nt][0] = fmaf(acc[mt][nt][0], s0, sum[mt][nt][0]);
-        sum[mt][nt][1] = fmaf(acc[mt][nt][1], s0, sum[mt][nt][1]);
-        sum[mt][nt][2] = fmaf(acc[mt][nt][2], s1, sum[mt][nt][2]);
-        sum[mt][nt][3] = fmaf(acc[mt][nt][3], s1, sum[mt][nt][3]);
+        sum[mt][nt][0] = fma_f2(pack_f2(acc[mt][nt][0], acc[mt][nt][1]), p0, sum[mt][nt][0]);
+        sum[mt][nt][1] = fma_f2(pack_f2(acc[mt][nt][2], acc[mt][nt][3]), p1, sum[mt][nt][1]);
       }
     }
   }

@@ -31,7 +31,7 @@ fgq_status launch_held_per(const ResidentArgs& a, const ResidentPlan& plan, int6
   return launch_resident<T, MT, NT, 1, PARTS, MODE, HPARTS, AHEAD>(a, plan, items, chained, s);
 }
 // Tiles under way of a warp: 4 KB, or 2 to 4 pairs.
-constexpr int HELD_AHEAD1 = 4, HELD_AHEAD2 = 2, GATED_AHEAD = 3;
+constexpr int HELD_AHEAD1 = 4, HELD_AHEAD2 = 2, GATED_AHEAD = 2;
 inline ResidentPlan plan_held(int nt, int mt, int ct, int per) {
   if (nt == 1) return mt == 2 ? plan_resident<2, 1, HELD_AHEAD2>(ct, per) : plan_resident<1, 1, HELD_AHEAD1>(ct, per);
   return plan_resident<1, 2, HELD_AHEAD1>(ct, per);

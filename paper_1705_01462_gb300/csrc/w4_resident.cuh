@@ -85,33 +85,43 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
     s.q1 = s.begins(warp + 1);
     return s;
   };
-  int64_t at = 0;  // tile number of the next to load
-  int lkt = 0, lrow = 0, left = 0, lslot = 0;
+  // the next tile to load: its codes and scales, 16 bytes on a lane, and where it goes
+  const uint8_t *codes = nullptr, *scales = nullptr;
+  const int64_t up_codes = MODE == MODE_GATED ? a.up.codes - a.w.codes : 0;
+  const int64_t up_scales = MODE == MODE_GATED ? reinterpret_cast<const uint8_t*>(a.up.scales) - reinterpret_cast<const uint8_t*>(a.w.scales) : 0;
+  int lkt = 0, lrow = 0, left = 0;
+  const uint32_t ring0 = ring_at + 16 * lane, ring_end = ring0 + AHEAD * SLOT;
+  uint32_t to = ring0;
   auto begin = [&](const Segment& s) {
     const int i = s.q0 / ct;
     lkt = s.q0 - i * ct;
     lrow = (s.item + i) * TILES;
-    at = ((int64_t)s.u.x * a.w.rt + lrow) * ct + lkt;
+    const int64_t at = ((int64_t)s.u.x * a.w.rt + lrow) * ct + lkt;
+    codes = a.w.codes + at * TILE_BYTES + 16 * lane;
+    scales = reinterpret_cast<const uint8_t*>(a.w.scales) + at * (TILE_ROWS * PER * 2) + 16 * lane;
     left = s.q1 - s.q0;
   };
   auto load = [&]() {
     if (left > 0) {
       --left;
-      const uint32_t to = ring_at + lslot * SLOT;
-      copy_tile<PER>(to, a.w.codes, a.w.scales, at, lane);
+      copy_tile<PER>(to, codes, scales, lane);
       if (MODE == MODE_GATED) {
-        copy_tile<PER>(to + TB, a.up.codes, a.up.scales, at, lane);
+        copy_tile<PER>(to + TB, codes + up_codes, scales + up_scales, lane);
       } else {
 #pragma unroll
-        for (int mt = 1; mt < MT; ++mt)  // a row tile past the last is read as the last
-          copy_tile<PER>(to + mt * TB, a.w.codes, a.w.scales, lrow + mt < a.w.rt ? at + (int64_t)mt * ct : at, lane);
+        for (int mt = 1; mt < MT; ++mt) {  // a row tile past the last is read as the last
+          const int64_t on = lrow + mt < a.w.rt ? (int64_t)mt * ct : 0;
+          copy_tile<PER>(to + mt * TB, codes + on * TILE_BYTES, scales + on * (TILE_ROWS * PER * 2), lane);
+        }
       }
-      lslot = lslot + 1 == AHEAD ? 0 : lslot + 1;
-      ++at;
+      to = to + SLOT == ring_end ? ring0 : to + SLOT;
+      codes += TILE_BYTES;
+      scales += TILE_ROWS * PER * 2;
       if (TILES > 1 && ++lkt == ct) {
         lkt = 0;
         lrow += TILES;
-        at += (int64_t)(TILES - 1) * ct;
+        codes += (int64_t)(TILES - 1) * ct * TILE_BYTES;
+        scales += (int64_t)(TILES - 1) * ct * (TILE_ROWS * PER * 2);
       }
     }
     cp_async_commit();
@@ -161,14 +171,12 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
     }
   };
 
-  float sum[MT][NT][4];
+  pair_t sum[MT][NT][2];
   auto clear = [&]() {
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[mt][nt][e] = 0.0f;
+      for (int nt = 0; nt < NT; ++nt) sum[mt][nt][0] = sum[mt][nt][1] = 0ull;
   };
   // this lane's sums as those of tokens
   auto whole = [&](int item) {
@@ -178,8 +186,9 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          const float* s = sum[mt][nt] + 2 * half;
-          const float* u = MODE == MODE_GATED ? sum[MT - 1][nt] + 2 * half : s;
+          float s[2], u[2];
+          unpack_f2(sum[mt][nt][half], s[0], s[1]);
+          unpack_f2(sum[MODE == MODE_GATED ? MT - 1 : mt][nt][half], u[0], u[1]);
           const int r = 16 * mt + g + 8 * half;
           if constexpr (CPT == 1) {
 #pragma unroll
@@ -203,27 +212,34 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) to[(8 * nt + 2 * t + (e & 1)) * LD + 16 * mt + g + 8 * (e >> 1)] = sum[mt][nt][e];
+        for (int half = 0; half < 2; ++half) {
+          float s0, s1;
+          unpack_f2(sum[mt][nt][half], s0, s1);
+          to[(8 * nt + 2 * t) * LD + 16 * mt + g + 8 * half] = s0;
+          to[(8 * nt + 2 * t + 1) * LD + 16 * mt + g + 8 * half] = s1;
+        }
   };
 
-  int slot = 0;
+  const uint8_t* from = ring;  // of the next tile to multiply
   for (int i = i0;;) {
     tokens();
     clear();
     int item = now.q0 / ct, kt = now.q0 - item * ct;
     const int first = item;
     bool cut = kt > 0;  // whether the item began in the warp before
+    const uint8_t* stage = w4_smem + kt * STAGE;
 #pragma unroll 1
-    for (int q = now.q0; q < now.q1; ++q) {
+    for (int q = now.q1 - now.q0; q > 0; --q) {
       cp_async_wait<AHEAD - 1>();
       __syncwarp();  // every lane's part of the tile is there
       Tile<PER> tile[MT];
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) read_tile<PER>(tile[mt], ring + slot * SLOT + mt * TB, lane);
-      multiply<T, MT, NT, PER>(tile, w4_smem + kt * STAGE, sum, lane);
+      for (int mt = 0; mt < MT; ++mt) read_tile<PER>(tile[mt], from + mt * TB, lane);
+      multiply<T, MT, NT, PER>(tile, stage, sum, lane);
       __syncwarp();  // and read
       load();
-      slot = slot + 1 == AHEAD ? 0 : slot + 1;
+      from = from + SLOT == ring + AHEAD * SLOT ? ring : from + SLOT;
+      stage += STAGE;
       if (++kt == ct) {
         if (cut)
           fragment(0);
@@ -232,6 +248,7 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
         clear();
         cut = false;
         kt = 0;
+        stage = w4_smem;
         ++item;
       }
     }

@@ -160,13 +160,14 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ R
     if (i < n) next_tokens();
     cp_async_commit();
   }
-  float sum[MT][NT][4];
+  pair_t sum[MT][NT][2];
+  auto clear = [&]() {
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt)
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[mt][nt][e] = 0.0f;
+      for (int nt = 0; nt < NT; ++nt) sum[mt][nt][0] = sum[mt][nt][1] = 0ull;
+  };
+  clear();
 
   // what becomes of a finished sum of row r (of the item's row tile) and token tok: gate's and up's, or one of the MT tiles'
   auto finish = [&](const Item& it, int rt, int r, int tok, float v, float w) {
@@ -192,8 +193,9 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ R
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const float* s = sum[mt][nt] + 2 * half;
-        const float* u = GATED ? sum[MT - 1][nt] + 2 * half : s;
+        float s[2], u[2];
+        unpack_f2(sum[mt][nt][half], s[0], s[1]);
+        unpack_f2(sum[GATED ? MT - 1 : mt][nt][half], u[0], u[1]);
         if constexpr (CPT == 1) {
 #pragma unroll
           for (int e = 0; e < 2; ++e)
@@ -224,12 +226,7 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ R
 #pragma unroll
         for (int mt = 0; mt < (GATED ? 1 : MT); ++mt)
           each(now, mt, [&](int r, int tok, float v, float w) { finish(now, now.rt + mt, r, tok, v, w); });
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sum[mt][nt][e] = 0.0f;
+        clear();
         if (++i0 < i1) now = item_at(i0);
       }
     }

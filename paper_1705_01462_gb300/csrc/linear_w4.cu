@@ -116,14 +116,13 @@ fgq_status launch_few(RowsArgs a, bool early, cudaStream_t s) {
   const int tokens = 8 * nt / cpt;
   const int64_t tiles = ((int64_t)a.P + tokens - 1) / tokens;
   if (nt <= 2) {  // one tile of tokens: held in shared memory where it fits
-    const int mt = nt == 1 && a.w.rt >= 40 * device_sms() ? 2 : 1;
-    const ResidentPlan plan = plan_held(nt, mt, a.w.ct, a.w.per);
+    const ResidentPlan plan = plan_held(nt, a.w.ct, a.w.per);
     if (plan.warps > 0) {
       ResidentArgs r = {};
       r.w = a.w, r.x = a.x, r.bias = a.bias, r.y = a.y, r.P = a.P, r.M = a.M, r.ytype = a.ytype, r.early = early;
-      r.items = (a.w.rt + mt - 1) / mt;
-      if (a.ytype == FGQ_F32) return launch_held_f32(r, nt, mt, plan, early, s);
-      return a.ytype == FGQ_BF16 ? launch_held_bf16(r, nt, mt, plan, early, s) : launch_held_f16(r, nt, mt, plan, early, s);
+      r.items = a.w.rt;
+      if (a.ytype == FGQ_F32) return launch_held_f32(r, nt, plan, early, s);
+      return a.ytype == FGQ_BF16 ? launch_held_bf16(r, nt, plan, early, s) : launch_held_f16(r, nt, plan, early, s);
     }
   }
   // two row tiles a warp where that leaves two blocks an SM

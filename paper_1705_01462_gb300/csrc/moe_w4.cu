@@ -33,6 +33,7 @@ struct RouteArgs {
   Unit* units;
   Choice* choices;
   int32_t* places;
+  unsigned* tops;
   int* nunits;
   int P, K, E, top, score, renormalize;
   float scale;
@@ -55,6 +56,30 @@ __device__ __forceinline__ float of_order(uint32_t o) { return __uint_as_float(o
 // A cluster of eight blocks takes four tokens: its 128 warps share the experts, `ks` of them each expert's row, and leave
 // the logits, as ordered pairs of fp32, in the first block's shared memory; there a warp a token takes the largest one by one.
 constexpr int RT_WARPS = 16, RT_CLUSTER = 8, RT_TOKENS = 4;
+
+// Eight elements as loaded, where the source has the load: the compiler may not move it to its use.
+template <typename T>
+struct Ahead8 {
+  uint4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i)
+      asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w)
+                   : "l"(reinterpret_cast<const uint4*>(p) + i));
+  }
+  __device__ __forceinline__ void unpack(float (&x)[8]) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        x[4 * i] = __uint_as_float(v[i].x), x[4 * i + 1] = __uint_as_float(v[i].y);
+        x[4 * i + 2] = __uint_as_float(v[i].z), x[4 * i + 3] = __uint_as_float(v[i].w);
+      }
+    } else {
+      unpack8(v[0], x, T());
+    }
+  }
+};
 
 // TOKENS of a cluster; VEC: 16-byte pieces of aligned rows.
 template <typename T, typename R, int TOKENS, bool VEC>
@@ -86,31 +111,30 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
         for (int j = 1; j < 8; ++j) s = fmaf(v[j], w[j], s);
         add_pair(hi[i], lo[i], s, 0.0f);
       };
-      if constexpr (VEC) {  // the next step's loads, all at once, ahead of a step's sums
-        Raw8<R> wn, wc;
-        Raw8<T> xn[TOKENS], xc[TOKENS];
-        auto fetch = [&](int k) {
-          if (k < a.K) {
-            wn.load(wr + k);
-#pragma unroll
-            for (int i = 0; i < TOKENS; ++i) xn[i].load(row[i] + k);
-          }
-        };
+      if constexpr (VEC) {  // BATCH steps' loads at once
+        constexpr int BATCH = sizeof(T) == 4 || sizeof(R) == 4 ? 2 : 4;
         const int step = 256 * ks;
-        int k = 8 * (lane + 32 * kpart);
-        fetch(k);
-        for (; k < a.K; k += step) {
-          wc = wn;
+        for (int k0 = 8 * (lane + 32 * kpart); k0 < a.K; k0 += BATCH * step) {
+          Ahead8<R> wc[BATCH];
+          Ahead8<T> xc[BATCH][TOKENS];
 #pragma unroll
-          for (int i = 0; i < TOKENS; ++i) xc[i] = xn[i];
-          fetch(k + step);
-          float w[8];
-          wc.unpack(w);
+          for (int b = 0; b < BATCH; ++b) {
+            const int k = min(k0 + b * step, a.K - 8);  // past the row: its last again, left out below
+            wc[b].load(wr + k);
 #pragma unroll
-          for (int i = 0; i < TOKENS; ++i) {
-            float v[8];
-            xc[i].unpack(v);
-            add(i, v, w);
+            for (int i = 0; i < TOKENS; ++i) xc[b][i].load(row[i] + k);
+          }
+#pragma unroll
+          for (int b = 0; b < BATCH; ++b) {
+            if (k0 + b * step >= a.K) break;
+            float w[8];
+            wc[b].unpack(w);
+#pragma unroll
+            for (int i = 0; i < TOKENS; ++i) {
+              float v[8];
+              xc[b][i].unpack(v);
+              add(i, v, w);
+            }
           }
         }
       } else {
@@ -180,15 +204,12 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
           id = e;
         }
       }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        const unsigned long long k2 = __shfl_xor_sync(FULL_MASK, k, o);
-        const int id2 = __shfl_xor_sync(FULL_MASK, id, o);
-        if (k2 > k || (k2 == k && id2 < id)) {
-          k = k2;
-          id = id2;
-        }
-      }
+      // the largest upper half, of those lanes the largest lower half, of those the lowest index
+      const unsigned h = __reduce_max_sync(FULL_MASK, (unsigned)(k >> 32));
+      const bool in = (unsigned)(k >> 32) == h;
+      const unsigned l = __reduce_max_sync(FULL_MASK, in ? (unsigned)k : 0u);
+      id = (int)__reduce_min_sync(FULL_MASK, in && (unsigned)k == l ? (unsigned)id : 0x7fffffffu);
+      k = (unsigned long long)h << 32 | l;
       if ((id & 31) == lane) taken |= 1u << (id >> 5);
       if (j == 0) best_h = of_order((uint32_t)(k >> 32)), best_l = of_order((uint32_t)k);
       const float f = a.score == FGQ_SCORE_SOFTMAX ? expf(value(k)) : 1.0f / (1.0f + expf(-of_order((uint32_t)(k >> 32))));
@@ -236,6 +257,7 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
   if (c < n) {
     a.choices[place] = {c / a.top, chosen_w[c]};
     a.places[c] = place;
+    a.tops[c] = 0u;
     if (lead) {
       int u = 0;
       for (int j = 0; j < n; ++j) u += ahead[j] && chosen[j] < e;
@@ -254,31 +276,10 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
 // ------------------------------------------------------------------ choices by expert
 constexpr int GR_THREADS = 1024;
 
-// Sum of the values of the threads before this one; `total`: of all.
-__device__ __forceinline__ int block_scan(int v, int* warp_sums, int& total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int s = v;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(FULL_MASK, s, o);
-    if (lane >= o) s += u;
-  }
-  __syncthreads();  // the sums of the scan before have been read
-  if (lane == 31) warp_sums[warp] = s;
-  __syncthreads();
-  int before = 0;
-  total = 0;
-  for (int i = 0; i < GR_THREADS / 32; ++i) {
-    const int u = warp_sums[i];
-    before += i < warp ? u : 0;
-    total += u;
-  }
-  return before + s - v;
-}
-
 __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, const float* weights, int A, int top, int E, int cap,
-                                                           Unit* units, Choice* choices, int32_t* places, int* nunits) {
+                                                           Unit* units, Choice* choices, int32_t* places, unsigned* tops, int* nunits) {
   __shared__ int count[MAX_EXPERTS], start[MAX_EXPERTS], id[CHUNK * MAX_TOP], warp_sums[GR_THREADS / 32];
+  __shared__ float weight[CHUNK * MAX_TOP];
   pdl_trigger();
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   count[t] = 0;
@@ -287,19 +288,35 @@ __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, c
   for (int i = t; i < A; i += GR_THREADS) {
     const int e = __ldcg(ids + i);
     id[i] = e;
+    weight[i] = __ldcg(weights + i);
+    tops[i] = 0u;
     if (e >= 0 && e < E)
       atomicAdd(&count[e], 1);
     else
       places[i] = -1;
   }
   __syncthreads();
-  const int n = count[t];  // 0 from E on
-  int total;
-  const int first = block_scan(n, warp_sums, total);
-  const int u0 = block_scan((n + cap - 1) / cap, warp_sums, total);
+  // choices and units before expert t, both in one word: at most 4096 each
+  const int n = count[t], mine = n | (n + cap - 1) / cap << 16;  // 0 from E on
+  int s = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int u = __shfl_up_sync(FULL_MASK, s, o);
+    if (lane >= o) s += u;
+  }
+  if (lane == 31) warp_sums[warp] = s;
+  __syncthreads();
+  int before = lane < warp ? warp_sums[lane] : 0, total = warp_sums[lane];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    before += __shfl_xor_sync(FULL_MASK, before, o);
+    total += __shfl_xor_sync(FULL_MASK, total, o);
+  }
+  before += s - mine;
+  const int first = before & 0xffff, u0 = before >> 16;
   start[t] = first;
   for (int u = 0; u * cap < n; ++u) units[u0 + u] = {t, first + u * cap, min(cap, n - u * cap), 0};
-  if (t == 0) *nunits = total;
+  if (t == 0) *nunits = total >> 16;
   __syncthreads();
   for (int e = warp; e < E; e += GR_THREADS / 32) {  // each expert's choices in the order they came
     const int want = count[e];
@@ -309,7 +326,7 @@ __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, c
       const unsigned m = __ballot_sync(FULL_MASK, hit);
       if (hit) {
         const int place = at + __popc(m & ((1u << lane) - 1u));
-        choices[place] = {(i + lane) / top, __ldcg(weights + i + lane)};
+        choices[place] = {(i + lane) / top, weight[i + lane]};
         places[i + lane] = place;
       }
       at += __popc(m);
@@ -496,23 +513,29 @@ __global__ void __launch_bounds__(THREADS) down_kernel(const __grid_constant__ D
 template <int V>
 __global__ void __launch_bounds__(256) combine_kernel(const float* z, const int32_t* places, const float* weights, int top, int K, void* y,
                                                       int ytype) {
+  __shared__ int at[MAX_TOP];
+  __shared__ float by[MAX_TOP];
   const int p = blockIdx.y, m = ((int)blockIdx.x * 256 + (int)threadIdx.x) * V;
+  // these are of kernels before the one that this one waits for
+  if ((int)threadIdx.x < top) {
+    at[threadIdx.x] = __ldcg(places + p * top + threadIdx.x);
+    by[threadIdx.x] = __ldcg(weights + p * top + threadIdx.x);
+  }
+  __syncthreads();
   pdl_wait();
   if (m >= K) return;
   float v[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) v[i] = 0.0f;
-#pragma unroll 4
+#pragma unroll 8
   for (int j = 0; j < top; ++j) {
-    const int at = __ldcg(places + p * top + j);
-    const float w = __ldcg(weights + p * top + j);
-    if (at < 0) continue;
-    const float* row = z + (int64_t)at * K + m;
+    if (at[j] < 0) continue;  // the same for the whole block
+    const float* row = z + (int64_t)at[j] * K + m;
     if constexpr (V == 4) {
       const float4 f = __ldcg(reinterpret_cast<const float4*>(row));
-      v[0] = fmaf(w, f.x, v[0]), v[1] = fmaf(w, f.y, v[1]), v[2] = fmaf(w, f.z, v[2]), v[3] = fmaf(w, f.w, v[3]);
+      v[0] = fmaf(by[j], f.x, v[0]), v[1] = fmaf(by[j], f.y, v[1]), v[2] = fmaf(by[j], f.z, v[2]), v[3] = fmaf(by[j], f.w, v[3]);
     } else {
-      v[0] = fmaf(w, __ldcg(row), v[0]);
+      v[0] = fmaf(by[j], __ldcg(row), v[0]);
     }
   }
 #pragma unroll
@@ -614,15 +637,15 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   // tokens held in shared memory where units of 8 (fp32: 4) do and they fit
   const int ctk = col_tiles(K), ctf = col_tiles(F);
   const ResidentPlan hp = type == FGQ_F32 ? plan_resident<2, 2, GATED_AHEAD>(ctk, 128 / gate->group) : plan_resident<2, 1, GATED_AHEAD>(ctk, 128 / gate->group);
-  const ResidentPlan dp = plan_resident<1, 2, HELD_AHEAD1>(ctf, 128 / down->group);
+  const ResidentPlan dp = plan_held(type == FGQ_BF16 ? 1 : 2, ctf, 128 / down->group);
   const bool held = hp.warps > 0 && dp.warps > 0 && (type == FGQ_F32 ? A <= 4ll * E : A <= 8ll * E);
   const int cap = held && type == FGQ_F32 ? 4 : unit_tokens(type, A, E);
   const int most_units = (A < E || P == 1 ? A : E) + A / cap;
-  const size_t b_x = direct ? 0 : up256(copied_bytes(type, pass, K)), b_h = up256((size_t)A * hparts * hpitch * 2);
+  const size_t b_x = direct ? 0 : up256(copied_bytes(type, pass, K)), b_h = up256((size_t)A * hpitch * (held ? 4 : 2 * hparts));
   const size_t b_units = up256(sizeof(Unit) * most_units), b_choices = up256(sizeof(Choice) * (size_t)A), b_n = 256;
-  const size_t b_places = up256(4 * (size_t)A), b_z = held ? up256(4 * (size_t)A * K) : 0;
+  const size_t b_places = up256(4 * (size_t)A), b_tops = b_places, b_z = held ? up256(4 * (size_t)A * K) : 0;
   const size_t b_ids = route ? up256(4 * (size_t)A) : 0;
-  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(b_x + b_h + b_units + b_choices + b_n + b_places + b_z + 2 * b_ids, s));
+  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(b_x + b_h + b_units + b_choices + b_n + b_places + b_tops + b_z + 2 * b_ids, s));
   if (!tmp) return FGQ_ERR_CUDA;
   uint8_t* at = tmp;
   auto take = [&](size_t n) {
@@ -636,6 +659,7 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   Choice* choices = reinterpret_cast<Choice*>(take(b_choices));
   int* nunits = reinterpret_cast<int*>(take(b_n));
   int32_t* places = reinterpret_cast<int32_t*>(take(b_places));
+  unsigned* tops = reinterpret_cast<unsigned*>(take(b_tops));
   float* z = reinterpret_cast<float*>(take(b_z));
   int32_t* own_ids = reinterpret_cast<int32_t*>(take(b_ids));
   float* own_weights = reinterpret_cast<float*>(take(b_ids));
@@ -655,16 +679,16 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
     const float* pw = weights ? weights + (int64_t)p0 * top : own_weights;
     const bool one = route && np <= RT_TOKENS;  // a cluster's tokens: it leaves units and choices itself
     if (route) {
-      const RouteArgs ra = {xp, route->router, ldx, own_ids, own_weights, one ? units : nullptr, choices, places, nunits, np, K, E, top,
+      const RouteArgs ra = {xp, route->router, ldx, own_ids, own_weights, one ? units : nullptr, choices, places, tops, nunits, np, K, E, top,
                             route->score, route->renormalize, route->scale};
       st = launch_route(ra, type, route->rtype, s);
       if (st != FGQ_OK) break;
     }
     if (!one) {
       if (route) {
-        st = launch_chained(group_kernel, dim3(1), GR_THREADS, 0, 1, s, pid, pw, na, top, E, cap, units, choices, places, nunits);
+        st = launch_chained(group_kernel, dim3(1), GR_THREADS, 0, 1, s, pid, pw, na, top, E, cap, units, choices, places, tops, nunits);
       } else {  // the kernel before is the caller's, or the copy
-        group_kernel<<<1, GR_THREADS, 0, s>>>(pid, pw, na, top, E, cap, units, choices, places, nunits);
+        group_kernel<<<1, GR_THREADS, 0, s>>>(pid, pw, na, top, E, cap, units, choices, places, tops, nunits);
         st = after_launch();
       }
       if (st != FGQ_OK) break;
@@ -678,13 +702,14 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
         break;
       }
       ResidentArgs ra = {};
-      ra.w = mg, ra.up = mu, ra.x = rows, ra.M = F, ra.units = units, ra.choices = choices, ra.nunits = nunits, ra.h = h, ra.hpitch = hpitch, ra.one = np == 1;
+      ra.w = mg, ra.up = mu, ra.x = rows, ra.M = F, ra.units = units, ra.choices = choices, ra.nunits = nunits;
+      ra.h = reinterpret_cast<float*>(h), ra.hpitch = hpitch, ra.top = tops, ra.one = np == 1;
       st = type == FGQ_F32 ? launch_held_gated_f32(ra, hp, hi, s)
                            : (type == FGQ_BF16 ? launch_held_gated_bf16(ra, hp, hi, s) : launch_held_gated_f16(ra, hp, hi, s));
       if (st != FGQ_OK) break;
-      ra.w = md, ra.x = {h, hparts * hpitch, (int)hpitch}, ra.M = K, ra.z = z;
-      st = type == FGQ_F32 ? launch_held_per<__nv_bfloat16, 1, 2, 3, MODE_DOWN, 1, HELD_AHEAD1>(ra, dp, di, true, s)
-                           : launch_held_per<__nv_bfloat16, 1, 2, 2, MODE_DOWN, 1, HELD_AHEAD1>(ra, dp, di, true, s);
+      ra.w = md, ra.M = K, ra.z = z;
+      st = type == FGQ_F32 ? launch_held_down_f32(ra, dp, di, s)
+                           : (type == FGQ_BF16 ? launch_held_down_bf16(ra, dp, di, s) : launch_held_down_f16(ra, dp, di, s));
       if (st != FGQ_OK) break;
       const bool four = K % 4 == 0;
       const dim3 cg((unsigned)((K + (four ? 1023 : 255)) / (four ? 1024 : 256)), (unsigned)np);
@@ -763,7 +788,7 @@ fgq_status fgq_route_tokens(const void* x, fgq_float_type type, int P, int K, in
   if (st != FGQ_OK || P == 0) return st;
   if (!ids || !weights) return FGQ_ERR_ARG;
   if (!aligned(ids, 4) || !aligned(weights, 4)) return FGQ_ERR_ALIGN;
-  return launch_route({x, router, P > 1 ? ldx : 0, ids, weights, nullptr, nullptr, nullptr, nullptr, P, K, E, top, score, renormalize, scale},
+  return launch_route({x, router, P > 1 ? ldx : 0, ids, weights, nullptr, nullptr, nullptr, nullptr, nullptr, P, K, E, top, score, renormalize, scale},
                       type, rtype, stream);
 }
 

@@ -16,31 +16,32 @@ fgq_status launch_gated_f16(const RowsArgs& a, int nt, unsigned grid, cudaStream
 fgq_status launch_gated_f32(const RowsArgs& a, unsigned grid, cudaStream_t s);
 
 // The same with tokens held in shared memory: up to 8 nt columns (nt 1 or 2), where plan_resident finds room for them.
-fgq_status launch_held_bf16(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s);
-fgq_status launch_held_f16(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s);
-fgq_status launch_held_f32(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s);
-// Gate and up, `items` at most: 8 tokens a unit (fp32: 4).
+fgq_status launch_held_bf16(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s);
+fgq_status launch_held_f16(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s);
+fgq_status launch_held_f32(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s);
+// Gate and up, and down, `items` at most: 8 tokens a unit (fp32: 4).
 fgq_status launch_held_gated_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
 fgq_status launch_held_gated_f16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
 fgq_status launch_held_gated_f32(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
+fgq_status launch_held_down_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
+fgq_status launch_held_down_f16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
+fgq_status launch_held_down_f32(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
 
-template <typename T, int MT, int NT, int PARTS, int MODE, int HPARTS, int AHEAD>
+template <typename T, int MT, int NT, int PARTS, int MODE, int AHEAD>
 fgq_status launch_held_per(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, bool chained, cudaStream_t s) {
-  if (a.w.per == 4) return launch_resident<T, MT, NT, 4, PARTS, MODE, HPARTS, AHEAD>(a, plan, items, chained, s);
-  if (a.w.per == 2) return launch_resident<T, MT, NT, 2, PARTS, MODE, HPARTS, AHEAD>(a, plan, items, chained, s);
-  return launch_resident<T, MT, NT, 1, PARTS, MODE, HPARTS, AHEAD>(a, plan, items, chained, s);
+  if (a.w.per == 4) return launch_resident<T, MT, NT, 4, PARTS, MODE, AHEAD>(a, plan, items, chained, s);
+  if (a.w.per == 2) return launch_resident<T, MT, NT, 2, PARTS, MODE, AHEAD>(a, plan, items, chained, s);
+  return launch_resident<T, MT, NT, 1, PARTS, MODE, AHEAD>(a, plan, items, chained, s);
 }
-// Tiles under way of a warp: 4 KB, or 2 to 4 pairs.
-constexpr int HELD_AHEAD1 = 4, HELD_AHEAD2 = 2, GATED_AHEAD = 2;
-inline ResidentPlan plan_held(int nt, int mt, int ct, int per) {
-  if (nt == 1) return mt == 2 ? plan_resident<2, 1, HELD_AHEAD2>(ct, per) : plan_resident<1, 1, HELD_AHEAD1>(ct, per);
-  return plan_resident<1, 2, HELD_AHEAD1>(ct, per);
+// Tiles under way of a warp: four, or two pairs.
+constexpr int HELD_AHEAD = 4, GATED_AHEAD = 2;
+inline ResidentPlan plan_held(int nt, int ct, int per) {
+  return nt == 1 ? plan_resident<1, 1, HELD_AHEAD>(ct, per) : plan_resident<1, 2, HELD_AHEAD>(ct, per);
 }
 template <typename T, int PARTS>
-fgq_status launch_held_type(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
-  if (nt == 1 && mt == 2) return launch_held_per<T, 2, 1, PARTS, MODE_LINEAR, 1, HELD_AHEAD2>(a, plan, a.items, chained, s);
-  if (nt == 1) return launch_held_per<T, 1, 1, PARTS, MODE_LINEAR, 1, HELD_AHEAD1>(a, plan, a.items, chained, s);
-  return launch_held_per<T, 1, 2, PARTS, MODE_LINEAR, 1, HELD_AHEAD1>(a, plan, a.items, chained, s);
+fgq_status launch_held_type(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
+  if (nt == 1) return launch_held_per<T, 1, 1, PARTS, MODE_LINEAR, HELD_AHEAD>(a, plan, a.items, chained, s);
+  return launch_held_per<T, 1, 2, PARTS, MODE_LINEAR, HELD_AHEAD>(a, plan, a.items, chained, s);
 }
 
 template <typename T, int MT, int NT, int PARTS, bool GATED, int HPARTS, int AHEAD>

@@ -26,22 +26,27 @@ struct ResidentArgs {
   const Unit* units;
   const Choice* choices;
   const int* nunits;
-  uint16_t* h;  // MODE_GATED: out, [choice][parts][hpitch]
+  float* h;     // [choice][hpitch]: MODE_GATED out, MODE_DOWN in
   int64_t hpitch;
+  unsigned* top;  // [choice]: the largest magnitude of its h, as fp32 bits (zeros before MODE_GATED)
   float* z;  // MODE_DOWN: out, [choice][M]
   int one;    // MODE_GATED: there is one token
   int early;  // the kernel before is this library's: weights may be loaded while it runs
 };
 
-constexpr int RES_MAX_WARPS = 24, RES_SMEM = 226 * 1024;  // a kilobyte is left for what is not dynamic
+constexpr int RES_SMEM = 226 * 1024;  // a kilobyte is left for what is not dynamic
+// Warps of a block at most: 80 registers a thread, or 96 where two row tiles meet 16 columns.
+constexpr int resident_warps(int mt, int nt) { return mt * nt >= 4 ? 20 : 24; }
 
-template <typename T, int MT, int NT, int PER, int PARTS, int MODE, int HPARTS, int AHEAD>
-__global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __grid_constant__ ResidentArgs a) {
+template <typename T, int MT, int NT, int PER, int PARTS, int MODE, int AHEAD>
+__global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(const __grid_constant__ ResidentArgs a) {
   constexpr int CPT = columns_per_token(PARTS), TOKENS = 8 * NT / CPT, COLS = 8 * NT, STAGE = COLS * 256;
   constexpr int TILES = MODE == MODE_GATED ? 1 : MT;  // row tiles of an item
   constexpr int LD = 16 * MT + 1, FRAGMENT = COLS * LD, TB = tile_bytes<PER>(), SLOT = MT * TB;
   extern __shared__ __align__(16) uint8_t w4_smem[];
-  __shared__ int row_of[TOKENS];
+  __shared__ int row_of[TOKENS];    // MODE_GATED: the tokens' rows
+  __shared__ float back[TOKENS];    // MODE_DOWN: what the tokens' scales are undone by
+  __shared__ unsigned tops[TOKENS];  // MODE_GATED: the tokens' largest hidden values in this block
   const int W = (int)blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int ct = a.w.ct;
   uint8_t* ring = w4_smem + ct * STAGE + warp * AHEAD * SLOT;
@@ -90,8 +95,7 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
   const int64_t up_codes = MODE == MODE_GATED ? a.up.codes - a.w.codes : 0;
   const int64_t up_scales = MODE == MODE_GATED ? reinterpret_cast<const uint8_t*>(a.up.scales) - reinterpret_cast<const uint8_t*>(a.w.scales) : 0;
   int lkt = 0, lrow = 0, left = 0;
-  const uint32_t ring0 = ring_at + 16 * lane, ring_end = ring0 + AHEAD * SLOT;
-  uint32_t to = ring0;
+  const uint32_t ring0 = ring_at + 16 * lane;
   auto begin = [&](const Segment& s) {
     const int i = s.q0 / ct;
     lkt = s.q0 - i * ct;
@@ -101,7 +105,8 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
     scales = reinterpret_cast<const uint8_t*>(a.w.scales) + at * (TILE_ROWS * PER * 2) + 16 * lane;
     left = s.q1 - s.q0;
   };
-  auto load = [&]() {
+  auto load = [&](int slot) {
+    const uint32_t to = ring0 + slot * SLOT;
     if (left > 0) {
       --left;
       copy_tile<PER>(to, codes, scales, lane);
@@ -114,7 +119,6 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
           copy_tile<PER>(to + mt * TB, codes + on * TILE_BYTES, scales + on * (TILE_ROWS * PER * 2), lane);
         }
       }
-      to = to + SLOT == ring_end ? ring0 : to + SLOT;
       codes += TILE_BYTES;
       scales += TILE_ROWS * PER * 2;
       if (TILES > 1 && ++lkt == ct) {
@@ -129,13 +133,60 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
   Segment now = segment_at(i0);
   begin(now);
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i) load();
+  for (int i = 0; i < AHEAD; ++i) load(i);
   if (MODE == MODE_DOWN || (MODE == MODE_LINEAR && a.early)) pdl_wait();
 
   const uint8_t* xb = static_cast<const uint8_t*>(a.x.data);
   const uint32_t xs = smem_u32(w4_smem);
   // the segment's columns, 16 bytes a thread and turn; columns of no token are left as they are: nothing reads their sums
   auto tokens = [&]() {
+    if constexpr (MODE == MODE_DOWN) {
+      // fp32 values in fp16 parts (fp32 outputs: bf16 ones, which need no scale), after a power of two that takes the token's largest
+      // to 2^14: one part is within 2^-12 (bf16 outputs), two within 2^-23 (fp16 ones), three exact
+      const int pieces = ct * 16, n = pieces * now.u.z;
+      for (int i = threadIdx.x; i < n; i += 32 * W) {
+        const int tok = i / pieces, j = i - tok * pieces, k = 8 * j;
+        float v[8], up = 1.0f, up2 = 1.0f;
+        if (PARTS < 3) {
+          const unsigned big = __ldcg(a.top + now.u.y + tok);
+          const int e = max((int)(big >> 23) - 127, -126);
+          up = pow2f((14 - e) / 2), up2 = pow2f((14 - e) - (14 - e) / 2);  // past fp32's largest for tiny ones
+          if (j == 0) back[tok] = e == 128 ? 1.0f : pow2f(e - 14);
+          if (e == 128) up = up2 = 1.0f;  // NaN or infinity
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+          if (k < a.hpitch) f = __ldcg(reinterpret_cast<const float4*>(a.h + (now.u.y + tok) * a.hpitch + k) + h);
+          v[4 * h] = f.x, v[4 * h + 1] = f.y, v[4 * h + 2] = f.z, v[4 * h + 3] = f.w;
+        }
+        uint32_t w[3][4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          if constexpr (PARTS == 3) {
+            uint16_t p[3], q[3];
+            three_parts(v[2 * h], p);
+            three_parts(v[2 * h + 1], q);
+#pragma unroll
+            for (int c = 0; c < 3; ++c) w[c][h] = p[c] | (uint32_t)q[c] << 16;
+          } else {
+            const float x0 = v[2 * h] * up * up2, x1 = v[2 * h + 1] * up * up2;
+            w[0][h] = pack2(x0, x1, __half());
+            if constexpr (PARTS == 2) {
+              const float2 r = unpack2(w[0][h], __half());
+              w[1][h] = pack2(x0 - r.x, x1 - r.y, __half());
+            }
+          }
+        }
+#pragma unroll
+        for (int c = 0; c < CPT; ++c)
+          *reinterpret_cast<uint4*>(w4_smem + (j >> 4) * STAGE + chunk_at(tok * CPT + c, j & 15)) =
+              c < PARTS ? make_uint4(w[c < PARTS ? c : 0][0], w[c < PARTS ? c : 0][1], w[c < PARTS ? c : 0][2], w[c < PARTS ? c : 0][3])
+                        : make_uint4(0u, 0u, 0u, 0u);
+      }
+      __syncthreads();
+      return;
+    }
     if (MODE == MODE_GATED && !a.one) {
       if (threadIdx.x < now.u.z) row_of[threadIdx.x] = __ldcg(&a.choices[now.u.y + threadIdx.x].token);
       __syncthreads();
@@ -143,7 +194,7 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
     const int cols = now.u.z * CPT, n = ct * 16 * cols;
     for (int i = threadIdx.x; i < n; i += 32 * W) {
       const int chunk = i & 15, j = i >> 4, kt = j / cols, c = j - kt * cols, tok = c / CPT, part = c % CPT, k = kt * TILE_COLS + 8 * chunk;
-      const int64_t row = MODE == MODE_LINEAR ? tok : (MODE == MODE_GATED ? (a.one ? 0 : row_of[tok]) : now.u.y + tok);
+      const int64_t row = MODE == MODE_LINEAR ? tok : (a.one ? 0 : row_of[tok]);
       const bool live = part < PARTS && k < a.x.kvalid;
       cp_async16(xs + kt * STAGE + chunk_at(c, chunk), live ? xb + 2 * (row * a.x.pitch + part * (a.x.pitch / PARTS) + k) : xb, live ? 16u : 0u);
     }
@@ -151,25 +202,31 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
     cp_async_wait<0>();
     __syncthreads();
   };
-  // what becomes of the finished sums of row r of an item and token tok: of gate and up, or of one matrix
+  // what becomes of the finished sums of row r of an item and token tok: of gate and up, or of one matrix.  MODE_GATED: the
+  // hidden value's magnitude
   auto finish = [&](int item, int r, int tok, float v, float u) {
     const int m = item * 16 * TILES + r;
     v *= Operand<T>::BACK;
     if (MODE == MODE_GATED) {
       u *= Operand<T>::BACK;
       const float f = m < a.M ? v / (1.0f + expf(-v)) * u : 0.0f;
-      uint16_t p[3];
-      hidden_parts<HPARTS>(f, p);
-      uint16_t* to = a.h + (int64_t)(now.u.y + tok) * HPARTS * a.hpitch + m;
-#pragma unroll
-      for (int part = 0; part < HPARTS; ++part) to[part * a.hpitch] = p[part];
-    } else if (m < a.M) {
+      a.h[(now.u.y + tok) * a.hpitch + m] = f;
+      return fabsf(f);
+    }
+    if (m < a.M) {
       if (MODE == MODE_DOWN)
-        a.z[(int64_t)(now.u.y + tok) * a.M + m] = v;
+        a.z[(int64_t)(now.u.y + tok) * a.M + m] = PARTS < 3 ? v * back[tok] : v;
       else
         store_typed(a.y, a.ytype, (int64_t)tok * a.M + m, v + (a.bias ? __ldg(a.bias + m) : 0.0f));
     }
+    return 0.0f;
   };
+  // a token's largest hidden value: of this lane's two tokens in registers, a segment long, then of the block, then of all (an
+  // atomic a warp and item took the hidden layer of 16 tokens from 48 to 86 us).  Magnitudes compare as whole numbers, NaN
+  // above all, and the order does not matter
+  constexpr bool TOPS = MODE == MODE_GATED && CPT == 1;
+  unsigned big[NT][2];
+  auto note = [&](int tok, float f) { atomicMax(tops + tok, __float_as_uint(f)); };
 
   pair_t sum[MT][NT][2];
   auto clear = [&]() {
@@ -183,7 +240,7 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
 #pragma unroll
     for (int mt = 0; mt < TILES; ++mt)
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           float s[2], u[2];
@@ -193,7 +250,7 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
           if constexpr (CPT == 1) {
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-              if (8 * nt + 2 * t + e < now.u.z) finish(item, r, 8 * nt + 2 * t + e, s[e], u[e]);
+              if (8 * nt + 2 * t + e < now.u.z) big[nt][e] = max(big[nt][e], __float_as_uint(finish(item, r, 8 * nt + 2 * t + e, s[e], u[e])));
           } else if constexpr (CPT == 2) {
             if (4 * nt + t < now.u.z) finish(item, r, 4 * nt + t, s[0] + s[1], u[0] + u[1]);
           } else {  // three parts, and a column that is zero
@@ -204,6 +261,7 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
             if ((t & 1) == 0 && tok < now.u.z) finish(item, r, tok, v, w);
           }
         }
+      }
   };
   auto fragment = [&](int slot) {
     float* to = sums + (2 * warp + slot) * FRAGMENT;
@@ -220,39 +278,57 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
         }
   };
 
-  const uint8_t* from = ring;  // of the next tile to multiply
   for (int i = i0;;) {
+    if (TOPS) {
+      if (threadIdx.x < TOKENS) tops[threadIdx.x] = 0u;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) big[nt][0] = big[nt][1] = 0u;
+    }
     tokens();
     clear();
     int item = now.q0 / ct, kt = now.q0 - item * ct;
     const int first = item;
     bool cut = kt > 0;  // whether the item began in the warp before
     const uint8_t* stage = w4_smem + kt * STAGE;
-#pragma unroll 1
-    for (int q = now.q1 - now.q0; q > 0; --q) {
-      cp_async_wait<AHEAD - 1>();
-      __syncwarp();  // every lane's part of the tile is there
-      Tile<PER> tile[MT];
+    for (int q = now.q1 - now.q0; q > 0;) {
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt) read_tile<PER>(tile[mt], from + mt * TB, lane);
-      multiply<T, MT, NT, PER>(tile, stage, sum, lane);
-      __syncwarp();  // and read
-      load();
-      from = from + SLOT == ring + AHEAD * SLOT ? ring : from + SLOT;
-      stage += STAGE;
-      if (++kt == ct) {
-        if (cut)
-          fragment(0);
-        else
-          whole(now.item + item);
-        clear();
-        cut = false;
-        kt = 0;
-        stage = w4_smem;
-        ++item;
+      for (int k = 0; k < AHEAD; ++k) {  // a segment begins with the ring's first tile
+        if (q == 0) break;
+        --q;
+        cp_async_wait<AHEAD - 1>();
+        __syncwarp();  // every lane's part of the tile is there
+        Tile<PER> tile[MT];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) read_tile<PER>(tile[mt], ring + k * SLOT + mt * TB, lane);
+        multiply<T, MT, NT, PER>(tile, stage, sum, lane);
+        __syncwarp();  // and read
+        load(k);
+        stage += STAGE;
+        if (++kt == ct) {
+          if (cut)
+            fragment(0);
+          else
+            whole(now.item + item);
+          clear();
+          cut = false;
+          kt = 0;
+          stage = w4_smem;
+          ++item;
+        }
       }
     }
     if (kt > 0 && now.q1 > now.q0) fragment(item == first ? 0 : 1);
+    if constexpr (TOPS) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int tok = 8 * nt + 2 * t + e;
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) big[nt][e] = max(big[nt][e], __shfl_xor_sync(FULL_MASK, big[nt][e], o));
+          if (g == 0 && tok < now.u.z) note(tok, __uint_as_float(big[nt][e]));
+        }
+    }
     // the next segment's first tiles
     i += now.count;
     Segment next = now;
@@ -260,7 +336,7 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
       next = segment_at(i);
       begin(next);
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) load();
+      for (int k = 0; k < AHEAD; ++k) load(k);
     }
     __syncthreads();
     // a cut item is put together by the first warp whose part begins inside it
@@ -280,8 +356,13 @@ __global__ void __launch_bounds__(32 * RES_MAX_WARPS) resident_kernel(const __gr
             if (MODE == MODE_GATED) u += from[part * LD + 16];
           }
         }
-        finish(now.item + it, r, tok, v, u);
+        const float f = finish(now.item + it, r, tok, v, u);
+        if (TOPS) note(tok, f);
       }
+    }
+    if (TOPS) {
+      __syncthreads();
+      if ((int)threadIdx.x < now.u.z) atomicMax(a.top + now.u.y + threadIdx.x, tops[threadIdx.x]);
     }
     if (i >= i1) break;
     __syncthreads();  // the parts are read, and the tokens
@@ -300,15 +381,15 @@ ResidentPlan plan_resident(int ct, int per) {
   const int tile = TILE_BYTES + TILE_ROWS * per * 2;
   const int each = AHEAD * MT * tile + 2 * 8 * NT * (16 * MT + 1) * 4;
   const int64_t room = (RES_SMEM - x) / each;
-  const int warps = room > RES_MAX_WARPS ? RES_MAX_WARPS : (int)room;
+  const int warps = room > resident_warps(MT, NT) ? resident_warps(MT, NT) : (int)room;
   if (warps < 8) return {0, 0};
   return {warps, (int)(x + (int64_t)warps * each)};
 }
 
-template <typename T, int MT, int NT, int PER, int PARTS, int MODE, int HPARTS, int AHEAD>
+template <typename T, int MT, int NT, int PER, int PARTS, int MODE, int AHEAD>
 fgq_status launch_resident(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, bool chained, cudaStream_t s) {
-  constexpr auto kernel = resident_kernel<T, MT, NT, PER, PARTS, MODE, HPARTS, AHEAD>;
-  if (!tc::smem_attr_once<resident_kernel<T, MT, NT, PER, PARTS, MODE, HPARTS, AHEAD>>(RES_SMEM)) return FGQ_ERR_CUDA;
+  constexpr auto kernel = resident_kernel<T, MT, NT, PER, PARTS, MODE, AHEAD>;
+  if (!tc::smem_attr_once<resident_kernel<T, MT, NT, PER, PARTS, MODE, AHEAD>>(RES_SMEM)) return FGQ_ERR_CUDA;
   const int64_t most = device_sms(), run = (items + most - 1) / most;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)((items + run - 1) / run));

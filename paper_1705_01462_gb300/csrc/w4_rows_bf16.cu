@@ -12,11 +12,14 @@ fgq_status launch_gated_bf16(const RowsArgs& a, int nt, unsigned grid, cudaStrea
   if (nt == 2) return launch_rows_per<__nv_bfloat16, 2, 2, 1, true, 2, 3>(a, grid, true, s);
   return launch_rows_per<__nv_bfloat16, 2, 4, 1, true, 2, 2>(a, grid, true, s);
 }
-fgq_status launch_held_bf16(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
-  return launch_held_type<__nv_bfloat16, 1>(a, nt, mt, plan, chained, s);
+fgq_status launch_held_bf16(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
+  return launch_held_type<__nv_bfloat16, 1>(a, nt, plan, chained, s);
 }
 fgq_status launch_held_gated_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
-  return launch_held_per<__nv_bfloat16, 2, 1, 1, MODE_GATED, 2, GATED_AHEAD>(a, plan, items, true, s);
+  return launch_held_per<__nv_bfloat16, 2, 1, 1, MODE_GATED, GATED_AHEAD>(a, plan, items, true, s);
+}
+fgq_status launch_held_down_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
+  return launch_held_per<__half, 1, 1, 1, MODE_DOWN, HELD_AHEAD>(a, plan, items, true, s);
 }
 
 }  // namespace w4

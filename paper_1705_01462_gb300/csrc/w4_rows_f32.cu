@@ -10,11 +10,14 @@ fgq_status launch_rows_f32(const RowsArgs& a, int nt, int mt, unsigned grid, boo
 fgq_status launch_gated_f32(const RowsArgs& a, unsigned grid, cudaStream_t s) {
   return launch_rows_per<__nv_bfloat16, 2, 4, 3, true, 3, 2>(a, grid, true, s);
 }
-fgq_status launch_held_f32(const ResidentArgs& a, int nt, int mt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
-  return launch_held_type<__nv_bfloat16, 3>(a, nt, mt, plan, chained, s);
+fgq_status launch_held_f32(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
+  return launch_held_type<__nv_bfloat16, 3>(a, nt, plan, chained, s);
 }
 fgq_status launch_held_gated_f32(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
-  return launch_held_per<__nv_bfloat16, 2, 2, 3, MODE_GATED, 3, GATED_AHEAD>(a, plan, items, true, s);
+  return launch_held_per<__nv_bfloat16, 2, 2, 3, MODE_GATED, GATED_AHEAD>(a, plan, items, true, s);
+}
+fgq_status launch_held_down_f32(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
+  return launch_held_per<__nv_bfloat16, 1, 2, 3, MODE_DOWN, HELD_AHEAD>(a, plan, items, true, s);
 }
 
 }  // namespace w4

@@ -230,7 +230,8 @@ def experts(x, ids, g, e_g, wg, wu, wd, G, Gd, dtype):
     P, K = x.shape
     E, F, _ = wg.shape
     y, e = np.zeros((P, K)), np.zeros((P, K))
-    held = 2.0 ** -17 if dtype != "f32" else u  # parts between the layers
+    # between the layers: bf16 tokens' values in 11 bits at least, half a step of them; fp16 ones' in two parts of 8 bits; fp32's exact
+    held = {"f32": u, "bf16": 2.0 ** -12, "f16": 2.0 ** -17}[dtype]
     for p in range(P):
         for j in range(ids.shape[1]):
             n = ids[p, j]
@@ -242,6 +243,8 @@ def experts(x, ids, g, e_g, wg, wu, wd, G, Gd, dtype):
             sig = 1 / (1 + np.exp(-a))
             h = a * sig * b
             eh = 1.1 * ea * (np.abs(b) + eb) + np.abs(a * sig) * eb + (held + 8 * u) * np.abs(h)
+            if dtype != "f32":  # values that fp16, scaled to a largest of 2^14, holds as subnormals: half their step
+                eh = eh + 2.0 ** -39 * np.abs(h).max()
             v = wd[n] @ h
             ev = np.abs(wd[n]) @ eh + beta(F, Gd) * (np.abs(wd[n]) @ np.abs(h))
             y[p] += g[p, j] * v

@@ -704,10 +704,11 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
       ResidentArgs ra = {};
       ra.w = mg, ra.up = mu, ra.x = rows, ra.M = F, ra.units = units, ra.choices = choices, ra.nunits = nunits;
       ra.h = reinterpret_cast<float*>(h), ra.hpitch = hpitch, ra.top = tops, ra.one = np == 1;
+      ra.items = one && np == 1 ? (int)hi : 0;  // one token picks distinct experts
       st = type == FGQ_F32 ? launch_held_gated_f32(ra, hp, hi, s)
                            : (type == FGQ_BF16 ? launch_held_gated_bf16(ra, hp, hi, s) : launch_held_gated_f16(ra, hp, hi, s));
       if (st != FGQ_OK) break;
-      ra.w = md, ra.M = K, ra.z = z;
+      ra.w = md, ra.M = K, ra.z = z, ra.items = ra.items ? (int)di : 0;
       st = type == FGQ_F32 ? launch_held_down_f32(ra, dp, di, s)
                            : (type == FGQ_BF16 ? launch_held_down_bf16(ra, dp, di, s) : launch_held_down_f16(ra, dp, di, s));
       if (st != FGQ_OK) break;

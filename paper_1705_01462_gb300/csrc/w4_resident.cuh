@@ -18,10 +18,11 @@ enum { MODE_LINEAR = 0, MODE_GATED = 1, MODE_DOWN = 2 };
 struct ResidentArgs {
   Matrix w, up;  // up: of a gated layer
   TokenRows x;
+  int items;  // where the host knows how many there are (MODE_LINEAR: it does), or 0
   // MODE_LINEAR
   const float* bias;
   void* y;
-  int P, M, ytype, items;
+  int P, M, ytype;
   // the experts: items (unit, rows)
   const Unit* units;
   const Choice* choices;
@@ -59,7 +60,7 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
     pdl_trigger();
   }
   const int groups = (a.w.rt + TILES - 1) / TILES;  // items of a unit
-  const int items = MODE == MODE_LINEAR ? a.items : __ldcg(a.nunits) * groups;
+  const int items = MODE == MODE_LINEAR || a.items > 0 ? a.items : __ldcg(a.nunits) * groups;
   const int run = (items + (int)gridDim.x - 1) / (int)gridDim.x;
   const int i0 = (int)blockIdx.x * run, i1 = min(i0 + run, items);
   if (i0 >= i1) return;

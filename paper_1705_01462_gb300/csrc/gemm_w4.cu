@@ -1,0 +1,350 @@
+// Many tokens with 4-bit weights on the tensor cores (tcgen05).
+//
+// y[p][m] = 2^(ex_p + ew_m) sum_k x'[p][k] w'[m][k] + bias[m], with w' = w 2^-ew_m and x' = x 2^-ex_p in fp16: a code times its scale has
+// 11 bits and is exact there, down to 2^-26 of its row's largest scale.  The weights stay in 4 bits in memory, and the block's
+// warps turn the 128 channels x 128 columns of a stage into the operand, in the shared memory that the MMA reads.  (Expanded
+// in memory first, 4096 -> 14336 took 55 us at 64 tokens, 36 of them for the expansion.)
+// A block takes a tile of 128 channels and BN tokens, or a part of its K.  Warp roles:
+//   warps 0-15  weights: warp w the row tile w % 8 of every other stage, loaded two of its stages ahead; warps 0-7 then the
+//               epilogue: warp w reads TMEM lanes 32 (w % 4) .. (channels), columns BN / 2 (w / 4) .. (tokens), applies
+//               scales and bias and stores runs of 32 channels;
+//   warp 16     TMEM allocation and MMA issue;
+//   warp 17     TMA producer of the tokens.
+// Few tiles split K over blocks (fp32 partial sums, joined with scales and bias by a second kernel).
+// (Pairs of SMs, cta_group::2, halve the operands' traffic, but each stage's weights then take arrivals across the pair: 1.1 us a stage of
+// 64 columns, where this form takes %s.)
+// Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded and each role leaves its loop; copies and MMAs under way are waited
+// for, and the tensor memory is freed.
+#include <cstring>
+
+#include "w4_many.h"
+
+namespace fgq {
+namespace w4 {
+namespace {
+
+using tc::make_map_2d;
+
+constexpr int G4_BM = 128, G4_KT = 128;  // channels and columns of a stage
+constexpr int G4_W_WARPS = 16, G4_MMA_WARP = 16, G4_TMA_WARP = 17;
+constexpr int G4_EPI_WARPS = 8;
+constexpr int G4_THREADS = 32 * 18;
+constexpr uint64_t G4_TIMEOUT_NS = 1000000000ull;  // 1 s per wait
+
+template <int BN>
+struct G4Cfg {
+  // each operand in two halves of 64 columns (128-byte rows)
+  static constexpr int A_HALF = G4_BM * 128, B_HALF = BN * 128, STAGE = 2 * (A_HALF + B_HALF);
+  static constexpr int STAGES = BN == 256 ? 2 : (BN == 128 ? 3 : 4);
+  static constexpr int SMEM = 1024 + STAGES * STAGE + 8 * (3 * STAGES + 2) + 16;
+};
+static_assert(G4Cfg<256>::SMEM <= 232448 && G4Cfg<128>::SMEM <= 232448 && G4Cfg<64>::SMEM <= 232448, "shared memory budget");
+
+struct G4Args {
+  CUtensorMap x_map;
+  Matrix w;
+  const float* scale;  // or nullptr: 1
+  const int* wexp;     // [M rounded up to row tiles]: w' = w 2^(12 - wexp)
+  const float* bias;
+  void* y;
+  float* part;  // [splits][P][M] partial sums, or nullptr
+  unsigned int* err;
+  uint64_t timeout_ns;
+  int P, M, mtiles, ptiles, splits, ytype;
+};
+
+// The first `live` of 32 values, one a row of M elements.
+template <typename T>
+__device__ __forceinline__ void store_column(T* y, int M, int live, const uint32_t (&r)[32]) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (i < live) from_float(__uint_as_float(r[i]), y[(int64_t)i * M]);
+}
+
+template <int BN, int PER>
+__global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_constant__ G4Args a) {
+  using C = G4Cfg<BN>;
+  constexpr int S = C::STAGES;
+  extern __shared__ uint8_t smem_g4[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_g4) + 1023) & ~uintptr_t(1023));
+  uint64_t* full_x = reinterpret_cast<uint64_t*>(smem + S * C::STAGE);  // the tokens have arrived
+  uint64_t* full_w = full_x + S;   // the weights have been written
+  uint64_t* empty = full_w + S;    // the MMAs have read both
+  uint64_t* acc_full = empty + S;  // the sums are complete
+  uint64_t* drain_bar = acc_full + 1;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
+  volatile uint32_t* abort_flag = tmem_slot + 1;
+  uint32_t* read = tmem_slot + 2;  // stages that MMAs were committed for
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint64_t tmo = a.timeout_ns;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S; ++i) {
+      mbar_init(&full_x[i], 1);
+      mbar_init(&full_w[i], G4_W_WARPS / 2);
+      mbar_init(&empty[i], 1);
+    }
+    mbar_init(acc_full, 1);
+    mbar_init(drain_bar, 1);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == G4_MMA_WARP) {
+    tmem_alloc(tmem_slot, BN);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  // tile -> channels, tokens, tile columns [c0, c1): neighbours share tokens
+  int id = blockIdx.x;
+  const int m0 = (id % a.mtiles) * G4_BM;
+  id /= a.mtiles;
+  const int sp = id % a.splits, p0 = (id / a.splits) * BN;
+  const int c0 = (int)((int64_t)a.w.ct * sp / a.splits), n = (int)((int64_t)a.w.ct * (sp + 1) / a.splits) - c0;
+  auto fail = [&]() {
+    *abort_flag = 1;
+    record_error(a.err, FGQ_ERR_TIMEOUT);
+  };
+  int issued = 0;  // by the producer
+  bool ok = true;
+
+  if (warp == G4_TMA_WARP && lane == 0) {
+    pdl_wait();  // the tokens may be those of the kernel before
+    for (; issued < n; ++issued) {
+      const int st = issued % S;
+      if (!mbar_wait_timed(&empty[st], ((issued / S) & 1) ^ 1, tmo, abort_flag, 0)) {
+        ok = false;
+        break;
+      }
+      const uint32_t B = smem_u32(smem + st * C::STAGE + 2 * C::A_HALF);
+      mbar_arrive_expect_tx(&full_x[st], 2 * C::B_HALF);
+      tma_load_2d(B, &a.x_map, (c0 + issued) * G4_KT, p0, &full_x[st]);
+      tma_load_2d(B + C::B_HALF, &a.x_map, (c0 + issued) * G4_KT + 64, p0, &full_x[st]);
+    }
+    // the last stages' commits: those before them were waited for
+    for (int i = n > S ? n - S : 0; i < n && ok; ++i) ok = mbar_wait_timed(&empty[i % S], (i / S) & 1, tmo, abort_flag, 0);
+    if (!ok && !*abort_flag) fail();
+  }
+
+  if (warp == G4_MMA_WARP) {  // converged, an elected lane issues
+    const uint32_t idesc = idesc_f16_f32(G4_BM, BN);
+    int j = 0;
+    for (; j < n; ++j) {
+      const int st = j % S;
+      ok = mbar_wait_warp(&full_x[st], (j / S) & 1, tmo, abort_flag) && mbar_wait_warp(&full_w[st], (j / S) & 1, tmo, abort_flag);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t A = smem_u32(smem + st * C::STAGE), B = A + 2 * C::A_HALF;
+      if (elect_one()) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint64_t ad = sdesc_k_sw128(A + half * C::A_HALF), bd = sdesc_k_sw128(B + half * C::B_HALF);
+#pragma unroll
+          for (int s = 0; s < 4; ++s) mma_f16(tmem, ad + 2 * s, bd + 2 * s, idesc, j > 0 || half > 0 || s > 0 ? 1u : 0u);
+        }
+        mma_commit(&empty[st]);
+      }
+      __syncwarp();
+    }
+    if (ok) {
+      if (elect_one()) mma_commit(acc_full);
+    } else {
+      if (lane == 0 && !*abort_flag) fail();
+      if (elect_one()) mma_commit(drain_bar);
+    }
+    if (lane == 0) *read = (uint32_t)j;
+  }
+
+  if (warp < G4_W_WARPS) {
+    const int d = warp & 7, first = warp >> 3, g = lane >> 2, t = lane & 3;  // every other stage
+    const int rt = min(m0 / TILE_ROWS + d, a.w.rt - 1);  // a row tile past the last is read as the last
+    const int64_t at = (int64_t)rt * a.w.ct + c0;
+    constexpr int AHEAD = 2;
+    Tile<PER> tile[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i)
+      if (first + 2 * i < n) tile[i].load(a.w.codes, a.w.scales, at + first + 2 * i, lane);
+    pdl_wait();  // the exponents are those of the kernel before
+    // what takes the rows' scales to fp16's range, in two factors: it passes fp32's largest for tiny ones
+    float up[2], up2[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+      const int e = 12 - __ldcg(a.wexp + rt * TILE_ROWS + g + 8 * r);
+      up[r] = pow2f(e / 2);
+      up2[r] = pow2f(e - e / 2);
+    }
+    for (int j0 = first; j0 < n && ok; j0 += 2 * AHEAD) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) {
+        const int j = j0 + 2 * i, st = j % S;
+        if (j >= n || !ok) break;
+        uint32_t s2[2][PER];  // scales as fp16 pairs
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int k = 0; k < PER; ++k) {
+            const float s = tile[i].s[r].get(k) * up[r] * up2[r];
+            s2[r][k] = pack2(s, s, __half());
+          }
+        uint4 v[2][4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) v[r][w] = scaled_codes(tile[i].word(r, w), s2[r][w * PER / 4]);
+        if (j + 2 * AHEAD < n) tile[i].load(a.w.codes, a.w.scales, at + j + 2 * AHEAD, lane);
+        ok = mbar_wait_warp(&empty[st], ((j / S) & 1) ^ 1, tmo, abort_flag);
+        if (!ok) break;
+        uint8_t* A = smem + st * C::STAGE;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+          for (int w = 0; w < 4; ++w)
+            *reinterpret_cast<uint4*>(A + (w >> 1) * C::A_HALF + tc::sw128(TILE_ROWS * d + 8 * r + g, 4 * (w & 1) + t)) = v[r][w];
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full_w[st]);
+      }
+    }
+    if (!ok && lane == 0 && !*abort_flag) fail();
+  }
+
+  if (warp < G4_EPI_WARPS && ok) {
+    const int quarter = warp & 3, half = warp >> 2;
+    ok = mbar_wait_warp(acc_full, 0, tmo, abort_flag);
+    if (!ok && lane == 0 && !*abort_flag) fail();
+    if (ok) {
+      tc_fence_after();
+      const int m = m0 + 32 * quarter + lane;
+      const bool mok = m < a.M;
+      const float sw = mok ? pow2f(__ldcg(a.wexp + m) - 12) : 0.0f;
+      const float bias = mok && a.bias ? __ldg(a.bias + m) : 0.0f;
+      const uint32_t ta = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(half * (BN / 2));
+      const int pw = p0 + half * (BN / 2);
+#pragma unroll 1
+      for (int c = 0; c < BN / 2; c += 32) {
+        uint32_t r[32];
+        tmem_ld32(ta + c, r);
+        // the 32 tokens' scales, one a lane
+        const float sx = !a.scale ? 1.0f : (pw + c + lane < a.P ? __ldcg(a.scale + pw + c + lane) : 0.0f);
+        tmem_ld_wait_regs(r);
+        const int live = mok ? a.P - (pw + c) : 0;  // tokens of these 32 that there are
+        if (a.part) {
+          float* dst = a.part + ((int64_t)sp * a.P + pw + c) * a.M + m;
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (i < live) dst[(int64_t)i * a.M] = __uint_as_float(r[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(fmaf(__uint_as_float(r[i]), __shfl_sync(FULL_MASK, sx, i) * sw, bias));
+          const int64_t out = (int64_t)(pw + c) * a.M + m;
+          if (a.ytype == FGQ_F32)
+            store_column(static_cast<float*>(a.y) + out, a.M, live, r);
+          else if (a.ytype == FGQ_BF16)
+            store_column(static_cast<__nv_bfloat16*>(a.y) + out, a.M, live, r);
+          else
+            store_column(static_cast<__half*>(a.y) + out, a.M, live, r);
+        }
+      }
+      tc_fence_before();
+    }
+  }
+
+  __syncthreads();
+  if (*abort_flag && warp == G4_TMA_WARP && lane == 0) {  // what is still under way: MMAs, then boxes that no MMA has read
+    const int done = (int)*read;
+    auto drain = [](uint64_t* bar, int phase) { mbar_wait_bounded(bar, (uint32_t)phase & 1u, 1u << 16); };
+    drain(done < n ? drain_bar : acc_full, 0);
+    for (int i = done > S ? done - S : 0; i < done; ++i) drain(&empty[i % S], i / S);
+    for (int i = done; i < issued; ++i) drain(&full_x[i % S], i / S);
+  }
+  __syncthreads();
+  if (warp == G4_MMA_WARP) {
+    tc_fence_after();
+    tmem_dealloc(tmem, BN);
+  }
+}
+
+// y from the splits' sums: a thread one channel of G4_JOIN tokens, so that their loads are in flight together.
+constexpr int G4_JOIN = 4;
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ G4Args a) {
+  const int64_t n = (int64_t)a.P * a.M;
+  const int m = blockIdx.x * 256 + threadIdx.x;
+  pdl_wait();
+  if (m >= a.M) return;
+  const float sw = pow2f(__ldcg(a.wexp + m) - 12), bias = a.bias ? __ldg(a.bias + m) : 0.0f;
+  for (int64_t p = (int64_t)blockIdx.y * G4_JOIN; p < a.P; p += (int64_t)gridDim.y * G4_JOIN) {
+    float v[G4_JOIN] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 2
+    for (int s = 0; s < a.splits; ++s)
+#pragma unroll
+      for (int i = 0; i < G4_JOIN; ++i)
+        if (p + i < a.P) v[i] += __ldcg(a.part + s * n + (p + i) * a.M + m);
+#pragma unroll
+    for (int i = 0; i < G4_JOIN; ++i)
+      if (p + i < a.P) store_typed(a.y, a.ytype, (p + i) * a.M + m, fmaf(v[i], (a.scale ? __ldcg(a.scale + p + i) : 1.0f) * sw, bias));
+  }
+}
+
+template <int BN, int PER>
+fgq_status launch_g4_per(const G4Args& a, int grid, cudaStream_t s) {
+  if (!tc::smem_attr_once<gemm_w4_kernel<BN, PER>>(G4Cfg<BN>::SMEM)) return FGQ_ERR_CUDA;
+  return after_launch(launch_pdl(gemm_w4_kernel<BN, PER>, dim3(grid), dim3(G4_THREADS), G4Cfg<BN>::SMEM, s, a));
+}
+template <int BN>
+fgq_status launch_g4(const G4Args& a, int grid, cudaStream_t s) {
+  if (a.w.per == 4) return launch_g4_per<BN, 4>(a, grid, s);
+  return a.w.per == 2 ? launch_g4_per<BN, 2>(a, grid, s) : launch_g4_per<BN, 1>(a, grid, s);
+}
+
+}  // namespace
+
+ManyPlan plan_many(int P, int ct, int M) {
+  ManyPlan g;
+  const int64_t sms = device_sms(), mt = ((int64_t)M + G4_BM - 1) / G4_BM;
+  g.bn = P <= 64 ? 64 : (P <= 128 || mt * ((P + 255) / 256) * 2 <= sms ? 128 : 256);
+  // K split over blocks where there are fewer tiles than half the SMs, four tile columns each at least
+  const int64_t tiles = mt * ((P + g.bn - 1) / g.bn), by_k = ct / 4;
+  int64_t splits = sms / tiles < by_k ? sms / tiles : by_k;
+  g.splits = (int)(splits < 1 ? 1 : (splits > 16 ? 16 : splits));
+  g.part_bytes = g.splits > 1 ? (size_t)g.splits * P * M * 4 : 0;
+  return g;
+}
+
+fgq_status launch_many(const ManyPlan& plan, const Matrix& w, const int* wexp, const void* x16, int64_t pitch, int K, const float* scale,
+                       int P, int M, float* part, const float* bias, void* y, int ytype, cudaStream_t s) {
+  G4Args a;
+  memset(&a, 0, sizeof a);
+  a.w = w;
+  a.scale = scale;
+  a.wexp = wexp;
+  a.bias = bias;
+  a.y = y;
+  a.part = plan.splits > 1 ? part : nullptr;
+  a.err = device_error_word();
+  const int64_t lim_us = debug_wait_limit_us();
+  a.timeout_ns = lim_us < 0 ? G4_TIMEOUT_NS : (uint64_t)lim_us * 1000u;
+  a.P = P;
+  a.M = M;
+  a.ytype = ytype;
+  a.mtiles = (int)(((int64_t)M + G4_BM - 1) / G4_BM);
+  a.ptiles = (P + plan.bn - 1) / plan.bn;
+  a.splits = plan.splits;
+  const int64_t tiles = (int64_t)a.mtiles * a.ptiles * a.splits;
+  if (tiles > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
+  if (!make_map_2d(&a.x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x16, (uint64_t)K, (uint64_t)P, (uint64_t)pitch * 2, 64,
+                   (uint32_t)plan.bn, CU_TENSOR_MAP_SWIZZLE_128B))
+    return FGQ_ERR_CUDA;
+  const int grid = (int)tiles;
+  fgq_status st = plan.bn == 256 ? launch_g4<256>(a, grid, s) : (plan.bn == 128 ? launch_g4<128>(a, grid, s) : launch_g4<64>(a, grid, s));
+  if (st == FGQ_OK && a.part) {
+    const int rows = (P + G4_JOIN - 1) / G4_JOIN;
+    const dim3 jg((unsigned)((M + 255) / 256), (unsigned)(rows < 65535 ? rows : 65535));
+    st = after_launch(launch_pdl(join_kernel, jg, dim3(256), 0, s, a));
+  }
+  return st;
+}
+
+}  // namespace w4
+}  // namespace fgq

@@ -7,6 +7,7 @@
 
 #include "linear_internal.cuh"
 #include "w4_launch.h"
+#include "w4_many.h"
 
 namespace fgq {
 namespace w4 {
@@ -116,7 +117,7 @@ fgq_status launch_few(RowsArgs a, bool early, cudaStream_t s) {
   const int tokens = 8 * nt / cpt;
   const int64_t tiles = ((int64_t)a.P + tokens - 1) / tokens;
   if (nt <= 2) {  // one tile of tokens: held in shared memory where it fits
-    const ResidentPlan plan = plan_held(nt, a.w.ct, a.w.per);
+    const ResidentPlan plan = plan_held(nt, a.w.ct, a.w.per, (int)columns);
     if (plan.warps > 0) {
       ResidentArgs r = {};
       r.w = a.w, r.x = a.x, r.bias = a.bias, r.y = a.y, r.P = a.P, r.M = a.M, r.ytype = a.ytype, r.early = early;
@@ -139,53 +140,62 @@ fgq_status launch_few(RowsArgs a, bool early, cudaStream_t s) {
 }
 
 // ------------------------------------------------------------------ operands of the product for many tokens
-// Weights as fp16 rows: c s 2^(12 - e) with 2^e <= the row's largest scale < 2^(e + 1), which has 11 bits at most and is exact down
-// to 2^-29 of it.  Blocks (row tile, part of K): each finds its 16 rows' largest scales, all of them, first.
-constexpr int EX_WARPS = 8;
-__global__ void __launch_bounds__(32 * EX_WARPS) expand_weights_kernel(const __grid_constant__ Matrix w, __half* dst, int64_t pitch,
-                                                                       int M, float* wscale) {
+// What the blocks past the tokens do: find the exponent of each weight row's largest scale (subnormal ones: of the smallest normal), and
+// where w16 is given, write its rows as fp16, c s 2^(12 - e), `parts` blocks a row tile.  Padding takes part.
+struct Weights {
+  Matrix w;
+  int* wexp;      // all rows of the tiles; or nullptr:
+  __half* w16;    // [M][pitch]
+  float* wscale;  // [M]: 2^(e - 12)
+  int64_t pitch;
+  int M, parts;
+};
+__device__ __forceinline__ void prepare_weights(const Weights& a, int block) {
   __shared__ uint32_t top[TILE_ROWS];
-  pdl_trigger();
-  const int mt = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const Matrix& w = a.w;
+  const int mt = block / a.parts, part = block - mt * a.parts;
   if (threadIdx.x < TILE_ROWS) top[threadIdx.x] = 0u;
   __syncthreads();
   const uint16_t* sc = w.scales + (int64_t)mt * w.ct * TILE_ROWS * w.per;
-  // magnitudes compare as whole numbers; the order of maxima does not matter
-  for (int64_t i = threadIdx.x; i < (int64_t)w.ct * TILE_ROWS * w.per; i += 32 * EX_WARPS)
-    atomicMax(&top[(int)(i / w.per) % TILE_ROWS], (uint32_t)(__ldg(sc + i) & 0x7fffu));
+  // magnitudes compare as whole numbers; the order of maxima does not matter.  Eight scales a load
+  const int n = w.ct * TILE_ROWS * w.per / 8;
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4*>(sc) + i);
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = 8 * i + 2 * k;
+      atomicMax(&top[at / w.per % TILE_ROWS], u[k] & 0x7fffu);
+      atomicMax(&top[(at + 1) / w.per % TILE_ROWS], u[k] >> 16 & 0x7fffu);
+    }
+  }
   __syncthreads();
-  auto exponent = [&](int r) {  // of the row's largest scale, subnormal ones as the smallest normal
-    const int e = (int)(top[r] >> 7) - 127;
-    return e < -126 ? -126 : e;
-  };
-  if (blockIdx.y == 0 && threadIdx.x < TILE_ROWS && mt * TILE_ROWS + (int)threadIdx.x < M)
-    wscale[mt * TILE_ROWS + threadIdx.x] = pow2f(exponent(threadIdx.x) - 12);
-  const int e0 = exponent(g), e1 = exponent(g + 8);
-  for (int kt = blockIdx.y * EX_WARPS + warp; kt < w.ct; kt += gridDim.y * EX_WARPS) {
+  auto exponent = [&](int r) { return max((int)(top[r] >> 7) - 127, -126); };
+  if (!a.w16) {
+    if (threadIdx.x < TILE_ROWS) a.wexp[mt * TILE_ROWS + threadIdx.x] = exponent(threadIdx.x);
+    return;
+  }
+  if (part == 0 && threadIdx.x < TILE_ROWS && mt * TILE_ROWS + (int)threadIdx.x < a.M)
+    a.wscale[mt * TILE_ROWS + threadIdx.x] = pow2f(exponent(threadIdx.x) - 12);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+  const int e0 = 12 - exponent(g), e1 = 12 - exponent(g + 8);
+  for (int kt = part * 8 + warp; kt < w.ct; kt += a.parts * 8) {
     const int64_t at = (int64_t)mt * w.ct + kt;
+    uint4 v[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) v[r] = __ldg(reinterpret_cast<const uint4*>(w.codes + at * TILE_BYTES) + 32 * r + lane);
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
       const int m = mt * TILE_ROWS + g + 8 * r, e = r ? e1 : e0;
-      if (m >= M) continue;
-      const uint4 v = __ldg(reinterpret_cast<const uint4*>(w.codes + at * TILE_BYTES) + 32 * r + lane);
-      const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+      if (m >= a.M) continue;
+      const uint32_t word[4] = {v[r].x, v[r].y, v[r].z, v[r].w};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int64_t k = (int64_t)kt * TILE_COLS + 32 * j + 8 * t;
-        if (k >= pitch) continue;
+        if (k >= a.pitch) continue;
         float s = __uint_as_float((uint32_t)__ldg(w.scales + at * (TILE_ROWS * w.per) + (g + 8 * r) * w.per + j * w.per / 4) << 16);
-        // 2^(12 - e) in two factors: it passes fp32's largest for subnormal rows
-        s = s * pow2f((12 - e) / 2) * pow2f((12 - e) - (12 - e) / 2);
-        uint32_t h[4];
-        code_pairs<__half>(word[j], h);
-        float c[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-          c[2 * i] = f.x * (s * Operand<__half>::BACK);
-          c[2 * i + 1] = f.y * (s * Operand<__half>::BACK);
-        }
-        store8(dst + (int64_t)m * pitch + k, c);
+        s = s * pow2f(e / 2) * pow2f(e - e / 2);  // in two factors: 2^e passes fp32's largest for subnormal rows
+        *reinterpret_cast<uint4*>(a.w16 + m * a.pitch + k) = scaled_codes(word[j], pack2(s, s, __half()));
       }
     }
   }
@@ -194,12 +204,15 @@ __global__ void __launch_bounds__(32 * EX_WARPS) expand_weights_kernel(const __g
 // Tokens as fp16 rows, a block each: fp16 as they are; bf16 times 2^(14 - e), 2^e <= the row's largest magnitude < 2^(e + 1).
 // A row with NaN or Inf: its scale is NaN, and so are its outputs.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) expand_tokens_kernel(const T* __restrict__ x, int K, int64_t ldx, __half* dst, int64_t pitch,
-                                                            float* scale) {
+__global__ void __launch_bounds__(256) prepare_kernel(const T* __restrict__ x, int P, int K, int64_t ldx, __half* dst, int64_t pitch,
+                                                      float* scale, const __grid_constant__ Weights w) {
   constexpr bool BF = std::is_same<T, __nv_bfloat16>::value;
   __shared__ float red[8];
   pdl_trigger();
-  pdl_wait();  // what reads these rows reads the weights' as well, and waits for this kernel only
+  if ((int)blockIdx.x >= P) {
+    prepare_weights(w, (int)blockIdx.x - P);
+    return;
+  }
   const int p = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const T* row = x + p * ldx;
   __half* to = dst + p * pitch;
@@ -258,42 +271,76 @@ __global__ void __launch_bounds__(256) expand_tokens_kernel(const T* __restrict_
   }
 }
 
+__global__ void __launch_bounds__(256) ones_kernel(float* p, int n) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) p[i] = 1.0f;
+}
+
 inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
-fgq_status launch_many(const void* x, int type, int P, int K, int64_t ldx, const fgq_w4* w, const float* bias, void* y,
-                       cudaStream_t s) {
+bool overlap(const void* x, const void* y, int type, int P, int K, int M, int64_t ldx) {
+  const uintptr_t xb = reinterpret_cast<uintptr_t>(x), yb = reinterpret_cast<uintptr_t>(y);
+  const uint64_t xn = ((uint64_t)(P - 1) * (P > 1 ? ldx : 0) + K) * float_bytes(type), yn = (uint64_t)P * M * float_bytes(type);
+  return xb < yb + yn && yb < xb + xn;
+}
+
+// From here on weights are expanded in memory for the product on pairs of SMs, which saves shared-memory traffic for the bytes.
+// bf16, us so and in gemm_w4.cu: 512 tokens, 4096 -> 14336 76.9 and 68.9; 1024 tokens 107.7 and 103.3, 4096 -> 4096 36.4 and 37.0;
+// 1536 tokens 149.6 and 169.4, 54.7 and 69.1; 2048 tokens 183 and 209, 57.5 and 70.9, but 1024 -> 2048 20.2 and 18.4.
+constexpr int EXPAND_MIN_P = 1025;
+constexpr int64_t EXPAND_MIN_WEIGHTS = 1 << 23;
+
+fgq_status run_many(const void* x, int type, int P, int K, int64_t ldx, const fgq_w4* w, const float* bias, void* y, cudaStream_t s) {
   const int M = w->rows;
-  const Matrix m = matrix(w);
-  const GemmPlan plan = plan_gemm_w8a8(P, K, M);
-  const size_t w_bytes = up256((size_t)M * plan.pitch * 2), x_bytes = up256((size_t)P * plan.pitch * 2);
-  const size_t ws_bytes = up256((size_t)M * 4), xs_bytes = up256((size_t)P * 4);
-  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(w_bytes + x_bytes + ws_bytes + xs_bytes + plan.part_bytes, s));
+  const bool expand = P >= EXPAND_MIN_P && (int64_t)K * M >= EXPAND_MIN_WEIGHTS;
+  Weights wt = {matrix(w), nullptr, nullptr, nullptr, 0, M, 1};
+  const ManyPlan plan = plan_many(P, wt.w.ct, M);
+  const GemmPlan pairs = expand ? plan_gemm_w8a8(P, K, M) : GemmPlan{};
+  // fp16 tokens are operands as they are (expanded: where their rows are whole K-tiles beside one another)
+  const bool vec = direct_tokens(x, type, P, K, ldx);
+  const bool direct = type == FGQ_F16 && vec && !overlap(x, y, type, P, K, M, ldx) && (!expand || (K == pairs.pitch && (P == 1 || ldx == K)));
+  const int64_t pitch = expand ? pairs.pitch : (direct && P > 1 ? ldx : copied_pitch(K));
+  const size_t e_bytes = up256((size_t)wt.w.rt * TILE_ROWS * 4), x_bytes = direct ? 0 : up256((size_t)P * pitch * 2);
+  const size_t s_bytes = direct && !expand ? 0 : up256((size_t)P * 4), w_bytes = expand ? up256((size_t)M * pitch * 2) : 0;
+  const size_t p_bytes = expand ? pairs.part_bytes : plan.part_bytes;
+  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(e_bytes + x_bytes + s_bytes + w_bytes + p_bytes, s));
   if (!tmp) return FGQ_ERR_CUDA;
-  __half* w16 = reinterpret_cast<__half*>(tmp);
-  __half* x16 = reinterpret_cast<__half*>(tmp + w_bytes);
-  float* wscale = reinterpret_cast<float*>(tmp + w_bytes + x_bytes);
-  float* xscale = reinterpret_cast<float*>(tmp + w_bytes + x_bytes + ws_bytes);
-  int parts = (m.ct + EX_WARPS - 1) / EX_WARPS;
-  while (parts > 1 && (int64_t)parts * m.rt > 4ll * device_sms()) parts = (parts + 1) / 2;
-  expand_weights_kernel<<<dim3(m.rt, parts), 32 * EX_WARPS, 0, s>>>(m, w16, plan.pitch, M, wscale);
-  fgq_status st = after_launch();
-  const bool vec = K % 8 == 0 && aligned(x, 16) && (P == 1 || stride16(ldx, type));
-  if (st == FGQ_OK) {
-    cudaError_t e;
+  __half* x16 = reinterpret_cast<__half*>(tmp + e_bytes);
+  float* xscale = s_bytes ? reinterpret_cast<float*>(tmp + e_bytes + x_bytes) : nullptr;
+  float* part = reinterpret_cast<float*>(tmp + e_bytes + x_bytes + s_bytes + w_bytes);
+  if (expand) {
+    wt.w16 = reinterpret_cast<__half*>(tmp + e_bytes + x_bytes + s_bytes);
+    wt.wscale = reinterpret_cast<float*>(tmp);
+    wt.pitch = pitch;
+    wt.parts = (wt.w.ct + 7) / 8;
+    while (wt.parts > 1 && (int64_t)wt.parts * wt.w.rt > 8ll * device_sms()) wt.parts = (wt.parts + 1) / 2;
+  } else {
+    wt.wexp = reinterpret_cast<int*>(tmp);
+  }
+  const int tokens = direct ? 0 : P;
+  const int64_t blocks = tokens + (int64_t)wt.w.rt * wt.parts;
+  fgq_status st = FGQ_ERR_UNSUPPORTED;
+  if (blocks <= INT32_MAX) {
+    const unsigned grid = (unsigned)blocks;
     if (type == FGQ_BF16) {
       const __nv_bfloat16* xb = static_cast<const __nv_bfloat16*>(x);
-      e = vec ? launch_pdl(expand_tokens_kernel<__nv_bfloat16, true>, dim3(P), dim3(256), 0, s, xb, K, ldx, x16, plan.pitch, xscale)
-              : launch_pdl(expand_tokens_kernel<__nv_bfloat16, false>, dim3(P), dim3(256), 0, s, xb, K, ldx, x16, plan.pitch, xscale);
+      vec ? prepare_kernel<__nv_bfloat16, true><<<grid, 256, 0, s>>>(xb, tokens, K, ldx, x16, pitch, xscale, wt)
+          : prepare_kernel<__nv_bfloat16, false><<<grid, 256, 0, s>>>(xb, tokens, K, ldx, x16, pitch, xscale, wt);
     } else {
       const __half* xh = static_cast<const __half*>(x);
-      e = vec ? launch_pdl(expand_tokens_kernel<__half, true>, dim3(P), dim3(256), 0, s, xh, K, ldx, x16, plan.pitch, xscale)
-              : launch_pdl(expand_tokens_kernel<__half, false>, dim3(P), dim3(256), 0, s, xh, K, ldx, x16, plan.pitch, xscale);
+      vec ? prepare_kernel<__half, true><<<grid, 256, 0, s>>>(xh, tokens, K, ldx, x16, pitch, xscale, wt)
+          : prepare_kernel<__half, false><<<grid, 256, 0, s>>>(xh, tokens, K, ldx, x16, pitch, xscale, wt);
     }
-    st = after_launch(e);
+    st = after_launch();
   }
+  if (st == FGQ_OK && expand && direct) {
+    ones_kernel<<<(P + 255) / 256, 256, 0, s>>>(xscale, P);
+    st = after_launch();
+  }
+  const void* rows = direct ? x : x16;
   if (st == FGQ_OK)
-    st = launch_gemm_w8a8(plan, x16, w16, reinterpret_cast<float*>(tmp + w_bytes + x_bytes + ws_bytes + xs_bytes), xscale, P,
-                          wscale, M, bias, y, type, s);
+    st = expand ? launch_gemm_w8a8(pairs, rows, wt.w16, part, xscale, P, wt.wscale, M, bias, y, type, s)
+                : launch_many(plan, wt.w, wt.wexp, rows, pitch, direct ? K : (int)pitch, xscale, P, M, part, bias, y, type, s);
   if (cudaFreeAsync(tmp, s) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
   return st;
 }
@@ -304,14 +351,9 @@ __global__ void __launch_bounds__(256) bias_kernel(const float* bias, void* y, i
     store_typed(y, ytype, i, bias ? __ldg(bias + i % M) : 0.0f);
 }
 
-// Tokens of 16 bits up to which the few-token kernel runs.
-constexpr int FEW_MAX_P = 64;
-
-bool overlap(const void* x, const void* y, int type, int P, int K, int M, int64_t ldx) {
-  const uintptr_t xb = reinterpret_cast<uintptr_t>(x), yb = reinterpret_cast<uintptr_t>(y);
-  const uint64_t xn = ((uint64_t)(P - 1) * (P > 1 ? ldx : 0) + K) * float_bytes(type), yn = (uint64_t)P * M * float_bytes(type);
-  return xb < yb + yn && yb < xb + xn;
-}
+// Tokens of 16 bits up to which the kernels of few tokens run.  bf16, us there and in gemm_w4.cu: 16 tokens, 4096 -> 4096 10.0 and 12.0, 4096 ->
+// 14336 14.5 and 25.0; 32 tokens 9.5 and 12.2, 28.1 and 25.3, 8192 -> 8192 27.2 and 28.2; 33 tokens 25.9 and 12.3, 49.8 and 25.3.
+constexpr int FEW_MAX_P = 32;
 
 }  // namespace
 
@@ -389,7 +431,7 @@ fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx,
     bias_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, stream>>>(bias, y, type, P, M);
     return after_launch();
   }
-  if (type != FGQ_F32 && P > FEW_MAX_P) return launch_many(x, type, P, K, ldx, w, bias, y, stream);
+  if (type != FGQ_F32 && P > FEW_MAX_P) return run_many(x, type, P, K, P > 1 ? ldx : 0, w, bias, y, stream);
   RowsArgs a = {};
   a.w = matrix(w), a.x = {x, P > 1 ? ldx : 0, K}, a.bias = bias, a.y = y, a.P = P, a.M = M, a.ytype = type;
   if (direct_tokens(x, type, P, K, ldx) && !overlap(x, y, type, P, K, M, ldx)) return launch_few(a, false, stream);

@@ -440,6 +440,7 @@ __global__ void __launch_bounds__(THREADS) down_kernel(const __grid_constant__ D
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) sum[0][nt][0] = sum[0][nt][1] = 0ull;
   float* own = part + warp * TILE_ROWS;
+  const Pieces<NT> pieces(8 * NT, lane);
   for (int64_t q = 0; q < n; q += AHEAD) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
@@ -448,7 +449,7 @@ __global__ void __launch_bounds__(THREADS) down_kernel(const __grid_constant__ D
       __syncthreads();  // the stage is there for everyone, and the one before has been read
       if (q + i + R::STAGES - 1 < n) next_tokens();
       cp_async_commit();
-      multiply<T, 1, NT, PER>(tile[i], w4_smem + slot * R::BYTES, sum, lane);
+      multiply<T, 1, NT, PER>(tile[i], w4_smem + slot * R::BYTES, pieces, sum);
       slot = slot + 1 == R::STAGES ? 0 : slot + 1;
       if (q + i + AHEAD < n) next_weights(i);
       const bool turn = now.kt == ct - 1;
@@ -636,8 +637,12 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   const int64_t hpitch = (int64_t)row_tiles(F) * TILE_ROWS;
   // tokens held in shared memory where units of 8 (fp32: 4) do and they fit
   const int ctk = col_tiles(K), ctf = col_tiles(F);
-  const ResidentPlan hp = type == FGQ_F32 ? plan_resident<2, 2, GATED_AHEAD>(ctk, 128 / gate->group) : plan_resident<2, 1, GATED_AHEAD>(ctk, 128 / gate->group);
-  const ResidentPlan dp = plan_held(type == FGQ_BF16 ? 1 : 2, ctf, 128 / down->group);
+  // tokens of a unit: a router picks an expert once for each
+  const int most = type == FGQ_F32 ? 4 : 8, held_tokens = route && pass < most ? pass : most;
+  const int dparts = type == FGQ_F32 ? 3 : (type == FGQ_F16 ? 2 : 1);
+  const ResidentPlan hp = type == FGQ_F32 ? plan_resident<2, 2, GATED_AHEAD>(ctk, 128 / gate->group, held_tokens * columns_per_token(3))
+                                          : plan_resident<2, 1, GATED_AHEAD>(ctk, 128 / gate->group, held_tokens);
+  const ResidentPlan dp = plan_held(dparts == 1 ? 1 : 2, ctf, 128 / down->group, held_tokens * columns_per_token(dparts));
   const bool held = hp.warps > 0 && dp.warps > 0 && (type == FGQ_F32 ? A <= 4ll * E : A <= 8ll * E);
   const int cap = held && type == FGQ_F32 ? 4 : unit_tokens(type, A, E);
   const int most_units = (A < E || P == 1 ? A : E) + A / cap;

@@ -171,12 +171,22 @@ __device__ __forceinline__ uint32_t chunk_at(int col, int chunk) { return (uint3
 // sum[mt][nt] += tile mt times the stage's columns; sums are in units of 1 / BACK.  Sums of two columns are a packed pair: [0] of
 // row g, [1] of row g + 8.
 using pair_t = unsigned long long;
+// Where a thread's pieces of a stage of `cols` columns are: chunk 4 j + t of column 8 nt + g, for even and odd j.  Columns that the
+// stage does not have are read as its last: nothing takes their sums.
+template <int NT>
+struct Pieces {
+  uint32_t even[NT], odd[NT];
+  __device__ __forceinline__ Pieces(int cols, int lane) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int c = min(8 * nt + (lane >> 2), cols - 1);
+      even[nt] = chunk_at(c, lane & 3);
+      odd[nt] = chunk_at(c, 4 + (lane & 3));
+    }
+  }
+};
 template <typename T, int MT, int NT, int PER>
-__device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint8_t* stage, pair_t (&sum)[MT][NT][2], int lane) {
-  const int g = lane >> 2, t = lane & 3;
-  // chunk 4 j + t of column g (chunk_at): even and odd j
-  const uint8_t* even = stage + chunk_at(g, t);
-  const uint8_t* odd = stage + chunk_at(g, 4 + t);
+__device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint8_t* stage, const Pieces<NT>& at, pair_t (&sum)[MT][NT][2]) {
 #pragma unroll
   for (int gi = 0; gi < PER; ++gi) {
     float acc[MT][NT][4];
@@ -184,7 +194,7 @@ __device__ __forceinline__ void multiply(const Tile<PER> (&tile)[MT], const uint
     for (int j = gi * (4 / PER); j < (gi + 1) * (4 / PER); ++j) {
       uint4 b[NT];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) b[nt] = *reinterpret_cast<const uint4*>((j & 1 ? odd : even) + nt * 2048 + (j >> 1) * 128);
+      for (int nt = 0; nt < NT; ++nt) b[nt] = *reinterpret_cast<const uint4*>(stage + (j & 1 ? at.odd[nt] : at.even[nt]) + (j >> 1) * 128);
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
         uint32_t u[4], v[4];

@@ -35,8 +35,8 @@ fgq_status launch_held_per(const ResidentArgs& a, const ResidentPlan& plan, int6
 }
 // Tiles under way of a warp: four, or two pairs.
 constexpr int HELD_AHEAD = 4, GATED_AHEAD = 2;
-inline ResidentPlan plan_held(int nt, int ct, int per) {
-  return nt == 1 ? plan_resident<1, 1, HELD_AHEAD>(ct, per) : plan_resident<1, 2, HELD_AHEAD>(ct, per);
+inline ResidentPlan plan_held(int nt, int ct, int per, int cols) {
+  return nt == 1 ? plan_resident<1, 1, HELD_AHEAD>(ct, per, cols) : plan_resident<1, 2, HELD_AHEAD>(ct, per, cols);
 }
 template <typename T, int PARTS>
 fgq_status launch_held_type(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s) {

@@ -1,6 +1,6 @@
 // The product of up to 8 or 16 columns of tokens with 4-bit weights, tokens held in shared memory.
 //
-// A block keeps its tokens' columns for all of K (8 NT x K x 2 bytes) and takes a run of items of 16 MT rows.  The run's tiles
+// A block keeps its tokens' columns for all of K (up to 8 NT x K x 2 bytes) and takes a run of items of 16 MT rows.  The run's tiles
 // are one sequence, tile columns of an item after one another, and its warps share it in equal parts, wherever those cut an
 // item: each warp streams its part through a ring of AHEAD tiles of its own in shared memory, with no barrier until the end.  (Loads to
 // registers that far ahead did not stay in flight: their waits have no names of their own in a loop with branches.)  An item
@@ -31,6 +31,7 @@ struct ResidentArgs {
   int64_t hpitch;
   unsigned* top;  // [choice]: the largest magnitude of its h, as fp32 bits (zeros before MODE_GATED)
   float* z;  // MODE_DOWN: out, [choice][M]
+  int cols;   // columns of tokens held
   int one;    // MODE_GATED: there is one token
   int early;  // the kernel before is this library's: weights may be loaded while it runs
 };
@@ -41,7 +42,8 @@ constexpr int resident_warps(int mt, int nt) { return mt * nt >= 4 ? 20 : 24; }
 
 template <typename T, int MT, int NT, int PER, int PARTS, int MODE, int AHEAD>
 __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(const __grid_constant__ ResidentArgs a) {
-  constexpr int CPT = columns_per_token(PARTS), TOKENS = 8 * NT / CPT, COLS = 8 * NT, STAGE = COLS * 256;
+  constexpr int CPT = columns_per_token(PARTS), TOKENS = 8 * NT / CPT, COLS = 8 * NT;
+  const int STAGE = a.cols * 256;  // bytes of a tile column's tokens
   constexpr int TILES = MODE == MODE_GATED ? 1 : MT;  // row tiles of an item
   constexpr int LD = 16 * MT + 1, FRAGMENT = COLS * LD, TB = tile_bytes<PER>(), SLOT = MT * TB;
   extern __shared__ __align__(16) uint8_t w4_smem[];
@@ -229,6 +231,7 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
   unsigned big[NT][2];
   auto note = [&](int tok, float f) { atomicMax(tops + tok, __float_as_uint(f)); };
 
+  const Pieces<NT> pieces(a.cols, lane);
   pair_t sum[MT][NT][2];
   auto clear = [&]() {
 #pragma unroll
@@ -301,7 +304,7 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
         Tile<PER> tile[MT];
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) read_tile<PER>(tile[mt], ring + k * SLOT + mt * TB, lane);
-        multiply<T, MT, NT, PER>(tile, stage, sum, lane);
+        multiply<T, MT, NT, PER>(tile, stage, pieces, sum);
         __syncwarp();  // and read
         load(k);
         stage += STAGE;
@@ -373,22 +376,23 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
 
 // How a block holds its tokens: one block an SM, its warps, its shared memory.
 struct ResidentPlan {
-  int warps, smem;
+  int warps, smem, cols;
 };
 // warps = 0: the tokens do not fit beside eight warps' rings.
 template <int MT, int NT, int AHEAD>
-ResidentPlan plan_resident(int ct, int per) {
-  const int64_t x = (int64_t)ct * 8 * NT * 256;
+ResidentPlan plan_resident(int ct, int per, int cols) {
+  const int64_t x = (int64_t)ct * cols * 256;
   const int tile = TILE_BYTES + TILE_ROWS * per * 2;
   const int each = AHEAD * MT * tile + 2 * 8 * NT * (16 * MT + 1) * 4;
   const int64_t room = (RES_SMEM - x) / each;
   const int warps = room > resident_warps(MT, NT) ? resident_warps(MT, NT) : (int)room;
-  if (warps < 8) return {0, 0};
-  return {warps, (int)(x + (int64_t)warps * each)};
+  if (warps < 8) return {0, 0, 0};
+  return {warps, (int)(x + (int64_t)warps * each), cols};
 }
 
 template <typename T, int MT, int NT, int PER, int PARTS, int MODE, int AHEAD>
-fgq_status launch_resident(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, bool chained, cudaStream_t s) {
+fgq_status launch_resident(ResidentArgs a, const ResidentPlan& plan, int64_t items, bool chained, cudaStream_t s) {
+  a.cols = plan.cols;
   constexpr auto kernel = resident_kernel<T, MT, NT, PER, PARTS, MODE, AHEAD>;
   if (!tc::smem_attr_once<resident_kernel<T, MT, NT, PER, PARTS, MODE, AHEAD>>(RES_SMEM)) return FGQ_ERR_CUDA;
   const int64_t most = device_sms(), run = (items + most - 1) / most;

@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ R
       }
   };
 
+  const Pieces<NT> pieces(8 * NT, lane);
   for (int64_t q = 0; q < n; q += AHEAD) {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
@@ -218,7 +219,7 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ R
       __syncthreads();  // the stage is there for everyone, and the one before has been read
       if (q + i + R::STAGES - 1 < n) next_tokens();
       cp_async_commit();
-      multiply<T, MT, NT, PER>(tile[i], w4_smem + slot * R::BYTES, sum, lane);
+      multiply<T, MT, NT, PER>(tile[i], w4_smem + slot * R::BYTES, pieces, sum);
       slot = slot + 1 == R::STAGES ? 0 : slot + 1;
       if (q + i + AHEAD < n) next_weights(i);
       if (++kt == ct && a.splits == 1) {

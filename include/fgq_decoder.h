@@ -266,10 +266,11 @@ fgq_status fgq_read_weights_w4(const fgq_w4* w, float* out, cudaStream_t stream)
  * A linear layer: y[p][m] = sum_k x[p][k] W[m][k] + bias[m].
  *   x    elements of `type`, [P][K] with K = w->cols, rows ldx elements apart (ldx >= K); bias fp32 [M] or NULL.
  *   y    out, elements of `type`, [P][M] contiguous, M = w->rows; may overlap x.
- * Codes and 16-bit tokens are exact operands of the products (fp32 tokens: three bf16 parts, exactly), a group's sum takes
- * its scale in fp32, y is rounded once.  More than 64 tokens of 16 bits run on fp16 operands on tcgen05: weights are exact there too within
- * 2^26 of their row's largest scale, bf16 tokens within 2^26 of their largest value (smaller ones are off by at most 2^-40
- * of those).  Scales 2^-100 to 2^100 there.  A token that holds NaN or Inf gives values that are not finite; other tokens are
+ * Few tokens: codes and 16-bit tokens are exact operands of the products (fp32 tokens: three bf16 parts, exactly), a group's sum
+ * takes its scale in fp32, y is rounded once.  More than 32 tokens, or more than 8 of fp32 with more than 2^22 weights, run on fp16
+ * operands on tcgen05: weights are exact there too within 2^26 of their row's largest scale, bf16 tokens within 2^26 of their largest
+ * value (smaller ones are off by at most 2^-39 of it), fp32 tokens within 2^-22 of each value (or 2^-39 of the largest).  Scales
+ * 2^-100 to 2^100 there, and outputs below 2^-100 may be 0.  A token that holds NaN or Inf gives values that are not finite; other tokens are
  * as without it.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type, bad weights, more than one matrix, ldx < K), FGQ_ERR_ALIGN (x or y
  * not aligned to their elements, codes or scales not 16-byte, bias not 4-byte aligned), FGQ_ERR_UNSUPPORTED (P, K or M above

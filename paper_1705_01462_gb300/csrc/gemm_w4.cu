@@ -5,14 +5,17 @@
 // warps turn the 128 channels x 128 columns of a stage into the operand, in the shared memory that the MMA reads.  (Expanded
 // in memory first, 4096 -> 14336 took 55 us at 64 tokens, 36 of them for the expansion.)
 // A block takes a tile of 128 channels and BN tokens, or a part of its K.  Warp roles:
-//   warps 0-15  weights: warp w the row tile w % 8 of every other stage, loaded two of its stages ahead; warps 0-7 then the
-//               epilogue: warp w reads TMEM lanes 32 (w % 4) .. (channels), columns BN / 2 (w / 4) .. (tokens), applies
-//               scales and bias and stores runs of 32 channels;
+//   warps 0-15  weights: warp w the row tile w % 8 of every other stage, loaded two of its stages ahead; warps 0-7 (fp32: up to
+//               all) then the epilogue: warp w reads TMEM lanes 32 (w % 4) .. (channels), an equal share of the columns (tokens),
+//               applies scales and bias and stores runs of 32 channels;
 //   warp 16     TMEM allocation and MMA issue;
 //   warp 17     TMA producer of the tokens.
 // Few tiles split K over blocks (fp32 partial sums, joined with scales and bias by a second kernel).
 // (Pairs of SMs, cta_group::2, halve the operands' traffic, but each stage's weights then take arrivals across the pair: 1.1 us a stage of
-// 64 columns, where this form takes %s.)
+// 64 columns, where this form takes 0.6 us for 128.)
+// fp32 tokens are two rows of fp16 that add up to them within 2^-22, and their sums leave the tensor memory for registers every
+// 256 columns: the tensor cores cut sums off, and over 4096 columns that took outputs to 2e-6 of 64-bit sums, over 16384 to 1e-5;
+// so it is 3e-7 for any length.  (2048 tokens, 4096 -> 4096: 139 us; without 133.)
 // Every wait is bounded; on expiry FGQ_ERR_TIMEOUT is recorded and each role leaves its loop; copies and MMAs under way are waited
 // for, and the tensor memory is freed.
 #include <cstring>
@@ -36,7 +39,7 @@ struct G4Cfg {
   // each operand in two halves of 64 columns (128-byte rows)
   static constexpr int A_HALF = G4_BM * 128, B_HALF = BN * 128, STAGE = 2 * (A_HALF + B_HALF);
   static constexpr int STAGES = BN == 256 ? 2 : (BN == 128 ? 3 : 4);
-  static constexpr int SMEM = 1024 + STAGES * STAGE + 8 * (3 * STAGES + 2) + 16;
+  static constexpr int SMEM = 1024 + STAGES * STAGE + 8 * (3 * STAGES + 5) + 16;
 };
 static_assert(G4Cfg<256>::SMEM <= 232448 && G4Cfg<128>::SMEM <= 232448 && G4Cfg<64>::SMEM <= 232448, "shared memory budget");
 
@@ -53,25 +56,31 @@ struct G4Args {
   int P, M, mtiles, ptiles, splits, ytype;
 };
 
-// The first `live` of 32 values, one a row of M elements.
-template <typename T>
-__device__ __forceinline__ void store_column(T* y, int M, int live, const uint32_t (&r)[32]) {
+// The first `live` of N values, one a row of M elements.
+template <typename T, int N>
+__device__ __forceinline__ void store_column(T* y, int M, int live, const float (&v)[N]) {
 #pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (i < live) from_float(__uint_as_float(r[i]), y[(int64_t)i * M]);
+  for (int i = 0; i < N; ++i)
+    if (i < live) from_float(v[i], y[(int64_t)i * M]);
 }
 
-template <int BN, int PER>
+constexpr int TAKE = 2;  // stages of fp32 sums (see above)
+// PARTS rows of x make a token (fp32: two).
+template <int BN, int PER, int PARTS>
 __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_constant__ G4Args a) {
   using C = G4Cfg<BN>;
   constexpr int S = C::STAGES;
+  // fp32: sums are taken from the tensor memory every TAKE stages, by TAKERS warps of COLUMNS columns each, from two places in turn
+  constexpr bool F32 = PARTS == 2;
+  constexpr int TAKERS = BN == 64 ? 8 : 16, COLUMNS = BN / (TAKERS / 4), TMEM = F32 ? 2 * BN : BN;
   extern __shared__ uint8_t smem_g4[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_g4) + 1023) & ~uintptr_t(1023));
   uint64_t* full_x = reinterpret_cast<uint64_t*>(smem + S * C::STAGE);  // the tokens have arrived
   uint64_t* full_w = full_x + S;   // the weights have been written
   uint64_t* empty = full_w + S;    // the MMAs have read both
-  uint64_t* acc_full = empty + S;  // the sums are complete
-  uint64_t* drain_bar = acc_full + 1;
+  uint64_t* acc_full = empty + S;   // [2] sums are complete
+  uint64_t* taken = acc_full + 2;  // [2] and in registers
+  uint64_t* drain_bar = taken + 2;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drain_bar + 1);
   volatile uint32_t* abort_flag = tmem_slot + 1;
   uint32_t* read = tmem_slot + 2;  // stages that MMAs were committed for
@@ -84,13 +93,16 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
       mbar_init(&full_w[i], G4_W_WARPS / 2);
       mbar_init(&empty[i], 1);
     }
-    mbar_init(acc_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&acc_full[i], 1);
+      mbar_init(&taken[i], TAKERS);
+    }
     mbar_init(drain_bar, 1);
     *abort_flag = 0;
     fence_mbar_init();
   }
   if (warp == G4_MMA_WARP) {
-    tmem_alloc(tmem_slot, BN);
+    tmem_alloc(tmem_slot, TMEM);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -107,6 +119,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
     *abort_flag = 1;
     record_error(a.err, FGQ_ERR_TIMEOUT);
   };
+  const int runs = F32 ? (n + TAKE - 1) / TAKE : 1;  // of stages that are summed in the tensor memory
   int issued = 0;  // by the producer
   bool ok = true;
 
@@ -132,7 +145,12 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
     const uint32_t idesc = idesc_f16_f32(G4_BM, BN);
     int j = 0;
     for (; j < n; ++j) {
-      const int st = j % S;
+      const int st = j % S, run = F32 ? j / TAKE : 0;
+      const bool fresh = F32 ? j % TAKE == 0 : j == 0;
+      if (F32 && fresh && run >= 2) {
+        ok = mbar_wait_warp(&taken[run & 1], ((run >> 1) & 1) ^ 1, tmo, abort_flag);
+        if (!ok) break;
+      }
       ok = mbar_wait_warp(&full_x[st], (j / S) & 1, tmo, abort_flag) && mbar_wait_warp(&full_w[st], (j / S) & 1, tmo, abort_flag);
       if (!ok) break;
       tc_fence_after();
@@ -142,26 +160,51 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
         for (int half = 0; half < 2; ++half) {
           const uint64_t ad = sdesc_k_sw128(A + half * C::A_HALF), bd = sdesc_k_sw128(B + half * C::B_HALF);
 #pragma unroll
-          for (int s = 0; s < 4; ++s) mma_f16(tmem, ad + 2 * s, bd + 2 * s, idesc, j > 0 || half > 0 || s > 0 ? 1u : 0u);
+          for (int s = 0; s < 4; ++s) mma_f16(tmem + (uint32_t)((run & 1) * BN), ad + 2 * s, bd + 2 * s, idesc, fresh && half == 0 && s == 0 ? 0u : 1u);
         }
         mma_commit(&empty[st]);
+        if (j == n - 1 || (F32 && j % TAKE == TAKE - 1)) mma_commit(&acc_full[run & 1]);
       }
       __syncwarp();
     }
-    if (ok) {
-      if (elect_one()) mma_commit(acc_full);
-    } else {
+    if (!ok) {
       if (lane == 0 && !*abort_flag) fail();
       if (elect_one()) mma_commit(drain_bar);
     }
     if (lane == 0) *read = (uint32_t)j;
   }
 
+  float acc[F32 ? COLUMNS / 2 : 1];
+  const int taker_column = (warp >> 2) * COLUMNS;
+  if (F32) {
+#pragma unroll
+    for (int i = 0; i < COLUMNS / 2; ++i) acc[i] = 0.0f;
+  }
+  int took = 0;  // runs that this warp has
+  auto take = [&]() {
+    const int at = took & 1;
+    ok = mbar_wait_warp(&acc_full[at], (took >> 1) & 1, tmo, abort_flag);
+    if (!ok) return;
+    tc_fence_after();
+#pragma unroll
+    for (int c = 0; c < COLUMNS; c += 32) {
+      uint32_t r[32];
+      tmem_ld32(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)(at * BN + taker_column + c), r);
+      tmem_ld_wait_regs(r);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[c / 2 + i] += __uint_as_float(r[2 * i]) + __uint_as_float(r[2 * i + 1]);
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&taken[at]);
+    ++took;
+  };
+
   if (warp < G4_W_WARPS) {
     const int d = warp & 7, first = warp >> 3, g = lane >> 2, t = lane & 3;  // every other stage
     const int rt = min(m0 / TILE_ROWS + d, a.w.rt - 1);  // a row tile past the last is read as the last
     const int64_t at = (int64_t)rt * a.w.ct + c0;
-    constexpr int AHEAD = 2;
+    constexpr int AHEAD = F32 && BN == 256 ? 1 : 2;  // 32 registers are the sums'
     Tile<PER> tile[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
@@ -205,46 +248,56 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&full_w[st]);
+        if (F32 && warp < TAKERS && took < j / TAKE) take();  // the run before this stage's
       }
     }
+    if (F32 && warp < TAKERS)
+      while (ok && took < runs) take();
     if (!ok && lane == 0 && !*abort_flag) fail();
   }
 
-  if (warp < G4_EPI_WARPS && ok) {
-    const int quarter = warp & 3, half = warp >> 2;
-    ok = mbar_wait_warp(acc_full, 0, tmo, abort_flag);
-    if (!ok && lane == 0 && !*abort_flag) fail();
+  if (warp < (F32 ? TAKERS : G4_EPI_WARPS) && ok) {
+    if (!F32) {
+      ok = mbar_wait_warp(acc_full, 0, tmo, abort_flag);
+      if (!ok && lane == 0 && !*abort_flag) fail();
+    }
     if (ok) {
       tc_fence_after();
-      const int m = m0 + 32 * quarter + lane;
+      constexpr int OWN = F32 ? COLUMNS : BN / 2, N = 32 / PARTS;  // columns of a warp, tokens of 32 columns
+      const int m = m0 + 32 * (warp & 3) + lane, column = (warp >> 2) * OWN;
       const bool mok = m < a.M;
       const float sw = mok ? pow2f(__ldcg(a.wexp + m) - 12) : 0.0f;
       const float bias = mok && a.bias ? __ldg(a.bias + m) : 0.0f;
-      const uint32_t ta = tmem + ((uint32_t)(32 * quarter) << 16) + (uint32_t)(half * (BN / 2));
-      const int pw = p0 + half * (BN / 2);
-#pragma unroll 1
-      for (int c = 0; c < BN / 2; c += 32) {
-        uint32_t r[32];
-        tmem_ld32(ta + c, r);
-        // the 32 tokens' scales, one a lane
-        const float sx = !a.scale ? 1.0f : (pw + c + lane < a.P ? __ldcg(a.scale + pw + c + lane) : 0.0f);
-        tmem_ld_wait_regs(r);
-        const int live = mok ? a.P - (pw + c) : 0;  // tokens of these 32 that there are
-        if (a.part) {
-          float* dst = a.part + ((int64_t)sp * a.P + pw + c) * a.M + m;
+#pragma unroll(F32 ? OWN / 32 : 1)
+      for (int c = 0; c < OWN; c += 32) {
+        const int tok = (p0 + column + c) / PARTS;
+        float v[N];
+        if constexpr (F32) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (i < live) dst[(int64_t)i * a.M] = __uint_as_float(r[i]);
+          for (int i = 0; i < N; ++i) v[i] = acc[c / 2 + i];
+        }
+        uint32_t r[32];
+        if (!F32) tmem_ld32(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + (uint32_t)(column + c), r);
+        // the tokens' scales, one a lane
+        const float sx = !a.scale ? 1.0f : (lane < N && tok + lane < a.P ? __ldcg(a.scale + tok + lane) : 0.0f);
+        if constexpr (!F32) {
+          tmem_ld_wait_regs(r);
+#pragma unroll
+          for (int i = 0; i < N; ++i) v[i] = __uint_as_float(r[i]);
+        }
+        const int live = mok ? a.P - tok : 0;  // how many tokens there are
+        if (a.part) {
+          store_column(a.part + ((int64_t)sp * a.P + tok) * a.M + m, a.M, live, v);
         } else {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(fmaf(__uint_as_float(r[i]), __shfl_sync(FULL_MASK, sx, i) * sw, bias));
-          const int64_t out = (int64_t)(pw + c) * a.M + m;
-          if (a.ytype == FGQ_F32)
-            store_column(static_cast<float*>(a.y) + out, a.M, live, r);
+          for (int i = 0; i < N; ++i) v[i] = fmaf(v[i], __shfl_sync(FULL_MASK, sx, i) * sw, bias);
+          const int64_t out = (int64_t)tok * a.M + m;
+          if constexpr (F32)
+            store_column(static_cast<float*>(a.y) + out, a.M, live, v);
           else if (a.ytype == FGQ_BF16)
-            store_column(static_cast<__nv_bfloat16*>(a.y) + out, a.M, live, r);
+            store_column(static_cast<__nv_bfloat16*>(a.y) + out, a.M, live, v);
           else
-            store_column(static_cast<__half*>(a.y) + out, a.M, live, r);
+            store_column(static_cast<__half*>(a.y) + out, a.M, live, v);
         }
       }
       tc_fence_before();
@@ -255,14 +308,14 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
   if (*abort_flag && warp == G4_TMA_WARP && lane == 0) {  // what is still under way: MMAs, then boxes that no MMA has read
     const int done = (int)*read;
     auto drain = [](uint64_t* bar, int phase) { mbar_wait_bounded(bar, (uint32_t)phase & 1u, 1u << 16); };
-    drain(done < n ? drain_bar : acc_full, 0);
+    drain(done < n ? drain_bar : &acc_full[(runs - 1) & 1], done < n ? 0 : (runs - 1) >> 1);
     for (int i = done > S ? done - S : 0; i < done; ++i) drain(&empty[i % S], i / S);
     for (int i = done; i < issued; ++i) drain(&full_x[i % S], i / S);
   }
   __syncthreads();
   if (warp == G4_MMA_WARP) {
     tc_fence_after();
-    tmem_dealloc(tmem, BN);
+    tmem_dealloc(tmem, TMEM);
   }
 }
 
@@ -287,25 +340,32 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ G4Arg
   }
 }
 
-template <int BN, int PER>
+template <int BN, int PER, int PARTS>
 fgq_status launch_g4_per(const G4Args& a, int grid, cudaStream_t s) {
-  if (!tc::smem_attr_once<gemm_w4_kernel<BN, PER>>(G4Cfg<BN>::SMEM)) return FGQ_ERR_CUDA;
-  return after_launch(launch_pdl(gemm_w4_kernel<BN, PER>, dim3(grid), dim3(G4_THREADS), G4Cfg<BN>::SMEM, s, a));
+  if (!tc::smem_attr_once<gemm_w4_kernel<BN, PER, PARTS>>(G4Cfg<BN>::SMEM)) return FGQ_ERR_CUDA;
+  return after_launch(launch_pdl(gemm_w4_kernel<BN, PER, PARTS>, dim3(grid), dim3(G4_THREADS), G4Cfg<BN>::SMEM, s, a));
 }
-template <int BN>
+template <int BN, int PARTS>
 fgq_status launch_g4(const G4Args& a, int grid, cudaStream_t s) {
-  if (a.w.per == 4) return launch_g4_per<BN, 4>(a, grid, s);
-  return a.w.per == 2 ? launch_g4_per<BN, 2>(a, grid, s) : launch_g4_per<BN, 1>(a, grid, s);
+  if (a.w.per == 4) return launch_g4_per<BN, 4, PARTS>(a, grid, s);
+  return a.w.per == 2 ? launch_g4_per<BN, 2, PARTS>(a, grid, s) : launch_g4_per<BN, 1, PARTS>(a, grid, s);
+}
+template <int PARTS>
+fgq_status launch_g4_tile(const G4Args& a, int bn, int grid, cudaStream_t s) {
+  if (bn == 256) return launch_g4<256, PARTS>(a, grid, s);
+  return bn == 128 ? launch_g4<128, PARTS>(a, grid, s) : launch_g4<64, PARTS>(a, grid, s);
 }
 
 }  // namespace
 
-ManyPlan plan_many(int P, int ct, int M) {
+ManyPlan plan_many(int P, int parts, int ct, int M) {
   ManyPlan g;
+  g.parts = parts;
+  const int64_t rows = (int64_t)P * parts;
   const int64_t sms = device_sms(), mt = ((int64_t)M + G4_BM - 1) / G4_BM;
-  g.bn = P <= 64 ? 64 : (P <= 128 || mt * ((P + 255) / 256) * 2 <= sms ? 128 : 256);
+  g.bn = rows <= 64 ? 64 : (rows <= 128 || mt * ((rows + 255) / 256) * 2 <= sms ? 128 : 256);
   // K split over blocks where there are fewer tiles than half the SMs, four tile columns each at least
-  const int64_t tiles = mt * ((P + g.bn - 1) / g.bn), by_k = ct / 4;
+  const int64_t tiles = mt * ((rows + g.bn - 1) / g.bn), by_k = ct / 4;
   int64_t splits = sms / tiles < by_k ? sms / tiles : by_k;
   g.splits = (int)(splits < 1 ? 1 : (splits > 16 ? 16 : splits));
   g.part_bytes = g.splits > 1 ? (size_t)g.splits * P * M * 4 : 0;
@@ -329,18 +389,19 @@ fgq_status launch_many(const ManyPlan& plan, const Matrix& w, const int* wexp, c
   a.M = M;
   a.ytype = ytype;
   a.mtiles = (int)(((int64_t)M + G4_BM - 1) / G4_BM);
-  a.ptiles = (P + plan.bn - 1) / plan.bn;
+  const int64_t rows = (int64_t)P * plan.parts;
+  a.ptiles = (int)((rows + plan.bn - 1) / plan.bn);
   a.splits = plan.splits;
   const int64_t tiles = (int64_t)a.mtiles * a.ptiles * a.splits;
   if (tiles > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
-  if (!make_map_2d(&a.x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x16, (uint64_t)K, (uint64_t)P, (uint64_t)pitch * 2, 64,
+  if (!make_map_2d(&a.x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x16, (uint64_t)K, (uint64_t)rows, (uint64_t)pitch * 2, 64,
                    (uint32_t)plan.bn, CU_TENSOR_MAP_SWIZZLE_128B))
     return FGQ_ERR_CUDA;
   const int grid = (int)tiles;
-  fgq_status st = plan.bn == 256 ? launch_g4<256>(a, grid, s) : (plan.bn == 128 ? launch_g4<128>(a, grid, s) : launch_g4<64>(a, grid, s));
+  fgq_status st = plan.parts == 2 ? launch_g4_tile<2>(a, plan.bn, grid, s) : launch_g4_tile<1>(a, plan.bn, grid, s);
   if (st == FGQ_OK && a.part) {
-    const int rows = (P + G4_JOIN - 1) / G4_JOIN;
-    const dim3 jg((unsigned)((M + 255) / 256), (unsigned)(rows < 65535 ? rows : 65535));
+    const int turns = (P + G4_JOIN - 1) / G4_JOIN;
+    const dim3 jg((unsigned)((M + 255) / 256), (unsigned)(turns < 65535 ? turns : 65535));
     st = after_launch(launch_pdl(join_kernel, jg, dim3(256), 0, s, a));
   }
   return st;

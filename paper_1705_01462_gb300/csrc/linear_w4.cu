@@ -1,8 +1,8 @@
 // Linear layers on 4-bit weights with a scale for each group: quantization, the product for few tokens, and operands
 // of the product for many.
 //
-// y[p][m] = sum_g s_mg sum_{k in g} c_mk x_pk + bias_m.  Codes c are exact matrix operands and 16-bit tokens are as they are
-// (fp32 ones in three bf16 parts), so a group's sum is that of exact products in fp32, and takes its scale in fp32.
+// y[p][m] = sum_g s_mg sum_{k in g} c_mk x_pk + bias_m.  For few tokens codes c are exact matrix operands and 16-bit tokens are as they
+// are (fp32 ones in three bf16 parts), so a group's sum is that of exact products in fp32, and takes its scale in fp32.
 #include <type_traits>
 
 #include "linear_internal.cuh"
@@ -113,7 +113,7 @@ __global__ void __launch_bounds__(256) copy_tokens_kernel(const T* __restrict__ 
 fgq_status launch_few(RowsArgs a, bool early, cudaStream_t s) {
   const int cpt = a.ytype == FGQ_F32 ? columns_per_token(3) : 1;
   const int64_t columns = (int64_t)a.P * cpt;
-  const int nt = columns <= 8 ? 1 : (columns <= 16 ? 2 : (columns <= 32 ? 4 : 8));
+  const int nt = columns <= 8 ? 1 : (columns <= 16 ? 2 : 4);
   const int tokens = 8 * nt / cpt;
   const int64_t tiles = ((int64_t)a.P + tokens - 1) / tokens;
   if (nt <= 2) {  // one tile of tokens: held in shared memory where it fits
@@ -126,17 +126,15 @@ fgq_status launch_few(RowsArgs a, bool early, cudaStream_t s) {
       return a.ytype == FGQ_BF16 ? launch_held_bf16(r, nt, plan, early, s) : launch_held_f16(r, nt, plan, early, s);
     }
   }
-  // two row tiles a warp where that leaves two blocks an SM
-  const int mt = nt <= 2 && (a.w.rt + 2 * WARPS - 1) / (2 * WARPS) * tiles >= 2 * device_sms() ? 2 : 1;
-  const int64_t items = (int64_t)((a.w.rt + WARPS * mt - 1) / (WARPS * mt)) * tiles;
+  const int64_t items = (int64_t)((a.w.rt + WARPS - 1) / WARPS) * tiles;
   if (items > INT32_MAX / 8) return FGQ_ERR_UNSUPPORTED;
   const RowsPlan plan = plan_rows(items, a.w.ct);
   a.items = (int)items;
   a.token_tiles = (int)tiles;
   a.splits = plan.splits;
   a.early = early;
-  if (a.ytype == FGQ_F32) return launch_rows_f32(a, nt, mt, plan.grid, early, s);
-  return a.ytype == FGQ_BF16 ? launch_rows_bf16(a, nt, mt, plan.grid, early, s) : launch_rows_f16(a, nt, mt, plan.grid, early, s);
+  if (a.ytype == FGQ_F32) return launch_rows_f32(a, nt, plan.grid, early, s);
+  return a.ytype == FGQ_BF16 ? launch_rows_bf16(a, nt, plan.grid, early, s) : launch_rows_f16(a, nt, plan.grid, early, s);
 }
 
 // ------------------------------------------------------------------ operands of the product for many tokens
@@ -201,12 +199,13 @@ __device__ __forceinline__ void prepare_weights(const Weights& a, int block) {
   }
 }
 
-// Tokens as fp16 rows, a block each: fp16 as they are; bf16 times 2^(14 - e), 2^e <= the row's largest magnitude < 2^(e + 1).
+// Tokens as fp16 rows, a block each: fp16 as they are; bf16 times 2^(14 - e), 2^e <= the row's largest magnitude < 2^(e + 1); fp32 so
+// scaled in two rows beside one another, the second what the first's rounding leaves (within 2^-22 of a value, 2^-39 of the largest).
 // A row with NaN or Inf: its scale is NaN, and so are its outputs.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) prepare_kernel(const T* __restrict__ x, int P, int K, int64_t ldx, __half* dst, int64_t pitch,
                                                       float* scale, const __grid_constant__ Weights w) {
-  constexpr bool BF = std::is_same<T, __nv_bfloat16>::value;
+  constexpr bool SCALED = !std::is_same<T, __half>::value, TWO = std::is_same<T, float>::value;
   __shared__ float red[8];
   pdl_trigger();
   if ((int)blockIdx.x >= P) {
@@ -215,9 +214,9 @@ __global__ void __launch_bounds__(256) prepare_kernel(const T* __restrict__ x, i
   }
   const int p = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const T* row = x + p * ldx;
-  __half* to = dst + p * pitch;
+  __half* to = dst + p * pitch * (TWO ? 2 : 1);
   float mul0 = 1.0f, mul1 = 1.0f;
-  if (BF) {
+  if (SCALED) {
     float mx = 0.0f;
     if (VEC) {
       for (int k = 8 * threadIdx.x; k < K; k += 2048) {
@@ -244,7 +243,7 @@ __global__ void __launch_bounds__(256) prepare_kernel(const T* __restrict__ x, i
     mul0 = bad ? 0.0f : pow2f((14 - e) / 2);
     mul1 = bad ? 0.0f : pow2f((14 - e) - (14 - e) / 2);
     if (bad) {
-      for (int64_t k = threadIdx.x; k < pitch; k += 256) to[k] = __float2half_rn(0.0f);
+      for (int64_t k = threadIdx.x; k < pitch * (TWO ? 2 : 1); k += 256) to[k] = __float2half_rn(0.0f);
       return;
     }
   } else if (threadIdx.x == 0) {
@@ -257,16 +256,23 @@ __global__ void __launch_bounds__(256) prepare_kernel(const T* __restrict__ x, i
       if (k < K) v.load(row + k);
       float f[8];
       v.unpack(f);
-      if (BF) {
+      if (SCALED) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = f[i] * mul0 * mul1;
       }
       store8(to + k, f);
+      if (TWO) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] -= __half2float(__float2half_rn(f[i]));
+        store8(to + pitch + k, f);
+      }
     }
   } else {
     for (int64_t k = threadIdx.x; k < pitch; k += 256) {
-      const float f = k < K ? to_float(row[k]) : 0.0f;
-      to[k] = __float2half_rn(BF ? f * mul0 * mul1 : f);
+      const float f = k < K ? to_float(row[k]) * mul0 * mul1 : 0.0f;
+      const __half h = __float2half_rn(f);
+      to[k] = h;
+      if (TWO) to[pitch + k] = __float2half_rn(f - __half2float(h));
     }
   }
 }
@@ -292,15 +298,16 @@ constexpr int64_t EXPAND_MIN_WEIGHTS = 1 << 23;
 
 fgq_status run_many(const void* x, int type, int P, int K, int64_t ldx, const fgq_w4* w, const float* bias, void* y, cudaStream_t s) {
   const int M = w->rows;
-  const bool expand = P >= EXPAND_MIN_P && (int64_t)K * M >= EXPAND_MIN_WEIGHTS;
+  const bool expand = type != FGQ_F32 && P >= EXPAND_MIN_P && (int64_t)K * M >= EXPAND_MIN_WEIGHTS;
   Weights wt = {matrix(w), nullptr, nullptr, nullptr, 0, M, 1};
-  const ManyPlan plan = plan_many(P, wt.w.ct, M);
+  const int parts = type == FGQ_F32 ? 2 : 1;
+  const ManyPlan plan = plan_many(P, parts, wt.w.ct, M);
   const GemmPlan pairs = expand ? plan_gemm_w8a8(P, K, M) : GemmPlan{};
   // fp16 tokens are operands as they are (expanded: where their rows are whole K-tiles beside one another)
-  const bool vec = direct_tokens(x, type, P, K, ldx);
+  const bool vec = K % 8 == 0 && aligned(x, 16) && (P == 1 || stride16(ldx, type));
   const bool direct = type == FGQ_F16 && vec && !overlap(x, y, type, P, K, M, ldx) && (!expand || (K == pairs.pitch && (P == 1 || ldx == K)));
   const int64_t pitch = expand ? pairs.pitch : (direct && P > 1 ? ldx : copied_pitch(K));
-  const size_t e_bytes = up256((size_t)wt.w.rt * TILE_ROWS * 4), x_bytes = direct ? 0 : up256((size_t)P * pitch * 2);
+  const size_t e_bytes = up256((size_t)wt.w.rt * TILE_ROWS * 4), x_bytes = direct ? 0 : up256((size_t)P * parts * pitch * 2);
   const size_t s_bytes = direct && !expand ? 0 : up256((size_t)P * 4), w_bytes = expand ? up256((size_t)M * pitch * 2) : 0;
   const size_t p_bytes = expand ? pairs.part_bytes : plan.part_bytes;
   uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(e_bytes + x_bytes + s_bytes + w_bytes + p_bytes, s));
@@ -326,6 +333,10 @@ fgq_status run_many(const void* x, int type, int P, int K, int64_t ldx, const fg
       const __nv_bfloat16* xb = static_cast<const __nv_bfloat16*>(x);
       vec ? prepare_kernel<__nv_bfloat16, true><<<grid, 256, 0, s>>>(xb, tokens, K, ldx, x16, pitch, xscale, wt)
           : prepare_kernel<__nv_bfloat16, false><<<grid, 256, 0, s>>>(xb, tokens, K, ldx, x16, pitch, xscale, wt);
+    } else if (type == FGQ_F32) {
+      const float* xf = static_cast<const float*>(x);
+      vec ? prepare_kernel<float, true><<<grid, 256, 0, s>>>(xf, tokens, K, ldx, x16, pitch, xscale, wt)
+          : prepare_kernel<float, false><<<grid, 256, 0, s>>>(xf, tokens, K, ldx, x16, pitch, xscale, wt);
     } else {
       const __half* xh = static_cast<const __half*>(x);
       vec ? prepare_kernel<__half, true><<<grid, 256, 0, s>>>(xh, tokens, K, ldx, x16, pitch, xscale, wt)
@@ -354,6 +365,13 @@ __global__ void __launch_bounds__(256) bias_kernel(const float* bias, void* y, i
 // Tokens of 16 bits up to which the kernels of few tokens run.  bf16, us there and in gemm_w4.cu: 16 tokens, 4096 -> 4096 10.0 and 12.0, 4096 ->
 // 14336 14.5 and 25.0; 32 tokens 9.5 and 12.2, 28.1 and 25.3, 8192 -> 8192 27.2 and 28.2; 33 tokens 25.9 and 12.3, 49.8 and 25.3.
 constexpr int FEW_MAX_P = 32;
+// fp32: 8 tokens, or 32 of a small matrix.  us there and in gemm_w4.cu: 8 tokens, 4096 -> 4096 8.7 and 13.1, 4096 -> 14336 24.0 and 26.9; 16 tokens
+// 13.1 and 13.3, 40.7 and 26.9; 24 tokens 22.1 and 13.4, 2048 -> 4096 13.5 and 10.8, but 2048 -> 2048 8.5 and 10.4.
+constexpr int FEW_MAX_P_F32 = 8;
+constexpr int64_t FEW_SMALL = 1 << 22;
+int few_tokens(int type, int K, int M) {
+  return type == FGQ_F32 && (int64_t)K * M > FEW_SMALL ? FEW_MAX_P_F32 : FEW_MAX_P;
+}
 
 }  // namespace
 
@@ -431,7 +449,7 @@ fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx,
     bias_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, stream>>>(bias, y, type, P, M);
     return after_launch();
   }
-  if (type != FGQ_F32 && P > FEW_MAX_P) return run_many(x, type, P, K, P > 1 ? ldx : 0, w, bias, y, stream);
+  if (P > few_tokens(type, K, M)) return run_many(x, type, P, K, P > 1 ? ldx : 0, w, bias, y, stream);
   RowsArgs a = {};
   a.w = matrix(w), a.x = {x, P > 1 ? ldx : 0, K}, a.bias = bias, a.y = y, a.P = P, a.M = M, a.ytype = type;
   if (direct_tokens(x, type, P, K, ldx) && !overlap(x, y, type, P, K, M, ldx)) return launch_few(a, false, stream);

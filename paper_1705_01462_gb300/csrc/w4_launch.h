@@ -6,10 +6,10 @@
 namespace fgq {
 namespace w4 {
 
-// Columns of tokens that a block takes: 8 nt.  A linear layer (mt row tiles a warp: 2 with nt up to 2, else 1).
-fgq_status launch_rows_bf16(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s);
-fgq_status launch_rows_f16(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s);
-fgq_status launch_rows_f32(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s);
+// Columns of tokens that a block takes: 8 nt, nt 1, 2 or 4.  A linear layer.
+fgq_status launch_rows_bf16(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s);
+fgq_status launch_rows_f16(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s);
+fgq_status launch_rows_f32(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s);
 // Gate and up of a gated layer.
 fgq_status launch_gated_bf16(const RowsArgs& a, int nt, unsigned grid, cudaStream_t s);
 fgq_status launch_gated_f16(const RowsArgs& a, int nt, unsigned grid, cudaStream_t s);
@@ -52,13 +52,10 @@ fgq_status launch_rows_per(const RowsArgs& a, unsigned grid, bool chained, cudaS
 }
 
 template <typename T, int PARTS>
-fgq_status launch_rows_type(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s) {
-  if (nt == 1 && mt == 2) return launch_rows_per<T, 2, 1, PARTS, false, 1, 3>(a, grid, chained, s);
+fgq_status launch_rows_type(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s) {
   if (nt == 1) return launch_rows_per<T, 1, 1, PARTS, false, 1, 4>(a, grid, chained, s);
-  if (nt == 2 && mt == 2) return launch_rows_per<T, 2, 2, PARTS, false, 1, 3>(a, grid, chained, s);
   if (nt == 2) return launch_rows_per<T, 1, 2, PARTS, false, 1, 4>(a, grid, chained, s);
-  if (nt == 4) return launch_rows_per<T, 1, 4, PARTS, false, 1, 4>(a, grid, chained, s);
-  return launch_rows_per<T, 1, 8, PARTS, false, 1, 3>(a, grid, chained, s);
+  return launch_rows_per<T, 1, 4, PARTS, false, 1, 4>(a, grid, chained, s);
 }
 
 }  // namespace w4

@@ -31,11 +31,11 @@ __device__ __forceinline__ uint4 scaled_codes(uint32_t w, uint32_t s) {
 // How a product is laid out: tile of tokens, splits of K, bytes of its partial sums.
 struct ManyPlan {
   size_t part_bytes;
-  int bn, splits;
+  int bn, splits, parts;
 };
-ManyPlan plan_many(int P, int ct, int M);
+ManyPlan plan_many(int P, int parts, int ct, int M);
 
-// x16: fp16 tokens, `pitch` elements apart (16-byte aligned rows), written or older than the kernel before; scale: what each is
+// x16: fp16 tokens, each in `plan.parts` rows that add up to it, `pitch` elements apart (16-byte aligned rows), written or older than the kernel before; scale: what each is
 // multiplied by at the end, or nullptr (1); wexp: the exponent of each row's largest scale, for all rows of the weights' tiles.
 fgq_status launch_many(const ManyPlan& plan, const Matrix& w, const int* wexp, const void* x16, int64_t pitch, int K, const float* scale,
                        int P, int M, float* part, const float* bias, void* y, int ytype, cudaStream_t s);

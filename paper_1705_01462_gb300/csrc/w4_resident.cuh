@@ -40,11 +40,12 @@ constexpr int RES_SMEM = 226 * 1024;  // a kilobyte is left for what is not dyna
 // Warps of a block at most: 80 registers a thread, or 96 where two row tiles meet 16 columns.
 constexpr int resident_warps(int mt, int nt) { return mt * nt >= 4 ? 20 : 24; }
 
+// MT: 2 tiles of MODE_GATED, gate's and up's, else 1.
 template <typename T, int MT, int NT, int PER, int PARTS, int MODE, int AHEAD>
 __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(const __grid_constant__ ResidentArgs a) {
   constexpr int CPT = columns_per_token(PARTS), TOKENS = 8 * NT / CPT, COLS = 8 * NT;
   const int STAGE = a.cols * 256;  // bytes of a tile column's tokens
-  constexpr int TILES = MODE == MODE_GATED ? 1 : MT;  // row tiles of an item
+  static_assert(MT == (MODE == MODE_GATED ? 2 : 1), "tiles of an item");
   constexpr int LD = 16 * MT + 1, FRAGMENT = COLS * LD, TB = tile_bytes<PER>(), SLOT = MT * TB;
   extern __shared__ __align__(16) uint8_t w4_smem[];
   __shared__ int row_of[TOKENS];    // MODE_GATED: the tokens' rows
@@ -61,8 +62,8 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
   } else if (MODE == MODE_DOWN) {
     pdl_trigger();
   }
-  const int groups = (a.w.rt + TILES - 1) / TILES;  // items of a unit
-  const int items = MODE == MODE_LINEAR || a.items > 0 ? a.items : __ldcg(a.nunits) * groups;
+  const int rt = a.w.rt;  // items of a unit
+  const int items = MODE == MODE_LINEAR || a.items > 0 ? a.items : __ldcg(a.nunits) * rt;
   const int run = (items + (int)gridDim.x - 1) / (int)gridDim.x;
   const int i0 = (int)blockIdx.x * run, i1 = min(i0 + run, items);
   if (i0 >= i1) return;
@@ -82,9 +83,9 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
       s.count = i1 - i;
       s.u = make_int4(0, 0, min(TOKENS, a.P), 0);
     } else {
-      const int unit = i / groups;
-      s.item = i - unit * groups;
-      s.count = min(i1 - i, groups - s.item);
+      const int unit = i / rt;
+      s.item = i - unit * rt;
+      s.count = min(i1 - i, rt - s.item);
       s.u = __ldcg(reinterpret_cast<const int4*>(a.units) + unit);
     }
     s.each = s.count * ct / W;
@@ -97,13 +98,10 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
   const uint8_t *codes = nullptr, *scales = nullptr;
   const int64_t up_codes = MODE == MODE_GATED ? a.up.codes - a.w.codes : 0;
   const int64_t up_scales = MODE == MODE_GATED ? reinterpret_cast<const uint8_t*>(a.up.scales) - reinterpret_cast<const uint8_t*>(a.w.scales) : 0;
-  int lkt = 0, lrow = 0, left = 0;
+  int left = 0;
   const uint32_t ring0 = ring_at + 16 * lane;
   auto begin = [&](const Segment& s) {
-    const int i = s.q0 / ct;
-    lkt = s.q0 - i * ct;
-    lrow = (s.item + i) * TILES;
-    const int64_t at = ((int64_t)s.u.x * a.w.rt + lrow) * ct + lkt;
+    const int64_t at = ((int64_t)s.u.x * rt + s.item) * ct + s.q0;  // an item's tiles follow the last's
     codes = a.w.codes + at * TILE_BYTES + 16 * lane;
     scales = reinterpret_cast<const uint8_t*>(a.w.scales) + at * (TILE_ROWS * PER * 2) + 16 * lane;
     left = s.q1 - s.q0;
@@ -113,23 +111,9 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
     if (left > 0) {
       --left;
       copy_tile<PER>(to, codes, scales, lane);
-      if (MODE == MODE_GATED) {
-        copy_tile<PER>(to + TB, codes + up_codes, scales + up_scales, lane);
-      } else {
-#pragma unroll
-        for (int mt = 1; mt < MT; ++mt) {  // a row tile past the last is read as the last
-          const int64_t on = lrow + mt < a.w.rt ? (int64_t)mt * ct : 0;
-          copy_tile<PER>(to + mt * TB, codes + on * TILE_BYTES, scales + on * (TILE_ROWS * PER * 2), lane);
-        }
-      }
+      if (MODE == MODE_GATED) copy_tile<PER>(to + TB, codes + up_codes, scales + up_scales, lane);
       codes += TILE_BYTES;
       scales += TILE_ROWS * PER * 2;
-      if (TILES > 1 && ++lkt == ct) {
-        lkt = 0;
-        lrow += TILES;
-        codes += (int64_t)(TILES - 1) * ct * TILE_BYTES;
-        scales += (int64_t)(TILES - 1) * ct * (TILE_ROWS * PER * 2);
-      }
     }
     cp_async_commit();
   };
@@ -208,7 +192,7 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
   // what becomes of the finished sums of row r of an item and token tok: of gate and up, or of one matrix.  MODE_GATED: the
   // hidden value's magnitude
   auto finish = [&](int item, int r, int tok, float v, float u) {
-    const int m = item * 16 * TILES + r;
+    const int m = item * TILE_ROWS + r;
     v *= Operand<T>::BACK;
     if (MODE == MODE_GATED) {
       u *= Operand<T>::BACK;
@@ -242,30 +226,28 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
   // this lane's sums as those of tokens
   auto whole = [&](int item) {
 #pragma unroll
-    for (int mt = 0; mt < TILES; ++mt)
+    for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
+      for (int half = 0; half < 2; ++half) {
+        float s[2], u[2];
+        unpack_f2(sum[0][nt][half], s[0], s[1]);
+        unpack_f2(sum[MT - 1][nt][half], u[0], u[1]);
+        const int r = g + 8 * half;
+        if constexpr (CPT == 1) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float s[2], u[2];
-          unpack_f2(sum[mt][nt][half], s[0], s[1]);
-          unpack_f2(sum[MODE == MODE_GATED ? MT - 1 : mt][nt][half], u[0], u[1]);
-          const int r = 16 * mt + g + 8 * half;
-          if constexpr (CPT == 1) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              if (8 * nt + 2 * t + e < now.u.z) big[nt][e] = max(big[nt][e], __float_as_uint(finish(item, r, 8 * nt + 2 * t + e, s[e], u[e])));
-          } else if constexpr (CPT == 2) {
-            if (4 * nt + t < now.u.z) finish(item, r, 4 * nt + t, s[0] + s[1], u[0] + u[1]);
-          } else {  // three parts, and a column that is zero
-            float v = s[0] + s[1], w = u[0] + u[1];
-            v += __shfl_xor_sync(FULL_MASK, v, 1);
-            if (MODE == MODE_GATED) w += __shfl_xor_sync(FULL_MASK, w, 1);
-            const int tok = 2 * nt + (t >> 1);
-            if ((t & 1) == 0 && tok < now.u.z) finish(item, r, tok, v, w);
-          }
+          for (int e = 0; e < 2; ++e)
+            if (8 * nt + 2 * t + e < now.u.z) big[nt][e] = max(big[nt][e], __float_as_uint(finish(item, r, 8 * nt + 2 * t + e, s[e], u[e])));
+        } else if constexpr (CPT == 2) {
+          if (4 * nt + t < now.u.z) finish(item, r, 4 * nt + t, s[0] + s[1], u[0] + u[1]);
+        } else {  // three parts, and a column that is zero
+          float v = s[0] + s[1], w = u[0] + u[1];
+          v += __shfl_xor_sync(FULL_MASK, v, 1);
+          if (MODE == MODE_GATED) w += __shfl_xor_sync(FULL_MASK, w, 1);
+          const int tok = 2 * nt + (t >> 1);
+          if ((t & 1) == 0 && tok < now.u.z) finish(item, r, tok, v, w);
         }
       }
+    }
   };
   auto fragment = [&](int slot) {
     float* to = sums + (2 * warp + slot) * FRAGMENT;
@@ -344,7 +326,7 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
     }
     __syncthreads();
     // a cut item is put together by the first warp whose part begins inside it
-    constexpr int ROWS = 16 * TILES;
+    constexpr int ROWS = TILE_ROWS;
     const int it = now.q0 / ct, lo = it * ct, hi = lo + ct;
     if (warp > 0 && now.q0 > lo && now.q0 < now.q1 && now.begins(warp - 1) <= lo) {
       int last = warp;  // the last warp with a part of it

@@ -4,8 +4,8 @@
 namespace fgq {
 namespace w4 {
 
-fgq_status launch_rows_bf16(const RowsArgs& a, int nt, int mt, unsigned grid, bool chained, cudaStream_t s) {
-  return launch_rows_type<__nv_bfloat16, 1>(a, nt, mt, grid, chained, s);
+fgq_status launch_rows_bf16(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s) {
+  return launch_rows_type<__nv_bfloat16, 1>(a, nt, grid, chained, s);
 }
 fgq_status launch_gated_bf16(const RowsArgs& a, int nt, unsigned grid, cudaStream_t s) {
   if (nt == 1) return launch_rows_per<__nv_bfloat16, 2, 1, 1, true, 2, 3>(a, grid, true, s);

@@ -180,10 +180,13 @@ def weights(c, s, G, dev, fill=0):
                          *c.shape[-2:])
 
 
-def beta(K, G, many=False):
+def beta(K, G, many=False, dtype=None):
     """Error of sums of K exact products, of the sum of their magnitudes.  A matrix instruction adds 16 products to a sum with
     each term cut off at 2^-24 of the largest at worst: 17 2^-24 an instruction and G / 16 a group; groups, warps, parts and a
-    cluster's blocks are added in fp32 (many: one sum over K, cut off once in 16 products by at most 2^-23, and up to 16 splits)."""
+    cluster's blocks are added in fp32 (many: one sum over K, cut off once in 16 products by at most 2^-23, and up to 16 splits; fp32: runs of 256
+    columns of two parts, 17 2^-24 in 16 products as above, the runs added in fp32, and 2^-22 = 4 u that the parts leave out)."""
+    if many and dtype == "f32":
+        return (17 * 16 + K / 256 + 24) * u
     if many:
         return K * 2.0 ** -27 + 20 * u
     return (17 * G / 16 + K / G + 40) * u
@@ -196,7 +199,7 @@ def in_range(y, dtype):
 
 def linear(x, w, G, bias, dtype, many=False):
     y = x @ w.T
-    e = beta(x.shape[1], G, many) * (np.abs(x) @ np.abs(w).T)
+    e = beta(x.shape[1], G, many, dtype) * (np.abs(x) @ np.abs(w).T)
     if many:  # bf16 tokens below 2^-28 of their largest and weights below 2^-28 of their row's lose bits
         e = e + 2.0 ** -36 * np.abs(x).max(1, keepdims=True) * np.abs(w).sum(1) + 2.0 ** -36 * np.abs(w).max(1) * np.abs(x).sum(1, keepdims=True)
     if bias is not None:

@@ -9,8 +9,12 @@ from paper_1705_01462_gb300 import fgq
 
 pytestmark = pytest.mark.gpu
 
-# tokens from which 16-bit types may run on the product for many tokens: its bound is the wider one
+# tokens from which the product for many tokens may run: its bound is the wider one
 MANY = 33
+
+
+def many(dtype, P, K, M):
+    return P >= MANY or (dtype == "f32" and P >= 9 and K * M > 1 << 22)
 
 
 @pytest.mark.parametrize("G", [32, 64, 128])
@@ -50,7 +54,7 @@ def run(rng, P, K, M, G, dtype, bias=True, ld=0, fill=0, spread=0.3, scale=1.0):
     y = fgq.fgq_linear_w4(x.to(dev())[:, :K], w, bias=None if b is None else torch.from_numpy(b).to(dev()))
     assert fgq.fgq_stream_status() == fgq.FGQ_OK
     want, bound = R.linear(x64[:, :K], R.dequantize_w4(c, s, G), G, None if b is None else b.astype(np.float64), dtype,
-                           many=dtype != "f32" and P >= MANY)
+                           many=many(dtype, P, K, M))
     R.check(y.double().cpu().numpy(), want, bound, f"linear {P} x {K} -> {M}")
     return y
 
@@ -61,6 +65,55 @@ def run(rng, P, K, M, G, dtype, bias=True, ld=0, fill=0, spread=0.3, scale=1.0):
                                    (17, 257, 50), (31, 2048, 48), (33, 640, 100), (64, 384, 31), (65, 384, 300), (130, 1000, 257)])
 def test_products(dtype, G, P, K, M):
     run(np.random.default_rng(P * K + M), P, K, M, G, dtype, bias=M % 2 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("G,P,K,M", [(64, 9, 4096, 1100), (32, 16, 8192, 520), (128, 40, 8200, 130), (64, 70, 2048, 2100),
+                                     (32, 130, 1000, 4300), (128, 300, 1111, 3800), (64, 260, 5120, 8200), (64, 1025, 520, 8000)])
+def test_many(dtype, G, P, K, M):
+    """Tiles of 64, 128 and 256 tokens, K in one piece and in parts, the last of them short."""
+    run(np.random.default_rng(P + K), P, K, M, G, dtype, bias=M % 200 == 0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("P,K,M,ld", [(1025, 4096, 2056, 0), (1030, 2500, 3360, 3), (1100, 2048, 4112, 8)])
+def test_expanded(dtype, P, K, M, ld):
+    """So many tokens that the weights are expanded once: tokens in place, copied, and with rows apart."""
+    run(np.random.default_rng(P), P, K, M, 64, dtype, bias=ld > 0, ld=ld)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("P,K", [(1, 16384), (4, 14336), (7, 12000), (8, 16400), (12, 6000), (16, 9000), (32, 9000)])
+def test_long_rows(dtype, P, K):
+    """Tokens that a block's shared memory holds only in part, or not at all."""
+    for M, G in ((100, 64), (2500, 32)):
+        run(np.random.default_rng(K), P, K, M, G, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("P,K,M", [(40, 4096, 260), (200, 2048, 2100), (1000, 1024, 8200)])
+def test_waits_that_run_out(dtype, P, K, M):
+    """A limit of a few microseconds for each wait: an error status, and the next calls are right."""
+    rng = np.random.default_rng(P)
+    x = R.rng_tensor(rng, (P, K), dtype)[0].to(dev())
+    w = R.weights(*R.random_w4(rng, (M, K), 64), 64, dev())
+    want = fgq.fgq_linear_w4(x, w)
+    assert fgq.fgq_stream_status() == fgq.FGQ_OK
+    seen = set()
+    for limit in (0, 1, 2, 3, 4, 6, 8, 12, 16, 24, 40, 80):
+        for _ in range(3):
+            prev = fgq.fgq_debug_set_wait_limit_us(limit)
+            try:
+                y = fgq.fgq_linear_w4(x, w)
+            finally:
+                fgq.fgq_debug_set_wait_limit_us(prev)
+            status = fgq.fgq_stream_status()
+            assert status in (fgq.FGQ_OK, fgq.FGQ_ERR_TIMEOUT)
+            assert status != fgq.FGQ_OK or torch.equal(y, want)
+            seen.add(status)
+            assert torch.equal(fgq.fgq_linear_w4(x, w), want)
+            assert fgq.fgq_stream_status() == fgq.FGQ_OK
+    assert fgq.FGQ_ERR_TIMEOUT in seen
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])

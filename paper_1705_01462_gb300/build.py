@@ -21,7 +21,7 @@ SOURCES = ["api.cu", "ternarize.cu", "ternarize_threshold.cu", "quantize.cu", "g
            "gemm_simt_g8.cu", "gemm_simt_g32.cu", "gemm_simt_g128.cu", "gemm_tc.cu", "gemm_tc4.cu", "gemm_fold.cu", "gemm_dense.cu",
            "gemm_few.cu", "gemv.cu", "elementwise.cu", "kv_cache.cu", "kv_attention.cu", "kv_prompt.cu", "kv_attention_d64.cu",
            "kv_attention_d128.cu", "kv_attention_d256.cu", "linear_w8a8.cu", "gemm_w8a8.cu",
-           "rope.cu", "add_norm.cu", "linear_w4.cu", "gemm_w4.cu", "w4_rows_bf16.cu", "w4_rows_f16.cu", "w4_rows_f32.cu", "moe_w4.cu"]
+           "rope.cu", "add_norm.cu", "linear_w4.cu", "gemm_w4.cu", "gemm_w4_experts.cu", "w4_rows_bf16.cu", "w4_rows_f16.cu", "w4_rows_f32.cu", "moe_w4.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fno-strict-aliasing",
               "--expt-relaxed-constexpr", "-I" + INCLUDE]

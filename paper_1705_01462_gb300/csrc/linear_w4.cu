@@ -199,82 +199,16 @@ __device__ __forceinline__ void prepare_weights(const Weights& a, int block) {
   }
 }
 
-// Tokens as fp16 rows, a block each: fp16 as they are; bf16 times 2^(14 - e), 2^e <= the row's largest magnitude < 2^(e + 1); fp32 so
-// scaled in two rows beside one another, the second what the first's rounding leaves (within 2^-22 of a value, 2^-39 of the largest).
-// A row with NaN or Inf: its scale is NaN, and so are its outputs.
+// A block a token, the blocks past them for the weights.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) prepare_kernel(const T* __restrict__ x, int P, int K, int64_t ldx, __half* dst, int64_t pitch,
                                                       float* scale, const __grid_constant__ Weights w) {
-  constexpr bool SCALED = !std::is_same<T, __half>::value, TWO = std::is_same<T, float>::value;
-  __shared__ float red[8];
   pdl_trigger();
-  if ((int)blockIdx.x >= P) {
-    prepare_weights(w, (int)blockIdx.x - P);
-    return;
-  }
-  const int p = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const T* row = x + p * ldx;
-  __half* to = dst + p * pitch * (TWO ? 2 : 1);
-  float mul0 = 1.0f, mul1 = 1.0f;
-  if (SCALED) {
-    float mx = 0.0f;
-    if (VEC) {
-      for (int k = 8 * threadIdx.x; k < K; k += 2048) {
-        Raw8<T> v;
-        v.load(row + k);
-        float lo, hi;
-        v.extremes(lo, hi);
-        mx = max_nan(mx, max_nan(-lo, hi));
-      }
-    } else {
-      for (int k = threadIdx.x; k < K; k += 256) mx = max_nan(mx, fabsf(to_float(row[k])));
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(FULL_MASK, mx, o));
-    if (lane == 0) red[warp] = mx;
-    __syncthreads();
-    mx = red[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) mx = max_nan(mx, red[i]);
-    int e = (int)(__float_as_uint(mx) >> 23 & 255u) - 127;
-    if (e < -126) e = -126;
-    const bool bad = nonfinite(mx);
-    if (threadIdx.x == 0) scale[p] = bad ? __uint_as_float(0x7fc00000u) : pow2f(e - 14);
-    mul0 = bad ? 0.0f : pow2f((14 - e) / 2);
-    mul1 = bad ? 0.0f : pow2f((14 - e) - (14 - e) / 2);
-    if (bad) {
-      for (int64_t k = threadIdx.x; k < pitch * (TWO ? 2 : 1); k += 256) to[k] = __float2half_rn(0.0f);
-      return;
-    }
-  } else if (threadIdx.x == 0) {
-    scale[p] = 1.0f;
-  }
-  if (VEC) {
-    for (int k = 8 * threadIdx.x; k < pitch; k += 2048) {
-      Raw8<T> v;
-      v.zero();
-      if (k < K) v.load(row + k);
-      float f[8];
-      v.unpack(f);
-      if (SCALED) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = f[i] * mul0 * mul1;
-      }
-      store8(to + k, f);
-      if (TWO) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] -= __half2float(__float2half_rn(f[i]));
-        store8(to + pitch + k, f);
-      }
-    }
-  } else {
-    for (int64_t k = threadIdx.x; k < pitch; k += 256) {
-      const float f = k < K ? to_float(row[k]) * mul0 * mul1 : 0.0f;
-      const __half h = __float2half_rn(f);
-      to[k] = h;
-      if (TWO) to[pitch + k] = __float2half_rn(f - __half2float(h));
-    }
-  }
+  const int p = blockIdx.x;
+  if (p < P)
+    token_row<T, VEC>(x + p * ldx, K, dst + p * pitch * (std::is_same<T, float>::value ? 2 : 1), pitch, scale + p);
+  else
+    prepare_weights(w, p - P);
 }
 
 __global__ void __launch_bounds__(256) ones_kernel(float* p, int n) {

@@ -6,21 +6,24 @@
 //   route_kernel    a cluster four tokens: products of 8 elements in fp32, their sums as pairs of fp32 (two-sum), so that a
 //                   logit is off by about one fp32 rounding and the choice is that of 64-bit sums but for near ties; the largest
 //                   one by one, and their weights;
-//   group_kernel    (more than four tokens, or choices that are given) one block: choices sorted by expert, and cut into units of up to 8 to 32 tokens that share an expert;
-//   rows_kernel     (w4_rows.cuh) 128 rows of gate and the same of up, for one unit: silu(gate) up, left as bf16 parts;
-//   down_kernel     128 rows of down, for all units: sums stay with the block, or its cluster, so that no order depends on which
-//                   comes first.
+//   group_kernel    (more than four tokens, or choices that are given) one block: choices sorted by expert, and cut into units of
+//                   tokens that share an expert;
+//   resident_kernel (w4_resident.cuh) 16 rows of gate and of up for a unit of up to 8 tokens: silu(gate) up in fp32; then of down;
+//   or, with more than 8 choices an expert, the kernels of gemm_w4_experts.cu for units of up to 64 or 128;
+//   combine_kernel  each token's choices by their weights, in their order.
 // Bound by the bytes of the experts' weights, each read once (again from L2 for each further unit of an expert).
 #include <type_traits>
 
 #include "w4_launch.h"
+#include "w4_many.h"
 
 namespace fgq {
 namespace w4 {
 namespace {
 
 constexpr int MAX_EXPERTS = 1024, MAX_TOP = 32;
-constexpr int CHUNK = 128;  // tokens of a pass
+constexpr int MAX_CHOICES = 4096;  // of a pass: what group_kernel holds
+static_assert(MAX_CHOICES < 1 << 16 && MAX_CHOICES >= MAX_TOP, "group_kernel's sums");
 
 // ------------------------------------------------------------------ routing
 struct RouteArgs {
@@ -34,7 +37,7 @@ struct RouteArgs {
   Choice* choices;
   int32_t* places;
   unsigned* tops;
-  int* nunits;
+  int* nunits;  // units, choices
   int P, K, E, top, score, renormalize;
   float scale;
 };
@@ -269,7 +272,7 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
     for (int j = lane; j < n; j += 32) u += ahead[j];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) u += __shfl_xor_sync(FULL_MASK, u, o);
-    if (lane == 0) *a.nunits = u;
+    if (lane == 0) a.nunits[0] = u, a.nunits[1] = n;
   }
 }
 
@@ -278,8 +281,8 @@ constexpr int GR_THREADS = 1024;
 
 __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, const float* weights, int A, int top, int E, int cap,
                                                            Unit* units, Choice* choices, int32_t* places, unsigned* tops, int* nunits) {
-  __shared__ int count[MAX_EXPERTS], start[MAX_EXPERTS], id[CHUNK * MAX_TOP], warp_sums[GR_THREADS / 32];
-  __shared__ float weight[CHUNK * MAX_TOP];
+  __shared__ int count[MAX_EXPERTS], start[MAX_EXPERTS], id[MAX_CHOICES], warp_sums[GR_THREADS / 32];
+  __shared__ float weight[MAX_CHOICES];
   pdl_trigger();
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   count[t] = 0;
@@ -296,7 +299,7 @@ __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, c
       places[i] = -1;
   }
   __syncthreads();
-  // choices and units before expert t, both in one word: at most 4096 each
+  // choices and units before expert t, both in one word
   const int n = count[t], mine = n | (n + cap - 1) / cap << 16;  // 0 from E on
   int s = mine;
 #pragma unroll
@@ -316,7 +319,7 @@ __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, c
   const int first = before & 0xffff, u0 = before >> 16;
   start[t] = first;
   for (int u = 0; u * cap < n; ++u) units[u0 + u] = {t, first + u * cap, min(cap, n - u * cap), 0};
-  if (t == 0) *nunits = total >> 16;
+  if (t == 0) nunits[0] = total >> 16, nunits[1] = total & 0xffff;
   __syncthreads();
   for (int e = warp; e < E; e += GR_THREADS / 32) {  // each expert's choices in the order they came
     const int want = count[e];
@@ -333,180 +336,6 @@ __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, c
       found += __popc(m);
     }
   }
-}
-
-// ------------------------------------------------------------------ down
-struct DownArgs {
-  Matrix down;
-  const uint16_t* h;
-  int64_t hpitch;
-  const Unit* units;
-  const Choice* choices;
-  const int* nunits;
-  void* y;
-  int P, K, ytype, splits;
-};
-
-constexpr int DOWN_ROWS = WARPS * TILE_ROWS;
-constexpr int DOWN_LD = DOWN_ROWS + 8;  // eight lanes that hold two tokens' rows meet different banks
-
-// A block takes 128 rows of down, 16 a warp, and all pairs (unit, tile column), or a cluster's block its share of them.  At a unit's end (or
-// its share's) each warp adds what it has, by the router's weights, to sums of its rows for every token.
-template <int NT, int PER, int HPARTS, int AHEAD>
-__global__ void __launch_bounds__(THREADS) down_kernel(const __grid_constant__ DownArgs a) {
-  using T = __nv_bfloat16;
-  using R = Ring<NT>;
-  constexpr int CPT = columns_per_token(HPARTS);
-  extern __shared__ __align__(16) uint8_t w4_smem[];
-  float* part = reinterpret_cast<float*>(w4_smem + R::TOTAL);  // [token][DOWN_LD]
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int sp = blockIdx.x % a.splits, rt = blockIdx.x / a.splits * WARPS + warp;
-  const int mt = min(rt, a.down.rt - 1);  // a row tile past the last is read as the last
-  for (int i = threadIdx.x; i < a.P * DOWN_LD; i += THREADS) part[i] = 0.0f;
-  // units and choices are those of kernels before the one that this one waits for
-  const int ct = a.down.ct;
-  const int64_t all = (int64_t)__ldcg(a.nunits) * ct;
-  const int64_t q0 = all * sp / a.splits, n = all * (sp + 1) / a.splits - q0;
-  // a place in the sequence of stages; the unit after it is asked for a unit ahead
-  struct Place {
-    int unit, kt;
-    int4 u, after;
-  };
-  const int units = (int)(all / ct);
-  auto unit_at = [&](int i) { return i < units ? __ldcg(reinterpret_cast<const int4*>(a.units) + i) : make_int4(0, 0, 0, 0); };
-  auto advance = [&](Place& c) {
-    if (++c.kt == ct) {
-      c.kt = 0;
-      ++c.unit;
-      c.u = c.after;
-      c.after = unit_at(c.unit + 1);
-      return true;
-    }
-    return false;
-  };
-  Place wp;
-  wp.unit = (int)(q0 / ct);
-  wp.kt = (int)(q0 - (int64_t)wp.unit * ct);
-  wp.u = unit_at(wp.unit);
-  wp.after = unit_at(wp.unit + 1);
-  Place xp = wp, now = wp;
-  Tile<PER> tile[AHEAD][1];
-  auto next_weights = [&](int slot) {
-    tile[slot][0].load(a.down.codes, a.down.scales, ((int64_t)wp.u.x * a.down.rt + mt) * ct + wp.kt, lane);
-    advance(wp);
-  };
-  Columns<NT> cols;
-  auto columns = [&]() {
-#pragma unroll
-    for (int i = 0; i < R::COPIES; ++i) {
-      const int col = (int)(threadIdx.x >> 4) + 16 * i, tok = col / CPT, p = col % CPT;
-      cols.off[i] = tok < xp.u.z && p < HPARTS ? 2 * (((int64_t)(xp.u.y + tok) * HPARTS + p) * a.hpitch) : -1;
-    }
-  };
-  const uint8_t* hb = reinterpret_cast<const uint8_t*>(a.h);
-  const uint32_t ring_at = smem_u32(w4_smem);
-  int xslot = 0, slot = 0;
-  auto next_tokens = [&]() {
-    cols.copy(ring_at + xslot * R::BYTES, hb, xp.kt, (int)a.hpitch);
-    xslot = xslot + 1 == R::STAGES ? 0 : xslot + 1;
-    if (advance(xp)) columns();
-  };
-  // the choices whose sums this lane will hold, asked for as their unit begins
-  constexpr int MINE = HPARTS == 2 ? NT : NT;
-  Choice mine[MINE];
-  auto choices = [&]() {
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int tok = HPARTS == 2 ? 4 * nt + t : 2 * nt + (t >> 1);
-      mine[nt] = {-1, 0.0f};
-      if (tok < now.u.z) {
-        const int2 c = __ldcg(reinterpret_cast<const int2*>(a.choices) + now.u.y + tok);
-        mine[nt] = {c.x, __int_as_float(c.y)};
-      }
-    }
-  };
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i)
-    if (i < n) next_weights(i);
-  columns();
-  choices();
-  pdl_wait();
-#pragma unroll
-  for (int i = 0; i < R::STAGES - 1; ++i) {
-    if (i < n) next_tokens();
-    cp_async_commit();
-  }
-  pair_t sum[1][NT][2];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) sum[0][nt][0] = sum[0][nt][1] = 0ull;
-  float* own = part + warp * TILE_ROWS;
-  const Pieces<NT> pieces(8 * NT, lane);
-  for (int64_t q = 0; q < n; q += AHEAD) {
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      if (q + i >= n) break;  // the same for the whole block
-      cp_async_wait<R::STAGES - 2>();
-      __syncthreads();  // the stage is there for everyone, and the one before has been read
-      if (q + i + R::STAGES - 1 < n) next_tokens();
-      cp_async_commit();
-      multiply<T, 1, NT, PER>(tile[i], w4_smem + slot * R::BYTES, pieces, sum);
-      slot = slot + 1 == R::STAGES ? 0 : slot + 1;
-      if (q + i + AHEAD < n) next_weights(i);
-      const bool turn = now.kt == ct - 1;
-      if (turn || q + i + 1 == n) {  // the unit's last tile here
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float s0, s1, u0, u1;
-          unpack_f2(sum[0][nt][0], s0, s1);
-          unpack_f2(sum[0][nt][1], u0, u1);
-          float v0 = s0 + s1, v1 = u0 + u1;  // rows g and g + 8 of this lane's token
-          bool live = mine[nt].token >= 0;
-          constexpr int STEP = HPARTS == 2 ? 1 : 2;
-          if (HPARTS == 3) {
-            v0 += __shfl_xor_sync(FULL_MASK, v0, 1);
-            v1 += __shfl_xor_sync(FULL_MASK, v1, 1);
-            live &= (t & 1) == 0;
-          }
-          const float w = mine[nt].weight * Operand<T>::BACK;
-          float* at = own + mine[nt].token * DOWN_LD;
-          auto add = [&]() {
-            at[g] = fmaf(w, v0, at[g]);
-            at[g + 8] = fmaf(w, v1, at[g + 8]);
-          };
-          // a token that has the expert twice has both places beside one another
-          const int before = __shfl_up_sync(FULL_MASK, mine[nt].token, STEP);
-          if (__any_sync(FULL_MASK, live && t >= STEP && before == mine[nt].token)) {
-            for (int k = 0; k < 4; ++k) {
-              if (live && t == k) add();
-              __syncwarp();
-            }
-          } else if (live) {
-            add();
-          }
-          __syncwarp();
-          sum[0][nt][0] = sum[0][nt][1] = 0ull;
-        }
-      }
-      if (advance(now)) choices();
-    }
-  }
-  cp_async_wait<0>();
-  if (a.splits > 1)
-    cluster_sync();
-  else
-    __syncthreads();
-  const int m0 = blockIdx.x / a.splits * DOWN_ROWS;
-  for (int i = threadIdx.x + THREADS * sp; i < a.P * DOWN_ROWS; i += THREADS * a.splits) {
-    const int p = i / DOWN_ROWS, r = i % DOWN_ROWS;
-    const float* at = part + p * DOWN_LD + r;
-    float v = 0.0f;
-    if (a.splits == 1)
-      v = at[0];
-    else
-      for (int k = 0; k < a.splits; ++k) v += ld_cluster(at, k);
-    if (m0 + r < a.K) store_typed(a.y, a.ytype, (int64_t)p * a.K + m0 + r, v);
-  }
-  if (a.splits > 1) cluster_sync();  // no block leaves while another may read its sums
 }
 
 // ------------------------------------------------------------------ the choices' outputs together
@@ -544,28 +373,6 @@ __global__ void __launch_bounds__(256) combine_kernel(const float* z, const int3
 }
 
 // ------------------------------------------------------------------ host side
-template <typename... KArgs>
-fgq_status launch_chained(void (*kernel)(KArgs...), dim3 grid, unsigned threads, size_t smem, int splits, cudaStream_t s, KArgs... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  unsigned n = 0;
-  attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  if (splits > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = (unsigned)splits;
-    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
-    ++n;
-  }
-  cfg.attrs = attr;
-  cfg.numAttrs = n;
-  return after_launch(cudaLaunchKernelEx(&cfg, kernel, args...));
-}
-
 template <typename T, typename R, int TOKENS>
 fgq_status launch_route_tokens(const RouteArgs& a, bool vec, cudaStream_t s) {
   int ks = 1;  // warps that share an expert's row
@@ -597,60 +404,51 @@ struct Route {
 
 inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
-template <int NT, int HPARTS, int PER, int AHEAD>
-fgq_status launch_down_k(const DownArgs& a, unsigned grid, cudaStream_t s) {
-  constexpr int RING = Ring<NT>::TOTAL, MOST = RING + CHUNK * DOWN_LD * 4;
-  static_assert(MOST <= 232448, "shared memory budget");
-  if (!tc::smem_attr_once<down_kernel<NT, PER, HPARTS, AHEAD>>(MOST)) return FGQ_ERR_CUDA;
-  return launch_chained(down_kernel<NT, PER, HPARTS, AHEAD>, dim3(grid), THREADS, RING + a.P * DOWN_LD * 4, a.splits, s, a);
-}
-template <int NT, int HPARTS, int AHEAD>
-fgq_status launch_down_per(const DownArgs& a, unsigned grid, cudaStream_t s) {
-  if (a.down.per == 4) return launch_down_k<NT, HPARTS, 4, AHEAD>(a, grid, s);
-  if (a.down.per == 2) return launch_down_k<NT, HPARTS, 2, AHEAD>(a, grid, s);
-  return launch_down_k<NT, HPARTS, 1, AHEAD>(a, grid, s);
-}
-
-// Tokens of a unit: 8, which the columns of one product hold, 16 or 32 where experts have more on average.  fp32 tokens take
-// four columns each, and 8.
-int unit_tokens(int type, int A, int E) {
-  if (type == FGQ_F32 || A <= 8ll * E) return 8;
-  return A <= 16ll * E ? 16 : 32;
-}
-fgq_status launch_hidden(const RowsArgs& a, int type, int cap, unsigned grid, cudaStream_t s) {
-  if (type == FGQ_F32) return launch_gated_f32(a, grid, s);
-  return type == FGQ_BF16 ? launch_gated_bf16(a, cap / 8, grid, s) : launch_gated_f16(a, cap / 8, grid, s);
-}
-fgq_status launch_down(const DownArgs& a, int type, int cap, unsigned grid, cudaStream_t s) {
-  if (type == FGQ_F32) return launch_down_per<4, 3, 4>(a, grid, s);
-  if (cap == 8) return launch_down_per<2, 2, 4>(a, grid, s);
-  return cap == 16 ? launch_down_per<4, 2, 4>(a, grid, s) : launch_down_per<8, 2, 3>(a, grid, s);
+// Choices of an expert, on average, up to which units of 8 (fp32: 4) tokens run, their operands in shared memory.
+#ifndef HLD
+#define HLD 8
+#define HLDF 4
+#endif
+constexpr int HELD_MAX = HLD, HELD_MAX_F32 = HLDF;
+// How they are held: tokens of a unit (0: not even one fits) and the plans of both layers.
+struct HeldPlan {
+  int cap;
+  ResidentPlan hidden, down;
+};
+HeldPlan plan_units(int type, int pass, int ctk, int per, int ctf, int down_per) {
+  HeldPlan p = {};
+  const int parts = type == FGQ_F32 ? 3 : (type == FGQ_F16 ? 2 : 1);  // columns of a hidden value
+  for (int cap = type == FGQ_F32 ? 4 : 8; cap > 0; cap /= 2) {
+    const int c = pass < cap ? pass : cap;
+    p.hidden = type == FGQ_F32 ? plan_resident<2, 2, GATED_AHEAD>(ctk, per, c * columns_per_token(3)) : plan_resident<2, 1, GATED_AHEAD>(ctk, per, c);
+    p.down = plan_held(parts == 1 ? 1 : 2, ctf, down_per, c * columns_per_token(parts));
+    p.cap = c;
+    if (p.hidden.warps > 0 && p.down.warps > 0) return p;
+  }
+  p.cap = 0;
+  return p;
 }
 
 // route == nullptr: ids and weights are given.
 fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route* route, const int32_t* ids, const float* weights,
                        int top, const fgq_w4* gate, const fgq_w4* up, const fgq_w4* down, void* y, cudaStream_t s) {
   const int K = gate->cols, F = gate->rows, E = gate->experts;
-  const int pass = P < CHUNK ? P : CHUNK, A = pass * top;  // of the largest pass
-  const int parts = type == FGQ_F32 ? 3 : 1, hparts = type == FGQ_F32 ? 3 : 2;
-  const bool direct = direct_tokens(x, type, P, K, ldx);
+  const int most = MAX_CHOICES / top, pass = P < most ? P : most, A = pass * top;  // tokens and choices of a pass
+  const int parts = type == FGQ_F32 ? 3 : 1;
   const int64_t hpitch = (int64_t)row_tiles(F) * TILE_ROWS;
-  // tokens held in shared memory where units of 8 (fp32: 4) do and they fit
-  const int ctk = col_tiles(K), ctf = col_tiles(F);
-  // tokens of a unit: a router picks an expert once for each
-  const int most = type == FGQ_F32 ? 4 : 8, held_tokens = route && pass < most ? pass : most;
-  const int dparts = type == FGQ_F32 ? 3 : (type == FGQ_F16 ? 2 : 1);
-  const ResidentPlan hp = type == FGQ_F32 ? plan_resident<2, 2, GATED_AHEAD>(ctk, 128 / gate->group, held_tokens * columns_per_token(3))
-                                          : plan_resident<2, 1, GATED_AHEAD>(ctk, 128 / gate->group, held_tokens);
-  const ResidentPlan dp = plan_held(dparts == 1 ? 1 : 2, ctf, 128 / down->group, held_tokens * columns_per_token(dparts));
-  const bool held = hp.warps > 0 && dp.warps > 0 && (type == FGQ_F32 ? A <= 4ll * E : A <= 8ll * E);
-  const int cap = held && type == FGQ_F32 ? 4 : unit_tokens(type, A, E);
-  const int most_units = (A < E || P == 1 ? A : E) + A / cap;
-  const size_t b_x = direct ? 0 : up256(copied_bytes(type, pass, K)), b_h = up256((size_t)A * hpitch * (held ? 4 : 2 * hparts));
+  const HeldPlan plan = plan_units(type, pass, col_tiles(K), TILE_COLS / gate->group, col_tiles(F), TILE_COLS / down->group);
+  const bool held = plan.cap > 0 && A <= (int64_t)(type == FGQ_F32 ? HELD_MAX_F32 : HELD_MAX) * E;
+#ifndef CAPT
+#define CAPT 64
+#endif
+  const int cap = held ? plan.cap : (A <= (int64_t)CAPT * E ? 64 : 128);
+  const bool direct = !held || direct_tokens(x, type, P, K, ldx);
+  const int most_units = (A < E || pass == 1 ? A : E) + A / cap;
+  const size_t b_x = direct ? 0 : up256(copied_bytes(type, pass, K));
+  const size_t b_h = held ? up256((size_t)A * hpitch * 4) : up256(experts_many_bytes(type, A, K, F));
   const size_t b_units = up256(sizeof(Unit) * most_units), b_choices = up256(sizeof(Choice) * (size_t)A), b_n = 256;
-  const size_t b_places = up256(4 * (size_t)A), b_tops = b_places, b_z = held ? up256(4 * (size_t)A * K) : 0;
-  const size_t b_ids = route ? up256(4 * (size_t)A) : 0;
-  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(b_x + b_h + b_units + b_choices + b_n + b_places + b_tops + b_z + 2 * b_ids, s));
+  const size_t b_places = up256(4 * (size_t)A), b_z = up256(4 * (size_t)A * K), b_ids = route ? b_places : 0;
+  uint8_t* tmp = static_cast<uint8_t*>(scratch_alloc(b_x + b_h + b_units + b_choices + b_n + 2 * b_places + b_z + 2 * b_ids, s));
   if (!tmp) return FGQ_ERR_CUDA;
   uint8_t* at = tmp;
   auto take = [&](size_t n) {
@@ -659,19 +457,19 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
     return p;
   };
   void* xc = take(b_x);
-  uint16_t* h = reinterpret_cast<uint16_t*>(take(b_h));
+  void* h = take(b_h);
   Unit* units = reinterpret_cast<Unit*>(take(b_units));
   Choice* choices = reinterpret_cast<Choice*>(take(b_choices));
   int* nunits = reinterpret_cast<int*>(take(b_n));
   int32_t* places = reinterpret_cast<int32_t*>(take(b_places));
-  unsigned* tops = reinterpret_cast<unsigned*>(take(b_tops));
+  unsigned* tops = reinterpret_cast<unsigned*>(take(b_places));
   float* z = reinterpret_cast<float*>(take(b_z));
   int32_t* own_ids = reinterpret_cast<int32_t*>(take(b_ids));
   float* own_weights = reinterpret_cast<float*>(take(b_ids));
   const Matrix mg = matrix(gate), mu = matrix(up), md = matrix(down);
   fgq_status st = FGQ_OK;
-  for (int p0 = 0; p0 < P && st == FGQ_OK; p0 += CHUNK) {
-    const int np = P - p0 < CHUNK ? P - p0 : CHUNK, na = np * top;
+  for (int p0 = 0; p0 < P && st == FGQ_OK; p0 += pass) {
+    const int np = P - p0 < pass ? P - p0 : pass, na = np * top;
     const uint8_t* xp = static_cast<const uint8_t*>(x) + p0 * ldx * float_bytes(type);
     TokenRows rows = {xp, ldx, K};
     if (!direct) {
@@ -682,7 +480,7 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
     }
     const int32_t* pid = ids ? ids + (int64_t)p0 * top : own_ids;
     const float* pw = weights ? weights + (int64_t)p0 * top : own_weights;
-    const bool one = route && np <= RT_TOKENS;  // a cluster's tokens: it leaves units and choices itself
+    const bool one = route && np <= RT_TOKENS && cap >= np;  // a cluster's tokens: it leaves units and choices itself
     if (route) {
       const RouteArgs ra = {xp, route->router, ldx, own_ids, own_weights, one ? units : nullptr, choices, places, tops, nunits, np, K, E, top,
                             route->score, route->renormalize, route->scale};
@@ -691,15 +489,14 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
     }
     if (!one) {
       if (route) {
-        st = launch_chained(group_kernel, dim3(1), GR_THREADS, 0, 1, s, pid, pw, na, top, E, cap, units, choices, places, tops, nunits);
+        st = after_launch(launch_pdl(group_kernel, dim3(1), dim3(GR_THREADS), 0, s, pid, pw, na, top, E, cap, units, choices, places, tops, nunits));
       } else {  // the kernel before is the caller's, or the copy
         group_kernel<<<1, GR_THREADS, 0, s>>>(pid, pw, na, top, E, cap, units, choices, places, tops, nunits);
         st = after_launch();
       }
       if (st != FGQ_OK) break;
     }
-    const int nu = one ? (na < E ? na : E) : (na < E || np == 1 ? na : E) + (np == 1 ? 0 : na / cap);  // units at most
-    uint8_t* yp = static_cast<uint8_t*>(y) + (int64_t)p0 * K * float_bytes(type);
+    const int nu = one ? (na < E ? na : E) : (na < E || np == 1 ? na : E + na / cap);  // units at most
     if (held) {
       const int64_t hi = (int64_t)nu * mg.rt, di = (int64_t)nu * md.rt;
       if (hi > INT32_MAX || di > INT32_MAX) {
@@ -708,38 +505,23 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
       }
       ResidentArgs ra = {};
       ra.w = mg, ra.up = mu, ra.x = rows, ra.M = F, ra.units = units, ra.choices = choices, ra.nunits = nunits;
-      ra.h = reinterpret_cast<float*>(h), ra.hpitch = hpitch, ra.top = tops, ra.one = np == 1;
+      ra.h = static_cast<float*>(h), ra.hpitch = hpitch, ra.top = tops, ra.one = np == 1;
       ra.items = one && np == 1 ? (int)hi : 0;  // one token picks distinct experts
-      st = type == FGQ_F32 ? launch_held_gated_f32(ra, hp, hi, s)
-                           : (type == FGQ_BF16 ? launch_held_gated_bf16(ra, hp, hi, s) : launch_held_gated_f16(ra, hp, hi, s));
+      st = type == FGQ_F32 ? launch_held_gated_f32(ra, plan.hidden, hi, s)
+                           : (type == FGQ_BF16 ? launch_held_gated_bf16(ra, plan.hidden, hi, s) : launch_held_gated_f16(ra, plan.hidden, hi, s));
       if (st != FGQ_OK) break;
       ra.w = md, ra.M = K, ra.z = z, ra.items = ra.items ? (int)di : 0;
-      st = type == FGQ_F32 ? launch_held_down_f32(ra, dp, di, s)
-                           : (type == FGQ_BF16 ? launch_held_down_bf16(ra, dp, di, s) : launch_held_down_f16(ra, dp, di, s));
-      if (st != FGQ_OK) break;
-      const bool four = K % 4 == 0;
-      const dim3 cg((unsigned)((K + (four ? 1023 : 255)) / (four ? 1024 : 256)), (unsigned)np);
-      st = four ? launch_chained(combine_kernel<4>, cg, 256, 0, 1, s, static_cast<const float*>(z), static_cast<const int32_t*>(places), pw,
-                                 top, K, static_cast<void*>(yp), type)
-                : launch_chained(combine_kernel<1>, cg, 256, 0, 1, s, static_cast<const float*>(z), static_cast<const int32_t*>(places), pw,
-                                 top, K, static_cast<void*>(yp), type);
-      continue;
+      st = type == FGQ_F32 ? launch_held_down_f32(ra, plan.down, di, s)
+                           : (type == FGQ_BF16 ? launch_held_down_bf16(ra, plan.down, di, s) : launch_held_down_f16(ra, plan.down, di, s));
+    } else {
+      st = launch_experts_many({mg, mu, md, units, choices, nunits, K, F, na, cap, nu, h, z}, xp, type, ldx, s);
     }
-    RowsArgs ha = {};
-    ha.w = mg, ha.up = mu, ha.x = rows, ha.M = F, ha.units = units, ha.choices = choices, ha.nunits = nunits, ha.h = h, ha.hpitch = hpitch;
-    const int64_t items = (int64_t)nu * ((mg.rt + WARPS - 1) / WARPS);
-    if (items > INT32_MAX / 8) {
-      st = FGQ_ERR_UNSUPPORTED;
-      break;
-    }
-    const RowsPlan plan = plan_rows(items, mg.ct);
-    ha.splits = plan.splits;
-    st = launch_hidden(ha, type, cap, plan.grid, s);
     if (st != FGQ_OK) break;
-    DownArgs da = {md, h, hpitch, units, choices, nunits, yp, np, K, type, 1};
-    const int groups = (md.rt + WARPS - 1) / WARPS;
-    while (da.splits < 8 && (int64_t)groups * da.splits * 2 <= 2 * device_sms() && (int64_t)nu * md.ct >= 4 * da.splits) da.splits *= 2;
-    st = launch_down(da, type, cap, (unsigned)(groups * da.splits), s);
+    const bool four = K % 4 == 0;
+    const dim3 cg((unsigned)((K + (four ? 1023 : 255)) / (four ? 1024 : 256)), (unsigned)np);
+    void* yp = static_cast<uint8_t*>(y) + (int64_t)p0 * K * float_bytes(type);
+    st = after_launch(launch_pdl(four ? combine_kernel<4> : combine_kernel<1>, cg, dim3(256), 0, s, static_cast<const float*>(z),
+                                 static_cast<const int32_t*>(places), pw, top, K, yp, type));
   }
   if (cudaFreeAsync(tmp, s) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
   return st;

@@ -253,6 +253,16 @@ struct Columns {
   }
 };
 
+// A unit of work of the experts: up to `cap` choices of one expert, `count` of them from `start` on in the order sorted by expert.
+struct Unit {
+  int expert, start, count, pad;
+};
+// A choice in that order: its token and the router's weight.
+struct Choice {
+  int token;
+  float weight;
+};
+
 // Tokens as operand rows: 16-bit elements, a token's `parts` rows beside one another (fp32: three bf16 parts that add up
 // to it exactly, in four columns of a product; 16-bit: themselves).
 struct TokenRows {

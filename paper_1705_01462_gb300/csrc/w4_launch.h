@@ -6,15 +6,10 @@
 namespace fgq {
 namespace w4 {
 
-// Columns of tokens that a block takes: 8 nt, nt 1, 2 or 4.  A linear layer.
+// A linear layer; columns of tokens that a block takes: 8 nt, nt 1, 2 or 4.
 fgq_status launch_rows_bf16(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s);
 fgq_status launch_rows_f16(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s);
 fgq_status launch_rows_f32(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s);
-// Gate and up of a gated layer.
-fgq_status launch_gated_bf16(const RowsArgs& a, int nt, unsigned grid, cudaStream_t s);
-fgq_status launch_gated_f16(const RowsArgs& a, int nt, unsigned grid, cudaStream_t s);
-fgq_status launch_gated_f32(const RowsArgs& a, unsigned grid, cudaStream_t s);
-
 // The same with tokens held in shared memory: up to 8 nt columns (nt 1 or 2), where plan_resident finds room for them.
 fgq_status launch_held_bf16(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s);
 fgq_status launch_held_f16(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s);
@@ -34,7 +29,7 @@ fgq_status launch_held_per(const ResidentArgs& a, const ResidentPlan& plan, int6
   return launch_resident<T, MT, NT, 1, PARTS, MODE, AHEAD>(a, plan, items, chained, s);
 }
 // Tiles under way of a warp: four, or two pairs.
-constexpr int HELD_AHEAD = 4, GATED_AHEAD = 2;
+constexpr int HELD_AHEAD = 4, GATED_AHEAD = 2, ROWS_AHEAD = 4;
 inline ResidentPlan plan_held(int nt, int ct, int per, int cols) {
   return nt == 1 ? plan_resident<1, 1, HELD_AHEAD>(ct, per, cols) : plan_resident<1, 2, HELD_AHEAD>(ct, per, cols);
 }
@@ -44,18 +39,16 @@ fgq_status launch_held_type(const ResidentArgs& a, int nt, const ResidentPlan& p
   return launch_held_per<T, 1, 2, PARTS, MODE_LINEAR, HELD_AHEAD>(a, plan, a.items, chained, s);
 }
 
-template <typename T, int MT, int NT, int PARTS, bool GATED, int HPARTS, int AHEAD>
+template <typename T, int NT, int PARTS>
 fgq_status launch_rows_per(const RowsArgs& a, unsigned grid, bool chained, cudaStream_t s) {
-  if (a.w.per == 4) return launch_rows<T, MT, NT, 4, PARTS, GATED, HPARTS, AHEAD>(a, grid, chained, s);
-  if (a.w.per == 2) return launch_rows<T, MT, NT, 2, PARTS, GATED, HPARTS, AHEAD>(a, grid, chained, s);
-  return launch_rows<T, MT, NT, 1, PARTS, GATED, HPARTS, AHEAD>(a, grid, chained, s);
+  if (a.w.per == 4) return launch_rows<T, NT, 4, PARTS, ROWS_AHEAD>(a, grid, chained, s);
+  if (a.w.per == 2) return launch_rows<T, NT, 2, PARTS, ROWS_AHEAD>(a, grid, chained, s);
+  return launch_rows<T, NT, 1, PARTS, ROWS_AHEAD>(a, grid, chained, s);
 }
-
 template <typename T, int PARTS>
 fgq_status launch_rows_type(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s) {
-  if (nt == 1) return launch_rows_per<T, 1, 1, PARTS, false, 1, 4>(a, grid, chained, s);
-  if (nt == 2) return launch_rows_per<T, 1, 2, PARTS, false, 1, 4>(a, grid, chained, s);
-  return launch_rows_per<T, 1, 4, PARTS, false, 1, 4>(a, grid, chained, s);
+  if (nt == 1) return launch_rows_per<T, 1, PARTS>(a, grid, chained, s);
+  return nt == 2 ? launch_rows_per<T, 2, PARTS>(a, grid, chained, s) : launch_rows_per<T, 4, PARTS>(a, grid, chained, s);
 }
 
 }  // namespace w4

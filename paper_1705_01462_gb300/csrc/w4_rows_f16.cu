@@ -7,11 +7,6 @@ namespace w4 {
 fgq_status launch_rows_f16(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s) {
   return launch_rows_type<__half, 1>(a, nt, grid, chained, s);
 }
-fgq_status launch_gated_f16(const RowsArgs& a, int nt, unsigned grid, cudaStream_t s) {
-  if (nt == 1) return launch_rows_per<__half, 2, 1, 1, true, 2, 3>(a, grid, true, s);
-  if (nt == 2) return launch_rows_per<__half, 2, 2, 1, true, 2, 3>(a, grid, true, s);
-  return launch_rows_per<__half, 2, 4, 1, true, 2, 2>(a, grid, true, s);
-}
 fgq_status launch_held_f16(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
   return launch_held_type<__half, 1>(a, nt, plan, chained, s);
 }

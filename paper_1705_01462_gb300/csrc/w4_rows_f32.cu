@@ -7,9 +7,6 @@ namespace w4 {
 fgq_status launch_rows_f32(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s) {
   return launch_rows_type<__nv_bfloat16, 3>(a, nt, grid, chained, s);
 }
-fgq_status launch_gated_f32(const RowsArgs& a, unsigned grid, cudaStream_t s) {
-  return launch_rows_per<__nv_bfloat16, 2, 4, 3, true, 3, 2>(a, grid, true, s);
-}
 fgq_status launch_held_f32(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s) {
   return launch_held_type<__nv_bfloat16, 3>(a, nt, plan, chained, s);
 }

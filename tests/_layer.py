@@ -233,23 +233,33 @@ def experts(x, ids, g, e_g, wg, wu, wd, G, Gd, dtype):
     P, K = x.shape
     E, F, _ = wg.shape
     y, e = np.zeros((P, K)), np.zeros((P, K))
+    # more than 8 (fp32: 4) choices an expert run on the products of many tokens
+    many = ids.size > (4 if dtype == "f32" else 8) * E
     # between the layers: bf16 tokens' values in 11 bits at least, half a step of them; fp16 ones' in two parts of 8 bits; fp32's exact
-    held = {"f32": u, "bf16": 2.0 ** -12, "f16": 2.0 ** -17}[dtype]
+    # (many: in two fp16 parts, within 2^-22)
+    held = {"f32": 4 * u if many else u, "bf16": 2.0 ** -12, "f16": 2.0 ** -17}[dtype]
+
+    def sums(w, v, n, G, dt):
+        """What the sums of w times v, of n products each, are off by."""
+        e = beta(n, G, many, dt) * (np.abs(w) @ np.abs(v))
+        if many:  # as for a linear layer
+            e = e + 2.0 ** -36 * np.abs(v).max() * np.abs(w).sum(1) + 2.0 ** -36 * np.abs(w).max(1) * np.abs(v).sum()
+        return e
+
     for p in range(P):
         for j in range(ids.shape[1]):
             n = ids[p, j]
             if n < 0 or n >= E:
                 continue
-            ax = np.abs(x[p])
             a, b = wg[n] @ x[p], wu[n] @ x[p]
-            ea, eb = beta(K, G) * (np.abs(wg[n]) @ ax), beta(K, G) * (np.abs(wu[n]) @ ax)
+            ea, eb = sums(wg[n], x[p], K, G, dtype), sums(wu[n], x[p], K, G, dtype)
             sig = 1 / (1 + np.exp(-a))
             h = a * sig * b
             eh = 1.1 * ea * (np.abs(b) + eb) + np.abs(a * sig) * eb + (held + 8 * u) * np.abs(h)
-            if dtype != "f32":  # values that fp16, scaled to a largest of 2^14, holds as subnormals: half their step
+            if dtype != "f32" or many:  # values that fp16, scaled to a largest of 2^14, holds as subnormals: half their step
                 eh = eh + 2.0 ** -39 * np.abs(h).max()
             v = wd[n] @ h
-            ev = np.abs(wd[n]) @ eh + beta(F, Gd) * (np.abs(wd[n]) @ np.abs(h))
+            ev = np.abs(wd[n]) @ eh + sums(wd[n], h, F, Gd, "bf16" if dtype == "bf16" else "f32")
             y[p] += g[p, j] * v
             e[p] += np.abs(g[p, j]) * (ev + e_g[p, 0] * np.abs(v))
             # sums of choices, warps and blocks

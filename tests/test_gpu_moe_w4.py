@@ -65,7 +65,10 @@ def run_experts(rng, P, K, F, E, top, G, dtype, Gd=None, ids=None, fill=0, ld=0)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("P,K,F,E,top,G", [(1, 128, 64, 4, 2, 64), (1, 1, 1, 1, 1, 32), (1, 1000, 700, 6, 3, 32), (3, 136, 40, 9, 4, 128),
                                            (8, 256, 96, 2, 1, 64), (20, 264, 33, 5, 2, 32), (40, 130, 70, 3, 3, 64),
-                                           (64, 128, 128, 16, 4, 64), (129, 64, 48, 4, 2, 64), (300, 40, 24, 2, 1, 32), (2, 2048, 16, 3, 2, 64)])
+                                           (64, 128, 128, 16, 4, 64), (129, 64, 48, 4, 2, 64), (300, 40, 24, 2, 1, 32), (2, 2048, 16, 3, 2, 64),
+                                           # units cut short of 64 and 128 tokens, two passes, long rows, layers that hold few tokens or none
+                                           (130, 520, 300, 3, 2, 64), (600, 130, 140, 6, 3, 128), (700, 64, 40, 5, 8, 32), (40, 4100, 36, 2, 1, 64),
+                                           (9, 64, 15000, 3, 1, 64), (6, 20000, 17, 3, 1, 128), (2, 16, 120000, 2, 1, 64)])
 def test_experts(dtype, P, K, F, E, top, G):
     run_experts(np.random.default_rng(P + K), P, K, F, E, top, G, dtype)
 

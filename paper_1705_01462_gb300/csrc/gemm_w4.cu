@@ -28,8 +28,8 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ G4Arg
 
 template <int PARTS>
 fgq_status launch_g4_tile(const G4Args& a, int bn, int grid, cudaStream_t s) {
-  if (bn == 256) return launch_g4<256, PARTS, false>(a, grid, s);
-  return bn == 128 ? launch_g4<128, PARTS, false>(a, grid, s) : launch_g4<64, PARTS, false>(a, grid, s);
+  if (bn == 256) return launch_g4<256, PARTS, false, 16>(a, grid, s);
+  return bn == 128 ? launch_g4<128, PARTS, false, 16>(a, grid, s) : launch_g4<64, PARTS, false, 16>(a, grid, s);
 }
 
 }  // namespace

@@ -5,14 +5,16 @@
 // warps turn the 128 channels x 128 columns of a stage into the operand, in the shared memory that the MMA reads.  (Expanded
 // in memory first, 4096 -> 14336 took 55 us at 64 tokens, 36 of them for the expansion.)
 // A block takes a tile of 128 channels and BN tokens, or a part of its K.  Warp roles:
-//   warps 0-15  weights: warp w the row tile w % 8 of every other stage, loaded two of its stages ahead; warps 0-7 (fp32: up to
-//               all) then the epilogue: warp w reads TMEM lanes 32 (w % 4) .. (channels), an equal share of the columns (tokens),
-//               applies scales and bias and stores runs of 32 channels;
-//   warp 16     TMEM allocation and MMA issue;
-//   warp 17     TMA producer of the tokens.
+//   warps 0 .. W-1  (W 16 or 8) weights: warp w the row tile w % 8 of every other stage (W = 8: of each), loaded two of its stages
+//                   ahead; warps 0-7 (fp32: up to all) then the epilogue: warp w reads TMEM lanes 32 (w % 4) .. (channels), an equal
+//                   share of the columns (tokens), applies scales and bias and stores runs of 32 channels;
+//   warp W          TMEM allocation and MMA issue;
+//   warp W + 1      TMA producer of the tokens.
 // Few tiles split K over blocks (fp32 partial sums, joined with scales and bias by a second kernel).
 // (Pairs of SMs, cta_group::2, halve the operands' traffic, but each stage's weights then take arrivals across the pair: 1.1 us a stage of
-// 64 columns, where this form takes 0.6 us for 128.)
+// 64 columns, where this form takes 0.55 us for 128.)
+// Bound by the instructions and shared-memory writes that turn a stage's codes into the operand: 64 tokens, 4096 -> 14336: 22.5 us
+// (28 without the order of stores that meets all banks); half of the issue slots and of the shared memory's cycles are in use.
 // fp32 tokens are two rows of fp16 that add up to them within 2^-22, and their sums leave the tensor memory for registers every
 // 256 columns: the tensor cores cut sums off, and over 4096 columns that took outputs to 2e-6 of 64-bit sums, over 16384 to 1e-5;
 // so it is 3e-7 for any length.  (2048 tokens, 4096 -> 4096: 139 us; without 133.)
@@ -30,19 +32,18 @@ namespace w4 {
 using tc::make_map_2d;
 
 constexpr int G4_BM = 128, G4_KT = 128;  // channels and columns of a stage
-constexpr int G4_W_WARPS = 16, G4_MMA_WARP = 16, G4_TMA_WARP = 17;
 constexpr int G4_EPI_WARPS = 8;
-constexpr int G4_THREADS = 32 * 18;
 constexpr uint64_t G4_TIMEOUT_NS = 1000000000ull;  // 1 s per wait
 
-template <int BN>
+template <int BN, int W>
 struct G4Cfg {
+  static constexpr int MMA_WARP = W, TMA_WARP = W + 1, THREADS = 32 * (W + 2), BLOCKS = W == 8 ? 2 : 1;  // blocks an SM
   // each operand in two halves of 64 columns (128-byte rows)
   static constexpr int A_HALF = G4_BM * 128, B_HALF = BN * 128, STAGE = 2 * (A_HALF + B_HALF);
-  static constexpr int STAGES = BN == 256 ? 2 : (BN == 128 ? 3 : 4);
+  static constexpr int STAGES = BN == 256 || W == 8 ? 2 : (BN == 128 ? 3 : 4);
   static constexpr int SMEM = 1024 + STAGES * STAGE + 8 * (3 * STAGES + 5) + 16;
+  static_assert(BLOCKS * (SMEM + 1536) <= 233472 && SMEM + 512 <= 232448, "shared memory budget");
 };
-static_assert(G4Cfg<256>::SMEM <= 232448 && G4Cfg<128>::SMEM <= 232448 && G4Cfg<64>::SMEM <= 232448, "shared memory budget");
 
 struct G4Args {
   CUtensorMap x_map;
@@ -74,9 +75,9 @@ __device__ __forceinline__ void store_column(T* y, int M, int live, const float 
 constexpr int TAKE = 2;  // stages of fp32 sums (see above)
 // PARTS rows of x make a token (fp32: two).
 // GROUPED: the rows' exponents are found by the block itself (a scan of its scales, while the kernel before it runs).
-template <int BN, int PER, int PARTS, bool GROUPED>
-__global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_constant__ G4Args a) {
-  using C = G4Cfg<BN>;
+template <int BN, int PER, int PARTS, bool GROUPED, int W>
+__global__ void __launch_bounds__(G4Cfg<BN, W>::THREADS, G4Cfg<BN, W>::BLOCKS) gemm_w4_kernel(const __grid_constant__ G4Args a) {
+  using C = G4Cfg<BN, W>;
   constexpr int S = C::STAGES;
   // fp32: sums are taken from the tensor memory every TAKE stages, by TAKERS warps of COLUMNS columns each, from two places in turn
   constexpr bool F32 = PARTS == 2;
@@ -121,7 +122,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
   if (threadIdx.x == 0) {
     for (int i = 0; i < S; ++i) {
       mbar_init(&full_x[i], 1);
-      mbar_init(&full_w[i], G4_W_WARPS / 2);
+      mbar_init(&full_w[i], 8);
       mbar_init(&empty[i], 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -132,7 +133,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
     *abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == G4_MMA_WARP) {
+  if (warp == C::MMA_WARP) {
     tmem_alloc(tmem_slot, TMEM);
     tmem_relinquish();
   }
@@ -140,12 +141,12 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
   if constexpr (GROUPED) {
     if (threadIdx.x < G4_BM) tops[threadIdx.x] = 0u;
     __syncthreads();
-    if (warp < G4_W_WARPS) {  // as magnitudes, which compare as whole numbers: warp w row tile w % 8, every other column
+    if (warp < W) {  // as magnitudes, which compare as whole numbers: warp w row tile w % 8, every other column
       constexpr int CHUNKS = 2 * PER;  // pieces of eight scales, 8 / PER rows, of a tile
       const int d = warp & 7, rt = min(m0 / TILE_ROWS + d, w.rt - 1), chunk = lane % CHUNKS;
       const uint16_t* sc = w.scales + (first_tile + (int64_t)rt * w.ct) * (TILE_ROWS * PER) + chunk * 8;
       uint32_t top[8 / PER] = {};
-      for (int c = lane / CHUNKS + 32 / CHUNKS * (warp >> 3); c < n; c += 2 * (32 / CHUNKS)) {
+      for (int c = lane / CHUNKS + 32 / CHUNKS * (warp >> 3); c < n; c += W / 8 * (32 / CHUNKS)) {
         const uint4 v = __ldg(reinterpret_cast<const uint4*>(sc + (int64_t)c * (TILE_ROWS * PER)));
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
   int issued = 0;  // by the producer
   bool ok = true;
 
-  if (warp == G4_TMA_WARP && lane == 0) {
+  if (warp == C::TMA_WARP && lane == 0) {
     pdl_wait();  // the tokens may be those of the kernel before
     for (; issued < n; ++issued) {
       const int st = issued % S;
@@ -193,7 +194,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
     if (!ok && !*abort_flag) fail();
   }
 
-  if (warp == G4_MMA_WARP) {  // converged, an elected lane issues
+  if (warp == C::MMA_WARP) {  // converged, an elected lane issues
     const uint32_t idesc = idesc_f16_f32(G4_BM, BN);
     int j = 0;
     for (; j < n; ++j) {
@@ -252,15 +253,16 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
     ++took;
   };
 
-  if (warp < G4_W_WARPS) {
-    const int d = warp & 7, first = warp >> 3, g = lane >> 2, t = lane & 3;  // every other stage
+  if (warp < W) {
+    const int d = warp & 7, first = warp >> 3, g = lane >> 2, t = lane & 3;
     const int own = min(TILE_ROWS * d, (w.rt - 1) * TILE_ROWS - m0);  // a row tile past the last is read as the last
     const int64_t at = first_tile + (int64_t)(m0 + own) / TILE_ROWS * w.ct + c0;
+    constexpr int STEP = W / 8;  // every other stage, or each
     constexpr int AHEAD = F32 && BN == 256 ? 1 : 2;  // 32 registers are the sums'
     Tile<PER> tile[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i)
-      if (first + 2 * i < n) tile[i].load(w.codes, w.scales, at + first + 2 * i, lane);
+      if (first + STEP * i < n) tile[i].load(w.codes, w.scales, at + first + STEP * i, lane);
     pdl_wait();  // the exponents are those of the kernel before
     // what takes the rows' scales to fp16's range, in two factors: it passes fp32's largest for tiny ones
     float up[2], up2[2];
@@ -270,25 +272,27 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
       up[r] = pow2f(e / 2);
       up2[r] = pow2f(e - e / 2);
     }
-    for (int j0 = first; j0 < n && ok; j0 += 2 * AHEAD) {
+    // lanes of odd rows take a word's neighbour first: stores of eight lanes, two rows, then meet all banks
+    const int odd = g & 1;
+    for (int j0 = first; j0 < n && ok; j0 += STEP * AHEAD) {
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
-        const int j = j0 + 2 * i, st = j % S;
+        const int j = j0 + STEP * i, st = j % S;
         if (j >= n || !ok) break;
         uint32_t s2[2][PER];  // scales as fp16 pairs
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
           for (int k = 0; k < PER; ++k) {
-            const float s = tile[i].s[r].get(k) * up[r] * up2[r];
+            const float s = (PER == 4 && odd ? tile[i].s[r].get(k ^ 1) : tile[i].s[r].get(k)) * up[r] * up2[r];
             s2[r][k] = pack2(s, s, __half());
           }
         uint4 v[2][4];
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[r][k] = scaled_codes(tile[i].word(r, k), s2[r][k * PER / 4]);
-        if (j + 2 * AHEAD < n) tile[i].load(w.codes, w.scales, at + j + 2 * AHEAD, lane);
+          for (int k = 0; k < 4; ++k) v[r][k] = scaled_codes(odd ? tile[i].word(r, k ^ 1) : tile[i].word(r, k), s2[r][k * PER / 4]);
+        if (j + STEP * AHEAD < n) tile[i].load(w.codes, w.scales, at + j + STEP * AHEAD, lane);
         ok = mbar_wait_warp(&empty[st], ((j / S) & 1) ^ 1, tmo, abort_flag);
         if (!ok) break;
         uint8_t* A = smem + st * C::STAGE;
@@ -296,7 +300,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
         for (int r = 0; r < 2; ++r)
 #pragma unroll
           for (int k = 0; k < 4; ++k)
-            *reinterpret_cast<uint4*>(A + (k >> 1) * C::A_HALF + tc::sw128(TILE_ROWS * d + 8 * r + g, 4 * (k & 1) + t)) = v[r][k];
+            *reinterpret_cast<uint4*>(A + (k >> 1) * C::A_HALF + tc::sw128(TILE_ROWS * d + 8 * r + g, 4 * ((k & 1) ^ odd) + t)) = v[r][k];
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(&full_w[st]);
@@ -357,7 +361,7 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
   }
 
   __syncthreads();
-  if (*abort_flag && warp == G4_TMA_WARP && lane == 0) {  // what is still under way: MMAs, then boxes that no MMA has read
+  if (*abort_flag && warp == C::TMA_WARP && lane == 0) {  // what is still under way: MMAs, then boxes that no MMA has read
     const int done = (int)*read;
     auto drain = [](uint64_t* bar, int phase) { mbar_wait_bounded(bar, (uint32_t)phase & 1u, 1u << 16); };
     drain(done < n ? drain_bar : &acc_full[(runs - 1) & 1], done < n ? 0 : (runs - 1) >> 1);
@@ -365,21 +369,22 @@ __global__ void __launch_bounds__(G4_THREADS, 1) gemm_w4_kernel(const __grid_con
     for (int i = done; i < issued; ++i) drain(&full_x[i % S], i / S);
   }
   __syncthreads();
-  if (warp == G4_MMA_WARP) {
+  if (warp == C::MMA_WARP) {
     tc_fence_after();
     tmem_dealloc(tmem, TMEM);
   }
 }
 
-template <int BN, int PER, int PARTS, bool GROUPED>
+template <int BN, int PER, int PARTS, bool GROUPED, int W>
 fgq_status launch_g4_per(const G4Args& a, int grid, cudaStream_t s) {
-  if (!tc::smem_attr_once<gemm_w4_kernel<BN, PER, PARTS, GROUPED>>(G4Cfg<BN>::SMEM)) return FGQ_ERR_CUDA;
-  return after_launch(launch_pdl(gemm_w4_kernel<BN, PER, PARTS, GROUPED>, dim3(grid), dim3(G4_THREADS), G4Cfg<BN>::SMEM, s, a));
+  using C = G4Cfg<BN, W>;
+  if (!tc::smem_attr_once<gemm_w4_kernel<BN, PER, PARTS, GROUPED, W>>(C::SMEM)) return FGQ_ERR_CUDA;
+  return after_launch(launch_pdl(gemm_w4_kernel<BN, PER, PARTS, GROUPED, W>, dim3(grid), dim3(C::THREADS), C::SMEM, s, a));
 }
-template <int BN, int PARTS, bool GROUPED>
+template <int BN, int PARTS, bool GROUPED, int W>
 fgq_status launch_g4(const G4Args& a, int grid, cudaStream_t s) {
-  if (a.w.per == 4) return launch_g4_per<BN, 4, PARTS, GROUPED>(a, grid, s);
-  return a.w.per == 2 ? launch_g4_per<BN, 2, PARTS, GROUPED>(a, grid, s) : launch_g4_per<BN, 1, PARTS, GROUPED>(a, grid, s);
+  if (a.w.per == 4) return launch_g4_per<BN, 4, PARTS, GROUPED, W>(a, grid, s);
+  return a.w.per == 2 ? launch_g4_per<BN, 2, PARTS, GROUPED, W>(a, grid, s) : launch_g4_per<BN, 1, PARTS, GROUPED, W>(a, grid, s);
 }
 
 }  // namespace w4

@@ -1,5 +1,5 @@
 // The experts' layers of many tokens with 4-bit weights: tokens as rows in the order of their experts, the products of gemm_w4.cuh for
-// a unit of up to 64 or 128 of them and 128 rows of gate, up or down, and the hidden values between them.
+// a unit of up to 32, 64 or 128 of them and 128 rows of gate, up or down, and the hidden values between them.
 #include "gemm_w4.cuh"
 
 namespace fgq {
@@ -63,7 +63,10 @@ __global__ void __launch_bounds__(256) hidden_kernel(const float* g, const float
 
 template <int PARTS>
 fgq_status launch_unit_products(const G4Args& a, int bn, int grid, cudaStream_t s) {
-  return bn == 64 * PARTS ? launch_g4<64 * PARTS, PARTS, true>(a, grid, s) : launch_g4<128 * PARTS, PARTS, true>(a, grid, s);
+  // two smaller blocks an SM where there are tiles for them: one works while the other begins or ends.  us so and with one: 32 experts 4096
+  // -> 1024, 4 a token, 128 tokens 136 and 169; but 8 experts 2048 -> 1024, 2 a token 49 and 40
+  if (bn == 64) return grid >= 2 * device_sms() ? launch_g4<64, PARTS, true, 8>(a, grid, s) : launch_g4<64, PARTS, true, 16>(a, grid, s);
+  return bn == 128 || PARTS == 1 ? launch_g4<128, PARTS, true, 16>(a, grid, s) : launch_g4<128 * PARTS, PARTS, true, 16>(a, grid, s);
 }
 fgq_status launch_products(const ExpertsMany& e, const Matrix& w, const Matrix* up, const __half* x16, int64_t pitch, const float* scale,
                            int parts, int M, float* y, float* y_up, cudaStream_t s) {

@@ -9,7 +9,7 @@
 //   group_kernel    (more than four tokens, or choices that are given) one block: choices sorted by expert, and cut into units of
 //                   tokens that share an expert;
 //   resident_kernel (w4_resident.cuh) 16 rows of gate and of up for a unit of up to 8 tokens: silu(gate) up in fp32; then of down;
-//   or, with more than 8 choices an expert, the kernels of gemm_w4_experts.cu for units of up to 64 or 128;
+//   or, with more choices an expert, the kernels of gemm_w4_experts.cu for units of up to 32, 64 or 128;
 //   combine_kernel  each token's choices by their weights, in their order.
 // Bound by the bytes of the experts' weights, each read once (again from L2 for each further unit of an expert).
 #include <type_traits>
@@ -404,15 +404,9 @@ struct Route {
 
 inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
 
-// Choices of an expert, on average, up to which units of 8 (fp32: 4) tokens run, their operands in shared memory.
-#ifndef HLD
-#define HLD 8
-#define HLDF 4
-#endif
-constexpr int HELD_MAX = HLD, HELD_MAX_F32 = HLDF;
-// How they are held: tokens of a unit (0: not even one fits) and the plans of both layers.
+// How tokens are held in shared memory: as many as a unit may have (0: not even one fits), a unit's, and the plans of both layers.
 struct HeldPlan {
-  int cap;
+  int most, cap;
   ResidentPlan hidden, down;
 };
 HeldPlan plan_units(int type, int pass, int ctk, int per, int ctf, int down_per) {
@@ -422,12 +416,22 @@ HeldPlan plan_units(int type, int pass, int ctk, int per, int ctf, int down_per)
     const int c = pass < cap ? pass : cap;
     p.hidden = type == FGQ_F32 ? plan_resident<2, 2, GATED_AHEAD>(ctk, per, c * columns_per_token(3)) : plan_resident<2, 1, GATED_AHEAD>(ctk, per, c);
     p.down = plan_held(parts == 1 ? 1 : 2, ctf, down_per, c * columns_per_token(parts));
+    p.most = cap;
     p.cap = c;
     if (p.hidden.warps > 0 && p.down.warps > 0) return p;
   }
-  p.cap = 0;
+  p.most = p.cap = 0;
   return p;
 }
+
+// Units of an expert on average up to which tokens are held.  bf16, us so and on the products of many tokens: 8 experts 2048 -> 1024, 2 a
+// token, 64 tokens 40 and 41, 128 tokens 49 and 44; 128 experts 2048 -> 768, 8 a token, 128 tokens 130 and 231, 256 tokens 216 and 254;
+// units of 4 (8 experts 4096 -> 14336) 32 tokens 301 and 371, 64 tokens 536 and 371; fp32, 32 experts 4096 -> 1024, 4 a token, 40 tokens
+// 127 and 150, 128 tokens 260 and 151.
+constexpr int HELD_UNITS = 2;
+// From more choices an expert on units have 64 tokens of fp32 in place of 32 (us at 64 tokens, 8 experts 4096 -> 14336: 555 and 416; 128 tokens
+// 557 and 569), and 128 in place of 64 (bf16, 128 tokens 479 and 373, 256 tokens 499 and 566, 512 tokens 747 and 813).
+constexpr int UNIT_32_MAX_F32 = 16, UNIT_64_MAX = 32;
 
 // route == nullptr: ids and weights are given.
 fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route* route, const int32_t* ids, const float* weights,
@@ -437,11 +441,9 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   const int parts = type == FGQ_F32 ? 3 : 1;
   const int64_t hpitch = (int64_t)row_tiles(F) * TILE_ROWS;
   const HeldPlan plan = plan_units(type, pass, col_tiles(K), TILE_COLS / gate->group, col_tiles(F), TILE_COLS / down->group);
-  const bool held = plan.cap > 0 && A <= (int64_t)(type == FGQ_F32 ? HELD_MAX_F32 : HELD_MAX) * E;
-#ifndef CAPT
-#define CAPT 64
-#endif
-  const int cap = held ? plan.cap : (A <= (int64_t)CAPT * E ? 64 : 128);
+  const bool held = A <= (int64_t)HELD_UNITS * plan.most * E;
+  const bool small = type == FGQ_F32 && A <= (int64_t)UNIT_32_MAX_F32 * E;
+  const int cap = held ? plan.cap : (small ? 32 : (A <= (int64_t)UNIT_64_MAX * E ? 64 : 128));
   const bool direct = !held || direct_tokens(x, type, P, K, ldx);
   const int most_units = (A < E || pass == 1 ? A : E) + A / cap;
   const size_t b_x = direct ? 0 : up256(copied_bytes(type, pass, K));

@@ -233,8 +233,8 @@ def experts(x, ids, g, e_g, wg, wu, wd, G, Gd, dtype):
     P, K = x.shape
     E, F, _ = wg.shape
     y, e = np.zeros((P, K)), np.zeros((P, K))
-    # more than 8 (fp32: 4) choices an expert run on the products of many tokens
-    many = ids.size > (4 if dtype == "f32" else 8) * E
+    # more than two units of 8 tokens an expert, or where long rows make units smaller, may run on the products of many tokens
+    many = ids.size > (8 if dtype == "f32" else 16) * E or max(K, F) > 4096
     # between the layers: bf16 tokens' values in 11 bits at least, half a step of them; fp16 ones' in two parts of 8 bits; fp32's exact
     # (many: in two fp16 parts, within 2^-22)
     held = {"f32": 4 * u if many else u, "bf16": 2.0 ** -12, "f16": 2.0 ** -17}[dtype]

@@ -68,9 +68,69 @@ def run_experts(rng, P, K, F, E, top, G, dtype, Gd=None, ids=None, fill=0, ld=0)
                                            (64, 128, 128, 16, 4, 64), (129, 64, 48, 4, 2, 64), (300, 40, 24, 2, 1, 32), (2, 2048, 16, 3, 2, 64),
                                            # units cut short of 64 and 128 tokens, two passes, long rows, layers that hold few tokens or none
                                            (130, 520, 300, 3, 2, 64), (600, 130, 140, 6, 3, 128), (700, 64, 40, 5, 8, 32), (40, 4100, 36, 2, 1, 64),
+                                           (24, 136, 72, 4, 2, 32), (50, 264, 130, 4, 2, 64), (200, 700, 1100, 16, 2, 64),
                                            (9, 64, 15000, 3, 1, 64), (6, 20000, 17, 3, 1, 128), (2, 16, 120000, 2, 1, 64)])
 def test_experts(dtype, P, K, F, E, top, G):
     run_experts(np.random.default_rng(P + K), P, K, F, E, top, G, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_many_odd_calls(dtype):
+    """Many choices of which some are no expert, some tokens have none or one expert often, and all are at one expert; any codes past
+    the matrices; rows apart; none at all."""
+    rng = np.random.default_rng(21)
+    ids = rng.integers(-1, 6, (130, 3)).astype(np.int32)
+    ids[5] = -1
+    ids[60:70] = 3
+    run_experts(rng, 130, 200, 72, 6, 3, 64, dtype, ids=ids, Gd=32, fill=4, ld=1)
+    run_experts(rng, 150, 136, 40, 4, 1, 128, dtype, ids=np.full((150, 1), 3, np.int32), ld=8)
+    run_experts(rng, 40, 128, 32, 2, 2, 32, dtype, ids=np.full((40, 2), -1, np.int32))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_many_nonfinite_and_graphs(dtype):
+    """A token with NaN leaves the others as they are; a captured call follows its inputs; two streams at once; waits that run out."""
+    rng = np.random.default_rng(22)
+    on, _ = layer(rng, 4, 256, 192, 64)
+    x = R.rng_tensor(rng, (90, 256), dtype)[0].to(dev())
+    r = R.rng_tensor(rng, (4, 256), dtype, 1 / 16)[0].to(dev())
+    ids, g = fgq.fgq_route_tokens(x, r, 2)
+    y = fgq.fgq_experts_w4(x, ids, g, *on)
+    z = x.clone()
+    z[7, 100] = float("nan")
+    out = fgq.fgq_experts_w4(z, ids, g, *on)
+    keep = [p for p in range(90) if p != 7]
+    assert torch.equal(out[keep], y[keep]) and not torch.isfinite(out[7]).any()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = fgq.fgq_moe_w4(x, r, 2, *on)
+    x.copy_(x.flip(0))
+    graph.replay()
+    assert torch.equal(out, y.flip(0))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            outs.append([fgq.fgq_moe_w4(x, r, 2, *on) for _ in range(5)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, out) for o in sum(outs, []))
+    assert fgq.fgq_stream_status() == fgq.FGQ_OK
+    seen = set()
+    for limit in (0, 1, 2, 4, 8, 16, 40):
+        for _ in range(3):
+            prev = fgq.fgq_debug_set_wait_limit_us(limit)
+            try:
+                o = fgq.fgq_moe_w4(x, r, 2, *on)
+            finally:
+                fgq.fgq_debug_set_wait_limit_us(prev)
+            status = fgq.fgq_stream_status()
+            assert status in (fgq.FGQ_OK, fgq.FGQ_ERR_TIMEOUT)
+            assert status != fgq.FGQ_OK or torch.equal(o, out)
+            seen.add(status)
+            assert torch.equal(fgq.fgq_moe_w4(x, r, 2, *on), out)
+            assert fgq.fgq_stream_status() == fgq.FGQ_OK
+    assert fgq.FGQ_ERR_TIMEOUT in seen
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])

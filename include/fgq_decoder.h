@@ -270,8 +270,8 @@ fgq_status fgq_read_weights_w4(const fgq_w4* w, float* out, cudaStream_t stream)
  * takes its scale in fp32, y is rounded once.  More than 32 tokens, or more than 8 of fp32 with more than 2^22 weights, run on fp16
  * operands on tcgen05: weights are exact there too within 2^26 of their row's largest scale, bf16 tokens within 2^26 of their largest
  * value (smaller ones are off by at most 2^-39 of it), fp32 tokens within 2^-22 of each value (or 2^-39 of the largest).  Scales
- * 2^-100 to 2^100 there, and outputs below 2^-100 may be 0.  A token that holds NaN or Inf gives values that are not finite; other tokens are
- * as without it.
+ * 2^-100 to 2^100 there, and outputs below 2^-100 may be 0.  A token that holds NaN or Inf gives values that are not finite; other
+ * tokens are as without it.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type, bad weights, more than one matrix, ldx < K), FGQ_ERR_ALIGN (x or y
  * not aligned to their elements, codes or scales not 16-byte, bias not 4-byte aligned), FGQ_ERR_UNSUPPORTED (P, K or M above
  * 2^31 - 2^16, more than 2^31 - 1 tiles), FGQ_ERR_CUDA (also where a temporary cannot be had).
@@ -306,8 +306,9 @@ fgq_status fgq_route_tokens(const void* x, fgq_float_type type, int P, int K, in
  *              twice.  weights  fp32 [P][top].
  *   y          out, elements of `type`, [P][K] contiguous; may be x where that is contiguous.
  * Between the layers values are held to 2^-12 (bf16 tokens, whose outputs round to 2^-9), 2^-17 (fp16) or exactly (fp32).  Sums are
- * fp32, in an order that depends on the sizes and on the tokens that share an expert.  Made for few tokens: 128 are taken at a
- * time, and each expert's weights are read again for those after.
+ * fp32, in an order that depends on the sizes and on the tokens that share an expert.  Up to 4096 choices are taken at a time; with more
+ * than 16 of them for an expert on average (8 of fp32; fewer where rows of more than 4096 leave room for fewer tokens) products run on
+ * fp16 operands as those of a linear layer of many tokens, with what is said there, and fp32 values between the layers are held to 2^-22.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type or weights, sizes that do not fit, top outside 1 .. 32, ldx < K),
  * FGQ_ERR_ALIGN, FGQ_ERR_UNSUPPORTED (E above 1024, K or F above 2^31 - 2^16, more than 2^31 - 1 tiles), FGQ_ERR_CUDA (also
  * where a temporary cannot be had).

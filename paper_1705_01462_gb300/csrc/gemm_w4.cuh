@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(G4Cfg<BN, W>::THREADS, G4Cfg<BN, W>::BLOCKS) g
         const uint4 v = __ldg(reinterpret_cast<const uint4*>(sc + (int64_t)c * (TILE_ROWS * PER)));
         const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top[i / PER] = max(top[i / PER], (i & 1 ? u[i / 2] >> 16 : u[i / 2]) & 0x7fffu);
+        for (int i = 0; i < 8; ++i)
+          if (i % PER < (c == n - 1 ? w.live : PER)) top[i / PER] = max(top[i / PER], (i & 1 ? u[i / 2] >> 16 : u[i / 2]) & 0x7fffu);
       }
 #pragma unroll
       for (int i = 0; i < 8 / PER; ++i) {
@@ -273,7 +274,7 @@ __global__ void __launch_bounds__(G4Cfg<BN, W>::THREADS, G4Cfg<BN, W>::BLOCKS) g
       up2[r] = pow2f(e - e / 2);
     }
     // lanes of odd rows take a word's neighbour first: stores of eight lanes, two rows, then meet all banks
-    const int odd = g & 1;
+    const int odd = g & 1, last = w.live < PER ? w.ct - 1 - c0 : -1;  // the stage with groups that are none
     for (int j0 = first; j0 < n && ok; j0 += STEP * AHEAD) {
 #pragma unroll
       for (int i = 0; i < AHEAD; ++i) {
@@ -284,7 +285,8 @@ __global__ void __launch_bounds__(G4Cfg<BN, W>::THREADS, G4Cfg<BN, W>::BLOCKS) g
         for (int r = 0; r < 2; ++r)
 #pragma unroll
           for (int k = 0; k < PER; ++k) {
-            const float s = (PER == 4 && odd ? tile[i].s[r].get(k ^ 1) : tile[i].s[r].get(k)) * up[r] * up2[r];
+            float s = (PER == 4 && odd ? tile[i].s[r].get(k ^ 1) : tile[i].s[r].get(k)) * up[r] * up2[r];
+            if (PER > 1 && j == last && (PER == 4 ? k ^ odd : k) >= w.live) s = 0.0f;
             s2[r][k] = pack2(s, s, __half());
           }
         uint4 v[2][4];

@@ -139,7 +139,7 @@ fgq_status launch_few(RowsArgs a, bool early, cudaStream_t s) {
 
 // ------------------------------------------------------------------ operands of the product for many tokens
 // What the blocks past the tokens do: find the exponent of each weight row's largest scale (subnormal ones: of the smallest normal), and
-// where w16 is given, write its rows as fp16, c s 2^(12 - e), `parts` blocks a row tile.  Padding takes part.
+// where w16 is given, write its rows as fp16, c s 2^(12 - e), `parts` blocks a row tile.  Groups past the matrix count as 0.
 struct Weights {
   Matrix w;
   int* wexp;      // all rows of the tiles; or nullptr:
@@ -162,9 +162,11 @@ __device__ __forceinline__ void prepare_weights(const Weights& a, int block) {
     const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const int at = 8 * i + 2 * k;
-      atomicMax(&top[at / w.per % TILE_ROWS], u[k] & 0x7fffu);
-      atomicMax(&top[(at + 1) / w.per % TILE_ROWS], u[k] >> 16 & 0x7fffu);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = 8 * i + 2 * k + h;
+        if (at % w.per < w.live || at < (w.ct - 1) * TILE_ROWS * w.per) atomicMax(&top[at / w.per % TILE_ROWS], u[k] >> 16 * h & 0x7fffu);
+      }
     }
   }
   __syncthreads();
@@ -193,6 +195,7 @@ __device__ __forceinline__ void prepare_weights(const Weights& a, int block) {
         if (k >= a.pitch) continue;
         float s = __uint_as_float((uint32_t)__ldg(w.scales + at * (TILE_ROWS * w.per) + (g + 8 * r) * w.per + j * w.per / 4) << 16);
         s = s * pow2f(e / 2) * pow2f(e - e / 2);  // in two factors: 2^e passes fp32's largest for subnormal rows
+        if (kt == w.ct - 1 && j * w.per / 4 >= w.live) s = 0.0f;
         *reinterpret_cast<uint4*>(a.w16 + m * a.pitch + k) = scaled_codes(word[j], pack2(s, s, __half()));
       }
     }

@@ -34,10 +34,11 @@ struct Matrix {
   const uint8_t* codes;
   const uint16_t* scales;  // bf16
   int rt, ct, per;
+  int live;  // groups of the last column tile that hold columns of the matrix: what stands for the others is no scale of its rows
 };
 inline Matrix matrix(const fgq_w4* w) {
   return {static_cast<const uint8_t*>(w->codes), static_cast<const uint16_t*>(w->scales), row_tiles(w->rows), col_tiles(w->cols),
-          TILE_COLS / w->group};
+          TILE_COLS / w->group, ((w->cols - 1) % TILE_COLS) / w->group + 1};
 }
 
 // Eight codes n of a word as four pairs of matrix operands (n - 8) UNIT: pair i holds values 2 i and 2 i + 1.  In the low

@@ -131,12 +131,13 @@ def quantize_w4(w, G):
 
 
 def pack_w4(c, s, G, fill=0):
-    """(codes uint8 [..][RT][CT][1024], scales uint16 [..][RT][CT][16][128 / G]); what stands past the matrix: code `fill`, scale 0."""
+    """(codes uint8 [..][RT][CT][1024], scales uint16 [..][RT][CT][16][128 / G]); what stands past the matrix: code `fill`, scale 0
+    (2^90 for other fills)."""
     lead, (M, K) = c.shape[:-2], c.shape[-2:]
     RT, CT, per = -(-M // 16), -(-K // 128), 128 // G
     n = np.full(lead + (RT * 16, CT * 128), fill + 8, np.uint8)
     n[..., :M, :K] = c + 8
-    sc = np.zeros(lead + (RT * 16, CT * per), np.float32)
+    sc = np.full(lead + (RT * 16, CT * per), 2.0 ** 90 if fill else 0.0, np.float32)
     sc[..., :M, :s.shape[-1]] = s
     codes = np.zeros(lead + (RT, CT, 1024), np.uint8)
     for m in range(16):

@@ -79,7 +79,7 @@ def test_many(dtype, G, P, K, M):
 @pytest.mark.parametrize("P,K,M,ld", [(1025, 4096, 2056, 0), (1030, 2500, 3360, 3), (1100, 2048, 4112, 8)])
 def test_expanded(dtype, P, K, M, ld):
     """So many tokens that the weights are expanded once: tokens in place, copied, and with rows apart."""
-    run(np.random.default_rng(P), P, K, M, 64, dtype, bias=ld > 0, ld=ld)
+    run(np.random.default_rng(P), P, K, M, 32, dtype, bias=ld > 0, ld=ld, fill=3)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
@@ -124,6 +124,8 @@ def test_strides_and_padding(dtype, P):
     for ld in (8, 1, 5):
         run(rng, P, 200, 40, 64, dtype, ld=ld, fill=5)
     run(rng, P, 205, 40, 64, dtype, fill=-3)
+    for G, K in ((32, 129), (32, 200), (64, 257), (128, 130), (32, 96)):
+        run(rng, P, K, 40, G, dtype, fill=6)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])

@@ -83,6 +83,7 @@ def test_many_odd_calls(dtype):
     ids[5] = -1
     ids[60:70] = 3
     run_experts(rng, 130, 200, 72, 6, 3, 64, dtype, ids=ids, Gd=32, fill=4, ld=1)
+    run_experts(rng, 90, 270, 140, 2, 1, 32, dtype, fill=-5)
     run_experts(rng, 150, 136, 40, 4, 1, 128, dtype, ids=np.full((150, 1), 3, np.int32), ld=8)
     run_experts(rng, 40, 128, 32, 2, 2, 32, dtype, ids=np.full((40, 2), -1, np.int32))
 

@@ -116,7 +116,11 @@ fgq_status launch_few(RowsArgs a, bool early, cudaStream_t s) {
   const int nt = columns <= 8 ? 1 : (columns <= 16 ? 2 : 4);
   const int tokens = 8 * nt / cpt;
   const int64_t tiles = ((int64_t)a.P + tokens - 1) / tokens;
-  if (nt <= 2) {  // one tile of tokens: held in shared memory where it fits
+  // One tile of tokens is held in shared memory where it fits, but a small matrix takes no longer to stream than the tokens to arrive.  bf16, us
+  // held and not: 8 tokens, 4096 -> 4096 7.5 and 6.0, 4096 -> 6144 8.2 and 8.5, 4096 -> 14336 11.2 and 14.2; one token 4096 -> 4096 5.6 and
+  // 5.6, 1024 -> 2048 3.5 and 3.7; 16 tokens, 4096 -> 8192 12.4 and 10.6, 4096 -> 14336 14.5 and 16.9.
+  const int64_t weights = (int64_t)a.w.rt * a.w.ct * (TILE_ROWS * TILE_COLS);
+  if (nt == 1 ? columns < 4 || weights > 1 << 24 : nt == 2 && weights > 1 << 25) {
     const ResidentPlan plan = plan_held(nt, a.w.ct, a.w.per, (int)columns);
     if (plan.warps > 0) {
       ResidentArgs r = {};
@@ -228,8 +232,8 @@ bool overlap(const void* x, const void* y, int type, int P, int K, int M, int64_
 }
 
 // From here on weights are expanded in memory for the product on pairs of SMs, which saves shared-memory traffic for the bytes.
-// bf16, us so and in gemm_w4.cu: 512 tokens, 4096 -> 14336 76.9 and 68.9; 1024 tokens 107.7 and 103.3, 4096 -> 4096 36.4 and 37.0;
-// 1536 tokens 149.6 and 169.4, 54.7 and 69.1; 2048 tokens 183 and 209, 57.5 and 70.9, but 1024 -> 2048 20.2 and 18.4.
+// bf16, us so and in gemm_w4.cu: 1024 tokens, 4096 -> 14336 108.8 and 102.0, 4096 -> 4096 36.9 and 36.1; 1280 tokens 130.9 and 134.0, 54.5 and
+// 65.2; 2048 tokens 184.8 and 206.4, 59.0 and 70.1, but 1024 -> 2048 20.2 and 18.4.
 constexpr int EXPAND_MIN_P = 1025;
 constexpr int64_t EXPAND_MIN_WEIGHTS = 1 << 23;
 
@@ -299,15 +303,14 @@ __global__ void __launch_bounds__(256) bias_kernel(const float* bias, void* y, i
     store_typed(y, ytype, i, bias ? __ldg(bias + i % M) : 0.0f);
 }
 
-// Tokens of 16 bits up to which the kernels of few tokens run.  bf16, us there and in gemm_w4.cu: 16 tokens, 4096 -> 4096 10.0 and 12.0, 4096 ->
-// 14336 14.5 and 25.0; 32 tokens 9.5 and 12.2, 28.1 and 25.3, 8192 -> 8192 27.2 and 28.2; 33 tokens 25.9 and 12.3, 49.8 and 25.3.
-constexpr int FEW_MAX_P = 32;
-// fp32: 8 tokens, or 32 of a small matrix.  us there and in gemm_w4.cu: 8 tokens, 4096 -> 4096 8.7 and 13.1, 4096 -> 14336 24.0 and 26.9; 16 tokens
-// 13.1 and 13.3, 40.7 and 26.9; 24 tokens 22.1 and 13.4, 2048 -> 4096 13.5 and 10.8, but 2048 -> 2048 8.5 and 10.4.
-constexpr int FEW_MAX_P_F32 = 8;
-constexpr int64_t FEW_SMALL = 1 << 22;
+// Tokens up to which the kernels of few tokens run: 16, or 32 of up to 2^25 weights.  bf16, us there and in gemm_w4.cu: 16 tokens, 4096 -> 4096
+// 10.0 and 12.7, 4096 -> 14336 14.5 and 22.5; 32 tokens 9.4 and 13.2, 4096 -> 8192 16.8 and 18.4, but 28.6 and 22.8, 8192 -> 65536 179 and 144.
+// fp32: 8 tokens, or 32 of up to 2^22 weights: 8 tokens, 4096 -> 4096 8.7 and 13.1, 4096 -> 14336 24.0 and 26.9; 16 tokens 13.1 and 13.3, 40.7 and
+// 26.9; 24 tokens 22.1 and 13.4, 2048 -> 4096 13.5 and 10.8, but 2048 -> 2048 8.5 and 10.4.
 int few_tokens(int type, int K, int M) {
-  return type == FGQ_F32 && (int64_t)K * M > FEW_SMALL ? FEW_MAX_P_F32 : FEW_MAX_P;
+  const int64_t weights = (int64_t)K * M;
+  if (type == FGQ_F32) return weights > 1 << 22 ? 8 : 32;
+  return weights > 1 << 25 ? 16 : 32;
 }
 
 }  // namespace

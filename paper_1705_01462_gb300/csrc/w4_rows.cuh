@@ -177,15 +177,21 @@ constexpr int rows_smem() {
   return Ring<NT>::TOTAL > sums ? Ring<NT>::TOTAL : sums;
 }
 
-// Blocks of a launch: an item a cluster, or as many as share the items evenly.  Two blocks an SM.
+// Blocks of a launch: an item a cluster, split down to a tile column or two a block where that is one block an SM at most (us, 32 tokens of
+// bf16, 1024 -> 2048 5.6, four columns at least 6.4) and to two or more where it is two (32 of fp32, 1111 -> 999 6.9, one or two 8.5); or
+// as many as share the items evenly, two an SM.
 struct RowsPlan {
   int splits;
   unsigned grid;
 };
 inline RowsPlan plan_rows(int64_t items, int ct) {
   RowsPlan p = {1, 0};
-  const int64_t most = 2ll * device_sms();
-  while (p.splits < 8 && items * p.splits * 2 <= most && ct >= 4 * p.splits) p.splits *= 2;
+  const int64_t sms = device_sms(), most = 2 * sms;
+  while (p.splits < 8 && ct >= 2 * p.splits) {
+    const int64_t blocks = items * p.splits * 2;
+    if (blocks > most || (blocks > sms && ct < 4 * p.splits)) break;
+    p.splits *= 2;
+  }
   if (p.splits > 1) {
     p.grid = (unsigned)(items * p.splits);
   } else {

@@ -14,7 +14,7 @@ MANY = 33
 
 
 def many(dtype, P, K, M):
-    return P >= MANY or (dtype == "f32" and P >= 9 and K * M > 1 << 22)
+    return P >= MANY or (P >= 9 and K * M > 1 << 22 if dtype == "f32" else P >= 17 and K * M > 1 << 25)
 
 
 @pytest.mark.parametrize("G", [32, 64, 128])
@@ -69,7 +69,7 @@ def test_products(dtype, G, P, K, M):
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("G,P,K,M", [(64, 9, 4096, 1100), (32, 16, 8192, 520), (128, 40, 8200, 130), (64, 70, 2048, 2100),
-                                     (32, 130, 1000, 4300), (128, 300, 1111, 3800), (64, 260, 5120, 8200), (64, 1025, 520, 8000)])
+                                     (32, 130, 1000, 4300), (128, 300, 1111, 3800), (64, 260, 5120, 8200), (64, 1025, 520, 8000), (64, 18, 8192, 4100)])
 def test_many(dtype, G, P, K, M):
     """Tiles of 64, 128 and 256 tokens, K in one piece and in parts, the last of them short."""
     run(np.random.default_rng(P + K), P, K, M, G, dtype, bias=M % 200 == 0)

@@ -64,8 +64,19 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
   }
   const int rt = a.w.rt;  // items of a unit
   const int items = MODE == MODE_LINEAR || a.items > 0 ? a.items : __ldcg(a.nunits) * rt;
-  const int run = (items + (int)gridDim.x - 1) / (int)gridDim.x;
-  const int i0 = (int)blockIdx.x * run, i1 = min(i0 + run, items);
+  int i0, i1;
+  const int units = items / rt;
+  // a few units: equal blocks each, as a run that crosses into the next unit has its tokens to wait for (one token, 8 experts of 64 2048 -> 1024
+  // 21.8 us without and 20.5; two tokens 29.5 and 25.6)
+  if (MODE != MODE_LINEAR && units > 0 && 2 * units <= (int)gridDim.x) {
+    const int blocks = (int)gridDim.x / units, run = (rt + blocks - 1) / blocks, unit = (int)blockIdx.x / blocks, j = (int)blockIdx.x - unit * blocks;
+    i0 = unit * rt + min(j * run, rt);
+    i1 = unit < units ? unit * rt + min((j + 1) * run, rt) : 0;
+  } else {
+    const int run = (items + (int)gridDim.x - 1) / (int)gridDim.x;
+    i0 = (int)blockIdx.x * run;
+    i1 = min(i0 + run, items);
+  }
   if (i0 >= i1) return;
 
   // a segment: the run's items of one unit
@@ -379,7 +390,7 @@ fgq_status launch_resident(ResidentArgs a, const ResidentPlan& plan, int64_t ite
   if (!tc::smem_attr_once<resident_kernel<T, MT, NT, PER, PARTS, MODE, AHEAD>>(RES_SMEM)) return FGQ_ERR_CUDA;
   const int64_t most = device_sms(), run = (items + most - 1) / most;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((items + run - 1) / run));
+  cfg.gridDim = dim3((unsigned)(MODE == MODE_LINEAR ? (items + run - 1) / run : (items < most ? items : most)));
   cfg.blockDim = dim3(32 * plan.warps);
   cfg.dynamicSmemBytes = plan.smem;
   cfg.stream = s;

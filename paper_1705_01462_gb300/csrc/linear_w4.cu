@@ -91,22 +91,12 @@ __global__ void __launch_bounds__(256) read_kernel(const uint8_t* codes, const u
   }
 }
 
-// ------------------------------------------------------------------ tokens as operand rows
-// A block a token: fp32 in three bf16 parts, 16-bit types copied to aligned rows; zeros up to a multiple of 8.
-template <typename T>
-__global__ void __launch_bounds__(256) copy_tokens_kernel(const T* __restrict__ x, int P, int K, int64_t ldx, uint16_t* dst, int64_t pitch) {
+// ------------------------------------------------------------------ tokens that outputs would overwrite
+// A block a token: its row, zeros up to `pitch` elements.
+template <typename E>
+__global__ void __launch_bounds__(256) copy_tokens_kernel(const E* __restrict__ x, int K, int64_t ldx, E* dst, int64_t pitch) {
   pdl_trigger();
-  const T* row = x + blockIdx.x * ldx;
-  for (int64_t k = threadIdx.x; k < pitch; k += 256) {
-    if constexpr (std::is_same<T, float>::value) {
-      uint16_t p[3];
-      three_parts(k < K ? row[k] : 0.0f, p);
-      uint16_t* to = dst + 3 * pitch * blockIdx.x + k;
-      to[0] = p[0], to[pitch] = p[1], to[2 * pitch] = p[2];
-    } else {
-      dst[pitch * blockIdx.x + k] = k < K ? *reinterpret_cast<const uint16_t*>(row + k) : (uint16_t)0;
-    }
-  }
+  for (int64_t k = threadIdx.x; k < pitch; k += 256) dst[pitch * blockIdx.x + k] = k < K ? x[blockIdx.x * ldx + k] : E(0);
 }
 
 // ------------------------------------------------------------------ few tokens
@@ -245,7 +235,7 @@ fgq_status run_many(const void* x, int type, int P, int K, int64_t ldx, const fg
   const ManyPlan plan = plan_many(P, parts, wt.w.ct, M);
   const GemmPlan pairs = expand ? plan_gemm_w8a8(P, K, M) : GemmPlan{};
   // fp16 tokens are operands as they are (expanded: where their rows are whole K-tiles beside one another)
-  const bool vec = K % 8 == 0 && aligned(x, 16) && (P == 1 || stride16(ldx, type));
+  const bool vec = K % 8 == 0 && pieces16(x, type, P, K, ldx);
   const bool direct = type == FGQ_F16 && vec && !overlap(x, y, type, P, K, M, ldx) && (!expand || (K == pairs.pitch && (P == 1 || ldx == K)));
   const int64_t pitch = expand ? pairs.pitch : (direct && P > 1 ? ldx : copied_pitch(K));
   const size_t e_bytes = up256((size_t)wt.w.rt * TILE_ROWS * 4), x_bytes = direct ? 0 : up256((size_t)P * parts * pitch * 2);
@@ -315,16 +305,6 @@ int few_tokens(int type, int K, int M) {
 
 }  // namespace
 
-fgq_status launch_copy_tokens(const void* x, int type, int P, int K, int64_t ldx, void* dst, cudaStream_t s) {
-  const int64_t pitch = copied_pitch(K);
-  uint16_t* d = static_cast<uint16_t*>(dst);
-  if (type == FGQ_F32)
-    copy_tokens_kernel<float><<<P, 256, 0, s>>>(static_cast<const float*>(x), P, K, ldx, d, pitch);
-  else
-    copy_tokens_kernel<__half><<<P, 256, 0, s>>>(static_cast<const __half*>(x), P, K, ldx, d, pitch);
-  return after_launch();
-}
-
 }  // namespace w4
 }  // namespace fgq
 
@@ -391,13 +371,19 @@ fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx,
   }
   if (P > few_tokens(type, K, M)) return run_many(x, type, P, K, P > 1 ? ldx : 0, w, bias, y, stream);
   RowsArgs a = {};
-  a.w = matrix(w), a.x = {x, P > 1 ? ldx : 0, K}, a.bias = bias, a.y = y, a.P = P, a.M = M, a.ytype = type;
-  if (direct_tokens(x, type, P, K, ldx) && !overlap(x, y, type, P, K, M, ldx)) return launch_few(a, false, stream);
-  void* tmp = scratch_alloc(copied_bytes(type, P, K), stream);
-  if (!tmp) return FGQ_ERR_CUDA;
+  a.w = matrix(w), a.x = token_rows(x, type, P, K, P > 1 ? ldx : 0), a.bias = bias, a.y = y, a.P = P, a.M = M, a.ytype = type;
+  // tokens that outputs would overwrite are copied first, and those of a large matrix that are not in pieces of 16 bytes (us, 8 tokens of bf16,
+  // 4095 -> 14336 11.9 in place of 21.0; 4095 -> 4096 takes 8.1 as it is)
+  if (!overlap(x, y, type, P, K, M, ldx) && (a.x.load != ROWS_SINGLE || P == 1 || (int64_t)K * M <= 1 << 24)) return launch_few(a, false, stream);
   const int64_t pitch = copied_pitch(K);
-  a.x = {tmp, type == FGQ_F32 ? 3 * pitch : pitch, (int)pitch};
-  fgq_status st = launch_copy_tokens(x, type, P, K, ldx, tmp, stream);
+  void* tmp = scratch_alloc((size_t)P * pitch * float_bytes(type), stream);
+  if (!tmp) return FGQ_ERR_CUDA;
+  if (type == FGQ_F32)
+    copy_tokens_kernel<<<P, 256, 0, stream>>>(static_cast<const float*>(x), K, ldx, static_cast<float*>(tmp), pitch);
+  else
+    copy_tokens_kernel<<<P, 256, 0, stream>>>(static_cast<const uint16_t*>(x), K, ldx, static_cast<uint16_t*>(tmp), pitch);
+  fgq_status st = after_launch();
+  a.x = {tmp, pitch, (int)pitch, type == FGQ_F32 ? ROWS_PIECES : ROWS_COPIED};
   if (st == FGQ_OK) st = launch_few(a, true, stream);
   if (cudaFreeAsync(tmp, stream) != cudaSuccess && st == FGQ_OK) st = FGQ_ERR_CUDA;
   return st;

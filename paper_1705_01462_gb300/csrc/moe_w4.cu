@@ -276,6 +276,25 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
   }
 }
 
+// ------------------------------------------------------------------ tokens as operand rows
+// A block a token: fp32 in three bf16 parts, 16-bit types copied to aligned rows; zeros up to a multiple of 8.  (Brought into form by the
+// products themselves, 64 tokens of 6 of 64 experts 4096 -> 1536 took 164 us, for all types, in place of 148: registers spilled.)
+template <typename T>
+__global__ void __launch_bounds__(256) operand_rows_kernel(const T* __restrict__ x, int K, int64_t ldx, uint16_t* dst, int64_t pitch) {
+  pdl_trigger();
+  const T* row = x + blockIdx.x * ldx;
+  for (int64_t k = threadIdx.x; k < pitch; k += 256) {
+    if constexpr (std::is_same<T, float>::value) {
+      uint16_t p[3];
+      three_parts(k < K ? row[k] : 0.0f, p);
+      uint16_t* to = dst + 3 * pitch * blockIdx.x + k;
+      to[0] = p[0], to[pitch] = p[1], to[2 * pitch] = p[2];
+    } else {
+      dst[pitch * blockIdx.x + k] = k < K ? row[k] : (uint16_t)0;
+    }
+  }
+}
+
 // ------------------------------------------------------------------ choices by expert
 constexpr int GR_THREADS = 1024;
 
@@ -439,14 +458,14 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   const int K = gate->cols, F = gate->rows, E = gate->experts;
   const int most = MAX_CHOICES / top, pass = P < most ? P : most, A = pass * top;  // tokens and choices of a pass
   const int parts = type == FGQ_F32 ? 3 : 1;
-  const int64_t hpitch = (int64_t)row_tiles(F) * TILE_ROWS;
+  const int64_t hpitch = (int64_t)row_tiles(F) * TILE_ROWS, xpitch = parts * copied_pitch(K);
   const HeldPlan plan = plan_units(type, pass, col_tiles(K), TILE_COLS / gate->group, col_tiles(F), TILE_COLS / down->group);
   const bool held = A <= (int64_t)HELD_UNITS * plan.most * E;
   const bool small = type == FGQ_F32 && A <= (int64_t)UNIT_32_MAX_F32 * E;
   const int cap = held ? plan.cap : (small ? 32 : (A <= (int64_t)UNIT_64_MAX * E ? 64 : 128));
-  const bool direct = !held || direct_tokens(x, type, P, K, ldx);
+  const bool direct = !held || (type != FGQ_F32 && pieces16(x, type, P, K, ldx));
   const int most_units = (A < E || pass == 1 ? A : E) + A / cap;
-  const size_t b_x = direct ? 0 : up256(copied_bytes(type, pass, K));
+  const size_t b_x = direct ? 0 : up256((size_t)pass * xpitch * 2);
   const size_t b_h = held ? up256((size_t)A * hpitch * 4) : up256(experts_many_bytes(type, A, K, F));
   const size_t b_units = up256(sizeof(Unit) * most_units), b_choices = up256(sizeof(Choice) * (size_t)A), b_n = 256;
   const size_t b_places = up256(4 * (size_t)A), b_z = up256(4 * (size_t)A * K), b_ids = route ? b_places : 0;
@@ -458,7 +477,7 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
     at += n;
     return p;
   };
-  void* xc = take(b_x);
+  uint16_t* xc = reinterpret_cast<uint16_t*>(take(b_x));
   void* h = take(b_h);
   Unit* units = reinterpret_cast<Unit*>(take(b_units));
   Choice* choices = reinterpret_cast<Choice*>(take(b_choices));
@@ -473,12 +492,15 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   for (int p0 = 0; p0 < P && st == FGQ_OK; p0 += pass) {
     const int np = P - p0 < pass ? P - p0 : pass, na = np * top;
     const uint8_t* xp = static_cast<const uint8_t*>(x) + p0 * ldx * float_bytes(type);
-    TokenRows rows = {xp, ldx, K};
+    TokenRows rows = {xp, ldx, K, ROWS_COPIED};
     if (!direct) {
-      st = launch_copy_tokens(xp, type, np, K, ldx, xc, s);
+      if (type == FGQ_F32)
+        operand_rows_kernel<<<np, 256, 0, s>>>(reinterpret_cast<const float*>(xp), K, ldx, xc, copied_pitch(K));
+      else
+        operand_rows_kernel<<<np, 256, 0, s>>>(reinterpret_cast<const uint16_t*>(xp), K, ldx, xc, copied_pitch(K));
+      st = after_launch();
       if (st != FGQ_OK) break;
-      const int64_t pitch = copied_pitch(K);
-      rows = {xc, parts * pitch, (int)pitch};
+      rows = {xc, xpitch, (int)copied_pitch(K), ROWS_COPIED};
     }
     const int32_t* pid = ids ? ids + (int64_t)p0 * top : own_ids;
     const float* pw = weights ? weights + (int64_t)p0 * top : own_weights;

@@ -237,7 +237,7 @@ struct Ring {
   static constexpr int TOTAL = STAGES * BYTES;
 };
 
-// The 16-byte pieces of a stage that one thread copies: piece tid % 16 of columns tid / 16 + 16 i.
+// The 16-byte pieces of a stage of 16-bit tokens that one thread copies: piece tid % 16 of columns tid / 16 + 16 i.
 template <int NT>
 struct Columns {
   int64_t off[Ring<NT>::COPIES];  // bytes from the tokens' start, or -1: zeros
@@ -264,12 +264,14 @@ struct Choice {
   float weight;
 };
 
-// Tokens as operand rows: 16-bit elements, a token's `parts` rows beside one another (fp32: three bf16 parts that add up
-// to it exactly, in four columns of a product; 16-bit: themselves).
+// Tokens as they are given, rows of elements of their type (the experts': 16-bit elements in pieces, fp32 in three rows of bf16 parts).
+enum { ROWS_COPIED = 0, ROWS_SINGLE = 1, ROWS_PIECES = 2 };
 struct TokenRows {
   const void* data;
   int64_t pitch;  // elements between tokens
-  int kvalid;     // elements of a row that hold values or zeros, a multiple of 8
+  int kvalid;     // elements of a row
+  // ROWS_COPIED: 16-bit elements in 16-byte pieces that are operands as they are; or elements to be loaded one by one, or (fp32) in pieces
+  int load;
 };
 __host__ __device__ constexpr int columns_per_token(int parts) { return parts == 3 ? 4 : parts; }
 
@@ -282,14 +284,62 @@ __device__ __forceinline__ void three_parts(float v, uint16_t (&p)[3]) {
   p[2] = (uint16_t)(__float_as_uint(c) >> 16);
 }
 
-// Whether 16-bit tokens can be read in place: 16-byte pieces that end with the row.
-inline bool direct_tokens(const void* x, int type, int P, int K, int64_t ldx) {
-  return type != FGQ_F32 && K % 8 == 0 && aligned(x, 16) && (P == 1 || stride16(ldx, type));
+// Eight elements of a token on their way through registers: fp32 to three bf16 parts, 16-bit ones as they are.
+template <int PARTS>
+struct Eight {
+  uint32_t v[PARTS == 3 ? 8 : 4];
+  // elements [k, + 8) of a row; zeros past its end, and where row < 0
+  __device__ __forceinline__ void load(const TokenRows& x, int64_t row, int k) {
+    const int n = row < 0 ? 0 : x.kvalid - k;
+    if constexpr (PARTS == 3) {
+      const uint32_t* p = static_cast<const uint32_t*>(x.data) + row * x.pitch + k;
+      if (x.load == ROWS_PIECES && n >= 8) {
+        const uint4 a = __ldcg(reinterpret_cast<const uint4*>(p)), b = __ldcg(reinterpret_cast<const uint4*>(p) + 1);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        return;
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < n ? __ldcg(p + i) : 0u;
+    } else {
+      const unsigned short* p = static_cast<const unsigned short*>(x.data) + row * x.pitch + k;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = 2 * i < n ? __ldcg(p + 2 * i) : 0u, hi = 2 * i + 1 < n ? __ldcg(p + 2 * i + 1) : 0u;
+        v[i] = lo | hi << 16;
+      }
+    }
+  }
+  // as columns of token `tok` in a stage, piece `chunk`; fp32: three of them, and one of zeros
+  __device__ __forceinline__ void store(uint8_t* stage, int tok, int chunk) const {
+    if constexpr (PARTS == 3) {
+      uint32_t w[3][4];
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        uint16_t p[3], q[3];
+        three_parts(__uint_as_float(v[2 * h]), p);
+        three_parts(__uint_as_float(v[2 * h + 1]), q);
+#pragma unroll
+        for (int c = 0; c < 3; ++c) w[c][h] = p[c] | (uint32_t)q[c] << 16;
+      }
+#pragma unroll
+      for (int c = 0; c < 3; ++c)
+        *reinterpret_cast<uint4*>(stage + chunk_at(4 * tok + c, chunk)) = make_uint4(w[c][0], w[c][1], w[c][2], w[c][3]);
+      *reinterpret_cast<uint4*>(stage + chunk_at(4 * tok + 3, chunk)) = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+      *reinterpret_cast<uint4*>(stage + chunk_at(tok, chunk)) = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+  }
+};
+
+// How tokens are loaded: pieces of 16 bytes where they end with the row.
+inline bool pieces16(const void* x, int type, int P, int K, int64_t ldx) {
+  return K % (type == FGQ_F32 ? 4 : 8) == 0 && aligned(x, 16) && (P == 1 || stride16(ldx, type));
+}
+inline TokenRows token_rows(const void* x, int type, int P, int K, int64_t ldx) {
+  const bool pieces = pieces16(x, type, P, K, ldx);
+  return {x, ldx, K, pieces ? (type == FGQ_F32 ? ROWS_PIECES : ROWS_COPIED) : ROWS_SINGLE};
 }
 inline int64_t copied_pitch(int K) { return ((int64_t)K + 7) / 8 * 8; }
-inline size_t copied_bytes(int type, int P, int K) { return (size_t)P * copied_pitch(K) * 2 * (type == FGQ_F32 ? 3 : 1); }
-// Tokens in operand rows at `dst` (copied_bytes of it).
-fgq_status launch_copy_tokens(const void* x, int type, int P, int K, int64_t ldx, void* dst, cudaStream_t s);
 
 }  // namespace w4
 }  // namespace fgq

@@ -39,11 +39,16 @@ fgq_status launch_held_type(const ResidentArgs& a, int nt, const ResidentPlan& p
   return launch_held_per<T, 1, 2, PARTS, MODE_LINEAR, HELD_AHEAD>(a, plan, a.items, chained, s);
 }
 
+template <typename T, int NT, int PER, int PARTS>
+fgq_status launch_rows_load(const RowsArgs& a, unsigned grid, bool chained, cudaStream_t s) {
+  if constexpr (PARTS == 1)
+    if (a.x.load == ROWS_COPIED) return launch_rows<T, NT, PER, PARTS, ROWS_AHEAD, false>(a, grid, chained, s);
+  return launch_rows<T, NT, PER, PARTS, ROWS_AHEAD, true>(a, grid, chained, s);
+}
 template <typename T, int NT, int PARTS>
 fgq_status launch_rows_per(const RowsArgs& a, unsigned grid, bool chained, cudaStream_t s) {
-  if (a.w.per == 4) return launch_rows<T, NT, 4, PARTS, ROWS_AHEAD>(a, grid, chained, s);
-  if (a.w.per == 2) return launch_rows<T, NT, 2, PARTS, ROWS_AHEAD>(a, grid, chained, s);
-  return launch_rows<T, NT, 1, PARTS, ROWS_AHEAD>(a, grid, chained, s);
+  if (a.w.per == 4) return launch_rows_load<T, NT, 4, PARTS>(a, grid, chained, s);
+  return a.w.per == 2 ? launch_rows_load<T, NT, 2, PARTS>(a, grid, chained, s) : launch_rows_load<T, NT, 1, PARTS>(a, grid, chained, s);
 }
 template <typename T, int PARTS>
 fgq_status launch_rows_type(const RowsArgs& a, int nt, unsigned grid, bool chained, cudaStream_t s) {

@@ -40,6 +40,26 @@ constexpr int RES_SMEM = 226 * 1024;  // a kilobyte is left for what is not dyna
 // Warps of a block at most: 80 registers a thread, or 96 where two row tiles meet 16 columns.
 constexpr int resident_warps(int mt, int nt) { return mt * nt >= 4 ? 20 : 24; }
 
+// Tokens through registers to shared memory, by a whole block.  A function of its own, or its registers would be the kernel's.
+template <int PARTS>
+__device__ __noinline__ void load_tokens(const TokenRows& x, int count, int ct, int stage, uint8_t* smem) {
+  constexpr int BATCH = PARTS == 3 ? 2 : 4;  // loads in flight
+  const int n = ct * 16 * count, threads = (int)blockDim.x;
+  for (int i0 = threadIdx.x; i0 < n; i0 += BATCH * threads) {
+    Eight<PARTS> e[BATCH];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = i0 + b * threads, j = i >> 4, kt = j / count, tok = j - kt * count;
+      if (i < n) e[b].load(x, tok, kt * TILE_COLS + 8 * (i & 15));
+    }
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = i0 + b * threads, j = i >> 4, kt = j / count, tok = j - kt * count;
+      if (i < n) e[b].store(smem + kt * stage, tok, i & 15);
+    }
+  }
+}
+
 // MT: 2 tiles of MODE_GATED, gate's and up's, else 1.
 template <typename T, int MT, int NT, int PER, int PARTS, int MODE, int AHEAD>
 __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(const __grid_constant__ ResidentArgs a) {
@@ -189,15 +209,20 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
       if (threadIdx.x < now.u.z) row_of[threadIdx.x] = __ldcg(&a.choices[now.u.y + threadIdx.x].token);
       __syncthreads();
     }
-    const int cols = now.u.z * CPT, n = ct * 16 * cols;
-    for (int i = threadIdx.x; i < n; i += 32 * W) {
-      const int chunk = i & 15, j = i >> 4, kt = j / cols, c = j - kt * cols, tok = c / CPT, part = c % CPT, k = kt * TILE_COLS + 8 * chunk;
-      const int64_t row = MODE == MODE_LINEAR ? tok : (a.one ? 0 : row_of[tok]);
-      const bool live = part < PARTS && k < a.x.kvalid;
-      cp_async16(xs + kt * STAGE + chunk_at(c, chunk), live ? xb + 2 * (row * a.x.pitch + part * (a.x.pitch / PARTS) + k) : xb, live ? 16u : 0u);
+    // pieces of 16 bytes as they are; the experts' fp32 tokens: three rows of bf16 parts beside one another
+    if (MODE == MODE_GATED || (PARTS == 1 && a.x.load == ROWS_COPIED)) {
+      const int cols = now.u.z * CPT, n = ct * 16 * cols;
+      for (int i = threadIdx.x; i < n; i += 32 * W) {
+        const int chunk = i & 15, j = i >> 4, kt = j / cols, c = j - kt * cols, tok = c / CPT, part = c % CPT, k = kt * TILE_COLS + 8 * chunk;
+        const int64_t row = MODE == MODE_LINEAR ? tok : (a.one ? 0 : row_of[tok]);
+        const bool live = part < PARTS && k < a.x.kvalid;
+        cp_async16(xs + kt * STAGE + chunk_at(c, chunk), live ? xb + 2 * (row * a.x.pitch + part * (a.x.pitch / PARTS) + k) : xb, live ? 16u : 0u);
+      }
+      cp_async_commit();
+      cp_async_wait<0>();
+    } else if constexpr (MODE == MODE_LINEAR) {
+      load_tokens<PARTS>(a.x, now.u.z, ct, STAGE, w4_smem);
     }
-    cp_async_commit();
-    cp_async_wait<0>();
     __syncthreads();
   };
   // what becomes of the finished sums of row r of an item and token tok: of gate and up, or of one matrix.  MODE_GATED: the

@@ -18,8 +18,9 @@ struct RowsArgs {
   int early;  // the kernel before is this library's: weights may be loaded while it runs
 };
 
-template <typename T, int NT, int PER, int PARTS, int AHEAD>
-__global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ RowsArgs a) {
+// RAW: tokens go through registers.
+template <typename T, int NT, int PER, int PARTS, int AHEAD, bool RAW>
+__global__ void __launch_bounds__(THREADS, 2) rows_kernel(const __grid_constant__ RowsArgs a) {
   using R = Ring<NT>;
   constexpr int CPT = columns_per_token(PARTS), TOKENS = 8 * NT / CPT;
   extern __shared__ __align__(16) uint8_t w4_smem[];
@@ -58,10 +59,10 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ R
   auto columns = [&](const Item& it) {
 #pragma unroll
     for (int i = 0; i < R::COPIES; ++i) {
-      const int col = (int)(threadIdx.x >> 4) + 16 * i, tok = col / CPT, part = col % CPT;
+      const int tok = (int)(threadIdx.x >> 4) + 16 * i;
       cols.off[i] = -1;
-      if (tok < it.count && part < PARTS) {
-        cols.off[i] = 2 * ((it.tok0 + tok) * a.x.pitch + part * (a.x.pitch / PARTS));
+      if (tok < it.count) {
+        cols.off[i] = 2 * ((it.tok0 + tok) * a.x.pitch);
       }
     }
   };
@@ -78,26 +79,61 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ R
       if (++wi < i1) wit = item_at(wi);
     }
   };
-  auto next_tokens = [&]() {
-    cols.copy(ring_at + xslot * R::BYTES, xb, c0 + xkt, a.x.kvalid);
-    xslot = xslot + 1 == R::STAGES ? 0 : xslot + 1;
+  auto next_place = [&]() {
     if (++xkt == ct) {
       xkt = 0;
       if (++xi < i1) {
         xit = item_at(xi);
-        columns(xit);
+        if (!RAW) columns(xit);
       }
     }
   };
+  auto next_slot = [&]() { xslot = xslot + 1 == R::STAGES ? 0 : xslot + 1; };
+  auto next_tokens = [&]() {
+    cols.copy(ring_at + xslot * R::BYTES, xb, c0 + xkt, a.x.kvalid);
+    next_slot();
+    next_place();
+  };
+  // tokens that go through registers: loaded a stage before they are stored
+  constexpr int PIECES = (TOKENS + 15) / 16;  // of a thread and stage
+  const int chunk = threadIdx.x & 15;
+  auto fetch = [&](Eight<PARTS>(&e)[PIECES]) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int tok = (int)(threadIdx.x >> 4) + 16 * i;
+      e[i].load(a.x, tok < xit.count ? xit.tok0 + tok : -1, (c0 + xkt) * TILE_COLS + 8 * chunk);
+    }
+    next_place();
+  };
+  auto put = [&](const Eight<PARTS>(&e)[PIECES]) {
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+      const int tok = (int)(threadIdx.x >> 4) + 16 * i;
+      if (tok < TOKENS) e[i].store(w4_smem + xslot * R::BYTES, tok, chunk);
+    }
+    next_slot();
+  };
+  Eight<PARTS> ahead[PIECES];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i)
     if (i < n) next_weights(i);
   if (a.early) pdl_wait();
-  columns(xit);
+  if constexpr (!RAW) {
+    columns(xit);
 #pragma unroll
-  for (int i = 0; i < R::STAGES - 1; ++i) {
-    if (i < n) next_tokens();
-    cp_async_commit();
+    for (int i = 0; i < R::STAGES - 1; ++i) {
+      if (i < n) next_tokens();
+      cp_async_commit();
+    }
+  } else {
+    Eight<PARTS> first[R::STAGES - 1][PIECES];
+#pragma unroll
+    for (int i = 0; i < R::STAGES - 1; ++i)
+      if (i < n) fetch(first[i]);
+    if (R::STAGES - 1 < n) fetch(ahead);
+#pragma unroll
+    for (int i = 0; i < R::STAGES - 1; ++i)
+      if (i < n) put(first[i]);
   }
   pair_t sum[1][NT][2];
   auto clear = [&]() {
@@ -140,8 +176,13 @@ __global__ void __launch_bounds__(THREADS) rows_kernel(const __grid_constant__ R
       if (q + i >= n) break;  // the same for the whole block
       cp_async_wait<R::STAGES - 2>();
       __syncthreads();  // the stage is there for everyone, and the one before has been read
-      if (q + i + R::STAGES - 1 < n) next_tokens();
-      cp_async_commit();
+      if constexpr (!RAW) {
+        if (q + i + R::STAGES - 1 < n) next_tokens();
+        cp_async_commit();
+      } else if (q + i + R::STAGES - 1 < n) {
+        put(ahead);
+        if (q + i + R::STAGES < n) fetch(ahead);
+      }
       multiply<T, 1, NT, PER>(tile[i], w4_smem + slot * R::BYTES, pieces, sum);
       slot = slot + 1 == R::STAGES ? 0 : slot + 1;
       if (q + i + AHEAD < n) next_weights(i);
@@ -201,11 +242,11 @@ inline RowsPlan plan_rows(int64_t items, int ct) {
   return p;
 }
 
-template <typename T, int NT, int PER, int PARTS, int AHEAD>
+template <typename T, int NT, int PER, int PARTS, int AHEAD, bool RAW>
 fgq_status launch_rows(const RowsArgs& a, unsigned grid, bool chained, cudaStream_t s) {
-  constexpr auto kernel = rows_kernel<T, NT, PER, PARTS, AHEAD>;
+  constexpr auto kernel = rows_kernel<T, NT, PER, PARTS, AHEAD, RAW>;
   constexpr int smem = rows_smem<NT>();
-  if (!tc::smem_attr_once<rows_kernel<T, NT, PER, PARTS, AHEAD>>(smem)) return FGQ_ERR_CUDA;
+  if (!tc::smem_attr_once<rows_kernel<T, NT, PER, PARTS, AHEAD, RAW>>(smem)) return FGQ_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(THREADS);

@@ -124,6 +124,8 @@ def test_strides_and_padding(dtype, P):
     for ld in (8, 1, 5):
         run(rng, P, 200, 40, 64, dtype, ld=ld, fill=5)
     run(rng, P, 205, 40, 64, dtype, fill=-3)
+    if P < 40:  # rows of a large matrix that are not in pieces of 16 bytes
+        run(rng, P, 4099, 4200, 64, dtype)
     for G, K in ((32, 129), (32, 200), (64, 257), (128, 130), (32, 96)):
         run(rng, P, K, 40, G, dtype, fill=6)
 
@@ -206,10 +208,12 @@ def test_no_scratch():
     w = R.weights(c, s, 64, dev())
     prev = fgq.fgq_debug_set_scratch_limit(0)
     try:
-        fgq.fgq_linear_w4(R.rng_tensor(rng, (4, 256), "bf16")[0].to(dev()), w)
-        for P, dtype in ((4, "f32"), (100, "bf16")):
+        for dtype in ("bf16", "f32"):
+            fgq.fgq_linear_w4(R.rng_tensor(rng, (4, 256), dtype)[0].to(dev()), w)
+        buf = torch.zeros((4, 256), device=dev())
+        for x, y in ((R.rng_tensor(rng, (100, 256), "bf16")[0].to(dev()), None), (buf, buf.view(-1)[:256].view(4, 64))):
             with pytest.raises(fgq.FGQError) as e:
-                fgq.fgq_linear_w4(R.rng_tensor(rng, (P, 256), dtype)[0].to(dev()), w)
+                fgq.fgq_linear_w4(x, w, y=y)
             assert e.value.code == fgq.FGQ_ERR_CUDA
     finally:
         fgq.fgq_debug_set_scratch_limit(prev)

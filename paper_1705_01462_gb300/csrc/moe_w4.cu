@@ -11,7 +11,9 @@
 //   resident_kernel (w4_resident.cuh) 16 rows of gate and of up for a unit of up to 8 tokens: silu(gate) up in fp32; then of down;
 //   or, with more choices an expert, the kernels of gemm_w4_experts.cu for units of up to 32, 64 or 128;
 //   combine_kernel  each token's choices by their weights, in their order.
-// Bound by the bytes of the experts' weights, each read once (again from L2 for each further unit of an expert).
+// Bound by the bytes of the experts' weights, each read once (again from L2 for each further unit of an expert), and before them by the way
+// from logits to units: of 148 us for 64 tokens of 6 of 64 experts, 4096 -> 1536, routing takes 11 and the grouping 7 more, combining 4; of 22 us for one
+// token of 8 of 64 experts, 2048 -> 1024, routing takes 5 (3 with one expert to choose), each layer about 7, combining 2.
 #include <type_traits>
 
 #include "w4_launch.h"

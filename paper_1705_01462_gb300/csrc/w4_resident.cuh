@@ -1,11 +1,15 @@
 // The product of up to 8 or 16 columns of tokens with 4-bit weights, tokens held in shared memory.
 //
-// A block keeps its tokens' columns for all of K (up to 8 NT x K x 2 bytes) and takes a run of items of 16 MT rows.  The run's tiles
+// A block keeps its tokens' columns for all of K (up to 8 NT x K x 2 bytes) and takes a run of items of 16 rows.  The run's tiles
 // are one sequence, tile columns of an item after one another, and its warps share it in equal parts, wherever those cut an
 // item: each warp streams its part through a ring of AHEAD tiles of its own in shared memory, with no barrier until the end.  (Loads to
 // registers that far ahead did not stay in flight: their waits have no names of their own in a loop with branches.)  An item
 // that a warp has whole goes from registers to its outputs; the parts of a cut one meet in shared memory once the warps are through,
 // in their order.
+// Bound by the weights' bytes and, a little later, by instructions (a tile is 4 words of 8 codes a lane and row: an AND and a packed multiply-add
+// a pair, a matrix instruction 16 columns).  Logits of 8 tokens, 4096 -> 131072, groups of 128: 49 us, 84% of the copy rate, issue slots 74%
+// busy (67 with the ring of w4_rows.cuh).  64 tokens of 6 of 64 experts, 4096 -> 1536, groups of 64: hidden values 82 us (5.3 TB/s, 70%), down 48
+// (4.6 TB/s, 71%).  Up to 24 warps of 80 registers: that many loads in flight, at 28 to 118 bytes of spills in the gated form.
 #pragma once
 
 #include "w4_rows.cuh"

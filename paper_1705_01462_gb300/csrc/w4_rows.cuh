@@ -1,4 +1,7 @@
-// The product of few tokens with 4-bit weights, tokens in a ring.
+// The product of few tokens with 4-bit weights, tokens in a ring that a block's eight warps share: for small matrices, and where tokens are
+// too many or too long to be held (w4_resident.cuh).  A small matrix is bound by the way to its first products and a cluster's join: 8
+// tokens of bf16, 4096 -> 4096, 6.0 us, 1.3 of them bytes; 1024 -> 2048 4.2.  A large one by the shared-memory reads of 16 or 32 columns, which
+// each warp makes for 16 rows of weights: 16 tokens, 8192 -> 131072, 192 us for 84.5 of bytes.
 #pragma once
 
 #include "linear_internal.cuh"

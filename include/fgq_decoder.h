@@ -210,7 +210,7 @@ fgq_status fgq_rope(const void* x, void* y, fgq_float_type type, int B, int T, i
  *   s      out, elements of `rtype`, rows lds apart, or NULL (not written).  May be r, with its stride.
  *   y      out, elements of `type`, [P][K] contiguous.  May be x where that is contiguous.
  * Everything between is fp32 and y is formed from s before it is rounded.  Sums of squares are fp32: values up to 1e18.
- * A token that holds NaN or Inf gives NaN (in s: what fp32 gives); other tokens are as without it.
+ * A token that holds NaN gives NaN, one that holds Inf what fp32 gives; other tokens are as without it.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, K = 0, bad types or kind, eps not above 0 or not finite, a scale that is not
  * finite, tokens_per_gate < 1 with a gate, a stride below K, y without pre or pre without y, neither s nor y),
  * FGQ_ERR_ALIGN (not aligned to the elements), FGQ_ERR_UNSUPPORTED (P or K above 2^31 - 2^16), FGQ_ERR_CUDA.

@@ -1,5 +1,5 @@
 // The experts' layers of many tokens with 4-bit weights: tokens as rows in the order of their experts, the products of gemm_w4.cuh for
-// a unit of up to 32, 64 or 128 of them and 128 rows of gate, up or down, and the hidden values between them.  Bound as those products are, by
+// a unit of up to 32, 64, 128 or 256 of them and 128 rows of gate, up or down, and the hidden values between them.  Bound as those products are, by
 // codes to operands, once for each unit of an expert: 128 tokens of 2 of 8 experts, 4096 -> 14336, 373 us for 110 of bytes.
 #include "gemm_w4.cuh"
 
@@ -67,7 +67,7 @@ fgq_status launch_unit_products(const G4Args& a, int bn, int grid, cudaStream_t 
   // two smaller blocks an SM where there are tiles for them: one works while the other begins or ends.  us so and with one: 32 experts 4096
   // -> 1024, 4 a token, 128 tokens 136 and 169; but 8 experts 2048 -> 1024, 2 a token 49 and 40
   if (bn == 64) return grid >= 2 * device_sms() ? launch_g4<64, PARTS, true, 8>(a, grid, s) : launch_g4<64, PARTS, true, 16>(a, grid, s);
-  return bn == 128 || PARTS == 1 ? launch_g4<128, PARTS, true, 16>(a, grid, s) : launch_g4<128 * PARTS, PARTS, true, 16>(a, grid, s);
+  return bn == 128 ? launch_g4<128, PARTS, true, 16>(a, grid, s) : launch_g4<256, PARTS, true, 16>(a, grid, s);
 }
 fgq_status launch_products(const ExpertsMany& e, const Matrix& w, const Matrix* up, const __half* x16, int64_t pitch, const float* scale,
                            int parts, int M, float* y, float* y_up, cudaStream_t s) {

@@ -9,7 +9,7 @@
 //   group_kernel    (more than four tokens, or choices that are given) one block: choices sorted by expert, and cut into units of
 //                   tokens that share an expert;
 //   resident_kernel (w4_resident.cuh) 16 rows of gate and of up for a unit of up to 8 tokens: silu(gate) up in fp32; then of down;
-//   or, with more choices an expert, the kernels of gemm_w4_experts.cu for units of up to 32, 64 or 128;
+//   or, with more choices an expert, the kernels of gemm_w4_experts.cu for units of 32 to 256;
 //   combine_kernel  each token's choices by their weights, in their order.
 // Bound by the bytes of the experts' weights, each read once (again from L2 for each further unit of an expert), and before them by the way
 // from logits to units: of 148 us for 64 tokens of 6 of 64 experts, 4096 -> 1536, routing takes 11 and the grouping 7 more, combining 4; of 22 us for one
@@ -451,8 +451,9 @@ HeldPlan plan_units(int type, int pass, int ctk, int per, int ctf, int down_per)
 // 127 and 150, 128 tokens 260 and 151.
 constexpr int HELD_UNITS = 2;
 // From more choices an expert on units have 64 tokens of fp32 in place of 32 (us at 64 tokens, 8 experts 4096 -> 14336: 555 and 416; 128 tokens
-// 557 and 569), and 128 in place of 64 (bf16, 128 tokens 479 and 373, 256 tokens 499 and 566, 512 tokens 747 and 813).
-constexpr int UNIT_32_MAX_F32 = 16, UNIT_64_MAX = 32;
+// 557 and 569), 128 in place of 64 (bf16, 128 tokens 479 and 373, 256 tokens 499 and 566, 512 tokens 747 and 813), and of bf16, whose hidden
+// values take one row each, 256 (1024 tokens 1174 and 1121, 2048 tokens 2232 and 1989, but 32 experts 4096 -> 1024, 4 a token 385 and 403).
+constexpr int UNIT_32_MAX_F32 = 16, UNIT_64_MAX = 32, UNIT_128_MAX_BF16 = 128;
 
 // route == nullptr: ids and weights are given.
 fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route* route, const int32_t* ids, const float* weights,
@@ -464,7 +465,8 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   const HeldPlan plan = plan_units(type, pass, col_tiles(K), TILE_COLS / gate->group, col_tiles(F), TILE_COLS / down->group);
   const bool held = A <= (int64_t)HELD_UNITS * plan.most * E;
   const bool small = type == FGQ_F32 && A <= (int64_t)UNIT_32_MAX_F32 * E;
-  const int cap = held ? plan.cap : (small ? 32 : (A <= (int64_t)UNIT_64_MAX * E ? 64 : 128));
+  const bool large = type == FGQ_BF16 && A > (int64_t)UNIT_128_MAX_BF16 * E;
+  const int cap = held ? plan.cap : (small ? 32 : (A <= (int64_t)UNIT_64_MAX * E ? 64 : (large ? 256 : 128)));
   const bool direct = !held || (type != FGQ_F32 && pieces16(x, type, P, K, ldx));
   const int most_units = (A < E || pass == 1 ? A : E) + A / cap;
   const size_t b_x = direct ? 0 : up256((size_t)pass * xpitch * 2);

@@ -69,6 +69,7 @@ def run_experts(rng, P, K, F, E, top, G, dtype, Gd=None, ids=None, fill=0, ld=0)
                                            # units cut short of 64 and 128 tokens, two passes, long rows, layers that hold few tokens or none
                                            (130, 520, 300, 3, 2, 64), (600, 130, 140, 6, 3, 128), (700, 64, 40, 5, 8, 32), (40, 4100, 36, 2, 1, 64),
                                            (24, 136, 72, 4, 2, 32), (50, 264, 130, 4, 2, 64), (200, 700, 1100, 16, 2, 64),
+                                           (300, 130, 136, 2, 1, 64),
                                            (9, 64, 15000, 3, 1, 64), (6, 20000, 17, 3, 1, 128), (2, 16, 120000, 2, 1, 64)])
 def test_experts(dtype, P, K, F, E, top, G):
     run_experts(np.random.default_rng(P + K), P, K, F, E, top, G, dtype)

@@ -90,6 +90,12 @@ int64_t fgq_debug_set_resident_blocks(int64_t blocks);
 int fgq_debug_set_attention_kernel(int which);
 
 /*
+ * Restricts this thread's fgq_linear_w4 calls to the kernels of few tokens (1) or of many (2); 0, the default: by sizes
+ * and type.  Returns the previous setting, or -1 for another value.
+ */
+int fgq_debug_set_linear_w4_kernel(int which);
+
+/*
  * Lets FGQ_PATH_DENSE run calls with fp32 alphas on this thread through the split-fp16
  * ablation (allow != 0), outside the fgq_gemm tolerance; 0 restores FGQ_ERR_UNSUPPORTED.
  * Returns the previous setting.

@@ -267,8 +267,8 @@ fgq_status fgq_read_weights_w4(const fgq_w4* w, float* out, cudaStream_t stream)
  *   x    elements of `type`, [P][K] with K = w->cols, rows ldx elements apart (ldx >= K); bias fp32 [M] or NULL.
  *   y    out, elements of `type`, [P][M] contiguous, M = w->rows; may overlap x.
  * Few tokens: codes and 16-bit tokens are exact operands of the products (fp32 tokens: three bf16 parts, exactly), a group's sum
- * takes its scale in fp32, y is rounded once.  More than 32 tokens (16 with more than 2^25 weights; fp32: 8 with more than 2^22) run on
- * fp16 operands on tcgen05: weights are exact there too within 2^26 of their row's largest scale, bf16 tokens within 2^26 of their largest
+ * takes its scale in fp32, y is rounded once.  More than 16 tokens (fp32: 8) whose product with the
+ * number of weights is above about 2^30 (2^27) run on fp16 operands on tcgen05: weights are exact there too within 2^26 of their row's largest scale, bf16 tokens within 2^26 of their largest
  * value (smaller ones are off by at most 2^-39 of it), fp32 tokens within 2^-22 of each value (or 2^-39 of the largest).  Scales
  * 2^-100 to 2^100 there, and outputs below 2^-100 may be 0.  A token that holds NaN or Inf gives values that are not finite; other
  * tokens are as without it.

@@ -27,6 +27,7 @@ thread_local int64_t t_scratch_limit = -1;
 thread_local int64_t t_resident_blocks = -1;
 thread_local int t_split_fold = 0;
 thread_local int t_attention_kernel = 0;
+thread_local int t_linear_w4_kernel = 0;
 thread_local int t_last_cuda_error = 0;  // cudaError_t of the last failed launch on this thread
 thread_local int t_cta_pairs = 0;        // remembered only: every contraction kernel runs on single CTAs
 thread_local int t_max_ksplit = 8;       // group ranges a G >= 64 tile may be split into
@@ -250,6 +251,7 @@ fgq_status after_launch(cudaError_t launch_result) {
 int64_t debug_wait_limit_us() { return t_wait_limit_us; }
 
 int debug_attention_kernel() { return t_attention_kernel; }
+int debug_linear_w4_kernel() { return t_linear_w4_kernel; }
 
 int debug_max_ksplit() { return t_max_ksplit; }
 
@@ -754,6 +756,13 @@ int fgq_debug_set_attention_kernel(int which) {
   if (which < 0 || which > 2) return -1;
   const int prev = t_attention_kernel;
   t_attention_kernel = which;
+  return prev;
+}
+
+int fgq_debug_set_linear_w4_kernel(int which) {
+  if (which < 0 || which > 2) return -1;
+  const int prev = t_linear_w4_kernel;
+  t_linear_w4_kernel = which;
   return prev;
 }
 

@@ -38,6 +38,7 @@ fgq_status after_launch(cudaError_t launch_result);  // the result of a cudaLaun
 // kernels' mbarrier waits (fgq_debug_set_wait_limit_us), or -1 for the kernels' own limits.
 int64_t debug_wait_limit_us();
 int debug_attention_kernel();  // 0, 1 or 2: fgq_debug_set_attention_kernel
+int debug_linear_w4_kernel();  // 0, 1 or 2: fgq_debug_set_linear_w4_kernel
 int debug_max_ksplit();    // 1 .. 8
 // Blocks that a test pretends a cooperative launch can keep resident, or -1.
 int64_t debug_resident_blocks();

@@ -293,14 +293,16 @@ __global__ void __launch_bounds__(256) bias_kernel(const float* bias, void* y, i
     store_typed(y, ytype, i, bias ? __ldg(bias + i % M) : 0.0f);
 }
 
-// Tokens up to which the kernels of few tokens run: 16, or 32 of up to 2^25 weights.  bf16, us there and in gemm_w4.cu: 16 tokens, 4096 -> 4096
-// 10.0 and 12.7, 4096 -> 14336 14.5 and 22.5; 32 tokens 9.4 and 13.2, 4096 -> 8192 16.8 and 18.4, but 28.6 and 22.8, 8192 -> 65536 179 and 144.
-// fp32: 8 tokens, or 32 of up to 2^22 weights: 8 tokens, 4096 -> 4096 8.7 and 13.1, 4096 -> 14336 24.0 and 26.9; 16 tokens 13.1 and 13.3, 40.7 and
-// 26.9; 24 tokens 22.1 and 13.4, 2048 -> 4096 13.5 and 10.8, but 2048 -> 2048 8.5 and 10.4.
-int few_tokens(int type, int K, int M) {
-  const int64_t weights = (int64_t)K * M;
-  if (type == FGQ_F32) return weights > 1 << 22 ? 8 : 32;
-  return weights > 1 << 25 ? 16 : 32;
+// Whether the kernels of few tokens run: up to 16 tokens (fp32: 8), or a product of tokens and weights up to which reading the weights again
+// for every 32 (8) tokens costs less than what the other way starts with.  bf16, us there and in gemm_w4.cu: 16 tokens, 4096 -> 14336 14.5 and 22.5;
+// 32 tokens, 4096 -> 8192 16.8 and 18.4, 4096 -> 14336 28.6 and 22.8; 64 tokens, 2048 -> 2048 6.9 and 11.1, 4096 -> 4096 14.2 and 14.7; 128 tokens
+// 24.0 and 17.7, 2048 -> 4096 14.7 and 15.2; 256 tokens 20.6 and 19.3, 1024 -> 2048 10.6 and 13.9.  fp32: 8 tokens, 4096 -> 14336 24.0 and 26.9; 16 tokens,
+// 4096 -> 4096 13.1 and 13.3; 64 tokens, 1024 -> 2048 9.0 and 11.1, 2048 -> 2048 14.0 and 11.8; 128 tokens, 512 -> 512 5.7 and 8.5.
+bool few_tokens(int type, int P, int K, int M) {
+  if (const int which = debug_linear_w4_kernel()) return which == 1;
+  const int few = type == FGQ_F32 ? 8 : 16, tile = type == FGQ_F32 ? 8 : 32;
+  const int64_t most = type == FGQ_F32 ? 1ll << 27 : 1ll << 30, tokens = ((int64_t)P + tile - 1) / tile * tile;
+  return P <= few || (tokens <= most && (int64_t)K * M <= most / tokens);
 }
 
 }  // namespace
@@ -369,7 +371,7 @@ fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx,
     bias_kernel<<<(unsigned)(blocks < most ? blocks : most), 256, 0, stream>>>(bias, y, type, P, M);
     return after_launch();
   }
-  if (P > few_tokens(type, K, M)) return run_many(x, type, P, K, P > 1 ? ldx : 0, w, bias, y, stream);
+  if (!few_tokens(type, P, K, M)) return run_many(x, type, P, K, P > 1 ? ldx : 0, w, bias, y, stream);
   RowsArgs a = {};
   a.w = matrix(w), a.x = token_rows(x, type, P, K, P > 1 ? ldx : 0), a.bias = bias, a.y = y, a.P = P, a.M = M, a.ytype = type;
   // tokens that outputs would overwrite are copied first, and those of a large matrix that are not in pieces of 16 bytes (us, 8 tokens of bf16,

@@ -88,6 +88,7 @@ SIGNATURES = [
     ("fgq_debug_set_scratch_limit", _i64, [_i64]),
     ("fgq_debug_set_resident_blocks", _i64, [_i64]),
     ("fgq_debug_set_attention_kernel", _i, [_i]),
+    ("fgq_debug_set_linear_w4_kernel", _i, [_i]),
     ("fgq_debug_allow_split_fold", _i, [_i]),
     ("fgq_debug_selftest_warp_wait", _i, [_u32, _vp]),
     ("fgq_debug_last_cuda_error", _i, [_vp, _sz]),
@@ -1022,6 +1023,11 @@ def fgq_debug_set_resident_blocks(blocks: int) -> int:
 def fgq_debug_set_attention_kernel(which: int) -> int:
     """Kernel of this thread's fgq_kv_attention calls: 1 few rows, 2 many rows, 0 the faster; the previous one."""
     return int(lib().fgq_debug_set_attention_kernel(int(which)))
+
+
+def fgq_debug_set_linear_w4_kernel(which: int) -> int:
+    """Kernels of this thread's fgq_linear_w4 calls: 1 those of few tokens, 2 of many, 0 by sizes and type; the previous ones."""
+    return int(lib().fgq_debug_set_linear_w4_kernel(int(which)))
 
 
 def fgq_debug_allow_split_fold(allow: bool) -> int:

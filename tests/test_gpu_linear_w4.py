@@ -9,12 +9,25 @@ from paper_1705_01462_gb300 import fgq
 
 pytestmark = pytest.mark.gpu
 
-# tokens from which the product for many tokens may run: its bound is the wider one
-MANY = 33
+WHICH = [0]  # kernels that calls are restricted to
+
+
+@pytest.fixture
+def kernels(request):
+    """1: the kernels of few tokens, 2: of many, 0: by sizes and type."""
+    prev = fgq.fgq_debug_set_linear_w4_kernel(request.param)
+    WHICH[0] = request.param
+    yield request.param
+    WHICH[0] = 0
+    assert fgq.fgq_debug_set_linear_w4_kernel(prev) == request.param
 
 
 def many(dtype, P, K, M):
-    return P >= MANY or (P >= 9 and K * M > 1 << 22 if dtype == "f32" else P >= 17 and K * M > 1 << 25)
+    """Whether the product for many tokens runs: its bound is the wider one."""
+    if WHICH[0]:
+        return WHICH[0] == 2
+    few, tile, most = (8, 8, 1 << 27) if dtype == "f32" else (16, 32, 1 << 30)
+    return P > few and -(-P // tile) * tile * K * M > most
 
 
 @pytest.mark.parametrize("G", [32, 64, 128])
@@ -59,18 +72,20 @@ def run(rng, P, K, M, G, dtype, bias=True, ld=0, fill=0, spread=0.3, scale=1.0):
     return y
 
 
+@pytest.mark.parametrize("kernels", [0, 2], indirect=True)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("G", [32, 64, 128])
 @pytest.mark.parametrize("P,K,M", [(1, 1, 1), (1, 128, 16), (1, 4096, 64), (2, 1000, 33), (3, 136, 40), (8, 1111, 999), (9, 512, 128),
                                    (17, 257, 50), (31, 2048, 48), (33, 640, 100), (64, 384, 31), (65, 384, 300), (130, 1000, 257)])
-def test_products(dtype, G, P, K, M):
+def test_products(kernels, dtype, G, P, K, M):
     run(np.random.default_rng(P * K + M), P, K, M, G, dtype, bias=M % 2 == 0)
 
 
+@pytest.mark.parametrize("kernels", [1, 2], indirect=True)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("G,P,K,M", [(64, 9, 4096, 1100), (32, 16, 8192, 520), (128, 40, 8200, 130), (64, 70, 2048, 2100),
                                      (32, 130, 1000, 4300), (128, 300, 1111, 3800), (64, 260, 5120, 8200), (64, 1025, 520, 8000), (64, 18, 8192, 4100)])
-def test_many(dtype, G, P, K, M):
+def test_many(kernels, dtype, G, P, K, M):
     """Tiles of 64, 128 and 256 tokens, K in one piece and in parts, the last of them short."""
     run(np.random.default_rng(P + K), P, K, M, G, dtype, bias=M % 200 == 0)
 
@@ -90,9 +105,10 @@ def test_long_rows(dtype, P, K):
         run(np.random.default_rng(K), P, K, M, G, dtype)
 
 
+@pytest.mark.parametrize("kernels", [2], indirect=True)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("P,K,M", [(40, 4096, 260), (200, 2048, 2100), (1000, 1024, 8200)])
-def test_waits_that_run_out(dtype, P, K, M):
+def test_waits_that_run_out(kernels, dtype, P, K, M):
     """A limit of a few microseconds for each wait: an error status, and the next calls are right."""
     rng = np.random.default_rng(P)
     x = R.rng_tensor(rng, (P, K), dtype)[0].to(dev())
@@ -116,9 +132,10 @@ def test_waits_that_run_out(dtype, P, K, M):
     assert fgq.FGQ_ERR_TIMEOUT in seen
 
 
+@pytest.mark.parametrize("kernels", [0, 2], indirect=True)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("P", [1, 5, 20, 70])
-def test_strides_and_padding(dtype, P):
+def test_strides_and_padding(kernels, dtype, P):
     """Rows apart, off 16-byte boundaries; whatever codes stand past the matrix."""
     rng = np.random.default_rng(P)
     for ld in (8, 1, 5):
@@ -130,8 +147,9 @@ def test_strides_and_padding(dtype, P):
         run(rng, P, K, 40, G, dtype, fill=6)
 
 
+@pytest.mark.parametrize("kernels", [0, 2], indirect=True)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
-def test_accuracy(dtype):
+def test_accuracy(kernels, dtype):
     """How far from 64 bits over many values: fp32 within 1e-6 of the output's norm, 16-bit types at their output's rounding.
     (Each rounding is uniform within half a step of a value of random mantissa: 0.41 of the largest, root mean square.)"""
     rng = np.random.default_rng(7)
@@ -144,9 +162,10 @@ def test_accuracy(dtype):
         assert rel <= {"f32": 1e-6, "bf16": 0.5 * 2.0 ** -8, "f16": 0.5 * 2.0 ** -11}[dtype], rel
 
 
+@pytest.mark.parametrize("kernels", [0, 2], indirect=True)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("P", [3, 90])
-def test_magnitudes(dtype, P):
+def test_magnitudes(kernels, dtype, P):
     """Scales that differ by 2^20 within a row, tokens far from 1."""
     rng = np.random.default_rng(11)
     run(rng, P, 512, 40, 32, dtype, spread=4.0, bias=False)
@@ -154,9 +173,10 @@ def test_magnitudes(dtype, P):
         run(rng, P, 512, 40, 32, dtype, scale=scale, bias=False)
 
 
+@pytest.mark.parametrize("kernels", [0, 2], indirect=True)
 @pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("P", [6, 80])
-def test_nonfinite_tokens(dtype, P):
+def test_nonfinite_tokens(kernels, dtype, P):
     rng = np.random.default_rng(5)
     x = R.rng_tensor(rng, (P, 300), dtype)[0].to(dev())
     c, s = R.random_w4(rng, (70, 300), 64)
@@ -170,7 +190,8 @@ def test_nonfinite_tokens(dtype, P):
     assert fgq.fgq_stream_status() == fgq.FGQ_OK
 
 
-def test_in_place_empty_streams_graphs():
+@pytest.mark.parametrize("kernels", [0, 2], indirect=True)
+def test_in_place_empty_streams_graphs(kernels):
     rng = np.random.default_rng(6)
     c, s = R.random_w4(rng, (256, 256), 64)
     w = R.weights(c, s, 64, dev())
@@ -211,12 +232,21 @@ def test_no_scratch():
         for dtype in ("bf16", "f32"):
             fgq.fgq_linear_w4(R.rng_tensor(rng, (4, 256), dtype)[0].to(dev()), w)
         buf = torch.zeros((4, 256), device=dev())
-        for x, y in ((R.rng_tensor(rng, (100, 256), "bf16")[0].to(dev()), None), (buf, buf.view(-1)[:256].view(4, 64))):
+        many = R.rng_tensor(rng, (100, 256), "bf16")[0].to(dev())
+        for x, y, which in ((many, None, 2), (buf, buf.view(-1)[:256].view(4, 64), 0)):
+            fgq.fgq_debug_set_linear_w4_kernel(which)
             with pytest.raises(fgq.FGQError) as e:
                 fgq.fgq_linear_w4(x, w, y=y)
             assert e.value.code == fgq.FGQ_ERR_CUDA
     finally:
+        fgq.fgq_debug_set_linear_w4_kernel(0)
         fgq.fgq_debug_set_scratch_limit(prev)
+
+
+def test_kernel_setting():
+    for which in (-1, 3):
+        assert fgq.fgq_debug_set_linear_w4_kernel(which) == -1
+    assert fgq.fgq_debug_set_linear_w4_kernel(1) == 0 and fgq.fgq_debug_set_linear_w4_kernel(0) == 1
 
 
 def test_refusals():

@@ -221,9 +221,10 @@ constexpr int rows_smem() {
   return Ring<NT>::TOTAL > sums ? Ring<NT>::TOTAL : sums;
 }
 
-// Blocks of a launch: an item a cluster, split down to a tile column or two a block where that is one block an SM at most (us, 32 tokens of
-// bf16, 1024 -> 2048 5.6, four columns at least 6.4) and to two or more where it is two (32 of fp32, 1111 -> 999 6.9, one or two 8.5); or
-// as many as share the items evenly, two an SM.
+// Blocks of a launch: an item a cluster.  Rows of four tile columns and more are split, down to one or two a block where that is one block an SM
+// at most (bf16, 32 tokens, 1024 -> 2048 5.6 us, four columns at least 6.4; but 256 -> 256 6.2 and not split 4.6), and to two or more where it is
+// two (fp32, 32 tokens, 1111 -> 999 6.9, one or two 8.5; bf16, 64 tokens, 2048 -> 4096 9.5, eight or more 11.1).  Or as many as share the items
+// evenly, two an SM.
 struct RowsPlan {
   int splits;
   unsigned grid;
@@ -231,7 +232,7 @@ struct RowsPlan {
 inline RowsPlan plan_rows(int64_t items, int ct) {
   RowsPlan p = {1, 0};
   const int64_t sms = device_sms(), most = 2 * sms;
-  while (p.splits < 8 && ct >= 2 * p.splits) {
+  while (p.splits < 8 && ct >= 4 && ct >= 2 * p.splits) {
     const int64_t blocks = items * p.splits * 2;
     if (blocks > most || (blocks > sms && ct < 4 * p.splits)) break;
     p.splits *= 2;

@@ -90,6 +90,13 @@ def test_many(kernels, dtype, G, P, K, M):
     run(np.random.default_rng(P + K), P, K, M, G, dtype, bias=M % 200 == 0)
 
 
+@pytest.mark.parametrize("kernels", [0, 2], indirect=True)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_very_many_tokens(kernels, dtype):
+    """More rows than a launch has blocks in its second dimension, of a small matrix."""
+    run(np.random.default_rng(3), 70001, 72, 40, 64, dtype)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("P,K,M,ld", [(1025, 4096, 2056, 0), (1030, 2500, 3360, 3), (1100, 2048, 4112, 8)])
 def test_expanded(dtype, P, K, M, ld):

@@ -360,7 +360,8 @@ __global__ void __launch_bounds__(GR_THREADS) group_kernel(const int32_t* ids, c
 }
 
 // ------------------------------------------------------------------ the choices' outputs together
-// y[p] = sum_j weights[p][j] z[places[p][j]], V values a thread.
+// y[p] = sum_j weights[p][j] z[places[p][j]], V values a thread.  (Done by whichever unit of a row tile is the last in the kernel before,
+// which saves a launch, one token took 25.1 us on the device in place of 21.5, four 50 in place of 32: a fence for each row tile.)
 template <int V>
 __global__ void __launch_bounds__(256) combine_kernel(const float* z, const int32_t* places, const float* weights, int top, int K, void* y,
                                                       int ytype) {

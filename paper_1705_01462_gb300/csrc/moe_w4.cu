@@ -96,6 +96,8 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
   __shared__ float chosen_w[TOKENS * MAX_TOP];
   __shared__ int ahead[TOKENS * MAX_TOP];
   pdl_trigger();
+  // another block's shared memory may be written once that block runs: they meet before the first keys, after the first products
+  asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = (int)blockIdx.x % RT_CLUSTER, p0 = (int)blockIdx.x / RT_CLUSTER * TOKENS;
   const int np = min(TOKENS, a.P - p0), kpart = warp % ks, per_pass = RT_CLUSTER * RT_WARPS / ks;
@@ -170,6 +172,7 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
         if (lane == 0) part[warp][i] = make_float2(hi[i], lo[i]);
       }
     __syncthreads();
+    if (e0 == 0) asm volatile("barrier.cluster.wait;" ::: "memory");
     const int el = (int)threadIdx.x / TOKENS, i = (int)threadIdx.x % TOKENS;  // an expert of this block, a token
     const int ee = e0 + rank * (RT_WARPS / ks) + el;
     if (el < RT_WARPS / ks && i < np && ee < a.E) {

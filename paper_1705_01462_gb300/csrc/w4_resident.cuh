@@ -101,7 +101,11 @@ __global__ void __launch_bounds__(32 * resident_warps(MT, NT)) resident_kernel(c
     i0 = (int)blockIdx.x * run;
     i1 = min(i0 + run, items);
   }
-  if (i0 >= i1) return;
+  if (i0 >= i1) {
+    // a block without items may be any, or all where no choice is an expert: what comes after this kernel comes after the one before
+    if (MODE == MODE_DOWN || (MODE == MODE_LINEAR && a.early)) pdl_wait();
+    return;
+  }
 
   // a segment: the run's items of one unit
   struct Segment {

@@ -305,10 +305,10 @@ fgq_status fgq_route_tokens(const void* x, fgq_float_type type, int P, int K, in
  *   ids        int32 [P][top], entries outside [0, E) are left out (a token without any gives zeros); an expert may be there
  *              twice.  weights  fp32 [P][top].
  *   y          out, elements of `type`, [P][K] contiguous; may be x where that is contiguous.
- * Between the layers values are held to 2^-12 (bf16 tokens, whose outputs round to 2^-9), 2^-17 (fp16) or exactly (fp32).  Sums are
+ * Between the layers values are held to 2^-22, or 2^-39 of a choice's largest (16-bit tokens), or exactly (fp32).  Sums are
  * fp32, in an order that depends on the sizes and on the tokens that share an expert.  Up to 4096 choices are taken at a time; with more
  * than 16 of them for an expert on average (8 of fp32; fewer where rows of more than 4096 leave room for fewer tokens) products run on
- * fp16 operands as those of a linear layer of many tokens, with what is said there, and fp32 values between the layers are held to 2^-22.
+ * fp16 operands as those of a linear layer of many tokens, with what is said there, and values between the layers are held as those of 16-bit tokens.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type or weights, sizes that do not fit, top outside 1 .. 32, ldx < K),
  * FGQ_ERR_ALIGN, FGQ_ERR_UNSUPPORTED (E above 1024, K or F above 2^31 - 2^16, more than 2^31 - 1 tiles), FGQ_ERR_CUDA (also
  * where a temporary cannot be had).

@@ -56,12 +56,13 @@ struct G4Args {
   unsigned int* err;
   uint64_t timeout_ns;
   int P, M, mtiles, ptiles, splits, ytype;
-  // GROUPED: tokens sorted by expert, a block one unit of them, and of w or of `up`; fp32 outputs without bias to y or y_up
+  // GROUPED: tokens sorted by expert, a block one unit of them, or BN rows of it, and of w or of `up`; fp32 outputs without bias to y or y_up
   Matrix up;
   void* y_up;
   const Unit* units;
   const int* nunits;
   int matrices;  // 2: w and up
+  int tiles;     // of BN rows, of a unit
 };
 
 // The first `live` of N values, one a row of M elements.
@@ -105,14 +106,20 @@ __global__ void __launch_bounds__(G4Cfg<BN, W>::THREADS, G4Cfg<BN, W>::BLOCKS) g
   if constexpr (GROUPED) {
     if (id % a.matrices) w = a.up, y = a.y_up;
     id /= a.matrices;
+    const int tile = id % a.tiles;
+    id /= a.tiles;
     if (id >= __ldcg(a.nunits)) {  // units are those of a kernel before the one that this one waits for
       pdl_wait();  // what comes after this kernel comes after that one
       return;
     }
     const int4 u = __ldcg(reinterpret_cast<const int4*>(a.units) + id);
     first_tile = (int64_t)u.x * w.rt * w.ct;
-    p0 = u.y * PARTS;
+    p0 = u.y * PARTS + tile * BN;
     end = u.y + u.z;
+    if (p0 >= end * PARTS) {
+      pdl_wait();
+      return;
+    }
   } else {
     sp = id % a.splits, p0 = (id / a.splits) * BN;
   }

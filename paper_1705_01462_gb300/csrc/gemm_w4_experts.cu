@@ -8,9 +8,9 @@ namespace w4 {
 namespace {
 
 inline size_t up256(size_t v) { return (v + 255) & ~size_t(255); }
-// rows of fp16 that a token, or a hidden value, takes: fp32 two, fp16 tokens' hidden values two (their outputs have 11 bits)
+// rows of fp16 that a token takes: fp32 two; a hidden value, which is fp32 whatever the tokens are, takes two
 int token_parts(int type) { return type == FGQ_F32 ? 2 : 1; }
-int hidden_parts(int type) { return type == FGQ_BF16 ? 1 : 2; }
+constexpr int HIDDEN_PARTS = 2;
 
 // Row `place` of x16: the token of that choice.
 template <typename T, bool VEC>
@@ -23,9 +23,8 @@ __global__ void __launch_bounds__(256) gather_kernel(const T* __restrict__ x, in
   token_row<T, VEC>(x + __ldcg(&choices[at].token) * ldx, K, dst + at * pitch * (std::is_same<T, float>::value ? 2 : 1), pitch, scale + at);
 }
 
-// h = silu(g) u as PARTS rows of fp16, after a power of two that takes a choice's largest to 2^14; a block a choice, twice over its
-// values.
-template <int PARTS>
+// h = silu(g) u as two rows of fp16 that add up to it (within 2^-22 of a value, 2^-39 of the largest), after a power of two that takes a
+// choice's largest to 2^14; a block a choice, twice over its values.
 __global__ void __launch_bounds__(256) hidden_kernel(const float* g, const float* u, int F, const int* nunits, __half* dst, int64_t pitch,
                                                      float* scale) {
   __shared__ float red[8];
@@ -34,7 +33,7 @@ __global__ void __launch_bounds__(256) hidden_kernel(const float* g, const float
   const int64_t at = blockIdx.x;
   if (at >= __ldcg(nunits + 1)) return;
   const float *gr = g + at * F, *ur = u + at * F;
-  __half* to = dst + at * pitch * PARTS;
+  __half* to = dst + at * pitch * HIDDEN_PARTS;
   auto value = [&](int k) {
     const float v = __ldcg(gr + k);
     return v / (1.0f + expf(-v)) * __ldcg(ur + k);
@@ -58,7 +57,7 @@ __global__ void __launch_bounds__(256) hidden_kernel(const float* g, const float
     const float v = k < F && !bad ? value(k) * up * up2 : 0.0f;
     const __half h = __float2half_rn(v);
     to[k] = h;
-    if (PARTS == 2) to[pitch + k] = __float2half_rn(v - __half2float(h));
+    to[pitch + k] = __float2half_rn(v - __half2float(h));
   }
 }
 
@@ -87,9 +86,10 @@ fgq_status launch_products(const ExpertsMany& e, const Matrix& w, const Matrix* 
   if (up) a.up = *up, a.y_up = y_up, a.matrices = 2;
   a.units = e.units;
   a.nunits = e.nunits;
-  const int64_t tiles = (int64_t)a.mtiles * a.matrices * e.most_units;
+  const int rows = e.cap * parts, bn = rows < 64 ? 64 : (rows > 256 ? 256 : rows);
+  a.tiles = rows / bn + (rows < bn);
+  const int64_t tiles = (int64_t)a.mtiles * a.matrices * a.tiles * e.most_units;
   if (tiles > INT32_MAX) return FGQ_ERR_UNSUPPORTED;
-  const int bn = e.cap * parts;
   if (!make_map_2d(&a.x_map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, x16, (uint64_t)pitch, (uint64_t)e.A * parts, (uint64_t)pitch * 2, 64, (uint32_t)bn,
                    CU_TENSOR_MAP_SWIZZLE_128B))
     return FGQ_ERR_CUDA;
@@ -110,7 +110,7 @@ struct Layout {
 };
 Layout layout(int type, int A, int K, int F) {
   const int64_t kp = copied_pitch(K), fp = copied_pitch(F);
-  return {kp, fp, up256((size_t)A * token_parts(type) * kp * 2), up256((size_t)A * F * 4), up256((size_t)A * hidden_parts(type) * fp * 2),
+  return {kp, fp, up256((size_t)A * token_parts(type) * kp * 2), up256((size_t)A * F * 4), up256((size_t)A * HIDDEN_PARTS * fp * 2),
           up256((size_t)A * 4)};
 }
 
@@ -140,9 +140,9 @@ fgq_status launch_experts_many(const ExpertsMany& a, const void* x, int type, in
                                                       : launch_gather<__half>(a, x, type, ldx, x16, l.kp, xs, s));
   if (st == FGQ_OK) st = launch_products(a, a.gate, &a.up, x16, l.kp, xs, token_parts(type), a.F, g, u, s);
   if (st == FGQ_OK)
-    st = after_launch(launch_pdl(hidden_parts(type) == 2 ? hidden_kernel<2> : hidden_kernel<1>, dim3(a.A), dim3(256), 0, s,
-                                 static_cast<const float*>(g), static_cast<const float*>(u), a.F, a.nunits, h16, l.fp, hs));
-  if (st == FGQ_OK) st = launch_products(a, a.down, nullptr, h16, l.fp, hs, hidden_parts(type), a.K, a.z, nullptr, s);
+    st = after_launch(launch_pdl(hidden_kernel, dim3(a.A), dim3(256), 0, s, static_cast<const float*>(g), static_cast<const float*>(u), a.F,
+                                 a.nunits, h16, l.fp, hs));
+  if (st == FGQ_OK) st = launch_products(a, a.down, nullptr, h16, l.fp, hs, HIDDEN_PARTS, a.K, a.z, nullptr, s);
   return st;
 }
 

@@ -436,11 +436,11 @@ struct HeldPlan {
 };
 HeldPlan plan_units(int type, int pass, int ctk, int per, int ctf, int down_per) {
   HeldPlan p = {};
-  const int parts = type == FGQ_F32 ? 3 : (type == FGQ_F16 ? 2 : 1);  // columns of a hidden value
+  const int parts = type == FGQ_F32 ? 3 : 2;  // of a hidden value
   for (int cap = type == FGQ_F32 ? 4 : 8; cap > 0; cap /= 2) {
     const int c = pass < cap ? pass : cap;
     p.hidden = type == FGQ_F32 ? plan_resident<2, 2, GATED_AHEAD>(ctk, per, c * columns_per_token(3)) : plan_resident<2, 1, GATED_AHEAD>(ctk, per, c);
-    p.down = plan_held(parts == 1 ? 1 : 2, ctf, down_per, c * columns_per_token(parts));
+    p.down = plan_held(2, ctf, down_per, c * columns_per_token(parts));
     p.most = cap;
     p.cap = c;
     if (p.hidden.warps > 0 && p.down.warps > 0) return p;
@@ -450,14 +450,15 @@ HeldPlan plan_units(int type, int pass, int ctk, int per, int ctf, int down_per)
 }
 
 // Units of an expert on average up to which tokens are held.  bf16, us so and on the products of many tokens: 8 experts 2048 -> 1024, 2 a
-// token, 64 tokens 40 and 41, 128 tokens 49 and 44; 128 experts 2048 -> 768, 8 a token, 128 tokens 130 and 231, 256 tokens 216 and 254;
-// units of 4 (8 experts 4096 -> 14336) 32 tokens 301 and 371, 64 tokens 536 and 371; fp32, 32 experts 4096 -> 1024, 4 a token, 40 tokens
+// token, 64 tokens 33 and 39, 128 tokens 45 and 42; 128 experts 2048 -> 768, 8 a token, 256 tokens 238 and 271, 512 tokens 425 and 402;
+// units of 2 (8 experts 4096 -> 14336) 16 tokens 327 and 413, 24 tokens 512 and 415; fp32, 32 experts 4096 -> 1024, 4 a token, 40 tokens
 // 127 and 150, 128 tokens 260 and 151.
 constexpr int HELD_UNITS = 2;
-// From more choices an expert on units have 64 tokens of fp32 in place of 32 (us at 64 tokens, 8 experts 4096 -> 14336: 555 and 416; 128 tokens
-// 557 and 569), 128 in place of 64 (bf16, 128 tokens 479 and 373, 256 tokens 499 and 566, 512 tokens 747 and 813), and of bf16, whose hidden
-// values take one row each, 256 (1024 tokens 1174 and 1121, 2048 tokens 2232 and 1989, but 32 experts 4096 -> 1024, 4 a token 385 and 403).
-constexpr int UNIT_32_MAX_F32 = 16, UNIT_64_MAX = 32, UNIT_128_MAX_BF16 = 128;
+// Up to so many choices an expert on average units have 32 tokens in place of 64 (us, 8 experts 4096 -> 14336, 2 a token: bf16, 64 tokens 404 and 436,
+// 128 tokens 555 and 439; fp32, 64 tokens 416 and 555, 128 tokens 569 and 557), 64 in place of 128 (bf16, 128 tokens 439 and 561; 8 experts
+// 2048 -> 1024, 256 tokens 71 and 54), and 128 in place of 256, of fp32 always, where two rows a token fill a product's columns (bf16, 32 experts
+// 4096 -> 1024, 4 a token, 1024 tokens 399 and 433; 8 experts 4096 -> 14336, 1024 tokens 1506 and 1402).
+constexpr int UNIT_32_MAX = 16, UNIT_64_MAX = 32, UNIT_128_MAX = 128;
 
 // route == nullptr: ids and weights are given.
 fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route* route, const int32_t* ids, const float* weights,
@@ -468,8 +469,7 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
   const int64_t hpitch = (int64_t)row_tiles(F) * TILE_ROWS, xpitch = parts * copied_pitch(K);
   const HeldPlan plan = plan_units(type, pass, col_tiles(K), TILE_COLS / gate->group, col_tiles(F), TILE_COLS / down->group);
   const bool held = A <= (int64_t)HELD_UNITS * plan.most * E;
-  const bool small = type == FGQ_F32 && A <= (int64_t)UNIT_32_MAX_F32 * E;
-  const bool large = type == FGQ_BF16 && A > (int64_t)UNIT_128_MAX_BF16 * E;
+  const bool small = A <= (int64_t)UNIT_32_MAX * E, large = type != FGQ_F32 && A > (int64_t)UNIT_128_MAX * E;
   const int cap = held ? plan.cap : (small ? 32 : (A <= (int64_t)UNIT_64_MAX * E ? 64 : (large ? 256 : 128)));
   const bool direct = !held || (type != FGQ_F32 && pieces16(x, type, P, K, ldx));
   const int most_units = (A < E || pass == 1 ? A : E) + A / cap;
@@ -543,8 +543,7 @@ fgq_status run_experts(const void* x, int type, int P, int64_t ldx, const Route*
                            : (type == FGQ_BF16 ? launch_held_gated_bf16(ra, plan.hidden, hi, s) : launch_held_gated_f16(ra, plan.hidden, hi, s));
       if (st != FGQ_OK) break;
       ra.w = md, ra.M = K, ra.z = z, ra.items = ra.items ? (int)di : 0;
-      st = type == FGQ_F32 ? launch_held_down_f32(ra, plan.down, di, s)
-                           : (type == FGQ_BF16 ? launch_held_down_bf16(ra, plan.down, di, s) : launch_held_down_f16(ra, plan.down, di, s));
+      st = type == FGQ_F32 ? launch_held_down_f32(ra, plan.down, di, s) : launch_held_down_16(ra, plan.down, di, s);
     } else {
       st = launch_experts_many({mg, mu, md, units, choices, nunits, K, F, na, cap, nu, h, z}, xp, type, ldx, s);
     }

@@ -14,12 +14,11 @@ fgq_status launch_rows_f32(const RowsArgs& a, int nt, unsigned grid, bool chaine
 fgq_status launch_held_bf16(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s);
 fgq_status launch_held_f16(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s);
 fgq_status launch_held_f32(const ResidentArgs& a, int nt, const ResidentPlan& plan, bool chained, cudaStream_t s);
-// Gate and up, and down, `items` at most: 8 tokens a unit (fp32: 4).
+// Gate and up, and down (of 16-bit tokens, of fp32), `items` at most: 8 tokens a unit (fp32: 4).
 fgq_status launch_held_gated_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
 fgq_status launch_held_gated_f16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
 fgq_status launch_held_gated_f32(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
-fgq_status launch_held_down_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
-fgq_status launch_held_down_f16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
+fgq_status launch_held_down_16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
 fgq_status launch_held_down_f32(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s);
 
 template <typename T, int MT, int NT, int PARTS, int MODE, int AHEAD>

@@ -112,7 +112,7 @@ ManyPlan plan_many(int P, int parts, int ct, int M);
 fgq_status launch_many(const ManyPlan& plan, const Matrix& w, const int* wexp, const void* x16, int64_t pitch, int K, const float* scale,
                        int P, int M, float* part, const float* bias, void* y, int ytype, cudaStream_t s);
 
-// The experts' layers of many tokens: choices sorted by expert, in units of up to `cap` (a power of two, rows of fp16 times cap from 64 to 256).
+// The experts' layers of many tokens: choices sorted by expert, in units of up to `cap` (32, 64, 128 or 256).
 struct ExpertsMany {
   Matrix gate, up, down;
   const Unit* units;

@@ -13,9 +13,6 @@ fgq_status launch_held_bf16(const ResidentArgs& a, int nt, const ResidentPlan& p
 fgq_status launch_held_gated_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
   return launch_held_per<__nv_bfloat16, 2, 1, 1, MODE_GATED, GATED_AHEAD>(a, plan, items, true, s);
 }
-fgq_status launch_held_down_bf16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
-  return launch_held_per<__half, 1, 1, 1, MODE_DOWN, HELD_AHEAD>(a, plan, items, true, s);
-}
 
 }  // namespace w4
 }  // namespace fgq

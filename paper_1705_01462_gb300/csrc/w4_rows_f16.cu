@@ -1,4 +1,4 @@
-// Few fp16 tokens with 4-bit weights.
+// Few fp16 tokens with 4-bit weights, and hidden values of both 16-bit types.
 #include "w4_launch.h"
 
 namespace fgq {
@@ -13,7 +13,7 @@ fgq_status launch_held_f16(const ResidentArgs& a, int nt, const ResidentPlan& pl
 fgq_status launch_held_gated_f16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
   return launch_held_per<__half, 2, 1, 1, MODE_GATED, GATED_AHEAD>(a, plan, items, true, s);
 }
-fgq_status launch_held_down_f16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
+fgq_status launch_held_down_16(const ResidentArgs& a, const ResidentPlan& plan, int64_t items, cudaStream_t s) {
   return launch_held_per<__half, 1, 2, 2, MODE_DOWN, HELD_AHEAD>(a, plan, items, true, s);
 }
 

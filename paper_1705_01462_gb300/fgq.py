@@ -850,7 +850,7 @@ def fgq_add_norm(x: torch.Tensor, residual: Optional[torch.Tensor] = None, norm:
     pg, ldg = None, 0
     if gate is not None:
         gty, rows, cols, ldg = _matrix(gate if gate.dim() == 2 else gate.view(1, -1), "gate")
-        if tokens_per_gate <= 0:
+        if tokens_per_gate <= 0 or tokens_per_gate > P:  # one row for all; what the library takes has 32 bits
             tokens_per_gate = max(P, 1)
         if gty != ty or cols != K or rows * tokens_per_gate < P:
             raise ValueError(f"gate must be {x.dtype} [rows][{K}], a row for each {tokens_per_gate} of {P} tokens")

@@ -274,7 +274,7 @@ fgq_status fgq_read_weights_w4(const fgq_w4* w, float* out, cudaStream_t stream)
  * tokens are as without it.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type, bad weights, more than one matrix, ldx < K), FGQ_ERR_ALIGN (x or y
  * not aligned to their elements, codes or scales not 16-byte, bias not 4-byte aligned), FGQ_ERR_UNSUPPORTED (P, K or M above
- * 2^31 - 2^16, more than 2^31 - 1 tiles), FGQ_ERR_CUDA (also where a temporary cannot be had).
+ * 2^31 - 2^16, more than 2^30 - 2^15 fp32 tokens, more than 2^31 - 1 tiles), FGQ_ERR_CUDA (also where a temporary cannot be had).
  */
 fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx, const fgq_w4* w, const float* bias, void* y,
                          cudaStream_t stream);

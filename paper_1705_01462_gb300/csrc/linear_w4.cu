@@ -362,7 +362,7 @@ fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx,
   const int K = w->cols, M = w->rows;
   if (P > 1 && ldx < K) return FGQ_ERR_ARG;
   if (P == 0 || M == 0) return FGQ_OK;
-  if (P > MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
+  if (P > (type == FGQ_F32 ? MAX_SIZE / 2 : MAX_SIZE)) return FGQ_ERR_UNSUPPORTED;  // many fp32 tokens are two rows each, counted in 32 bits
   if (!y || (K > 0 && !x)) return FGQ_ERR_ARG;
   const uintptr_t e = float_bytes(type);
   if (!aligned(x, e) || !aligned(y, e) || !aligned(bias, 4)) return FGQ_ERR_ALIGN;

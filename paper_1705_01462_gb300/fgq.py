@@ -9,6 +9,7 @@ loading fails loudly if the library is missing or CUDA is unavailable.
 from __future__ import annotations
 
 import ctypes
+import operator
 import os
 from typing import Optional, Tuple
 
@@ -781,27 +782,43 @@ class _NormStruct(ctypes.Structure):
     _fields_ = [("weight", _vp), ("bias", _vp), ("eps", _f), ("kind", _i)]
 
 
-class Norm:
-    """A norm of fgq_add_norm: kind "rms" or "layer", weight and bias fp32 [K] or None."""
+def _reads(name: str) -> property:
+    return property(operator.attrgetter("_" + name))
 
-    __slots__ = ("weight", "bias", "eps", "kind", "_size", "_c", "_ref")
+
+def _is(t: torch.Tensor, at: int, dtype, n: int) -> bool:
+    """Whether t is n contiguous values of the type at that address (0.2 us; setting a struct's field takes 0.1)."""
+    return t.data_ptr() == at and t.dtype is dtype and t.numel() == n and t.is_contiguous()
+
+
+class Norm:
+    """A norm of fgq_add_norm: kind "rms" or "layer", weight and bias fp32 [K] or None.  What it was made of can be read, and its
+    tensors' values may change."""
+
+    __slots__ = ("_weight", "_bias", "_eps", "_kind", "_pw", "_pb", "_c", "_ref")
+    weight, bias, eps, kind = (_reads(n) for n in ("weight", "bias", "eps", "kind"))
 
     def __init__(self, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, kind: str = "rms",
                  eps: float = 1e-6):
-        self.weight, self.bias, self.eps, self.kind = weight, bias, eps, kind
-        self._size = None if weight is None else weight.numel()
-        if bias is not None:
-            if weight is not None and bias.numel() != self._size:
-                raise ValueError("Norm: weight and bias differ in size")
-            self._size = bias.numel()
-        self._c = _NormStruct(None if weight is None else _dev(weight, torch.float32, "weight"),
-                              None if bias is None else _dev(bias, torch.float32, "bias"), eps,
-                              _named(NORM_KINDS, kind, "kind"))
+        self._weight, self._bias, self._eps, self._kind = weight, bias, eps, kind
+        if weight is not None and bias is not None and weight.numel() != bias.numel():
+            raise ValueError("Norm: weight and bias differ in size")
+        self._pw = None if weight is None else _dev(weight, torch.float32, "weight")
+        self._pb = None if bias is None else _dev(bias, torch.float32, "bias")
+        self._c = _NormStruct(self._pw, self._pb, eps, _named(NORM_KINDS, kind, "kind"))
         self._ref = ctypes.addressof(self._c)
 
     def _of(self, K: int) -> int:
-        if self._size is not None and self._size != K:
-            raise ValueError(f"Norm: weight and bias must have {K} entries")
+        """The library's struct, of the tensors as they are now (their storage may be another than when it was made)."""
+        weight, bias = self._weight, self._bias
+        if weight is not None and not _is(weight, self._pw, torch.float32, K):
+            self._pw = self._c.weight = _dev(weight, torch.float32, "weight")
+            if weight.numel() != K:
+                raise ValueError(f"Norm: weight must have {K} entries")
+        if bias is not None and not _is(bias, self._pb, torch.float32, K):
+            self._pb = self._c.bias = _dev(bias, torch.float32, "bias")
+            if bias.numel() != K:
+                raise ValueError(f"Norm: bias must have {K} entries")
         return self._ref
 
 
@@ -879,21 +896,34 @@ class _W4Struct(ctypes.Structure):
 class W4Weights:
     """Weights [rows][cols], or [experts][rows][cols], in 4 bits with a bf16 scale for each group: codes uint8 [experts][row
     tiles][column tiles][1024], scales bf16 [experts][row tiles][column tiles][16][128 / group] (include/fgq_decoder.h);
-    without the experts' axis: one matrix."""
+    without the experts' axis: one matrix.  What they were made of can be read, and the tensors' values may change."""
 
-    __slots__ = ("codes", "scales", "experts", "rows", "cols", "group", "_c", "_ref")
+    __slots__ = ("_codes", "_scales", "_experts", "_rows", "_cols", "_group", "_pc", "_ps", "_sizes", "_c", "_at")
+    codes, scales, experts, rows, cols, group = (_reads(n) for n in ("codes", "scales", "experts", "rows", "cols", "group"))
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, rows: int, cols: int):
-        pc, ps = _dev(codes, torch.uint8, "codes"), _dev(scales, torch.bfloat16, "scales")
+        self._pc, self._ps = _dev(codes, torch.uint8, "codes"), _dev(scales, torch.bfloat16, "scales")
         c, s = tuple(codes.shape), tuple(scales.shape)
         tiles = ((rows + 15) // 16, (cols + 127) // 128, 1024)
         if c[-3:] != tiles or len(c) > 4 or s[:-2] != c[:-1] or s[-2] != 16 or s[-1] not in (1, 2, 4):
             raise ValueError(f"W4Weights: codes are [experts][{tiles[0]}][{tiles[1]}][1024], scales "
                              f"[experts][{tiles[0]}][{tiles[1]}][16][128 / group]; got {c} and {s}")
-        self.codes, self.scales, self.rows, self.cols = codes, scales, rows, cols
-        self.experts, self.group = c[0] if len(c) == 4 else 1, 128 // s[-1]
-        self._c = _W4Struct(pc, ps, self.experts, rows, cols, self.group)
-        self._ref = ctypes.addressof(self._c)
+        self._codes, self._scales, self._rows, self._cols = codes, scales, rows, cols
+        self._experts, self._group = c[0] if len(c) == 4 else 1, 128 // s[-1]
+        self._sizes = codes.numel(), scales.numel()
+        self._c = _W4Struct(self._pc, self._ps, self._experts, rows, cols, self._group)
+        self._at = ctypes.addressof(self._c)
+
+    @property
+    def _ref(self) -> int:
+        """The library's struct, of the tensors as they are now (their storage may be another than when it was made)."""
+        codes, scales, sizes = self._codes, self._scales, self._sizes
+        if not (_is(codes, self._pc, torch.uint8, sizes[0]) and _is(scales, self._ps, torch.bfloat16, sizes[1])):
+            self._pc = self._c.codes = _dev(codes, torch.uint8, "codes")
+            self._ps = self._c.scales = _dev(scales, torch.bfloat16, "scales")
+            if (codes.numel(), scales.numel()) != sizes:
+                raise ValueError("W4Weights: codes and scales are not of the sizes that they had")
+        return self._at
 
 
 def fgq_quantize_weights_w4(w: torch.Tensor, group: int = 64, stream=None) -> W4Weights:
@@ -936,9 +966,9 @@ def fgq_linear_w4(x: torch.Tensor, w: W4Weights, bias: Optional[torch.Tensor] = 
     """A linear layer on 4-bit weights: x [P][cols] times w [rows][cols]^T plus bias, of x's type."""
     _require_cuda()
     ty, P, K, ldx = _matrix(x, "x")
-    if K != w.cols or (bias is not None and bias.numel() != w.rows):
+    if K != w._cols or (bias is not None and bias.numel() != w._rows):
         raise ValueError(f"x must be [tokens][{w.cols}], bias [{w.rows}]")
-    y, py = _outputs(x, y, P, w.rows)
+    y, py = _outputs(x, y, P, w._rows)
     _check(lib().fgq_linear_w4(x.data_ptr(), ty, P, ldx, w._ref, None if bias is None else _dev(bias, torch.float32, "bias"),
                                py, _stream(stream)), "fgq_linear_w4")
     return y
@@ -973,7 +1003,7 @@ def fgq_experts_w4(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, ga
     """sum_j weights[p][j] down_e (silu(gate_e x[p]) * (up_e x[p])), e = ids[p][j] (left out where it is no expert)."""
     _require_cuda()
     ty, P, K, ldx = _matrix(x, "x")
-    if K != gate.cols or ids.dim() != 2 or ids.shape[0] != P or weights.shape != ids.shape:
+    if K != gate._cols or ids.dim() != 2 or ids.shape[0] != P or weights.shape != ids.shape:
         raise ValueError(f"x must be [tokens][{gate.cols}], ids and weights [{P}][top]")
     y, py = _outputs(x, y, P, K)
     _check(lib().fgq_experts_w4(x.data_ptr(), ty, P, ldx, _dev(ids, torch.int32, "ids"), _dev(weights, torch.float32, "weights"),
@@ -988,7 +1018,7 @@ def fgq_moe_w4(x: torch.Tensor, router: torch.Tensor, top: int, gate: W4Weights,
     _require_cuda()
     ty, P, K, ldx = _matrix(x, "x")
     rty, E, pr = _router(router, x, K)
-    if K != gate.cols or E != gate.experts:
+    if K != gate._cols or E != gate._experts:
         raise ValueError(f"x must be [tokens][{gate.cols}], router [{gate.experts}][{gate.cols}]")
     y, py = _outputs(x, y, P, K)
     _check(lib().fgq_moe_w4(x.data_ptr(), ty, P, ldx, pr, rty, top, _named(SCORES, score, "score"), int(renormalize), scale,

@@ -220,7 +220,16 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
       k = (unsigned long long)h << 32 | l;
       if ((id & 31) == lane) taken |= 1u << (id >> 5);
       if (j == 0) best_h = of_order((uint32_t)(k >> 32)), best_l = of_order((uint32_t)k);
-      const float f = a.score == FGQ_SCORE_SOFTMAX ? expf(value(k)) : 1.0f / (1.0f + expf(-of_order((uint32_t)(k >> 32))));
+      // sigmoid scores through exponentials of numbers below 0, which do not overflow; where all are to be divided by their sum, without the
+      // largest's exponential, a factor of each: scores far below fp32's smallest have a ratio all the same
+      const float logit = of_order((uint32_t)(k >> 32));
+      float f;
+      if (a.score == FGQ_SCORE_SOFTMAX)
+        f = expf(value(k));
+      else if (logit < 0.0f)
+        f = expf(a.renormalize && best_h < 0.0f ? value(k) : logit) / (1.0f + expf(logit));
+      else
+        f = 1.0f / (1.0f + expf(-logit));
       if (lane == j) {
         mine = f;
         mine_id = id;

@@ -287,7 +287,7 @@ fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx,
  * times scale.  Logits are within about an fp32 rounding of their exact values, and are compared before they are rounded to fp32.
  *   router   elements of `rtype`, which is `type` or FGQ_F32, [E][K] contiguous.
  *   ids      out, int32 [P][top];  weights  out, fp32 [P][top].
- * A token that holds NaN gives weights NaN.
+ * A token that holds NaN gives weights NaN; one that holds Inf what its infinite logits give (softmax: NaN).
  * Errors: FGQ_ERR_ARG (null pointer, negative size, K or E below 1, bad types or score, top outside 1 .. E, renormalize neither 0
  * nor 1, a scale that is not finite, ldx < K), FGQ_ERR_ALIGN, FGQ_ERR_UNSUPPORTED (E above 1024, top above 32, P above 2^29, K above
  * 2^31 - 2^16), FGQ_ERR_CUDA.

@@ -178,8 +178,8 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
     if (el < RT_WARPS / ks && i < np && ee < a.E) {
       float h = part[el * ks][i].x, l = part[el * ks][i].y;
       for (int s = 1; s < ks; ++s) add_pair(h, l, part[el * ks + s][i].x, part[el * ks + s][i].y);
-      const float r = h + l, rest = l - (r - h);
-      // infinite sums have no rest; NaN counts as the smallest
+      // infinite sums have no rest, and what their two-sums left is NaN; NaN counts as the smallest
+      const float r = nonfinite(h) ? h : h + l, rest = l - (r - h);
       unsigned long long key = 1ull;
       if (r == r) key = (unsigned long long)order_of(r) << 32 | (nonfinite(r) ? 0x80000000u : order_of(rest));
       uint32_t at;

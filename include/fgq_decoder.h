@@ -284,7 +284,8 @@ fgq_status fgq_linear_w4(const void* x, fgq_float_type type, int P, int64_t ldx,
  * ones, and NaN, which counts as the smallest: lowest index first), and their weights
  *   FGQ_SCORE_SOFTMAX   exp(l_e) / sum over all experts of exp(l), or over the chosen ones where renormalize is 1;
  *   FGQ_SCORE_SIGMOID   1 / (1 + exp(-l_e)), divided by the chosen ones' sum where renormalize is 1;
- * times scale.  Logits are within about an fp32 rounding of their exact values, and are compared before they are rounded to fp32.
+ * times scale.  A logit's terms are added in fp32 by runs of eight, and the runs as pairs of fp32, unrounded: it is within 2^-21 of the sum
+ * of its terms' magnitudes (terms of random signs: about an fp32 rounding of itself), and is compared so.
  *   router   elements of `rtype`, which is `type` or FGQ_F32, [E][K] contiguous.
  *   ids      out, int32 [P][top];  weights  out, fp32 [P][top].
  * A token that holds NaN gives weights NaN; one that holds Inf what its infinite logits give (softmax: NaN).

@@ -4,8 +4,9 @@
 //
 // Kernels of a layer, each brought up while the one before it runs:
 //   route_kernel    a cluster four tokens: products of 8 elements in fp32, their sums as pairs of fp32 (two-sum), so that a
-//                   logit is off by about one fp32 rounding and the choice is that of 64-bit sums but for near ties; the largest
-//                   one by one, and their weights;
+//                   logit is off by 8 roundings of its terms' magnitudes at most (with terms of random signs by about one of itself,
+//                   so that the choice is that of 64-bit sums but for near ties; pairs throughout took 64 tokens of 64 experts from
+//                   11.2 to 18.3 us); the largest one by one, and their weights;
 //   group_kernel    (more than four tokens, or choices that are given) one block: choices sorted by expert, and cut into units of
 //                   tokens that share an expert;
 //   resident_kernel (w4_resident.cuh) 16 rows of gate and of up for a unit of up to 8 tokens: silu(gate) up in fp32; then of down;

@@ -209,7 +209,7 @@ fgq_status fgq_rope(const void* x, void* y, fgq_float_type type, int B, int T, i
  *   r      elements of `rtype`, which is `type` or FGQ_F32, rows ldr apart.
  *   s      out, elements of `rtype`, rows lds apart, or NULL (not written).  May be r, with its stride.
  *   y      out, elements of `type`, [P][K] contiguous.  May be x where that is contiguous.
- * Everything between is fp32 and y is formed from s before it is rounded.  Sums of squares are fp32: values up to 1e18.
+ * Everything between is fp32 and y is formed from s before it is rounded.  Sums of squares are fp32, of values up to 1e18 in rows of any length.
  * A token that holds NaN gives NaN, one that holds Inf what fp32 gives; other tokens are as without it.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, K = 0, bad types or kind, eps not above 0 or not finite, a scale that is not
  * finite, tokens_per_gate < 1 with a gate, a stride below K, y without pre or pre without y, neither s nor y),

@@ -38,7 +38,8 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sum over the NT threads of a row, in all of them.  `red` is the block's; two sums in turn take its two halves, so that
+// Sum over the NT threads of a row, in all of them.  (What they bring is their share of a mean, so that squares of values up to 1e18 stay in
+// fp32's range in rows of any length.)  `red` is the block's; two sums in turn take its two halves, so that
 // one barrier a sum is enough.
 template <int NT>
 __device__ __forceinline__ float row_sum(float v, float (*red)[32], int& turn) {
@@ -121,7 +122,7 @@ __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum = add_f2(sum, v[c][i]);
     unpack_f2(sum, a, b);
-    const float mean = row_sum<NT>(a + b, red, turn) * inv_k;
+    const float mean = row_sum<NT>((a + b) * inv_k, red, turn);
     const f2 off = pack_f2(-mean, -mean);
 #pragma unroll
     for (int c = 0; c < CH; ++c)
@@ -138,7 +139,7 @@ __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) sq = fma_f2(v[c][i], v[c][i], sq);
   unpack_f2(sq, a, b);
-  const float inv = rsqrtf(row_sum<NT>(a + b, red, turn) * inv_k + n.eps);
+  const float inv = rsqrtf(row_sum<NT>((a + b) * inv_k, red, turn) + n.eps);
   const f2 inv2 = pack_f2(inv, inv);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -227,8 +228,8 @@ __global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constan
   const R* r = a.r ? static_cast<const R*>(a.r) + p * a.ldr : nullptr;
   const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)(p / a.tokens_per_gate) * a.ldg : nullptr;
   const float inv_k = 1.0f / (float)a.K;
-  // sums of f(k) over the row, in pieces that keep fp32's bits
-  auto sum_of = [&](auto f) {
+  // means of f(k) over the row, in pieces that keep fp32's bits
+  auto mean_of = [&](auto f) {
     float total = 0.0f;
     for (int k = threadIdx.x; k < a.K; k += LONG_THREADS * 64) {
       float part = 0.0f;
@@ -236,18 +237,18 @@ __global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constan
         const int64_t at = (int64_t)k + (int64_t)i * LONG_THREADS;
         if (at < a.K) part += f((int)at);
       }
-      total += part;
+      total += part * inv_k;
     }
     return row_sum<LONG_THREADS>(total, red, turn);
   };
   auto stats = [&](auto value, const fgq_norm& n, float& mean, float& inv) {
     mean = 0.0f;
-    if (n.kind == FGQ_NORM_LAYER) mean = sum_of(value) * inv_k;
+    if (n.kind == FGQ_NORM_LAYER) mean = mean_of(value);
     const float m = mean;
-    inv = rsqrtf(sum_of([&](int k) {
+    inv = rsqrtf(mean_of([&](int k) {
                    const float z = value(k) - m;
                    return z * z;
-                 }) * inv_k + n.eps);
+                 }) + n.eps);
   };
   auto apply = [&](float z, const fgq_norm& n, float mean, float inv, int k) {
     z = (z - mean) * inv;

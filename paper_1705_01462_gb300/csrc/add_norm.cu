@@ -58,14 +58,22 @@ __device__ __forceinline__ float row_sum(float v, float (*red)[32], int& turn) {
 
 using f2 = unsigned long long;  // two fp32 values, as the packed instructions take them
 
-// Eight consecutive elements as four pairs.
+// Eight consecutive elements as four pairs.  CONST: of memory that the kernel does not write (weights, gates; x and r may be outputs' places, and go
+// past L1, which is left to the weights, unless two pieces share its sectors: 8192 x 4096 fp32 85.7 us so and 90.5 past it, 8192 x 8192
+// bf16 93.3 and 88.8).
+template <bool CONST>
 __device__ __forceinline__ void load_pairs(const float* p, f2 (&v)[4]) {
-  const ulonglong2 a = __ldg(reinterpret_cast<const ulonglong2*>(p)), b = __ldg(reinterpret_cast<const ulonglong2*>(p) + 1);
+  ulonglong2 a, b;
+  if constexpr (CONST)
+    a = __ldg(reinterpret_cast<const ulonglong2*>(p)), b = __ldg(reinterpret_cast<const ulonglong2*>(p) + 1);
+  else
+    a = reinterpret_cast<const ulonglong2*>(p)[0], b = reinterpret_cast<const ulonglong2*>(p)[1];
   v[0] = a.x, v[1] = a.y, v[2] = b.x, v[3] = b.y;
 }
-template <typename T>
+template <bool CONST, typename T>
 __device__ __forceinline__ void load_pairs(const T* p, f2 (&v)[4]) {
-  const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
+  const uint4* q = reinterpret_cast<const uint4*>(p);
+  const uint4 u = CONST ? __ldg(q) : __ldcg(q);
   const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -75,12 +83,12 @@ __device__ __forceinline__ void load_pairs(const T* p, f2 (&v)[4]) {
 }
 
 // Piece c of a row, eight elements of thread tid (VEC: consecutive ones); zeros past the row.
-template <typename T, bool VEC>
+template <typename T, bool VEC, bool CONST>
 __device__ __forceinline__ void load_piece(const T* row, int c, int tid, int NT, int K, f2 (&v)[4]) {
   if constexpr (VEC) {
     const int k = 8 * (tid + c * NT);
     if (k < K) {
-      load_pairs(row + k, v);
+      load_pairs<CONST>(row + k, v);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = 0ull;
@@ -147,12 +155,12 @@ __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int
     for (int i = 0; i < 4; ++i) v[c][i] = mul_f2(v[c][i], inv2);
     f2 w[4];
     if (n.weight) {
-      load_piece<float, VEC>(n.weight, c, tid, NT, K, w);
+      load_piece<float, VEC, true>(n.weight, c, tid, NT, K, w);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[c][i] = mul_f2(v[c][i], w[i]);
     }
     if (n.bias) {
-      load_piece<float, VEC>(n.bias, c, tid, NT, K, w);
+      load_piece<float, VEC, true>(n.bias, c, tid, NT, K, w);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[c][i] = add_f2(v[c][i], w[i]);
     }
@@ -174,16 +182,16 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT, NT == 512 && CH == 2 ? 3 
   const T* x = static_cast<const T*>(a.x) + p * a.ldx;
   const R* res = static_cast<const R*>(a.r) + p * a.ldr;
 #pragma unroll
-  for (int c = 0; c < CH; ++c) load_piece<T, VEC>(x, c, tid, NT, a.K, v[c]);
+  for (int c = 0; c < CH; ++c) load_piece<T, VEC, false>(x, c, tid, NT, a.K, v[c]);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     if constexpr (VEC) {
       raw[c].zero();
-      if (a.r && 8 * (tid + c * NT) < a.K) raw[c].load(res + 8 * (tid + c * NT));
+      if (a.r && 8 * (tid + c * NT) < a.K) raw[c].template load_written<sizeof(T) == 4>(res + 8 * (tid + c * NT));
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) rs[c][i] = 0ull;
-      if (a.r) load_piece<R, false>(res, c, tid, NT, a.K, rs[c]);
+      if (a.r) load_piece<R, false, false>(res, c, tid, NT, a.K, rs[c]);
     }
   }
   if (a.has_post) normalise<NT, CH, VEC>(v, a.post, a.K, tid, red, turn);
@@ -193,7 +201,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT, NT == 512 && CH == 2 ? 3 
   for (int c = 0; c < CH; ++c) {
     if (gate) {
       f2 g[4];
-      load_piece<T, VEC>(gate, c, tid, NT, a.K, g);
+      load_piece<T, VEC, true>(gate, c, tid, NT, a.K, g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[c][i] = mul_f2(v[c][i], g[i]);
     }

@@ -148,6 +148,9 @@ struct Raw8 {
     hi = max_nan(b.x, b.y);
   }
   __device__ __forceinline__ void load(const T* p) { v = __ldg(reinterpret_cast<const uint4*>(p)); }
+  // from memory that the kernel may write as well
+  template <bool L1 = false>
+  __device__ __forceinline__ void load_written(const T* p) { v = L1 ? *reinterpret_cast<const uint4*>(p) : __ldcg(reinterpret_cast<const uint4*>(p)); }
   __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
   __device__ __forceinline__ void unpack(float (&x)[8]) const { unpack8(v, x, T()); }
 };
@@ -159,6 +162,12 @@ struct Raw8<float> {
     hi = max_nan(max_nan(max_nan(x[0], x[1]), max_nan(x[2], x[3])), max_nan(max_nan(x[4], x[5]), max_nan(x[6], x[7])));
   }
   __device__ __forceinline__ void load(const float* p) { load8(p, x); }
+  template <bool L1 = false>
+  __device__ __forceinline__ void load_written(const float* p) {
+    const float4* q = reinterpret_cast<const float4*>(p);
+    const float4 a = L1 ? q[0] : __ldcg(q), b = L1 ? q[1] : __ldcg(q + 1);
+    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+  }
   __device__ __forceinline__ void zero() {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = 0.0f;

@@ -188,7 +188,7 @@ fgq_status fgq_rope_table(int rot, double base, fgq_rope_scaling scaling, double
  * Values past rot, and tokens i >= lens[b], are those of x.  y may be x (with its strides), or must not overlap it.
  * Products and sums are fp32, angles within 2^-24 of half a turn, y is rounded once.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, rot not even, below 2 or above head_dim, a bad type, layout or inverse, a
- * magnitude that is not finite, y at x with other strides), FGQ_ERR_ALIGN (x or y not aligned to their elements,
+ * magnitude that is not finite, y at x with other strides, strides with which y's tokens overlap), FGQ_ERR_ALIGN (x or y not aligned to their elements,
  * table not 8-byte, starts or lens not 4-byte aligned), FGQ_ERR_UNSUPPORTED (B T heads above 2^31 - 1, head_dim above 65536),
  * FGQ_ERR_CUDA.
  */
@@ -212,7 +212,8 @@ fgq_status fgq_rope(const void* x, void* y, fgq_float_type type, int B, int T, i
  * Everything between is fp32 and y is formed from s before it is rounded.  Sums of squares are fp32, of values up to 1e18 in rows of any length.
  * A token that holds NaN gives NaN, one that holds Inf what fp32 gives; other tokens are as without it.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, K = 0, bad types or kind, eps not above 0 or not finite, a scale that is not
- * finite, tokens_per_gate < 1 with a gate, a stride below K, y without pre or pre without y, neither s nor y),
+ * finite, tokens_per_gate < 1 with a gate, a stride below K, y without pre or pre without y, neither s nor y, y at x or s at r with
+ * other strides),
  * FGQ_ERR_ALIGN (not aligned to the elements), FGQ_ERR_UNSUPPORTED (P or K above 2^31 - 2^16), FGQ_ERR_CUDA.
  */
 typedef enum { FGQ_NORM_RMS = 0, FGQ_NORM_LAYER = 1 } fgq_norm_kind;

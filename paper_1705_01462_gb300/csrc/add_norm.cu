@@ -335,6 +335,7 @@ extern "C" fgq_status fgq_add_norm(const void* x, fgq_float_type type, int P, in
   if ((pre != nullptr) != (y != nullptr) || (!y && !s) || (gate && tokens_per_gate < 1) || !x) return FGQ_ERR_ARG;
   if (P > 1 && (ldx < K || (r && ldr < K) || (s && lds < K))) return FGQ_ERR_ARG;
   if (gate && P > tokens_per_gate && ldg < K) return FGQ_ERR_ARG;
+  if (P > 1 && ((y == x && ldx != K) || (s && s == r && lds != ldr))) return FGQ_ERR_ARG;  // another row's inputs would be overwritten
   if (P > dec::MAX_SIZE || K > dec::MAX_SIZE) return FGQ_ERR_UNSUPPORTED;
   const uintptr_t e = dec::float_bytes(type), re = dec::float_bytes(rtype);
   if (!dec::aligned(x, e) || !dec::aligned(gate, e) || !dec::aligned(r, re) || !dec::aligned(s, re) || !dec::aligned(y, e))

@@ -165,6 +165,12 @@ fgq_status launch_rope(RopeArgs a, int layout, cudaStream_t s) {
   return after_launch();
 }
 
+// Whether no two of the outputs' tokens, n elements each, share memory: one axis steps past all of the other.
+bool apart(int B, int64_t batch_stride, int T, int64_t token_stride, double n) {
+  const double b = fabs((double)batch_stride), t = fabs((double)token_stride);
+  return (T == 1 || t >= n) && (B == 1 || b >= n) && (T == 1 || B == 1 || b >= (T - 1) * t + n || t >= (B - 1) * b + n);
+}
+
 }  // namespace
 }  // namespace fgq
 
@@ -211,6 +217,7 @@ fgq_status fgq_rope(const void* x, void* y, fgq_float_type type, int B, int T, i
     return FGQ_ERR_ALIGN;
   if (head_dim > 65536 || heads > INT32_MAX / head_dim || (int64_t)B * T > INT32_MAX || (int64_t)B * T * heads > INT32_MAX)
     return FGQ_ERR_UNSUPPORTED;
+  if (!apart(B, y_batch_stride, T, y_token_stride, (double)heads * head_dim)) return FGQ_ERR_ARG;
   // an axis of one element may have any stride
   RopeArgs a = {};
   a.x = x, a.y = y;

@@ -736,6 +736,13 @@ NORM_KINDS = {"rms": 0, "layer": 1}
 SCORES = {"softmax": 0, "sigmoid": 1}
 
 
+def _fits(*sizes: int) -> None:
+    """What the library takes as sizes has 32 bits, and ctypes would cut off the rest."""
+    for n in sizes:
+        if n > 0x7fffffff:
+            raise FGQError(FGQ_ERR_UNSUPPORTED, f"a size of {n}")
+
+
 def _named(table, name: str, what: str) -> int:
     value = table.get(name)
     if value is None:
@@ -747,6 +754,7 @@ def rope_table(rot: int, base: float = 10000.0, scaling: str = "none", factor: f
                low: float = 1.0, high: float = 32.0, device="cuda") -> torch.Tensor:
     """The angles of fgq_rope: turns a position of each of rot / 2 pairs, in units of 2^-64 (int64), scaled for long contexts
     as include/fgq_decoder.h says ("linear", "base", "ramp": the last between low and high turns over `length` positions)."""
+    _fits(rot)
     table = torch.empty(max(rot, 0) // 2, dtype=torch.int64)
     _check(lib().fgq_rope_table(rot, base, _named(ROPE_SCALINGS, scaling, "scaling"), factor, length, low, high,
                                 table.data_ptr()), "fgq_rope_table")
@@ -762,6 +770,7 @@ def fgq_rope(x: torch.Tensor, table: torch.Tensor, starts: torch.Tensor, lens: O
     if not isinstance(x, torch.Tensor) or x.dim() != 4:
         raise ValueError("x must be [B][T][heads][D]")
     B, T, heads, D = x.shape
+    _fits(B, T, heads, D, 2 * table.numel())
     ty, xb, xt = _heads(x, heads, D, "x")
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
@@ -833,6 +842,8 @@ def _matrix(x: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
     ld, one = x.stride()
     if one != 1 and K > 1:
         raise ValueError(f"{name} must be [tokens][features] with contiguous rows")
+    if P > 0x7fffffff or K > 0x7fffffff:
+        _fits(P, K)
     return ty, P, K, ld if P > 1 else K
 
 
@@ -908,6 +919,7 @@ class W4Weights:
         if c[-3:] != tiles or len(c) > 4 or s[:-2] != c[:-1] or s[-2] != 16 or s[-1] not in (1, 2, 4):
             raise ValueError(f"W4Weights: codes are [experts][{tiles[0]}][{tiles[1]}][1024], scales "
                              f"[experts][{tiles[0]}][{tiles[1]}][16][128 / group]; got {c} and {s}")
+        _fits(rows, cols, *c)
         self._codes, self._scales, self._rows, self._cols = codes, scales, rows, cols
         self._experts, self._group = c[0] if len(c) == 4 else 1, 128 // s[-1]
         self._sizes = codes.numel(), scales.numel()
@@ -933,6 +945,7 @@ def fgq_quantize_weights_w4(w: torch.Tensor, group: int = 64, stream=None) -> W4
         raise ValueError("w must be [rows][cols] or [experts][rows][cols]")
     if group not in (32, 64, 128):
         raise ValueError("group must be 32, 64 or 128")
+    _fits(*w.shape)
     pw = _dev(w, torch.float32, "w")
     rows, cols = w.shape[-2:]
     tiles = tuple(w.shape[:-2]) + ((rows + 15) // 16, (cols + 127) // 128)
@@ -990,6 +1003,7 @@ def fgq_route_tokens(x: torch.Tensor, router: torch.Tensor, top: int, score: str
     _require_cuda()
     ty, P, K, ldx = _matrix(x, "x")
     rty, E, pr = _router(router, x, K)
+    _fits(top)
     ids = torch.empty((P, max(top, 0)), dtype=torch.int32, device=x.device)
     weights = torch.empty((P, max(top, 0)), dtype=torch.float32, device=x.device)
     _check(lib().fgq_route_tokens(x.data_ptr(), ty, P, K, ldx, pr, rty, E, top, _named(SCORES, score, "score"),
@@ -1018,6 +1032,7 @@ def fgq_moe_w4(x: torch.Tensor, router: torch.Tensor, top: int, gate: W4Weights,
     _require_cuda()
     ty, P, K, ldx = _matrix(x, "x")
     rty, E, pr = _router(router, x, K)
+    _fits(top)
     if K != gate._cols or E != gate._experts:
         raise ValueError(f"x must be [tokens][{gate.cols}], router [{gate.experts}][{gate.cols}]")
     y, py = _outputs(x, y, P, K)

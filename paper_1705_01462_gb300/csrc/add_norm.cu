@@ -38,8 +38,8 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// Sum over the NT threads of a row, in all of them.  (What they bring is their share of a mean, so that squares of values up to 1e18 stay in
-// fp32's range in rows of any length.)  `red` is the block's; two sums in turn take its two halves, so that
+// Sum over the NT threads of a row, in all of them.  (What they bring has been divided by about the row's length, so that squares of values up
+// to 1e18 stay in fp32's range in rows of any length.)  `red` is the block's; two sums in turn take its two halves, so that
 // one barrier a sum is enough.
 template <int NT>
 __device__ __forceinline__ float row_sum(float v, float (*red)[32], int& turn) {
@@ -118,10 +118,19 @@ __device__ __forceinline__ void store_piece(T* row, int c, int tid, int NT, int 
   }
 }
 
+// 1 / K as a power of two, which costs no bits, and the rest.
+struct Length {
+  float part, rest;
+};
+__device__ __forceinline__ Length length_of(int K) {
+  const float part = pow2f(127 - (int)(__float_as_uint((float)K) >> 23));
+  return {part, 1.0f / ((float)K * part)};
+}
+
 // v to its norm, in registers.  Elements past the row are 0 before and after.
 template <int NT, int CH, bool VEC>
 __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int K, int tid, float (*red)[32], int& turn) {
-  const float inv_k = 1.0f / (float)K;
+  const Length len = length_of(K);
   float a, b;
   if (n.kind == FGQ_NORM_LAYER) {
     f2 sum = 0ull;
@@ -130,7 +139,7 @@ __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum = add_f2(sum, v[c][i]);
     unpack_f2(sum, a, b);
-    const float mean = row_sum<NT>((a + b) * inv_k, red, turn);
+    const float mean = row_sum<NT>((a + b) * len.part, red, turn) * len.rest;
     const f2 off = pack_f2(-mean, -mean);
 #pragma unroll
     for (int c = 0; c < CH; ++c)
@@ -147,7 +156,7 @@ __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) sq = fma_f2(v[c][i], v[c][i], sq);
   unpack_f2(sq, a, b);
-  const float inv = rsqrtf(row_sum<NT>((a + b) * inv_k, red, turn) + n.eps);
+  const float inv = rsqrtf(row_sum<NT>((a + b) * len.part, red, turn) * len.rest + n.eps);
   const f2 inv2 = pack_f2(inv, inv);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -235,7 +244,7 @@ __global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constan
   const T* x = static_cast<const T*>(a.x) + p * a.ldx;
   const R* r = a.r ? static_cast<const R*>(a.r) + p * a.ldr : nullptr;
   const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)(p / a.tokens_per_gate) * a.ldg : nullptr;
-  const float inv_k = 1.0f / (float)a.K;
+  const Length len = length_of(a.K);
   // means of f(k) over the row, in pieces that keep fp32's bits
   auto mean_of = [&](auto f) {
     float total = 0.0f;
@@ -245,9 +254,9 @@ __global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constan
         const int64_t at = (int64_t)k + (int64_t)i * LONG_THREADS;
         if (at < a.K) part += f((int)at);
       }
-      total += part * inv_k;
+      total += part * len.part;
     }
-    return row_sum<LONG_THREADS>(total, red, turn);
+    return row_sum<LONG_THREADS>(total, red, turn) * len.rest;
   };
   auto stats = [&](auto value, const fgq_norm& n, float& mean, float& inv) {
     mean = 0.0f;

@@ -29,6 +29,7 @@ struct NormArgs {
   int64_t ldx, ldg, ldr, lds;
   fgq_norm post, pre;
   float scale;
+  float part, rest;  // 1 / K: a power of two, which costs no bits, times the rest
   int P, K, tokens_per_gate, has_post, has_pre;
 };
 
@@ -118,19 +119,10 @@ __device__ __forceinline__ void store_piece(T* row, int c, int tid, int NT, int 
   }
 }
 
-// 1 / K as a power of two, which costs no bits, and the rest.
-struct Length {
-  float part, rest;
-};
-__device__ __forceinline__ Length length_of(int K) {
-  const float part = pow2f(127 - (int)(__float_as_uint((float)K) >> 23));
-  return {part, 1.0f / ((float)K * part)};
-}
-
 // v to its norm, in registers.  Elements past the row are 0 before and after.
 template <int NT, int CH, bool VEC>
-__device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int K, int tid, float (*red)[32], int& turn) {
-  const Length len = length_of(K);
+__device__ __forceinline__ void normalise(f2 (&v)[CH][4], const NormArgs& args, const fgq_norm& n, int tid, float (*red)[32], int& turn) {
+  const int K = args.K;
   float a, b;
   if (n.kind == FGQ_NORM_LAYER) {
     f2 sum = 0ull;
@@ -139,7 +131,7 @@ __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum = add_f2(sum, v[c][i]);
     unpack_f2(sum, a, b);
-    const float mean = row_sum<NT>((a + b) * len.part, red, turn) * len.rest;
+    const float mean = row_sum<NT>((a + b) * args.part, red, turn) * args.rest;
     const f2 off = pack_f2(-mean, -mean);
 #pragma unroll
     for (int c = 0; c < CH; ++c)
@@ -156,7 +148,7 @@ __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const fgq_norm& n, int
 #pragma unroll
     for (int i = 0; i < 4; ++i) sq = fma_f2(v[c][i], v[c][i], sq);
   unpack_f2(sq, a, b);
-  const float inv = rsqrtf(row_sum<NT>((a + b) * len.part, red, turn) * len.rest + n.eps);
+  const float inv = rsqrtf(row_sum<NT>((a + b) * args.part, red, turn) * args.rest + n.eps);
   const f2 inv2 = pack_f2(inv, inv);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -203,7 +195,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT, NT == 512 && CH == 2 ? 3 
       if (a.r) load_piece<R, false, false>(res, c, tid, NT, a.K, rs[c]);
     }
   }
-  if (a.has_post) normalise<NT, CH, VEC>(v, a.post, a.K, tid, red, turn);
+  if (a.has_post) normalise<NT, CH, VEC>(v, a, a.post, tid, red, turn);
   const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)(p / a.tokens_per_gate) * a.ldg : nullptr;
   const f2 scale = pack_f2(a.scale, a.scale);
 #pragma unroll
@@ -226,7 +218,7 @@ __global__ void __launch_bounds__(NT < 128 ? 128 : NT, NT == 512 && CH == 2 ? 3 
     if (a.s) store_piece<R, VEC>(static_cast<R*>(a.s) + p * a.lds, c, tid, NT, a.K, v[c]);
   }
   if (a.has_pre) {
-    normalise<NT, CH, VEC>(v, a.pre, a.K, tid, red, turn);
+    normalise<NT, CH, VEC>(v, a, a.pre, tid, red, turn);
     T* y = static_cast<T*>(a.y) + (int64_t)p * a.K;
 #pragma unroll
     for (int c = 0; c < CH; ++c) store_piece<T, VEC>(y, c, tid, NT, a.K, v[c]);
@@ -244,7 +236,6 @@ __global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constan
   const T* x = static_cast<const T*>(a.x) + p * a.ldx;
   const R* r = a.r ? static_cast<const R*>(a.r) + p * a.ldr : nullptr;
   const T* gate = a.gate ? static_cast<const T*>(a.gate) + (int64_t)(p / a.tokens_per_gate) * a.ldg : nullptr;
-  const Length len = length_of(a.K);
   // means of f(k) over the row, in pieces that keep fp32's bits
   auto mean_of = [&](auto f) {
     float total = 0.0f;
@@ -254,9 +245,9 @@ __global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constan
         const int64_t at = (int64_t)k + (int64_t)i * LONG_THREADS;
         if (at < a.K) part += f((int)at);
       }
-      total += part * len.part;
+      total += part * a.part;
     }
-    return row_sum<LONG_THREADS>(total, red, turn) * len.rest;
+    return row_sum<LONG_THREADS>(total, red, turn) * a.rest;
   };
   auto stats = [&](auto value, const fgq_norm& n, float& mean, float& inv) {
     mean = 0.0f;
@@ -357,6 +348,9 @@ extern "C" fgq_status fgq_add_norm(const void* x, fgq_float_type type, int P, in
   a.ldx = P > 1 ? ldx : 0, a.ldr = P > 1 ? ldr : 0, a.lds = P > 1 ? lds : 0, a.ldg = gate && P > tokens_per_gate ? ldg : 0;
   if (post) a.post = *post, a.has_post = 1;
   if (pre) a.pre = *pre, a.has_pre = 1;
+  int log2k = 0;
+  frexp((double)K, &log2k);
+  a.part = (float)ldexp(1.0, -log2k), a.rest = (float)(1.0 / ldexp((double)K, -log2k));
   a.scale = scale, a.P = P, a.K = K, a.tokens_per_gate = gate ? tokens_per_gate : 1;
   if (type == FGQ_F32) return launch_add_norm<float, float>(a, type, rtype, stream);
   if (type == FGQ_BF16)

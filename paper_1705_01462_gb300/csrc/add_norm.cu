@@ -169,8 +169,10 @@ __device__ __forceinline__ void normalise(f2 (&v)[CH][4], const NormArgs& args, 
 }
 
 // NT threads a row; blocks of at least 128 threads.
+// 512 threads with two pieces: three blocks an SM (8192 x 8192 bf16 86 us, 95 with two), of rows that are not 16-byte pieces two (8192 x 8001 155 us, 199
+// with three, whose registers spill).
 template <typename T, typename R, int NT, int CH, bool VEC>
-__global__ void __launch_bounds__(NT < 128 ? 128 : NT, NT == 512 && CH == 2 ? 3 : 1)  // three blocks an SM: 8192 x 8192 84 us, 95 with two
+__global__ void __launch_bounds__(NT < 128 ? 128 : NT, NT == 512 && CH == 2 ? (VEC ? 3 : 2) : 1)
     add_norm_kernel(const __grid_constant__ NormArgs a) {
   constexpr int RPB = NT < 128 ? 128 / NT : 1;
   __shared__ float red[2][32];

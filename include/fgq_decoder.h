@@ -270,7 +270,8 @@ fgq_status fgq_read_weights_w4(const fgq_w4* w, float* out, cudaStream_t stream)
  * Few tokens: codes and 16-bit tokens are exact operands of the products (fp32 tokens: three bf16 parts, exactly), a group's sum
  * takes its scale in fp32, y is rounded once.  More than 16 tokens (fp32: 8) whose product with the
  * number of weights is above about 2^30 (2^27) run on fp16 operands on tcgen05: weights are exact there too within 2^26 of their row's largest scale, bf16 tokens within 2^26 of their largest
- * value (smaller ones are off by at most 2^-39 of it), fp32 tokens within 2^-22 of each value (or 2^-39 of the largest).  Scales
+ * value (smaller ones are off by at most 2^-39 of it), fp32 tokens within 2^-22 of each value (or 2^-39 of the largest).  Sums
+ * of 16 products are cut off at 2^-23 of the sum so far, fp32 tokens' over runs of 256 columns that are added in fp32.  Scales
  * 2^-100 to 2^100 there, and outputs below 2^-100 may be 0.  A token that holds NaN or Inf gives values that are not finite; other
  * tokens are as without it.
  * Errors: FGQ_ERR_ARG (null pointer, negative size, bad type, bad weights, more than one matrix, ldx < K), FGQ_ERR_ALIGN (x or y

@@ -8,9 +8,9 @@
 // CH pieces of 8 elements, two in a packed register pair; a layer norm takes its mean first and then the squares of what is
 // left, so that a large mean costs no bits.  Sums of a row meet in the same order always: in registers, by shuffles, over the
 // warps through shared memory.  Rows past 16384 elements are read again for each sum instead (long_kernel).
-// 8192 x 4096, device time (floor): fp32 79.5 us (79), bf16 layer norms 43 (39.5), bf16 with both norms and a gate 49.5 (39.5;
-// 57 with unpacked arithmetic).  What did not help there: a persistent block with the next row's loads under way to registers (56) or
-// to a ring in shared memory, which takes the place of the weights in L1 (80); 128 threads a row (57).
+// 8192 x 4096, device time (floor): fp32 78.7 us (79), bf16 layer norms 42.3 (39.5), bf16 with both norms and a gate for each 2048
+// 48.5 (39.5; 57 with unpacked arithmetic, then 49.5).  What did not help there, beside 49.5: a persistent block with the next row's loads under way to
+// registers (56) or to a ring in shared memory, which takes the place of the weights in L1 (80); 128 threads a row (57).
 #include <cmath>
 
 #include "decoder_internal.cuh"
@@ -285,8 +285,8 @@ __global__ void __launch_bounds__(LONG_THREADS) long_kernel(const __grid_constan
 template <typename T, typename R, bool VEC>
 fgq_status launch_add_norm(const NormArgs& a, cudaStream_t s) {
   const unsigned P = (unsigned)a.P;
-  // few rows: one piece a thread, for shorter chains of a single row; many: two, for fewer barriers a byte.  4096 bf16 values, us so and
-  // so: 1 row 2.98 and 3.08, 304 rows 3.61 and 3.54, 2432 rows 18.2 and 17.2
+  // few rows: one piece a thread, for shorter chains of a single row; many: two, for fewer barriers a byte.  4096 bf16 values, both norms, us so
+  // and so: 1 row 2.83 and 2.99, 304 rows 3.61 and 3.74, 2432 rows 16.8 and 14.9; of 2048 values 2.36 and 2.64, 2.93 and 3.22, 8.1 and 7.2
   const bool few = a.P <= 2 * device_sms();
   if (a.K <= 512)
     add_norm_kernel<T, R, 32, 2, VEC><<<(P + 3) / 4, 128, 0, s>>>(a);

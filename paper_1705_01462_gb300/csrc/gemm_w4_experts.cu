@@ -1,6 +1,7 @@
 // The experts' layers of many tokens with 4-bit weights: tokens as rows in the order of their experts, the products of gemm_w4.cuh for
 // a unit of up to 32, 64, 128 or 256 of them and 128 rows of gate, up or down, and the hidden values between them.  Bound as those products are, by
-// codes to operands, once for each unit of an expert: 128 tokens of 2 of 8 experts, 4096 -> 14336, 373 us for 110 of bytes.
+// codes to operands, once for each unit of an expert: 128 tokens of 2 of 8 experts, 4096 -> 14336, 436 us for 110 of bytes
+// (hidden values take two rows of fp16, and down's sums leave the tensor memory every 256 columns).
 #include "gemm_w4.cuh"
 
 namespace fgq {

@@ -13,7 +13,7 @@
 //   or, with more choices an expert, the kernels of gemm_w4_experts.cu for units of 32 to 256;
 //   combine_kernel  each token's choices by their weights, in their order.
 // Bound by the bytes of the experts' weights, each read once (again from L2 for each further unit of an expert), and before them by the way
-// from logits to units: of 148 us for 64 tokens of 6 of 64 experts, 4096 -> 1536, routing takes 11 and the grouping 7 more, combining 4; of 22 us for one
+// from logits to units: of 165 us for 64 tokens of 6 of 64 experts, 4096 -> 1536, routing takes 11 and the grouping 7 more, combining 4; of 22 us for one
 // token of 8 of 64 experts, 2048 -> 1024, routing takes 5 (3 with one expert to choose), each layer about 7, combining 2.
 #include <type_traits>
 
@@ -293,7 +293,7 @@ __global__ void __cluster_dims__(RT_CLUSTER, 1, 1) __launch_bounds__(32 * RT_WAR
 
 // ------------------------------------------------------------------ tokens as operand rows
 // A block a token: fp32 in three bf16 parts, 16-bit types copied to aligned rows; zeros up to a multiple of 8.  (Brought into form by the
-// products themselves, 64 tokens of 6 of 64 experts 4096 -> 1536 took 164 us, for all types, in place of 148: registers spilled.)
+// products themselves, 64 tokens of 6 of 64 experts 4096 -> 1536 took 16 us more, for all types: registers spilled.)
 template <typename T>
 __global__ void __launch_bounds__(256) operand_rows_kernel(const T* __restrict__ x, int K, int64_t ldx, uint16_t* dst, int64_t pitch) {
   pdl_trigger();

@@ -9,7 +9,8 @@
 namespace fgq {
 namespace w4 {
 
-// Eight codes of a word as four pairs of fp16 whole numbers: in the low bits of 1024's fp16 a nibble n is 1024 + n, four bits up 1024 + 16 n.
+// Eight codes of a word as four pairs of fp16 whole numbers, a known way with 4-bit weights: in the low bits of 1024's fp16 a nibble n is 1024 + n,
+// four bits up 1024 + 16 n.
 __device__ __forceinline__ uint32_t h2_sub(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));

@@ -8,8 +8,9 @@
 // in their order.
 // Bound by the weights' bytes and, a little later, by instructions (a tile is 4 words of 8 codes a lane and row: an AND and a packed multiply-add
 // a pair, a matrix instruction 16 columns).  Logits of 8 tokens, 4096 -> 131072, groups of 128: 49 us, 84% of the copy rate, issue slots 74%
-// busy (67 with the ring of w4_rows.cuh).  64 tokens of 6 of 64 experts, 4096 -> 1536, groups of 64: hidden values 82 us (5.3 TB/s, 70%), down 48
-// (4.6 TB/s, 71%).  Up to 24 warps of 80 registers: that many loads in flight, at 28 to 118 bytes of spills in the gated form.
+// busy (67 with the ring of w4_rows.cuh).  64 tokens of 6 of 64 experts, 4096 -> 1536, groups of 64: hidden values 83 us (5.3 TB/s, 67% of the DRAM
+// peak, issue slots 70% busy), down, whose tokens have two columns each, 65 (3.5 TB/s, 44%; 62%; with one 48).  Up to 24 warps of 80
+// registers: that many loads in flight, at 28 to 118 bytes of spills in the gated form.
 #pragma once
 
 #include "w4_rows.cuh"
